@@ -15,7 +15,7 @@ def __getattr__(name):
     if name in ("Geometry", "Projector"):
         from . import projector
         return getattr(projector, name)
-    if name == "recon":
+    if name in ("recon", "activations"):
         import importlib
-        return importlib.import_module(".recon", __name__)
+        return importlib.import_module("." + name, __name__)
     raise AttributeError(name)

@@ -1,0 +1,399 @@
+"""Operators for networks trained through the projector, with what the backward pass needs kept in 8 bits.
+
+"PyTorch Interfaces and CT Parameters" puts the projector into a network's training loop, and every unrolled iteration keeps
+volume-sized activations until its backward pass.  Here they are kept, and worked on, as 8-bit floats whose groups of 32
+neighbours share a power of two: 1 + 1/32 bytes a value (include/leap_activations.h defines the format and the operators).
+
+    packed = pack8(x); x_again = packed.unpack(torch.float32)          # any tensor, to 8 bits and back
+    with keep_in_8_bits(): loss = network(volume)                      # what autograd saves inside is kept packed
+    y, x = feed_forward8(y, norm_weight, up, down, residual=x)         # a block that keeps 8 bits only; differentiable
+    block = FeedForward8(512, 1024); y, x = block(y, x)                # the same as a module
+
+and its parts, forward and backward, for blocks of another make: rms_norm8, linear8, gated_linear8 and their *_backward.
+A row is whatever the last dimension holds: a voxel's channels, a patch of a volume.
+
+All run in libleap_hip.so on the current HIP stream; PyTorch supplies memory.  Tensors are on one GPU; the values of a row
+are neighbours and the rows evenly spaced (else ValueError: `.contiguous()` them).  A rounding to 8 bits has the gradient 1.
+As with any operator, do not capture a backward pass into a graph while an eager graph of the same leaves is alive.
+"""
+from __future__ import annotations
+
+import torch
+
+from . import binding as B
+from .projector import _current_stream
+
+GROUP = 32
+_TYPES = {torch.float32: B.LEAP_F32, torch.bfloat16: B.LEAP_BF16, torch.float16: B.LEAP_F16}
+_CODES = torch.float8_e4m3fn
+
+
+class Packed8:
+    """A tensor held in 8 bits: codes (float8_e4m3fn, its shape) and scales (uint8, one for each 32 values of a row: the
+    power of two + 127)."""
+
+    __slots__ = ("codes", "scales")
+
+    def __init__(self, codes: torch.Tensor, scales: torch.Tensor):
+        if codes.dtype is not _CODES or scales.dtype is not torch.uint8:
+            raise ValueError("codes are float8_e4m3fn, scales uint8")
+        if codes.dim() < 1 or scales.shape != codes.shape[:-1] + (-(-codes.shape[-1] // GROUP),):
+            raise ValueError(f"scales of shape {tuple(scales.shape)} do not fit codes of shape {tuple(codes.shape)}")
+        if not codes.is_contiguous() or not scales.is_contiguous() or codes.device != scales.device:
+            raise ValueError("codes and scales must be contiguous, on one device")
+        self.codes, self.scales = codes, scales
+
+    @property
+    def shape(self):
+        return self.codes.shape
+
+    @property
+    def device(self):
+        return self.codes.device
+
+    def unpack(self, dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
+        return unpack8(self, dtype)
+
+    def __repr__(self):
+        return f"Packed8(shape={tuple(self.shape)}, device={self.device})"
+
+
+def _type_of(t: torch.Tensor, what: str) -> int:
+    kind = _TYPES.get(t.dtype)
+    if kind is None:
+        raise ValueError(f"{what} must be float32, bfloat16 or float16, not {t.dtype}")
+    return kind
+
+
+def _on_gpu(t: torch.Tensor, what: str, device=None) -> None:
+    if t.device.type != "cuda":
+        raise ValueError(f"{what} must be on a GPU")
+    if device is not None and t.device != device:
+        raise ValueError(f"{what} must be on {device}")
+
+
+def _rows(t: torch.Tensor, what: str):
+    """(rows, columns, distance between rows) of a tensor whose last dimension is a row."""
+    dims = t.shape
+    if len(dims) == 0 or dims[-1] < 1:
+        raise ValueError(f"{what} must have rows of at least one value")
+    cols = dims[-1]
+    if t.is_contiguous():
+        return t.numel() // cols, cols, cols
+    strides = t.stride()
+    if strides[-1] == 1 or cols == 1:
+        rows, step = 1, None
+        for n, s in zip(reversed(dims[:-1]), reversed(strides[:-1])):
+            if n == 0:
+                return 0, cols, cols
+            if n == 1:
+                continue
+            if step is None:
+                step = s
+            elif s != step * rows:
+                break
+            rows *= n
+        else:
+            if step is None or step >= cols:
+                return rows, cols, cols if step is None else step
+    raise ValueError(f"{what}: the values of a row must be neighbours and the rows evenly spaced; call .contiguous()")
+
+
+def _weight(w: torch.Tensor, cols: int, device, what: str = "weight"):
+    """(rows, distance between them) of a bfloat16 weight [rows, cols]."""
+    _on_gpu(w, what, device)
+    if w.dtype is not torch.bfloat16 or w.dim() != 2 or w.shape[1] != cols or w.shape[0] < 1:
+        raise ValueError(f"{what} must be bfloat16 [outputs, {cols}], got {w.dtype} {tuple(w.shape)}")
+    rows, _, stride = _rows(w, what)
+    return rows, stride
+
+
+def _gradient(g: torch.Tensor, shape, device, types, what: str):
+    _on_gpu(g, what, device)
+    if g.shape != shape or g.dtype not in types:
+        raise ValueError(f"{what} must be {' or '.join(str(t) for t in types)} {tuple(shape)}, got {g.dtype} {tuple(g.shape)}")
+    return _rows(g, what)
+
+
+def _call(name: str, device, *arguments) -> None:
+    """The library's function on `device`, on its current stream."""
+    lib = B._activations or B.load_activations()
+    index = device.index
+    if torch.cuda.current_device() == index:
+        status = getattr(lib, name)(*arguments, _current_stream(index))
+    else:
+        with torch.cuda.device(index):
+            status = getattr(lib, name)(*arguments, _current_stream(index))
+    if status != B.LEAP_OK:
+        B._check(lib, status)
+
+
+def _empty_packed(shape, device) -> Packed8:
+    p = Packed8.__new__(Packed8)
+    p.codes = torch.empty(shape, dtype=_CODES, device=device)
+    p.scales = torch.empty(tuple(shape[:-1]) + (-(-shape[-1] // GROUP),), dtype=torch.uint8, device=device)
+    return p
+
+
+def _work(name: str, device, *sizes):
+    """Workspace of so many bytes as the library asks for, or None."""
+    lib = B._activations or B.load_activations()
+    n = getattr(lib, name)(*sizes)
+    return torch.empty(n, dtype=torch.uint8, device=device) if n else None
+
+
+def _address(t):
+    return None if t is None else t.data_ptr()
+
+
+# ---- packing ------------------------------------------------------------------------------------------------------------
+
+
+def pack8(x: torch.Tensor) -> Packed8:
+    """x (float32, bfloat16, float16; [..., columns]) in 8 bits."""
+    _on_gpu(x, "x")
+    kind = _type_of(x, "x")
+    rows, cols, stride = _rows(x, "x")
+    p = _empty_packed(x.shape, x.device)
+    _call("leap_pack8", x.device, x.data_ptr(), kind, stride, rows, cols, p.codes.data_ptr(), p.scales.data_ptr())
+    return p
+
+
+def unpack8(packed: Packed8, dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
+    """The values held; bfloat16 and float32 hold them exactly (but for 2^128, to which float32's largest numbers round and which is
+    infinity there), float16 those between 2^-14 and 65504."""
+    kind = _TYPES.get(dtype)
+    if kind is None:
+        raise ValueError(f"dtype must be float32, bfloat16 or float16, not {dtype}")
+    codes = packed.codes
+    _on_gpu(codes, "packed")
+    rows, cols, _ = _rows(codes, "packed")
+    out = torch.empty(codes.shape, dtype=dtype, device=codes.device)
+    _call("leap_unpack8", codes.device, codes.data_ptr(), packed.scales.data_ptr(), rows, cols, out.data_ptr(), kind)
+    return out
+
+
+class keep_in_8_bits(torch.autograd.graph.saved_tensors_hooks):
+    """Inside this context what autograd saves for the backward pass is kept packed: tensors on a GPU of float32, bfloat16 or
+    float16 with at least `min_values` values and evenly spaced rows.  Leaves that want a gradient (weights) and everything
+    else are kept as they are.  The gradients are those of the values held (3 mantissa bits)."""
+
+    def __init__(self, min_values: int = 1 << 16):
+        def pack(t):
+            if t.device.type != "cuda" or t.dtype not in _TYPES or t.numel() < min_values or (t.is_leaf and t.requires_grad):
+                return t
+            try:
+                _rows(t, "tensor")
+            except ValueError:
+                return t
+            return pack8(t.detach()), t.dtype
+
+        def unpack(kept):
+            return kept if isinstance(kept, torch.Tensor) else kept[0].unpack(kept[1])
+
+        super().__init__(pack, unpack)
+
+
+# ---- the norm -----------------------------------------------------------------------------------------------------------
+
+
+def rms_norm8(x: torch.Tensor, weight: torch.Tensor, residual: torch.Tensor = None, eps: float = 1e-6, keep: bool = True):
+    """(sum, normed, kept, rstd): sum = x + residual (x itself without one), normed = packed sum * rstd * weight with rstd =
+    1 / sqrt(mean(sum^2) + eps) over the row; kept = packed sum and rstd (float32) are for rms_norm8_backward (None with
+    keep=False).  residual: x's type and shape; weight: [columns], x's type or float32."""
+    _on_gpu(x, "x")
+    device, kind = x.device, _type_of(x, "x")
+    rows, cols, stride = _rows(x, "x")
+    if residual is not None:
+        _, _, residual_stride = _gradient(residual, x.shape, device, (x.dtype,), "residual")
+    _norm_weight(weight, x, cols)
+    normed = _empty_packed(x.shape, device)
+    total = x if residual is None else torch.empty(x.shape, dtype=x.dtype, device=device)
+    kept, rstd = (_empty_packed(x.shape, device), torch.empty(x.shape[:-1], dtype=torch.float32, device=device)) if keep else (None, None)
+    _call("leap_rms_norm8", device, x.data_ptr(), stride, _address(residual), residual_stride if residual is not None else 0, kind,
+          weight.data_ptr(), _TYPES[weight.dtype], rows, cols, eps, None if residual is None else total.data_ptr(), normed.codes.data_ptr(),
+          normed.scales.data_ptr(), kept.codes.data_ptr() if keep else None, kept.scales.data_ptr() if keep else None, _address(rstd))
+    return total, normed, kept, rstd
+
+
+def _norm_weight(weight: torch.Tensor, x, cols: int) -> None:
+    _on_gpu(weight, "weight", x.device)
+    if weight.shape != (cols,) or not weight.is_contiguous() or (weight.dtype is not torch.float32 and weight.dtype is not x.dtype):
+        raise ValueError(f"weight must be contiguous [{cols}], float32 or {x.dtype}")
+
+
+def rms_norm8_backward(grad: torch.Tensor, kept: Packed8, rstd: torch.Tensor, weight: torch.Tensor, grad_sum: torch.Tensor = None,
+                       dtype: torch.dtype = None):
+    """(grad_x, grad_weight) from the gradient of `normed` and, where there is one, of `sum`.  grad_x is the residual's gradient
+    too, of type `dtype` (grad's if not given); grad: that type or float32."""
+    dtype = grad.dtype if dtype is None else dtype
+    if dtype not in _TYPES:
+        raise ValueError(f"gradients are float32, bfloat16 or float16, not {dtype}")
+    device = kept.device
+    _on_gpu(kept.codes, "kept")
+    rows, cols, stride = _gradient(grad, kept.shape, device, (dtype, torch.float32), "grad")
+    sum_stride = 0 if grad_sum is None else _gradient(grad_sum, kept.shape, device, (dtype,), "grad_sum")[2]
+    grad_x = torch.empty(kept.shape, dtype=dtype, device=device)
+    _norm_weight(weight, grad_x, cols)
+    _on_gpu(rstd, "rstd", device)
+    if rstd.shape != kept.shape[:-1] or rstd.dtype is not torch.float32 or not rstd.is_contiguous():
+        raise ValueError(f"rstd must be contiguous float32 {tuple(kept.shape[:-1])}")
+    grad_weight = torch.empty(cols, dtype=weight.dtype, device=device)
+    lib = B._activations or B.load_activations()
+    work = torch.empty(lib.leap_rms_norm8_work(rows, cols), dtype=torch.float32, device=device)
+    _call("leap_rms_norm8_backward", device, grad.data_ptr(), _TYPES[grad.dtype], stride, _address(grad_sum), sum_stride, _TYPES[dtype],
+          kept.codes.data_ptr(), kept.scales.data_ptr(), rstd.data_ptr(), weight.data_ptr(), _TYPES[weight.dtype], rows, cols,
+          grad_x.data_ptr(), grad_weight.data_ptr(), work.data_ptr())
+    return grad_x, grad_weight
+
+
+# ---- products -----------------------------------------------------------------------------------------------------------
+
+
+def _packed_rows(x: Packed8, what: str = "x"):
+    _on_gpu(x.codes, what)
+    return _rows(x.codes, what)[:2]
+
+
+def linear8(x: Packed8, weight: torch.Tensor) -> torch.Tensor:
+    """x W^T, bfloat16 [..., outputs], from packed rows and a bfloat16 weight [outputs, columns]."""
+    rows, cols = _packed_rows(x)
+    out, w_stride = _weight(weight, cols, x.device)
+    y = torch.empty(x.shape[:-1] + (out,), dtype=torch.bfloat16, device=x.device)
+    _call("leap_linear8", x.device, x.codes.data_ptr(), x.scales.data_ptr(), rows, cols, weight.data_ptr(), w_stride, out, y.data_ptr())
+    return y
+
+
+def linear8_backward(grad: torch.Tensor, x: Packed8, weight: torch.Tensor, need_x: bool = True, need_weight: bool = True,
+                     dtype: torch.dtype = torch.bfloat16):
+    """(grad_x, grad_weight): dy W (bfloat16, or float32 by `dtype`) and dy^T x (bfloat16); None for one that is not needed."""
+    rows, cols = _packed_rows(x)
+    out, w_stride = _weight(weight, cols, x.device)
+    _, _, stride = _gradient(grad, x.shape[:-1] + (out,), x.device, (torch.bfloat16,), "grad")
+    if dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError("grad_x is bfloat16 or float32")
+    grad_x = torch.empty(x.shape, dtype=dtype, device=x.device) if need_x else None
+    grad_weight = torch.empty((out, cols), dtype=torch.bfloat16, device=x.device) if need_weight else None
+    work = _work("leap_linear8_work", x.device, rows, cols, out)
+    _call("leap_linear8_backward", x.device, grad.data_ptr(), stride, x.codes.data_ptr(), x.scales.data_ptr(), rows, cols, weight.data_ptr(),
+          w_stride, out, _address(grad_x), _TYPES[dtype], _address(grad_weight), _address(work))
+    return grad_x, grad_weight
+
+
+def _halves(weight: torch.Tensor, cols: int, device, what: str = "weight"):
+    out, w_stride = _weight(weight, cols, device, what)
+    if out % 2:
+        raise ValueError(f"{what} must have twice as many rows as there are gated outputs, the gate's first; got {out}")
+    return out // 2, w_stride
+
+
+def gated_linear8(x: Packed8, weight: torch.Tensor, keep: bool = True):
+    """(gated, kept): with u = x W^T = (g, p), W bfloat16 [2 * outputs, columns], gated = packed g * sigmoid(g) * p [...,
+    outputs] and kept = packed u [..., 2, outputs] for the backward pass (None with keep=False).  u is 32 bits and never stored."""
+    rows, cols = _packed_rows(x)
+    out, w_stride = _halves(weight, cols, x.device)
+    gated = _empty_packed(x.shape[:-1] + (out,), x.device)
+    kept = _empty_packed(x.shape[:-1] + (2, out), x.device) if keep else None
+    work = _work("leap_gated_linear8_work", x.device, rows, cols, out)
+    _call("leap_gated_linear8", x.device, x.codes.data_ptr(), x.scales.data_ptr(), rows, cols, weight.data_ptr(), w_stride, out,
+          gated.codes.data_ptr(), gated.scales.data_ptr(), kept.codes.data_ptr() if keep else None, kept.scales.data_ptr() if keep else None,
+          _address(work))
+    return gated, kept
+
+
+def _kept_halves(kept: Packed8):
+    _on_gpu(kept.codes, "kept")
+    shape = kept.shape
+    if len(shape) < 2 or shape[-2] != 2:
+        raise ValueError(f"kept must be [..., 2, outputs], got {tuple(shape)}")
+    return shape[:-2], shape[-1]
+
+
+def gate8_backward(grad: torch.Tensor, kept: Packed8) -> torch.Tensor:
+    """du [..., 2 * outputs] (bfloat16), the gradient of gated_linear8's u, from that of `gated`."""
+    lead, out = _kept_halves(kept)
+    rows, _, stride = _gradient(grad, lead + (out,), kept.device, (torch.bfloat16,), "grad")
+    du = torch.empty(lead + (2 * out,), dtype=torch.bfloat16, device=kept.device)
+    _call("leap_gate8_backward", kept.device, grad.data_ptr(), stride, kept.codes.data_ptr(), kept.scales.data_ptr(), rows, out, du.data_ptr())
+    return du
+
+
+def linear_gate8_backward(grad: torch.Tensor, weight: torch.Tensor, kept: Packed8) -> torch.Tensor:
+    """gate8_backward of grad W, which stays in 32 bits: du from the gradient of the product linear8(gated, weight)."""
+    lead, out = _kept_halves(kept)
+    following, w_stride = _weight(weight, out, kept.device)
+    rows, _, stride = _gradient(grad, lead + (following,), kept.device, (torch.bfloat16,), "grad")
+    du = torch.empty(lead + (2 * out,), dtype=torch.bfloat16, device=kept.device)
+    work = _work("leap_linear_gate8_work", kept.device, rows, out, following)
+    _call("leap_linear_gate8_backward", kept.device, grad.data_ptr(), stride, weight.data_ptr(), w_stride, following, kept.codes.data_ptr(),
+          kept.scales.data_ptr(), rows, out, du.data_ptr(), _address(work))
+    return du
+
+
+def gated_linear8_backward(grad: torch.Tensor, kept: Packed8, x: Packed8, weight: torch.Tensor, need_x: bool = True, need_weight: bool = True):
+    """(grad_x, grad_weight) of gated_linear8 from the gradient of `gated` (bfloat16)."""
+    if kept.shape[:-2] != x.shape[:-1]:
+        raise ValueError(f"kept {tuple(kept.shape)} is not of this x {tuple(x.shape)}")
+    return linear8_backward(gate8_backward(grad, kept), x, weight, need_x, need_weight)
+
+
+# ---- the block ----------------------------------------------------------------------------------------------------------
+
+
+class _FeedForward8(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, residual, norm_weight, up, down, eps):
+        total, normed, kept_sum, rstd = rms_norm8(x, norm_weight, residual, eps)
+        gated, kept = gated_linear8(normed, up)
+        y = linear8(gated, down)
+        # a tensor apart from its input: autograd would take it for a view
+        total = total.view_as(total) if residual is None else total
+        ctx.save_for_backward(norm_weight, up, down, rstd, *(t for p in (normed, kept_sum, gated, kept) for t in (p.codes, p.scales)))
+        ctx.set_materialize_grads(False)
+        ctx.added = residual is not None
+        return y, total
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, grad_y, grad_sum):
+        norm_weight, up, down, rstd, *packed = ctx.saved_tensors
+        normed, kept_sum, gated, kept = (Packed8(*packed[i:i + 2]) for i in range(0, 8, 2))
+        need_x, need_r, need_norm, need_up, need_down = ctx.needs_input_grad[:5]
+        if grad_y is None:
+            return grad_sum, grad_sum if ctx.added else None, None, None, None, None
+        grad_y = grad_y.contiguous()
+        grad_down = linear8_backward(grad_y, gated, down, need_x=False)[1] if need_down else None
+        grad_x = grad_norm = grad_up = None
+        if need_x or need_r or need_norm or need_up:
+            du = linear_gate8_backward(grad_y, down, kept)
+            # 32 bits between the product and the norm: a rounding less in grad_x
+            dn, grad_up = linear8_backward(du, normed, up, need_x or need_r or need_norm, need_up, torch.float32)
+            if dn is not None:
+                grad_x, grad_norm = rms_norm8_backward(dn, kept_sum, rstd, norm_weight, None if grad_sum is None else grad_sum.contiguous(),
+                                                       torch.bfloat16)
+        return grad_x if need_x else None, grad_x if need_r else None, grad_norm if need_norm else None, grad_up, grad_down, None
+
+
+def feed_forward8(x: torch.Tensor, norm_weight: torch.Tensor, up: torch.Tensor, down: torch.Tensor, residual: torch.Tensor = None,
+                  eps: float = 1e-6):
+    """(y, sum), differentiable: sum = x + residual and y = linear8(gated_linear8(rms_norm8(sum), up), down).  x, residual: bfloat16
+    [..., columns]; up: [2 * hidden, columns], the gate's rows first; down: [outputs, hidden].  For a stack of blocks y and sum are the next one's
+    x and residual.  Kept for the backward pass: the norm's output, sum and the hidden rows (three times), all in 8 bits."""
+    _on_gpu(x, "x")
+    if x.dtype is not torch.bfloat16:
+        raise ValueError(f"x must be bfloat16, not {x.dtype}")
+    return _FeedForward8.apply(x, residual, norm_weight, up, down, eps)
+
+
+class FeedForward8(torch.nn.Module):
+    """feed_forward8 with weights of its own (bfloat16): (x, residual) -> (y, sum)."""
+
+    def __init__(self, columns: int, hidden: int, eps: float = 1e-6, device="cuda:0"):
+        super().__init__()
+        self.eps = eps
+        self.norm_weight = torch.nn.Parameter(torch.ones(columns, dtype=torch.bfloat16, device=device))
+        self.up = torch.nn.Parameter((torch.randn(2 * hidden, columns, device=device) / columns ** 0.5).to(torch.bfloat16))
+        self.down = torch.nn.Parameter((torch.randn(columns, hidden, device=device) / hidden ** 0.5).to(torch.bfloat16))
+
+    def forward(self, x: torch.Tensor, residual: torch.Tensor = None):
+        return feed_forward8(x, self.norm_weight, self.up, self.down, residual, self.eps)

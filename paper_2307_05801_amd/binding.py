@@ -22,6 +22,24 @@ EXPORTS = ("leap_geometry_create", "leap_geometry_destroy", "leap_project", "lea
            "leap_status_string", "leap_last_error", "leap_geometry_describe",
            "leap_recon_workspace_floats", "leap_sirt", "leap_least_squares_descent")
 
+LEAP_F32, LEAP_BF16, LEAP_F16 = 0, 1, 2                      # element types of include/leap_activations.h
+_P, _I, _L = C.c_void_p, C.c_int32, C.c_int64
+ACTIVATION_EXPORTS = {                                       # name: (result, arguments)
+    "leap_pack8": (C.c_int, [_P, _I, _L, _L, _L, _P, _P, _P]),
+    "leap_unpack8": (C.c_int, [_P, _P, _L, _L, _P, _I, _P]),
+    "leap_rms_norm8": (C.c_int, [_P, _L, _P, _L, _I, _P, _I, _L, _L, C.c_float] + [_P] * 7),
+    "leap_rms_norm8_work": (_L, [_L, _L]),
+    "leap_rms_norm8_backward": (C.c_int, [_P, _I, _L, _P, _L, _I, _P, _P, _P, _P, _I, _L, _L, _P, _P, _P, _P]),
+    "leap_linear8": (C.c_int, [_P, _P, _L, _L, _P, _L, _L, _P, _P]),
+    "leap_linear8_work": (_L, [_L, _L, _L]),
+    "leap_linear8_backward": (C.c_int, [_P, _L, _P, _P, _L, _L, _P, _L, _L, _P, _I, _P, _P, _P]),
+    "leap_gated_linear8_work": (_L, [_L, _L, _L]),
+    "leap_gated_linear8": (C.c_int, [_P, _P, _L, _L, _P, _L, _L, _P, _P, _P, _P, _P, _P]),
+    "leap_gate8_backward": (C.c_int, [_P, _L, _P, _P, _L, _L, _P, _P]),
+    "leap_linear_gate8_work": (_L, [_L, _L, _L]),
+    "leap_linear_gate8_backward": (C.c_int, [_P, _L, _P, _L, _L, _P, _P, _L, _L, _P, _P, _P]),
+}
+
 
 class leap_geometry_desc(C.Structure):
     _fields_ = [
@@ -92,6 +110,22 @@ def load_library(path: Optional[str] = None):
     if path is None:
         _lib = lib
     return lib
+
+
+_activations = None
+
+
+def load_activations():
+    """The library with the prototypes of include/leap_activations.h (apart from load_library: another build of the library,
+    under LEAP_LIB_PATH, need not have them)."""
+    global _activations
+    if _activations is None:
+        lib = load_library()
+        for name, (result, arguments) in ACTIVATION_EXPORTS.items():
+            fn = getattr(lib, name)
+            fn.restype, fn.argtypes = result, arguments
+        _activations = lib
+    return _activations
 
 
 def _check(lib, status: int) -> None:

@@ -1,0 +1,144 @@
+"""Operators on activations in 8 bits, what needs no GPU: the ABI, the refusals, the format's reference."""
+import ctypes as C
+import os
+import re
+
+import pytest
+import torch
+
+import activations_reference as R
+from paper_2307_05801_amd import binding as B
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+BF16, F32 = torch.bfloat16, torch.float32
+
+
+@pytest.fixture(scope="module")
+def lib():
+    if not os.path.exists(B.LIB_PATH):
+        from paper_2307_05801_amd.build import build_library
+        build_library()
+    return B.load_activations()
+
+
+def test_every_declared_symbol_is_exported_and_bound(lib):
+    header = open(os.path.join(ROOT, "include", "leap_activations.h")).read()
+    header = re.sub(r"/\*.*?\*/", "", header, flags=re.S)
+    declared = dict(re.findall(r"\b(leap_[a-z0-9_]+)\s*\(([^)]*)\)", header))
+    assert set(declared) == set(B.ACTIVATION_EXPORTS)
+    for name, arguments in declared.items():
+        assert getattr(lib, name) is not None
+        assert len(arguments.split(",")) == len(B.ACTIVATION_EXPORTS[name][1]), name
+
+
+# Addresses are never touched: every call below is refused before anything is launched.
+P = 0x1000
+
+
+@pytest.mark.parametrize("name,good,bad", [
+    ("leap_pack8", (P, 1, 64, 4, 64, P, P, 0), [(1, 3), (1, -1), (2, -1), (2, 63), (2, 1 << 59), (3, -1), (4, 0), (4, 1 << 21), (3, 1 << 40), (0, 0), (5, 0), (6, 0)]),
+    ("leap_unpack8", (P, P, 4, 64, P, 1, 0), [(5, 9), (2, -1), (3, 0), (0, 0), (1, 0), (4, 0)]),
+    ("leap_rms_norm8", (P, 64, P, 64, 1, P, 1, 4, 64, 1e-6, P, P, P, P, P, P, 0),
+     [(4, 3), (6, 2), (6, 5), (7, -4), (8, 0), (1, 63), (3, 63), (9, -1.0), (9, float("nan")), (0, 0), (5, 0), (11, 0), (12, 0), (13, 0), (14, 0), (7, 1 << 32)]),
+    ("leap_rms_norm8_backward", (P, 1, 64, P, 64, 1, P, P, P, P, 1, 4, 64, P, P, P, 0),
+     [(1, 2), (5, 8), (10, 2), (2, 1), (4, 1), (11, -1), (12, 0), (0, 0), (6, 0), (7, 0), (8, 0), (9, 0), (13, 0), (15, 0), (11, 1 << 32)]),
+    ("leap_linear8", (P, P, 4, 64, P, 64, 8, P, 0), [(2, -1), (3, 0), (5, 63), (6, 0), (0, 0), (1, 0), (4, 0), (7, 0), (6, 1 << 21)]),
+    ("leap_linear8_backward", (P, 8, P, P, 4, 64, P, 64, 8, P, 1, P, P, 0), [(1, 7), (4, -1), (5, 0), (7, 1), (8, 0), (10, 2), (0, 0), (2, 0), (3, 0), (6, 0)]),
+    ("leap_gated_linear8", (P, P, 4, 64, P, 64, 8, P, P, P, P, P, 0), [(2, -1), (3, 0), (5, 63), (6, 0), (6, 1 << 20), (0, 0), (1, 0), (4, 0), (7, 0), (8, 0), (9, 0), (10, 0)]),
+    ("leap_gate8_backward", (P, 8, P, P, 4, 8, P, 0), [(1, 7), (4, -1), (5, 0), (5, 1 << 20), (0, 0), (2, 0), (3, 0), (6, 0)]),
+    ("leap_linear_gate8_backward", (P, 8, P, 16, 8, P, P, 4, 16, P, P, 0), [(1, 7), (3, 15), (4, 0), (7, -1), (8, 0), (8, 1 << 20), (0, 0), (2, 0), (5, 0), (6, 0), (9, 0)]),
+])
+def test_bad_arguments_are_refused_with_a_message(lib, name, good, bad):
+    for at, value in bad:
+        arguments = list(good)
+        arguments[at] = value
+        assert getattr(lib, name)(*arguments) == B.LEAP_INVALID_ARG, (name, at, value)
+        assert lib.leap_last_error().decode()
+
+
+def test_no_rows_is_fine(lib):
+    assert lib.leap_pack8(None, 0, 64, 0, 64, None, None, None) == B.LEAP_OK
+    assert lib.leap_unpack8(None, None, 0, 64, None, 0, None) == B.LEAP_OK
+    assert lib.leap_rms_norm8(None, 64, None, 0, 1, None, 1, 0, 64, 1e-6, *[None] * 7) == B.LEAP_OK
+    assert lib.leap_linear8(None, None, 0, 64, None, 64, 8, None, None) == B.LEAP_OK
+    assert lib.leap_gate8_backward(None, 8, None, None, 0, 8, None, None) == B.LEAP_OK
+
+
+def test_workspaces_of_bad_sizes_are_nothing(lib):
+    assert lib.leap_rms_norm8_work(-1, 64) == 0 and lib.leap_rms_norm8_work(5, 0) == 0
+    assert lib.leap_linear8_work(-1, 64, 8) == 0 and lib.leap_gated_linear8_work(4, 0, 8) == 0 and lib.leap_linear_gate8_work(4, 8, -1) == 0
+
+
+def _packed(rows, cols):
+    from paper_2307_05801_amd.activations import Packed8
+    return Packed8(torch.zeros(rows, cols).to(torch.float8_e4m3fn), torch.zeros(rows, -(-cols // 32), dtype=torch.uint8))
+
+
+def test_packed8_checks_its_parts():
+    from paper_2307_05801_amd.activations import Packed8
+    codes, scales = torch.zeros(3, 40).to(torch.float8_e4m3fn), torch.zeros(3, 2, dtype=torch.uint8)
+    assert Packed8(codes, scales).shape == (3, 40)
+    for bad in ((codes.view(torch.uint8), scales), (codes, scales.float()), (codes, scales[:, :1]), (codes, scales[:2]),
+                (codes.view(torch.uint8).t().contiguous().t().view(torch.float8_e4m3fn), scales)):
+        with pytest.raises(ValueError):
+            Packed8(*bad)
+
+
+def test_tensors_on_the_cpu_are_refused():
+    from paper_2307_05801_amd import activations as A
+    x, w, p = torch.zeros(4, 64, dtype=BF16), torch.ones(64, dtype=BF16), _packed(4, 64)
+    big = torch.zeros(8, 64, dtype=BF16)
+    for call in (lambda: A.pack8(x), lambda: A.unpack8(p), lambda: A.rms_norm8(x, w), lambda: A.linear8(p, big),
+                 lambda: A.gated_linear8(p, big), lambda: A.gate8_backward(x, _packed(4, 64)), lambda: A.feed_forward8(x, w, big, big),
+                 lambda: A.rms_norm8_backward(x, p, torch.ones(4), w), lambda: A.linear8_backward(x, p, big)):
+        with pytest.raises(ValueError):
+            call()
+
+
+@pytest.mark.parametrize("make,want", [
+    (lambda: torch.zeros(4, 6), (4, 6, 6)),
+    (lambda: torch.zeros(6), (1, 6, 6)),
+    (lambda: torch.zeros(4, 10)[:, :6], (4, 6, 10)),
+    (lambda: torch.zeros(8, 6)[::2], (4, 6, 12)),
+    (lambda: torch.zeros(2, 3, 10)[..., 2:8], (6, 6, 10)),
+    (lambda: torch.zeros(2, 1, 3, 10)[..., :6], (6, 6, 10)),
+    (lambda: torch.zeros(0, 6), (0, 6, 6)),
+    (lambda: torch.zeros(3, 0, 10)[..., :6], (0, 6, 6)),
+    (lambda: torch.zeros(4, 1), (4, 1, 1)),
+    (lambda: torch.zeros(1, 10)[:, :6], (1, 6, 6)),
+])
+def test_rows_of_a_tensor(make, want):
+    from paper_2307_05801_amd.activations import _rows
+    assert _rows(make(), "x") == want
+
+
+@pytest.mark.parametrize("make", [
+    lambda: torch.zeros(6, 4).t(), lambda: torch.zeros(4, 12)[:, ::2], lambda: torch.zeros(2, 5, 6)[:, :3], lambda: torch.tensor(1.0),
+    lambda: torch.zeros(4, 0), lambda: torch.zeros(1, 6).expand(4, 6), lambda: torch.zeros(9).as_strided((4, 6), (1, 1)),
+])
+def test_rows_that_are_not_evenly_spaced_are_refused(make):
+    from paper_2307_05801_amd.activations import _rows
+    with pytest.raises(ValueError):
+        _rows(make(), "x")
+
+
+def test_the_reference_of_the_format_agrees_with_torchs_cast():
+    g = torch.Generator().manual_seed(5)
+    x = (torch.randn(200, 70, generator=g) * torch.exp(torch.randn(200, 1, generator=g) * 8)).bfloat16().double()
+    codes, scales = R.pack(x)
+    power = (2.0 ** (scales.double() - 127)).repeat_interleave(32, -1)[..., :70]
+    want = (x / power).float().to(torch.float8_e4m3fn)
+    assert torch.equal(codes, want.view(torch.uint8))
+    assert float((R.grouped(x).abs().amax(-1) / 2.0 ** (scales.double() - 127)).max()) <= 448
+
+
+def test_the_reference_notices_a_wrong_code():
+    """The bound of a held value, on a mistake planted in the reference: every code one too high, and a scale half as large."""
+    from paper_2307_05801_amd.activations import Packed8
+    x = torch.randn(8, 64, generator=torch.Generator().manual_seed(6)).double()
+    codes, scales = R.pack(x)
+    none = torch.zeros_like(x)
+    R.assert_held(Packed8(codes.view(torch.float8_e4m3fn), scales), x, none)
+    for wrong in ((codes + 1, scales), (codes, scales - 1)):
+        with pytest.raises(AssertionError):
+            R.assert_held(Packed8(wrong[0].view(torch.float8_e4m3fn), wrong[1]), x, none)
