@@ -62,21 +62,25 @@ int leap_rms_norm8_backward(const void *d_grad, int32_t grad_type, int64_t grad_
                             int32_t weight_type, int64_t rows, int64_t cols, void *d_grad_x, void *d_grad_weight, float *d_work,
                             void *hip_stream);
 
-/* y [rows][out] (bfloat16, no gaps) = v W^T, v the packed rows [rows][cols], W [out][cols] bfloat16, its rows w_stride apart. */
+/* y [rows][out] (bfloat16, no gaps) = v W^T, v the packed rows [rows][cols], W [out][cols] bfloat16, its rows w_stride apart.
+ * d_work (all products): as many bytes as the function of that name + "_work" says, 16-byte aligned; NULL where it says 0.
+ * It holds copies of what is not laid out for the kernels: codes whose columns are no multiple of 16, weights and gradients
+ * whose rows do not begin and end at multiples of 16 bytes (the pointers handed over are looked at for that alone). */
+int64_t leap_linear8_work(const uint8_t *d_codes, int64_t rows, int64_t cols, const void *d_weight, int64_t w_stride, int64_t out);
 int leap_linear8(const uint8_t *d_codes, const uint8_t *d_scales, int64_t rows, int64_t cols, const void *d_weight, int64_t w_stride,
-                 int64_t out, void *d_y, void *hip_stream);
+                 int64_t out, void *d_y, void *d_work, void *hip_stream);
 
 /* Its gradients: grad_x [rows][cols] = dy W, of grad_x_type (LEAP_BF16 or LEAP_F32), and grad_weight [out][cols] = dy^T v,
- * bfloat16; either may be NULL.  dy: [rows][out] bfloat16 with a stride.  d_work: leap_linear8_work() bytes, 16-byte aligned. */
-int64_t leap_linear8_work(int64_t rows, int64_t cols, int64_t out);
+ * bfloat16; either may be NULL.  dy: [rows][out] bfloat16 with a stride. */
+int64_t leap_linear8_backward_work(const void *d_dy, int64_t dy_stride, const uint8_t *d_codes, int64_t rows, int64_t cols, const void *d_weight,
+                                   int64_t w_stride, int64_t out);
 int leap_linear8_backward(const void *d_dy, int64_t dy_stride, const uint8_t *d_codes, const uint8_t *d_scales, int64_t rows, int64_t cols,
                           const void *d_weight, int64_t w_stride, int64_t out, void *d_grad_x, int32_t grad_x_type,
                           void *d_grad_weight, void *d_work, void *hip_stream);
 
 /* The gated product.  u = v W^T in 32 bits with W [2 * out][cols], the gate's rows first: u = (g, p);
  * gated = packed g * sigmoid(g) * p, [rows][out];  kept = packed u as [rows][2][out] (the groups of the two halves apart), or
- * NULL.  d_work: leap_gated_linear8_work() bytes, 16-byte aligned. */
-int64_t leap_gated_linear8_work(int64_t rows, int64_t cols, int64_t out);
+ * NULL.  d_work: leap_linear8_work() of this weight with its 2 * out rows. */
 int leap_gated_linear8(const uint8_t *d_codes, const uint8_t *d_scales, int64_t rows, int64_t cols, const void *d_weight, int64_t w_stride,
                        int64_t out, uint8_t *d_gated_codes, uint8_t *d_gated_scales, uint8_t *d_kept_codes, uint8_t *d_kept_scales,
                        void *d_work, void *hip_stream);
@@ -85,10 +89,10 @@ int leap_gated_linear8(const uint8_t *d_codes, const uint8_t *d_scales, int64_t 
  * other da * g * s, with s = sigmoid(g).  With u's gradient in hand leap_linear8_backward gives those of v and W.
  * leap_gate8_backward reads da [rows][out] (bfloat16, with a stride); leap_linear_gate8_backward forms it, in 32 bits, as
  * dy W with W [next][out] bfloat16 (the weight of the product that read `gated`) and dy [rows][next] bfloat16.
- * d_work: leap_linear_gate8_work() bytes, 16-byte aligned. */
+ * d_work: leap_linear_gate8_work() bytes. */
 int leap_gate8_backward(const void *d_da, int64_t da_stride, const uint8_t *d_kept_codes, const uint8_t *d_kept_scales, int64_t rows,
                         int64_t out, void *d_du, void *hip_stream);
-int64_t leap_linear_gate8_work(int64_t rows, int64_t out, int64_t next);
+int64_t leap_linear_gate8_work(const void *d_dy, int64_t dy_stride, const void *d_weight, int64_t w_stride, int64_t next, int64_t rows, int64_t out);
 int leap_linear_gate8_backward(const void *d_dy, int64_t dy_stride, const void *d_weight, int64_t w_stride, int64_t next,
                                const uint8_t *d_kept_codes, const uint8_t *d_kept_scales, int64_t rows, int64_t out, void *d_du,
                                void *d_work, void *hip_stream);

@@ -260,7 +260,8 @@ def linear8(x: Packed8, weight: torch.Tensor) -> torch.Tensor:
     rows, cols = _packed_rows(x)
     out, w_stride = _weight(weight, cols, x.device)
     y = torch.empty(x.shape[:-1] + (out,), dtype=torch.bfloat16, device=x.device)
-    _call("leap_linear8", x.device, x.codes.data_ptr(), x.scales.data_ptr(), rows, cols, weight.data_ptr(), w_stride, out, y.data_ptr())
+    work = _work("leap_linear8_work", x.device, x.codes.data_ptr(), rows, cols, weight.data_ptr(), w_stride, out)
+    _call("leap_linear8", x.device, x.codes.data_ptr(), x.scales.data_ptr(), rows, cols, weight.data_ptr(), w_stride, out, y.data_ptr(), _address(work))
     return y
 
 
@@ -274,7 +275,7 @@ def linear8_backward(grad: torch.Tensor, x: Packed8, weight: torch.Tensor, need_
         raise ValueError("grad_x is bfloat16 or float32")
     grad_x = torch.empty(x.shape, dtype=dtype, device=x.device) if need_x else None
     grad_weight = torch.empty((out, cols), dtype=torch.bfloat16, device=x.device) if need_weight else None
-    work = _work("leap_linear8_work", x.device, rows, cols, out)
+    work = _work("leap_linear8_backward_work", x.device, grad.data_ptr(), stride, x.codes.data_ptr(), rows, cols, weight.data_ptr(), w_stride, out)
     _call("leap_linear8_backward", x.device, grad.data_ptr(), stride, x.codes.data_ptr(), x.scales.data_ptr(), rows, cols, weight.data_ptr(),
           w_stride, out, _address(grad_x), _TYPES[dtype], _address(grad_weight), _address(work))
     return grad_x, grad_weight
@@ -294,7 +295,7 @@ def gated_linear8(x: Packed8, weight: torch.Tensor, keep: bool = True):
     out, w_stride = _halves(weight, cols, x.device)
     gated = _empty_packed(x.shape[:-1] + (out,), x.device)
     kept = _empty_packed(x.shape[:-1] + (2, out), x.device) if keep else None
-    work = _work("leap_gated_linear8_work", x.device, rows, cols, out)
+    work = _work("leap_linear8_work", x.device, x.codes.data_ptr(), rows, cols, weight.data_ptr(), w_stride, 2 * out)
     _call("leap_gated_linear8", x.device, x.codes.data_ptr(), x.scales.data_ptr(), rows, cols, weight.data_ptr(), w_stride, out,
           gated.codes.data_ptr(), gated.scales.data_ptr(), kept.codes.data_ptr() if keep else None, kept.scales.data_ptr() if keep else None,
           _address(work))
@@ -324,7 +325,7 @@ def linear_gate8_backward(grad: torch.Tensor, weight: torch.Tensor, kept: Packed
     following, w_stride = _weight(weight, out, kept.device)
     rows, _, stride = _gradient(grad, lead + (following,), kept.device, (torch.bfloat16,), "grad")
     du = torch.empty(lead + (2 * out,), dtype=torch.bfloat16, device=kept.device)
-    work = _work("leap_linear_gate8_work", kept.device, rows, out, following)
+    work = _work("leap_linear_gate8_work", kept.device, grad.data_ptr(), stride, weight.data_ptr(), w_stride, following, rows, out)
     _call("leap_linear_gate8_backward", kept.device, grad.data_ptr(), stride, weight.data_ptr(), w_stride, following, kept.codes.data_ptr(),
           kept.scales.data_ptr(), rows, out, du.data_ptr(), _address(work))
     return du

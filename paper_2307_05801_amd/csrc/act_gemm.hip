@@ -1,156 +1,144 @@
-// Products with rows held in 8 bits, and the gated product: leap_linear8 and its kin.
+// Products with rows held in 8 bits, and the gated product: leap_linear8 and its kin (act_product.h has the kernel).
 //
-// All of them are D[j][i] = sum over k of P(i, k) Q(j, k) for two operands that are rows of bfloat16 or of packed values, read
-// along k or across it.  A packed value is exact in bfloat16, so tiles of both go to shared memory as bfloat16 and through the
-// matrix instructions, which sum in 32 bits.
-#include "act_common.h"
+// Its fetches want memory rows that begin at multiples of 16 bytes.  Operands that do not (odd sizes, odd strides) are
+// first laid out anew in the workspace, a pass over them that costs a few percent of the product.
+#include "act_product.h"
 
 namespace {
 
 using namespace act;
 
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef float f32x16 __attribute__((ext_vector_type(16)));
-
 constexpr int BLOCK = 256;
-constexpr int TILE = 128, DEPTH = 32;      // a block's share of D is TILE x TILE, DEPTH values of k at a time
-constexpr int PITCH = DEPTH + 8;           // of a tile's rows in shared memory: neighbouring rows in other banks
 
-enum { ALONG, ACROSS };                    // an operand's values of one k-run are neighbours; or those of one k
+// ---- operands laid out for the product ----
 
-// An operand: `rows` rows of `depth` values of k.  ALONG: memory rows are the operand's rows; ACROSS: they are k.
-struct operand {
-    const uint8_t *data;         // bfloat16 values, or codes
-    const uint8_t *scales;       // null: bfloat16
-    int64_t stride, groups;      // between memory rows: elements, scale bytes
-    int64_t rows, depth;
+// to[r] <- from[r], `bytes` long, then zeros up to `pitch` (a multiple of 16)
+__global__ __launch_bounds__(BLOCK) void k_lay_out(const uint8_t *__restrict__ from, int64_t stride, int64_t rows, int64_t bytes, uint8_t *__restrict__ to,
+                                                   int64_t pitch, divider pieces, int64_t row0)
+{
+    const uint32_t q = blockIdx.x * (uint32_t)BLOCK + threadIdx.x, in = pieces(q);
+    const int64_t row = row0 + in, at = (int64_t)(q - in * pieces.by) * 16;
+    if (row >= rows) return;
+    uint8_t piece[16] = {};
+    if (bytes - at >= 16) {
+        __builtin_memcpy(piece, from + row * stride + at, 16);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 15; ++i)
+            if (at + i < bytes) piece[i] = from[row * stride + at + i];
+    }
+    __builtin_memcpy(to + row * pitch + at, piece, 16);
+}
+
+int64_t up16(int64_t n) { return (n + 15) / 16 * 16; }
+
+// Memory rows as the product takes them: as they are, or a copy of them in the workspace.
+struct laid {
+    const uint8_t *data;
+    int64_t stride, rows, bytes, pitch;              // in bytes
+    bool copied;
+    laid(const void *p, int64_t stride_, int64_t rows_, int64_t cols, int size)
+        : data((const uint8_t *)p), stride(stride_ * size), rows(rows_), bytes(cols * size), pitch(up16(cols * size))
+    {
+        copied = rows > 0 && (stride % 16 != 0 || bytes % 16 != 0 || (uintptr_t)p % 16 != 0);
+    }
+    int64_t room() const { return copied ? rows * pitch : 0; }
+
+    // The copy, at `to`, which moves on.
+    int lay_out(uint8_t *&to, hipStream_t st)
+    {
+        if (!copied) return LEAP_OK;
+        const int64_t pieces = pitch / 16, most = ((int64_t)1 << 30) / pieces;
+        for (int64_t row0 = 0; row0 < rows; row0 += most) {
+            const int64_t part = rows - row0 < most ? rows - row0 : most;
+            hipLaunchKernelGGL(k_lay_out, dim3((unsigned)((part * pieces + BLOCK - 1) / BLOCK)), dim3(BLOCK), 0, st, data, stride, rows, bytes, to, pitch,
+                               divider((uint32_t)pieces), row0);
+            const int rc = launched();
+            if (rc != LEAP_OK) return rc;
+        }
+        data = to, stride = pitch, copied = false;
+        to += rows * pitch;
+        return LEAP_OK;
+    }
+
+    operand wide(int64_t i, int64_t k) const { return {data, nullptr, stride / 2, 0, i, k}; }
+    operand codes(const uint8_t *scales, int64_t cols, int64_t i, int64_t k) const { return {data, scales, stride, groups_of(cols), i, k}; }
 };
 
-// Eight values from (row, col) of the memory on, n of them there, as bfloat16.
-template <bool PACKED> __device__ inline bf16x8 fetch8(const operand &O, int64_t row, int64_t col, int n)
+// ---- launches ----
+
+int64_t cut(int64_t n, int64_t by) { return (n + by - 1) / by; }
+
+// Tiles of 256 x 256 where they fill the 256 compute units, else of 128 x 128.
+bool large_tiles(int64_t i, int64_t j, int64_t parts = 1) { return cut(i, 256) * cut(j, 256) * parts >= 200; }
+
+template <int PKIND, int QKIND, int TO, int TI, int TJ, int WI, int WJ>
+int launch(const operand &P, const operand &Q, const result &R, int64_t depth_part, hipStream_t st)
 {
-    float v[CHUNK] = {};
-    if (n > 0) {
-        if constexpr (PACKED) decode8(load_codes(O.data + row * O.stride + col, n), scale_value(O.scales[row * O.groups + col / GROUP]), v);
-        else load8<LEAP_BF16>(O.data, row * O.stride + col, n, v);
-    }
-    bf16x8 b;
-#pragma unroll
-    for (int i = 0; i < CHUNK; ++i) b[i] = (__bf16)v[i];
-    return b;
+    const int64_t across = TO == TO_GATED ? cut(R.columns, TI / 2) : cut(P.rows, TI), along = cut(Q.rows, TJ), parts = depth_part ? cut(P.depth, depth_part) : 1;
+    if (across * along * parts > 0x7fffffff) return refuse("more rows and columns than one launch covers");
+    hipLaunchKernelGGL((k_product<PKIND, QKIND, TO, TI, TJ, WI, WJ>), dim3((unsigned)(across * along * parts)), dim3(WI * WJ * 64), 0, st, P, Q, R,
+                       (uint32_t)across, (uint32_t)along, depth_part ? depth_part : P.depth);
+    return launched();
 }
 
-__device__ inline int clip8(int64_t left) { return left <= 0 ? 0 : left < CHUNK ? (int)left : CHUNK; }
-
-// tile[r][k] <- O(row0 + r, k0 + k), zeros beyond its ends
-template <int HOW, bool PACKED> __device__ inline void fill(const operand &O, int64_t row0, int64_t k0, __bf16 (*tile)[PITCH])
+template <int PKIND, int QKIND, int TO> int product(const operand &P, const operand &Q, const result &R, hipStream_t st)
 {
-    for (int c = threadIdx.x; c < TILE * DEPTH / CHUNK; c += BLOCK) {
-        if constexpr (HOW == ALONG) {
-            const int r = c / (DEPTH / CHUNK), k = c % (DEPTH / CHUNK) * CHUNK;
-            const bf16x8 b = fetch8<PACKED>(O, row0 + r, k0 + k, row0 + r < O.rows ? clip8(O.depth - k0 - k) : 0);
-            *(bf16x8 *)&tile[r][k] = b;
+    if (large_tiles(P.rows, Q.rows)) return launch<PKIND, QKIND, TO, 256, 256, 2, 4>(P, Q, R, 0, st);
+    return launch<PKIND, QKIND, TO, 128, 128, 2, 2>(P, Q, R, 0, st);
+}
+
+// grad_weight: few tiles, many rows to sum over.  The rows are cut into parts, as many as give every compute unit a tile,
+// of at least 512 rows; each part's sum goes to the workspace in 32 bits, and a kernel adds them in order.
+struct weight_plan {
+    bool large;
+    int64_t parts, depth_part;
+    weight_plan(int64_t rows, int64_t cols, int64_t out)
+    {
+        const int64_t tiles = cut(cols, 256) * cut(out, 256);
+        large = tiles * cut(rows, 1024) >= 256;
+        const int64_t t = large ? tiles : cut(cols, 128) * cut(out, 128), want = (large ? 256 : 512) / t;
+        parts = want < 1 ? 1 : want;
+        if (parts > cut(rows, 512)) parts = cut(rows, 512);
+        if (parts < 1) parts = 1;
+        depth_part = cut(cut(rows, parts), STEP) * STEP;
+        if (depth_part < STEP) depth_part = STEP;
+        parts = rows ? cut(rows, depth_part) : 1;
+    }
+    int64_t room(int64_t cols, int64_t out) const { return parts > 1 ? up16(parts * cols * out * (int64_t)sizeof(float)) : 0; }
+};
+
+__global__ __launch_bounds__(BLOCK) void k_add_parts(const float *__restrict__ from, int64_t parts, int64_t n, uint16_t *__restrict__ to)
+{
+    const int64_t at = ((int64_t)blockIdx.x * BLOCK + threadIdx.x) * 4;
+    if (at >= n) return;
+    float sum[4] = {};
+    const int left = n - at < 4 ? (int)(n - at) : 4;
+    for (int64_t p = 0; p < parts; ++p) {
+        if (left == 4) {
+            float f[4];
+            __builtin_memcpy(f, from + p * n + at, 16);
+#pragma unroll
+            for (int x = 0; x < 4; ++x) sum[x] += f[x];
         } else {
-            const int k = c / (TILE / CHUNK), r = c % (TILE / CHUNK) * CHUNK;
-            const bf16x8 b = fetch8<PACKED>(O, k0 + k, row0 + r, k0 + k < O.depth ? clip8(O.rows - row0 - r) : 0);
-#pragma unroll
-            for (int i = 0; i < CHUNK; ++i) tile[r + i][k] = b[i];
+            for (int x = 0; x < left; ++x) sum[x] += from[p * n + at + x];
         }
     }
+    for (int x = 0; x < left; ++x) to[at + x] = element<LEAP_BF16>::from_float(sum[x]);
 }
 
-// out[j][i] of OTYPE, its rows `stride` apart
-template <int PHOW, bool PPACKED, int QHOW, bool QPACKED, int OTYPE>
-__global__ __launch_bounds__(BLOCK) void k_product(operand P, operand Q, void *__restrict__ out, int64_t stride)
-{
-    __shared__ __attribute__((aligned(16))) __bf16 p[TILE][PITCH], q[TILE][PITCH];
-    const int64_t i0 = (int64_t)blockIdx.x * TILE, j0 = (int64_t)blockIdx.y * TILE;
-    const int wave = threadIdx.x / 64, lane = threadIdx.x % 64, wi = wave % 2 * 64, wj = wave / 2 * 64;
-    f32x16 acc[2][2] = {};
-    for (int64_t k0 = 0; k0 < P.depth; k0 += DEPTH) {
-        __syncthreads();
-        fill<PHOW, PPACKED>(P, i0, k0, p);
-        fill<QHOW, QPACKED>(Q, j0, k0, q);
-        __syncthreads();
-#pragma unroll
-        for (int k = 0; k < DEPTH; k += 16) {
-            bf16x8 a[2], b[2];
-#pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                a[t] = *(const bf16x8 *)&p[wi + t * 32 + lane % 32][k + lane / 32 * 8];
-                b[t] = *(const bf16x8 *)&q[wj + t * 32 + lane % 32][k + lane / 32 * 8];
-            }
-#pragma unroll
-            for (int s = 0; s < 2; ++s)
-#pragma unroll
-                for (int t = 0; t < 2; ++t) acc[s][t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[s], b[t], acc[s][t], 0, 0, 0);
-        }
-    }
-#pragma unroll
-    for (int s = 0; s < 2; ++s)
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int64_t i = i0 + wi + s * 32 + r / 4 * 8 + lane / 32 * 4 + r % 4, j = j0 + wj + t * 32 + lane % 32;
-                if (i < P.rows && j < Q.rows) ((typename element<OTYPE>::raw *)out)[j * stride + i] = element<OTYPE>::from_float(acc[s][t][r]);
-            }
-}
+// ---- the gate by itself ----
 
-operand plain(const void *p, int64_t stride, int64_t rows, int64_t depth) { return {(const uint8_t *)p, nullptr, stride, 0, rows, depth}; }
-operand packed(const uint8_t *codes, const uint8_t *scales, int64_t cols, int64_t rows, int64_t depth)
-{
-    return {codes, scales, cols, groups_of(cols), rows, depth};
-}
-
-template <int PHOW, bool PPACKED, int QHOW, bool QPACKED, int OTYPE>
-int product(const operand &P, const operand &Q, void *out, int64_t stride, hipStream_t st)
-{
-    const int64_t across = (P.rows + TILE - 1) / TILE;
-    for (int64_t j0 = 0; j0 < Q.rows; j0 += (int64_t)65535 * TILE) {       // a launch's second dimension ends at 65535
-        operand part = Q;
-        part.rows = Q.rows - j0 < (int64_t)65535 * TILE ? Q.rows - j0 : (int64_t)65535 * TILE;
-        part.data += QHOW == ALONG ? j0 * Q.stride * (QPACKED ? 1 : 2) : j0 * (QPACKED ? 1 : 2);
-        if (QPACKED) part.scales += QHOW == ALONG ? j0 * Q.groups : j0 / GROUP;
-        hipLaunchKernelGGL((k_product<PHOW, PPACKED, QHOW, QPACKED, OTYPE>), dim3((unsigned)across, (unsigned)((part.rows + TILE - 1) / TILE)),
-                           dim3(BLOCK), 0, st, P, part, (char *)out + j0 * stride * (OTYPE == LEAP_F32 ? 4 : 2), stride);
-        const int rc = launched();
-        if (rc != LEAP_OK) return rc;
-    }
-    return LEAP_OK;
-}
-
-// ---- the gate ----
-
-// gated, kept <- u = (g, p), [rows][2 * out] float; one chunk of `out` a lane
-__global__ __launch_bounds__(BLOCK) void k_gate(const float *__restrict__ u, int64_t rows, int64_t out, uint8_t *__restrict__ gated_codes,
-                                                uint8_t *__restrict__ gated_scales, uint8_t *__restrict__ kept_codes, uint8_t *__restrict__ kept_scales)
-{
-    const int64_t groups = groups_of(out), per_row = groups * (GROUP / CHUNK), c = (int64_t)blockIdx.x * BLOCK + threadIdx.x;
-    const int64_t row = c / per_row, col = (c - row * per_row) * CHUNK;
-    const int n = row < rows ? clip8(out - col) : 0;
-    float g[CHUNK], p[CHUNK], a[CHUNK];
-    load8<LEAP_F32>(u, row * 2 * out + col, n, g);
-    load8<LEAP_F32>(u, row * 2 * out + out + col, n, p);
-#pragma unroll
-    for (int i = 0; i < CHUNK; ++i) a[i] = g[i] * sigmoid(g[i]) * p[i];
-    pack_chunk(a, n, gated_codes, gated_scales, row, out, groups, col);
-    if (kept_codes) {
-        pack_chunk(g, n, kept_codes, kept_scales, 2 * row, out, groups, col);
-        pack_chunk(p, n, kept_codes, kept_scales, 2 * row + 1, out, groups, col);
-    }
-}
-
-template <int TYPE>
+// du <- da and what is kept; one chunk of `out` a lane
 __global__ __launch_bounds__(BLOCK) void k_gate_grad(const void *__restrict__ da, int64_t stride, const uint8_t *__restrict__ kept_codes,
                                                      const uint8_t *__restrict__ kept_scales, int64_t rows, int64_t out, void *__restrict__ du)
 {
     const int64_t groups = groups_of(out), per_row = groups * (GROUP / CHUNK), c = (int64_t)blockIdx.x * BLOCK + threadIdx.x;
     const int64_t row = c / per_row, col = (c - row * per_row) * CHUNK;
-    const int n = row < rows ? clip8(out - col) : 0;
+    const int n = row < rows ? (out - col < CHUNK ? (int)(out - col) : CHUNK) : 0;
     if (n <= 0) return;
     float d[CHUNK], g[CHUNK], p[CHUNK], dg[CHUNK], dp[CHUNK];
-    load8<TYPE>(da, row * stride + col, n, d);
+    load8<LEAP_BF16>(da, row * stride + col, n, d);
     decode8(load_codes(kept_codes + 2 * row * out + col, n), scale_value(kept_scales[2 * row * groups + col / GROUP]), g);
     decode8(load_codes(kept_codes + (2 * row + 1) * out + col, n), scale_value(kept_scales[(2 * row + 1) * groups + col / GROUP]), p);
 #pragma unroll
@@ -163,13 +151,6 @@ __global__ __launch_bounds__(BLOCK) void k_gate_grad(const void *__restrict__ da
     store8<LEAP_BF16>(du, row * 2 * out + out + col, n, dp);
 }
 
-// Blocks of the gate's kernels; 0: more than a launch holds.
-unsigned gate_blocks(int64_t rows, int64_t out)
-{
-    const int64_t blocks = (rows * groups_of(out) * (GROUP / CHUNK) + BLOCK - 1) / BLOCK;
-    return blocks <= 0x7fffffff ? (unsigned)blocks : 0u;
-}
-
 const char *bad_product(int64_t rows, int64_t cols, int64_t w_stride, int64_t out)
 {
     if (const char *why = bad_sizes(rows, cols)) return why;
@@ -177,22 +158,40 @@ const char *bad_product(int64_t rows, int64_t cols, int64_t w_stride, int64_t ou
     return bad_stride(w_stride, out, cols);
 }
 
+constexpr const char *GATED_LIMIT = "more than 2^19 gated columns";
+
 }  // namespace
 
+extern "C" int64_t leap_linear8_work(const uint8_t *d_codes, int64_t rows, int64_t cols, const void *d_weight, int64_t w_stride, int64_t out)
+{
+    if (bad_product(rows, cols, w_stride, out)) return 0;
+    return laid(d_codes, cols, rows, cols, 1).room() + laid(d_weight, w_stride, out, cols, 2).room();
+}
+
 extern "C" int leap_linear8(const uint8_t *d_codes, const uint8_t *d_scales, int64_t rows, int64_t cols, const void *d_weight, int64_t w_stride,
-                            int64_t out, void *d_y, void *hip_stream)
+                            int64_t out, void *d_y, void *d_work, void *hip_stream)
 {
     if (const char *why = bad_product(rows, cols, w_stride, out)) return refuse(why);
     if (!rows) return LEAP_OK;
     if (!d_codes || !d_scales || !d_weight || !d_y) return refuse("null data pointer");
-    return product<ALONG, false, ALONG, true, LEAP_BF16>(plain(d_weight, w_stride, out, cols), packed(d_codes, d_scales, cols, rows, cols), d_y, out,
-                                                         stream_of(hip_stream));
+    if (!d_work && leap_linear8_work(d_codes, rows, cols, d_weight, w_stride, out)) return refuse("null workspace");
+    const hipStream_t st = stream_of(hip_stream);
+    uint8_t *room = (uint8_t *)d_work;
+    laid W(d_weight, w_stride, out, cols, 2), X(d_codes, cols, rows, cols, 1);
+    int rc = W.lay_out(room, st);
+    if (rc == LEAP_OK) rc = X.lay_out(room, st);
+    if (rc != LEAP_OK) return rc;
+    result R{};
+    R.out = d_y, R.stride = out;
+    return product<WIDE_ALONG, CODES_ALONG, TO_WIDE>(W.wide(out, cols), X.codes(d_scales, cols, rows, cols), R, st);
 }
 
-extern "C" int64_t leap_linear8_work(int64_t rows, int64_t cols, int64_t out)
+extern "C" int64_t leap_linear8_backward_work(const void *d_dy, int64_t dy_stride, const uint8_t *d_codes, int64_t rows, int64_t cols, const void *d_weight,
+                                              int64_t w_stride, int64_t out)
 {
-    (void)rows, (void)cols, (void)out;
-    return 0;
+    if (bad_product(rows, cols, w_stride, out) || bad_stride(dy_stride, rows, out)) return 0;
+    return weight_plan(rows, cols, out).room(cols, out) + laid(d_dy, dy_stride, rows, out, 2).room() + laid(d_codes, cols, rows, cols, 1).room() +
+           laid(d_weight, w_stride, out, cols, 2).room();
 }
 
 extern "C" int leap_linear8_backward(const void *d_dy, int64_t dy_stride, const uint8_t *d_codes, const uint8_t *d_scales, int64_t rows, int64_t cols,
@@ -203,82 +202,100 @@ extern "C" int leap_linear8_backward(const void *d_dy, int64_t dy_stride, const 
     if (const char *why = bad_stride(dy_stride, rows, out)) return refuse(why);
     if (grad_x_type != LEAP_BF16 && grad_x_type != LEAP_F32) return refuse("grad_x is bfloat16 or float32");
     if (rows && (!d_dy || !d_codes || !d_scales || !d_weight)) return refuse("null data pointer");
-    if (!d_work && leap_linear8_work(rows, cols, out)) return refuse("null workspace");
+    if (!d_work && leap_linear8_backward_work(d_dy, dy_stride, d_codes, rows, cols, d_weight, w_stride, out)) return refuse("null workspace");
     const hipStream_t st = stream_of(hip_stream);
-    int rc = LEAP_OK;
-    if (d_grad_x && rows) {
-        const operand W = plain(d_weight, w_stride, cols, out), G = plain(d_dy, dy_stride, rows, out);
-        rc = grad_x_type == LEAP_F32 ? product<ACROSS, false, ALONG, false, LEAP_F32>(W, G, d_grad_x, cols, st)
-                                     : product<ACROSS, false, ALONG, false, LEAP_BF16>(W, G, d_grad_x, cols, st);
+    uint8_t *room = (uint8_t *)d_work;
+    laid G(d_dy, dy_stride, rows, out, 2);
+    int rc = G.lay_out(room, st);
+    if (rc == LEAP_OK && d_grad_x && rows) {
+        laid W(d_weight, w_stride, out, cols, 2);
+        rc = W.lay_out(room, st);
+        if (rc != LEAP_OK) return rc;
+        result R{};
+        R.out = d_grad_x, R.stride = cols;
+        const operand P = W.wide(cols, out), Q = G.wide(rows, out);
+        rc = grad_x_type == LEAP_F32 ? product<WIDE_ACROSS, WIDE_ALONG, TO_FULL>(P, Q, R, st) : product<WIDE_ACROSS, WIDE_ALONG, TO_WIDE>(P, Q, R, st);
     }
     if (rc != LEAP_OK || !d_grad_weight) return rc;
-    return product<ACROSS, true, ACROSS, false, LEAP_BF16>(packed(d_codes, d_scales, cols, cols, rows), plain(d_dy, dy_stride, out, rows), d_grad_weight,
-                                                           cols, st);
-}
-
-extern "C" int64_t leap_gated_linear8_work(int64_t rows, int64_t cols, int64_t out)
-{
-    return bad_product(rows, cols, cols, out) ? 0 : rows * 2 * out * (int64_t)sizeof(float);
+    laid X(d_codes, cols, rows, cols, 1);
+    rc = X.lay_out(room, st);
+    if (rc != LEAP_OK) return rc;
+    const weight_plan plan(rows, cols, out);
+    const operand P = X.codes(d_scales, cols, cols, rows), Q = G.wide(out, rows);
+    result R{};
+    R.stride = cols, R.part = cols * out;
+    if (plan.parts == 1) {
+        R.out = d_grad_weight;
+        return plan.large ? launch<CODES_ACROSS, WIDE_ACROSS, TO_WIDE, 256, 256, 2, 4>(P, Q, R, 0, st)
+                          : launch<CODES_ACROSS, WIDE_ACROSS, TO_WIDE, 128, 128, 2, 2>(P, Q, R, 0, st);
+    }
+    R.out = room;
+    rc = plan.large ? launch<CODES_ACROSS, WIDE_ACROSS, TO_FULL, 256, 256, 2, 4>(P, Q, R, plan.depth_part, st)
+                    : launch<CODES_ACROSS, WIDE_ACROSS, TO_FULL, 128, 128, 2, 2>(P, Q, R, plan.depth_part, st);
+    if (rc != LEAP_OK) return rc;
+    hipLaunchKernelGGL(k_add_parts, dim3((unsigned)cut(cols * out, 4 * BLOCK)), dim3(BLOCK), 0, st, (const float *)room, plan.parts, cols * out,
+                       (uint16_t *)d_grad_weight);
+    return launched();
 }
 
 extern "C" int leap_gated_linear8(const uint8_t *d_codes, const uint8_t *d_scales, int64_t rows, int64_t cols, const void *d_weight, int64_t w_stride,
                                   int64_t out, uint8_t *d_gated_codes, uint8_t *d_gated_scales, uint8_t *d_kept_codes, uint8_t *d_kept_scales,
                                   void *d_work, void *hip_stream)
 {
-    if (out > MOST_COLS / 2) return refuse("more than 2^19 gated columns");
+    if (out > MOST_COLS / 2) return refuse(GATED_LIMIT);
     if (const char *why = bad_product(rows, cols, w_stride, 2 * out)) return refuse(why);
     if (!rows) return LEAP_OK;
-    if (!d_codes || !d_scales || !d_weight || !d_gated_codes || !d_gated_scales || !d_work) return refuse("null data pointer");
+    if (!d_codes || !d_scales || !d_weight || !d_gated_codes || !d_gated_scales) return refuse("null data pointer");
     if (!d_kept_codes != !d_kept_scales) return refuse("kept codes and scales: both or neither");
-    const unsigned blocks = gate_blocks(rows, out);
-    if (!blocks) return refuse("more values than one launch covers");
+    if (!d_work && leap_linear8_work(d_codes, rows, cols, d_weight, w_stride, 2 * out)) return refuse("null workspace");
     const hipStream_t st = stream_of(hip_stream);
-    const int rc = product<ALONG, false, ALONG, true, LEAP_F32>(plain(d_weight, w_stride, 2 * out, cols), packed(d_codes, d_scales, cols, rows, cols),
-                                                                d_work, 2 * out, st);
+    uint8_t *room = (uint8_t *)d_work;
+    laid W(d_weight, w_stride, 2 * out, cols, 2), X(d_codes, cols, rows, cols, 1);
+    int rc = W.lay_out(room, st);
+    if (rc == LEAP_OK) rc = X.lay_out(room, st);
     if (rc != LEAP_OK) return rc;
-    hipLaunchKernelGGL(k_gate, dim3(blocks), dim3(BLOCK), 0, st, (const float *)d_work, rows, out, d_gated_codes, d_gated_scales, d_kept_codes, d_kept_scales);
-    return launched();
+    result R{};
+    R.columns = out, R.gated_codes = d_gated_codes, R.gated_scales = d_gated_scales, R.kept_codes = d_kept_codes, R.kept_scales = d_kept_scales;
+    return product<WIDE_ALONG, CODES_ALONG, TO_GATED>(W.wide(2 * out, cols), X.codes(d_scales, cols, rows, cols), R, st);
 }
-
-namespace {
-
-template <int TYPE> int gate_backward(const void *da, int64_t stride, const uint8_t *codes, const uint8_t *scales, int64_t rows, int64_t out, void *du, hipStream_t st)
-{
-    const unsigned blocks = gate_blocks(rows, out);
-    if (!blocks) return refuse("more values than one launch covers");
-    hipLaunchKernelGGL((k_gate_grad<TYPE>), dim3(blocks), dim3(BLOCK), 0, st, da, stride, codes, scales, rows, out, du);
-    return launched();
-}
-
-}  // namespace
 
 extern "C" int leap_gate8_backward(const void *d_da, int64_t da_stride, const uint8_t *d_kept_codes, const uint8_t *d_kept_scales, int64_t rows,
                                    int64_t out, void *d_du, void *hip_stream)
 {
-    if (out > MOST_COLS / 2) return refuse("more than 2^19 gated columns");
+    if (out > MOST_COLS / 2) return refuse(GATED_LIMIT);
     if (const char *why = bad_sizes(rows, out)) return refuse(why);
     if (const char *why = bad_stride(da_stride, rows, out)) return refuse(why);
     if (!rows) return LEAP_OK;
     if (!d_da || !d_kept_codes || !d_kept_scales || !d_du) return refuse("null data pointer");
-    return gate_backward<LEAP_BF16>(d_da, da_stride, d_kept_codes, d_kept_scales, rows, out, d_du, stream_of(hip_stream));
+    const int64_t blocks = cut(rows * groups_of(out) * (GROUP / CHUNK), BLOCK);
+    if (blocks > 0x7fffffff) return refuse("more values than one launch covers");
+    hipLaunchKernelGGL(k_gate_grad, dim3((unsigned)blocks), dim3(BLOCK), 0, stream_of(hip_stream), d_da, da_stride, d_kept_codes, d_kept_scales, rows, out, d_du);
+    return launched();
 }
 
-extern "C" int64_t leap_linear_gate8_work(int64_t rows, int64_t out, int64_t next)
+extern "C" int64_t leap_linear_gate8_work(const void *d_dy, int64_t dy_stride, const void *d_weight, int64_t w_stride, int64_t next, int64_t rows, int64_t out)
 {
-    return bad_product(rows, next, next, out) ? 0 : rows * out * (int64_t)sizeof(float);
+    if (bad_product(rows, out, w_stride, next) || bad_stride(dy_stride, rows, next)) return 0;
+    return laid(d_dy, dy_stride, rows, next, 2).room() + laid(d_weight, w_stride, next, out, 2).room();
 }
 
 extern "C" int leap_linear_gate8_backward(const void *d_dy, int64_t dy_stride, const void *d_weight, int64_t w_stride, int64_t next,
                                           const uint8_t *d_kept_codes, const uint8_t *d_kept_scales, int64_t rows, int64_t out, void *d_du,
                                           void *d_work, void *hip_stream)
 {
-    if (out > MOST_COLS / 2) return refuse("more than 2^19 gated columns");
+    if (out > MOST_COLS / 2) return refuse(GATED_LIMIT);
     if (const char *why = bad_product(rows, out, w_stride, next)) return refuse(why);
     if (const char *why = bad_stride(dy_stride, rows, next)) return refuse(why);
     if (!rows) return LEAP_OK;
-    if (!d_dy || !d_weight || !d_kept_codes || !d_kept_scales || !d_du || !d_work) return refuse("null data pointer");
+    if (!d_dy || !d_weight || !d_kept_codes || !d_kept_scales || !d_du) return refuse("null data pointer");
+    if (!d_work && leap_linear_gate8_work(d_dy, dy_stride, d_weight, w_stride, next, rows, out)) return refuse("null workspace");
     const hipStream_t st = stream_of(hip_stream);
-    const int rc = product<ACROSS, false, ALONG, false, LEAP_F32>(plain(d_weight, w_stride, out, next), plain(d_dy, dy_stride, rows, next), d_work, out, st);
+    uint8_t *room = (uint8_t *)d_work;
+    laid W(d_weight, w_stride, next, out, 2), G(d_dy, dy_stride, rows, next, 2);
+    int rc = W.lay_out(room, st);
+    if (rc == LEAP_OK) rc = G.lay_out(room, st);
     if (rc != LEAP_OK) return rc;
-    return gate_backward<LEAP_F32>(d_work, out, d_kept_codes, d_kept_scales, rows, out, d_du, st);
+    result R{};
+    R.out = d_du, R.columns = out, R.kept_codes = (uint8_t *)d_kept_codes, R.kept_scales = (uint8_t *)d_kept_scales;
+    return product<WIDE_ACROSS, WIDE_ALONG, TO_GATE_GRAD>(W.wide(out, next), G.wide(rows, next), R, st);
 }

@@ -42,7 +42,7 @@ P = 0x1000
      [(4, 3), (6, 2), (6, 5), (7, -4), (8, 0), (1, 63), (3, 63), (9, -1.0), (9, float("nan")), (0, 0), (5, 0), (11, 0), (12, 0), (13, 0), (14, 0), (7, 1 << 32)]),
     ("leap_rms_norm8_backward", (P, 1, 64, P, 64, 1, P, P, P, P, 1, 4, 64, P, P, P, 0),
      [(1, 2), (5, 8), (10, 2), (2, 1), (4, 1), (11, -1), (12, 0), (0, 0), (6, 0), (7, 0), (8, 0), (9, 0), (13, 0), (15, 0), (11, 1 << 32)]),
-    ("leap_linear8", (P, P, 4, 64, P, 64, 8, P, 0), [(2, -1), (3, 0), (5, 63), (6, 0), (0, 0), (1, 0), (4, 0), (7, 0), (6, 1 << 21)]),
+    ("leap_linear8", (P, P, 4, 64, P, 64, 8, P, P, 0), [(2, -1), (3, 0), (5, 63), (6, 0), (0, 0), (1, 0), (4, 0), (7, 0), (6, 1 << 21)]),
     ("leap_linear8_backward", (P, 8, P, P, 4, 64, P, 64, 8, P, 1, P, P, 0), [(1, 7), (4, -1), (5, 0), (7, 1), (8, 0), (10, 2), (0, 0), (2, 0), (3, 0), (6, 0)]),
     ("leap_gated_linear8", (P, P, 4, 64, P, 64, 8, P, P, P, P, P, 0), [(2, -1), (3, 0), (5, 63), (6, 0), (6, 1 << 20), (0, 0), (1, 0), (4, 0), (7, 0), (8, 0), (9, 0), (10, 0)]),
     ("leap_gate8_backward", (P, 8, P, P, 4, 8, P, 0), [(1, 7), (4, -1), (5, 0), (5, 1 << 20), (0, 0), (2, 0), (3, 0), (6, 0)]),
@@ -60,13 +60,30 @@ def test_no_rows_is_fine(lib):
     assert lib.leap_pack8(None, 0, 64, 0, 64, None, None, None) == B.LEAP_OK
     assert lib.leap_unpack8(None, None, 0, 64, None, 0, None) == B.LEAP_OK
     assert lib.leap_rms_norm8(None, 64, None, 0, 1, None, 1, 0, 64, 1e-6, *[None] * 7) == B.LEAP_OK
-    assert lib.leap_linear8(None, None, 0, 64, None, 64, 8, None, None) == B.LEAP_OK
+    assert lib.leap_linear8(None, None, 0, 64, None, 64, 8, None, None, None) == B.LEAP_OK
     assert lib.leap_gate8_backward(None, 8, None, None, 0, 8, None, None) == B.LEAP_OK
 
 
 def test_workspaces_of_bad_sizes_are_nothing(lib):
     assert lib.leap_rms_norm8_work(-1, 64) == 0 and lib.leap_rms_norm8_work(5, 0) == 0
-    assert lib.leap_linear8_work(-1, 64, 8) == 0 and lib.leap_gated_linear8_work(4, 0, 8) == 0 and lib.leap_linear_gate8_work(4, 8, -1) == 0
+    assert lib.leap_linear8_work(P, -1, 64, P, 64, 8) == 0 and lib.leap_linear8_backward_work(P, 8, P, 4, 0, P, 64, 8) == 0
+    assert lib.leap_linear_gate8_work(P, 8, P, 16, 8, 4, -1) == 0
+
+
+def test_workspaces_hold_copies_of_what_is_not_laid_out(lib):
+    """Codes of 40 columns in rows of 48, weights of 40 in rows of 40 values; addresses and strides that are no multiple of 16 bytes."""
+    assert lib.leap_linear8_work(P, 5, 64, P, 64, 8) == 0
+    assert lib.leap_linear8_work(P, 5, 40, P, 40, 8) == 5 * 48
+    assert lib.leap_linear8_work(P + 1, 5, 64, P, 64, 8) == 5 * 64
+    assert lib.leap_linear8_work(P, 5, 64, P, 65, 8) == 8 * 64 * 2
+    assert lib.leap_linear8_work(P, 5, 63, P, 64, 8) == 5 * 64 + 8 * 64 * 2
+    assert lib.leap_linear8_backward_work(P, 8, P, 5, 64, P, 64, 8) == 0
+    assert lib.leap_linear8_backward_work(P, 9, P, 5, 64, P, 64, 9) == 5 * 16 * 2
+    assert lib.leap_linear_gate8_work(P + 2, 8, P, 16, 8, 4, 16) == 4 * 8 * 2
+    # a missing workspace is refused where one is needed
+    assert lib.leap_linear8(P, P, 5, 40, P, 40, 8, P, None, None) == B.LEAP_INVALID_ARG
+    assert lib.leap_linear8_backward(P, 9, P, P, 5, 64, P, 64, 9, P, 1, P, None, None) == B.LEAP_INVALID_ARG
+    assert lib.leap_linear_gate8_backward(P, 9, P, 16, 9, P, P, 4, 16, P, None, None) == B.LEAP_INVALID_ARG
 
 
 def _packed(rows, cols):
