@@ -165,7 +165,13 @@ __device__ inline void pack_chunk(const float (&v)[CHUNK], int n, uint8_t *codes
     }
 }
 
-__device__ inline float sigmoid(float g) { return 1.0f / (1.0f + __expf(-g)); }
+// 1 / (1 + exp(-g)) within a few units of the last place: 2^-32 (1 + exp(-g)) does not overflow before the result is zero, and
+// its reciprocal, which the hardware forms within a unit but not as a subnormal number, is brought back by a product.
+__device__ inline float sigmoid(float g)
+{
+    const float scaled = __builtin_amdgcn_exp2f(__builtin_fmaf(g, -1.44269504f, -32.0f)) + 0x1p-32f;
+    return __builtin_amdgcn_rcpf(scaled) * 0x1p-32f;
+}
 
 // ---- division of 32-bit numbers by one that a launch knows ----
 

@@ -69,23 +69,38 @@ struct laid {
 
 int64_t cut(int64_t n, int64_t by) { return (n + by - 1) / by; }
 
-// Tiles of 256 x 256 where they fill the 256 compute units, else of 128 x 128.
-bool large_tiles(int64_t i, int64_t j, int64_t parts = 1) { return cut(i, 256) * cut(j, 256) * parts >= 200; }
+// Tiles of 256 x 256, eight waves and a block a compute unit; or of 128 x 128, four waves and two blocks, at 0.8 of the rate (262144 x
+// 512 -> 1024, y: 339 and 411 us) but with less left over where tiles are few.  In units of the time of a large tile, 256 units
+// taking tiles at once:
+bool large_tiles(int64_t i, int64_t j)
+{
+    return (double)cut(cut(i, 256) * cut(j, 256), 256) <= 0.62 * (double)cut(cut(i, 128) * cut(j, 128), 512);
+}
 
-template <int PKIND, int QKIND, int TO, int TI, int TJ, int WI, int WJ>
+template <int PKIND, int QKIND, int TO, int TI, int TJ, int WI, int WJ, int STEP>
 int launch(const operand &P, const operand &Q, const result &R, int64_t depth_part, hipStream_t st)
 {
     const int64_t across = TO == TO_GATED ? cut(R.columns, TI / 2) : cut(P.rows, TI), along = cut(Q.rows, TJ), parts = depth_part ? cut(P.depth, depth_part) : 1;
     if (across * along * parts > 0x7fffffff) return refuse("more rows and columns than one launch covers");
-    hipLaunchKernelGGL((k_product<PKIND, QKIND, TO, TI, TJ, WI, WJ>), dim3((unsigned)(across * along * parts)), dim3(WI * WJ * 64), 0, st, P, Q, R,
-                       (uint32_t)across, (uint32_t)along, depth_part ? depth_part : P.depth);
+    // as many blocks as the 256 compute units hold at once, by shared memory and registers
+    constexpr int RESIDENT = WI * WJ > 4 ? 1 : 2;
+    const int64_t blocks = !stays<TO>() || across * along * parts < 256 * RESIDENT ? across * along * parts : 256 * RESIDENT;
+    hipLaunchKernelGGL((k_product<PKIND, QKIND, TO, TI, TJ, WI, WJ, STEP>), dim3((unsigned)blocks), dim3(WI * WJ * 64), 0, st, P, Q, R, (uint32_t)across,
+                       (uint32_t)along, (uint32_t)parts, depth_part ? depth_part : P.depth);
     return launched();
+}
+
+template <int PKIND, int QKIND, int TO> int product(const operand &P, const operand &Q, const result &R, int64_t depth_part, bool large, hipStream_t st)
+{
+    // the gate's gradient moves more than it multiplies: small tiles always (262144 x 512 -> 2 * 512: 300 us, large ones 369)
+    if constexpr (TO != TO_GATE_GRAD)
+        if (large) return launch<PKIND, QKIND, TO, 256, 256, 2, 4, 64>(P, Q, R, depth_part, st);
+    return launch<PKIND, QKIND, TO, 128, 128, 2, 2, 64>(P, Q, R, depth_part, st);
 }
 
 template <int PKIND, int QKIND, int TO> int product(const operand &P, const operand &Q, const result &R, hipStream_t st)
 {
-    if (large_tiles(P.rows, Q.rows)) return launch<PKIND, QKIND, TO, 256, 256, 2, 4>(P, Q, R, 0, st);
-    return launch<PKIND, QKIND, TO, 128, 128, 2, 2>(P, Q, R, 0, st);
+    return product<PKIND, QKIND, TO>(P, Q, R, 0, large_tiles(P.rows, Q.rows), st);
 }
 
 // grad_weight: few tiles, many rows to sum over.  The rows are cut into parts, as many as give every compute unit a tile,
@@ -101,8 +116,8 @@ struct weight_plan {
         parts = want < 1 ? 1 : want;
         if (parts > cut(rows, 512)) parts = cut(rows, 512);
         if (parts < 1) parts = 1;
-        depth_part = cut(cut(rows, parts), STEP) * STEP;
-        if (depth_part < STEP) depth_part = STEP;
+        depth_part = cut(cut(rows, parts), 64) * 64;
+        if (depth_part < 64) depth_part = 64;
         parts = rows ? cut(rows, depth_part) : 1;
     }
     int64_t room(int64_t cols, int64_t out) const { return parts > 1 ? up16(parts * cols * out * (int64_t)sizeof(float)) : 0; }
@@ -217,6 +232,11 @@ extern "C" int leap_linear8_backward(const void *d_dy, int64_t dy_stride, const 
         rc = grad_x_type == LEAP_F32 ? product<WIDE_ACROSS, WIDE_ALONG, TO_FULL>(P, Q, R, st) : product<WIDE_ACROSS, WIDE_ALONG, TO_WIDE>(P, Q, R, st);
     }
     if (rc != LEAP_OK || !d_grad_weight) return rc;
+    const dim3 adders((unsigned)cut(cols * out, 4 * BLOCK));
+    if (!rows) {                                     // a sum of nothing
+        hipLaunchKernelGGL(k_add_parts, adders, dim3(BLOCK), 0, st, (const float *)nullptr, (int64_t)0, cols * out, (uint16_t *)d_grad_weight);
+        return launched();
+    }
     laid X(d_codes, cols, rows, cols, 1);
     rc = X.lay_out(room, st);
     if (rc != LEAP_OK) return rc;
@@ -226,14 +246,12 @@ extern "C" int leap_linear8_backward(const void *d_dy, int64_t dy_stride, const 
     R.stride = cols, R.part = cols * out;
     if (plan.parts == 1) {
         R.out = d_grad_weight;
-        return plan.large ? launch<CODES_ACROSS, WIDE_ACROSS, TO_WIDE, 256, 256, 2, 4>(P, Q, R, 0, st)
-                          : launch<CODES_ACROSS, WIDE_ACROSS, TO_WIDE, 128, 128, 2, 2>(P, Q, R, 0, st);
+        return product<CODES_ACROSS, WIDE_ACROSS, TO_WIDE>(P, Q, R, 0, plan.large, st);
     }
     R.out = room;
-    rc = plan.large ? launch<CODES_ACROSS, WIDE_ACROSS, TO_FULL, 256, 256, 2, 4>(P, Q, R, plan.depth_part, st)
-                    : launch<CODES_ACROSS, WIDE_ACROSS, TO_FULL, 128, 128, 2, 2>(P, Q, R, plan.depth_part, st);
+    rc = product<CODES_ACROSS, WIDE_ACROSS, TO_FULL>(P, Q, R, plan.depth_part, plan.large, st);
     if (rc != LEAP_OK) return rc;
-    hipLaunchKernelGGL(k_add_parts, dim3((unsigned)cut(cols * out, 4 * BLOCK)), dim3(BLOCK), 0, st, (const float *)room, plan.parts, cols * out,
+    hipLaunchKernelGGL(k_add_parts, adders, dim3(BLOCK), 0, st, (const float *)room, plan.parts, cols * out,
                        (uint16_t *)d_grad_weight);
     return launched();
 }

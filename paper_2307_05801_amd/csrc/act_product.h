@@ -1,6 +1,6 @@
 // The tiled product behind leap_linear8 and its kin: D[j][i] = sum over k of P(i, k) Q(j, k).
 //
-// A block owns TI x TJ of D and walks over k in steps of 64; a step's tiles of P and Q are fetched into shared memory (mostly
+// A block owns TI x TJ of D and walks over k in steps of 64 or 32; a step's tiles of P and Q are fetched into shared memory (mostly
 // straight from memory, past the registers) while the step before is multiplied: two buffers, one barrier a step.  i runs along a lane's
 // registers and j across lanes, so a lane ends with runs of neighbouring i: what a row of an output, and a group of 32 that
 // shares a scale, is made of.
@@ -22,7 +22,6 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 typedef __attribute__((address_space(3))) uint8_t lds_byte;
 
-constexpr int STEP = 64;                   // values of k a step
 constexpr uint32_t NOWHERE = 0x80000000u;  // an offset beyond every buffer: reads as zeros
 
 // How an operand lies in memory: rows of bfloat16 along k; rows of k; codes along k; rows of k of codes.
@@ -36,14 +35,27 @@ struct operand {
     int64_t rows, depth;
 };
 
-// The first `bytes` from `base` on: reads beyond them give zeros.
-__device__ inline u32x4 buffer(const uint8_t *base, int64_t bytes)
-{
-    const uint64_t at = (uint64_t)base;
-    const auto uniform = [](uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)v); };        // it is; the compiler has to see it
-    return u32x4{uniform((uint32_t)at), uniform((uint32_t)(at >> 32) & 0xffffu),
-                 uniform(bytes <= 0 ? 0u : bytes < 0x7ffffff0 ? (uint32_t)bytes : 0x7ffffff0u), 0x00020000u};
-}
+// What of an operand lies from the current k on: a buffer that moves along it, and ends where the operand does (reads beyond
+// give zeros).
+struct window {
+    const uint8_t *base;
+    int64_t left;              // bytes
+    uint32_t step;             // bytes from one step to the next
+
+    __device__ inline u32x4 buffer() const
+    {
+        const uint64_t at = (uint64_t)base;
+        const auto uniform = [](uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)v); };    // it is; the compiler has to see it
+        return u32x4{uniform((uint32_t)at), uniform((uint32_t)(at >> 32) & 0xffffu),
+                     uniform(left <= 0 ? 0u : left < 0x7ffffff0 ? (uint32_t)left : 0x7ffffff0u), 0x00020000u};
+    }
+    // The same for the compiler's own loads.
+    __device__ inline __amdgpu_buffer_rsrc_t resource() const
+    {
+        return __builtin_amdgcn_make_buffer_rsrc((void *)base, 0, left <= 0 ? 0 : left < 0x7ffffff0 ? (int)left : 0x7ffffff0, 0x00020000);
+    }
+    __device__ inline void advance() { base += step, left -= step; }
+};
 
 // n in whole pieces of 16 bytes: a fetch that ends inside a word reads nothing of it.
 __device__ inline int64_t whole(int64_t n, int piece) { return (n + piece - 1) / piece * piece; }
@@ -56,46 +68,80 @@ __device__ inline void fetch16(const u32x4 &from, uint32_t offset, lds_byte *to)
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"((uint32_t)(uintptr_t)to), "v"(offset), "s"(from) : "memory");
 }
 
-// A tile of T rows of an operand in shared memory, by KIND.  ALONG: T rows of 128 (codes: 64) bytes, their 16-byte pieces
-// in an order that spreads 16 neighbouring rows over all banks; ACROSS: 64 rows of 2 T bytes, pieces likewise spread for the
-// transposing read, which takes four of them at once.
-template <int KIND, int T, int THREADS> struct tile {
+// A tile of T rows and STEP values of k of an operand in shared memory, by KIND.  ALONG: T rows of 2 * STEP (codes: STEP)
+// bytes, their 16-byte pieces in an order that spreads 16 neighbouring rows over all banks; ACROSS: STEP rows of 2 T bytes,
+// pieces likewise spread for the transposing read, which takes four of them at once.
+template <int KIND, int T, int STEP, int THREADS> struct tile {
     static constexpr int BYTES = KIND == CODES_ALONG ? T * STEP : T * STEP * 2;
     static constexpr int WAVES = THREADS / 64, PIECES = BYTES / 1024, EACH = PIECES / WAVES;       // 1 KiB pieces: a wave's fetch
     static_assert(PIECES % WAVES == 0, "a tile is fetched by all waves alike");
+    static constexpr int VALUE = KIND == CODES_ALONG ? 1 : 2;                // bytes
+    static constexpr int ROW = STEP * VALUE, CHUNKS = ROW / 16;              // ALONG: bytes and 16-byte pieces of a row
+    static constexpr int ROWS = 1024 / ROW;                                  // and rows of a 1 KiB piece
 
-    // Starts the fetch of k0 .. k0 + 63 of rows row(0) .. ; row maps a multiple of 8 in the tile to the operand's row.
-    template <class ROW> static __device__ inline void fetch(const operand &O, int64_t k0, int wave, int lane, lds_byte *to, ROW &&row)
-    {
+    // Where piece `chunk` of row r goes (and what is found there): rows 256 / ROW apart begin in the same bank.
+    static __device__ inline int place(int r, int chunk) { return chunk ^ (r / (256 / ROW) % CHUNKS); }
+
+    // A wave's part in fetching tiles of the operand from row0 on, k after k.  HALVES 2: the tile's rows are, span by span, the
+    // same rows of two operands, `apart` bytes apart (the gate's and the other half).
+    template <int HALVES, int SPAN> struct stream {
+        uint32_t offset[EACH];
+        window at[HALVES];
+        static constexpr int half_of(int e) { return HALVES == 1 ? 0 : e * WAVES * ROWS % SPAN / (SPAN / 2); }
+        static_assert(HALVES == 1 || (KIND == WIDE_ALONG && WAVES * ROWS <= SPAN / 2), "all waves fetch of one half at a time");
+
+        __device__ inline void init(const operand &O, int wave, int lane)
+        {
 #pragma unroll
-        for (int e = 0; e < EACH; ++e) {
-            const int piece = e * WAVES + wave;
-            if constexpr (KIND == WIDE_ALONG) {
-                const int64_t r = row(piece * 8), left = ((O.rows - 1 - r) * O.stride + whole(O.depth, 8) - k0) * 2;
-                const int chunk = (lane % 8) ^ (lane / 16) ^ (piece % 2 * 4);
-                const uint32_t offset = k0 + chunk * 8 < O.depth ? (uint32_t)(lane / 8) * (uint32_t)O.stride * 2 + chunk * 16 : NOWHERE;
-                fetch16(buffer(O.data + (r * O.stride + k0) * 2, r < O.rows ? left : 0), offset, to + piece * 1024);
-            } else if constexpr (KIND == CODES_ALONG) {
-                const int64_t r = row(piece * 16), left = (O.rows - 1 - r) * O.stride + whole(O.depth, 16) - k0;
-                const int chunk = (lane % 4) ^ (lane / 16);
-                const uint32_t offset = k0 + chunk * 16 < O.depth ? (uint32_t)(lane / 4) * (uint32_t)O.stride + chunk * 16 : NOWHERE;
-                fetch16(buffer(O.data + r * O.stride + k0, r < O.rows ? left : 0), offset, to + piece * 1024);
-            } else if constexpr (KIND == WIDE_ACROSS) {
-                constexpr int DEEP = 512 / T;                                                       // rows of k in a piece
-                const int64_t k = k0 + piece * DEEP, r = row(0), left = ((O.depth - 1 - k) * O.stride + whole(O.rows, 8) - r) * 2;
-                const int in = lane / (T / 8), chunk = (lane % (T / 8)) ^ ((piece * DEEP + in) % 4 * 4);
-                fetch16(buffer(O.data + (k * O.stride + r) * 2, k < O.depth ? left : 0), (uint32_t)in * (uint32_t)O.stride * 2 + chunk * 16, to + piece * 1024);
+            for (int e = 0; e < EACH; ++e) {
+                const int piece = e * WAVES + wave;
+                if constexpr (KIND == WIDE_ACROSS) {
+                    constexpr int DEEP = 512 / T;                            // rows of k in a piece
+                    const int k = piece * DEEP + lane / (T / 8), chunk = (lane % (T / 8)) ^ (k % 4 * 4);
+                    offset[e] = (uint32_t)k * (uint32_t)O.stride * 2 + chunk * 16;
+                } else {
+                    const int r = piece * ROWS + lane / CHUNKS, row = HALVES == 1 ? r : r / SPAN * (SPAN / 2) + r % (SPAN / 2);
+                    offset[e] = (uint32_t)row * (uint32_t)O.stride * VALUE + place(r, lane % CHUNKS) * 16;
+                }
             }
         }
-    }
+
+        // Rows from row0 on, k from `first` on, of an operand that ends at `rows` and at k = `last`.
+        __device__ inline void aim(const operand &O, int64_t rows, int64_t row0, int64_t first, int64_t last, int64_t apart)
+        {
+            if constexpr (KIND == WIDE_ACROSS)
+                at[0] = {O.data + (first * O.stride + row0) * 2, ((last - 1 - first) * O.stride + whole(rows, 8) - row0) * 2, (uint32_t)(STEP * O.stride * 2)};
+            else
+                at[0] = {O.data + (row0 * O.stride + first) * VALUE, ((rows - 1 - row0) * O.stride + whole(last, 16 / VALUE) - first) * VALUE, STEP * VALUE};
+            if constexpr (HALVES == 2) at[1] = {at[0].base + apart, at[0].left, at[0].step};
+        }
+
+        // Starts the fetch of the next tile, `k` values of k from the operand's end.
+        __device__ inline void fetch(int64_t k, int wave, int lane, lds_byte *to)
+        {
+            u32x4 from[HALVES];
+#pragma unroll
+            for (int h = 0; h < HALVES; ++h) from[h] = at[h].buffer(), at[h].advance();
+            if (KIND == WIDE_ACROSS || k >= STEP) {
+#pragma unroll
+                for (int e = 0; e < EACH; ++e) fetch16(from[half_of(e)], offset[e], to + (e * WAVES + wave) * 1024);
+            } else {
+#pragma unroll
+                for (int e = 0; e < EACH; ++e) {
+                    const int chunk = place((e * WAVES + wave) * ROWS + lane / CHUNKS, lane % CHUNKS);
+                    fetch16(from[half_of(e)], chunk * (16 / VALUE) < k ? offset[e] : NOWHERE, to + (e * WAVES + wave) * 1024);
+                }
+            }
+        }
+    };
 
     // The eight values of turn s of 32-run `run` of the tile's rows first .. first + 31.
     static __device__ inline bf16x8 read(const lds_byte *from, int first, int run, int s, int lane)
     {
         const int half = lane / 32;
         if constexpr (KIND == WIDE_ALONG) {
-            const int r = first + lane % 32, chunk = (run * 4 + half * 2 + s) ^ (r / 2 % 8);
-            return *(const __attribute__((address_space(3))) bf16x8 *)(from + r * 128 + chunk * 16);
+            const int r = first + lane % 32;
+            return *(const __attribute__((address_space(3))) bf16x8 *)(from + r * ROW + place(r, run * 4 + half * 2 + s) * 16);
         } else {
             const int k = run * 32 + half * 16 + s * 8 + lane % 16 / 4, col = first + lane / 16 % 2 * 16 + lane % 4 * 4;
             const lds_byte *at = from + k * (T * 2) + ((col / 8) ^ (k % 4 * 4)) * 16 + col % 8 * 2;
@@ -108,8 +154,8 @@ template <int KIND, int T, int THREADS> struct tile {
     // Both turns from codes along k, with their scale.
     static __device__ inline void read_codes(const lds_byte *from, int first, int run, int lane, uint32_t byte, bf16x8 (&v)[2])
     {
-        const int r = first + lane % 32, chunk = (run * 2 + lane / 32) ^ (r / 4 % 4);
-        const u32x4 c = *(const __attribute__((address_space(3))) u32x4 *)(from + r * 64 + chunk * 16);
+        const int r = first + lane % 32;
+        const u32x4 c = *(const __attribute__((address_space(3))) u32x4 *)(from + r * ROW + place(r, run * 2 + lane / 32) * 16);
         const float scale = __uint_as_float(byte << 23);
 #pragma unroll
         for (int s = 0; s < 2; ++s) v[s] = widen(c[2 * s], c[2 * s + 1], scale);
@@ -124,38 +170,46 @@ template <int KIND, int T, int THREADS> struct tile {
     }
 };
 
-// Codes across k on their way through the registers: widened between fetch and store.
-template <int T, int THREADS> struct staged_codes {
-    static constexpr int EACH = T * STEP / 16 / THREADS;
-    u32x4 codes[EACH];
+// Codes across k on their way through the registers: widened between fetch and store, eight at a time.
+template <int T, int STEP, int THREADS> struct staged_codes {
+    static constexpr int EACH = T * STEP / 8 / THREADS, ROWS = THREADS / (T / 8);       // rows of k the block takes at once
+    uint2 codes[EACH];
     uint32_t byte[EACH];
+    uint32_t offset, scale_offset, stride, groups;
+    window at, scales;
 
-    __device__ inline void fetch(const operand &O, int64_t k0, int64_t row0)
+    __device__ inline void init(const operand &O)
     {
+        const uint32_t k = threadIdx.x / (T / 8), i = threadIdx.x % (T / 8) * 8;
+        stride = (uint32_t)O.stride * ROWS, groups = (uint32_t)O.groups * ROWS;
+        offset = k * (uint32_t)O.stride + i, scale_offset = k * (uint32_t)O.groups + i / GROUP;
+    }
+
+    __device__ inline void aim(const operand &O, int64_t row0, int64_t first, int64_t last)
+    {
+        at = {O.data + first * O.stride + row0, (last - 1 - first) * O.stride + whole(O.rows, 16) - row0, (uint32_t)(STEP * O.stride)};
+        scales = {O.scales + first * O.groups + row0 / GROUP, (last - first) * O.groups - row0 / GROUP, (uint32_t)(STEP * O.groups)};
+    }
+
+    __device__ inline void fetch()
+    {
+        const __amdgpu_buffer_rsrc_t from = at.resource(), with = scales.resource();
+        at.advance(), scales.advance();
 #pragma unroll
         for (int e = 0; e < EACH; ++e) {
-            const int q = e * THREADS + threadIdx.x, k = q / (T / 16);
-            const int64_t r = row0 + q % (T / 16) * 16;
-            codes[e] = u32x4{0, 0, 0, 0};
-            byte[e] = 0;
-            if (k0 + k < O.depth && r < O.rows) {
-                codes[e] = *(const u32x4 *)(O.data + (k0 + k) * O.stride + r);
-                byte[e] = O.scales[(k0 + k) * O.groups + r / GROUP];
-            }
+            codes[e] = __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(from, offset + e * stride, 0, 0));
+            byte[e] = __builtin_amdgcn_raw_buffer_load_b8(with, scale_offset + e * groups, 0, 0);
         }
     }
 
     __device__ inline void store(lds_byte *to) const
     {
-        using as = tile<WIDE_ACROSS, T, THREADS>;
+        using as = tile<WIDE_ACROSS, T, STEP, THREADS>;
+        const int k = threadIdx.x / (T / 8), chunk = threadIdx.x % (T / 8);
 #pragma unroll
-        for (int e = 0; e < EACH; ++e) {
-            const int q = e * THREADS + threadIdx.x, k = q / (T / 16), chunk = (q % (T / 16) * 2) ^ (k % 4 * 4);
-            const float scale = __uint_as_float(byte[e] << 23);
-            lds_byte *at = to + k * (T * 2) + chunk * 16;
-            *(__attribute__((address_space(3))) bf16x8 *)at = as::widen(codes[e][0], codes[e][1], scale);
-            *(__attribute__((address_space(3))) bf16x8 *)(at + 16) = as::widen(codes[e][2], codes[e][3], scale);
-        }
+        for (int e = 0; e < EACH; ++e)
+            *(__attribute__((address_space(3))) bf16x8 *)(to + (k + e * ROWS) * (T * 2) + (chunk ^ ((k + e * ROWS) % 4 * 4)) * 16) =
+                as::widen(codes[e].x, codes[e].y, __uint_as_float(byte[e] << 23));
     }
 };
 
@@ -182,55 +236,139 @@ __device__ inline void split_runs(uint32_t (&run)[4])
 
 __device__ inline uint32_t two_bf16(float a, float b) { return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)a, (__bf16)b}); }
 
-// 16 neighbours of a row, `n` of them inside it, as bfloat16; v as the matrix instruction leaves it.
-__device__ inline void store_wide(uint16_t *row, int64_t i, int64_t n, int half, const f32x16 &v)
+// A wave's shared memory between its results, 32 rows (j, a lane each, twice) of which a lane holds pieces, and memory, which
+// wants runs of a row from neighbouring lanes: with a lane a row every store would touch 32 lines.  Rows of PITCH bytes whose
+// 16-byte pieces are in an order that keeps 16 lanes, of neighbouring rows or of one, in different banks.
+template <int PITCH> struct exchange {
+    static constexpr int CHUNKS = PITCH / 16, ROWS = 64 / CHUNKS, TURNS = 32 / ROWS;     // pieces a row, rows a turn of all lanes
+    lds_byte *room;
+
+    __device__ inline lds_byte *place(int row, int chunk) const
+    {
+        constexpr int A_LINE = PITCH >= 256 ? 1 : 256 / PITCH;
+        return room + row * PITCH + ((chunk ^ (row / A_LINE % CHUNKS)) * 16);
+    }
+    __device__ inline void put(int row, int chunk, const u32x4 &v) const { *(__attribute__((address_space(3))) u32x4 *)place(row, chunk) = v; }
+    __device__ inline u32x4 get(int row, int chunk) const { return *(const __attribute__((address_space(3))) u32x4 *)place(row, chunk); }
+
+    // Half a piece; the halves change places every 16 rows, for the banks' sake.
+    __device__ inline void put_half(int row, int chunk, int half, uint32_t a, uint32_t b) const
+    {
+        *(__attribute__((address_space(3))) uint64_t *)(place(row, chunk) + (half ^ (row / 16)) * 8) = (uint64_t)b << 32 | a;
+    }
+    __device__ inline u32x4 get_halves(int row, int chunk) const
+    {
+        const u32x4 v = get(row, chunk);
+        return row / 16 ? u32x4{v[2], v[3], v[0], v[1]} : v;
+    }
+    // The lanes' stores are there for its loads: a wave's accesses are carried out in order.
+    __device__ static inline void turn() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
+};
+
+// The first n of 16 bytes; SIZE bytes a value.
+template <int SIZE> __device__ inline void store_piece(uint8_t *to, int64_t n, const u32x4 &v)
 {
-    uint32_t w[4][2];
-#pragma unroll
-    for (int q = 0; q < 4; ++q) w[q][0] = two_bf16(v[4 * q], v[4 * q + 1]), w[q][1] = two_bf16(v[4 * q + 2], v[4 * q + 3]);
-    join_runs(w);
-    uint16_t *at = row + i + half * 16;
-    n -= half * 16;
     if (n >= 16) {
-        __builtin_memcpy(at, w, 32);
+        __builtin_memcpy(to, &v, 16);
     } else {
-        uint16_t e[16];
-        __builtin_memcpy(e, w, 32);
+        uint8_t b[16];
+        __builtin_memcpy(b, &v, 16);
+#pragma unroll
+        for (int x = 0; x < 16; x += SIZE)
+            if (x < n) __builtin_memcpy(to + x, b + x, SIZE);
+    }
+}
+
+__device__ inline u32x4 load_piece(const uint8_t *from, int64_t n)
+{
+    u32x4 v = {0, 0, 0, 0};
+    if (n >= 16) {
+        __builtin_memcpy(&v, from, 16);
+    } else {
+        uint8_t b[16] = {};
 #pragma unroll
         for (int x = 0; x < 15; ++x)
-            if (x < n) at[x] = e[x];
+            if (x < n) b[x] = from[x];
+        __builtin_memcpy(&v, b, 16);
     }
+    return v;
 }
 
-__device__ inline void store_full(float *row, int64_t i, int64_t n, int half, const f32x16 &v)
-{
-    float *at = row + i + half * 4;
-    n -= half * 4;
+// Rows of an array in memory from (j, i) on, `left` of them, that a wave writes (or reads) in pieces of 16 bytes.  `whole`: all its
+// columns are there, and the buffer's end keeps the rows apart that are not.
+struct landing {
+    uint8_t *base;
+    int64_t left, bytes;                   // rows; bytes of a row
+    uint32_t pitch;                        // bytes between rows
+    bool whole;
+    __amdgpu_buffer_rsrc_t buffer;
+
+    __device__ inline landing(const void *array, int64_t j, int64_t rows, int64_t pitch_, int64_t i, int64_t end, int width)
+        : base((uint8_t *)array + j * pitch_ + i), left(rows - j), bytes(end - i), pitch((uint32_t)pitch_), whole(end - i >= width)
+    {
+        const int64_t all = left * pitch_ - i;
+        buffer = __builtin_amdgcn_make_buffer_rsrc(base, 0, left <= 0 || all <= 0 ? 0 : all < 0x7ffffff0 ? (int)all : 0x7ffffff0, 0x00020000);
+    }
+    // What `room` holds, to row `first` on, byte `at` on.
+    template <int SIZE, bool HALVES, class ROOM> __device__ inline void write(const ROOM &room, int first, int at, int lane) const
+    {
+        const int row = lane / ROOM::CHUNKS, chunk = lane % ROOM::CHUNKS;
+        if (whole) {
+            const uint32_t offset = (first + row) * pitch + at + chunk * 16;
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        if (n >= 8 * q + 4) {
-            const float f[4] = {v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
-            __builtin_memcpy(at + 8 * q, f, 16);
+            for (int turn = 0; turn < ROOM::TURNS; ++turn) {
+                const int r = turn * ROOM::ROWS + row;
+                __builtin_amdgcn_raw_buffer_store_b128(HALVES ? room.get_halves(r, chunk) : room.get(r, chunk), buffer, offset + turn * ROOM::ROWS * pitch, 0, 0);
+            }
         } else {
-#pragma unroll
-            for (int x = 0; x < 3; ++x)
-                if (8 * q + x < n) at[8 * q + x] = v[4 * q + x];
+#pragma unroll 1
+            for (int turn = 0; turn < ROOM::TURNS; ++turn) {
+                const int r = turn * ROOM::ROWS + row;
+                store_piece<SIZE>(base + (int64_t)(first + r) * pitch + at + chunk * 16, first + r < left ? bytes - at - chunk * 16 : 0,
+                                  HALVES ? room.get_halves(r, chunk) : room.get(r, chunk));
+            }
         }
     }
-}
-
-// The group of 32 that two lanes hold of a row, packed; n of its values are inside the row.
-__device__ inline void pack_group(uint8_t *codes, uint8_t *scale, int64_t n, int half, const f32x16 &v)
-{
-    uint32_t amax = 0;
+    template <class ROOM> __device__ inline void read(u32x4 (&to)[ROOM::TURNS], int first, int lane) const
+    {
+        const int row = lane / ROOM::CHUNKS, chunk = lane % ROOM::CHUNKS;
+        if (whole) {
+            const uint32_t offset = (first + row) * pitch + chunk * 16;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-        const uint32_t m = 8 * (r / 4) + 4 * half + r % 4 < n ? finite_magnitude(v[r]) : 0u;
-        amax = m > amax ? m : amax;
+            for (int turn = 0; turn < ROOM::TURNS; ++turn)
+                to[turn] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(buffer, offset + turn * ROOM::ROWS * pitch, 0, 0));
+        } else {
+#pragma unroll
+            for (int turn = 0; turn < ROOM::TURNS; ++turn) {
+                const int r = first + turn * ROOM::ROWS + row;
+                to[turn] = load_piece(base + (int64_t)r * pitch + chunk * 16, r < left ? bytes - chunk * 16 : 0);
+            }
+        }
+    }
+};
+
+// The largest magnitude of the finite values among the 16 that a lane holds and the 16 of the other half's lane, as bits.
+__device__ inline uint32_t group_magnitude(const f32x16 &v)
+{
+    float most = 0.0f;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) most = __builtin_fmaxf(most, __builtin_fabsf(v[r]));       // passes over NaN
+    uint32_t amax = __float_as_uint(most);
+    if (amax >= 0x7f800000u) {                                                              // an infinity: without it
+        amax = 0;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const uint32_t m = finite_magnitude(v[r]);
+            amax = m > amax ? m : amax;
+        }
     }
     const auto other = __builtin_amdgcn_permlane32_swap(amax, amax, false, false);
-    amax = other[0] > other[1] ? other[0] : other[1];
-    const uint32_t byte = scale_byte(amax);
+    return other[0] > other[1] ? other[0] : other[1];
+}
+
+// Codes of a group of 32 that two lanes hold of a row: 16 neighbours each.
+__device__ inline u32x4 encode_group(const f32x16 &v, uint32_t byte)
+{
     const float inverse = scale_inverse(byte);
     uint32_t w[4][1];
 #pragma unroll
@@ -239,36 +377,13 @@ __device__ inline void pack_group(uint8_t *codes, uint8_t *scale, int64_t n, int
         w[q][0] = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * q + 2] * inverse, v[4 * q + 3] * inverse, lo, true);
     }
     join_runs(w);
-    if (n <= 0) return;
-    if (half == 0) *scale = (uint8_t)byte;
-    uint8_t *at = codes + half * 16;
-    n -= half * 16;
-    if (n >= 16) {
-        __builtin_memcpy(at, w, 16);
-    } else {
-        uint8_t b[16];
-        __builtin_memcpy(b, w, 16);
-#pragma unroll
-        for (int x = 0; x < 15; ++x)
-            if (x < n) at[x] = b[x];
-    }
+    return u32x4{w[0][0], w[1][0], w[2][0], w[3][0]};
 }
 
-// The values of a packed group as the matrix instruction would leave them.
-__device__ inline f32x16 unpack_group(const uint8_t *codes, uint32_t byte, int64_t n, int half)
+// And back.
+__device__ inline f32x16 decode_group(const u32x4 &codes, uint32_t byte)
 {
-    uint32_t w[4] = {};
-    const uint8_t *at = codes + half * 16;
-    n -= half * 16;
-    if (n >= 16) {
-        __builtin_memcpy(w, at, 16);
-    } else {
-        uint8_t b[16] = {};
-#pragma unroll
-        for (int x = 0; x < 15; ++x)
-            if (x < n) b[x] = at[x];
-        __builtin_memcpy(w, b, 16);
-    }
+    uint32_t w[4] = {codes[0], codes[1], codes[2], codes[3]};
     split_runs(w);
     const float scale = scale_value(byte);
     f32x16 v;
@@ -280,9 +395,35 @@ __device__ inline f32x16 unpack_group(const uint8_t *codes, uint32_t byte, int64
     return v;
 }
 
+// The scale bytes of a row's next 16 groups, a register a four: read every 512 values of k.
+struct scale_run {
+    uint32_t w[4];
+    __device__ inline void load(const uint8_t *p, int64_t n)
+    {
+        if (n >= 16) {
+            __builtin_memcpy(w, p, 16);
+        } else {
+            uint8_t b[16] = {};
+#pragma unroll
+            for (int i = 0; i < 15; ++i)
+                if (i < n) b[i] = p[i];
+            __builtin_memcpy(w, b, 16);
+        }
+    }
+    __device__ inline uint32_t byte(int i) const { return w[0] >> (8 * i) & 255u; }
+    template <int N> __device__ inline void pass()
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = __builtin_amdgcn_alignbyte(i < 3 ? w[i + 1] : 0u, w[i], N);
+    }
+};
+
 // What becomes of D: rows of bfloat16; of float (of its part of k, `part` floats apart); gate and the other half packed, and
 // their gated product; the gradient of those two from D and what is kept of them.
 enum { TO_WIDE, TO_FULL, TO_GATED, TO_GATE_GRAD };
+
+// Whether a block goes on to further tiles; where not, all of its shared memory is write()'s.
+template <int TO> constexpr bool stays() { return TO != TO_GATE_GRAD; }
 
 struct result {
     void *out;
@@ -291,146 +432,286 @@ struct result {
     uint8_t *gated_codes, *gated_scales, *kept_codes, *kept_scales;
 };
 
-// WI x WJ waves share TI x TJ of D.  Blocks: `across` tiles of i, `along` of j, parts of `depth_part` values of k.
-template <int PKIND, int QKIND, int TO, int TI, int TJ, int WI, int WJ>
-__global__ __launch_bounds__(WI * WJ * 64) void k_product(operand P, operand Q, result R, uint32_t across, uint32_t along, int64_t depth_part)
+// WI x WJ waves share TI x TJ of D.  Tiles: `across` of i, `along` of j, `parts` of depth_part values of k.  A block takes
+// tile after tile; the first step's fetch of the next one is under way while this one's results are written.
+template <int PKIND, int QKIND, int TO, int TI, int TJ, int WI, int WJ, int STEP>
+__global__ __launch_bounds__(WI * WJ * 64, WI * WJ > 4 ? 1 : 2) void k_product(operand P, operand Q, result R, uint32_t across, uint32_t along, uint32_t parts,
+                                                                               int64_t depth_part)
 {
-    constexpr int THREADS = WI * WJ * 64, FI = TI / WI / 32, FJ = TJ / WJ / 32;
+    constexpr int THREADS = WI * WJ * 64, FI = TI / WI / 32, FJ = TJ / WJ / 32, RUNS = STEP / 32;
     constexpr int PWIDE = PKIND == CODES_ACROSS ? WIDE_ACROSS : PKIND;
-    using ptile = tile<PWIDE, TI, THREADS>;
-    using qtile = tile<QKIND, TJ, THREADS>;
-    __shared__ __attribute__((aligned(1024))) uint8_t room[2][ptile::BYTES + qtile::BYTES];
+    using ptile = tile<PWIDE, TI, STEP, THREADS>;
+    using qtile = tile<QKIND, TJ, STEP, THREADS>;
+    constexpr int TILES = ptile::BYTES + qtile::BYTES, AREA = WI * WJ * FI * 2048;       // a step's; what write() takes of a buffer
+    constexpr int BUFFER = TILES > AREA ? TILES : AREA;
+    __shared__ __attribute__((aligned(1024))) uint8_t room[2 * BUFFER];
+    lds_byte *const lds = (lds_byte *)room;
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), half = lane / 32;
     const int wi = wave % WI, wj = wave / WI;
 
-    // neighbouring tiles to one of the eight dies, so that what they share comes from its cache: blocks go round the dies
-    const uint32_t all = gridDim.x, die = blockIdx.x % 8, nth = blockIdx.x / 8, share = all / 8, more = all % 8;
-    const uint32_t at = die * share + (die < more ? die : more) + nth;
-    const uint32_t part = at / (across * along), in = at % (across * along);
-    const int64_t i0 = (int64_t)(in % across) * (TO == TO_GATED ? TI / 2 : TI), j0 = (int64_t)(in / across) * TJ;
-    const int64_t first = part * depth_part, last = first + depth_part < P.depth ? first + depth_part : P.depth;
-    P.depth = Q.depth = last;
+    // Blocks go round the eight dies; each die has a run of neighbouring tiles, so that what they share comes from its cache.
+    constexpr bool STAYS = stays<TO>();
+    const uint32_t all = across * along * parts, die = blockIdx.x % 8, share = all / 8, more = all % 8;
+    const uint32_t tiles_end = (die + 1) * share + (die < more ? die + 1 : more), next = (gridDim.x - die + 7) / 8;
+    uint32_t now = die * share + (die < more ? die : more) + blockIdx.x / 8;
+    if (now >= tiles_end) return;
+    int64_t i0, j0, first, last;
+    uint32_t part;
 
-    const auto prow = [&](int r) -> int64_t {
-        if constexpr (TO != TO_GATED) return i0 + r;
-        // a wave's fragments: its columns of the gate, then the same ones of the other half; beyond the end there are no rows
-        constexpr int SPAN = TI / WI;
-        const int64_t col = i0 + r / SPAN * (SPAN / 2) + r % (SPAN / 2);
-        return col >= R.columns ? P.rows : r % SPAN < SPAN / 2 ? col : R.columns + col;
+    typename ptile::template stream<TO == TO_GATED ? 2 : 1, TI / WI> pstream;
+    typename qtile::template stream<1, TJ> qstream;
+    staged_codes<TI, STEP, THREADS> through;
+    const uint8_t *byte_at[FJ];
+    scale_run bytes[FJ];
+    if constexpr (PKIND == CODES_ACROSS) through.init(P);
+    else pstream.init(P, wave, lane);
+    qstream.init(Q, wave, lane);
+
+    const auto aim = [&] {
+        part = now / (across * along);
+        const uint32_t in = now % (across * along);
+        i0 = (int64_t)(in % across) * (TO == TO_GATED ? TI / 2 : TI), j0 = (int64_t)(in / across) * TJ;
+        first = part * depth_part, last = first + depth_part < P.depth ? first + depth_part : P.depth;
+        if constexpr (PKIND == CODES_ACROSS) through.aim(P, i0, first, last);
+        else pstream.aim(P, TO == TO_GATED ? R.columns : P.rows, i0, first, last, R.columns * P.stride * 2);
+        qstream.aim(Q, Q.rows, j0, first, last, 0);
     };
-    const auto qrow = [&](int r) -> int64_t { return j0 + r; };
-
-    lds_byte *const lds = (lds_byte *)&room[0][0];
-    const auto ptile_at = [&](int b) { return lds + b * (ptile::BYTES + qtile::BYTES); };
-    const auto qtile_at = [&](int b) { return lds + b * (ptile::BYTES + qtile::BYTES) + ptile::BYTES; };
-
-    f32x16 acc[FI][FJ] = {};
-    staged_codes<TI, THREADS> through;
-    uint32_t byte[FJ][2], byte_next[FJ][2];
-    const auto start = [&](int64_t k0, int b) {
-        if constexpr (PKIND == CODES_ACROSS) through.fetch(P, k0, i0);
-        else ptile::fetch(P, k0, wave, lane, ptile_at(b), prow);
+    // Starts the fetch of a step's tiles, k values of k from the end.
+    const auto start = [&](int64_t k, lds_byte *to) {
+        if constexpr (PKIND == CODES_ACROSS) through.fetch();
+        else pstream.fetch(k, wave, lane, to);
+        qstream.fetch(k, wave, lane, to + ptile::BYTES);
+    };
+    const auto start_scales = [&] {
         if constexpr (QKIND == CODES_ALONG) {
 #pragma unroll
-            for (int t = 0; t < FJ; ++t)
-#pragma unroll
-                for (int run = 0; run < 2; ++run) {
-                    int64_t r = j0 + (wj * FJ + t) * 32 + lane % 32, g = k0 / GROUP + run;
-                    r = r < Q.rows ? r : Q.rows - 1;
-                    g = g < Q.groups ? g : Q.groups - 1;                        // its codes are zeros
-                    byte_next[t][run] = Q.scales[r * Q.groups + g];
-                }
+            for (int t = 0; t < FJ; ++t) {
+                const int64_t j = j0 + (wj * FJ + t) * 32 + lane % 32;
+                byte_at[t] = Q.scales + (j < Q.rows ? j : Q.rows - 1) * Q.groups;
+                bytes[t].load(byte_at[t], Q.groups);
+            }
         }
-        qtile::fetch(Q, k0, wave, lane, qtile_at(b), qrow);
     };
-    const auto arrive = [&](int b) {
-        if constexpr (PKIND == CODES_ACROSS) through.store(ptile_at(b));
-        if constexpr (QKIND == CODES_ALONG) {
-#pragma unroll
-            for (int t = 0; t < FJ; ++t) byte[t][0] = byte_next[t][0], byte[t][1] = byte_next[t][1];
-        }
-        __builtin_amdgcn_s_waitcnt(0x0070);          // vmcnt(0) lgkmcnt(0): what this wave fetched and stored has arrived
-        __syncthreads();
-    };
-
-    if (first < last) {
-        start(first, 0);
-        arrive(0);
-    }
-    int b = 0;
-    for (int64_t k0 = first; k0 < last; k0 += STEP, b ^= 1) {
-        const bool more_k = k0 + STEP < last;
-        if (more_k) start(k0 + STEP, b ^ 1);
-#pragma unroll
-        for (int run = 0; run < 2; ++run) {
-            bf16x8 q[FJ][2];
+    f32x16 acc[FI][FJ];
+    // A step in turns of 16 values of k: a turn's operands are read while the turn before is multiplied.
+    const auto multiply = [&](const lds_byte *ptile_at, const lds_byte *qtile_at) {
+        constexpr int TURNS = 2 * RUNS;
+        bf16x8 p[2][FI], q[2][FJ][2];
+        const auto read = [&](int turn) {
+            const int run = turn / 2, s = turn % 2;
 #pragma unroll
             for (int t = 0; t < FJ; ++t) {
                 const int r = (wj * FJ + t) * 32;
                 if constexpr (QKIND == CODES_ALONG) {
-                    qtile::read_codes(qtile_at(b), r, run, lane, byte[t][run], q[t]);
+                    if (s == 0) qtile::read_codes(qtile_at, r, run, lane, bytes[t].byte(run), q[run % 2][t]);
                 } else {
-                    q[t][0] = qtile::read(qtile_at(b), r, run, 0, lane);
-                    q[t][1] = qtile::read(qtile_at(b), r, run, 1, lane);
+                    q[run % 2][t][s] = qtile::read(qtile_at, r, run, s, lane);
                 }
             }
 #pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                bf16x8 p[FI];
+            for (int f = 0; f < FI; ++f) p[turn % 2][f] = ptile::read(ptile_at, (wi * FI + f) * 32, run, s, lane);
+        };
+        read(0);
 #pragma unroll
-                for (int f = 0; f < FI; ++f) p[f] = ptile::read(ptile_at(b), (wi * FI + f) * 32, run, s, lane);
+        for (int turn = 0; turn < TURNS; ++turn) {
+            if (turn + 1 < TURNS) read(turn + 1);
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int f = 0; f < FI; ++f)
+            for (int f = 0; f < FI; ++f)
 #pragma unroll
-                    for (int t = 0; t < FJ; ++t) acc[f][t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(p[f], q[t][s], acc[f][t], 0, 0, 0);
-            }
+                for (int t = 0; t < FJ; ++t)
+                    acc[f][t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(p[turn % 2][f], q[turn / 2 % 2][t][turn % 2], acc[f][t], 0, 0, 0);
         }
-        if (more_k) arrive(b ^ 1);
-    }
-
-#pragma unroll
-    for (int t = 0; t < FJ; ++t) {
-        const int64_t j = j0 + (wj * FJ + t) * 32 + lane % 32;
-        const bool there = j < Q.rows;
+    };
+    // The tile's results, through the buffer that was multiplied last.  A wave's: rows j_wave .. , columns i_wave .. .
+    const auto write = [&](int64_t i0, int64_t j0, uint32_t part, lds_byte *area) {
+        const int64_t j_wave = j0 + wj * FJ * 32, i_wave = i0 + wi * (TO == TO_GATED ? FI / 2 : FI) * 32, groups = groups_of(R.columns);
+        area += wave * (TO == TO_GATE_GRAD ? FI * 4096 : FI * 2048);
+        // addresses are formed here: worked out ahead of the tiles they would take registers from the products
+        int lane = threadIdx.x % 64;
+        asm volatile("" : "+v"(lane));
+        const int half = lane / 32;
+        __syncthreads();
         if constexpr (TO == TO_WIDE || TO == TO_FULL) {
+            using room = exchange<FI * 64>;                          // FI * 32 values of 16 bits, or half as many of 32
+            constexpr int SIZE = TO == TO_WIDE ? 2 : 4, AT_ONCE = TO == TO_WIDE ? FI : FI / 2;
+            const room x{area};
+            const landing to((uint8_t *)R.out + (TO == TO_FULL ? part * R.part * SIZE : 0), j_wave, Q.rows, R.stride * SIZE, i_wave * SIZE,
+                             P.rows * SIZE, FI * 32 * SIZE);
 #pragma unroll
-            for (int f = 0; f < FI; ++f) {
-                const int64_t i = i0 + (wi * FI + f) * 32, n = there ? P.rows - i : 0;
-                if constexpr (TO == TO_WIDE) store_wide((uint16_t *)R.out + j * R.stride, i, n, half, acc[f][t]);
-                else store_full((float *)R.out + part * R.part + j * R.stride, i, n, half, acc[f][t]);
-            }
-        } else {
-            const int64_t groups = groups_of(R.columns);
+            for (int t = 0; t < FJ; ++t)
 #pragma unroll
-            for (int f = 0; f < (TO == TO_GATED ? FI / 2 : FI); ++f) {
-                const int64_t i = i0 + (TO == TO_GATED ? wi * (FI / 2) + f : wi * FI + f) * 32, n = there ? R.columns - i : 0;
-                if constexpr (TO == TO_GATED) {
-                    const f32x16 g = acc[f][t], p = acc[f + FI / 2][t];
+                for (int f0 = 0; f0 < FI; f0 += AT_ONCE) {
+#pragma unroll
+                    for (int f = 0; f < AT_ONCE; ++f) {
+                        const f32x16 &v = acc[f0 + f][t];
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            if constexpr (TO == TO_WIDE) {
+                                x.put_half(lane % 32, f * 4 + q, half, two_bf16(v[4 * q], v[4 * q + 1]), two_bf16(v[4 * q + 2], v[4 * q + 3]));
+                            } else {
+                                x.put(lane % 32, f * 8 + q * 2 + half, u32x4{__float_as_uint(v[4 * q]), __float_as_uint(v[4 * q + 1]),
+                                                                            __float_as_uint(v[4 * q + 2]), __float_as_uint(v[4 * q + 3])});
+                            }
+                        }
+                    }
+                    x.turn();
+                    to.template write<SIZE, TO == TO_WIDE>(x, t * 32, f0 * 32 * SIZE, lane);
+                    x.turn();
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+        } else if constexpr (TO == TO_GATED) {
+            using room = exchange<FI * 16>;                          // FI / 2 * 32 codes
+            constexpr int COLUMNS = FI / 2 * 32, ARRAY = 32 * FI * 16;
+            const landing gated(R.gated_codes, j_wave, Q.rows, R.columns, i_wave, R.columns, COLUMNS);
+            const landing kept_g(R.kept_codes, j_wave, Q.rows, 2 * R.columns, i_wave, R.columns, COLUMNS);
+            const landing kept_p(R.kept_codes, j_wave, Q.rows, 2 * R.columns, R.columns + i_wave, 2 * R.columns, COLUMNS);
+#pragma unroll
+            for (int t = 0; t < FJ; ++t) {
+                uint32_t byte[3][FI / 2];
+#pragma unroll
+                for (int f = 0; f < FI / 2; ++f) {
+                    const f32x16 &g = acc[f][t], &p = acc[f + FI / 2][t];
                     f32x16 a;
 #pragma unroll
                     for (int x = 0; x < 16; ++x) a[x] = g[x] * sigmoid(g[x]) * p[x];
-                    pack_group(R.gated_codes + j * R.columns + i, R.gated_scales + j * groups + i / GROUP, n, half, a);
-                    if (R.kept_codes) {
-                        pack_group(R.kept_codes + 2 * j * R.columns + i, R.kept_scales + 2 * j * groups + i / GROUP, n, half, g);
-                        pack_group(R.kept_codes + (2 * j + 1) * R.columns + i, R.kept_scales + (2 * j + 1) * groups + i / GROUP, n, half, p);
-                    }
-                } else {
-                    const uint32_t gb = n > 0 ? R.kept_scales[2 * j * groups + i / GROUP] : 0u, pb = n > 0 ? R.kept_scales[(2 * j + 1) * groups + i / GROUP] : 0u;
-                    const f32x16 g = unpack_group(R.kept_codes + 2 * j * R.columns + i, gb, n, half);
-                    const f32x16 p = unpack_group(R.kept_codes + (2 * j + 1) * R.columns + i, pb, n, half), d = acc[f][t];
-                    f32x16 dg, dp;
+                    // columns beyond the end hold zeros: their rows of the weight read as such
+                    const auto pack = [&](const f32x16 &v, int array) {
+                        byte[array][f] = scale_byte(group_magnitude(v));
+                        room{area + array * ARRAY}.put(lane % 32, f * 2 + half, encode_group(v, byte[array][f]));
+                    };
+                    pack(a, 0);
+                    if (R.kept_codes) pack(g, 1), pack(p, 2);
+                }
+                const int64_t j = j_wave + t * 32 + lane % 32, g0 = i_wave / GROUP;
+                // the halves of the wave write an array each, then the second one the third
+                const auto scales = [&](uint8_t *to, int array, bool mine) {
 #pragma unroll
-                    for (int x = 0; x < 16; ++x) {
-                        const float s = sigmoid(g[x]);
-                        dg[x] = d[x] * p[x] * s * (1.0f + g[x] * (1.0f - s));
-                        dp[x] = d[x] * g[x] * s;
+                    for (int f = 0; f < FI / 2; ++f)
+                        if (mine && j < Q.rows && g0 + f < groups) to[f] = (uint8_t)byte[array][f];
+                };
+                scales(R.gated_scales + j * groups + g0, 0, half == 0);
+                if (R.kept_codes) {
+                    scales(R.kept_scales + 2 * j * groups + g0, 1, half == 1);
+                    scales(R.kept_scales + (2 * j + 1) * groups + g0, 2, half == 0);
+                }
+                room::turn();
+                gated.template write<1, false>(room{area}, t * 32, 0, lane);
+                if (R.kept_codes) {
+                    kept_g.template write<1, false>(room{area + ARRAY}, t * 32, 0, lane);
+                    kept_p.template write<1, false>(room{area + 2 * ARRAY}, t * 32, 0, lane);
+                }
+                room::turn();
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        } else {
+            using room = exchange<FI * 32>;                          // FI * 32 codes of each half
+            using wide = exchange<FI * 64>;
+            constexpr int ARRAY = 32 * FI * 32;
+            const landing kept_g(R.kept_codes, j_wave, Q.rows, 2 * R.columns, i_wave, R.columns, FI * 32);
+            const landing kept_p(R.kept_codes, j_wave, Q.rows, 2 * R.columns, R.columns + i_wave, 2 * R.columns, FI * 32);
+            const landing to_g(R.out, j_wave, Q.rows, 4 * R.columns, 2 * i_wave, 2 * R.columns, FI * 64);
+            const landing to_p(R.out, j_wave, Q.rows, 4 * R.columns, 2 * (R.columns + i_wave), 4 * R.columns, FI * 64);
+            u32x4 raw[2][room::TURNS];
+            uint32_t bytes_of[2];                                    // a byte a group: at most four
+            const auto load = [&](int t) {
+                kept_g.template read<room>(raw[0], t * 32, lane);
+                kept_p.template read<room>(raw[1], t * 32, lane);
+                const int64_t j = j_wave + t * 32 + lane % 32, g0 = i_wave / GROUP, n = j < Q.rows ? groups - g0 : 0;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const uint8_t *from = R.kept_scales + (2 * j + h) * groups + g0;
+                    bytes_of[h] = 0;
+                    if (n >= FI) {
+                        __builtin_memcpy(&bytes_of[h], from, FI);
+                    } else {
+#pragma unroll
+                        for (int f = 0; f < FI - 1; ++f)
+                            if (f < n) bytes_of[h] |= (uint32_t)from[f] << (8 * f);
                     }
-                    uint16_t *row = (uint16_t *)R.out + j * 2 * R.columns;
-                    store_wide(row, i, n, half, dg);
-                    store_wide(row + R.columns, i, n, half, dp);
+                }
+            };
+            load(0);
+#pragma unroll
+            for (int t = 0; t < FJ; ++t) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int turn = 0; turn < room::TURNS; ++turn)
+                        room{area + h * ARRAY}.put(turn * room::ROWS + lane / room::CHUNKS, lane % room::CHUNKS, raw[h][turn]);
+                const uint32_t bytes_now[2] = {bytes_of[0], bytes_of[1]};
+                room::turn();
+                __builtin_amdgcn_sched_barrier(0);
+                if (t + 1 < FJ) load(t + 1);
+                const wide x{area + 2 * ARRAY};
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                    for (int f = 0; f < FI; ++f) {
+                        f32x16 v = acc[f][t];                        // the other half's gradient waits in acc
+                        if (h == 0) {
+                            const f32x16 g = decode_group(room{area}.get(lane % 32, f * 2 + half), bytes_now[0] >> (8 * f) & 255u);
+                            const f32x16 p = decode_group(room{area + ARRAY}.get(lane % 32, f * 2 + half), bytes_now[1] >> (8 * f) & 255u);
+#pragma unroll
+                            for (int x = 0; x < 16; ++x) {
+                                const float s = sigmoid(g[x]), ds = v[x] * s;
+                                acc[f][t][x] = ds * g[x];
+                                v[x] = ds * p[x] * (1.0f + g[x] * (1.0f - s));
+                            }
+                        }
+#pragma unroll
+                        for (int q = 0; q < 4; ++q)
+                            x.put_half(lane % 32, f * 4 + q, half, two_bf16(v[4 * q], v[4 * q + 1]), two_bf16(v[4 * q + 2], v[4 * q + 3]));
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                    x.turn();
+                    (h ? to_p : to_g).template write<2, true>(x, t * 32, 0, lane);
+                    x.turn();
+                    __builtin_amdgcn_sched_barrier(0);
                 }
             }
         }
+    };
+
+    aim();
+    start(last - first, lds);
+    start_scales();
+    if constexpr (PKIND == CODES_ACROSS) through.store(lds);
+    for (int at = 0;;) {                             // offset of the step's tiles
+#pragma unroll
+        for (int f = 0; f < FI; ++f)
+#pragma unroll
+            for (int t = 0; t < FJ; ++t) acc[f][t] = f32x16{};
+        const int64_t i_now = i0, j_now = j0, length = last - first, k_first = first;
+        const uint32_t part_now = part;
+        bool more_tiles = true;
+        for (int64_t k = 0; k < length; k += STEP, at = BUFFER - at) {
+            __builtin_amdgcn_s_waitcnt(0x0070);      // vmcnt(0) lgkmcnt(0): what this wave fetched and stored has arrived
+            __syncthreads();
+            // the other buffer, which every wave is done with, takes the next step's tiles
+            const bool ends = k + STEP >= length;
+            if (ends) {
+                now += next;
+                more_tiles = STAYS && now < tiles_end;
+                if (more_tiles) aim();
+            }
+            if (more_tiles) start(ends ? last - first : length - k - STEP, lds + (BUFFER - at));
+            multiply(lds + at, lds + at + ptile::BYTES);
+            if constexpr (PKIND == CODES_ACROSS) {
+                if (more_tiles) through.store(lds + (BUFFER - at));
+            }
+            if constexpr (QKIND == CODES_ALONG) {
+                const int64_t g = (k_first + k + STEP) / GROUP;
+#pragma unroll
+                for (int t = 0; t < FJ; ++t) {
+                    bytes[t].template pass<RUNS>();
+                    if (!ends && g % 16 == 0) bytes[t].load(byte_at[t] + g, Q.groups - g);
+                }
+            }
+        }
+        if (more_tiles) start_scales();
+        write(i_now, j_now, part_now, STAYS ? lds + (BUFFER - at) : lds);
+        if (!more_tiles) break;
     }
 }
 
