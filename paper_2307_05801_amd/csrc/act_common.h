@@ -60,7 +60,37 @@ template <int TYPE> __device__ inline void load8(const void *base, int64_t at, i
     for (int i = 0; i < CHUNK; ++i) v[i] = element<TYPE>::to_float(r[i]);
 }
 
-template <int TYPE> __device__ inline void store8(void *base, int64_t at, int n, const float (&v)[CHUNK])
+// Outputs of more than this go past the caches: little of them is left there when they are read, and they push out what is (2^27
+// bfloat16 values unpacked: 57 us, 68 through the caches; packed 61 and 70).
+constexpr int64_t PAST_CACHES = (int64_t)64 << 20;
+
+typedef uint32_t words4 __attribute__((ext_vector_type(4), aligned(1)));
+typedef uint32_t words2 __attribute__((ext_vector_type(2), aligned(1)));
+
+// BYTES (8, 16 or 32) to any address.
+template <int BYTES> __device__ inline void store_bytes(void *to, const void *from, bool past)
+{
+    if (past) {
+        asm volatile("");            // between two of these the compiler does not make one plain store of both branches
+        if constexpr (BYTES == 8) {
+            words2 w;
+            __builtin_memcpy(&w, from, 8);
+            __builtin_nontemporal_store(w, (words2 *)to);
+        } else {
+#pragma unroll
+            for (int i = 0; i < BYTES; i += 16) {
+                words4 w;
+                __builtin_memcpy(&w, (const char *)from + i, 16);
+                __builtin_nontemporal_store(w, (words4 *)((char *)to + i));
+            }
+        }
+        asm volatile("");
+    } else {
+        __builtin_memcpy(to, from, BYTES);
+    }
+}
+
+template <int TYPE> __device__ inline void store8(void *base, int64_t at, int n, const float (&v)[CHUNK], bool past = false)
 {
     using raw = typename element<TYPE>::raw;
     raw *p = (raw *)base + at;
@@ -68,7 +98,7 @@ template <int TYPE> __device__ inline void store8(void *base, int64_t at, int n,
 #pragma unroll
     for (int i = 0; i < CHUNK; ++i) r[i] = element<TYPE>::from_float(v[i]);
     if (n >= CHUNK) {
-        __builtin_memcpy(p, r, sizeof r);
+        store_bytes<sizeof r>(p, r, past);
     } else {
 #pragma unroll
         for (int i = 0; i < CHUNK - 1; ++i)
@@ -130,10 +160,10 @@ __device__ inline uint2 load_codes(const uint8_t *p, int n)
     return c;
 }
 
-__device__ inline void store_codes(uint8_t *p, int n, uint2 c)
+__device__ inline void store_codes(uint8_t *p, int n, uint2 c, bool past)
 {
     if (n >= CHUNK) {
-        __builtin_memcpy(p, &c, CHUNK);
+        store_bytes<CHUNK>(p, &c, past);
     } else {
         uint8_t b[CHUNK];
         __builtin_memcpy(b, &c, CHUNK);
@@ -145,7 +175,8 @@ __device__ inline void store_codes(uint8_t *p, int n, uint2 c)
 
 // Packs the eight values of this lane, n of them there; its three neighbours of a quad hold the rest of the group.  All four
 // lanes of a quad call it together.
-__device__ inline void pack_chunk(const float (&v)[CHUNK], int n, uint8_t *codes, uint8_t *scales, int64_t row, int64_t cols, int64_t groups, int64_t col)
+__device__ inline void pack_chunk(const float (&v)[CHUNK], int n, uint8_t *codes, uint8_t *scales, int64_t row, int64_t cols, int64_t groups, int64_t col,
+                                  bool past)
 {
     uint32_t amax = 0;
 #pragma unroll
@@ -160,7 +191,7 @@ __device__ inline void pack_chunk(const float (&v)[CHUNK], int n, uint8_t *codes
     amax = other > amax ? other : amax;
     const uint32_t byte = scale_byte(amax);
     if (n > 0) {
-        store_codes(codes + row * cols + col, n, encode8(v, scale_inverse(byte)));
+        store_codes(codes + row * cols + col, n, encode8(v, scale_inverse(byte)), past);
         if (col % GROUP == 0) scales[row * groups + col / GROUP] = (uint8_t)byte;
     }
 }

@@ -162,8 +162,8 @@ __global__ __launch_bounds__(BLOCK) void k_gate_grad(const void *__restrict__ da
         dg[i] = d[i] * p[i] * s * (1.0f + g[i] * (1.0f - s));
         dp[i] = d[i] * g[i] * s;
     }
-    store8<LEAP_BF16>(du, row * 2 * out + col, n, dg);
-    store8<LEAP_BF16>(du, row * 2 * out + out + col, n, dp);
+    store8<LEAP_BF16>(du, row * 2 * out + col, n, dg, rows * out * 4 > PAST_CACHES);
+    store8<LEAP_BF16>(du, row * 2 * out + out + col, n, dp, rows * out * 4 > PAST_CACHES);
 }
 
 const char *bad_product(int64_t rows, int64_t cols, int64_t w_stride, int64_t out)

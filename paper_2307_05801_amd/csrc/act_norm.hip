@@ -40,6 +40,7 @@ struct norm_args {
     void *sum;
     uint8_t *normed_codes, *normed_scales, *kept_codes, *kept_scales;
     float *rstd;
+    bool past;                   // outputs past the caches
 };
 
 // s of one chunk: x + residual, as the type holds it
@@ -57,13 +58,13 @@ template <int TYPE, bool ADD> __device__ inline void sum_chunk(const norm_args &
 template <int TYPE, int WTYPE>
 __device__ inline void norm_chunk(const norm_args &A, int64_t row, int64_t col, int n, const float (&s)[CHUNK], float rstd)
 {
-    if (A.sum && n > 0) store8<TYPE>(A.sum, row * A.cols + col, n, s);
-    if (A.kept_codes) pack_chunk(s, n, A.kept_codes, A.kept_scales, row, A.cols, A.groups, col);
+    if (A.sum && n > 0) store8<TYPE>(A.sum, row * A.cols + col, n, s, A.past);
+    if (A.kept_codes) pack_chunk(s, n, A.kept_codes, A.kept_scales, row, A.cols, A.groups, col, A.past);
     float w[CHUNK], v[CHUNK];
     load8<WTYPE>(A.weight, col, n, w);
 #pragma unroll
     for (int i = 0; i < CHUNK; ++i) v[i] = s[i] * rstd * w[i];
-    pack_chunk(v, n, A.normed_codes, A.normed_scales, row, A.cols, A.groups, col);
+    pack_chunk(v, n, A.normed_codes, A.normed_scales, row, A.cols, A.groups, col, A.past);
 }
 
 // Rows of up to LANES * CHUNKS chunks, BLOCK / LANES of them in a block.
@@ -118,35 +119,36 @@ struct grad_args {
     const float *rstd;
     void *grad_x;
     float *part;                 // [blocks][cols]: each block's sum of grad h, or null
+    bool past;
 };
 
-// h of one chunk
-__device__ inline void unit_chunk(const grad_args &A, int64_t row, int64_t col, int n, float rstd, float (&h)[CHUNK])
+// How many of a chunk's values a row has, from what is left of it.
+__device__ inline int there(int64_t left) { return left <= 0 ? 0 : left < CHUNK ? (int)left : CHUNK; }
+
+// What is kept of one chunk; h is rstd times that
+__device__ inline void unit_chunk(const grad_args &A, int64_t row, int64_t col, int n, float (&h)[CHUNK])
 {
     const uint2 c = load_codes(A.kept_codes + row * A.cols + col, n);
     decode8(c, scale_value(n > 0 ? A.kept_scales[row * A.groups + col / GROUP] : 0u), h);
-#pragma unroll
-    for (int i = 0; i < CHUNK; ++i) h[i] *= rstd;
 }
 
 template <int TYPE>
-__device__ inline void grad_chunk(const grad_args &A, int64_t row, int64_t col, int n, const float (&d)[CHUNK], const float (&h)[CHUNK], float rstd,
-                                  float mean)
+__device__ inline void grad_chunk(const grad_args &A, int64_t row, int64_t col, int n, const float (&d)[CHUNK], const float (&h)[CHUNK],
+                                  const float (&gs)[CHUNK], float rstd, float mean)
 {
     if (n <= 0) return;
-    float o[CHUNK], gs[CHUNK] = {};
-    if (A.grad_sum) load8<TYPE>(A.grad_sum, row * A.grad_sum_stride + col, n, gs);
+    float o[CHUNK];
 #pragma unroll
     for (int i = 0; i < CHUNK; ++i) o[i] = gs[i] + rstd * (d[i] - h[i] * mean);
-    store8<TYPE>(A.grad_x, row * A.cols + col, n, o);
+    store8<TYPE>(A.grad_x, row * A.cols + col, n, o, A.past);
 }
 
-// Blocks walk over the rows; a lane sums grad h of its own columns in registers, the block's rows of lanes join in shared
-// memory at the end.
+// Blocks walk over the rows, AHEAD of them at a time so that loads of a few rows are under way at once; a lane sums grad h of
+// its own columns in registers, the block's rows of lanes join in shared memory at the end.
 template <int TYPE, int GTYPE, int WTYPE, int LANES, int CHUNKS>
 __global__ __launch_bounds__(BLOCK) void k_norm_grad(grad_args A)
 {
-    constexpr int ROWS = BLOCK / LANES;
+    constexpr int ROWS = BLOCK / LANES, AHEAD = CHUNKS == 1 ? 2 : 1;
     __shared__ float room[ROWS > 1 ? BLOCK * CHUNK : 1];
     const int lane = threadIdx.x % LANES;
     float w[CHUNKS][CHUNK], dw[CHUNKS][CHUNK] = {};
@@ -155,28 +157,43 @@ __global__ __launch_bounds__(BLOCK) void k_norm_grad(grad_args A)
         const int64_t left = A.cols - (int64_t)(k * LANES + lane) * CHUNK;
         load8<WTYPE>(A.weight, (int64_t)(k * LANES + lane) * CHUNK, left <= 0 ? 0 : left < CHUNK ? (int)left : CHUNK, w[k]);
     }
-    for (int64_t row0 = (int64_t)blockIdx.x * ROWS; row0 < A.rows; row0 += (int64_t)gridDim.x * ROWS) {
-        const int64_t row = row0 + threadIdx.x / LANES;
-        const bool there = row < A.rows;
-        const float rstd = there ? A.rstd[row] : 0.0f;
-        float d[CHUNKS][CHUNK], h[CHUNKS][CHUNK], dot = 0.0f;
-        int n[CHUNKS];
+    for (int64_t row0 = (int64_t)blockIdx.x * (ROWS * AHEAD); row0 < A.rows; row0 += (int64_t)gridDim.x * (ROWS * AHEAD)) {
+        float d[AHEAD][CHUNKS][CHUNK], h[AHEAD][CHUNKS][CHUNK], gs[AHEAD][CHUNKS][CHUNK], rstd[AHEAD];
 #pragma unroll
-        for (int k = 0; k < CHUNKS; ++k) {
-            const int64_t col = (int64_t)(k * LANES + lane) * CHUNK, left = A.cols - col;
-            n[k] = !there || left <= 0 ? 0 : left < CHUNK ? (int)left : CHUNK;
-            load8<GTYPE>(A.grad, row * A.grad_stride + col, n[k], d[k]);
-            unit_chunk(A, row, col, n[k], rstd, h[k]);
+        for (int a = 0; a < AHEAD; ++a) {
+            const int64_t row = row0 + a * ROWS + threadIdx.x / LANES;
+            rstd[a] = row < A.rows ? A.rstd[row] : 0.0f;
 #pragma unroll
-            for (int i = 0; i < CHUNK; ++i) {
-                if (n[k] > 0) dw[k][i] += d[k][i] * h[k][i];
-                d[k][i] *= w[k][i];
-                dot += d[k][i] * h[k][i];
+            for (int k = 0; k < CHUNKS; ++k) {
+                const int64_t col = (int64_t)(k * LANES + lane) * CHUNK;
+                const int n = row < A.rows ? there(A.cols - col) : 0;
+                load8<GTYPE>(A.grad, row * A.grad_stride + col, n, d[a][k]);
+                unit_chunk(A, row, col, n, h[a][k]);
+                load8<TYPE>(A.grad_sum, row * A.grad_sum_stride + col, A.grad_sum ? n : 0, gs[a][k]);
             }
         }
-        const float mean = row_sum<LANES>(dot) * A.inverse_cols;
 #pragma unroll
-        for (int k = 0; k < CHUNKS; ++k) grad_chunk<TYPE>(A, row, (int64_t)(k * LANES + lane) * CHUNK, n[k], d[k], h[k], rstd, mean);
+        for (int a = 0; a < AHEAD; ++a) {
+            const int64_t row = row0 + a * ROWS + threadIdx.x / LANES;
+            float dot = 0.0f;
+#pragma unroll
+            for (int k = 0; k < CHUNKS; ++k) {
+                const bool here = row < A.rows && there(A.cols - (int64_t)(k * LANES + lane) * CHUNK) > 0;
+#pragma unroll
+                for (int i = 0; i < CHUNK; ++i) {
+                    h[a][k][i] *= rstd[a];
+                    if (here) dw[k][i] += d[a][k][i] * h[a][k][i];
+                    d[a][k][i] *= w[k][i];
+                    dot += d[a][k][i] * h[a][k][i];
+                }
+            }
+            const float mean = row_sum<LANES>(dot) * A.inverse_cols;
+#pragma unroll
+            for (int k = 0; k < CHUNKS; ++k) {
+                const int64_t col = (int64_t)(k * LANES + lane) * CHUNK;
+                grad_chunk<TYPE>(A, row, col, row < A.rows ? there(A.cols - col) : 0, d[a][k], h[a][k], gs[a][k], rstd[a], mean);
+            }
+        }
     }
     if (!A.part) return;
 #pragma unroll
@@ -211,19 +228,21 @@ template <int TYPE, int GTYPE, int WTYPE> __global__ __launch_bounds__(BLOCK) vo
         const int n = (int)(A.cols - col < CHUNK ? A.cols - col : CHUNK);
         load8<GTYPE>(A.grad, row * A.grad_stride + col, n, d);
         load8<WTYPE>(A.weight, col, n, w);
-        unit_chunk(A, row, col, n, rstd, h);
+        unit_chunk(A, row, col, n, h);
 #pragma unroll
-        for (int i = 0; i < CHUNK; ++i) dot += d[i] * w[i] * h[i];
+        for (int i = 0; i < CHUNK; ++i) dot += d[i] * w[i] * (h[i] * rstd);
     }
     const float mean = block_sum(dot, room) * A.inverse_cols;
     for (int64_t col = threadIdx.x * CHUNK; col < A.cols; col += BLOCK * CHUNK) {
         const int n = (int)(A.cols - col < CHUNK ? A.cols - col : CHUNK);
         load8<GTYPE>(A.grad, row * A.grad_stride + col, n, d);
         load8<WTYPE>(A.weight, col, n, w);
-        unit_chunk(A, row, col, n, rstd, h);
+        unit_chunk(A, row, col, n, h);
+        float gs[CHUNK];
+        load8<TYPE>(A.grad_sum, row * A.grad_sum_stride + col, A.grad_sum ? n : 0, gs);
 #pragma unroll
-        for (int i = 0; i < CHUNK; ++i) d[i] *= w[i];
-        grad_chunk<TYPE>(A, row, col, n, d, h, rstd, mean);
+        for (int i = 0; i < CHUNK; ++i) d[i] *= w[i], h[i] *= rstd;
+        grad_chunk<TYPE>(A, row, col, n, d, h, gs, rstd, mean);
     }
 }
 
@@ -237,27 +256,32 @@ template <int GTYPE> __global__ __launch_bounds__(BLOCK) void k_norm_grad_weight
     for (int64_t row = blockIdx.y; row < A.rows; row += gridDim.y) {
         float g[CHUNK], h[CHUNK];
         load8<GTYPE>(A.grad, row * A.grad_stride + col, n, g);
-        unit_chunk(A, row, col, n, A.rstd[row], h);
+        unit_chunk(A, row, col, n, h);
 #pragma unroll
-        for (int i = 0; i < CHUNK; ++i) dw[i] += g[i] * h[i];
+        for (int i = 0; i < CHUNK; ++i) dw[i] += g[i] * (h[i] * A.rstd[row]);
     }
     store8<LEAP_F32>(A.part, blockIdx.y * A.cols + col, n, dw);
 }
 
-// grad_weight <- the sum of the parts, 64 columns a block, its waves taking every fourth part.
-template <int WTYPE> __global__ __launch_bounds__(BLOCK) void k_join(const float *__restrict__ part, int64_t parts, int64_t cols, void *__restrict__ out)
+// grad_weight <- the sum of the parts: 16 columns a block, 64 threads to a column, each of which adds every 64th part.
+template <int WTYPE> __global__ __launch_bounds__(1024) void k_join(const float *__restrict__ part, int64_t parts, int64_t cols, void *__restrict__ out)
 {
-    __shared__ float room[BLOCK];
-    const int64_t col = (int64_t)blockIdx.x * WAVE + threadIdx.x % WAVE;
+    constexpr int COLS = 16, AT_ONCE = 64;
+    __shared__ float room[AT_ONCE][COLS];
+    const int c = threadIdx.x % COLS, r = threadIdx.x / COLS;
+    const int64_t col = (int64_t)blockIdx.x * COLS + c;
     float sum = 0.0f;
-    if (col < cols)
-        for (int64_t p = threadIdx.x / WAVE; p < parts; p += BLOCK / WAVE) sum += part[p * cols + col];
-    room[threadIdx.x] = sum;
-    __syncthreads();
-    if (threadIdx.x < WAVE && col < cols) {
-        for (int i = 1; i < BLOCK / WAVE; ++i) sum += room[i * WAVE + threadIdx.x];
-        ((typename element<WTYPE>::raw *)out)[col] = element<WTYPE>::from_float(sum);
+    if (col < cols) {
+#pragma unroll 8
+        for (int64_t p = r; p < parts; p += AT_ONCE) sum += part[p * cols + col];
     }
+    room[r][c] = sum;
+    __syncthreads();
+    for (int half = AT_ONCE / 2; half > 0; half /= 2) {
+        if (r < half) room[r][c] += room[r + half][c];
+        __syncthreads();
+    }
+    if (r == 0 && col < cols) ((typename element<WTYPE>::raw *)out)[col] = element<WTYPE>::from_float(room[0][c]);
 }
 
 constexpr int MOST_CHUNKS = 4;                                       // chunks a lane holds
@@ -280,8 +304,9 @@ template <class F> int by_length(int64_t cols, F &&f)
 int64_t grad_blocks(int64_t rows, int64_t cols)
 {
     if (cols > LONG) return rows < 256 ? (rows > 0 ? rows : 1) : 256;
-    const int64_t lanes = cols <= 64 ? 8 : cols <= 128 ? 16 : cols <= 256 ? 32 : 64, all = (rows + BLOCK / lanes - 1) / (BLOCK / lanes);
-    return all < 1 ? 1 : all < 2048 ? all : 2048;
+    const int64_t lanes = cols <= 64 ? 8 : cols <= 128 ? 16 : cols <= 256 ? 32 : 64, at_once = BLOCK / lanes * (cols <= 512 ? 2 : 1), all = (rows + at_once - 1) / at_once;
+    const int64_t most = cols <= 512 ? 1024 : 2048;                   // (262144 x 512: 180 us, 185 with 2048; 131072 x 1024: 217, 257 with 1024)
+    return all < 1 ? 1 : all < most ? all : most;
 }
 
 template <class F> int by_weight(int32_t type, int32_t weight_type, F &&f)
@@ -314,7 +339,7 @@ extern "C" int leap_rms_norm8(const void *d_x, int64_t x_stride, const void *d_r
     if (!d_kept_codes != !d_kept_scales) return refuse("kept codes and scales: both or neither");
     if (rows > 0x7fffffff) return refuse("more than 2^31 rows");
     const norm_args A{d_x, d_residual, d_weight, x_stride, residual_stride, rows, cols, groups_of(cols), eps, 1.0f / (float)cols,
-                      d_sum, d_normed_codes, d_normed_scales, d_kept_codes, d_kept_scales, d_rstd};
+                      d_sum, d_normed_codes, d_normed_scales, d_kept_codes, d_kept_scales, d_rstd, rows * cols * 2 > PAST_CACHES};
     return by_weight(type, weight_type, [&](auto t, auto w) {
         constexpr int T = decltype(t)::value, W = decltype(w)::value;
         const hipStream_t st = stream_of(hip_stream);
@@ -352,7 +377,7 @@ extern "C" int leap_rms_norm8_backward(const void *d_grad, int32_t grad_type, in
     if (rows && (!d_grad || !d_kept_codes || !d_kept_scales || !d_rstd || !d_weight || !d_grad_x)) return refuse("null data pointer");
     if (d_grad_weight && !d_work) return refuse("the weight's gradient needs the workspace");
     const grad_args A{d_grad, d_grad_sum, d_weight, grad_stride, grad_sum_stride, rows, cols, groups_of(cols), 1.0f / (float)cols,
-                      d_kept_codes, d_kept_scales, d_rstd, d_grad_x, d_grad_weight ? d_work : nullptr};
+                      d_kept_codes, d_kept_scales, d_rstd, d_grad_x, d_grad_weight ? d_work : nullptr, rows * cols * 2 > PAST_CACHES};
     const hipStream_t st = stream_of(hip_stream);
     const int64_t parts = rows ? grad_blocks(rows, cols) : 0;
     int rc = LEAP_OK;
@@ -379,7 +404,7 @@ extern "C" int leap_rms_norm8_backward(const void *d_grad, int32_t grad_type, in
         });
     if (rc != LEAP_OK || !d_grad_weight) return rc;
     return by_type(weight_type, [&](auto w) {
-        hipLaunchKernelGGL((k_join<decltype(w)::value>), dim3((unsigned)((cols + WAVE - 1) / WAVE)), dim3(BLOCK), 0, st, d_work, parts, cols, d_grad_weight);
+        hipLaunchKernelGGL((k_join<decltype(w)::value>), dim3((unsigned)((cols + 15) / 16)), dim3(1024), 0, st, d_work, parts, cols, d_grad_weight);
         return launched();
     });
 }

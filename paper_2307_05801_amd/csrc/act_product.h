@@ -300,11 +300,12 @@ struct landing {
     uint8_t *base;
     int64_t left, bytes;                   // rows; bytes of a row
     uint32_t pitch;                        // bytes between rows
-    bool whole;
+    bool whole, past;                      // past: stores go past the caches, which pays where they fill whole lines of memory
     __amdgpu_buffer_rsrc_t buffer;
 
     __device__ inline landing(const void *array, int64_t j, int64_t rows, int64_t pitch_, int64_t i, int64_t end, int width)
-        : base((uint8_t *)array + j * pitch_ + i), left(rows - j), bytes(end - i), pitch((uint32_t)pitch_), whole(end - i >= width)
+        : base((uint8_t *)array + j * pitch_ + i), left(rows - j), bytes(end - i), pitch((uint32_t)pitch_), whole(end - i >= width),
+          past((pitch_ | (int64_t)(uintptr_t)base) % 64 == 0)
     {
         const int64_t all = left * pitch_ - i;
         buffer = __builtin_amdgcn_make_buffer_rsrc(base, 0, left <= 0 || all <= 0 ? 0 : all < 0x7ffffff0 ? (int)all : 0x7ffffff0, 0x00020000);
@@ -315,11 +316,16 @@ struct landing {
         const int row = lane / ROOM::CHUNKS, chunk = lane % ROOM::CHUNKS;
         if (whole) {
             const uint32_t offset = (first + row) * pitch + at + chunk * 16;
+            const auto rows = [&](auto hint) {
 #pragma unroll
-            for (int turn = 0; turn < ROOM::TURNS; ++turn) {
-                const int r = turn * ROOM::ROWS + row;
-                __builtin_amdgcn_raw_buffer_store_b128(HALVES ? room.get_halves(r, chunk) : room.get(r, chunk), buffer, offset + turn * ROOM::ROWS * pitch, 0, 0);
-            }
+                for (int turn = 0; turn < ROOM::TURNS; ++turn) {
+                    const int r = turn * ROOM::ROWS + row;
+                    __builtin_amdgcn_raw_buffer_store_b128(HALVES ? room.get_halves(r, chunk) : room.get(r, chunk), buffer,
+                                                           offset + turn * ROOM::ROWS * pitch, 0, decltype(hint)::value);
+                }
+            };
+            if (past) rows(std::integral_constant<int, 2>{});
+            else rows(std::integral_constant<int, 0>{});
         } else {
 #pragma unroll 1
             for (int turn = 0; turn < ROOM::TURNS; ++turn) {
@@ -536,8 +542,9 @@ __global__ __launch_bounds__(WI * WJ * 64, WI * WJ > 4 ? 1 : 2) void k_product(o
             using room = exchange<FI * 64>;                          // FI * 32 values of 16 bits, or half as many of 32
             constexpr int SIZE = TO == TO_WIDE ? 2 : 4, AT_ONCE = TO == TO_WIDE ? FI : FI / 2;
             const room x{area};
-            const landing to((uint8_t *)R.out + (TO == TO_FULL ? part * R.part * SIZE : 0), j_wave, Q.rows, R.stride * SIZE, i_wave * SIZE,
-                             P.rows * SIZE, FI * 32 * SIZE);
+            landing to((uint8_t *)R.out + (TO == TO_FULL ? part * R.part * SIZE : 0), j_wave, Q.rows, R.stride * SIZE, i_wave * SIZE,
+                       P.rows * SIZE, FI * 32 * SIZE);
+            if (parts > 1) to.past = false;                          // they are read again at once
 #pragma unroll
             for (int t = 0; t < FJ; ++t)
 #pragma unroll
