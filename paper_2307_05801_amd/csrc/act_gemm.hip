@@ -77,7 +77,7 @@ bool large_tiles(int64_t i, int64_t j)
     return (double)cut(cut(i, 256) * cut(j, 256), 256) <= 0.62 * (double)cut(cut(i, 128) * cut(j, 128), 512);
 }
 
-template <int PKIND, int QKIND, int TO, int TI, int TJ, int WI, int WJ, int STEP>
+template <int PKIND, int QKIND, int TO, int TI, int TJ, int WI, int WJ>
 int launch(const operand &P, const operand &Q, const result &R, int64_t depth_part, hipStream_t st)
 {
     const int64_t across = TO == TO_GATED ? cut(R.columns, TI / 2) : cut(P.rows, TI), along = cut(Q.rows, TJ), parts = depth_part ? cut(P.depth, depth_part) : 1;
@@ -85,7 +85,7 @@ int launch(const operand &P, const operand &Q, const result &R, int64_t depth_pa
     // as many blocks as the 256 compute units hold at once, by shared memory and registers
     constexpr int RESIDENT = WI * WJ > 4 ? 1 : 2;
     const int64_t blocks = !stays<TO>() || across * along * parts < 256 * RESIDENT ? across * along * parts : 256 * RESIDENT;
-    hipLaunchKernelGGL((k_product<PKIND, QKIND, TO, TI, TJ, WI, WJ, STEP>), dim3((unsigned)blocks), dim3(WI * WJ * 64), 0, st, P, Q, R, (uint32_t)across,
+    hipLaunchKernelGGL((k_product<PKIND, QKIND, TO, TI, TJ, WI, WJ>), dim3((unsigned)blocks), dim3(WI * WJ * 64), 0, st, P, Q, R, (uint32_t)across,
                        (uint32_t)along, (uint32_t)parts, depth_part ? depth_part : P.depth);
     return launched();
 }
@@ -94,8 +94,8 @@ template <int PKIND, int QKIND, int TO> int product(const operand &P, const oper
 {
     // the gate's gradient moves more than it multiplies: small tiles always (262144 x 512 -> 2 * 512: 300 us, large ones 369)
     if constexpr (TO != TO_GATE_GRAD)
-        if (large) return launch<PKIND, QKIND, TO, 256, 256, 2, 4, 64>(P, Q, R, depth_part, st);
-    return launch<PKIND, QKIND, TO, 128, 128, 2, 2, 64>(P, Q, R, depth_part, st);
+        if (large) return launch<PKIND, QKIND, TO, 256, 256, 2, 4>(P, Q, R, depth_part, st);
+    return launch<PKIND, QKIND, TO, 128, 128, 2, 2>(P, Q, R, depth_part, st);
 }
 
 template <int PKIND, int QKIND, int TO> int product(const operand &P, const operand &Q, const result &R, hipStream_t st)

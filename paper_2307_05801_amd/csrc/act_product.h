@@ -82,13 +82,14 @@ template <int KIND, int T, int STEP, int THREADS> struct tile {
     // Where piece `chunk` of row r goes (and what is found there): rows 256 / ROW apart begin in the same bank.
     static __device__ inline int place(int r, int chunk) { return chunk ^ (r / (256 / ROW) % CHUNKS); }
 
-    // A wave's part in fetching tiles of the operand from row0 on, k after k.  HALVES 2: the tile's rows are, span by span, the
-    // same rows of two operands, `apart` bytes apart (the gate's and the other half).
+    // A wave's part in fetching tiles of the operand, k after k.  HALVES 2: the tile's rows are, span by span, the same rows of
+    // two operands, `apart` bytes apart (the gate's and the other half).
     template <int HALVES, int SPAN> struct stream {
         uint32_t offset[EACH];
-        window at[HALVES];
-        static constexpr int half_of(int e) { return HALVES == 1 ? 0 : e * WAVES * ROWS % SPAN / (SPAN / 2); }
+        window at;
+        const uint8_t *other;                  // where the second half's window begins
         static_assert(HALVES == 1 || (KIND == WIDE_ALONG && WAVES * ROWS <= SPAN / 2), "all waves fetch of one half at a time");
+        static constexpr int half_of(int e) { return HALVES == 1 ? 0 : e * WAVES * ROWS % SPAN / (SPAN / 2); }
 
         __device__ inline void init(const operand &O, int wave, int lane)
         {
@@ -110,29 +111,27 @@ template <int KIND, int T, int STEP, int THREADS> struct tile {
         __device__ inline void aim(const operand &O, int64_t rows, int64_t row0, int64_t first, int64_t last, int64_t apart)
         {
             if constexpr (KIND == WIDE_ACROSS)
-                at[0] = {O.data + (first * O.stride + row0) * 2, ((last - 1 - first) * O.stride + whole(rows, 8) - row0) * 2, (uint32_t)(STEP * O.stride * 2)};
+                at = {O.data + (first * O.stride + row0) * 2, ((last - 1 - first) * O.stride + whole(rows, 8) - row0) * 2, (uint32_t)(STEP * O.stride * 2)};
             else
-                at[0] = {O.data + (row0 * O.stride + first) * VALUE, ((rows - 1 - row0) * O.stride + whole(last, 16 / VALUE) - first) * VALUE, STEP * VALUE};
-            if constexpr (HALVES == 2) at[1] = {at[0].base + apart, at[0].left, at[0].step};
+                at = {O.data + (row0 * O.stride + first) * VALUE, ((rows - 1 - row0) * O.stride + whole(last, 16 / VALUE) - first) * VALUE, STEP * VALUE};
+            other = at.base + apart;
         }
 
-        // Starts the fetch of the next tile, `k` values of k from the operand's end.
-        __device__ inline void fetch(int64_t k, int wave, int lane, lds_byte *to)
+        // Makes the next tile's fetch ready, `k` values of k from the operand's end: pieces beyond that read as zeros.
+        u32x4 from[HALVES];
+        uint32_t dead;
+        __device__ inline void ready(int64_t k, int wave, int lane)
         {
-            u32x4 from[HALVES];
-#pragma unroll
-            for (int h = 0; h < HALVES; ++h) from[h] = at[h].buffer(), at[h].advance();
-            if (KIND == WIDE_ACROSS || k >= STEP) {
-#pragma unroll
-                for (int e = 0; e < EACH; ++e) fetch16(from[half_of(e)], offset[e], to + (e * WAVES + wave) * 1024);
-            } else {
-#pragma unroll
-                for (int e = 0; e < EACH; ++e) {
-                    const int chunk = place((e * WAVES + wave) * ROWS + lane / CHUNKS, lane % CHUNKS);
-                    fetch16(from[half_of(e)], chunk * (16 / VALUE) < k ? offset[e] : NOWHERE, to + (e * WAVES + wave) * 1024);
-                }
-            }
+            from[0] = at.buffer();
+            if constexpr (HALVES == 2) from[1] = window{other, at.left, 0}.buffer(), other += at.step;
+            at.advance();
+            dead = 0;
+            // (the pieces a lane fetches are of the same place in their rows)
+            static_assert(KIND == WIDE_ACROSS || WAVES * ROWS / (256 / ROW) % CHUNKS == 0, "");
+            if constexpr (KIND != WIDE_ACROSS) dead = place(wave * ROWS + lane / CHUNKS, lane % CHUNKS) * (16 / VALUE) < k ? 0u : NOWHERE;
         }
+        // Starts the fetch of its piece e.
+        __device__ inline void fetch(int e, int wave, lds_byte *to) const { fetch16(from[half_of(e)], offset[e] | dead, to + (e * WAVES + wave) * 1024); }
     };
 
     // The eight values of turn s of 32-run `run` of the tile's rows first .. first + 31.
@@ -151,14 +150,11 @@ template <int KIND, int T, int STEP, int THREADS> struct tile {
         }
     }
 
-    // Both turns from codes along k, with their scale.
-    static __device__ inline void read_codes(const lds_byte *from, int first, int run, int lane, uint32_t byte, bf16x8 (&v)[2])
+    // The 16 codes of both turns.
+    static __device__ inline u32x4 read_codes(const lds_byte *from, int first, int run, int lane)
     {
         const int r = first + lane % 32;
-        const u32x4 c = *(const __attribute__((address_space(3))) u32x4 *)(from + r * ROW + place(r, run * 2 + lane / 32) * 16);
-        const float scale = __uint_as_float(byte << 23);
-#pragma unroll
-        for (int s = 0; s < 2; ++s) v[s] = widen(c[2 * s], c[2 * s + 1], scale);
+        return *(const __attribute__((address_space(3))) u32x4 *)(from + r * ROW + place(r, run * 2 + lane / 32) * 16);
     }
 
     // Eight codes as bfloat16; `scale` counts by its exponent alone.
@@ -439,110 +435,134 @@ struct result {
 };
 
 // WI x WJ waves share TI x TJ of D.  Tiles: `across` of i, `along` of j, `parts` of depth_part values of k.  A block takes
-// tile after tile; the first step's fetch of the next one is under way while this one's results are written.
-template <int PKIND, int QKIND, int TO, int TI, int TJ, int WI, int WJ, int STEP>
+// tile after tile (but for the gate's gradient), and its fetches run ahead of its products across their borders.
+//
+// A step is multiplied in turns of 16 values of k.  What a turn takes is read while the turn before is multiplied; the next
+// step's fetches are started while the first turn's operands are on their way from shared memory.
+template <int PKIND, int QKIND, int TO, int TI, int TJ, int WI, int WJ>
 __global__ __launch_bounds__(WI * WJ * 64, WI * WJ > 4 ? 1 : 2) void k_product(operand P, operand Q, result R, uint32_t across, uint32_t along, uint32_t parts,
                                                                                int64_t depth_part)
 {
-    constexpr int THREADS = WI * WJ * 64, FI = TI / WI / 32, FJ = TJ / WJ / 32, RUNS = STEP / 32;
-    constexpr int PWIDE = PKIND == CODES_ACROSS ? WIDE_ACROSS : PKIND;
+    constexpr bool THROUGH = PKIND == CODES_ACROSS, STAYS = stays<TO>();
+    constexpr int THREADS = WI * WJ * 64, FI = TI / WI / 32, FJ = TJ / WJ / 32, STEP = 64, TURNS = STEP / 16;
+    constexpr int PWIDE = THROUGH ? WIDE_ACROSS : PKIND;
     using ptile = tile<PWIDE, TI, STEP, THREADS>;
     using qtile = tile<QKIND, TJ, STEP, THREADS>;
-    constexpr int TILES = ptile::BYTES + qtile::BYTES, AREA = WI * WJ * FI * 2048;       // a step's; what write() takes of a buffer
-    constexpr int BUFFER = TILES > AREA ? TILES : AREA;
+    constexpr int TILES = ptile::BYTES + qtile::BYTES, AREA = 4096;            // a step's; what a wave's results go through
+    constexpr int BUFFER = TILES > WI * WJ * AREA ? TILES : WI * WJ * AREA;
     __shared__ __attribute__((aligned(1024))) uint8_t room[2 * BUFFER];
     lds_byte *const lds = (lds_byte *)room;
-    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), half = lane / 32;
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int wi = wave % WI, wj = wave / WI;
 
     // Blocks go round the eight dies; each die has a run of neighbouring tiles, so that what they share comes from its cache.
-    constexpr bool STAYS = stays<TO>();
     const uint32_t all = across * along * parts, die = blockIdx.x % 8, share = all / 8, more = all % 8;
-    const uint32_t tiles_end = (die + 1) * share + (die < more ? die + 1 : more), next = (gridDim.x - die + 7) / 8;
-    uint32_t now = die * share + (die < more ? die : more) + blockIdx.x / 8;
-    if (now >= tiles_end) return;
-    int64_t i0, j0, first, last;
-    uint32_t part;
+    const uint32_t tiles_end = (die + 1) * share + (die < more ? die + 1 : more), stride = (gridDim.x - die + 7) / 8;
+    const uint32_t tile_first = die * share + (die < more ? die : more) + blockIdx.x / 8;
+    if (tile_first >= tiles_end) return;
+    struct place {
+        int64_t i, j, first, length;
+        uint32_t part;
+    };
+    const auto place_of = [&](uint32_t tile) {
+        place at;
+        at.part = tile / (across * along);
+        const uint32_t in = tile % (across * along);
+        at.i = (int64_t)(in % across) * (TO == TO_GATED ? TI / 2 : TI), at.j = (int64_t)(in / across) * TJ;
+        at.first = at.part * depth_part;
+        at.length = P.depth - at.first < depth_part ? P.depth - at.first : depth_part;
+        return at;
+    };
 
     typename ptile::template stream<TO == TO_GATED ? 2 : 1, TI / WI> pstream;
     typename qtile::template stream<1, TJ> qstream;
     staged_codes<TI, STEP, THREADS> through;
-    const uint8_t *byte_at[FJ];
-    scale_run bytes[FJ];
-    if constexpr (PKIND == CODES_ACROSS) through.init(P);
+    if constexpr (THROUGH) through.init(P);
     else pstream.init(P, wave, lane);
     qstream.init(Q, wave, lane);
 
+    // What is fetched next: k_left values of k of tile `tile_ahead` (none: no tiles are left).
+    uint32_t tile_ahead = tile_first;
+    int64_t k_left = 0;
     const auto aim = [&] {
-        part = now / (across * along);
-        const uint32_t in = now % (across * along);
-        i0 = (int64_t)(in % across) * (TO == TO_GATED ? TI / 2 : TI), j0 = (int64_t)(in / across) * TJ;
-        first = part * depth_part, last = first + depth_part < P.depth ? first + depth_part : P.depth;
-        if constexpr (PKIND == CODES_ACROSS) through.aim(P, i0, first, last);
-        else pstream.aim(P, TO == TO_GATED ? R.columns : P.rows, i0, first, last, R.columns * P.stride * 2);
-        qstream.aim(Q, Q.rows, j0, first, last, 0);
+        const place at = place_of(tile_ahead);
+        if constexpr (THROUGH) through.aim(P, at.i, at.first, at.first + at.length);
+        else pstream.aim(P, TO == TO_GATED ? R.columns : P.rows, at.i, at.first, at.first + at.length, R.columns * P.stride * 2);
+        qstream.aim(Q, Q.rows, at.j, at.first, at.first + at.length, 0);
+        k_left = at.length;
     };
-    // Starts the fetch of a step's tiles, k values of k from the end.
-    const auto start = [&](int64_t k, lds_byte *to) {
-        if constexpr (PKIND == CODES_ACROSS) through.fetch();
-        else pstream.fetch(k, wave, lane, to);
-        qstream.fetch(k, wave, lane, to + ptile::BYTES);
+    // The next step's fetch, made ready, in FETCHES pieces, and done.
+    constexpr int FETCHES = THROUGH ? 1 + qtile::EACH : ptile::EACH + qtile::EACH;
+    const auto ready = [&] {
+        if constexpr (!THROUGH) pstream.ready(k_left, wave, lane);
+        qstream.ready(k_left, wave, lane);
     };
-    const auto start_scales = [&] {
+    const auto fetch = [&](int piece, int to) {
+        constexpr int OF_P = THROUGH ? 1 : ptile::EACH;
+        if (piece >= OF_P) {
+            qstream.fetch(piece - OF_P, wave, lds + to + ptile::BYTES);
+        } else {
+            if constexpr (THROUGH) through.fetch();
+            else pstream.fetch(piece, wave, lds + to);
+        }
+    };
+    const auto fetched = [&] {
+        k_left -= STEP;
+        if (k_left <= 0) {
+            tile_ahead += stride;
+            k_left = 0;
+            if (STAYS && tile_ahead < tiles_end) aim();
+        }
+    };
+    aim();
+
+    f32x16 acc[FI][FJ];
+    scale_run bytes[FJ];
+    const auto scales_of = [&](int64_t j, int64_t g) {
         if constexpr (QKIND == CODES_ALONG) {
 #pragma unroll
             for (int t = 0; t < FJ; ++t) {
-                const int64_t j = j0 + (wj * FJ + t) * 32 + lane % 32;
-                byte_at[t] = Q.scales + (j < Q.rows ? j : Q.rows - 1) * Q.groups;
-                bytes[t].load(byte_at[t], Q.groups);
+                const int64_t row = j + (wj * FJ + t) * 32 + lane % 32;
+                bytes[t].load(Q.scales + (row < Q.rows ? row : Q.rows - 1) * Q.groups + g, Q.groups - g);
             }
         }
     };
-    f32x16 acc[FI][FJ];
-    // A step in turns of 16 values of k: a turn's operands are read while the turn before is multiplied.
-    const auto multiply = [&](const lds_byte *ptile_at, const lds_byte *qtile_at) {
-        constexpr int TURNS = 2 * RUNS;
-        bf16x8 p[2][FI], q[2][FJ][2];
-        const auto read = [&](int turn) {
-            const int run = turn / 2, s = turn % 2;
+    const auto clear = [&] {
 #pragma unroll
-            for (int t = 0; t < FJ; ++t) {
-                const int r = (wj * FJ + t) * 32;
-                if constexpr (QKIND == CODES_ALONG) {
-                    if (s == 0) qtile::read_codes(qtile_at, r, run, lane, bytes[t].byte(run), q[run % 2][t]);
-                } else {
-                    q[run % 2][t][s] = qtile::read(qtile_at, r, run, s, lane);
-                }
+        for (int f = 0; f < FI; ++f)
+#pragma unroll
+            for (int t = 0; t < FJ; ++t) acc[f][t] = f32x16{};
+    };
+    bf16x8 p[2][FI], q[2][FJ];
+    u32x4 codes[FJ];
+    const auto read = [&](int turn, int at) {
+        const int run = turn / 2, s = turn % 2;
+#pragma unroll
+        for (int f = 0; f < FI; ++f) p[s][f] = ptile::read(lds + at, (wi * FI + f) * 32, run, s, lane);
+#pragma unroll
+        for (int t = 0; t < FJ; ++t) {
+            const int first = (wj * FJ + t) * 32;
+            if constexpr (QKIND == CODES_ALONG) {
+                if (s == 0) codes[t] = qtile::read_codes(lds + at + ptile::BYTES, first, run, lane);
+                q[s][t] = qtile::widen(codes[t][2 * s], codes[t][2 * s + 1], __uint_as_float(bytes[t].byte(run) << 23));
+            } else {
+                q[s][t] = qtile::read(lds + at + ptile::BYTES, first, run, s, lane);
             }
-#pragma unroll
-            for (int f = 0; f < FI; ++f) p[turn % 2][f] = ptile::read(ptile_at, (wi * FI + f) * 32, run, s, lane);
-        };
-        read(0);
-#pragma unroll
-        for (int turn = 0; turn < TURNS; ++turn) {
-            if (turn + 1 < TURNS) read(turn + 1);
-            __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-            for (int f = 0; f < FI; ++f)
-#pragma unroll
-                for (int t = 0; t < FJ; ++t)
-                    acc[f][t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(p[turn % 2][f], q[turn / 2 % 2][t][turn % 2], acc[f][t], 0, 0, 0);
         }
     };
-    // The tile's results, through the buffer that was multiplied last.  A wave's: rows j_wave .. , columns i_wave .. .
-    const auto write = [&](int64_t i0, int64_t j0, uint32_t part, lds_byte *area) {
-        const int64_t j_wave = j0 + wj * FJ * 32, i_wave = i0 + wi * (TO == TO_GATED ? FI / 2 : FI) * 32, groups = groups_of(R.columns);
-        area += wave * (TO == TO_GATE_GRAD ? FI * 4096 : FI * 2048);
+    // A tile's results, through the buffer that was multiplied last.  A wave's: rows j_wave .. , columns i_wave .. .
+    const auto write = [&](const place &of, lds_byte *area) {
+        const int64_t j_wave = of.j + wj * FJ * 32, i_wave = of.i + wi * (TO == TO_GATED ? FI / 2 : FI) * 32, groups = groups_of(R.columns);
+        area += wave * (TO == TO_GATE_GRAD ? FI * 4096 : AREA);
         // addresses are formed here: worked out ahead of the tiles they would take registers from the products
         int lane = threadIdx.x % 64;
         asm volatile("" : "+v"(lane));
         const int half = lane / 32;
-        __syncthreads();
         if constexpr (TO == TO_WIDE || TO == TO_FULL) {
-            using room = exchange<FI * 64>;                          // FI * 32 values of 16 bits, or half as many of 32
-            constexpr int SIZE = TO == TO_WIDE ? 2 : 4, AT_ONCE = TO == TO_WIDE ? FI : FI / 2;
+            using room = exchange<128>;                              // 64 values of 16 bits, or 32 of 32
+            constexpr int SIZE = TO == TO_WIDE ? 2 : 4, AT_ONCE = 4 / SIZE;
             const room x{area};
-            landing to((uint8_t *)R.out + (TO == TO_FULL ? part * R.part * SIZE : 0), j_wave, Q.rows, R.stride * SIZE, i_wave * SIZE,
+            landing to((uint8_t *)R.out + (TO == TO_FULL ? of.part * R.part * SIZE : 0), j_wave, Q.rows, R.stride * SIZE, i_wave * SIZE,
                        P.rows * SIZE, FI * 32 * SIZE);
             if (parts > 1) to.past = false;                          // they are read again at once
 #pragma unroll
@@ -573,40 +593,34 @@ __global__ __launch_bounds__(WI * WJ * 64, WI * WJ > 4 ? 1 : 2) void k_product(o
             const landing gated(R.gated_codes, j_wave, Q.rows, R.columns, i_wave, R.columns, COLUMNS);
             const landing kept_g(R.kept_codes, j_wave, Q.rows, 2 * R.columns, i_wave, R.columns, COLUMNS);
             const landing kept_p(R.kept_codes, j_wave, Q.rows, 2 * R.columns, R.columns + i_wave, 2 * R.columns, COLUMNS);
+            static_assert(2 * ARRAY <= AREA, "two arrays of a group of rows at a time");
 #pragma unroll
             for (int t = 0; t < FJ; ++t) {
-                uint32_t byte[3][FI / 2];
+                const int64_t j = j_wave + t * 32 + lane % 32, g0 = i_wave / GROUP;
+                // columns beyond the end hold zeros: their rows of the weight read as such
+                const auto pack = [&](const f32x16 &v, int f, int slot, uint8_t *scales, bool mine) {
+                    const uint32_t byte = scale_byte(group_magnitude(v));
+                    room{area + slot * ARRAY}.put(lane % 32, f * 2 + half, encode_group(v, byte));
+                    if (mine && j < Q.rows && g0 + f < groups) scales[g0 + f] = (uint8_t)byte;
+                };
 #pragma unroll
                 for (int f = 0; f < FI / 2; ++f) {
                     const f32x16 &g = acc[f][t], &p = acc[f + FI / 2][t];
                     f32x16 a;
 #pragma unroll
                     for (int x = 0; x < 16; ++x) a[x] = g[x] * sigmoid(g[x]) * p[x];
-                    // columns beyond the end hold zeros: their rows of the weight read as such
-                    const auto pack = [&](const f32x16 &v, int array) {
-                        byte[array][f] = scale_byte(group_magnitude(v));
-                        room{area + array * ARRAY}.put(lane % 32, f * 2 + half, encode_group(v, byte[array][f]));
-                    };
-                    pack(a, 0);
-                    if (R.kept_codes) pack(g, 1), pack(p, 2);
-                }
-                const int64_t j = j_wave + t * 32 + lane % 32, g0 = i_wave / GROUP;
-                // the halves of the wave write an array each, then the second one the third
-                const auto scales = [&](uint8_t *to, int array, bool mine) {
-#pragma unroll
-                    for (int f = 0; f < FI / 2; ++f)
-                        if (mine && j < Q.rows && g0 + f < groups) to[f] = (uint8_t)byte[array][f];
-                };
-                scales(R.gated_scales + j * groups + g0, 0, half == 0);
-                if (R.kept_codes) {
-                    scales(R.kept_scales + 2 * j * groups + g0, 1, half == 1);
-                    scales(R.kept_scales + (2 * j + 1) * groups + g0, 2, half == 0);
+                    pack(a, f, 0, R.gated_scales + j * groups, half == 0);
+                    if (R.kept_codes) pack(g, f, 1, R.kept_scales + 2 * j * groups, half == 1);
                 }
                 room::turn();
                 gated.template write<1, false>(room{area}, t * 32, 0, lane);
                 if (R.kept_codes) {
                     kept_g.template write<1, false>(room{area + ARRAY}, t * 32, 0, lane);
-                    kept_p.template write<1, false>(room{area + 2 * ARRAY}, t * 32, 0, lane);
+                    room::turn();
+#pragma unroll
+                    for (int f = 0; f < FI / 2; ++f) pack(acc[f + FI / 2][t], f, 0, R.kept_scales + (2 * j + 1) * groups, half == 0);
+                    room::turn();
+                    kept_p.template write<1, false>(room{area}, t * 32, 0, lane);
                 }
                 room::turn();
                 __builtin_amdgcn_sched_barrier(0);
@@ -680,45 +694,61 @@ __global__ __launch_bounds__(WI * WJ * 64, WI * WJ > 4 ? 1 : 2) void k_product(o
         }
     };
 
-    aim();
-    start(last - first, lds);
-    start_scales();
-    if constexpr (PKIND == CODES_ACROSS) through.store(lds);
-    for (int at = 0;;) {                             // offset of the step's tiles
+    ready();
 #pragma unroll
-        for (int f = 0; f < FI; ++f)
-#pragma unroll
-            for (int t = 0; t < FJ; ++t) acc[f][t] = f32x16{};
-        const int64_t i_now = i0, j_now = j0, length = last - first, k_first = first;
-        const uint32_t part_now = part;
-        bool more_tiles = true;
-        for (int64_t k = 0; k < length; k += STEP, at = BUFFER - at) {
+    for (int e = 0; e < FETCHES; ++e) fetch(e, 0);
+    fetched();
+    if constexpr (THROUGH) through.store(lds);
+    place now = place_of(tile_first);
+    scales_of(now.j, now.first / GROUP);
+    for (uint32_t tile = tile_first, at = 0;;) {
+        clear();
+        for (int64_t k = 0; k < now.length; k += STEP, at = BUFFER - at) {
             __builtin_amdgcn_s_waitcnt(0x0070);      // vmcnt(0) lgkmcnt(0): what this wave fetched and stored has arrived
             __syncthreads();
-            // the other buffer, which every wave is done with, takes the next step's tiles
-            const bool ends = k + STEP >= length;
-            if (ends) {
-                now += next;
-                more_tiles = STAYS && now < tiles_end;
-                if (more_tiles) aim();
+            const bool ahead = k_left > 0;           // the other buffer, which every wave is done with, takes the next step's tiles
+            const int other = BUFFER - at;
+            read(0, at);
+            if (ahead) ready();
+            __builtin_amdgcn_sched_barrier(0);
+            if (ahead) {
+#pragma unroll
+                for (int e = 0; e < FETCHES; ++e) fetch(e, other);
             }
-            if (more_tiles) start(ends ? last - first : length - k - STEP, lds + (BUFFER - at));
-            multiply(lds + at, lds + at + ptile::BYTES);
-            if constexpr (PKIND == CODES_ACROSS) {
-                if (more_tiles) through.store(lds + (BUFFER - at));
+#pragma unroll
+            for (int turn = 0; turn < TURNS; ++turn) {
+                if (turn + 1 < TURNS) read(turn + 1, at);
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int f = 0; f < FI; ++f)
+#pragma unroll
+                    for (int t = 0; t < FJ; ++t) acc[f][t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(p[turn % 2][f], q[turn % 2][t], acc[f][t], 0, 0, 0);
+            }
+            if (ahead) {
+                fetched();
+                if constexpr (THROUGH) through.store(lds + other);
             }
             if constexpr (QKIND == CODES_ALONG) {
-                const int64_t g = (k_first + k + STEP) / GROUP;
+                const int64_t g = (now.first + k + STEP) / GROUP;
+                if (k + STEP < now.length) {
+                    if (g % 16 == 0) scales_of(now.j, g);
+                    else {
 #pragma unroll
-                for (int t = 0; t < FJ; ++t) {
-                    bytes[t].template pass<RUNS>();
-                    if (!ends && g % 16 == 0) bytes[t].load(byte_at[t] + g, Q.groups - g);
+                        for (int t = 0; t < FJ; ++t) bytes[t].template pass<STEP / GROUP>();
+                    }
                 }
             }
         }
-        if (more_tiles) start_scales();
-        write(i_now, j_now, part_now, STAYS ? lds + (BUFFER - at) : lds);
-        if (!more_tiles) break;
+        const place done = now;
+        tile += stride;
+        const bool on = STAYS && tile < tiles_end;
+        if (on) {
+            now = place_of(tile);
+            scales_of(now.j, now.first / GROUP);
+        }
+        __syncthreads();
+        write(done, STAYS ? lds + (BUFFER - at) : lds);
+        if (!on) break;
     }
 }
 
