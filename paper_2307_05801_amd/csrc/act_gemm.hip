@@ -12,24 +12,42 @@ constexpr int BLOCK = 256;
 
 // ---- operands laid out for the product ----
 
-// to[r] <- from[r], `bytes` long, then zeros up to `pitch` (a multiple of 16)
-__global__ __launch_bounds__(BLOCK) void k_lay_out(const uint8_t *__restrict__ from, int64_t stride, int64_t rows, int64_t bytes, uint8_t *__restrict__ to,
-                                                   int64_t pitch, divider pieces, int64_t row0)
+// An array whose rows, `bytes` long, are copied to rows of `pitch` bytes (a multiple of 16) with zeros at their ends.
+struct copied_rows {
+    const uint8_t *from;
+    uint8_t *to;
+    int64_t stride, rows, bytes, pitch;
+    divider pieces;              // of 16 bytes, of a row
+    uint32_t blocks;             // that copy it
+};
+
+struct copies {
+    copied_rows of[3];
+};
+
+__global__ __launch_bounds__(BLOCK) void k_lay_out(copies C)
 {
-    const uint32_t q = blockIdx.x * (uint32_t)BLOCK + threadIdx.x, in = pieces(q);
-    const int64_t row = row0 + in, at = (int64_t)(q - in * pieces.by) * 16;
-    if (row >= rows) return;
+    uint32_t block = blockIdx.x;
+    int c = 0;
+    while (c < 2 && block >= C.of[c].blocks) block -= C.of[c++].blocks;
+    const copied_rows &A = C.of[c];
+    // a block's first piece may lie beyond 32 bits, what it holds of rows may not
+    const int64_t first = (int64_t)block * BLOCK, row0 = first / A.pieces.by;
+    const uint32_t q = (uint32_t)(first - row0 * A.pieces.by) + threadIdx.x, in = A.pieces(q);
+    const int64_t row = row0 + in, at = (int64_t)(q - in * A.pieces.by) * 16;
+    if (row >= A.rows) return;
     uint8_t piece[16] = {};
-    if (bytes - at >= 16) {
-        __builtin_memcpy(piece, from + row * stride + at, 16);
+    if (A.bytes - at >= 16) {
+        __builtin_memcpy(piece, A.from + row * A.stride + at, 16);
     } else {
 #pragma unroll
         for (int i = 0; i < 15; ++i)
-            if (at + i < bytes) piece[i] = from[row * stride + at + i];
+            if (at + i < A.bytes) piece[i] = A.from[row * A.stride + at + i];
     }
-    __builtin_memcpy(to + row * pitch + at, piece, 16);
+    __builtin_memcpy(A.to + row * A.pitch + at, piece, 16);
 }
 
+int64_t cut(int64_t n, int64_t by) { return (n + by - 1) / by; }
 int64_t up16(int64_t n) { return (n + 15) / 16 * 16; }
 
 // Memory rows as the product takes them: as they are, or a copy of them in the workspace.
@@ -44,30 +62,31 @@ struct laid {
     }
     int64_t room() const { return copied ? rows * pitch : 0; }
 
-    // The copy, at `to`, which moves on.
-    int lay_out(uint8_t *&to, hipStream_t st)
-    {
-        if (!copied) return LEAP_OK;
-        const int64_t pieces = pitch / 16, most = ((int64_t)1 << 30) / pieces;
-        for (int64_t row0 = 0; row0 < rows; row0 += most) {
-            const int64_t part = rows - row0 < most ? rows - row0 : most;
-            hipLaunchKernelGGL(k_lay_out, dim3((unsigned)((part * pieces + BLOCK - 1) / BLOCK)), dim3(BLOCK), 0, st, data, stride, rows, bytes, to, pitch,
-                               divider((uint32_t)pieces), row0);
-            const int rc = launched();
-            if (rc != LEAP_OK) return rc;
-        }
-        data = to, stride = pitch, copied = false;
-        to += rows * pitch;
-        return LEAP_OK;
-    }
-
     operand wide(int64_t i, int64_t k) const { return {data, nullptr, stride / 2, 0, i, k}; }
     operand codes(const uint8_t *scales, int64_t cols, int64_t i, int64_t k) const { return {data, scales, stride, groups_of(cols), i, k}; }
 };
 
-// ---- launches ----
+// The copies of up to three arrays, into `room` one after the other, which moves on.
+int lay_out(uint8_t *&room, hipStream_t st, laid *a, laid *b = nullptr, laid *c = nullptr)
+{
+    copies C = {{{nullptr, nullptr, 0, 0, 0, 16, divider(1), 0}, {nullptr, nullptr, 0, 0, 0, 16, divider(1), 0}, {nullptr, nullptr, 0, 0, 0, 16, divider(1), 0}}};
+    int64_t blocks = 0;
+    int n = 0;
+    for (laid *x : {a, b, c}) {
+        if (!x || !x->copied) continue;
+        const int64_t mine = cut(x->rows * (x->pitch / 16), BLOCK);
+        blocks += mine;
+        if (blocks > 0x7fffffff) return refuse("more values to lay out than one launch covers");
+        C.of[n++] = {x->data, room, x->stride, x->rows, x->bytes, x->pitch, divider((uint32_t)(x->pitch / 16)), (uint32_t)mine};
+        x->data = room, x->stride = x->pitch, x->copied = false;
+        room += x->rows * x->pitch;
+    }
+    if (!n) return LEAP_OK;
+    hipLaunchKernelGGL(k_lay_out, dim3((unsigned)blocks), dim3(BLOCK), 0, st, C);
+    return launched();
+}
 
-int64_t cut(int64_t n, int64_t by) { return (n + by - 1) / by; }
+// ---- launches ----
 
 // Tiles of 256 x 256, eight waves and a block a compute unit; or of 128 x 128, four waves and two blocks, at 0.8 of the rate (262144 x
 // 512 -> 1024, y: 339 and 411 us) but with less left over where tiles are few.  In units of the time of a large tile, 256 units
@@ -77,15 +96,15 @@ bool large_tiles(int64_t i, int64_t j)
     return (double)cut(cut(i, 256) * cut(j, 256), 256) <= 0.62 * (double)cut(cut(i, 128) * cut(j, 128), 512);
 }
 
-template <int PKIND, int QKIND, int TO, int TI, int TJ, int WI, int WJ>
+template <int PKIND, int QKIND, int TO, int TI, int TJ, int WI, int WJ, int GROUPS>
 int launch(const operand &P, const operand &Q, const result &R, int64_t depth_part, hipStream_t st)
 {
     const int64_t across = TO == TO_GATED ? cut(R.columns, TI / 2) : cut(P.rows, TI), along = cut(Q.rows, TJ), parts = depth_part ? cut(P.depth, depth_part) : 1;
     if (across * along * parts > 0x7fffffff) return refuse("more rows and columns than one launch covers");
     // as many blocks as the 256 compute units hold at once, by shared memory and registers
-    constexpr int RESIDENT = WI * WJ > 4 ? 1 : 2;
-    const int64_t blocks = !stays<TO>() || across * along * parts < 256 * RESIDENT ? across * along * parts : 256 * RESIDENT;
-    hipLaunchKernelGGL((k_product<PKIND, QKIND, TO, TI, TJ, WI, WJ>), dim3((unsigned)blocks), dim3(WI * WJ * 64), 0, st, P, Q, R, (uint32_t)across,
+    constexpr int RESIDENT = WI * WJ * GROUPS > 4 ? 1 : 2;
+    const int64_t blocks = !stays<TO>() || GROUPS > 1 || across * along * parts < 256 * RESIDENT ? across * along * parts : 256 * RESIDENT;
+    hipLaunchKernelGGL((k_product<PKIND, QKIND, TO, TI, TJ, WI, WJ, GROUPS>), dim3((unsigned)blocks), dim3(WI * WJ * GROUPS * 64), 0, st, P, Q, R, (uint32_t)across,
                        (uint32_t)along, (uint32_t)parts, depth_part ? depth_part : P.depth);
     return launched();
 }
@@ -94,8 +113,10 @@ template <int PKIND, int QKIND, int TO> int product(const operand &P, const oper
 {
     // the gate's gradient moves more than it multiplies: small tiles always (262144 x 512 -> 2 * 512: 300 us, large ones 369)
     if constexpr (TO != TO_GATE_GRAD)
-        if (large) return launch<PKIND, QKIND, TO, 256, 256, 2, 4>(P, Q, R, depth_part, st);
-    return launch<PKIND, QKIND, TO, 128, 128, 2, 2>(P, Q, R, depth_part, st);
+        if (large) return launch<PKIND, QKIND, TO, 256, 256, 2, 4, 1>(P, Q, R, depth_part, st);
+    if constexpr (PKIND != CODES_ACROSS)
+        if (cut(TO == TO_GATED ? 2 * R.columns : P.rows, 128) * cut(Q.rows, 128) <= 256) return launch<PKIND, QKIND, TO, 128, 128, 2, 2, 2>(P, Q, R, depth_part, st);
+    return launch<PKIND, QKIND, TO, 128, 128, 2, 2, 1>(P, Q, R, depth_part, st);
 }
 
 template <int PKIND, int QKIND, int TO> int product(const operand &P, const operand &Q, const result &R, hipStream_t st)
@@ -110,9 +131,10 @@ struct weight_plan {
     int64_t parts, depth_part;
     weight_plan(int64_t rows, int64_t cols, int64_t out)
     {
-        const int64_t tiles = cut(cols, 256) * cut(out, 256);
-        large = tiles * cut(rows, 1024) >= 256;
-        const int64_t t = large ? tiles : cut(cols, 128) * cut(out, 128), want = (large ? 256 : 512) / t;
+        const int64_t tiles = cut(cols, 256) * cut(out, 256), small = cut(cols, 128) * cut(out, 128);
+        // a small tile takes 0.31 of a large one's time; what of a tile lies beyond the edges is work for nothing
+        large = tiles * cut(rows, 1024) >= 256 && (double)tiles <= 0.31 * (double)small;
+        const int64_t t = large ? tiles : small, want = (large ? 256 : 512) / t;
         parts = want < 1 ? 1 : want;
         if (parts > cut(rows, 512)) parts = cut(rows, 512);
         if (parts < 1) parts = 1;
@@ -123,23 +145,38 @@ struct weight_plan {
     int64_t room(int64_t cols, int64_t out) const { return parts > 1 ? up16(parts * cols * out * (int64_t)sizeof(float)) : 0; }
 };
 
+// to <- the sum of the parts, in a fixed order: 16 threads to four values each, which add every 16th part, 64 values a block.
+constexpr int ADDED = 64;
+
 __global__ __launch_bounds__(BLOCK) void k_add_parts(const float *__restrict__ from, int64_t parts, int64_t n, uint16_t *__restrict__ to)
 {
-    const int64_t at = ((int64_t)blockIdx.x * BLOCK + threadIdx.x) * 4;
-    if (at >= n) return;
-    float sum[4] = {};
+    constexpr int WAYS = BLOCK / (ADDED / 4);
+    __shared__ float room[WAYS][ADDED];
+    const int way = threadIdx.x / (ADDED / 4), in = threadIdx.x % (ADDED / 4) * 4;
+    const int64_t at = (int64_t)blockIdx.x * ADDED + in;
     const int left = n - at < 4 ? (int)(n - at) : 4;
-    for (int64_t p = 0; p < parts; ++p) {
-        if (left == 4) {
+    float sum[4] = {};
+    if (left == 4) {
+#pragma unroll 4
+        for (int64_t p = way; p < parts; p += WAYS) {
             float f[4];
             __builtin_memcpy(f, from + p * n + at, 16);
 #pragma unroll
             for (int x = 0; x < 4; ++x) sum[x] += f[x];
-        } else {
-            for (int x = 0; x < left; ++x) sum[x] += from[p * n + at + x];
         }
+    } else {
+        for (int64_t p = way; p < parts; p += WAYS)
+            for (int x = 0; x < left; ++x) sum[x] += from[p * n + at + x];
     }
-    for (int x = 0; x < left; ++x) to[at + x] = element<LEAP_BF16>::from_float(sum[x]);
+#pragma unroll
+    for (int x = 0; x < 4; ++x) room[way][in + x] = sum[x];
+    __syncthreads();
+    if (threadIdx.x < ADDED && (int64_t)blockIdx.x * ADDED + threadIdx.x < n) {
+        float total = 0.0f;
+#pragma unroll
+        for (int w = 0; w < WAYS; ++w) total += room[w][threadIdx.x];
+        to[(int64_t)blockIdx.x * ADDED + threadIdx.x] = element<LEAP_BF16>::from_float(total);
+    }
 }
 
 // ---- the gate by itself ----
@@ -193,8 +230,7 @@ extern "C" int leap_linear8(const uint8_t *d_codes, const uint8_t *d_scales, int
     const hipStream_t st = stream_of(hip_stream);
     uint8_t *room = (uint8_t *)d_work;
     laid W(d_weight, w_stride, out, cols, 2), X(d_codes, cols, rows, cols, 1);
-    int rc = W.lay_out(room, st);
-    if (rc == LEAP_OK) rc = X.lay_out(room, st);
+    const int rc = lay_out(room, st, &W, &X);
     if (rc != LEAP_OK) return rc;
     result R{};
     R.out = d_y, R.stride = out;
@@ -220,26 +256,22 @@ extern "C" int leap_linear8_backward(const void *d_dy, int64_t dy_stride, const 
     if (!d_work && leap_linear8_backward_work(d_dy, dy_stride, d_codes, rows, cols, d_weight, w_stride, out)) return refuse("null workspace");
     const hipStream_t st = stream_of(hip_stream);
     uint8_t *room = (uint8_t *)d_work;
-    laid G(d_dy, dy_stride, rows, out, 2);
-    int rc = G.lay_out(room, st);
+    laid G(d_dy, dy_stride, rows, out, 2), W(d_weight, w_stride, out, cols, 2), X(d_codes, cols, rows, cols, 1);
+    int rc = lay_out(room, st, &G, d_grad_x && rows ? &W : nullptr, d_grad_weight ? &X : nullptr);
     if (rc == LEAP_OK && d_grad_x && rows) {
-        laid W(d_weight, w_stride, out, cols, 2);
-        rc = W.lay_out(room, st);
-        if (rc != LEAP_OK) return rc;
         result R{};
         R.out = d_grad_x, R.stride = cols;
         const operand P = W.wide(cols, out), Q = G.wide(rows, out);
         rc = grad_x_type == LEAP_F32 ? product<WIDE_ACROSS, WIDE_ALONG, TO_FULL>(P, Q, R, st) : product<WIDE_ACROSS, WIDE_ALONG, TO_WIDE>(P, Q, R, st);
     }
     if (rc != LEAP_OK || !d_grad_weight) return rc;
-    const dim3 adders((unsigned)cut(cols * out, 4 * BLOCK));
+    const int64_t added = cut(cols * out, ADDED);
+    if (added > 0x7fffffff) return refuse("a weight of more than 2^37 values");
+    const dim3 adders((unsigned)added);
     if (!rows) {                                     // a sum of nothing
         hipLaunchKernelGGL(k_add_parts, adders, dim3(BLOCK), 0, st, (const float *)nullptr, (int64_t)0, cols * out, (uint16_t *)d_grad_weight);
         return launched();
     }
-    laid X(d_codes, cols, rows, cols, 1);
-    rc = X.lay_out(room, st);
-    if (rc != LEAP_OK) return rc;
     const weight_plan plan(rows, cols, out);
     const operand P = X.codes(d_scales, cols, cols, rows), Q = G.wide(out, rows);
     result R{};
@@ -269,8 +301,7 @@ extern "C" int leap_gated_linear8(const uint8_t *d_codes, const uint8_t *d_scale
     const hipStream_t st = stream_of(hip_stream);
     uint8_t *room = (uint8_t *)d_work;
     laid W(d_weight, w_stride, 2 * out, cols, 2), X(d_codes, cols, rows, cols, 1);
-    int rc = W.lay_out(room, st);
-    if (rc == LEAP_OK) rc = X.lay_out(room, st);
+    const int rc = lay_out(room, st, &W, &X);
     if (rc != LEAP_OK) return rc;
     result R{};
     R.columns = out, R.gated_codes = d_gated_codes, R.gated_scales = d_gated_scales, R.kept_codes = d_kept_codes, R.kept_scales = d_kept_scales;
@@ -310,8 +341,7 @@ extern "C" int leap_linear_gate8_backward(const void *d_dy, int64_t dy_stride, c
     const hipStream_t st = stream_of(hip_stream);
     uint8_t *room = (uint8_t *)d_work;
     laid W(d_weight, w_stride, next, out, 2), G(d_dy, dy_stride, rows, next, 2);
-    int rc = W.lay_out(room, st);
-    if (rc == LEAP_OK) rc = G.lay_out(room, st);
+    const int rc = lay_out(room, st, &W, &G);
     if (rc != LEAP_OK) return rc;
     result R{};
     R.out = d_du, R.columns = out, R.kept_codes = (uint8_t *)d_kept_codes, R.kept_scales = (uint8_t *)d_kept_scales;

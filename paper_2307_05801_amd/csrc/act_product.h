@@ -108,12 +108,12 @@ template <int KIND, int T, int STEP, int THREADS> struct tile {
         }
 
         // Rows from row0 on, k from `first` on, of an operand that ends at `rows` and at k = `last`.
-        __device__ inline void aim(const operand &O, int64_t rows, int64_t row0, int64_t first, int64_t last, int64_t apart)
+        __device__ inline void aim(const operand &O, int64_t rows, int64_t row0, int64_t first, int64_t last, int64_t apart, int every)
         {
             if constexpr (KIND == WIDE_ACROSS)
-                at = {O.data + (first * O.stride + row0) * 2, ((last - 1 - first) * O.stride + whole(rows, 8) - row0) * 2, (uint32_t)(STEP * O.stride * 2)};
+                at = {O.data + (first * O.stride + row0) * 2, ((last - 1 - first) * O.stride + whole(rows, 8) - row0) * 2, (uint32_t)(every * STEP * O.stride * 2)};
             else
-                at = {O.data + (row0 * O.stride + first) * VALUE, ((rows - 1 - row0) * O.stride + whole(last, 16 / VALUE) - first) * VALUE, STEP * VALUE};
+                at = {O.data + (row0 * O.stride + first) * VALUE, ((rows - 1 - row0) * O.stride + whole(last, 16 / VALUE) - first) * VALUE, (uint32_t)(every * STEP * VALUE)};
             other = at.base + apart;
         }
 
@@ -174,17 +174,20 @@ template <int T, int STEP, int THREADS> struct staged_codes {
     uint32_t offset, scale_offset, stride, groups;
     window at, scales;
 
-    __device__ inline void init(const operand &O)
+    int thread;                                        // of the group
+
+    __device__ inline void init(const operand &O, int thread_)
     {
-        const uint32_t k = threadIdx.x / (T / 8), i = threadIdx.x % (T / 8) * 8;
+        thread = thread_;
+        const uint32_t k = thread / (T / 8), i = thread % (T / 8) * 8;
         stride = (uint32_t)O.stride * ROWS, groups = (uint32_t)O.groups * ROWS;
         offset = k * (uint32_t)O.stride + i, scale_offset = k * (uint32_t)O.groups + i / GROUP;
     }
 
-    __device__ inline void aim(const operand &O, int64_t row0, int64_t first, int64_t last)
+    __device__ inline void aim(const operand &O, int64_t row0, int64_t first, int64_t last, int every)
     {
-        at = {O.data + first * O.stride + row0, (last - 1 - first) * O.stride + whole(O.rows, 16) - row0, (uint32_t)(STEP * O.stride)};
-        scales = {O.scales + first * O.groups + row0 / GROUP, (last - first) * O.groups - row0 / GROUP, (uint32_t)(STEP * O.groups)};
+        at = {O.data + first * O.stride + row0, (last - 1 - first) * O.stride + whole(O.rows, 16) - row0, (uint32_t)(every * STEP * O.stride)};
+        scales = {O.scales + first * O.groups + row0 / GROUP, (last - first) * O.groups - row0 / GROUP, (uint32_t)(every * STEP * O.groups)};
     }
 
     __device__ inline void fetch()
@@ -201,7 +204,7 @@ template <int T, int STEP, int THREADS> struct staged_codes {
     __device__ inline void store(lds_byte *to) const
     {
         using as = tile<WIDE_ACROSS, T, STEP, THREADS>;
-        const int k = threadIdx.x / (T / 8), chunk = threadIdx.x % (T / 8);
+        const int k = thread / (T / 8), chunk = thread % (T / 8);
 #pragma unroll
         for (int e = 0; e < EACH; ++e)
             *(__attribute__((address_space(3))) bf16x8 *)(to + (k + e * ROWS) * (T * 2) + (chunk ^ ((k + e * ROWS) % 4 * 4)) * 16) =
@@ -413,10 +416,14 @@ struct scale_run {
         }
     }
     __device__ inline uint32_t byte(int i) const { return w[0] >> (8 * i) & 255u; }
-    template <int N> __device__ inline void pass()
+    template <int N> __device__ inline void pass()               // over N of them
     {
+        static_assert(N <= 4, "");
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = __builtin_amdgcn_alignbyte(i < 3 ? w[i + 1] : 0u, w[i], N);
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t above = i < 3 ? w[i + 1] : 0u;
+            w[i] = N == 4 ? above : __builtin_amdgcn_alignbyte(above, w[i], N);
+        }
     }
 };
 
@@ -439,20 +446,24 @@ struct result {
 //
 // A step is multiplied in turns of 16 values of k.  What a turn takes is read while the turn before is multiplied; the next
 // step's fetches are started while the first turn's operands are on their way from shared memory.
-template <int PKIND, int QKIND, int TO, int TI, int TJ, int WI, int WJ>
-__global__ __launch_bounds__(WI * WJ * 64, WI * WJ > 4 ? 1 : 2) void k_product(operand P, operand Q, result R, uint32_t across, uint32_t along, uint32_t parts,
+//
+// Where tiles are few, GROUPS of WI x WJ waves share one: each takes every GROUPS-th step, by itself but for the meetings, and
+// their sums are added through shared memory at the end.  A wave alone on its unit spends two thirds of a step waiting.
+template <int PKIND, int QKIND, int TO, int TI, int TJ, int WI, int WJ, int GROUPS>
+__global__ __launch_bounds__(WI * WJ * GROUPS * 64, WI * WJ * GROUPS > 4 ? 1 : 2) void k_product(operand P, operand Q, result R, uint32_t across, uint32_t along, uint32_t parts,
                                                                                int64_t depth_part)
 {
-    constexpr bool THROUGH = PKIND == CODES_ACROSS, STAYS = stays<TO>();
-    constexpr int THREADS = WI * WJ * 64, FI = TI / WI / 32, FJ = TJ / WJ / 32, STEP = 64, TURNS = STEP / 16;
+    constexpr bool THROUGH = PKIND == CODES_ACROSS, STAYS = stays<TO>() && GROUPS == 1;
+    constexpr int THREADS = WI * WJ * 64 /* of a group */, FI = TI / WI / 32, FJ = TJ / WJ / 32, STEP = 64, TURNS = STEP / 16;
     constexpr int PWIDE = THROUGH ? WIDE_ACROSS : PKIND;
     using ptile = tile<PWIDE, TI, STEP, THREADS>;
     using qtile = tile<QKIND, TJ, STEP, THREADS>;
     constexpr int TILES = ptile::BYTES + qtile::BYTES, AREA = 4096;            // a step's; what a wave's results go through
     constexpr int BUFFER = TILES > WI * WJ * AREA ? TILES : WI * WJ * AREA;
-    __shared__ __attribute__((aligned(1024))) uint8_t room[2 * BUFFER];
-    lds_byte *const lds = (lds_byte *)room;
-    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    __shared__ __attribute__((aligned(1024))) uint8_t room[2 * GROUPS * BUFFER];
+    const int lane = threadIdx.x % 64, in_block = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int group = in_block / (WI * WJ), wave = in_block % (WI * WJ);
+    lds_byte *const lds = (lds_byte *)room + group * (2 * BUFFER);
     const int wi = wave % WI, wj = wave / WI;
 
     // Blocks go round the eight dies; each die has a run of neighbouring tiles, so that what they share comes from its cache.
@@ -477,25 +488,26 @@ __global__ __launch_bounds__(WI * WJ * 64, WI * WJ > 4 ? 1 : 2) void k_product(o
     typename ptile::template stream<TO == TO_GATED ? 2 : 1, TI / WI> pstream;
     typename qtile::template stream<1, TJ> qstream;
     staged_codes<TI, STEP, THREADS> through;
-    if constexpr (THROUGH) through.init(P);
+    if constexpr (THROUGH) through.init(P, threadIdx.x % THREADS);
     else pstream.init(P, wave, lane);
     qstream.init(Q, wave, lane);
 
-    // What is fetched next: k_left values of k of tile `tile_ahead` (none: no tiles are left).
+    // What is fetched next: k_left values of k, the groups' together, of tile `tile_ahead` (none: no tiles are left).
     uint32_t tile_ahead = tile_first;
     int64_t k_left = 0;
     const auto aim = [&] {
         const place at = place_of(tile_ahead);
-        if constexpr (THROUGH) through.aim(P, at.i, at.first, at.first + at.length);
-        else pstream.aim(P, TO == TO_GATED ? R.columns : P.rows, at.i, at.first, at.first + at.length, R.columns * P.stride * 2);
-        qstream.aim(Q, Q.rows, at.j, at.first, at.first + at.length, 0);
+        const int64_t first = at.first + group * STEP, last = at.first + at.length;
+        if constexpr (THROUGH) through.aim(P, at.i, first, last, GROUPS);
+        else pstream.aim(P, TO == TO_GATED ? R.columns : P.rows, at.i, first, last, R.columns * P.stride * 2, GROUPS);
+        qstream.aim(Q, Q.rows, at.j, first, last, 0, GROUPS);
         k_left = at.length;
     };
     // The next step's fetch, made ready, in FETCHES pieces, and done.
     constexpr int FETCHES = THROUGH ? 1 + qtile::EACH : ptile::EACH + qtile::EACH;
     const auto ready = [&] {
-        if constexpr (!THROUGH) pstream.ready(k_left, wave, lane);
-        qstream.ready(k_left, wave, lane);
+        if constexpr (!THROUGH) pstream.ready(k_left - group * STEP, wave, lane);
+        qstream.ready(k_left - group * STEP, wave, lane);
     };
     const auto fetch = [&](int piece, int to) {
         constexpr int OF_P = THROUGH ? 1 : ptile::EACH;
@@ -507,7 +519,7 @@ __global__ __launch_bounds__(WI * WJ * 64, WI * WJ > 4 ? 1 : 2) void k_product(o
         }
     };
     const auto fetched = [&] {
-        k_left -= STEP;
+        k_left -= GROUPS * STEP;
         if (k_left <= 0) {
             tile_ahead += stride;
             k_left = 0;
@@ -700,10 +712,11 @@ __global__ __launch_bounds__(WI * WJ * 64, WI * WJ > 4 ? 1 : 2) void k_product(o
     fetched();
     if constexpr (THROUGH) through.store(lds);
     place now = place_of(tile_first);
-    scales_of(now.j, now.first / GROUP);
+    constexpr int SCALES = GROUPS * STEP / GROUP;    // of a row, from one of a group's steps to its next
+    scales_of(now.j, now.first / GROUP + group * (STEP / GROUP));
     for (uint32_t tile = tile_first, at = 0;;) {
         clear();
-        for (int64_t k = 0; k < now.length; k += STEP, at = BUFFER - at) {
+        for (int64_t k = 0; k < now.length; k += GROUPS * STEP, at = BUFFER - at) {
             __builtin_amdgcn_s_waitcnt(0x0070);      // vmcnt(0) lgkmcnt(0): what this wave fetched and stored has arrived
             __syncthreads();
             const bool ahead = k_left > 0;           // the other buffer, which every wave is done with, takes the next step's tiles
@@ -729,12 +742,12 @@ __global__ __launch_bounds__(WI * WJ * 64, WI * WJ > 4 ? 1 : 2) void k_product(o
                 if constexpr (THROUGH) through.store(lds + other);
             }
             if constexpr (QKIND == CODES_ALONG) {
-                const int64_t g = (now.first + k + STEP) / GROUP;
-                if (k + STEP < now.length) {
-                    if (g % 16 == 0) scales_of(now.j, g);
+                const int64_t g = (now.first + k + GROUPS * STEP) / GROUP;
+                if (k + GROUPS * STEP < now.length) {
+                    if (g % 16 == 0) scales_of(now.j, g + group * (STEP / GROUP));
                     else {
 #pragma unroll
-                        for (int t = 0; t < FJ; ++t) bytes[t].template pass<STEP / GROUP>();
+                        for (int t = 0; t < FJ; ++t) bytes[t].template pass<SCALES>();
                     }
                 }
             }
@@ -747,7 +760,36 @@ __global__ __launch_bounds__(WI * WJ * 64, WI * WJ > 4 ? 1 : 2) void k_product(o
             scales_of(now.j, now.first / GROUP);
         }
         __syncthreads();
-        write(done, STAYS ? lds + (BUFFER - at) : lds);
+        if constexpr (GROUPS > 1) {
+            // a fragment's 16 sums of a lane beside those of its neighbours
+            static_assert((GROUPS - 1) * FI * FJ * 4096 * WI * WJ <= 2 * GROUPS * BUFFER, "the groups' sums fit");
+            typedef float f32x4 __attribute__((ext_vector_type(4)));
+            const auto sums = [&](int g, int f, int t, int q) {
+                return (__attribute__((address_space(3))) f32x4 *)((lds_byte *)room + ((((g * WI * WJ + wave) * FI + f) * FJ + t) * 4 + q) * 1024 + lane * 16);
+            };
+#pragma unroll
+            for (int f = 0; f < FI; ++f)
+#pragma unroll
+                for (int t = 0; t < FJ; ++t)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        if (group > 0) *sums(group - 1, f, t, q) = f32x4{acc[f][t][4 * q], acc[f][t][4 * q + 1], acc[f][t][4 * q + 2], acc[f][t][4 * q + 3]};
+            __syncthreads();
+            if (group > 0) return;
+#pragma unroll
+            for (int g = 0; g < GROUPS - 1; ++g)
+#pragma unroll
+                for (int f = 0; f < FI; ++f)
+#pragma unroll
+                    for (int t = 0; t < FJ; ++t)
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            const f32x4 v = *sums(g, f, t, q);
+#pragma unroll
+                            for (int x = 0; x < 4; ++x) acc[f][t][4 * q + x] += v[x];
+                        }
+        }
+        write(done, STAYS ? lds + (BUFFER - at) : lds + (GROUPS - 1) * (FI * FJ * 4096 * WI * WJ));
         if (!on) break;
     }
 }
