@@ -50,7 +50,10 @@ __global__ __launch_bounds__(BLOCK) void k_lay_out(copies C)
 int64_t cut(int64_t n, int64_t by) { return (n + by - 1) / by; }
 int64_t up16(int64_t n) { return (n + 15) / 16 * 16; }
 
-// Memory rows as the product takes them: as they are, or a copy of them in the workspace.
+// Memory rows as the product takes them: as they are, or a copy of them in the workspace.  Rows further apart than this are copied too, so
+// that a tile's rows lie within 31-bit offsets, and rows that overlap (one for all), so that what lies beyond the last reads as zeros.
+constexpr int64_t FAR_APART = (int64_t)1 << 22;                          // bytes; 2^20 columns, the most, are half of it
+
 struct laid {
     const uint8_t *data;
     int64_t stride, rows, bytes, pitch;              // in bytes
@@ -58,7 +61,7 @@ struct laid {
     laid(const void *p, int64_t stride_, int64_t rows_, int64_t cols, int size)
         : data((const uint8_t *)p), stride(stride_ * size), rows(rows_), bytes(cols * size), pitch(up16(cols * size))
     {
-        copied = rows > 0 && (stride % 16 != 0 || bytes % 16 != 0 || (uintptr_t)p % 16 != 0);
+        copied = rows > 0 && (stride % 16 != 0 || bytes % 16 != 0 || (uintptr_t)p % 16 != 0 || stride < bytes || stride > FAR_APART);
     }
     int64_t room() const { return copied ? rows * pitch : 0; }
 

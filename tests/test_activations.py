@@ -86,6 +86,16 @@ def test_workspaces_hold_copies_of_what_is_not_laid_out(lib):
     assert lib.leap_linear_gate8_backward(P, 9, P, 16, 9, P, P, 4, 16, P, None, None) == B.LEAP_INVALID_ARG
 
 
+def test_rows_far_apart_or_on_top_of_each_other_are_copied(lib):
+    """A tile of 256 rows that are 2^23 bytes apart passes 31 bits; rows of one address have nothing beyond the last that reads as zeros."""
+    assert lib.leap_linear8_work(P, 5, 64, P, 1 << 21, 8) == 0
+    assert lib.leap_linear8_work(P, 5, 64, P, (1 << 21) + 8, 8) == 8 * 64 * 2
+    assert lib.leap_linear8_work(P, 5, 64, P, 0, 8) == 8 * 64 * 2
+    assert lib.leap_linear8_backward_work(P, 1 << 24, P, 5, 64, P, 64, 8) == 5 * 8 * 2
+    assert lib.leap_linear8_backward_work(P, 0, P, 5, 64, P, 64, 8) == 5 * 8 * 2
+    assert lib.leap_linear_gate8_work(P, 0, P, 1 << 24, 8, 4, 16) == 4 * 8 * 2 + 8 * 16 * 2
+
+
 def _packed(rows, cols):
     from paper_2307_05801_amd.activations import Packed8
     return Packed8(torch.zeros(rows, cols).to(torch.float8_e4m3fn), torch.zeros(rows, -(-cols // 32), dtype=torch.uint8))

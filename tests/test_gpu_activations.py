@@ -286,6 +286,23 @@ def test_long_products(A):
     R.assert_close(dw[some], (g.T @ v).cpu(), (g.T @ v).abs().cpu() * R.half_step(BF16) + R.sum_error(rows) * (g.abs().T @ v.abs()).cpu(), "grad_weight")
 
 
+def test_rows_far_apart(A):
+    """Weights and gradients whose rows are 2^25 bytes apart: 64 of them pass 31 bits."""
+    rows, cols, out, apart = 70, 96, 72, 1 << 24
+    x, v = packed(A, rand((rows, cols), F32, 24).double())
+    room = torch.empty(apart * out, dtype=BF16, device="cuda")
+    for w, g, wg, gg in ((weight_of(out, cols, 25), rand((rows, out), BF16, 26), (apart, 1), None), (weight_of(out, cols, 25), rand((rows, out), BF16, 26), None, (apart, 1))):
+        wd, gd = w.double(), g.double()
+        w = w.cuda() if wg is None else room.as_strided(w.shape, wg).copy_(w)
+        g = g.cuda() if gg is None else room.as_strided(g.shape, gg).copy_(g)
+        want = v @ wd.T
+        R.assert_close(A.linear8(x, w), want, want.abs() * R.half_step(BF16) + R.sum_error(cols) * (v.abs() @ wd.abs().T), "y")
+        dx, dw = A.linear8_backward(g, x, w)
+        want, want_w = gd @ wd, gd.T @ v
+        R.assert_close(dx, want, want.abs() * R.half_step(BF16) + R.sum_error(out) * (gd.abs() @ wd.abs()), "grad_x")
+        R.assert_close(dw, want_w, want_w.abs() * R.half_step(BF16) + R.sum_error(rows) * (gd.abs().T @ v.abs()), "grad_weight")
+
+
 def test_refusals_on_the_gpu(A):
     dev = "cuda"
     x, w = torch.zeros(4, 64, dtype=BF16, device=dev), torch.ones(64, dtype=BF16, device=dev)
