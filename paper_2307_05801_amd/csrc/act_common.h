@@ -196,12 +196,13 @@ __device__ inline void pack_chunk(const float (&v)[CHUNK], int n, uint8_t *codes
     }
 }
 
-// 1 / (1 + exp(-g)) within a few units of the last place: 2^-32 (1 + exp(-g)) does not overflow before the result is zero, and
-// its reciprocal, which the hardware forms within a unit but not as a subnormal number, is brought back by a product.
+// 1 / (1 + exp(-g)) within a few units of the last place.  exp(-g) is the square of exp(-g / 2): an exponent that carries an offset
+// would lose what the offset's size rounds away.  Its 2^-32nd part does not overflow before the result is zero, and the reciprocal
+// of that, which the hardware forms within a unit but not as a subnormal number, is brought back by a product.
 __device__ inline float sigmoid(float g)
 {
-    const float scaled = __builtin_amdgcn_exp2f(__builtin_fmaf(g, -1.44269504f, -32.0f)) + 0x1p-32f;
-    return __builtin_amdgcn_rcpf(scaled) * 0x1p-32f;
+    const float root = __builtin_amdgcn_exp2f(g * -0.72134752f);
+    return __builtin_amdgcn_rcpf(__builtin_fmaf(root * 0x1p-32f, root, 0x1p-32f)) * 0x1p-32f;
 }
 
 // ---- division of 32-bit numbers by one that a launch knows ----
