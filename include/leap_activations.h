@@ -97,6 +97,27 @@ int leap_linear_gate8_backward(const void *d_dy, int64_t dy_stride, const void *
                                const uint8_t *d_kept_codes, const uint8_t *d_kept_scales, int64_t rows, int64_t out, void *d_du,
                                void *d_work, void *hip_stream);
 
+/* A feed-forward block of these, as one call:  s = x + residual (NULL: s = x);  y [rows][out] = gated(norm(s) up^T) down^T, with up
+ * [2 * hidden][cols] and down [out][hidden], their rows up_stride and down_stride apart, everything plain in bfloat16 (the norm's
+ * weight in norm_weight_type).  d_sum: [rows][cols], or NULL.  d_kept: leap_feed_forward8_kept() bytes, 16-byte aligned, that the backward
+ * pass reads: what the operators above keep, in 8 bits.  d_work: leap_feed_forward8_work() bytes, NULL where that is 0.
+ * Backward: grad_x (the residual's gradient too), and the weights' gradients, each [as its weight] without gaps; NULL for what is not
+ * wanted (the norm's weight gradient comes with grad_x).  grad_sum: what reaches s from elsewhere, or NULL.  d_work:
+ * leap_feed_forward8_backward_work() bytes, 16-byte aligned, never NULL. */
+int64_t leap_feed_forward8_kept(int64_t rows, int64_t cols, int64_t hidden);
+int64_t leap_feed_forward8_work(int64_t rows, int64_t cols, const void *d_up, int64_t up_stride, int64_t hidden, const void *d_down,
+                                int64_t down_stride, int64_t out);
+int leap_feed_forward8(const void *d_x, int64_t x_stride, const void *d_residual, int64_t residual_stride, const void *d_norm_weight,
+                       int32_t norm_weight_type, int64_t rows, int64_t cols, float eps, const void *d_up, int64_t up_stride, int64_t hidden,
+                       const void *d_down, int64_t down_stride, int64_t out, void *d_sum, void *d_y, void *d_kept, void *d_work,
+                       void *hip_stream);
+int64_t leap_feed_forward8_backward_work(const void *d_dy, int64_t dy_stride, int64_t rows, int64_t cols, const void *d_up, int64_t up_stride,
+                                         int64_t hidden, const void *d_down, int64_t down_stride, int64_t out);
+int leap_feed_forward8_backward(const void *d_dy, int64_t dy_stride, const void *d_grad_sum, int64_t grad_sum_stride, const void *d_norm_weight,
+                                int32_t norm_weight_type, int64_t rows, int64_t cols, const void *d_up, int64_t up_stride, int64_t hidden,
+                                const void *d_down, int64_t down_stride, int64_t out, const void *d_kept, void *d_grad_x,
+                                void *d_grad_norm_weight, void *d_grad_up, void *d_grad_down, void *d_work, void *hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

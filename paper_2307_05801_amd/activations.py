@@ -344,35 +344,46 @@ def gated_linear8_backward(grad: torch.Tensor, kept: Packed8, x: Packed8, weight
 class _FeedForward8(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, residual, norm_weight, up, down, eps):
-        total, normed, kept_sum, rstd = rms_norm8(x, norm_weight, residual, eps)
-        gated, kept = gated_linear8(normed, up)
-        y = linear8(gated, down)
-        # a tensor apart from its input: autograd would take it for a view
-        total = total.view_as(total) if residual is None else total
-        ctx.save_for_backward(norm_weight, up, down, rstd, *(t for p in (normed, kept_sum, gated, kept) for t in (p.codes, p.scales)))
+        device = x.device
+        rows, cols, stride = _rows(x, "x")
+        residual_stride = 0 if residual is None else _gradient(residual, x.shape, device, (x.dtype,), "residual")[2]
+        _norm_weight(norm_weight, x, cols)
+        hidden, up_stride = _halves(up, cols, device, "up")
+        out, down_stride = _weight(down, hidden, device, "down")
+        total = None if residual is None else torch.empty(x.shape, dtype=x.dtype, device=device)
+        y = torch.empty(x.shape[:-1] + (out,), dtype=x.dtype, device=device)
+        lib = B._activations or B.load_activations()
+        kept = torch.empty(lib.leap_feed_forward8_kept(rows, cols, hidden), dtype=torch.uint8, device=device)
+        weights = (up.data_ptr(), up_stride, hidden, down.data_ptr(), down_stride, out)
+        work = _work("leap_feed_forward8_work", device, rows, cols, *weights)
+        _call("leap_feed_forward8", device, x.data_ptr(), stride, _address(residual), residual_stride, norm_weight.data_ptr(), _TYPES[norm_weight.dtype],
+              rows, cols, eps, *weights, _address(total), y.data_ptr(), kept.data_ptr(), _address(work))
+        ctx.save_for_backward(norm_weight, up, down, kept)
         ctx.set_materialize_grads(False)
-        ctx.added = residual is not None
-        return y, total
+        ctx.added, ctx.shape, ctx.sizes = residual is not None, x.shape, (rows, cols, up_stride, hidden, down_stride, out)
+        # without a residual a tensor apart from its input: autograd would take it for a view
+        return y, x.view_as(x) if total is None else total
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, grad_y, grad_sum):
-        norm_weight, up, down, rstd, *packed = ctx.saved_tensors
-        normed, kept_sum, gated, kept = (Packed8(*packed[i:i + 2]) for i in range(0, 8, 2))
-        need_x, need_r, need_norm, need_up, need_down = ctx.needs_input_grad[:5]
         if grad_y is None:
             return grad_sum, grad_sum if ctx.added else None, None, None, None, None
+        norm_weight, up, down, kept = ctx.saved_tensors
+        rows, cols, up_stride, hidden, down_stride, out = ctx.sizes
+        need_x, need_r, need_norm, need_up, need_down = ctx.needs_input_grad[:5]
+        device = kept.device
         grad_y = grad_y.contiguous()
-        grad_down = linear8_backward(grad_y, gated, down, need_x=False)[1] if need_down else None
-        grad_x = grad_norm = grad_up = None
-        if need_x or need_r or need_norm or need_up:
-            du = linear_gate8_backward(grad_y, down, kept)
-            # 32 bits between the product and the norm: a rounding less in grad_x
-            dn, grad_up = linear8_backward(du, normed, up, need_x or need_r or need_norm, need_up, torch.float32)
-            if dn is not None:
-                grad_x, grad_norm = rms_norm8_backward(dn, kept_sum, rstd, norm_weight, None if grad_sum is None else grad_sum.contiguous(),
-                                                       torch.bfloat16)
-        return grad_x if need_x else None, grad_x if need_r else None, grad_norm if need_norm else None, grad_up, grad_down, None
+        grad_sum = None if grad_sum is None else grad_sum.contiguous()
+        grad_x = torch.empty(ctx.shape, dtype=torch.bfloat16, device=device) if need_x or need_r or need_norm else None
+        grad_norm = torch.empty(cols, dtype=norm_weight.dtype, device=device) if need_norm else None
+        grad_up = torch.empty((2 * hidden, cols), dtype=torch.bfloat16, device=device) if need_up else None
+        grad_down = torch.empty((out, hidden), dtype=torch.bfloat16, device=device) if need_down else None
+        weights = (up.data_ptr(), up_stride, hidden, down.data_ptr(), down_stride, out)
+        work = _work("leap_feed_forward8_backward_work", device, grad_y.data_ptr(), out, rows, cols, *weights)
+        _call("leap_feed_forward8_backward", device, grad_y.data_ptr(), out, _address(grad_sum), cols, norm_weight.data_ptr(), _TYPES[norm_weight.dtype],
+              rows, cols, *weights, kept.data_ptr(), _address(grad_x), _address(grad_norm), _address(grad_up), _address(grad_down), _address(work))
+        return grad_x if need_x else None, grad_x if need_r else None, grad_norm, grad_up, grad_down, None
 
 
 def feed_forward8(x: torch.Tensor, norm_weight: torch.Tensor, up: torch.Tensor, down: torch.Tensor, residual: torch.Tensor = None,

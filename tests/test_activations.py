@@ -64,6 +64,36 @@ def test_no_rows_is_fine(lib):
     assert lib.leap_gate8_backward(None, 8, None, None, 0, 8, None, None) == B.LEAP_OK
 
 
+BLOCK_FORWARD = (P, 64, P, 64, P, 1, 4, 64, 1e-6, P, 64, 8, P, 8, 16, P, P, P, P, 0)
+BLOCK_BACKWARD = (P, 16, P, 64, P, 1, 4, 64, P, 64, 8, P, 8, 16, P, P, P, P, P, P, 0)
+
+
+@pytest.mark.parametrize("name,good,bad", [
+    ("leap_feed_forward8", BLOCK_FORWARD, [(5, 2), (6, -1), (6, 1 << 32), (7, 0), (7, 1 << 21), (1, 63), (3, 63), (8, -1.0), (10, 63), (11, 0), (11, 1 << 20),
+                                           (13, 7), (14, 0), (0, 0), (4, 0), (9, 0), (12, 0), (16, 0), (17, 0), (17, P + 8)]),
+    ("leap_feed_forward8_backward", BLOCK_BACKWARD, [(1, 15), (3, 63), (4, 0), (5, 2), (15, 0), (6, -1), (7, 0), (9, 63), (10, 0), (10, 1 << 20), (12, 7), (13, 0), (0, 0), (8, 0), (11, 0), (14, 0),
+                                                     (14, P + 4), (19, 0), (19, P + 8)]),
+])
+def test_bad_arguments_of_a_block_are_refused_with_a_message(lib, name, good, bad):
+    for at, value in bad:
+        arguments = list(good)
+        arguments[at] = value
+        assert getattr(lib, name)(*arguments) == B.LEAP_INVALID_ARG, (name, at, value)
+        assert lib.leap_last_error()
+
+
+def test_memory_of_a_block(lib):
+    """Codes and scales of the norm's output, of the sum, of the gated rows and of both halves, rstd: each in whole 16 bytes."""
+    assert lib.leap_feed_forward8_kept(4, 64, 40) == 2 * (256 + 16) + 160 + 16 + 320 + 16 + 16
+    assert lib.leap_feed_forward8_kept(0, 64, 40) == 0 and lib.leap_feed_forward8_kept(4, 64, 0) == 0 and lib.leap_feed_forward8_kept(-1, 64, 40) == 0
+    assert lib.leap_feed_forward8_work(4, 64, P, 64, 16, P, 16, 24) == 0 and lib.leap_feed_forward8_work(4, 64, P, 64, 16, P, 16, 0) == 0
+    assert lib.leap_feed_forward8_work(4, 64, P, 65, 16, P, 16, 24) == 32 * 64 * 2
+    least = 4 * 2 * 16 * 2 + 4 * 64 * 4 + lib.leap_rms_norm8_work(4, 64) * 4
+    assert lib.leap_feed_forward8_backward_work(P, 24, 4, 64, P, 64, 16, P, 16, 24) >= least
+    assert lib.leap_feed_forward8_backward_work(P, 23, 4, 64, P, 64, 16, P, 16, 24) == 0
+    assert lib.leap_feed_forward8(None, 64, None, 64, None, 1, 0, 64, 1e-6, None, 64, 8, None, 8, 16, *[None] * 5) == B.LEAP_OK
+
+
 def test_workspaces_of_bad_sizes_are_nothing(lib):
     assert lib.leap_rms_norm8_work(-1, 64) == 0 and lib.leap_rms_norm8_work(5, 0) == 0
     assert lib.leap_linear8_work(P, -1, 64, P, 64, 8) == 0 and lib.leap_linear8_backward_work(P, 8, P, 4, 0, P, 64, 8) == 0

@@ -396,6 +396,31 @@ def test_block_against_differences(A):
         assert abs(slope / float(d.square().sum()) - 1) <= 2.0 ** -3, (what, slope, float(d.square().sum()))
 
 
+@pytest.mark.parametrize("rows,cols,hidden,out", [(1, 32, 32, 32), (130, 343, 70, 90), (200, 96, 130, 520)])
+def test_a_block_is_its_operators(A, rows, cols, hidden, out):
+    """The same bits, for inputs and weights in longer rows too; as many outputs as wanted."""
+    x, r, nw, up, _, _, gs = _block(rows, cols, hidden, seed=100)
+    down, gy = weight_of(out, hidden, 108), rand((rows, out), BF16, 109)
+    x, r, nw, up, down, gy, gs = _offset(x, 3), _offset(r, 5), nw.cuda(), _offset(up, 1), _offset(down, 8), gy.cuda(), gs.cuda()
+    total, normed, kept_sum, rstd = A.rms_norm8(x, nw, r)
+    gated, kept = A.gated_linear8(normed, up)
+    du = A.linear_gate8_backward(gy, down, kept)
+    dn, dup = A.linear8_backward(du, normed, up, dtype=F32)
+    dx, dnw = A.rms_norm8_backward(dn, kept_sum, rstd, nw, gs, BF16)
+    want = (A.linear8(gated, down), total, dx, dnw, dup, A.linear8_backward(gy, gated, down, need_x=False)[1], dx)
+    leaves = [t.detach().requires_grad_(True) for t in (x, nw, up, down, r)]
+    y, s = A.feed_forward8(*leaves[:4], residual=leaves[4])
+    got = (y, s, *torch.autograd.grad((y, s), leaves, (gy, gs)))
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_a_block_of_no_rows(A):
+    leaves = [t.cuda().requires_grad_(True) for t in (torch.empty(0, 64, dtype=BF16), torch.ones(64, dtype=BF16), weight_of(96, 64, 1), weight_of(64, 48, 2))]
+    y, s = A.feed_forward8(*leaves)
+    grads = torch.autograd.grad((y, s), leaves, (torch.empty_like(y), torch.empty_like(s)))
+    assert y.shape == (0, 64) and grads[0].shape == (0, 64) and not any(g.any() for g in grads[1:])
+
+
 def test_blocks_in_a_row_as_modules(A):
     torch.manual_seed(3)
     blocks = [A.FeedForward8(64, 48) for _ in range(3)]
