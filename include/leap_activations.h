@@ -85,6 +85,15 @@ int leap_gated_linear8(const uint8_t *d_codes, const uint8_t *d_scales, int64_t 
                        int64_t out, uint8_t *d_gated_codes, uint8_t *d_gated_scales, uint8_t *d_kept_codes, uint8_t *d_kept_scales,
                        void *d_work, void *hip_stream);
 
+/* Its gradients from da = dL/d gated ([rows][out] bfloat16 with a stride): leap_gate8_backward (below), then leap_linear8_backward of du, which is
+ * in the workspace; grad_x [rows][cols] of grad_x_type and grad_weight [2 * out][cols], either may be NULL.  d_work:
+ * leap_gated_linear8_backward_work() bytes, 16-byte aligned (no rows: may be NULL). */
+int64_t leap_gated_linear8_backward_work(const uint8_t *d_codes, int64_t rows, int64_t cols, const void *d_weight, int64_t w_stride, int64_t out);
+int leap_gated_linear8_backward(const void *d_da, int64_t da_stride, const uint8_t *d_kept_codes, const uint8_t *d_kept_scales,
+                                const uint8_t *d_codes, const uint8_t *d_scales, int64_t rows, int64_t cols, const void *d_weight,
+                                int64_t w_stride, int64_t out, void *d_grad_x, int32_t grad_x_type, void *d_grad_weight, void *d_work,
+                                void *hip_stream);
+
 /* du [rows][2 * out] (bfloat16) from kept = (g, p) and da = dL/d gated: the gate's half da * p * s * (1 + g * (1 - s)), the
  * other da * g * s, with s = sigmoid(g).  With u's gradient in hand leap_linear8_backward gives those of v and W.
  * leap_gate8_backward reads da [rows][out] (bfloat16, with a stride); leap_linear_gate8_backward forms it, in 32 bits, as

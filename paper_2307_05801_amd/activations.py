@@ -26,6 +26,7 @@ from .projector import _current_stream
 GROUP = 32
 _TYPES = {torch.float32: B.LEAP_F32, torch.bfloat16: B.LEAP_BF16, torch.float16: B.LEAP_F16}
 _CODES = torch.float8_e4m3fn
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
 class Packed8:
@@ -66,7 +67,7 @@ def _type_of(t: torch.Tensor, what: str) -> int:
 
 
 def _on_gpu(t: torch.Tensor, what: str, device=None) -> None:
-    if t.device.type != "cuda":
+    if not t.is_cuda:
         raise ValueError(f"{what} must be on a GPU")
     if device is not None and t.device != device:
         raise ValueError(f"{what} must be on {device}")
@@ -119,7 +120,7 @@ def _call(name: str, device, *arguments) -> None:
     """The library's function on `device`, on its current stream."""
     lib = B._activations or B.load_activations()
     index = device.index
-    if torch.cuda.current_device() == index:
+    if _current_device() == index:
         status = getattr(lib, name)(*arguments, _current_stream(index))
     else:
         with torch.cuda.device(index):
@@ -131,7 +132,7 @@ def _call(name: str, device, *arguments) -> None:
 def _empty_packed(shape, device) -> Packed8:
     p = Packed8.__new__(Packed8)
     p.codes = torch.empty(shape, dtype=_CODES, device=device)
-    p.scales = torch.empty(tuple(shape[:-1]) + (-(-shape[-1] // GROUP),), dtype=torch.uint8, device=device)
+    p.scales = torch.empty((*shape[:-1], -(-shape[-1] // GROUP)), dtype=torch.uint8, device=device)
     return p
 
 
@@ -180,7 +181,7 @@ class keep_in_8_bits(torch.autograd.graph.saved_tensors_hooks):
 
     def __init__(self, min_values: int = 1 << 16):
         def pack(t):
-            if t.device.type != "cuda" or t.dtype not in _TYPES or t.numel() < min_values or (t.is_leaf and t.requires_grad):
+            if not t.is_cuda or t.dtype not in _TYPES or t.numel() < min_values or (t.is_leaf and t.requires_grad):
                 return t
             try:
                 _rows(t, "tensor")
@@ -335,7 +336,18 @@ def gated_linear8_backward(grad: torch.Tensor, kept: Packed8, x: Packed8, weight
     """(grad_x, grad_weight) of gated_linear8 from the gradient of `gated` (bfloat16)."""
     if kept.shape[:-2] != x.shape[:-1]:
         raise ValueError(f"kept {tuple(kept.shape)} is not of this x {tuple(x.shape)}")
-    return linear8_backward(gate8_backward(grad, kept), x, weight, need_x, need_weight)
+    lead, out = _kept_halves(kept)
+    rows, cols = _packed_rows(x)
+    halves, w_stride = _halves(weight, cols, x.device)
+    if halves != out or kept.device != x.device:
+        raise ValueError(f"kept {tuple(kept.shape)} is not of this weight {tuple(weight.shape)}, or on another device")
+    stride = _gradient(grad, lead + (out,), x.device, (torch.bfloat16,), "grad")[2]
+    grad_x = torch.empty(x.shape, dtype=torch.bfloat16, device=x.device) if need_x else None
+    grad_weight = torch.empty((2 * out, cols), dtype=torch.bfloat16, device=x.device) if need_weight else None
+    work = _work("leap_gated_linear8_backward_work", x.device, x.codes.data_ptr(), rows, cols, weight.data_ptr(), w_stride, out)
+    _call("leap_gated_linear8_backward", x.device, grad.data_ptr(), stride, kept.codes.data_ptr(), kept.scales.data_ptr(), x.codes.data_ptr(), x.scales.data_ptr(),
+          rows, cols, weight.data_ptr(), w_stride, out, _address(grad_x), B.LEAP_BF16, _address(grad_weight), _address(work))
+    return grad_x, grad_weight
 
 
 # ---- the block ----------------------------------------------------------------------------------------------------------

@@ -35,6 +35,8 @@ ACTIVATION_EXPORTS = {                                       # name: (result, ar
     "leap_linear8_backward_work": (_L, [_P, _L, _P, _L, _L, _P, _L, _L]),
     "leap_linear8_backward": (C.c_int, [_P, _L, _P, _P, _L, _L, _P, _L, _L, _P, _I, _P, _P, _P]),
     "leap_gated_linear8": (C.c_int, [_P, _P, _L, _L, _P, _L, _L, _P, _P, _P, _P, _P, _P]),
+    "leap_gated_linear8_backward_work": (_L, [_P, _L, _L, _P, _L, _L]),
+    "leap_gated_linear8_backward": (C.c_int, [_P, _L, _P, _P, _P, _P, _L, _L, _P, _L, _L, _P, _I, _P, _P, _P]),
     "leap_gate8_backward": (C.c_int, [_P, _L, _P, _P, _L, _L, _P, _P]),
     "leap_linear_gate8_work": (_L, [_P, _L, _P, _L, _L, _L, _L]),
     "leap_linear_gate8_backward": (C.c_int, [_P, _L, _P, _L, _L, _P, _P, _L, _L, _P, _P, _P]),

@@ -54,7 +54,7 @@ struct block_sizes {
         return a > b ? a : b;
     }
     // The parts' workspaces take turns behind du (bfloat16) and the norm's gradient (32 bits).
-    int64_t du_bytes() const { return up16(rows * 2 * hidden * 2); }
+    int64_t du_bytes() const { return rows * padded_row(2 * hidden) * 2; }
     int64_t dn_bytes() const { return up16(rows * cols * 4); }
     int64_t backward_work(const void *dy, int64_t dy_stride, const void *kept) const
     {
@@ -63,7 +63,7 @@ struct block_sizes {
         int64_t most = leap_rms_norm8_work(rows, cols) * 4;
         for (int64_t n : {leap_linear8_backward_work(dy, dy_stride, K.gated, rows, hidden, down, down_stride, out),
                           leap_linear_gate8_work(dy, dy_stride, down, down_stride, out, rows, hidden),
-                          leap_linear8_backward_work(du, 2 * hidden, K.normed, rows, cols, up, up_stride, 2 * hidden)})
+                          linear8_backward_work(du, padded_row(2 * hidden), true, K.normed, rows, cols, up, up_stride, 2 * hidden)})
             most = n > most ? n : most;
         return du_bytes() + dn_bytes() + up16(most);
     }
@@ -133,11 +133,11 @@ extern "C" int leap_feed_forward8_backward(const void *d_dy, int64_t dy_stride, 
     if (d_grad_down)
         rc = leap_linear8_backward(d_dy, dy_stride, K.gated, K.gated_scales, rows, hidden, d_down, down_stride, out, nullptr, LEAP_BF16, d_grad_down, work, hip_stream);
     if (rc == LEAP_OK && (d_grad_x || d_grad_up)) {
-        rc = leap_linear_gate8_backward(d_dy, dy_stride, d_down, down_stride, out, K.gate, K.gate_scales, rows, hidden, du, work, hip_stream);
+        rc = linear_gate8_backward(d_dy, dy_stride, d_down, down_stride, out, K.gate, K.gate_scales, rows, hidden, du, padded_row(2 * hidden), work, hip_stream);
         // 32 bits between the product and the norm: a rounding less in grad_x
         if (rc == LEAP_OK)
-            rc = leap_linear8_backward(du, 2 * hidden, K.normed, K.normed_scales, rows, cols, d_up, up_stride, 2 * hidden, d_grad_x ? dn : nullptr, LEAP_F32,
-                                       d_grad_up, work, hip_stream);
+            rc = linear8_backward(du, padded_row(2 * hidden), true, K.normed, K.normed_scales, rows, cols, d_up, up_stride, 2 * hidden, d_grad_x ? dn : nullptr,
+                                  LEAP_F32, d_grad_up, work, hip_stream);
     }
     if (rc == LEAP_OK && (d_grad_x || d_grad_norm_weight))
         rc = leap_rms_norm8_backward(dn, LEAP_F32, cols, d_grad_sum, grad_sum_stride, LEAP_BF16, K.sum, K.sum_scales, K.rstd, d_norm_weight, norm_weight_type,

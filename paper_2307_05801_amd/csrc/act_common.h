@@ -266,4 +266,19 @@ template <class F> inline int by_type(int32_t type, F &&f)
     }
 }
 
+// ---- products that other operators are made of (act_gemm.hip) ----
+
+// Values from one row to the next where rows of bfloat16 are followed by zeros up to a multiple of 16 bytes: such rows are not laid out anew.
+inline int64_t padded_row(int64_t cols) { return (cols + 7) / 8 * 8; }
+
+// leap_linear8_backward of a dy whose rows are so padded, or are not; leap_linear_gate8_backward to a du with rows du_stride apart, zeros
+// between them.
+int64_t linear8_backward_work(const void *d_dy, int64_t dy_stride, bool padded, const uint8_t *d_codes, int64_t rows, int64_t cols, const void *d_weight,
+                              int64_t w_stride, int64_t out);
+int linear8_backward(const void *d_dy, int64_t dy_stride, bool padded, const uint8_t *d_codes, const uint8_t *d_scales, int64_t rows, int64_t cols,
+                     const void *d_weight, int64_t w_stride, int64_t out, void *d_grad_x, int32_t grad_x_type, void *d_grad_weight, void *d_work,
+                     void *hip_stream);
+int linear_gate8_backward(const void *d_dy, int64_t dy_stride, const void *d_weight, int64_t w_stride, int64_t next, const uint8_t *d_kept_codes,
+                          const uint8_t *d_kept_scales, int64_t rows, int64_t out, void *d_du, int64_t du_stride, void *d_work, void *hip_stream);
+
 }  // namespace act

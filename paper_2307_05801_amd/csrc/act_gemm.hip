@@ -58,10 +58,11 @@ struct laid {
     const uint8_t *data;
     int64_t stride, rows, bytes, pitch;              // in bytes
     bool copied;
-    laid(const void *p, int64_t stride_, int64_t rows_, int64_t cols, int size)
+    // padded: its rows are followed by zeros up to a multiple of 16 bytes
+    laid(const void *p, int64_t stride_, int64_t rows_, int64_t cols, int size, bool padded = false)
         : data((const uint8_t *)p), stride(stride_ * size), rows(rows_), bytes(cols * size), pitch(up16(cols * size))
     {
-        copied = rows > 0 && (stride % 16 != 0 || bytes % 16 != 0 || (uintptr_t)p % 16 != 0 || stride < bytes || stride > FAR_APART);
+        copied = rows > 0 && (stride % 16 != 0 || (bytes % 16 != 0 && !padded) || (uintptr_t)p % 16 != 0 || stride < bytes || stride > FAR_APART);
     }
     int64_t room() const { return copied ? rows * pitch : 0; }
 
@@ -99,7 +100,7 @@ bool large_tiles(int64_t i, int64_t j)
     return (double)cut(cut(i, 256) * cut(j, 256), 256) <= 0.62 * (double)cut(cut(i, 128) * cut(j, 128), 512);
 }
 
-template <int PKIND, int QKIND, int TO, int TI, int TJ, int WI, int WJ, int GROUPS>
+template <int PKIND, int QKIND, int TO, int TI, int TJ, int WI, int WJ, int GROUPS, int DEPTH>
 int launch(const operand &P, const operand &Q, const result &R, int64_t depth_part, hipStream_t st)
 {
     const int64_t across = TO == TO_GATED ? cut(R.columns, TI / 2) : cut(P.rows, TI), along = cut(Q.rows, TJ), parts = depth_part ? cut(P.depth, depth_part) : 1;
@@ -107,7 +108,7 @@ int launch(const operand &P, const operand &Q, const result &R, int64_t depth_pa
     // as many blocks as the 256 compute units hold at once, by shared memory and registers
     constexpr int RESIDENT = WI * WJ * GROUPS > 4 ? 1 : 2;
     const int64_t blocks = !stays<TO>() || GROUPS > 1 || across * along * parts < 256 * RESIDENT ? across * along * parts : 256 * RESIDENT;
-    hipLaunchKernelGGL((k_product<PKIND, QKIND, TO, TI, TJ, WI, WJ, GROUPS>), dim3((unsigned)blocks), dim3(WI * WJ * GROUPS * 64), 0, st, P, Q, R, (uint32_t)across,
+    hipLaunchKernelGGL((k_product<PKIND, QKIND, TO, TI, TJ, WI, WJ, GROUPS, DEPTH>), dim3((unsigned)blocks), dim3(WI * WJ * GROUPS * 64), 0, st, P, Q, R, (uint32_t)across,
                        (uint32_t)along, (uint32_t)parts, depth_part ? depth_part : P.depth);
     return launched();
 }
@@ -116,10 +117,15 @@ template <int PKIND, int QKIND, int TO> int product(const operand &P, const oper
 {
     // the gate's gradient moves more than it multiplies: small tiles always (262144 x 512 -> 2 * 512: 300 us, large ones 369)
     if constexpr (TO != TO_GATE_GRAD)
-        if (large) return launch<PKIND, QKIND, TO, 256, 256, 2, 4, 1>(P, Q, R, depth_part, st);
-    if constexpr (PKIND != CODES_ACROSS)
-        if (cut(TO == TO_GATED ? 2 * R.columns : P.rows, 128) * cut(Q.rows, 128) <= 256) return launch<PKIND, QKIND, TO, 128, 128, 2, 2, 2>(P, Q, R, depth_part, st);
-    return launch<PKIND, QKIND, TO, 128, 128, 2, 2, 1>(P, Q, R, depth_part, st);
+        if (large) return launch<PKIND, QKIND, TO, 256, 256, 2, 4, 1, 2>(P, Q, R, depth_part, st);
+    // At most as many tiles as units: two groups of waves share one, and half as many rows a tile while that makes no second round of
+    // them (4096 x 2048 -> 512: 17 us in 256 tiles of 64 rows, 29 in 128 of 128 and two buffers).
+    if constexpr (PKIND != CODES_ACROSS) {
+        const int64_t across = cut(TO == TO_GATED ? 2 * R.columns : P.rows, 128);
+        if (across * cut(Q.rows, 64) <= 256) return launch<PKIND, QKIND, TO, 128, 64, 2, 2, 2, 3>(P, Q, R, depth_part, st);
+        if (across * cut(Q.rows, 128) <= 256) return launch<PKIND, QKIND, TO, 128, 128, 2, 2, 2, QKIND == CODES_ALONG ? 3 : 2>(P, Q, R, depth_part, st);
+    }
+    return launch<PKIND, QKIND, TO, 128, 128, 2, 2, 1, 2>(P, Q, R, depth_part, st);
 }
 
 template <int PKIND, int QKIND, int TO> int product(const operand &P, const operand &Q, const result &R, hipStream_t st)
@@ -184,9 +190,10 @@ __global__ __launch_bounds__(BLOCK) void k_add_parts(const float *__restrict__ f
 
 // ---- the gate by itself ----
 
-// du <- da and what is kept; one chunk of `out` a lane
+// du, rows of du_stride, <- da and what is kept, and zeros between its rows; one chunk of `out` a lane
 __global__ __launch_bounds__(BLOCK) void k_gate_grad(const void *__restrict__ da, int64_t stride, const uint8_t *__restrict__ kept_codes,
-                                                     const uint8_t *__restrict__ kept_scales, int64_t rows, int64_t out, void *__restrict__ du)
+                                                     const uint8_t *__restrict__ kept_scales, int64_t rows, int64_t out, void *__restrict__ du,
+                                                     int64_t du_stride)
 {
     const int64_t groups = groups_of(out), per_row = groups * (GROUP / CHUNK), c = (int64_t)blockIdx.x * BLOCK + threadIdx.x;
     const int64_t row = c / per_row, col = (c - row * per_row) * CHUNK;
@@ -202,8 +209,18 @@ __global__ __launch_bounds__(BLOCK) void k_gate_grad(const void *__restrict__ da
         dg[i] = d[i] * p[i] * s * (1.0f + g[i] * (1.0f - s));
         dp[i] = d[i] * g[i] * s;
     }
-    store8<LEAP_BF16>(du, row * 2 * out + col, n, dg, rows * out * 4 > PAST_CACHES);
-    store8<LEAP_BF16>(du, row * 2 * out + out + col, n, dp, rows * out * 4 > PAST_CACHES);
+    store8<LEAP_BF16>(du, row * du_stride + col, n, dg, rows * out * 4 > PAST_CACHES);
+    store8<LEAP_BF16>(du, row * du_stride + out + col, n, dp, rows * out * 4 > PAST_CACHES);
+    if (col + n == out)
+        for (int64_t i = 2 * out; i < du_stride; ++i) ((uint16_t *)du)[row * du_stride + i] = 0;
+}
+
+// Zeros between rows, behind the `cols` values of each.
+__global__ __launch_bounds__(BLOCK) void k_pad_rows(uint16_t *__restrict__ to, int64_t stride, int64_t rows, int64_t cols)
+{
+    const int64_t row = (int64_t)blockIdx.x * BLOCK + threadIdx.x;
+    if (row >= rows) return;
+    for (int64_t i = cols; i < stride; ++i) to[row * stride + i] = 0;
 }
 
 const char *bad_product(int64_t rows, int64_t cols, int64_t w_stride, int64_t out)
@@ -240,26 +257,26 @@ extern "C" int leap_linear8(const uint8_t *d_codes, const uint8_t *d_scales, int
     return product<WIDE_ALONG, CODES_ALONG, TO_WIDE>(W.wide(out, cols), X.codes(d_scales, cols, rows, cols), R, st);
 }
 
-extern "C" int64_t leap_linear8_backward_work(const void *d_dy, int64_t dy_stride, const uint8_t *d_codes, int64_t rows, int64_t cols, const void *d_weight,
-                                              int64_t w_stride, int64_t out)
+int64_t act::linear8_backward_work(const void *d_dy, int64_t dy_stride, bool padded, const uint8_t *d_codes, int64_t rows, int64_t cols, const void *d_weight,
+                                   int64_t w_stride, int64_t out)
 {
     if (bad_product(rows, cols, w_stride, out) || bad_stride(dy_stride, rows, out)) return 0;
-    return weight_plan(rows, cols, out).room(cols, out) + laid(d_dy, dy_stride, rows, out, 2).room() + laid(d_codes, cols, rows, cols, 1).room() +
+    return weight_plan(rows, cols, out).room(cols, out) + laid(d_dy, dy_stride, rows, out, 2, padded).room() + laid(d_codes, cols, rows, cols, 1).room() +
            laid(d_weight, w_stride, out, cols, 2).room();
 }
 
-extern "C" int leap_linear8_backward(const void *d_dy, int64_t dy_stride, const uint8_t *d_codes, const uint8_t *d_scales, int64_t rows, int64_t cols,
-                                     const void *d_weight, int64_t w_stride, int64_t out, void *d_grad_x, int32_t grad_x_type, void *d_grad_weight,
-                                     void *d_work, void *hip_stream)
+int act::linear8_backward(const void *d_dy, int64_t dy_stride, bool padded, const uint8_t *d_codes, const uint8_t *d_scales, int64_t rows, int64_t cols,
+                          const void *d_weight, int64_t w_stride, int64_t out, void *d_grad_x, int32_t grad_x_type, void *d_grad_weight, void *d_work,
+                          void *hip_stream)
 {
     if (const char *why = bad_product(rows, cols, w_stride, out)) return refuse(why);
     if (const char *why = bad_stride(dy_stride, rows, out)) return refuse(why);
     if (grad_x_type != LEAP_BF16 && grad_x_type != LEAP_F32) return refuse("grad_x is bfloat16 or float32");
     if (rows && (!d_dy || !d_codes || !d_scales || !d_weight)) return refuse("null data pointer");
-    if (!d_work && leap_linear8_backward_work(d_dy, dy_stride, d_codes, rows, cols, d_weight, w_stride, out)) return refuse("null workspace");
+    if (!d_work && act::linear8_backward_work(d_dy, dy_stride, padded, d_codes, rows, cols, d_weight, w_stride, out)) return refuse("null workspace");
     const hipStream_t st = stream_of(hip_stream);
     uint8_t *room = (uint8_t *)d_work;
-    laid G(d_dy, dy_stride, rows, out, 2), W(d_weight, w_stride, out, cols, 2), X(d_codes, cols, rows, cols, 1);
+    laid G(d_dy, dy_stride, rows, out, 2, padded), W(d_weight, w_stride, out, cols, 2), X(d_codes, cols, rows, cols, 1);
     int rc = lay_out(room, st, &G, d_grad_x && rows ? &W : nullptr, d_grad_weight ? &X : nullptr);
     if (rc == LEAP_OK && d_grad_x && rows) {
         result R{};
@@ -291,6 +308,20 @@ extern "C" int leap_linear8_backward(const void *d_dy, int64_t dy_stride, const 
     return launched();
 }
 
+extern "C" int64_t leap_linear8_backward_work(const void *d_dy, int64_t dy_stride, const uint8_t *d_codes, int64_t rows, int64_t cols, const void *d_weight,
+                                              int64_t w_stride, int64_t out)
+{
+    return act::linear8_backward_work(d_dy, dy_stride, false, d_codes, rows, cols, d_weight, w_stride, out);
+}
+
+extern "C" int leap_linear8_backward(const void *d_dy, int64_t dy_stride, const uint8_t *d_codes, const uint8_t *d_scales, int64_t rows, int64_t cols,
+                                     const void *d_weight, int64_t w_stride, int64_t out, void *d_grad_x, int32_t grad_x_type, void *d_grad_weight,
+                                     void *d_work, void *hip_stream)
+{
+    return act::linear8_backward(d_dy, dy_stride, false, d_codes, d_scales, rows, cols, d_weight, w_stride, out, d_grad_x, grad_x_type, d_grad_weight, d_work,
+                                 hip_stream);
+}
+
 extern "C" int leap_gated_linear8(const uint8_t *d_codes, const uint8_t *d_scales, int64_t rows, int64_t cols, const void *d_weight, int64_t w_stride,
                                   int64_t out, uint8_t *d_gated_codes, uint8_t *d_gated_scales, uint8_t *d_kept_codes, uint8_t *d_kept_scales,
                                   void *d_work, void *hip_stream)
@@ -311,8 +342,10 @@ extern "C" int leap_gated_linear8(const uint8_t *d_codes, const uint8_t *d_scale
     return product<WIDE_ALONG, CODES_ALONG, TO_GATED>(W.wide(2 * out, cols), X.codes(d_scales, cols, rows, cols), R, st);
 }
 
-extern "C" int leap_gate8_backward(const void *d_da, int64_t da_stride, const uint8_t *d_kept_codes, const uint8_t *d_kept_scales, int64_t rows,
-                                   int64_t out, void *d_du, void *hip_stream)
+namespace {
+
+int gate_backward(const void *d_da, int64_t da_stride, const uint8_t *d_kept_codes, const uint8_t *d_kept_scales, int64_t rows, int64_t out, void *d_du,
+                  int64_t du_stride, void *hip_stream)
 {
     if (out > MOST_COLS / 2) return refuse(GATED_LIMIT);
     if (const char *why = bad_sizes(rows, out)) return refuse(why);
@@ -321,8 +354,42 @@ extern "C" int leap_gate8_backward(const void *d_da, int64_t da_stride, const ui
     if (!d_da || !d_kept_codes || !d_kept_scales || !d_du) return refuse("null data pointer");
     const int64_t blocks = cut(rows * groups_of(out) * (GROUP / CHUNK), BLOCK);
     if (blocks > 0x7fffffff) return refuse("more values than one launch covers");
-    hipLaunchKernelGGL(k_gate_grad, dim3((unsigned)blocks), dim3(BLOCK), 0, stream_of(hip_stream), d_da, da_stride, d_kept_codes, d_kept_scales, rows, out, d_du);
+    hipLaunchKernelGGL(k_gate_grad, dim3((unsigned)blocks), dim3(BLOCK), 0, stream_of(hip_stream), d_da, da_stride, d_kept_codes, d_kept_scales, rows, out, d_du,
+                       du_stride);
     return launched();
+}
+
+}  // namespace
+
+extern "C" int leap_gate8_backward(const void *d_da, int64_t da_stride, const uint8_t *d_kept_codes, const uint8_t *d_kept_scales, int64_t rows,
+                                   int64_t out, void *d_du, void *hip_stream)
+{
+    return gate_backward(d_da, da_stride, d_kept_codes, d_kept_scales, rows, out, d_du, 2 * out, hip_stream);
+}
+
+extern "C" int64_t leap_gated_linear8_backward_work(const uint8_t *d_codes, int64_t rows, int64_t cols, const void *d_weight, int64_t w_stride, int64_t out)
+{
+    if (out > MOST_COLS / 2 || out < 1 || bad_product(rows, cols, w_stride, 2 * out)) return 0;
+    return rows * padded_row(2 * out) * 2 + act::linear8_backward_work((const void *)16, padded_row(2 * out), true, d_codes, rows, cols, d_weight, w_stride, 2 * out);
+}
+
+extern "C" int leap_gated_linear8_backward(const void *d_da, int64_t da_stride, const uint8_t *d_kept_codes, const uint8_t *d_kept_scales,
+                                           const uint8_t *d_codes, const uint8_t *d_scales, int64_t rows, int64_t cols, const void *d_weight,
+                                           int64_t w_stride, int64_t out, void *d_grad_x, int32_t grad_x_type, void *d_grad_weight, void *d_work,
+                                           void *hip_stream)
+{
+    if (out > MOST_COLS / 2) return refuse(GATED_LIMIT);
+    if (const char *why = bad_product(rows, cols, w_stride, 2 * out)) return refuse(why);
+    if (const char *why = bad_stride(da_stride, rows, out)) return refuse(why);
+    if (grad_x_type != LEAP_BF16 && grad_x_type != LEAP_F32) return refuse("grad_x is bfloat16 or float32");
+    if (rows && (!d_codes || !d_scales || !d_weight)) return refuse("null data pointer");
+    if (rows && (!d_work || (uintptr_t)d_work % 16 != 0)) return refuse("the workspace needs memory from a multiple of 16 bytes on");
+    if (!d_grad_x && !d_grad_weight) return LEAP_OK;
+    const int64_t stride = padded_row(2 * out);
+    const int rc = gate_backward(d_da, da_stride, d_kept_codes, d_kept_scales, rows, out, d_work, stride, hip_stream);
+    if (rc != LEAP_OK) return rc;
+    return act::linear8_backward(d_work, stride, true, d_codes, d_scales, rows, cols, d_weight, w_stride, 2 * out, d_grad_x, grad_x_type, d_grad_weight,
+                                 rows ? (uint8_t *)d_work + rows * stride * 2 : nullptr, hip_stream);
 }
 
 extern "C" int64_t leap_linear_gate8_work(const void *d_dy, int64_t dy_stride, const void *d_weight, int64_t w_stride, int64_t next, int64_t rows, int64_t out)
@@ -331,9 +398,8 @@ extern "C" int64_t leap_linear_gate8_work(const void *d_dy, int64_t dy_stride, c
     return laid(d_dy, dy_stride, rows, next, 2).room() + laid(d_weight, w_stride, next, out, 2).room();
 }
 
-extern "C" int leap_linear_gate8_backward(const void *d_dy, int64_t dy_stride, const void *d_weight, int64_t w_stride, int64_t next,
-                                          const uint8_t *d_kept_codes, const uint8_t *d_kept_scales, int64_t rows, int64_t out, void *d_du,
-                                          void *d_work, void *hip_stream)
+int act::linear_gate8_backward(const void *d_dy, int64_t dy_stride, const void *d_weight, int64_t w_stride, int64_t next, const uint8_t *d_kept_codes,
+                               const uint8_t *d_kept_scales, int64_t rows, int64_t out, void *d_du, int64_t du_stride, void *d_work, void *hip_stream)
 {
     if (out > MOST_COLS / 2) return refuse(GATED_LIMIT);
     if (const char *why = bad_product(rows, out, w_stride, next)) return refuse(why);
@@ -346,7 +412,15 @@ extern "C" int leap_linear_gate8_backward(const void *d_dy, int64_t dy_stride, c
     laid W(d_weight, w_stride, next, out, 2), G(d_dy, dy_stride, rows, next, 2);
     const int rc = lay_out(room, st, &W, &G);
     if (rc != LEAP_OK) return rc;
+    if (du_stride > 2 * out) hipLaunchKernelGGL(k_pad_rows, dim3((unsigned)cut(rows, BLOCK)), dim3(BLOCK), 0, st, (uint16_t *)d_du, du_stride, rows, 2 * out);
     result R{};
-    R.out = d_du, R.columns = out, R.kept_codes = (uint8_t *)d_kept_codes, R.kept_scales = (uint8_t *)d_kept_scales;
+    R.out = d_du, R.stride = du_stride, R.columns = out, R.kept_codes = (uint8_t *)d_kept_codes, R.kept_scales = (uint8_t *)d_kept_scales;
     return product<WIDE_ACROSS, WIDE_ALONG, TO_GATE_GRAD>(W.wide(out, next), G.wide(rows, next), R, st);
+}
+
+extern "C" int leap_linear_gate8_backward(const void *d_dy, int64_t dy_stride, const void *d_weight, int64_t w_stride, int64_t next,
+                                          const uint8_t *d_kept_codes, const uint8_t *d_kept_scales, int64_t rows, int64_t out, void *d_du,
+                                          void *d_work, void *hip_stream)
+{
+    return act::linear_gate8_backward(d_dy, dy_stride, d_weight, w_stride, next, d_kept_codes, d_kept_scales, rows, out, d_du, 2 * out, d_work, hip_stream);
 }

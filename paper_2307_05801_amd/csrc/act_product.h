@@ -1,7 +1,7 @@
 // The tiled product behind leap_linear8 and its kin: D[j][i] = sum over k of P(i, k) Q(j, k).
 //
-// A block owns TI x TJ of D and walks over k in steps of 64 or 32; a step's tiles of P and Q are fetched into shared memory (mostly
-// straight from memory, past the registers) while the step before is multiplied: two buffers, one barrier a step.  i runs along a lane's
+// A block owns TI x TJ of D and walks over k in steps of 64; a step's tiles of P and Q are fetched into shared memory (mostly straight
+// from memory, past the registers) while the one or two steps before are multiplied: two or three buffers, one barrier a step.  i runs along a lane's
 // registers and j across lanes, so a lane ends with runs of neighbouring i: what a row of an output, and a group of 32 that
 // shares a scale, is made of.
 //
@@ -65,7 +65,7 @@ __device__ inline int64_t whole(int64_t n, int piece) { return (n + piece - 1) /
 // is reserved: nothing the compiler makes of these kernels uses it.)
 __device__ inline void fetch16(const u32x4 &from, uint32_t offset, lds_byte *to)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"((uint32_t)(uintptr_t)to), "v"(offset), "s"(from) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(__builtin_amdgcn_readfirstlane((int)(uintptr_t)to)), "v"(offset), "s"(from) : "memory");
 }
 
 // A tile of T rows and STEP values of k of an operand in shared memory, by KIND.  ALONG: T rows of 2 * STEP (codes: STEP)
@@ -448,8 +448,10 @@ struct result {
 // step's fetches are started while the first turn's operands are on their way from shared memory.
 //
 // Where tiles are few, GROUPS of WI x WJ waves share one: each takes every GROUPS-th step, by itself but for the meetings, and
-// their sums are added through shared memory at the end.  A wave alone on its unit spends two thirds of a step waiting.
-template <int PKIND, int QKIND, int TO, int TI, int TJ, int WI, int WJ, int GROUPS>
+// their sums are added through shared memory at the end.  A wave alone on its unit spends two thirds of a step waiting.  A step of
+// one block a compute unit still lasts as long as its fetch (1.6 us), hence DEPTH 3 there, where shared memory allows: two fetches under way.
+// It gains nothing where two blocks a unit hide the fetch, nor for the large tiles (262144 x 512 -> 1024: 318 us, 301 with two).
+template <int PKIND, int QKIND, int TO, int TI, int TJ, int WI, int WJ, int GROUPS, int DEPTH>
 __global__ __launch_bounds__(WI * WJ * GROUPS * 64, WI * WJ * GROUPS > 4 ? 1 : 2) void k_product(operand P, operand Q, result R, uint32_t across, uint32_t along, uint32_t parts,
                                                                                int64_t depth_part)
 {
@@ -460,10 +462,11 @@ __global__ __launch_bounds__(WI * WJ * GROUPS * 64, WI * WJ * GROUPS > 4 ? 1 : 2
     using qtile = tile<QKIND, TJ, STEP, THREADS>;
     constexpr int TILES = ptile::BYTES + qtile::BYTES, AREA = 4096;            // a step's; what a wave's results go through
     constexpr int BUFFER = TILES > WI * WJ * AREA ? TILES : WI * WJ * AREA;
-    __shared__ __attribute__((aligned(1024))) uint8_t room[2 * GROUPS * BUFFER];
+    static_assert(DEPTH == 2 || !THROUGH, "what goes through the registers is one step ahead");
+    __shared__ __attribute__((aligned(1024))) uint8_t room[DEPTH * GROUPS * BUFFER];
     const int lane = threadIdx.x % 64, in_block = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int group = in_block / (WI * WJ), wave = in_block % (WI * WJ);
-    lds_byte *const lds = (lds_byte *)room + group * (2 * BUFFER);
+    lds_byte *const lds = (lds_byte *)room + group * (DEPTH * BUFFER);
     const int wi = wave % WI, wj = wave / WI;
 
     // Blocks go round the eight dies; each die has a run of neighbouring tiles, so that what they share comes from its cache.
@@ -505,6 +508,7 @@ __global__ __launch_bounds__(WI * WJ * GROUPS * 64, WI * WJ * GROUPS > 4 ? 1 : 2
     };
     // The next step's fetch, made ready, in FETCHES pieces, and done.
     constexpr int FETCHES = THROUGH ? 1 + qtile::EACH : ptile::EACH + qtile::EACH;
+    static_assert(FETCHES < 16, "counted by four bits");
     const auto ready = [&] {
         if constexpr (!THROUGH) pstream.ready(k_left - group * STEP, wave, lane);
         qstream.ready(k_left - group * STEP, wave, lane);
@@ -643,8 +647,8 @@ __global__ __launch_bounds__(WI * WJ * GROUPS * 64, WI * WJ * GROUPS > 4 ? 1 : 2
             constexpr int ARRAY = 32 * FI * 32;
             const landing kept_g(R.kept_codes, j_wave, Q.rows, 2 * R.columns, i_wave, R.columns, FI * 32);
             const landing kept_p(R.kept_codes, j_wave, Q.rows, 2 * R.columns, R.columns + i_wave, 2 * R.columns, FI * 32);
-            const landing to_g(R.out, j_wave, Q.rows, 4 * R.columns, 2 * i_wave, 2 * R.columns, FI * 64);
-            const landing to_p(R.out, j_wave, Q.rows, 4 * R.columns, 2 * (R.columns + i_wave), 4 * R.columns, FI * 64);
+            const landing to_g(R.out, j_wave, Q.rows, 2 * R.stride, 2 * i_wave, 2 * R.columns, FI * 64);
+            const landing to_p(R.out, j_wave, Q.rows, 2 * R.stride, 2 * (R.columns + i_wave), 4 * R.columns, FI * 64);
             u32x4 raw[2][room::TURNS];
             uint32_t bytes_of[2];                                    // a byte a group: at most four
             const auto load = [&](int t) {
@@ -706,21 +710,34 @@ __global__ __launch_bounds__(WI * WJ * GROUPS * 64, WI * WJ * GROUPS > 4 ? 1 : 2
         }
     };
 
-    ready();
+    const auto after = [](uint32_t at) { return at + BUFFER == DEPTH * BUFFER ? 0u : at + BUFFER; };
+    int under_way = 0;                               // steps fetched and not multiplied
 #pragma unroll
-    for (int e = 0; e < FETCHES; ++e) fetch(e, 0);
-    fetched();
+    for (int d = 0; d < DEPTH - 1; ++d) {
+        const bool more_of_it = k_left > 0;
+        ready();                                     // (of nothing, where no step is left: it is not fetched)
+        if (more_of_it) {
+#pragma unroll
+            for (int e = 0; e < FETCHES; ++e) fetch(e, d * BUFFER);
+            fetched();
+            ++under_way;
+        }
+    }
     if constexpr (THROUGH) through.store(lds);
     place now = place_of(tile_first);
     constexpr int SCALES = GROUPS * STEP / GROUP;    // of a row, from one of a group's steps to its next
     scales_of(now.j, now.first / GROUP + group * (STEP / GROUP));
     for (uint32_t tile = tile_first, at = 0;;) {
         clear();
-        for (int64_t k = 0; k < now.length; k += GROUPS * STEP, at = BUFFER - at) {
-            __builtin_amdgcn_s_waitcnt(0x0070);      // vmcnt(0) lgkmcnt(0): what this wave fetched and stored has arrived
+        for (int64_t k = 0; k < now.length; k += GROUPS * STEP, at = after(at)) {
+            // What this wave fetched and stored for this step has arrived (lgkmcnt(0), and vmcnt(0) or as many as a later step's
+            // fetches are: loads arrive in order, and whatever else is under way was started after this step's).
+            if (DEPTH > 2 && under_way > 1) __builtin_amdgcn_s_waitcnt(0x0070 | FETCHES);
+            else __builtin_amdgcn_s_waitcnt(0x0070);
             __syncthreads();
-            const bool ahead = k_left > 0;           // the other buffer, which every wave is done with, takes the next step's tiles
-            const int other = BUFFER - at;
+            const bool ahead = k_left > 0;           // the buffer before this one, which every wave is done with, takes the next tiles
+            const int other = DEPTH == 2 ? after(at) : after(after(at));
+            --under_way;
             read(0, at);
             if (ahead) ready();
             __builtin_amdgcn_sched_barrier(0);
@@ -739,6 +756,7 @@ __global__ __launch_bounds__(WI * WJ * GROUPS * 64, WI * WJ * GROUPS > 4 ? 1 : 2
             }
             if (ahead) {
                 fetched();
+                ++under_way;
                 if constexpr (THROUGH) through.store(lds + other);
             }
             if constexpr (QKIND == CODES_ALONG) {
@@ -762,7 +780,7 @@ __global__ __launch_bounds__(WI * WJ * GROUPS * 64, WI * WJ * GROUPS > 4 ? 1 : 2
         __syncthreads();
         if constexpr (GROUPS > 1) {
             // a fragment's 16 sums of a lane beside those of its neighbours
-            static_assert((GROUPS - 1) * FI * FJ * 4096 * WI * WJ <= 2 * GROUPS * BUFFER, "the groups' sums fit");
+            static_assert(GROUPS * FI * FJ * 4096 * WI * WJ <= DEPTH * GROUPS * BUFFER, "the groups' sums fit");
             typedef float f32x4 __attribute__((ext_vector_type(4)));
             const auto sums = [&](int g, int f, int t, int q) {
                 return (__attribute__((address_space(3))) f32x4 *)((lds_byte *)room + ((((g * WI * WJ + wave) * FI + f) * FJ + t) * 4 + q) * 1024 + lane * 16);
@@ -789,7 +807,7 @@ __global__ __launch_bounds__(WI * WJ * GROUPS * 64, WI * WJ * GROUPS > 4 ? 1 : 2
                             for (int x = 0; x < 4; ++x) acc[f][t][4 * q + x] += v[x];
                         }
         }
-        write(done, STAYS ? lds + (BUFFER - at) : lds + (GROUPS - 1) * (FI * FJ * 4096 * WI * WJ));
+        write(done, STAYS ? lds + (at == 0 ? DEPTH - 1 : at / BUFFER - 1) * BUFFER : lds + (GROUPS - 1) * (FI * FJ * 4096 * WI * WJ));
         if (!on) break;
     }
 }

@@ -64,6 +64,19 @@ def test_no_rows_is_fine(lib):
     assert lib.leap_gate8_backward(None, 8, None, None, 0, 8, None, None) == B.LEAP_OK
 
 
+def test_bad_arguments_of_the_gated_gradient_are_refused_with_a_message(lib):
+    good = (P, 8, P, P, P, P, 4, 64, P, 64, 8, P, 1, P, P, 0)
+    for at, value in [(1, 7), (6, -1), (7, 0), (9, 63), (10, 0), (10, 1 << 20), (12, 2), (0, 0), (2, 0), (3, 0), (4, 0), (5, 0), (8, 0), (14, 0), (14, P + 8)]:
+        arguments = list(good)
+        arguments[at] = value
+        assert lib.leap_gated_linear8_backward(*arguments) == B.LEAP_INVALID_ARG, (at, value)
+        assert lib.leap_last_error()
+    # du in rows of whole 16 bytes, which are not copied again
+    assert lib.leap_gated_linear8_backward_work(P, 5, 64, P, 64, 9) == 5 * 24 * 2
+    assert lib.leap_gated_linear8_backward_work(P, 5, 40, P, 64, 8) == 5 * 16 * 2 + 5 * 48
+    assert lib.leap_gated_linear8_backward_work(P, 5, 64, P, 64, 0) == 0 and lib.leap_gated_linear8_backward_work(P, -1, 64, P, 64, 8) == 0
+
+
 BLOCK_FORWARD = (P, 64, P, 64, P, 1, 4, 64, 1e-6, P, 64, 8, P, 8, 16, P, P, P, P, 0)
 BLOCK_BACKWARD = (P, 16, P, 64, P, 1, 4, 64, P, 64, 8, P, 8, 16, P, P, P, P, P, P, 0)
 

@@ -421,6 +421,19 @@ def test_a_block_of_no_rows(A):
     assert y.shape == (0, 64) and grads[0].shape == (0, 64) and not any(g.any() for g in grads[1:])
 
 
+@pytest.mark.parametrize("rows,cols,out", [(1, 40, 3), (70, 64, 33), (300, 96, 130), (513, 343, 205)])
+def test_gradients_of_the_gated_product_are_those_of_its_parts(A, rows, cols, out):
+    """The same bits by one call, whose du is in padded rows, and by two."""
+    x, _ = packed(A, rand((rows, cols), F32, 27).double())
+    w, g = _offset(weight_of(2 * out, cols, 28), 3), _offset(rand((rows, out), BF16, 29), 5)
+    _, kept = A.gated_linear8(x, w)
+    want = A.linear8_backward(A.gate8_backward(g, kept), x, w)
+    got = A.gated_linear8_backward(g, kept, x, w)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    assert A.gated_linear8_backward(g, kept, x, w, need_weight=False)[1] is None
+    assert torch.equal(A.gated_linear8_backward(g, kept, x, w, need_x=False)[1], want[1])
+
+
 def test_blocks_in_a_row_as_modules(A):
     torch.manual_seed(3)
     blocks = [A.FeedForward8(64, 48) for _ in range(3)]
