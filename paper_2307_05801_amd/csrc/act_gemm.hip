@@ -209,8 +209,8 @@ __global__ __launch_bounds__(BLOCK) void k_gate_grad(const void *__restrict__ da
         dg[i] = d[i] * p[i] * s * (1.0f + g[i] * (1.0f - s));
         dp[i] = d[i] * g[i] * s;
     }
-    store8<LEAP_BF16>(du, row * du_stride + col, n, dg, rows * out * 4 > PAST_CACHES);
-    store8<LEAP_BF16>(du, row * du_stride + out + col, n, dp, rows * out * 4 > PAST_CACHES);
+    store8<LEAP_BF16>(du, row * du_stride + col, n, dg, rows * out * 4 > READ_NEXT);
+    store8<LEAP_BF16>(du, row * du_stride + out + col, n, dp, rows * out * 4 > READ_NEXT);
     if (col + n == out)
         for (int64_t i = 2 * out; i < du_stride; ++i) ((uint16_t *)du)[row * du_stride + i] = 0;
 }

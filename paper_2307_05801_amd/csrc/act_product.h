@@ -580,7 +580,7 @@ __global__ __launch_bounds__(WI * WJ * GROUPS * 64, WI * WJ * GROUPS > 4 ? 1 : 2
             const room x{area};
             landing to((uint8_t *)R.out + (TO == TO_FULL ? of.part * R.part * SIZE : 0), j_wave, Q.rows, R.stride * SIZE, i_wave * SIZE,
                        P.rows * SIZE, FI * 32 * SIZE);
-            if (parts > 1) to.past = false;                          // they are read again at once
+            if (parts > 1 || (TO == TO_FULL && Q.rows * R.stride * SIZE <= READ_NEXT)) to.past = false;      // they are read again at once
 #pragma unroll
             for (int t = 0; t < FJ; ++t)
 #pragma unroll
@@ -647,8 +647,9 @@ __global__ __launch_bounds__(WI * WJ * GROUPS * 64, WI * WJ * GROUPS > 4 ? 1 : 2
             constexpr int ARRAY = 32 * FI * 32;
             const landing kept_g(R.kept_codes, j_wave, Q.rows, 2 * R.columns, i_wave, R.columns, FI * 32);
             const landing kept_p(R.kept_codes, j_wave, Q.rows, 2 * R.columns, R.columns + i_wave, 2 * R.columns, FI * 32);
-            const landing to_g(R.out, j_wave, Q.rows, 2 * R.stride, 2 * i_wave, 2 * R.columns, FI * 64);
-            const landing to_p(R.out, j_wave, Q.rows, 2 * R.stride, 2 * (R.columns + i_wave), 4 * R.columns, FI * 64);
+            landing to_g(R.out, j_wave, Q.rows, 2 * R.stride, 2 * i_wave, 2 * R.columns, FI * 64);
+            landing to_p(R.out, j_wave, Q.rows, 2 * R.stride, 2 * (R.columns + i_wave), 4 * R.columns, FI * 64);
+            if (Q.rows * R.stride * 2 <= READ_NEXT) to_g.past = to_p.past = false;
             u32x4 raw[2][room::TURNS];
             uint32_t bytes_of[2];                                    // a byte a group: at most four
             const auto load = [&](int t) {
