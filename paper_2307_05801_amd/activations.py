@@ -177,7 +177,8 @@ def unpack8(packed: Packed8, dtype: torch.dtype = torch.bfloat16) -> torch.Tenso
 class keep_in_8_bits(torch.autograd.graph.saved_tensors_hooks):
     """Inside this context what autograd saves for the backward pass is kept packed: tensors on a GPU of float32, bfloat16 or
     float16 with at least `min_values` values and evenly spaced rows.  Leaves that want a gradient (weights) and everything
-    else are kept as they are.  The gradients are those of the values held (3 mantissa bits)."""
+    else are kept as they are; a weight's cast or slice is no leaf: keep its use outside.  The gradients are those of the values held
+    (3 mantissa bits)."""
 
     def __init__(self, min_values: int = 1 << 16):
         def pack(t):
@@ -372,7 +373,7 @@ class _FeedForward8(torch.autograd.Function):
               rows, cols, eps, *weights, _address(total), y.data_ptr(), kept.data_ptr(), _address(work))
         ctx.save_for_backward(norm_weight, up, down, kept)
         ctx.set_materialize_grads(False)
-        ctx.added, ctx.shape, ctx.sizes = residual is not None, x.shape, (rows, cols, up_stride, hidden, down_stride, out)
+        ctx.added, ctx.shape, ctx.sizes = residual is not None, x.shape, (rows, cols, hidden, out)
         # without a residual a tensor apart from its input: autograd would take it for a view
         return y, x.view_as(x) if total is None else total
 
@@ -382,9 +383,11 @@ class _FeedForward8(torch.autograd.Function):
         if grad_y is None:
             return grad_sum, grad_sum if ctx.added else None, None, None, None, None
         norm_weight, up, down, kept = ctx.saved_tensors
-        rows, cols, up_stride, hidden, down_stride, out = ctx.sizes
+        rows, cols, hidden, out = ctx.sizes
         need_x, need_r, need_norm, need_up, need_down = ctx.needs_input_grad[:5]
         device = kept.device
+        # hooks on saved tensors may have laid the weights out anew
+        up_stride, down_stride = _weight(up, cols, device, "up")[1], _weight(down, hidden, device, "down")[1]
         grad_y = grad_y.contiguous()
         grad_sum = None if grad_sum is None else grad_sum.contiguous()
         grad_x = torch.empty(ctx.shape, dtype=torch.bfloat16, device=device) if need_x or need_r or need_norm else None

@@ -529,3 +529,18 @@ def test_what_autograd_saves_kept_in_8_bits(A):
     with A.keep_in_8_bits(min_values=10 ** 9):
         value = loss()
     assert all(torch.equal(a, b) for a, b in zip(torch.autograd.grad(value, (x, w)), plain))
+
+
+def test_a_block_whose_saved_weights_come_back_laid_out_anew(A):
+    """Weights that are slices of wider ones, kept in 8 bits: the backward pass gets them without gaps, and as they are held."""
+    x, r, nw, up, down, gy, gs = (t.cuda() for t in _block(70, 64, 48, seed=110))
+    wide_up, wide_down = (torch.cat([t, torch.full_like(t, float("nan"))], 1).requires_grad_(True) for t in (up, down))
+    with A.keep_in_8_bits(min_values=1000):
+        y, s = A.feed_forward8(x, nw, wide_up[:, :64], wide_down[:, :48], residual=r)
+    got = torch.autograd.grad((y, s), (wide_up, wide_down), (gy, gs))
+    total, normed, kept_sum, rstd = A.rms_norm8(x, nw, r)
+    gated, kept = A.gated_linear8(normed, up)
+    assert torch.equal(y, A.linear8(gated, down))
+    du = A.linear_gate8_backward(gy, A.pack8(down).unpack(BF16), kept)
+    assert torch.equal(got[0][:, :64], A.linear8_backward(du, normed, up, need_x=False)[1]) and not got[0][:, 64:].any()
+    assert torch.equal(got[1][:, :48], A.linear8_backward(gy, gated, down, need_x=False)[1]) and not got[1][:, 48:].any()
