@@ -65,7 +65,8 @@ int leap_rms_norm8_backward(const void *d_grad, int32_t grad_type, int64_t grad_
 /* y [rows][out] (bfloat16, no gaps) = v W^T, v the packed rows [rows][cols], W [out][cols] bfloat16, its rows w_stride apart.
  * d_work (all products): as many bytes as the function of that name + "_work" says, 16-byte aligned; NULL where it says 0.
  * It holds copies of what is not laid out for the kernels: codes whose columns are no multiple of 16, weights and gradients
- * whose rows do not begin and end at multiples of 16 bytes (the pointers handed over are looked at for that alone). */
+ * whose rows do not begin and end at multiples of 16 bytes (the pointers handed over are looked at for that alone); and sums over
+ * parts of long rows where outputs are few. */
 int64_t leap_linear8_work(const uint8_t *d_codes, int64_t rows, int64_t cols, const void *d_weight, int64_t w_stride, int64_t out);
 int leap_linear8(const uint8_t *d_codes, const uint8_t *d_scales, int64_t rows, int64_t cols, const void *d_weight, int64_t w_stride,
                  int64_t out, void *d_y, void *d_work, void *hip_stream);

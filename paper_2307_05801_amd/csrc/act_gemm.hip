@@ -93,7 +93,7 @@ int lay_out(uint8_t *&room, hipStream_t st, laid *a, laid *b = nullptr, laid *c 
 // ---- launches ----
 
 // Tiles of 256 x 256, eight waves and a block a compute unit; or of 128 x 128, four waves and two blocks, at 0.8 of the rate (262144 x
-// 512 -> 1024, y: 339 and 411 us) but with less left over where tiles are few.  In units of the time of a large tile, 256 units
+// 512 -> 2 * 1024, gated: 844 and 1056 us) but with less left over where tiles are few.  In units of the time of a large tile, 256 units
 // taking tiles at once:
 bool large_tiles(int64_t i, int64_t j)
 {
@@ -157,7 +157,7 @@ struct weight_plan {
 // to <- the sum of the parts, in a fixed order: 16 threads to four values each, which add every 16th part, 64 values a block.
 constexpr int ADDED = 64;
 
-__global__ __launch_bounds__(BLOCK) void k_add_parts(const float *__restrict__ from, int64_t parts, int64_t n, uint16_t *__restrict__ to)
+template <int TYPE> __global__ __launch_bounds__(BLOCK) void k_add_parts(const float *__restrict__ from, int64_t parts, int64_t n, void *__restrict__ to)
 {
     constexpr int WAYS = BLOCK / (ADDED / 4);
     __shared__ float room[WAYS][ADDED];
@@ -184,8 +184,38 @@ __global__ __launch_bounds__(BLOCK) void k_add_parts(const float *__restrict__ f
         float total = 0.0f;
 #pragma unroll
         for (int w = 0; w < WAYS; ++w) total += room[w][threadIdx.x];
-        to[(int64_t)blockIdx.x * ADDED + threadIdx.x] = element<LEAP_BF16>::from_float(total);
+        ((typename element<TYPE>::raw *)to)[(int64_t)blockIdx.x * ADDED + threadIdx.x] = element<TYPE>::from_float(total);
     }
+}
+
+// y and grad_x of few rows and columns, with many values of k to sum over: the same, in parts of k, 256 at least.  128 values of k take a
+// tile of 128 x 64 0.8 us, another launch 3 us, and the parts' sums the more the more tiles there are: from 1024 values on, and
+// 64 for each tile (1 x 2048 -> 512: 7.0 us, 14.8 in one; 512 x 2048 -> 512, 32 tiles: 12.4 and 16.2; 1024 x 1024 -> 512, 64 tiles: 13.6 and 10.2).
+struct depth_plan {
+    int64_t parts, depth_part;
+    depth_plan(int64_t i, int64_t j, int64_t depth)
+    {
+        const int64_t tiles = cut(i, 128) * cut(j, 64);
+        parts = 1, depth_part = depth;
+        if (tiles < 1 || tiles * 64 > depth || depth < 1024) return;
+        parts = 256 / tiles < depth / 256 ? 256 / tiles : depth / 256;
+        if (parts < 1) parts = 1;
+        depth_part = cut(cut(depth, parts), 128) * 128;
+        parts = cut(depth, depth_part);
+    }
+    int64_t room(int64_t i, int64_t j) const { return parts > 1 ? up16(parts * i * j * (int64_t)sizeof(float)) : 0; }
+};
+
+template <int PKIND, int QKIND> int product_in_parts(const operand &P, const operand &Q, void *out, int32_t type, const depth_plan &plan, uint8_t *room, hipStream_t st)
+{
+    result R{};
+    R.out = room, R.stride = P.rows, R.part = P.rows * Q.rows;
+    const int rc = launch<PKIND, QKIND, TO_FULL, 128, 64, 2, 2, 2, 3>(P, Q, R, plan.depth_part, st);
+    if (rc != LEAP_OK) return rc;
+    const dim3 adders((unsigned)cut(R.part, ADDED));
+    if (type == LEAP_F32) hipLaunchKernelGGL((k_add_parts<LEAP_F32>), adders, dim3(BLOCK), 0, st, (const float *)room, plan.parts, R.part, out);
+    else hipLaunchKernelGGL((k_add_parts<LEAP_BF16>), adders, dim3(BLOCK), 0, st, (const float *)room, plan.parts, R.part, out);
+    return launched();
 }
 
 // ---- the gate by itself ----
@@ -237,7 +267,7 @@ constexpr const char *GATED_LIMIT = "more than 2^19 gated columns";
 extern "C" int64_t leap_linear8_work(const uint8_t *d_codes, int64_t rows, int64_t cols, const void *d_weight, int64_t w_stride, int64_t out)
 {
     if (bad_product(rows, cols, w_stride, out)) return 0;
-    return laid(d_codes, cols, rows, cols, 1).room() + laid(d_weight, w_stride, out, cols, 2).room();
+    return depth_plan(out, rows, cols).room(out, rows) + laid(d_codes, cols, rows, cols, 1).room() + laid(d_weight, w_stride, out, cols, 2).room();
 }
 
 extern "C" int leap_linear8(const uint8_t *d_codes, const uint8_t *d_scales, int64_t rows, int64_t cols, const void *d_weight, int64_t w_stride,
@@ -252,6 +282,9 @@ extern "C" int leap_linear8(const uint8_t *d_codes, const uint8_t *d_scales, int
     laid W(d_weight, w_stride, out, cols, 2), X(d_codes, cols, rows, cols, 1);
     const int rc = lay_out(room, st, &W, &X);
     if (rc != LEAP_OK) return rc;
+    const depth_plan plan(out, rows, cols);
+    if (plan.parts > 1)
+        return product_in_parts<WIDE_ALONG, CODES_ALONG>(W.wide(out, cols), X.codes(d_scales, cols, rows, cols), d_y, LEAP_BF16, plan, room, st);
     result R{};
     R.out = d_y, R.stride = out;
     return product<WIDE_ALONG, CODES_ALONG, TO_WIDE>(W.wide(out, cols), X.codes(d_scales, cols, rows, cols), R, st);
@@ -261,7 +294,7 @@ int64_t act::linear8_backward_work(const void *d_dy, int64_t dy_stride, bool pad
                                    int64_t w_stride, int64_t out)
 {
     if (bad_product(rows, cols, w_stride, out) || bad_stride(dy_stride, rows, out)) return 0;
-    return weight_plan(rows, cols, out).room(cols, out) + laid(d_dy, dy_stride, rows, out, 2, padded).room() + laid(d_codes, cols, rows, cols, 1).room() +
+    return weight_plan(rows, cols, out).room(cols, out) + depth_plan(cols, rows, out).room(cols, rows) + laid(d_dy, dy_stride, rows, out, 2, padded).room() + laid(d_codes, cols, rows, cols, 1).room() +
            laid(d_weight, w_stride, out, cols, 2).room();
 }
 
@@ -282,14 +315,19 @@ int act::linear8_backward(const void *d_dy, int64_t dy_stride, bool padded, cons
         result R{};
         R.out = d_grad_x, R.stride = cols;
         const operand P = W.wide(cols, out), Q = G.wide(rows, out);
-        rc = grad_x_type == LEAP_F32 ? product<WIDE_ACROSS, WIDE_ALONG, TO_FULL>(P, Q, R, st) : product<WIDE_ACROSS, WIDE_ALONG, TO_WIDE>(P, Q, R, st);
+        const depth_plan plan(cols, rows, out);
+        if (plan.parts > 1) {
+            rc = product_in_parts<WIDE_ACROSS, WIDE_ALONG>(P, Q, d_grad_x, grad_x_type, plan, room, st);
+            room += plan.room(cols, rows);
+        } else
+            rc = grad_x_type == LEAP_F32 ? product<WIDE_ACROSS, WIDE_ALONG, TO_FULL>(P, Q, R, st) : product<WIDE_ACROSS, WIDE_ALONG, TO_WIDE>(P, Q, R, st);
     }
     if (rc != LEAP_OK || !d_grad_weight) return rc;
     const int64_t added = cut(cols * out, ADDED);
     if (added > 0x7fffffff) return refuse("a weight of more than 2^37 values");
     const dim3 adders((unsigned)added);
     if (!rows) {                                     // a sum of nothing
-        hipLaunchKernelGGL(k_add_parts, adders, dim3(BLOCK), 0, st, (const float *)nullptr, (int64_t)0, cols * out, (uint16_t *)d_grad_weight);
+        hipLaunchKernelGGL((k_add_parts<LEAP_BF16>), adders, dim3(BLOCK), 0, st, (const float *)nullptr, (int64_t)0, cols * out, d_grad_weight);
         return launched();
     }
     const weight_plan plan(rows, cols, out);
@@ -303,8 +341,7 @@ int act::linear8_backward(const void *d_dy, int64_t dy_stride, bool padded, cons
     R.out = room;
     rc = product<CODES_ACROSS, WIDE_ACROSS, TO_FULL>(P, Q, R, plan.depth_part, plan.large, st);
     if (rc != LEAP_OK) return rc;
-    hipLaunchKernelGGL(k_add_parts, adders, dim3(BLOCK), 0, st, (const float *)room, plan.parts, cols * out,
-                       (uint16_t *)d_grad_weight);
+    hipLaunchKernelGGL((k_add_parts<LEAP_BF16>), adders, dim3(BLOCK), 0, st, (const float *)room, plan.parts, cols * out, d_grad_weight);
     return launched();
 }
 

@@ -129,6 +129,15 @@ def test_workspaces_hold_copies_of_what_is_not_laid_out(lib):
     assert lib.leap_linear_gate8_backward(P, 9, P, 16, 9, P, P, 4, 16, P, None, None) == B.LEAP_INVALID_ARG
 
 
+def test_workspaces_hold_the_parts_of_long_sums(lib):
+    """Few outputs of 1024 values of k or more: sums in 32 bits of parts of at least 256."""
+    assert lib.leap_linear8_work(P, 5, 1008, P, 1008, 8) == 0
+    assert lib.leap_linear8_work(P, 5, 1024, P, 1024, 8) == 4 * 5 * 8 * 4
+    assert lib.leap_linear8_work(P, 64 * 65, 1024, P, 1024, 8) == 0
+    assert lib.leap_linear8_backward_work(P, 2048, P, 5, 64, P, 64, 2048) == 8 * 5 * 64 * 4
+    assert lib.leap_linear8(P, P, 5, 1024, P, 1024, 8, P, None, None) == B.LEAP_INVALID_ARG
+
+
 def test_rows_far_apart_or_on_top_of_each_other_are_copied(lib):
     """A tile of 256 rows that are 2^23 bytes apart passes 31 bits; rows of one address have nothing beyond the last that reads as zeros."""
     assert lib.leap_linear8_work(P, 5, 64, P, 1 << 21, 8) == 0

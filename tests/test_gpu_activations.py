@@ -202,6 +202,13 @@ def test_linear(A, rows, cols, out, wide):
     assert none is None and torch.equal(again, dw)
 
 
+@pytest.mark.parametrize("wide", [0, 3])
+@pytest.mark.parametrize("rows,cols,out", [(1, 1024, 64), (1, 64, 1024), (5, 300, 1500), (70, 1030, 2500), (33, 2048, 1100), (513, 3000, 130)])
+def test_linear_in_parts(A, rows, cols, out, wide):
+    """Few outputs and long sums: y, grad_x or both are added up from parts."""
+    test_linear(A, rows, cols, out, wide)
+
+
 @pytest.mark.parametrize("rows,cols,out", [s for s in SIZES if s[2] < 600])
 def test_gated_linear(A, rows, cols, out):
     x, v = packed(A, rand((rows, cols), F32, 14).double())
