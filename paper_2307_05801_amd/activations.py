@@ -136,6 +136,23 @@ def _empty_packed(shape, device) -> Packed8:
     return p
 
 
+_PLAIN = (torch.Tensor, torch.nn.Parameter)
+
+
+def _like(t: torch.Tensor, dtype: torch.dtype) -> torch.Tensor:
+    """A plain tensor without gaps of t's shape and device (empty_like takes 0.4 us less than empty, but keeps gaps and subclasses)."""
+    if type(t) in _PLAIN and t.is_contiguous():
+        return torch.empty_like(t, dtype=dtype)
+    return torch.empty(t.shape, dtype=dtype, device=t.device)
+
+
+def _packed_like(t: torch.Tensor) -> Packed8:
+    p = Packed8.__new__(Packed8)
+    p.codes = _like(t, _CODES)
+    p.scales = torch.empty((*t.shape[:-1], -(-t.shape[-1] // GROUP)), dtype=torch.uint8, device=t.device)
+    return p
+
+
 def _work(name: str, device, *sizes):
     """Workspace of so many bytes as the library asks for, or None."""
     lib = B._activations or B.load_activations()
@@ -155,7 +172,7 @@ def pack8(x: torch.Tensor) -> Packed8:
     _on_gpu(x, "x")
     kind = _type_of(x, "x")
     rows, cols, stride = _rows(x, "x")
-    p = _empty_packed(x.shape, x.device)
+    p = _packed_like(x)
     _call("leap_pack8", x.device, x.data_ptr(), kind, stride, rows, cols, p.codes.data_ptr(), p.scales.data_ptr())
     return p
 
@@ -169,7 +186,7 @@ def unpack8(packed: Packed8, dtype: torch.dtype = torch.bfloat16) -> torch.Tenso
     codes = packed.codes
     _on_gpu(codes, "packed")
     rows, cols, _ = _rows(codes, "packed")
-    out = torch.empty(codes.shape, dtype=dtype, device=codes.device)
+    out = _like(codes, dtype)
     _call("leap_unpack8", codes.device, codes.data_ptr(), packed.scales.data_ptr(), rows, cols, out.data_ptr(), kind)
     return out
 
@@ -209,9 +226,13 @@ def rms_norm8(x: torch.Tensor, weight: torch.Tensor, residual: torch.Tensor = No
     if residual is not None:
         _, _, residual_stride = _gradient(residual, x.shape, device, (x.dtype,), "residual")
     _norm_weight(weight, x, cols)
-    normed = _empty_packed(x.shape, device)
-    total = x if residual is None else torch.empty(x.shape, dtype=x.dtype, device=device)
-    kept, rstd = (_empty_packed(x.shape, device), torch.empty(x.shape[:-1], dtype=torch.float32, device=device)) if keep else (None, None)
+    normed = _packed_like(x)
+    total = x if residual is None else _like(x, x.dtype)
+    kept = rstd = None
+    if keep:
+        kept = Packed8.__new__(Packed8)
+        kept.codes, kept.scales = torch.empty_like(normed.codes), torch.empty_like(normed.scales)
+        rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device=device)
     _call("leap_rms_norm8", device, x.data_ptr(), stride, _address(residual), residual_stride if residual is not None else 0, kind,
           weight.data_ptr(), _TYPES[weight.dtype], rows, cols, eps, None if residual is None else total.data_ptr(), normed.codes.data_ptr(),
           normed.scales.data_ptr(), kept.codes.data_ptr() if keep else None, kept.scales.data_ptr() if keep else None, _address(rstd))
@@ -235,12 +256,12 @@ def rms_norm8_backward(grad: torch.Tensor, kept: Packed8, rstd: torch.Tensor, we
     _on_gpu(kept.codes, "kept")
     rows, cols, stride = _gradient(grad, kept.shape, device, (dtype, torch.float32), "grad")
     sum_stride = 0 if grad_sum is None else _gradient(grad_sum, kept.shape, device, (dtype,), "grad_sum")[2]
-    grad_x = torch.empty(kept.shape, dtype=dtype, device=device)
+    grad_x = _like(kept.codes, dtype)
     _norm_weight(weight, grad_x, cols)
     _on_gpu(rstd, "rstd", device)
     if rstd.shape != kept.shape[:-1] or rstd.dtype is not torch.float32 or not rstd.is_contiguous():
         raise ValueError(f"rstd must be contiguous float32 {tuple(kept.shape[:-1])}")
-    grad_weight = torch.empty(cols, dtype=weight.dtype, device=device)
+    grad_weight = _like(weight, weight.dtype)
     lib = B._activations or B.load_activations()
     work = torch.empty(lib.leap_rms_norm8_work(rows, cols), dtype=torch.float32, device=device)
     _call("leap_rms_norm8_backward", device, grad.data_ptr(), _TYPES[grad.dtype], stride, _address(grad_sum), sum_stride, _TYPES[dtype],
@@ -275,8 +296,8 @@ def linear8_backward(grad: torch.Tensor, x: Packed8, weight: torch.Tensor, need_
     _, _, stride = _gradient(grad, x.shape[:-1] + (out,), x.device, (torch.bfloat16,), "grad")
     if dtype not in (torch.bfloat16, torch.float32):
         raise ValueError("grad_x is bfloat16 or float32")
-    grad_x = torch.empty(x.shape, dtype=dtype, device=x.device) if need_x else None
-    grad_weight = torch.empty((out, cols), dtype=torch.bfloat16, device=x.device) if need_weight else None
+    grad_x = _like(x.codes, dtype) if need_x else None
+    grad_weight = _like(weight, torch.bfloat16) if need_weight else None
     work = _work("leap_linear8_backward_work", x.device, grad.data_ptr(), stride, x.codes.data_ptr(), rows, cols, weight.data_ptr(), w_stride, out)
     _call("leap_linear8_backward", x.device, grad.data_ptr(), stride, x.codes.data_ptr(), x.scales.data_ptr(), rows, cols, weight.data_ptr(),
           w_stride, out, _address(grad_x), _TYPES[dtype], _address(grad_weight), _address(work))
@@ -343,8 +364,8 @@ def gated_linear8_backward(grad: torch.Tensor, kept: Packed8, x: Packed8, weight
     if halves != out or kept.device != x.device:
         raise ValueError(f"kept {tuple(kept.shape)} is not of this weight {tuple(weight.shape)}, or on another device")
     stride = _gradient(grad, lead + (out,), x.device, (torch.bfloat16,), "grad")[2]
-    grad_x = torch.empty(x.shape, dtype=torch.bfloat16, device=x.device) if need_x else None
-    grad_weight = torch.empty((2 * out, cols), dtype=torch.bfloat16, device=x.device) if need_weight else None
+    grad_x = _like(x.codes, torch.bfloat16) if need_x else None
+    grad_weight = _like(weight, torch.bfloat16) if need_weight else None
     work = _work("leap_gated_linear8_backward_work", x.device, x.codes.data_ptr(), rows, cols, weight.data_ptr(), w_stride, out)
     _call("leap_gated_linear8_backward", x.device, grad.data_ptr(), stride, kept.codes.data_ptr(), kept.scales.data_ptr(), x.codes.data_ptr(), x.scales.data_ptr(),
           rows, cols, weight.data_ptr(), w_stride, out, _address(grad_x), B.LEAP_BF16, _address(grad_weight), _address(work))
@@ -363,7 +384,7 @@ class _FeedForward8(torch.autograd.Function):
         _norm_weight(norm_weight, x, cols)
         hidden, up_stride = _halves(up, cols, device, "up")
         out, down_stride = _weight(down, hidden, device, "down")
-        total = None if residual is None else torch.empty(x.shape, dtype=x.dtype, device=device)
+        total = None if residual is None else _like(x, x.dtype)
         y = torch.empty(x.shape[:-1] + (out,), dtype=x.dtype, device=device)
         lib = B._activations or B.load_activations()
         kept = torch.empty(lib.leap_feed_forward8_kept(rows, cols, hidden), dtype=torch.uint8, device=device)
@@ -391,9 +412,9 @@ class _FeedForward8(torch.autograd.Function):
         grad_y = grad_y.contiguous()
         grad_sum = None if grad_sum is None else grad_sum.contiguous()
         grad_x = torch.empty(ctx.shape, dtype=torch.bfloat16, device=device) if need_x or need_r or need_norm else None
-        grad_norm = torch.empty(cols, dtype=norm_weight.dtype, device=device) if need_norm else None
-        grad_up = torch.empty((2 * hidden, cols), dtype=torch.bfloat16, device=device) if need_up else None
-        grad_down = torch.empty((out, hidden), dtype=torch.bfloat16, device=device) if need_down else None
+        grad_norm = _like(norm_weight, norm_weight.dtype) if need_norm else None
+        grad_up = _like(up, torch.bfloat16) if need_up else None
+        grad_down = _like(down, torch.bfloat16) if need_down else None
         weights = (up.data_ptr(), up_stride, hidden, down.data_ptr(), down_stride, out)
         work = _work("leap_feed_forward8_backward_work", device, grad_y.data_ptr(), out, rows, cols, *weights)
         _call("leap_feed_forward8_backward", device, grad_y.data_ptr(), out, _address(grad_sum), cols, norm_weight.data_ptr(), _TYPES[norm_weight.dtype],
