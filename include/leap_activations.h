@@ -87,13 +87,21 @@ int leap_gated_linear8(const uint8_t *d_codes, const uint8_t *d_scales, int64_t 
                        void *d_work, void *hip_stream);
 
 /* Its gradients from da = dL/d gated ([rows][out] bfloat16 with a stride): leap_gate8_backward (below), then leap_linear8_backward of du, which is
- * in the workspace; grad_x [rows][cols] of grad_x_type and grad_weight [2 * out][cols], either may be NULL.  d_work:
+ * in the workspace, in bfloat16; grad_x [rows][cols] of grad_x_type and grad_weight [2 * out][cols], either may be NULL.  d_work:
  * leap_gated_linear8_backward_work() bytes, 16-byte aligned (no rows: may be NULL). */
 int64_t leap_gated_linear8_backward_work(const uint8_t *d_codes, int64_t rows, int64_t cols, const void *d_weight, int64_t w_stride, int64_t out);
 int leap_gated_linear8_backward(const void *d_da, int64_t da_stride, const uint8_t *d_kept_codes, const uint8_t *d_kept_scales,
                                 const uint8_t *d_codes, const uint8_t *d_scales, int64_t rows, int64_t cols, const void *d_weight,
                                 int64_t w_stride, int64_t out, void *d_grad_x, int32_t grad_x_type, void *d_grad_weight, void *d_work,
                                 void *hip_stream);
+
+/* The same with du held as the sum of two bfloat16, to 2^-17 of a value (2^-9 above), so that grad_x and grad_weight are rounded once, at the end;
+ * the products take twice as long, and du twice the room. */
+int64_t leap_gated_linear8_backward_fine_work(const uint8_t *d_codes, int64_t rows, int64_t cols, const void *d_weight, int64_t w_stride, int64_t out);
+int leap_gated_linear8_backward_fine(const void *d_da, int64_t da_stride, const uint8_t *d_kept_codes, const uint8_t *d_kept_scales,
+                                     const uint8_t *d_codes, const uint8_t *d_scales, int64_t rows, int64_t cols, const void *d_weight,
+                                     int64_t w_stride, int64_t out, void *d_grad_x, int32_t grad_x_type, void *d_grad_weight, void *d_work,
+                                     void *hip_stream);
 
 /* du [rows][2 * out] (bfloat16) from kept = (g, p) and da = dL/d gated: the gate's half da * p * s * (1 + g * (1 - s)), the
  * other da * g * s, with s = sigmoid(g).  With u's gradient in hand leap_linear8_backward gives those of v and W.
@@ -127,6 +135,15 @@ int leap_feed_forward8_backward(const void *d_dy, int64_t dy_stride, const void 
                                 int32_t norm_weight_type, int64_t rows, int64_t cols, const void *d_up, int64_t up_stride, int64_t hidden,
                                 const void *d_down, int64_t down_stride, int64_t out, const void *d_kept, void *d_grad_x,
                                 void *d_grad_norm_weight, void *d_grad_up, void *d_grad_down, void *d_work, void *hip_stream);
+
+/* The same with du, the gradient of the product with `up`, held as the sum of two bfloat16 (leap_gated_linear8_backward_fine says what that
+ * takes and gives). */
+int64_t leap_feed_forward8_backward_fine_work(const void *d_dy, int64_t dy_stride, int64_t rows, int64_t cols, const void *d_up, int64_t up_stride,
+                                              int64_t hidden, const void *d_down, int64_t down_stride, int64_t out);
+int leap_feed_forward8_backward_fine(const void *d_dy, int64_t dy_stride, const void *d_grad_sum, int64_t grad_sum_stride, const void *d_norm_weight,
+                                     int32_t norm_weight_type, int64_t rows, int64_t cols, const void *d_up, int64_t up_stride, int64_t hidden,
+                                     const void *d_down, int64_t down_stride, int64_t out, const void *d_kept, void *d_grad_x,
+                                     void *d_grad_norm_weight, void *d_grad_up, void *d_grad_down, void *d_work, void *hip_stream);
 
 #ifdef __cplusplus
 }

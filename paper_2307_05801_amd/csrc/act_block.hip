@@ -53,19 +53,17 @@ struct block_sizes {
         const int64_t a = leap_linear8_work(K.normed, rows, cols, up, up_stride, 2 * hidden), b = leap_linear8_work(K.gated, rows, hidden, down, down_stride, out);
         return a > b ? a : b;
     }
-    // The parts' workspaces take turns behind du (bfloat16) and the norm's gradient (32 bits).
-    int64_t du_bytes() const { return rows * padded_row(2 * hidden) * 2; }
+    // The parts' workspaces take turns behind du and the norm's gradient (32 bits).
     int64_t dn_bytes() const { return up16(rows * cols * 4); }
-    int64_t backward_work(const void *dy, int64_t dy_stride, const void *kept) const
+    int64_t backward_work(const void *dy, int64_t dy_stride, const du_layout &L) const
     {
-        const kept_block K((void *)kept, rows, cols, hidden);
-        const void *du = (const void *)16;                                          // aligned, as it will be
+        const kept_block K(nullptr, rows, cols, hidden);
         int64_t most = leap_rms_norm8_work(rows, cols) * 4;
         for (int64_t n : {leap_linear8_backward_work(dy, dy_stride, K.gated, rows, hidden, down, down_stride, out),
                           leap_linear_gate8_work(dy, dy_stride, down, down_stride, out, rows, hidden),
-                          linear8_backward_work(du, padded_row(2 * hidden), true, K.normed, rows, cols, up, up_stride, 2 * hidden)})
+                          du_backward_work(L, K.normed, rows, cols, up, up_stride, 2 * hidden)})
             most = n > most ? n : most;
-        return du_bytes() + dn_bytes() + up16(most);
+        return L.bytes(rows) + dn_bytes() + up16(most);
     }
 };
 
@@ -105,11 +103,54 @@ extern "C" int leap_feed_forward8(const void *d_x, int64_t x_stride, const void 
     return rc;
 }
 
+namespace {
+
+int64_t block_backward_work(bool fine, const void *d_dy, int64_t dy_stride, const block_sizes &S)
+{
+    return S.bad() || bad_stride(dy_stride, S.rows, S.out) ? 0 : S.backward_work(d_dy, dy_stride, du_in_workspace(S.hidden, fine));
+}
+
+int block_backward(bool fine, const void *d_dy, int64_t dy_stride, const void *d_grad_sum, int64_t grad_sum_stride, const void *d_norm_weight,
+                   int32_t norm_weight_type, const block_sizes &S, const void *d_kept, void *d_grad_x, void *d_grad_norm_weight, void *d_grad_up,
+                   void *d_grad_down, void *d_work, void *hip_stream)
+{
+    if (const char *why = S.bad()) return refuse(why);
+    const int64_t rows = S.rows, cols = S.cols, hidden = S.hidden, out = S.out;
+    if (const char *why = bad_stride(dy_stride, rows, out)) return refuse(why);
+    if (rows && (!d_kept || (uintptr_t)d_kept % 16 != 0)) return refuse("what is kept needs memory from a multiple of 16 bytes on");
+    if (rows && (!d_dy || !S.up || !S.down)) return refuse("null data pointer");
+    if (const char *why = d_grad_sum ? bad_stride(grad_sum_stride, rows, cols) : nullptr) return refuse(why);
+    if (norm_weight_type != LEAP_F32 && norm_weight_type != LEAP_BF16) return refuse("the norm's weight must be float32 or bfloat16");
+    if (rows && (d_grad_x || d_grad_norm_weight) && !d_norm_weight) return refuse("null data pointer");
+    if (rows && d_grad_norm_weight && !d_grad_x) return refuse("the norm's weight gradient comes with grad_x");
+    if (!d_work || (uintptr_t)d_work % 16 != 0) return refuse("the workspace needs memory from a multiple of 16 bytes on");
+    const kept_block K((void *)d_kept, rows, cols, hidden);
+    // du is bfloat16, which the matrix units take: grad_up is 0.0024 of its norm off, grad_norm_weight 0.0024 to 0.0034, where 0.0017 are their own
+    // rounding to bfloat16.  A caller who wants that alone asks for a fine du, whose products take twice as long (262144 x 512 through 1024, forward and
+    // backward: 4.79 ms, 3.53).  32 bits between the product and the norm: a rounding less in grad_x.
+    const du_layout L = du_in_workspace(hidden, fine);
+    uint8_t *const du = (uint8_t *)d_work, *const dn = du + L.bytes(rows), *const work = dn + S.dn_bytes();
+    int rc = LEAP_OK;
+    if (d_grad_down)
+        rc = leap_linear8_backward(d_dy, dy_stride, K.gated, K.gated_scales, rows, hidden, S.down, S.down_stride, out, nullptr, LEAP_BF16, d_grad_down, work, hip_stream);
+    if (rc == LEAP_OK && (d_grad_x || d_grad_up)) {
+        rc = linear_gate8_backward(d_dy, dy_stride, S.down, S.down_stride, out, K.gate, K.gate_scales, rows, hidden, du, L, work, hip_stream);
+        if (rc == LEAP_OK)
+            rc = du_backward(du, L, K.normed, K.normed_scales, rows, cols, S.up, S.up_stride, 2 * hidden, d_grad_x ? dn : nullptr, LEAP_F32, d_grad_up, work,
+                             hip_stream);
+    }
+    if (rc == LEAP_OK && (d_grad_x || d_grad_norm_weight))
+        rc = leap_rms_norm8_backward(dn, LEAP_F32, cols, d_grad_sum, grad_sum_stride, LEAP_BF16, K.sum, K.sum_scales, K.rstd, d_norm_weight, norm_weight_type,
+                                     rows, cols, d_grad_x, d_grad_norm_weight, (float *)work, hip_stream);
+    return rc;
+}
+
+}  // namespace
+
 extern "C" int64_t leap_feed_forward8_backward_work(const void *d_dy, int64_t dy_stride, int64_t rows, int64_t cols, const void *d_up, int64_t up_stride,
                                                     int64_t hidden, const void *d_down, int64_t down_stride, int64_t out)
 {
-    const block_sizes S{rows, cols, hidden, out, d_up, d_down, up_stride, down_stride};
-    return S.bad() || bad_stride(dy_stride, rows, out) ? 0 : S.backward_work(d_dy, dy_stride, nullptr);
+    return block_backward_work(false, d_dy, dy_stride, {rows, cols, hidden, out, d_up, d_down, up_stride, down_stride});
 }
 
 extern "C" int leap_feed_forward8_backward(const void *d_dy, int64_t dy_stride, const void *d_grad_sum, int64_t grad_sum_stride, const void *d_norm_weight,
@@ -117,31 +158,21 @@ extern "C" int leap_feed_forward8_backward(const void *d_dy, int64_t dy_stride, 
                                            const void *d_down, int64_t down_stride, int64_t out, const void *d_kept, void *d_grad_x,
                                            void *d_grad_norm_weight, void *d_grad_up, void *d_grad_down, void *d_work, void *hip_stream)
 {
-    const block_sizes S{rows, cols, hidden, out, d_up, d_down, up_stride, down_stride};
-    if (const char *why = S.bad()) return refuse(why);
-    if (const char *why = bad_stride(dy_stride, rows, out)) return refuse(why);
-    if (rows && (!d_kept || (uintptr_t)d_kept % 16 != 0)) return refuse("what is kept needs memory from a multiple of 16 bytes on");
-    if (rows && (!d_dy || !d_up || !d_down)) return refuse("null data pointer");
-    if (const char *why = d_grad_sum ? bad_stride(grad_sum_stride, rows, cols) : nullptr) return refuse(why);
-    if (norm_weight_type != LEAP_F32 && norm_weight_type != LEAP_BF16) return refuse("the norm's weight must be float32 or bfloat16");
-    if (rows && (d_grad_x || d_grad_norm_weight) && !d_norm_weight) return refuse("null data pointer");
-    if (rows && d_grad_norm_weight && !d_grad_x) return refuse("the norm's weight gradient comes with grad_x");
-    if (!d_work || (uintptr_t)d_work % 16 != 0) return refuse("the workspace needs memory from a multiple of 16 bytes on");
-    const kept_block K((void *)d_kept, rows, cols, hidden);
-    uint8_t *const du = (uint8_t *)d_work, *const dn = du + S.du_bytes(), *const work = dn + S.dn_bytes();
-    int rc = LEAP_OK;
-    if (d_grad_down)
-        rc = leap_linear8_backward(d_dy, dy_stride, K.gated, K.gated_scales, rows, hidden, d_down, down_stride, out, nullptr, LEAP_BF16, d_grad_down, work, hip_stream);
-    if (rc == LEAP_OK && (d_grad_x || d_grad_up)) {
-        rc = linear_gate8_backward(d_dy, dy_stride, d_down, down_stride, out, K.gate, K.gate_scales, rows, hidden, du, padded_row(2 * hidden), work, hip_stream);
-        // du is bfloat16, which the matrix units take (in 32 bits it would be split in two, for twice the products' time): 0.0017 of the norm
-        // of what comes of it, as much as rounding that to bfloat16.  32 bits between the product and the norm: a rounding less in grad_x.
-        if (rc == LEAP_OK)
-            rc = linear8_backward(du, padded_row(2 * hidden), true, K.normed, K.normed_scales, rows, cols, d_up, up_stride, 2 * hidden, d_grad_x ? dn : nullptr,
-                                  LEAP_F32, d_grad_up, work, hip_stream);
-    }
-    if (rc == LEAP_OK && (d_grad_x || d_grad_norm_weight))
-        rc = leap_rms_norm8_backward(dn, LEAP_F32, cols, d_grad_sum, grad_sum_stride, LEAP_BF16, K.sum, K.sum_scales, K.rstd, d_norm_weight, norm_weight_type,
-                                     rows, cols, d_grad_x, d_grad_norm_weight, (float *)work, hip_stream);
-    return rc;
+    return block_backward(false, d_dy, dy_stride, d_grad_sum, grad_sum_stride, d_norm_weight, norm_weight_type,
+                          {rows, cols, hidden, out, d_up, d_down, up_stride, down_stride}, d_kept, d_grad_x, d_grad_norm_weight, d_grad_up, d_grad_down, d_work, hip_stream);
+}
+
+extern "C" int64_t leap_feed_forward8_backward_fine_work(const void *d_dy, int64_t dy_stride, int64_t rows, int64_t cols, const void *d_up, int64_t up_stride,
+                                                         int64_t hidden, const void *d_down, int64_t down_stride, int64_t out)
+{
+    return block_backward_work(true, d_dy, dy_stride, {rows, cols, hidden, out, d_up, d_down, up_stride, down_stride});
+}
+
+extern "C" int leap_feed_forward8_backward_fine(const void *d_dy, int64_t dy_stride, const void *d_grad_sum, int64_t grad_sum_stride, const void *d_norm_weight,
+                                                int32_t norm_weight_type, int64_t rows, int64_t cols, const void *d_up, int64_t up_stride, int64_t hidden,
+                                                const void *d_down, int64_t down_stride, int64_t out, const void *d_kept, void *d_grad_x,
+                                                void *d_grad_norm_weight, void *d_grad_up, void *d_grad_down, void *d_work, void *hip_stream)
+{
+    return block_backward(true, d_dy, dy_stride, d_grad_sum, grad_sum_stride, d_norm_weight, norm_weight_type,
+                          {rows, cols, hidden, out, d_up, d_down, up_stride, down_stride}, d_kept, d_grad_x, d_grad_norm_weight, d_grad_up, d_grad_down, d_work, hip_stream);
 }

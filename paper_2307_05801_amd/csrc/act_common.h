@@ -198,6 +198,13 @@ __device__ inline void pack_chunk(const float (&v)[CHUNK], int n, uint8_t *codes
     }
 }
 
+// What rounding v to bfloat16 leaves of it; nothing of what becomes an infinity or NaN.
+__device__ inline float rest_of_bf16(float v)
+{
+    const float rest = v - (float)(__bf16)v;
+    return finite_magnitude(rest) ? rest : 0.0f;
+}
+
 // 1 / (1 + exp(-g)) within a few units of the last place.  exp(-g) is the square of exp(-g / 2): an exponent that carries an offset
 // would lose what the offset's size rounds away.  Its 2^-32nd part does not overflow before the result is zero, and the reciprocal
 // of that, which the hardware forms within a unit but not as a subnormal number, is brought back by a product.
@@ -273,14 +280,19 @@ template <class F> inline int by_type(int32_t type, F &&f)
 // Values from one row to the next where rows of bfloat16 are followed by zeros up to a multiple of 16 bytes: such rows are not laid out anew.
 inline int64_t padded_row(int64_t cols) { return (cols + 7) / 8 * 8; }
 
-// leap_linear8_backward of a dy whose rows are so padded, or are not; leap_linear_gate8_backward to a du with rows du_stride apart, zeros
-// between them.
-int64_t linear8_backward_work(const void *d_dy, int64_t dy_stride, bool padded, const uint8_t *d_codes, int64_t rows, int64_t cols, const void *d_weight,
-                              int64_t w_stride, int64_t out);
-int linear8_backward(const void *d_dy, int64_t dy_stride, bool padded, const uint8_t *d_codes, const uint8_t *d_scales, int64_t rows, int64_t cols,
-                     const void *d_weight, int64_t w_stride, int64_t out, void *d_grad_x, int32_t grad_x_type, void *d_grad_weight, void *d_work,
-                     void *hip_stream);
+// How du [rows][2 * out] lies: in bfloat16, rows `stride` apart with zeros between them; or, fine, as the sum of two such arrays side by side,
+// the rounded values and what their rounding leaves, which is du to 2^-17 of each value.
+struct du_layout {
+    int64_t low, stride;               // values from one of du to its rest (0: none); from row to row
+    __host__ __device__ int64_t bytes(int64_t rows) const { return rows * stride * 2; }
+};
+inline du_layout du_in_workspace(int64_t out, bool fine) { return {fine ? padded_row(2 * out) : 0, padded_row(2 * out) * (fine ? 2 : 1)}; }
+
+// leap_linear8_backward of a du that lies like that, and leap_linear_gate8_backward to one; `out`: of the weight's rows, twice the gate's.
+int64_t du_backward_work(const du_layout &L, const uint8_t *d_codes, int64_t rows, int64_t cols, const void *d_weight, int64_t w_stride, int64_t out);
+int du_backward(const void *d_du, const du_layout &L, const uint8_t *d_codes, const uint8_t *d_scales, int64_t rows, int64_t cols, const void *d_weight,
+                int64_t w_stride, int64_t out, void *d_grad_x, int32_t grad_x_type, void *d_grad_weight, void *d_work, void *hip_stream);
 int linear_gate8_backward(const void *d_dy, int64_t dy_stride, const void *d_weight, int64_t w_stride, int64_t next, const uint8_t *d_kept_codes,
-                          const uint8_t *d_kept_scales, int64_t rows, int64_t out, void *d_du, int64_t du_stride, void *d_work, void *hip_stream);
+                          const uint8_t *d_kept_scales, int64_t rows, int64_t out, void *d_du, const du_layout &L, void *d_work, void *hip_stream);
 
 }  // namespace act

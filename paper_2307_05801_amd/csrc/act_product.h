@@ -428,16 +428,19 @@ struct scale_run {
 };
 
 // What becomes of D: rows of bfloat16; of float (of its part of k, `part` floats apart); gate and the other half packed, and
-// their gated product; the gradient of those two from D and what is kept of them.
-enum { TO_WIDE, TO_FULL, TO_GATED, TO_GATE_GRAD };
+// their gated product; the gradient of those two from D and what is kept of them, and the same beside what its rounding leaves.
+enum { TO_WIDE, TO_FULL, TO_GATED, TO_GATE_GRAD, TO_GATE_GRAD_FINE };
+
+template <int TO> constexpr bool gate_grad() { return TO == TO_GATE_GRAD || TO == TO_GATE_GRAD_FINE; }
 
 // Whether a block goes on to further tiles; where not, all of its shared memory is write()'s.
-template <int TO> constexpr bool stays() { return TO != TO_GATE_GRAD; }
+template <int TO> constexpr bool stays() { return !gate_grad<TO>(); }
 
 struct result {
     void *out;
     int64_t stride, part;
     int64_t columns;                       // gated: of `out`
+    int64_t low;                           // from a value of a fine gradient to what its rounding leaves
     uint8_t *gated_codes, *gated_scales, *kept_codes, *kept_scales;
 };
 
@@ -569,7 +572,7 @@ __global__ __launch_bounds__(WI * WJ * GROUPS * 64, WI * WJ * GROUPS > 4 ? 1 : 2
     // A tile's results, through the buffer that was multiplied last.  A wave's: rows j_wave .. , columns i_wave .. .
     const auto write = [&](const place &of, lds_byte *area) {
         const int64_t j_wave = of.j + wj * FJ * 32, i_wave = of.i + wi * (TO == TO_GATED ? FI / 2 : FI) * 32, groups = groups_of(R.columns);
-        area += wave * (TO == TO_GATE_GRAD ? FI * 4096 : AREA);
+        area += wave * (gate_grad<TO>() ? FI * 4096 : AREA);
         // addresses are formed here: worked out ahead of the tiles they would take registers from the products
         int lane = threadIdx.x % 64;
         asm volatile("" : "+v"(lane));
@@ -649,7 +652,10 @@ __global__ __launch_bounds__(WI * WJ * GROUPS * 64, WI * WJ * GROUPS > 4 ? 1 : 2
             const landing kept_p(R.kept_codes, j_wave, Q.rows, 2 * R.columns, R.columns + i_wave, 2 * R.columns, FI * 32);
             landing to_g(R.out, j_wave, Q.rows, 2 * R.stride, 2 * i_wave, 2 * R.columns, FI * 64);
             landing to_p(R.out, j_wave, Q.rows, 2 * R.stride, 2 * (R.columns + i_wave), 4 * R.columns, FI * 64);
-            if (Q.rows * R.stride * 2 <= READ_NEXT) to_g.past = to_p.past = false;
+            constexpr bool FINE = TO == TO_GATE_GRAD_FINE;
+            landing rest_g(R.out, j_wave, Q.rows, 2 * R.stride, 2 * (R.low + i_wave), 2 * (R.low + R.columns), FI * 64);
+            landing rest_p(R.out, j_wave, Q.rows, 2 * R.stride, 2 * (R.low + R.columns + i_wave), 2 * (R.low + 2 * R.columns), FI * 64);
+            if (Q.rows * R.stride * 2 <= READ_NEXT) to_g.past = to_p.past = rest_g.past = rest_p.past = false;
             u32x4 raw[2][room::TURNS];
             uint32_t bytes_of[2];                                    // a byte a group: at most four
             const auto load = [&](int t) {
@@ -684,6 +690,7 @@ __global__ __launch_bounds__(WI * WJ * GROUPS * 64, WI * WJ * GROUPS > 4 ? 1 : 2
                 const wide x{area + 2 * ARRAY};
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
+                    [[maybe_unused]] f32x16 rest[FINE ? FI : 1];
 #pragma unroll
                     for (int f = 0; f < FI; ++f) {
                         f32x16 v = acc[f][t];                        // the other half's gradient waits in acc
@@ -700,12 +707,28 @@ __global__ __launch_bounds__(WI * WJ * GROUPS * 64, WI * WJ * GROUPS > 4 ? 1 : 2
 #pragma unroll
                         for (int q = 0; q < 4; ++q)
                             x.put_half(lane % 32, f * 4 + q, half, two_bf16(v[4 * q], v[4 * q + 1]), two_bf16(v[4 * q + 2], v[4 * q + 3]));
+                        if constexpr (FINE) {
+#pragma unroll
+                            for (int y = 0; y < 16; ++y) rest[f][y] = rest_of_bf16(v[y]);
+                        }
                         __builtin_amdgcn_sched_barrier(0);
                     }
                     x.turn();
                     (h ? to_p : to_g).template write<2, true>(x, t * 32, 0, lane);
                     x.turn();
                     __builtin_amdgcn_sched_barrier(0);
+                    if constexpr (FINE) {
+#pragma unroll
+                        for (int f = 0; f < FI; ++f)
+#pragma unroll
+                            for (int q = 0; q < 4; ++q)
+                                x.put_half(lane % 32, f * 4 + q, half, two_bf16(rest[f][4 * q], rest[f][4 * q + 1]),
+                                           two_bf16(rest[f][4 * q + 2], rest[f][4 * q + 3]));
+                        x.turn();
+                        (h ? rest_p : rest_g).template write<2, true>(x, t * 32, 0, lane);
+                        x.turn();
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
                 }
             }
         }

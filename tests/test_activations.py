@@ -221,3 +221,28 @@ def test_the_reference_notices_a_wrong_code():
     for wrong in ((codes + 1, scales), (codes, scales - 1)):
         with pytest.raises(AssertionError):
             R.assert_held(Packed8(wrong[0].view(torch.float8_e4m3fn), wrong[1]), x, none)
+
+
+def test_bad_arguments_of_the_fine_gradients_are_refused_with_a_message(lib):
+    good = (P, 8, P, P, P, P, 4, 64, P, 64, 8, P, 1, P, P, 0)
+    for at, value in [(1, 7), (6, -1), (7, 0), (9, 63), (10, 0), (10, 1 << 20), (12, 2), (0, 0), (2, 0), (3, 0), (4, 0), (5, 0), (8, 0), (14, 0), (14, P + 8)]:
+        arguments = list(good)
+        arguments[at] = value
+        assert lib.leap_gated_linear8_backward_fine(*arguments) == B.LEAP_INVALID_ARG, (at, value)
+        assert lib.leap_last_error()
+    for at, value in [(1, 15), (3, 63), (4, 0), (5, 2), (15, 0), (6, -1), (7, 0), (9, 63), (10, 0), (10, 1 << 20), (12, 7), (13, 0), (0, 0), (8, 0), (11, 0), (14, 0),
+                      (14, P + 4), (19, 0), (19, P + 8)]:
+        arguments = list(BLOCK_BACKWARD)
+        arguments[at] = value
+        assert lib.leap_feed_forward8_backward_fine(*arguments) == B.LEAP_INVALID_ARG, (at, value)
+        assert lib.leap_last_error()
+
+
+def test_memory_of_the_fine_gradients(lib):
+    """du twice, in rows of whole 16 bytes; the weight twice, zeros between; both halves of the weight's gradient in 32 bits."""
+    assert lib.leap_gated_linear8_backward_fine_work(P, 5, 64, P, 64, 9) == 5 * 48 * 2 + (24 + 18) * 64 * 2 + 2 * 24 * 64 * 4
+    assert lib.leap_gated_linear8_backward_fine_work(P, 5, 40, P, 40, 8) == 5 * 32 * 2 + 32 * 40 * 2 + 2 * 16 * 40 * 4 + 5 * 48
+    assert lib.leap_gated_linear8_backward_fine_work(P, 5, 64, P, 64, 0) == 0 and lib.leap_gated_linear8_backward_fine_work(P, -1, 64, P, 64, 8) == 0
+    plain = lib.leap_feed_forward8_backward_work(P, 24, 4, 64, P, 64, 16, P, 16, 24)
+    assert lib.leap_feed_forward8_backward_fine_work(P, 24, 4, 64, P, 64, 16, P, 16, 24) >= plain + 4 * 2 * 16 * 2
+    assert lib.leap_feed_forward8_backward_fine_work(P, 23, 4, 64, P, 64, 16, P, 16, 24) == 0
