@@ -313,6 +313,7 @@ namespace {
 // twice as long with the weight twice, one below the other, and grad_weight adds the two halves of twice as many rows.
 int64_t backward_work(const laid &G, int64_t low, const uint8_t *d_codes, int64_t rows, int64_t cols, const void *d_weight, int64_t w_stride, int64_t out)
 {
+    if (!rows) return 0;                             // of nothing: nothing is laid out
     const int64_t deep = low + out;
     laid W(d_weight, w_stride, out, cols, 2);
     const int64_t weight = low ? (low + out) * W.pitch : W.room();

@@ -246,3 +246,14 @@ def test_memory_of_the_fine_gradients(lib):
     plain = lib.leap_feed_forward8_backward_work(P, 24, 4, 64, P, 64, 16, P, 16, 24)
     assert lib.leap_feed_forward8_backward_fine_work(P, 24, 4, 64, P, 64, 16, P, 16, 24) >= plain + 4 * 2 * 16 * 2
     assert lib.leap_feed_forward8_backward_fine_work(P, 23, 4, 64, P, 64, 16, P, 16, 24) == 0
+
+
+def test_no_rows_need_no_workspace(lib):
+    """The gradients of nothing: no copy of a weight that is not laid out (343 columns), no parts."""
+    assert lib.leap_linear8_backward_work(None, 8, None, 0, 343, None, 343, 8) == 0
+    assert lib.leap_gated_linear8_backward_work(None, 0, 343, None, 343, 8) == 0
+    assert lib.leap_gated_linear8_backward_fine_work(None, 0, 343, None, 343, 8) == 0
+    assert lib.leap_linear8_backward(None, 8, None, None, 0, 343, None, 343, 8, P, 1, None, None, None) == B.LEAP_OK
+    for name in ("leap_gated_linear8_backward", "leap_gated_linear8_backward_fine"):
+        for work in (None, P):
+            assert getattr(lib, name)(None, 8, None, None, None, None, 0, 343, None, 343, 8, P, 1, None, work, None) == B.LEAP_OK
