@@ -198,13 +198,15 @@ class keep_in_8_bits(torch.autograd.graph.saved_tensors_hooks):
     (3 mantissa bits)."""
 
     def __init__(self, min_values: int = 1 << 16):
+        # What is kept as it is is kept detached: an output that its own operation saves would hold its graph, and that the output.
+        # Autograd takes it back into the graph by itself.
         def pack(t):
             if not t.is_cuda or t.dtype not in _TYPES or t.numel() < min_values or (t.is_leaf and t.requires_grad):
-                return t
+                return t.detach()
             try:
                 _rows(t, "tensor")
             except ValueError:
-                return t
+                return t.detach()
             return pack8(t.detach()), t.dtype
 
         def unpack(kept):

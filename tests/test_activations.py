@@ -257,3 +257,37 @@ def test_no_rows_need_no_workspace(lib):
     for name in ("leap_gated_linear8_backward", "leap_gated_linear8_backward_fine"):
         for work in (None, P):
             assert getattr(lib, name)(None, 8, None, None, None, None, 0, 343, None, 343, 8, P, 1, None, work, None) == B.LEAP_OK
+
+
+# ---- keep_in_8_bits: what it keeps as it is (on the CPU that is everything) ----
+
+
+def test_outputs_kept_for_a_backward_pass_that_never_runs_are_freed():
+    """exp saves its own output, whose graph leads back to it: the hook must not close that circle."""
+    import gc
+    import weakref
+    from paper_2307_05801_amd.activations import keep_in_8_bits
+    x = torch.randn(100, requires_grad=True)
+    with keep_in_8_bits():
+        y = (x * 1.0).exp()
+    alive = weakref.ref(y)
+    del y
+    gc.collect()
+    assert alive() is None
+
+
+def test_gradients_through_what_is_kept_as_it_is():
+    """First and second derivatives, outputs and leaves that are saved, operations in place that save their result."""
+    from paper_2307_05801_amd.activations import keep_in_8_bits
+    x, w = (torch.randn(50, dtype=torch.float64, generator=torch.Generator().manual_seed(k), requires_grad=True) for k in (1, 2))
+
+    def f():
+        return (torch.tanh(x * w).exp_() * w).sigmoid_().sum()
+
+    want = torch.autograd.grad(f(), (x, w), create_graph=True)
+    want += torch.autograd.grad(want[0].square().sum(), (x, w))
+    with keep_in_8_bits():
+        value = f()
+        got = torch.autograd.grad(value, (x, w), create_graph=True)
+        got += torch.autograd.grad(got[0].square().sum(), (x, w))
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
