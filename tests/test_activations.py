@@ -282,7 +282,7 @@ def test_gradients_through_what_is_kept_as_it_is():
     x, w = (torch.randn(50, dtype=torch.float64, generator=torch.Generator().manual_seed(k), requires_grad=True) for k in (1, 2))
 
     def f():
-        return (torch.tanh(x * w).exp_() * w).sigmoid_().sum()
+        return ((torch.tanh(x * w) * w).exp_() * x).sigmoid_().sum()
 
     want = torch.autograd.grad(f(), (x, w), create_graph=True)
     want += torch.autograd.grad(want[0].square().sum(), (x, w))
