@@ -199,18 +199,27 @@ class keep_in_8_bits(torch.autograd.graph.saved_tensors_hooks):
 
     def __init__(self, min_values: int = 1 << 16):
         # What is kept as it is is kept detached: an output that its own operation saves would hold its graph, and that the output.
-        # Autograd takes it back into the graph by itself.
+        # Autograd takes it back into the graph by itself, but leaves it to the hooks to notice that it was changed in place.
+        def as_it_is(t):
+            return t.detach(), t._version
+
         def pack(t):
             if not t.is_cuda or t.dtype not in _TYPES or t.numel() < min_values or (t.is_leaf and t.requires_grad):
-                return t.detach()
+                return as_it_is(t)
             try:
                 _rows(t, "tensor")
             except ValueError:
-                return t.detach()
+                return as_it_is(t)
             return pack8(t.detach()), t.dtype
 
         def unpack(kept):
-            return kept if isinstance(kept, torch.Tensor) else kept[0].unpack(kept[1])
+            held, known = kept
+            if isinstance(held, Packed8):
+                return held.unpack(known)
+            if held._version != known:
+                raise RuntimeError(f"a tensor kept for the backward pass, {held.dtype} {tuple(held.shape)}, was changed in place (version {held._version}, "
+                                   f"kept at {known})")
+            return held
 
         super().__init__(pack, unpack)
 

@@ -291,3 +291,17 @@ def test_gradients_through_what_is_kept_as_it_is():
         got = torch.autograd.grad(value, (x, w), create_graph=True)
         got += torch.autograd.grad(got[0].square().sum(), (x, w))
     assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_what_is_kept_as_it_is_must_not_change_before_the_backward_pass():
+    """As without the context: an error, not a gradient of other values."""
+    from paper_2307_05801_amd.activations import keep_in_8_bits
+    x, w = torch.ones(5, requires_grad=True), torch.ones(5, requires_grad=True)
+    with keep_in_8_bits():
+        saved_output, saved_leaf = (x * 1.0).exp(), (x * w).sum()
+    saved_output.mul_(3.0)
+    with torch.no_grad():
+        w.add_(1.0)
+    for value in (saved_output.sum(), saved_leaf):
+        with pytest.raises(RuntimeError, match="in place"):
+            torch.autograd.grad(value, x)
