@@ -191,9 +191,30 @@ def unpack8(packed: Packed8, dtype: torch.dtype = torch.bfloat16) -> torch.Tenso
     return out
 
 
+_LONGEST = 1 << 20                                            # columns that the library takes
+_PIECE = 1 << 15                                              # a row that the values of longer ones are cut into: whole groups
+
+
+def _pack_flat(t: torch.Tensor):
+    """The values of a tensor without gaps, whatever its shape, in rows of _PIECE and a last shorter one: [Packed8, ...]."""
+    flat = t.view(-1)
+    whole = flat.numel() // _PIECE * _PIECE
+    return [pack8(part) for part in (flat[:whole].view(-1, _PIECE), flat[whole:]) if part.numel()]
+
+
+def _unpack_flat(parts, shape, dtype: torch.dtype) -> torch.Tensor:
+    out = torch.empty(shape, dtype=dtype, device=parts[0].device)
+    to = out.data_ptr()
+    for p in parts:
+        rows, cols, _ = _rows(p.codes, "packed")
+        _call("leap_unpack8", p.device, p.codes.data_ptr(), p.scales.data_ptr(), rows, cols, to, _TYPES[dtype])
+        to += rows * cols * dtype.itemsize
+    return out
+
+
 class keep_in_8_bits(torch.autograd.graph.saved_tensors_hooks):
-    """Inside this context what autograd saves for the backward pass is kept packed: tensors on a GPU of float32, bfloat16 or
-    float16 with at least `min_values` values and evenly spaced rows.  Leaves that want a gradient (weights) and everything
+    """Inside this context what autograd saves for the backward pass is kept packed: plain tensors on a GPU of float32, bfloat16 or
+    float16 with at least `min_values` values and evenly spaced rows (no gaps, where they have more than 2^20 columns).  Leaves that want a gradient (weights) and everything
     else are kept as they are; a weight's cast or slice is no leaf: keep its use outside.  The gradients are those of the values held
     (3 mantissa bits)."""
 
@@ -204,18 +225,23 @@ class keep_in_8_bits(torch.autograd.graph.saved_tensors_hooks):
             return t.detach(), t._version
 
         def pack(t):
-            if not t.is_cuda or t.dtype not in _TYPES or t.numel() < min_values or (t.is_leaf and t.requires_grad):
+            if (not t.is_cuda or t.dtype not in _TYPES or type(t) not in _PLAIN or t.layout is not torch.strided or t.is_nested or t.numel() < min_values
+                    or (t.is_leaf and t.requires_grad)):
                 return as_it_is(t)
             try:
-                _rows(t, "tensor")
+                cols = _rows(t, "tensor")[1]
             except ValueError:
                 return as_it_is(t)
-            return pack8(t.detach()), t.dtype
+            if cols <= _LONGEST:
+                return pack8(t.detach()), t.dtype
+            return (_pack_flat(t.detach()), (t.shape, t.dtype)) if t.is_contiguous() else as_it_is(t)
 
         def unpack(kept):
             held, known = kept
             if isinstance(held, Packed8):
                 return held.unpack(known)
+            if isinstance(held, list):
+                return _unpack_flat(held, *known)
             if held._version != known:
                 raise RuntimeError(f"a tensor kept for the backward pass, {held.dtype} {tuple(held.shape)}, was changed in place (version {held._version}, "
                                    f"kept at {known})")

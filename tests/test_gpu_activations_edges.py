@@ -1,4 +1,6 @@
 """Operators on activations in 8 bits on the GPU, at the edges of what they take: no rows, many rows, tensors that autograd saves."""
+import gc
+
 import pytest
 import torch
 
@@ -20,3 +22,63 @@ def test_gradients_of_no_rows(A, cols, out, fine):  # noqa: F811
     dx, dw = A.gated_linear8_backward(g[:, :out], kept, x, w, fine=fine)
     assert dx.shape == (0, cols) and dw.shape == w.shape and not dw.any()
     assert A.linear_gate8_backward(g, weight_of(2 * out, out, 302).cuda(), kept).shape == (0, 2 * out)
+
+
+def _kept(A, values, **options):  # noqa: F811
+    """What the context hands back of a tensor saved within it, and how many bytes stay allocated meanwhile for one saved alone."""
+    class Keep(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x, saved):
+            ctx.save_for_backward(saved)
+            return x.clone()
+
+        @staticmethod
+        def backward(ctx, g):
+            Keep.back = ctx.saved_tensors[0]
+            return g, None
+
+    x = torch.ones(1, device="cuda", requires_grad=True)
+    saved = values()
+    gc.collect()                                             # earlier classes hold what they were handed
+    before = torch.cuda.memory_allocated()
+    with A.keep_in_8_bits(**options):
+        y = Keep.apply(x, saved)
+    after = torch.cuda.memory_allocated()
+    torch.autograd.grad(y, x)
+    return saved, Keep.back, after - before
+
+
+@pytest.mark.parametrize("n", [(1 << 20) + 1, 1 << 21, (1 << 21) + 77, 3 * (1 << 20) - 1])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_saved_rows_of_more_than_a_million_values(A, n, dtype):  # noqa: F811
+    """A flattened volume is packed like any other, in groups of 32 of its memory."""
+    g = torch.Generator(device="cuda").manual_seed(303)
+    for shape in ((n,), (2, n)):
+        saved, back, room = _kept(A, lambda: torch.randn(shape, device="cuda", generator=g).to(dtype))
+        assert back.dtype is dtype and back.shape == saved.shape and saved.numel() < room < 1.1 * saved.numel() + 4096
+        codes, scales = R.pack(saved.reshape(1, -1).cpu())
+        assert torch.equal(back.double().cpu().reshape(1, -1), R.values(codes, scales))
+
+
+def test_a_loss_over_flattened_volumes(A):  # noqa: F811
+    """2 (a - b) of the values held."""
+    a = torch.randn(128, 128, 128, device="cuda", generator=torch.Generator(device="cuda").manual_seed(304), requires_grad=True)
+    b = torch.randn(128, 128, 128, device="cuda", generator=torch.Generator(device="cuda").manual_seed(305))
+    with A.keep_in_8_bits():
+        loss = (a.flatten() - b.flatten()).square().sum()
+    got = torch.autograd.grad(loss, a)[0]
+    d = (a - b).detach().flatten()
+    want = 2.0 * A.pack8(d.reshape(-1, 1024)).unpack(F32).reshape(a.shape)
+    assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("make", [
+    lambda t: t.to_sparse_csr(), lambda t: t.to_sparse(),
+    lambda t: t.as_subclass(type("Tagged", (torch.Tensor,), {})), lambda t: t.t(), lambda t: t.double(), lambda t: t.reshape(-1)[:1 << 21].expand(2, -1),
+    lambda t: torch.randn(2, (1 << 21) + 5, device="cuda")[:, :1 << 21],
+], ids=["csr", "coo", "subclass", "across", "64 bits", "expanded", "long rows apart"])
+def test_what_is_not_packed_is_kept_as_it_is(A, make):  # noqa: F811
+    saved, back, _ = _kept(A, lambda: make(torch.randn(300, 300, device="cuda", generator=torch.Generator(device="cuda").manual_seed(306))))
+    assert type(back) is type(saved) and back.layout is saved.layout
+    dense = (lambda t: t.to_dense()) if saved.layout is not torch.strided else (lambda t: t.resolve_neg())
+    assert torch.equal(dense(back).as_subclass(torch.Tensor), dense(saved).as_subclass(torch.Tensor))
