@@ -78,6 +78,8 @@ def _rows(t: torch.Tensor, what: str):
     dims = t.shape
     if len(dims) == 0 or dims[-1] < 1:
         raise ValueError(f"{what} must have rows of at least one value")
+    if t.is_neg():
+        raise ValueError(f"{what} is a negated view, whose memory holds other values; call .resolve_neg()")
     cols = dims[-1]
     if t.is_contiguous():
         return t.numel() // cols, cols, cols
@@ -278,7 +280,7 @@ def rms_norm8(x: torch.Tensor, weight: torch.Tensor, residual: torch.Tensor = No
 
 def _norm_weight(weight: torch.Tensor, x, cols: int) -> None:
     _on_gpu(weight, "weight", x.device)
-    if weight.shape != (cols,) or not weight.is_contiguous() or (weight.dtype is not torch.float32 and weight.dtype is not x.dtype):
+    if weight.shape != (cols,) or not weight.is_contiguous() or weight.is_neg() or (weight.dtype is not torch.float32 and weight.dtype is not x.dtype):
         raise ValueError(f"weight must be contiguous [{cols}], float32 or {x.dtype}")
 
 

@@ -305,3 +305,11 @@ def test_what_is_kept_as_it_is_must_not_change_before_the_backward_pass():
     for value in (saved_output.sum(), saved_leaf):
         with pytest.raises(RuntimeError, match="in place"):
             torch.autograd.grad(value, x)
+
+
+@pytest.mark.parametrize("make", [lambda: torch._neg_view(torch.zeros(4, 6)), lambda: torch.zeros(4, 1, dtype=torch.complex64).conj().imag])
+def test_rows_of_negated_views_are_refused(make):
+    """The imaginary part of a conjugate: its memory holds the values with the other sign."""
+    from paper_2307_05801_amd.activations import _rows
+    with pytest.raises(ValueError, match="negated"):
+        _rows(make(), "x")

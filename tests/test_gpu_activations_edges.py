@@ -73,12 +73,22 @@ def test_a_loss_over_flattened_volumes(A):  # noqa: F811
 
 
 @pytest.mark.parametrize("make", [
-    lambda t: t.to_sparse_csr(), lambda t: t.to_sparse(),
+    lambda t: t.to_sparse_csr(), lambda t: t.to_sparse(), lambda t: torch._neg_view(t), lambda t: torch.complex(t, t).reshape(-1, 1).conj().imag,
     lambda t: t.as_subclass(type("Tagged", (torch.Tensor,), {})), lambda t: t.t(), lambda t: t.double(), lambda t: t.reshape(-1)[:1 << 21].expand(2, -1),
     lambda t: torch.randn(2, (1 << 21) + 5, device="cuda")[:, :1 << 21],
-], ids=["csr", "coo", "subclass", "across", "64 bits", "expanded", "long rows apart"])
+], ids=["csr", "coo", "negated", "imaginary", "subclass", "across", "64 bits", "expanded", "long rows apart"])
 def test_what_is_not_packed_is_kept_as_it_is(A, make):  # noqa: F811
     saved, back, _ = _kept(A, lambda: make(torch.randn(300, 300, device="cuda", generator=torch.Generator(device="cuda").manual_seed(306))))
     assert type(back) is type(saved) and back.layout is saved.layout
     dense = (lambda t: t.to_dense()) if saved.layout is not torch.strided else (lambda t: t.resolve_neg())
     assert torch.equal(dense(back).as_subclass(torch.Tensor), dense(saved).as_subclass(torch.Tensor))
+
+
+def test_negated_views_are_refused(A):  # noqa: F811
+    """Their memory holds the values with the other sign."""
+    x, w = torch._neg_view(torch.ones(4, 64, device="cuda")), torch.ones(64, device="cuda")
+    for call in (lambda: A.pack8(x), lambda: A.rms_norm8(x, w), lambda: A.rms_norm8(x.resolve_neg(), w, residual=x), lambda: A.rms_norm8(w.reshape(1, -1), torch._neg_view(w)),
+                 lambda: A.rms_norm8_backward(x, A.pack8(x.resolve_neg()), torch.ones(4, device="cuda"), w)):
+        with pytest.raises(ValueError):
+            call()
+    assert torch.equal(A.pack8(x.resolve_neg()).unpack(F32), -torch.ones(4, 64, device="cuda"))
