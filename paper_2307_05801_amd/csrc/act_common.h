@@ -238,6 +238,18 @@ inline int launched()
     return e == hipSuccess ? LEAP_OK : leap_hip_fail(e, "kernel launch");
 }
 
+// launch(first, blocks) over `all` blocks in as many launches as it takes: one has fewer than 2^32 threads (2^30 rows of 8 channels are 2^33).
+constexpr int64_t MOST_BLOCKS = (int64_t)1 << 21;
+template <class F> inline int over_blocks(int64_t all, F &&launch)
+{
+    for (int64_t first = 0; first < all; first += MOST_BLOCKS) {
+        launch(first, (unsigned)(all - first < MOST_BLOCKS ? all - first : MOST_BLOCKS));
+        const int rc = launched();
+        if (rc != LEAP_OK) return rc;
+    }
+    return LEAP_OK;
+}
+
 inline int refuse(const char *why)
 {
     try {

@@ -26,9 +26,9 @@ struct copies {
     copied_rows of[3];
 };
 
-__global__ __launch_bounds__(BLOCK) void k_lay_out(copies C)
+__global__ __launch_bounds__(BLOCK) void k_lay_out(copies C, uint32_t first_block)
 {
-    uint32_t block = blockIdx.x;
+    uint32_t block = first_block + blockIdx.x;
     int c = 0;
     while (c < 2 && block >= C.of[c].blocks) block -= C.of[c++].blocks;
     const copied_rows &A = C.of[c];
@@ -82,14 +82,12 @@ int lay_out(uint8_t *&room, hipStream_t st, laid *a, laid *b = nullptr, laid *c 
         if (!x || !x->copied) continue;
         const int64_t mine = cut(x->rows_to * (x->pitch / 16), BLOCK);
         blocks += mine;
-        if (blocks > 0x7fffffff) return refuse("more values to lay out than one launch covers");
+        if (blocks > 0x7fffffff) return refuse("more values to lay out than 31 bits count blocks for");
         C.of[n++] = {x->data, room, x->stride, x->rows, x->rows_to, x->bytes, x->pitch, divider((uint32_t)(x->pitch / 16)), (uint32_t)mine};
         x->data = room, x->stride = x->pitch, x->copied = false;
         room += x->rows_to * x->pitch;
     }
-    if (!n) return LEAP_OK;
-    hipLaunchKernelGGL(k_lay_out, dim3((unsigned)blocks), dim3(BLOCK), 0, st, C);
-    return launched();
+    return over_blocks(blocks, [&](int64_t first, unsigned some) { hipLaunchKernelGGL(k_lay_out, dim3(some), dim3(BLOCK), 0, st, C, (uint32_t)first); });
 }
 
 // ---- launches ----
@@ -160,12 +158,13 @@ struct weight_plan {
 // to <- the sum of the parts, n values every `apart`, in a fixed order: 16 threads to four values each, which add every 16th part, 64 values a block.
 constexpr int ADDED = 64;
 
-template <int TYPE> __global__ __launch_bounds__(BLOCK) void k_add_parts(const float *__restrict__ from, int64_t parts, int64_t apart, int64_t n, void *__restrict__ to)
+template <int TYPE> __global__ __launch_bounds__(BLOCK) void k_add_parts(const float *__restrict__ from, int64_t parts, int64_t apart, int64_t n, void *__restrict__ to,
+                                                                             int64_t first_block)
 {
     constexpr int WAYS = BLOCK / (ADDED / 4);
     __shared__ float room[WAYS][ADDED];
     const int way = threadIdx.x / (ADDED / 4), in = threadIdx.x % (ADDED / 4) * 4;
-    const int64_t at = (int64_t)blockIdx.x * ADDED + in;
+    const int64_t begin = (first_block + blockIdx.x) * ADDED, at = begin + in;
     const int left = n - at < 4 ? (int)(n - at) : 4;
     float sum[4] = {};
     if (left == 4) {
@@ -183,12 +182,20 @@ template <int TYPE> __global__ __launch_bounds__(BLOCK) void k_add_parts(const f
 #pragma unroll
     for (int x = 0; x < 4; ++x) room[way][in + x] = sum[x];
     __syncthreads();
-    if (threadIdx.x < ADDED && (int64_t)blockIdx.x * ADDED + threadIdx.x < n) {
+    if (threadIdx.x < ADDED && begin + threadIdx.x < n) {
         float total = 0.0f;
 #pragma unroll
         for (int w = 0; w < WAYS; ++w) total += room[w][threadIdx.x];
-        ((typename element<TYPE>::raw *)to)[(int64_t)blockIdx.x * ADDED + threadIdx.x] = element<TYPE>::from_float(total);
+        ((typename element<TYPE>::raw *)to)[begin + threadIdx.x] = element<TYPE>::from_float(total);
     }
+}
+
+int add_parts(const float *from, int64_t parts, int64_t apart, int64_t n, void *to, int32_t type, hipStream_t st)
+{
+    return over_blocks(cut(n, ADDED), [&](int64_t first, unsigned blocks) {
+        if (type == LEAP_F32) hipLaunchKernelGGL((k_add_parts<LEAP_F32>), dim3(blocks), dim3(BLOCK), 0, st, from, parts, apart, n, to, first);
+        else hipLaunchKernelGGL((k_add_parts<LEAP_BF16>), dim3(blocks), dim3(BLOCK), 0, st, from, parts, apart, n, to, first);
+    });
 }
 
 // y and grad_x of few rows and columns, with many values of k to sum over: the same, in parts of k, 256 at least.  128 values of k take a
@@ -215,10 +222,7 @@ template <int PKIND, int QKIND> int product_in_parts(const operand &P, const ope
     R.out = room, R.stride = P.rows, R.part = P.rows * Q.rows;
     const int rc = launch<PKIND, QKIND, TO_FULL, 128, 64, 2, 2, 2, 3>(P, Q, R, plan.depth_part, st);
     if (rc != LEAP_OK) return rc;
-    const dim3 adders((unsigned)cut(R.part, ADDED));
-    if (type == LEAP_F32) hipLaunchKernelGGL((k_add_parts<LEAP_F32>), adders, dim3(BLOCK), 0, st, (const float *)room, plan.parts, R.part, R.part, out);
-    else hipLaunchKernelGGL((k_add_parts<LEAP_BF16>), adders, dim3(BLOCK), 0, st, (const float *)room, plan.parts, R.part, R.part, out);
-    return launched();
+    return add_parts((const float *)room, plan.parts, R.part, R.part, out, type, st);
 }
 
 // ---- the gate by itself ----
@@ -235,9 +239,9 @@ __device__ inline void pad_row(uint16_t *row, int64_t values, const du_layout &L
 // du <- da and what is kept, and zeros between its rows; one chunk of `out` a lane
 __global__ __launch_bounds__(BLOCK) void k_gate_grad(const void *__restrict__ da, int64_t stride, const uint8_t *__restrict__ kept_codes,
                                                      const uint8_t *__restrict__ kept_scales, int64_t rows, int64_t out, void *__restrict__ du,
-                                                     du_layout L)
+                                                     du_layout L, int64_t first_block)
 {
-    const int64_t groups = groups_of(out), per_row = groups * (GROUP / CHUNK), c = (int64_t)blockIdx.x * BLOCK + threadIdx.x;
+    const int64_t groups = groups_of(out), per_row = groups * (GROUP / CHUNK), c = (first_block + blockIdx.x) * BLOCK + threadIdx.x;
     const int64_t row = c / per_row, col = (c - row * per_row) * CHUNK;
     const int n = row < rows ? (out - col < CHUNK ? (int)(out - col) : CHUNK) : 0;
     if (n <= 0) return;
@@ -264,9 +268,9 @@ __global__ __launch_bounds__(BLOCK) void k_gate_grad(const void *__restrict__ da
 }
 
 // The same zeros by themselves, a row a thread.
-__global__ __launch_bounds__(BLOCK) void k_pad_rows(uint16_t *__restrict__ du, int64_t rows, int64_t values, du_layout L)
+__global__ __launch_bounds__(BLOCK) void k_pad_rows(uint16_t *__restrict__ du, int64_t rows, int64_t values, du_layout L, int64_t first_block)
 {
-    const int64_t row = (int64_t)blockIdx.x * BLOCK + threadIdx.x;
+    const int64_t row = (first_block + blockIdx.x) * BLOCK + threadIdx.x;
     if (row < rows) pad_row(du + row * L.stride, values, L);
 }
 
@@ -346,13 +350,7 @@ int backward(laid G, int64_t low, const uint8_t *d_codes, const uint8_t *d_scale
             rc = grad_x_type == LEAP_F32 ? product<WIDE_ACROSS, WIDE_ALONG, TO_FULL>(P, Q, R, st) : product<WIDE_ACROSS, WIDE_ALONG, TO_WIDE>(P, Q, R, st);
     }
     if (rc != LEAP_OK || !d_grad_weight) return rc;
-    const int64_t added = cut(cols * out, ADDED);
-    if (added > 0x7fffffff) return refuse("a weight of more than 2^37 values");
-    const dim3 adders((unsigned)added);
-    if (!rows) {                                     // a sum of nothing
-        hipLaunchKernelGGL((k_add_parts<LEAP_BF16>), adders, dim3(BLOCK), 0, st, (const float *)nullptr, (int64_t)0, (int64_t)0, cols * out, d_grad_weight);
-        return launched();
-    }
+    if (!rows) return add_parts(nullptr, 0, 0, cols * out, d_grad_weight, LEAP_BF16, st);        // a sum of nothing
     const weight_plan plan(rows, cols, deep);
     const operand P = X.codes(d_scales, cols, cols, rows), Q = G.wide(deep, rows);
     result R{};
@@ -364,9 +362,7 @@ int backward(laid G, int64_t low, const uint8_t *d_codes, const uint8_t *d_scale
     R.out = room;
     rc = product<CODES_ACROSS, WIDE_ACROSS, TO_FULL>(P, Q, R, plan.depth_part, plan.large, st);
     if (rc != LEAP_OK) return rc;
-    hipLaunchKernelGGL((k_add_parts<LEAP_BF16>), adders, dim3(BLOCK), 0, st, (const float *)room, low ? 2 * plan.parts : plan.parts, low ? low * cols : R.part, cols * out,
-                       d_grad_weight);
-    return launched();
+    return add_parts((const float *)room, low ? 2 * plan.parts : plan.parts, low ? low * cols : R.part, cols * out, d_grad_weight, LEAP_BF16, st);
 }
 
 // du's rows end at a multiple of 16 bytes: they are never copied.
@@ -434,11 +430,9 @@ int gate_backward(const void *d_da, int64_t da_stride, const uint8_t *d_kept_cod
     if (const char *why = bad_stride(da_stride, rows, out)) return refuse(why);
     if (!rows) return LEAP_OK;
     if (!d_da || !d_kept_codes || !d_kept_scales || !d_du) return refuse("null data pointer");
-    const int64_t blocks = cut(rows * groups_of(out) * (GROUP / CHUNK), BLOCK);
-    if (blocks > 0x7fffffff) return refuse("more values than one launch covers");
-    hipLaunchKernelGGL(k_gate_grad, dim3((unsigned)blocks), dim3(BLOCK), 0, stream_of(hip_stream), d_da, da_stride, d_kept_codes, d_kept_scales, rows, out, d_du,
-                       L);
-    return launched();
+    return over_blocks(cut(rows * groups_of(out) * (GROUP / CHUNK), BLOCK), [&](int64_t first, unsigned blocks) {
+        hipLaunchKernelGGL(k_gate_grad, dim3(blocks), dim3(BLOCK), 0, stream_of(hip_stream), d_da, da_stride, d_kept_codes, d_kept_scales, rows, out, d_du, L, first);
+    });
 }
 
 }  // namespace
@@ -526,14 +520,24 @@ int act::linear_gate8_backward(const void *d_dy, int64_t dy_stride, const void *
     const hipStream_t st = stream_of(hip_stream);
     uint8_t *room = (uint8_t *)d_work;
     laid W(d_weight, w_stride, next, out, 2), G(d_dy, dy_stride, rows, next, 2);
-    const int rc = lay_out(room, st, &W, &G);
-    if (rc != LEAP_OK) return rc;
-    if (2 * out % 8 != 0 && L.stride > 2 * out)
-        hipLaunchKernelGGL(k_pad_rows, dim3((unsigned)cut(rows, BLOCK)), dim3(BLOCK), 0, st, (uint16_t *)d_du, rows, 2 * out, L);
-    result R{};
-    R.out = d_du, R.stride = L.stride, R.low = L.low, R.columns = out, R.kept_codes = (uint8_t *)d_kept_codes, R.kept_scales = (uint8_t *)d_kept_scales;
-    if (L.low) return product<WIDE_ACROSS, WIDE_ALONG, TO_GATE_GRAD_FINE>(W.wide(out, next), G.wide(rows, next), R, st);
-    return product<WIDE_ACROSS, WIDE_ALONG, TO_GATE_GRAD>(W.wide(out, next), G.wide(rows, next), R, st);
+    int rc = lay_out(room, st, &W, &G);
+    if (rc == LEAP_OK && 2 * out % 8 != 0 && L.stride > 2 * out)
+        rc = over_blocks(cut(rows, BLOCK), [&](int64_t first, unsigned blocks) {
+            hipLaunchKernelGGL(k_pad_rows, dim3(blocks), dim3(BLOCK), 0, st, (uint16_t *)d_du, rows, 2 * out, L, first);
+        });
+    // a block a tile here: as many rows at once as a launch has blocks for
+    const int64_t at_once = MOST_BLOCKS / cut(out, 128) * 128;
+    for (int64_t row0 = 0; rc == LEAP_OK && row0 < rows; row0 += at_once) {
+        const int64_t n = rows - row0 < at_once ? rows - row0 : at_once;
+        operand Q = G.wide(n, next);
+        Q.data += row0 * G.stride;
+        result R{};
+        R.out = (uint8_t *)d_du + L.bytes(row0), R.stride = L.stride, R.low = L.low, R.columns = out;
+        R.kept_codes = (uint8_t *)d_kept_codes + row0 * 2 * out, R.kept_scales = (uint8_t *)d_kept_scales + row0 * 2 * groups_of(out);
+        rc = L.low ? product<WIDE_ACROSS, WIDE_ALONG, TO_GATE_GRAD_FINE>(W.wide(out, next), Q, R, st)
+                   : product<WIDE_ACROSS, WIDE_ALONG, TO_GATE_GRAD>(W.wide(out, next), Q, R, st);
+    }
+    return rc;
 }
 
 extern "C" int leap_linear_gate8_backward(const void *d_dy, int64_t dy_stride, const void *d_weight, int64_t w_stride, int64_t next,

@@ -42,6 +42,7 @@ struct norm_args {
     uint8_t *normed_codes, *normed_scales, *kept_codes, *kept_scales;
     float *rstd;
     bool past;                   // outputs past the caches
+    int64_t first;               // block of this launch
 };
 
 // s of one chunk: x + residual, as the type holds it
@@ -73,7 +74,7 @@ template <int TYPE, int WTYPE, bool ADD, int LANES, int CHUNKS>
 __global__ __launch_bounds__(BLOCK) void k_norm(norm_args A)
 {
     const int lane = threadIdx.x % LANES;
-    const int64_t row = (int64_t)blockIdx.x * (BLOCK / LANES) + threadIdx.x / LANES;
+    const int64_t row = (A.first + blockIdx.x) * (BLOCK / LANES) + threadIdx.x / LANES;
     const bool there = row < A.rows;
     float s[CHUNKS][CHUNK], square = 0.0f;
     int n[CHUNKS];
@@ -95,7 +96,7 @@ __global__ __launch_bounds__(BLOCK) void k_norm(norm_args A)
 template <int TYPE, int WTYPE, bool ADD> __global__ __launch_bounds__(BLOCK) void k_norm_long(norm_args A)
 {
     __shared__ float room[BLOCK / WAVE];
-    const int64_t row = blockIdx.x, most = A.groups * GROUP;
+    const int64_t row = A.first + blockIdx.x, most = A.groups * GROUP;
     float square = 0.0f, s[CHUNK];
     for (int64_t col = threadIdx.x * CHUNK; col < A.cols; col += BLOCK * CHUNK) {
         sum_chunk<TYPE, ADD>(A, row, col, (int)(A.cols - col < CHUNK ? A.cols - col : CHUNK), s);
@@ -121,6 +122,7 @@ struct grad_args {
     void *grad_x;
     float *part;                 // [blocks][cols]: each block's sum of grad h, or null
     bool past;
+    int64_t first;               // block of this launch, of those that take a row each
 };
 
 // How many of a chunk's values a row has, from what is left of it.
@@ -222,7 +224,7 @@ __global__ __launch_bounds__(BLOCK) void k_norm_grad(grad_args A)
 template <int TYPE, int GTYPE, int WTYPE> __global__ __launch_bounds__(BLOCK) void k_norm_grad_long(grad_args A)
 {
     __shared__ float room[BLOCK / WAVE];
-    const int64_t row = blockIdx.x;
+    const int64_t row = A.first + blockIdx.x;
     const float rstd = A.rstd[row];
     float d[CHUNK], h[CHUNK], w[CHUNK], dot = 0.0f;
     for (int64_t col = threadIdx.x * CHUNK; col < A.cols; col += BLOCK * CHUNK) {
@@ -339,22 +341,24 @@ extern "C" int leap_rms_norm8(const void *d_x, int64_t x_stride, const void *d_r
     if (!d_x || !d_weight || !d_normed_codes || !d_normed_scales) return refuse("null data pointer");
     if (!d_kept_codes != !d_kept_scales) return refuse("kept codes and scales: both or neither");
     if (rows > 0x7fffffff) return refuse("more than 2^31 rows");
-    const norm_args A{d_x, d_residual, d_weight, x_stride, residual_stride, rows, cols, groups_of(cols), eps, 1.0f / (float)cols,
-                      d_sum, d_normed_codes, d_normed_scales, d_kept_codes, d_kept_scales, d_rstd, rows * cols * 2 > PAST_CACHES};
+    norm_args A{d_x, d_residual, d_weight, x_stride, residual_stride, rows, cols, groups_of(cols), eps, 1.0f / (float)cols,
+                      d_sum, d_normed_codes, d_normed_scales, d_kept_codes, d_kept_scales, d_rstd, rows * cols * 2 > PAST_CACHES, 0};
     return by_weight(type, weight_type, [&](auto t, auto w) {
         constexpr int T = decltype(t)::value, W = decltype(w)::value;
         const hipStream_t st = stream_of(hip_stream);
-        if (cols > LONG) {
-            if (d_residual) hipLaunchKernelGGL((k_norm_long<T, W, true>), dim3((unsigned)rows), dim3(BLOCK), 0, st, A);
-            else hipLaunchKernelGGL((k_norm_long<T, W, false>), dim3((unsigned)rows), dim3(BLOCK), 0, st, A);
-            return launched();
-        }
+        if (cols > LONG)
+            return over_blocks(rows, [&](int64_t first, unsigned blocks) {
+                A.first = first;
+                if (d_residual) hipLaunchKernelGGL((k_norm_long<T, W, true>), dim3(blocks), dim3(BLOCK), 0, st, A);
+                else hipLaunchKernelGGL((k_norm_long<T, W, false>), dim3(blocks), dim3(BLOCK), 0, st, A);
+            });
         return by_length(cols, [&](auto l, auto c) {
             constexpr int L = decltype(l)::value, C = decltype(c)::value;
-            const unsigned blocks = (unsigned)((rows + BLOCK / L - 1) / (BLOCK / L));
-            if (d_residual) hipLaunchKernelGGL((k_norm<T, W, true, L, C>), dim3(blocks), dim3(BLOCK), 0, st, A);
-            else hipLaunchKernelGGL((k_norm<T, W, false, L, C>), dim3(blocks), dim3(BLOCK), 0, st, A);
-            return launched();
+            return over_blocks((rows + BLOCK / L - 1) / (BLOCK / L), [&](int64_t first, unsigned blocks) {
+                A.first = first;
+                if (d_residual) hipLaunchKernelGGL((k_norm<T, W, true, L, C>), dim3(blocks), dim3(BLOCK), 0, st, A);
+                else hipLaunchKernelGGL((k_norm<T, W, false, L, C>), dim3(blocks), dim3(BLOCK), 0, st, A);
+            });
         });
     });
 }
@@ -377,8 +381,8 @@ extern "C" int leap_rms_norm8_backward(const void *d_grad, int32_t grad_type, in
     if (rows > 0x7fffffff) return refuse("more than 2^31 rows");
     if (rows && (!d_grad || !d_kept_codes || !d_kept_scales || !d_rstd || !d_weight || !d_grad_x)) return refuse("null data pointer");
     if (d_grad_weight && !d_work) return refuse("the weight's gradient needs the workspace");
-    const grad_args A{d_grad, d_grad_sum, d_weight, grad_stride, grad_sum_stride, rows, cols, groups_of(cols), 1.0f / (float)cols,
-                      d_kept_codes, d_kept_scales, d_rstd, d_grad_x, d_grad_weight ? d_work : nullptr, rows * cols * 2 > PAST_CACHES};
+    grad_args A{d_grad, d_grad_sum, d_weight, grad_stride, grad_sum_stride, rows, cols, groups_of(cols), 1.0f / (float)cols,
+                      d_kept_codes, d_kept_scales, d_rstd, d_grad_x, d_grad_weight ? d_work : nullptr, rows * cols * 2 > PAST_CACHES, 0};
     const hipStream_t st = stream_of(hip_stream);
     const int64_t parts = rows ? grad_blocks(rows, cols) : 0;
     int rc = LEAP_OK;
@@ -388,7 +392,11 @@ extern "C" int leap_rms_norm8_backward(const void *d_grad, int32_t grad_type, in
             const auto run = [&](auto g) {
                 constexpr int G = decltype(g)::value;
                 if (cols > LONG) {
-                    hipLaunchKernelGGL((k_norm_grad_long<T, G, W>), dim3((unsigned)rows), dim3(BLOCK), 0, st, A);
+                    const int status = over_blocks(rows, [&](int64_t first, unsigned blocks) {
+                        A.first = first;
+                        hipLaunchKernelGGL((k_norm_grad_long<T, G, W>), dim3(blocks), dim3(BLOCK), 0, st, A);
+                    });
+                    if (status != LEAP_OK) return status;
                     if (A.part) {
                         const unsigned across = (unsigned)((cols + BLOCK * CHUNK - 1) / (BLOCK * CHUNK));
                         hipLaunchKernelGGL((k_norm_grad_weight_long<G>), dim3(across, (unsigned)parts), dim3(BLOCK), 0, st, A);

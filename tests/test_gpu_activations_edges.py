@@ -92,3 +92,75 @@ def test_negated_views_are_refused(A):  # noqa: F811
         with pytest.raises(ValueError):
             call()
     assert torch.equal(A.pack8(x.resolve_neg()).unpack(F32), -torch.ones(4, 64, device="cuda"))
+
+
+# ---- more blocks than one launch takes: what lies at the border between two launches, and at the end ----
+
+CHANNELS = [(0, 40), ((1 << 26) - 40, (1 << 26) + 40), ((1 << 27) - 40, (1 << 27) + 40)]
+
+
+def _channels(rows, cols, seed):
+    return torch.randn(rows, cols, device="cuda", generator=torch.Generator(device="cuda").manual_seed(seed), dtype=torch.float32).to(BF16)
+
+
+def test_norm_of_many_short_rows(A):  # noqa: F811
+    rows, cols = (1 << 27) + 77, 3
+    x, w = _channels(rows, cols, 307), torch.tensor([1.0, 0.5, 2.0], device="cuda")
+    _, normed, kept, rstd = A.rms_norm8(x, w)
+    for begin, end in CHANNELS + [(rows - 50, rows)]:
+        _, inverse, v = R.rms_norm(x[begin:end].cpu(), w.cpu(), None, 1e-6, BF16)
+        part = A.Packed8(normed.codes[begin:end].contiguous(), normed.scales[begin:end].contiguous())
+        R.assert_close(rstd[begin:end], inverse, inverse * R.sum_error(cols), "rstd")
+        R.assert_held(part, v, v.abs() * R.sum_error(cols), "normed")
+        assert torch.equal(kept.scales[begin:end].cpu(), R.pack(x[begin:end].cpu())[1])
+
+
+def test_norm_of_many_long_rows(A):  # noqa: F811
+    """2^21 rows of 2049: a block each, both ways."""
+    rows, cols = (1 << 21) + 5, 2049
+    x = torch.empty(rows, cols, dtype=BF16, device="cuda").normal_(generator=torch.Generator(device="cuda").manual_seed(308))
+    w = torch.ones(cols, device="cuda")
+    _, normed, kept, rstd = A.rms_norm8(x, w)
+    dx, dw = A.rms_norm8_backward(x, kept, rstd, w)
+    for begin, end in [(0, 2), ((1 << 21) - 2, (1 << 21) + 2), (rows - 2, rows)]:
+        some = x[begin:end].cpu()
+        _, inverse, v = R.rms_norm(some, w.cpu(), None, 1e-6, BF16)
+        R.assert_close(rstd[begin:end], inverse, inverse * R.sum_error(cols), "rstd")
+        R.assert_held(A.Packed8(normed.codes[begin:end].contiguous(), normed.scales[begin:end].contiguous()), v, v.abs() * R.sum_error(cols), "normed")
+        held = R.held(A.Packed8(kept.codes[begin:end].contiguous(), kept.scales[begin:end].contiguous()))
+        want, size, _, _ = R.rms_norm_backward(some, held, rstd[begin:end].cpu(), w.cpu(), None)
+        R.assert_close(dx[begin:end], want, want.abs() * R.half_step(BF16) + size * R.sum_error(cols), "grad_x")
+
+
+def test_gate_gradient_of_many_short_rows(A):  # noqa: F811
+    """du of one gated column; the same through a product of one column."""
+    rows = (1 << 28) + 77
+    da = _channels(rows, 1, 309)
+    kept = A.Packed8(torch.full((rows, 2, 1), 56, dtype=torch.uint8, device="cuda").view(torch.float8_e4m3fn),        # code 56: 1.0
+                     torch.full((rows, 2, 1), 127, dtype=torch.uint8, device="cuda"))
+    kept.codes.view(torch.uint8)[1::3, 0] = 64                                                                       # 2.0
+    one = torch.ones(1, 1, dtype=BF16, device="cuda")
+    for du in (lambda: A.gate8_backward(da, kept), lambda: A.linear_gate8_backward(da, one, kept)):
+        got = du()
+        for begin, end in CHANNELS + [((1 << 28) - 40, (1 << 28) + 40), (rows - 50, rows)]:
+            want, size = R.gate_backward(da[begin:end].cpu(), R.values(kept.codes[begin:end].view(torch.uint8).cpu(), kept.scales[begin:end].cpu()))
+            R.assert_close(got[begin:end], want, want.abs() * R.half_step(BF16) + 2.0 ** -18 * size, "du")
+        del got
+
+
+def test_rows_laid_out_by_several_launches(A):  # noqa: F811
+    """Codes of one column, in rows of 16 bytes: 2^29 of them are one launch's."""
+    rows = (1 << 29) + 300
+    x = A.Packed8(torch.full((rows, 1), 56, dtype=torch.uint8, device="cuda").view(torch.float8_e4m3fn), torch.full((rows, 1), 127, dtype=torch.uint8, device="cuda"))
+    x.scales[1::2] = 128
+    y = A.linear8(x, torch.full((1, 1), 3.0, dtype=BF16, device="cuda"))
+    assert bool((y[0::2] == 3.0).all()) and bool((y[1::2] == 6.0).all())
+
+
+def test_weight_gradient_of_no_rows_and_2_27_values(A):  # noqa: F811
+    out, cols = (1 << 14) + 1, 1 << 13
+    w = torch.ones(out, cols, dtype=BF16, device="cuda")
+    del_me = torch.ones(out, cols, dtype=BF16, device="cuda")
+    del del_me                                               # the gradient's memory holds ones
+    x = A.Packed8(torch.empty(0, cols, dtype=torch.float8_e4m3fn, device="cuda"), torch.empty(0, cols // 32, dtype=torch.uint8, device="cuda"))
+    assert not A.linear8_backward(torch.empty(0, out, dtype=BF16, device="cuda"), x, w)[1].any()
