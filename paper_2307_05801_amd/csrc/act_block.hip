@@ -90,9 +90,9 @@ extern "C" int leap_feed_forward8(const void *d_x, int64_t x_stride, const void 
     const block_sizes S{rows, cols, hidden, out, d_up, d_down, up_stride, down_stride};
     if (const char *why = S.bad()) return refuse(why);
     if (!rows) return LEAP_OK;
-    if (!d_kept || (uintptr_t)d_kept % 16 != 0) return refuse("what is kept needs memory from a multiple of 16 bytes on");
+    if (unaligned(d_kept)) return refuse("what is kept needs memory from a multiple of 16 bytes on");
     if (!d_up || !d_down || !d_y) return refuse("null data pointer");
-    if (!d_work && S.work(d_kept)) return refuse("null workspace");
+    if (unaligned(d_work) && S.work(d_kept)) return refuse(NO_WORK);
     if (norm_weight_type != LEAP_F32 && norm_weight_type != LEAP_BF16) return refuse("the norm's weight must be float32 or bfloat16");
     const kept_block K(d_kept, rows, cols, hidden);
     int rc = leap_rms_norm8(d_x, x_stride, d_residual, residual_stride, LEAP_BF16, d_norm_weight, norm_weight_type, rows, cols, eps, d_sum, K.normed,
@@ -117,13 +117,13 @@ int block_backward(bool fine, const void *d_dy, int64_t dy_stride, const void *d
     if (const char *why = S.bad()) return refuse(why);
     const int64_t rows = S.rows, cols = S.cols, hidden = S.hidden, out = S.out;
     if (const char *why = bad_stride(dy_stride, rows, out)) return refuse(why);
-    if (rows && (!d_kept || (uintptr_t)d_kept % 16 != 0)) return refuse("what is kept needs memory from a multiple of 16 bytes on");
+    if (rows && unaligned(d_kept)) return refuse("what is kept needs memory from a multiple of 16 bytes on");
     if (rows && (!d_dy || !S.up || !S.down)) return refuse("null data pointer");
     if (const char *why = d_grad_sum ? bad_stride(grad_sum_stride, rows, cols) : nullptr) return refuse(why);
     if (norm_weight_type != LEAP_F32 && norm_weight_type != LEAP_BF16) return refuse("the norm's weight must be float32 or bfloat16");
     if (rows && (d_grad_x || d_grad_norm_weight) && !d_norm_weight) return refuse("null data pointer");
     if (rows && d_grad_norm_weight && !d_grad_x) return refuse("the norm's weight gradient comes with grad_x");
-    if (!d_work || (uintptr_t)d_work % 16 != 0) return refuse("the workspace needs memory from a multiple of 16 bytes on");
+    if (unaligned(d_work)) return refuse(NO_WORK);
     const kept_block K((void *)d_kept, rows, cols, hidden);
     // du is bfloat16, which the matrix units take: grad_up is 0.0024 of its norm off, grad_norm_weight 0.0024 to 0.0034, where 0.0017 are their own
     // rounding to bfloat16.  A caller who wants that alone asks for a fine du, whose products take twice as long (262144 x 512 through 1024, forward and

@@ -277,6 +277,10 @@ inline const char *bad_stride(int64_t stride, int64_t rows, int64_t cols)
     return nullptr;
 }
 
+// A workspace is memory from a multiple of 16 bytes on.
+inline bool unaligned(const void *p) { return !p || (uintptr_t)p % 16 != 0; }
+constexpr const char *NO_WORK = "the workspace needs memory from a multiple of 16 bytes on";
+
 // f(the type as a constant) for a type known at run time.
 template <class F> inline int by_type(int32_t type, F &&f)
 {

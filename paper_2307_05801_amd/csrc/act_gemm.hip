@@ -297,7 +297,7 @@ extern "C" int leap_linear8(const uint8_t *d_codes, const uint8_t *d_scales, int
     if (const char *why = bad_product(rows, cols, w_stride, out)) return refuse(why);
     if (!rows) return LEAP_OK;
     if (!d_codes || !d_scales || !d_weight || !d_y) return refuse("null data pointer");
-    if (!d_work && leap_linear8_work(d_codes, rows, cols, d_weight, w_stride, out)) return refuse("null workspace");
+    if (unaligned(d_work) && leap_linear8_work(d_codes, rows, cols, d_weight, w_stride, out)) return refuse(NO_WORK);
     const hipStream_t st = stream_of(hip_stream);
     uint8_t *room = (uint8_t *)d_work;
     laid W(d_weight, w_stride, out, cols, 2), X(d_codes, cols, rows, cols, 1);
@@ -330,7 +330,7 @@ int backward(laid G, int64_t low, const uint8_t *d_codes, const uint8_t *d_scale
 {
     if (grad_x_type != LEAP_BF16 && grad_x_type != LEAP_F32) return refuse("grad_x is bfloat16 or float32");
     if (rows && (!G.data || !d_codes || !d_scales || !d_weight)) return refuse("null data pointer");
-    if (!d_work && backward_work(G, low, d_codes, rows, cols, d_weight, w_stride, out)) return refuse("null workspace");
+    if (unaligned(d_work) && backward_work(G, low, d_codes, rows, cols, d_weight, w_stride, out)) return refuse(NO_WORK);
     const hipStream_t st = stream_of(hip_stream);
     uint8_t *room = (uint8_t *)d_work;
     const int64_t deep = low + out;
@@ -409,7 +409,7 @@ extern "C" int leap_gated_linear8(const uint8_t *d_codes, const uint8_t *d_scale
     if (!rows) return LEAP_OK;
     if (!d_codes || !d_scales || !d_weight || !d_gated_codes || !d_gated_scales) return refuse("null data pointer");
     if (!d_kept_codes != !d_kept_scales) return refuse("kept codes and scales: both or neither");
-    if (!d_work && leap_linear8_work(d_codes, rows, cols, d_weight, w_stride, 2 * out)) return refuse("null workspace");
+    if (unaligned(d_work) && leap_linear8_work(d_codes, rows, cols, d_weight, w_stride, 2 * out)) return refuse(NO_WORK);
     const hipStream_t st = stream_of(hip_stream);
     uint8_t *room = (uint8_t *)d_work;
     laid W(d_weight, w_stride, 2 * out, cols, 2), X(d_codes, cols, rows, cols, 1);
@@ -461,7 +461,7 @@ int gated_backward(bool fine, const void *d_da, int64_t da_stride, const uint8_t
     if (const char *why = bad_stride(da_stride, rows, out)) return refuse(why);
     if (grad_x_type != LEAP_BF16 && grad_x_type != LEAP_F32) return refuse("grad_x is bfloat16 or float32");
     if (rows && (!d_codes || !d_scales || !d_weight)) return refuse("null data pointer");
-    if (rows && (!d_work || (uintptr_t)d_work % 16 != 0)) return refuse("the workspace needs memory from a multiple of 16 bytes on");
+    if (rows && unaligned(d_work)) return refuse(NO_WORK);
     if (!d_grad_x && !d_grad_weight) return LEAP_OK;
     // du is bfloat16, which the matrix units take: the results are 0.0024 of their norm off, of which their own rounding to bfloat16 is 0.0017.
     // A caller who wants that alone asks for a fine du, whose products take twice as long (262144 x 512 -> 2 * 1024 forward and backward: 3.47 ms, 2.25).
@@ -516,7 +516,7 @@ int act::linear_gate8_backward(const void *d_dy, int64_t dy_stride, const void *
     if (const char *why = bad_stride(dy_stride, rows, next)) return refuse(why);
     if (!rows) return LEAP_OK;
     if (!d_dy || !d_weight || !d_kept_codes || !d_kept_scales || !d_du) return refuse("null data pointer");
-    if (!d_work && leap_linear_gate8_work(d_dy, dy_stride, d_weight, w_stride, next, rows, out)) return refuse("null workspace");
+    if (unaligned(d_work) && leap_linear_gate8_work(d_dy, dy_stride, d_weight, w_stride, next, rows, out)) return refuse(NO_WORK);
     const hipStream_t st = stream_of(hip_stream);
     uint8_t *room = (uint8_t *)d_work;
     laid W(d_weight, w_stride, next, out, 2), G(d_dy, dy_stride, rows, next, 2);

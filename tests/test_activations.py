@@ -313,3 +313,14 @@ def test_rows_of_negated_views_are_refused(make):
     from paper_2307_05801_amd.activations import _rows
     with pytest.raises(ValueError, match="negated"):
         _rows(make(), "x")
+
+
+def test_workspaces_that_are_not_aligned_are_refused(lib):
+    """Where one is needed; the copies in it would not be laid out for the kernels."""
+    for name, arguments in (("leap_linear8", (P, P, 5, 40, P, 40, 8, P)), ("leap_linear8", (P, P, 5, 1024, P, 1024, 8, P)),
+                            ("leap_linear8_backward", (P, 9, P, P, 5, 64, P, 64, 9, P, 1, P)), ("leap_gated_linear8", (P, P, 5, 40, P, 40, 8, P, P, P, P)),
+                            ("leap_linear_gate8_backward", (P, 9, P, 16, 9, P, P, 4, 16, P)),
+                            ("leap_feed_forward8", (P, 64, None, 0, P, 1, 4, 64, 1e-6, P, 65, 8, P, 8, 16, P, P, P))):
+        for work in (P + 8, P + 1, None):
+            assert getattr(lib, name)(*arguments, work, None) == B.LEAP_INVALID_ARG, (name, work)
+            assert lib.leap_last_error()
