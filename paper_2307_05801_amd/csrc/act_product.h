@@ -61,11 +61,15 @@ struct window {
 __device__ inline int64_t whole(int64_t n, int piece) { return (n + piece - 1) / piece * piece; }
 
 // Starts a fetch of 16 bytes a lane, from `offset` of the buffer to 16 * lane beyond `to`.  In assembly, because the compiler would
-// wait for the fetch before the next read of any shared memory; it has no result but shared memory, and arrive() waits for it.  (m0
-// is reserved: nothing the compiler makes of these kernels uses it.)
+// wait for the fetch before the next read of any shared memory; it has no result but shared memory, and every step begins by waiting for it.  m0, through
+// which the address goes, cannot be declared as overwritten: it gets back what it held.
 __device__ inline void fetch16(const u32x4 &from, uint32_t offset, lds_byte *to)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(__builtin_amdgcn_readfirstlane((int)(uintptr_t)to)), "v"(offset), "s"(from) : "memory");
+    uint32_t m0;
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %3, 0 offen lds\n\ts_mov_b32 m0, %0"
+                 : "=&s"(m0)
+                 : "s"(__builtin_amdgcn_readfirstlane((int)(uintptr_t)to)), "v"(offset), "s"(from)
+                 : "memory");
 }
 
 // A tile of T rows and STEP values of k of an operand in shared memory, by KIND.  ALONG: T rows of 2 * STEP (codes: STEP)
