@@ -9,7 +9,8 @@ neighbours share a power of two: 1 + 1/32 bytes a value (include/leap_activation
     y, x = feed_forward8(y, norm_weight, up, down, residual=x)         # a block that keeps 8 bits only; differentiable
     block = FeedForward8(512, 1024); y, x = block(y, x)                # the same as a module
 
-and its parts, forward and backward, for blocks of another make: rms_norm8, linear8, gated_linear8 and their *_backward.
+and its parts, forward and backward, for blocks of another make: rms_norm8, linear8, gated_linear8 and their *_backward.  The parts record no
+gradients and refuse tensors that want one while autograd records: call them within torch.no_grad() or an autograd.Function.
 A row is whatever the last dimension holds: a voxel's channels, a patch of a volume.
 
 All run in libleap_hip.so on the current HIP stream; PyTorch supplies memory.  Tensors are on one GPU; the values of a row
@@ -57,6 +58,15 @@ class Packed8:
 
     def __repr__(self):
         return f"Packed8(shape={tuple(self.shape)}, device={self.device})"
+
+
+def _not_recorded(*tensors) -> None:
+    """The results have no graph: silently without one they would train with a part of the gradient."""
+    if torch.is_grad_enabled():
+        for t in tensors:
+            if t is not None and t.requires_grad:
+                raise ValueError("this operator records no gradient, and an argument requires one: use feed_forward8, call it within torch.no_grad() or an "
+                                 "autograd.Function (with the *_backward operators), or hand it .detach()ed tensors")
 
 
 def _type_of(t: torch.Tensor, what: str) -> int:
@@ -171,6 +181,7 @@ def _address(t):
 
 def pack8(x: torch.Tensor) -> Packed8:
     """x (float32, bfloat16, float16; [..., columns]) in 8 bits."""
+    _not_recorded(x)
     _on_gpu(x, "x")
     kind = _type_of(x, "x")
     rows, cols, stride = _rows(x, "x")
@@ -259,6 +270,7 @@ def rms_norm8(x: torch.Tensor, weight: torch.Tensor, residual: torch.Tensor = No
     """(sum, normed, kept, rstd): sum = x + residual (x itself without one), normed = packed sum * rstd * weight with rstd =
     1 / sqrt(mean(sum^2) + eps) over the row; kept = packed sum and rstd (float32) are for rms_norm8_backward (None with
     keep=False).  residual: x's type and shape; weight: [columns], x's type or float32."""
+    _not_recorded(x, weight, residual)
     _on_gpu(x, "x")
     device, kind = x.device, _type_of(x, "x")
     rows, cols, stride = _rows(x, "x")
@@ -288,6 +300,7 @@ def rms_norm8_backward(grad: torch.Tensor, kept: Packed8, rstd: torch.Tensor, we
                        dtype: torch.dtype = None):
     """(grad_x, grad_weight) from the gradient of `normed` and, where there is one, of `sum`.  grad_x is the residual's gradient
     too, of type `dtype` (grad's if not given); grad: that type or float32."""
+    _not_recorded(grad, grad_sum)
     dtype = grad.dtype if dtype is None else dtype
     if dtype not in _TYPES:
         raise ValueError(f"gradients are float32, bfloat16 or float16, not {dtype}")
@@ -319,6 +332,7 @@ def _packed_rows(x: Packed8, what: str = "x"):
 
 def linear8(x: Packed8, weight: torch.Tensor) -> torch.Tensor:
     """x W^T, bfloat16 [..., outputs], from packed rows and a bfloat16 weight [outputs, columns]."""
+    _not_recorded(weight)
     rows, cols = _packed_rows(x)
     out, w_stride = _weight(weight, cols, x.device)
     y = torch.empty(x.shape[:-1] + (out,), dtype=torch.bfloat16, device=x.device)
@@ -330,6 +344,7 @@ def linear8(x: Packed8, weight: torch.Tensor) -> torch.Tensor:
 def linear8_backward(grad: torch.Tensor, x: Packed8, weight: torch.Tensor, need_x: bool = True, need_weight: bool = True,
                      dtype: torch.dtype = torch.bfloat16):
     """(grad_x, grad_weight): dy W (bfloat16, or float32 by `dtype`) and dy^T x (bfloat16); None for one that is not needed."""
+    _not_recorded(grad)
     rows, cols = _packed_rows(x)
     out, w_stride = _weight(weight, cols, x.device)
     _, _, stride = _gradient(grad, x.shape[:-1] + (out,), x.device, (torch.bfloat16,), "grad")
@@ -353,6 +368,7 @@ def _halves(weight: torch.Tensor, cols: int, device, what: str = "weight"):
 def gated_linear8(x: Packed8, weight: torch.Tensor, keep: bool = True):
     """(gated, kept): with u = x W^T = (g, p), W bfloat16 [2 * outputs, columns], gated = packed g * sigmoid(g) * p [...,
     outputs] and kept = packed u [..., 2, outputs] for the backward pass (None with keep=False).  u is 32 bits and never stored."""
+    _not_recorded(weight)
     rows, cols = _packed_rows(x)
     out, w_stride = _halves(weight, cols, x.device)
     gated = _empty_packed(x.shape[:-1] + (out,), x.device)
@@ -374,6 +390,7 @@ def _kept_halves(kept: Packed8):
 
 def gate8_backward(grad: torch.Tensor, kept: Packed8) -> torch.Tensor:
     """du [..., 2 * outputs] (bfloat16), the gradient of gated_linear8's u, from that of `gated`."""
+    _not_recorded(grad)
     lead, out = _kept_halves(kept)
     rows, _, stride = _gradient(grad, lead + (out,), kept.device, (torch.bfloat16,), "grad")
     du = torch.empty(lead + (2 * out,), dtype=torch.bfloat16, device=kept.device)
@@ -383,6 +400,7 @@ def gate8_backward(grad: torch.Tensor, kept: Packed8) -> torch.Tensor:
 
 def linear_gate8_backward(grad: torch.Tensor, weight: torch.Tensor, kept: Packed8) -> torch.Tensor:
     """gate8_backward of grad W, which stays in 32 bits: du from the gradient of the product linear8(gated, weight)."""
+    _not_recorded(grad)
     lead, out = _kept_halves(kept)
     following, w_stride = _weight(weight, out, kept.device)
     rows, _, stride = _gradient(grad, lead + (following,), kept.device, (torch.bfloat16,), "grad")
@@ -398,6 +416,7 @@ def gated_linear8_backward(grad: torch.Tensor, kept: Packed8, x: Packed8, weight
     """(grad_x, grad_weight) of gated_linear8 from the gradient of `gated` (bfloat16).  In between is du, the gradient of u: in bfloat16
     (the results are 0.0024 of their norm off, 0.0017 of it their own rounding), or, fine, as the sum of two, so that the results' rounding is the only
     one; the products take twice as long."""
+    _not_recorded(grad)
     if kept.shape[:-2] != x.shape[:-1]:
         raise ValueError(f"kept {tuple(kept.shape)} is not of this x {tuple(x.shape)}")
     lead, out = _kept_halves(kept)

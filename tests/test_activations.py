@@ -324,3 +324,25 @@ def test_workspaces_that_are_not_aligned_are_refused(lib):
         for work in (P + 8, P + 1, None):
             assert getattr(lib, name)(*arguments, work, None) == B.LEAP_INVALID_ARG, (name, work)
             assert lib.leap_last_error()
+
+
+def test_parts_refuse_to_cut_a_graph():
+    """Tensors that want a gradient, while autograd records: the results would have none.  Without recording they are looked at as ever
+    (and refused here for being on the CPU)."""
+    from paper_2307_05801_amd import activations as A
+    x, w, big, p = torch.zeros(4, 64, dtype=BF16), torch.ones(64, dtype=BF16), torch.zeros(8, 64, dtype=BF16), _packed(4, 64)
+    wants = lambda t: t.clone().requires_grad_(True)  # noqa: E731
+    kept, rstd = _packed(4, 64), torch.ones(4)
+    for call in (lambda: A.pack8(wants(x)), lambda: A.rms_norm8(wants(x), w), lambda: A.rms_norm8(x, wants(w)), lambda: A.rms_norm8(x, w, residual=wants(x)),
+                 lambda: A.linear8(p, wants(big)), lambda: A.gated_linear8(p, wants(big)), lambda: A.linear8_backward(wants(x), p, big),
+                 lambda: A.gate8_backward(wants(x), p), lambda: A.linear_gate8_backward(wants(x), big, p), lambda: A.gated_linear8_backward(wants(x), kept, p, big),
+                 lambda: A.rms_norm8_backward(wants(x), kept, rstd, w), lambda: A.rms_norm8_backward(x, kept, rstd, w, grad_sum=wants(x))):
+        with pytest.raises(ValueError, match="records no gradient"):
+            call()
+        with torch.no_grad(), pytest.raises(ValueError) as refused:
+            call()
+        assert "records no gradient" not in str(refused.value)
+    # weights' gradients from parameters as they are, in a training step written by hand
+    with pytest.raises(ValueError) as refused:
+        A.linear8_backward(x, p, wants(big))
+    assert "records no gradient" not in str(refused.value)

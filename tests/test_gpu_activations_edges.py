@@ -164,3 +164,29 @@ def test_weight_gradient_of_no_rows_and_2_27_values(A):  # noqa: F811
     del del_me                                               # the gradient's memory holds ones
     x = A.Packed8(torch.empty(0, cols, dtype=torch.float8_e4m3fn, device="cuda"), torch.empty(0, cols // 32, dtype=torch.uint8, device="cuda"))
     assert not A.linear8_backward(torch.empty(0, out, dtype=BF16, device="cuda"), x, w)[1].any()
+
+
+def test_parts_within_a_function_of_ones_own(A):  # noqa: F811
+    """Forward and backward of linear8 as an autograd.Function, where nothing is recorded, on parameters; and not outside."""
+    class Linear(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x, w):
+            ctx.packed = A.pack8(x)
+            ctx.save_for_backward(w)
+            return A.linear8(ctx.packed, w)
+
+        @staticmethod
+        def backward(ctx, g):
+            return A.linear8_backward(g, ctx.packed, ctx.saved_tensors[0])
+
+    x = torch.randn(40, 64, device="cuda", generator=torch.Generator(device="cuda").manual_seed(310)).to(BF16).requires_grad_(True)
+    w = torch.nn.Parameter(weight_of(32, 64, 311).cuda())
+    dx, dw = torch.autograd.grad(Linear.apply(x, w).float().square().sum(), (x, w))
+    with torch.no_grad():
+        packed = A.pack8(x)
+        g = (2 * A.linear8(packed, w).float()).to(BF16)
+        want = A.linear8_backward(g, packed, w)
+    assert torch.equal(dx, want[0]) and torch.equal(dw, want[1])
+    for call in (lambda: A.pack8(x), lambda: A.linear8(packed, w), lambda: A.gated_linear8(packed, w), lambda: A.rms_norm8(x, torch.ones(64, device="cuda"))):
+        with pytest.raises(ValueError, match="records no gradient"):
+            call()
