@@ -129,6 +129,13 @@ int leap_feed_forward8(const void *d_x, int64_t x_stride, const void *d_residual
                        int32_t norm_weight_type, int64_t rows, int64_t cols, float eps, const void *d_up, int64_t up_stride, int64_t hidden,
                        const void *d_down, int64_t down_stride, int64_t out, void *d_sum, void *d_y, void *d_kept, void *d_work,
                        void *hip_stream);
+/* Forward with nothing kept, where no backward pass follows: y and d_sum are those of leap_feed_forward8.  d_work: as many bytes as the function
+ * with "_work" says, 16-byte aligned, never NULL (no rows: may be NULL). */
+int64_t leap_feed_forward8_alone_work(int64_t rows, int64_t cols, const void *d_up, int64_t up_stride, int64_t hidden, const void *d_down,
+                                      int64_t down_stride, int64_t out);
+int leap_feed_forward8_alone(const void *d_x, int64_t x_stride, const void *d_residual, int64_t residual_stride, const void *d_norm_weight,
+                             int32_t norm_weight_type, int64_t rows, int64_t cols, float eps, const void *d_up, int64_t up_stride, int64_t hidden,
+                             const void *d_down, int64_t down_stride, int64_t out, void *d_sum, void *d_y, void *d_work, void *hip_stream);
 int64_t leap_feed_forward8_backward_work(const void *d_dy, int64_t dy_stride, int64_t rows, int64_t cols, const void *d_up, int64_t up_stride,
                                          int64_t hidden, const void *d_down, int64_t down_stride, int64_t out);
 int leap_feed_forward8_backward(const void *d_dy, int64_t dy_stride, const void *d_grad_sum, int64_t grad_sum_stride, const void *d_norm_weight,

@@ -437,28 +437,36 @@ def gated_linear8_backward(grad: torch.Tensor, kept: Packed8, x: Packed8, weight
 # ---- the block ----------------------------------------------------------------------------------------------------------
 
 
+def _block_forward(x, residual, norm_weight, up, down, eps, keep):
+    """(y, sum, kept, (rows, columns, hidden, outputs)); kept None where there is nothing to keep it for."""
+    device = x.device
+    rows, cols, stride = _rows(x, "x")
+    residual_stride = 0 if residual is None else _gradient(residual, x.shape, device, (x.dtype,), "residual")[2]
+    _norm_weight(norm_weight, x, cols)
+    hidden, up_stride = _halves(up, cols, device, "up")
+    out, down_stride = _weight(down, hidden, device, "down")
+    total = None if residual is None else _like(x, x.dtype)
+    y = torch.empty(x.shape[:-1] + (out,), dtype=x.dtype, device=device)
+    weights = (up.data_ptr(), up_stride, hidden, down.data_ptr(), down_stride, out)
+    name, kept = "leap_feed_forward8" if keep else "leap_feed_forward8_alone", None
+    if keep:
+        lib = B._activations or B.load_activations()
+        kept = torch.empty(lib.leap_feed_forward8_kept(rows, cols, hidden), dtype=torch.uint8, device=device)
+    work = _work(name + "_work", device, rows, cols, *weights)
+    _call(name, device, x.data_ptr(), stride, _address(residual), residual_stride, norm_weight.data_ptr(), _TYPES[norm_weight.dtype], rows, cols, eps,
+          *weights, _address(total), y.data_ptr(), *((kept.data_ptr(),) if keep else ()), _address(work))
+    # without a residual a tensor apart from its input: autograd would take it for a view
+    return y, x.view_as(x) if total is None else total, kept, (rows, cols, hidden, out)
+
+
 class _FeedForward8(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, residual, norm_weight, up, down, eps, fine):
-        device = x.device
-        rows, cols, stride = _rows(x, "x")
-        residual_stride = 0 if residual is None else _gradient(residual, x.shape, device, (x.dtype,), "residual")[2]
-        _norm_weight(norm_weight, x, cols)
-        hidden, up_stride = _halves(up, cols, device, "up")
-        out, down_stride = _weight(down, hidden, device, "down")
-        total = None if residual is None else _like(x, x.dtype)
-        y = torch.empty(x.shape[:-1] + (out,), dtype=x.dtype, device=device)
-        lib = B._activations or B.load_activations()
-        kept = torch.empty(lib.leap_feed_forward8_kept(rows, cols, hidden), dtype=torch.uint8, device=device)
-        weights = (up.data_ptr(), up_stride, hidden, down.data_ptr(), down_stride, out)
-        work = _work("leap_feed_forward8_work", device, rows, cols, *weights)
-        _call("leap_feed_forward8", device, x.data_ptr(), stride, _address(residual), residual_stride, norm_weight.data_ptr(), _TYPES[norm_weight.dtype],
-              rows, cols, eps, *weights, _address(total), y.data_ptr(), kept.data_ptr(), _address(work))
+        y, total, kept, sizes = _block_forward(x, residual, norm_weight, up, down, eps, True)
         ctx.save_for_backward(norm_weight, up, down, kept)
         ctx.set_materialize_grads(False)
-        ctx.added, ctx.shape, ctx.sizes, ctx.fine = residual is not None, x.shape, (rows, cols, hidden, out), fine
-        # without a residual a tensor apart from its input: autograd would take it for a view
-        return y, x.view_as(x) if total is None else total
+        ctx.added, ctx.shape, ctx.sizes, ctx.fine = residual is not None, x.shape, sizes, fine
+        return y, total
 
     @staticmethod
     @torch.autograd.function.once_differentiable
@@ -489,12 +497,15 @@ def feed_forward8(x: torch.Tensor, norm_weight: torch.Tensor, up: torch.Tensor, 
                   eps: float = 1e-6, fine: bool = False):
     """(y, sum), differentiable: sum = x + residual and y = linear8(gated_linear8(rms_norm8(sum), up), down).  x, residual: bfloat16
     [..., columns]; up: [2 * hidden, columns], the gate's rows first; down: [outputs, hidden].  For a stack of blocks y and sum are the next one's
-    x and residual.  Kept for the backward pass: the norm's output, sum and the hidden rows (three times), all in 8 bits.
+    x and residual.  Kept for the backward pass, if there is one to come: the norm's output, sum and the hidden rows (three times), all in 8 bits.
     fine: the gradient of up's product is not rounded to bfloat16 on its way to the gradients of x, norm_weight and up (gated_linear8_backward)."""
     _on_gpu(x, "x")
     if x.dtype is not torch.bfloat16:
         raise ValueError(f"x must be bfloat16, not {x.dtype}")
-    return _FeedForward8.apply(x, residual, norm_weight, up, down, eps, fine)
+    tensors = (x, residual, norm_weight, up, down)
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):
+        return _FeedForward8.apply(*tensors, eps, fine)
+    return _block_forward(*tensors, eps, False)[:2]
 
 
 class FeedForward8(torch.nn.Module):

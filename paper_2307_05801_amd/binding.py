@@ -45,6 +45,8 @@ ACTIVATION_EXPORTS = {                                       # name: (result, ar
     "leap_feed_forward8_kept": (_L, [_L, _L, _L]),
     "leap_feed_forward8_work": (_L, [_L, _L, _P, _L, _L, _P, _L, _L]),
     "leap_feed_forward8": (C.c_int, [_P, _L, _P, _L, _P, _I, _L, _L, C.c_float, _P, _L, _L, _P, _L, _L] + [_P] * 5),
+    "leap_feed_forward8_alone_work": (_L, [_L, _L, _P, _L, _L, _P, _L, _L]),
+    "leap_feed_forward8_alone": (C.c_int, [_P, _L, _P, _L, _P, _I, _L, _L, C.c_float, _P, _L, _L, _P, _L, _L] + [_P] * 4),
     "leap_feed_forward8_backward_work": (_L, [_P, _L, _L, _L, _P, _L, _L, _P, _L, _L]),
     "leap_feed_forward8_backward": (C.c_int, [_P, _L, _P, _L, _P, _I, _L, _L, _P, _L, _L, _P, _L, _L] + [_P] * 7),
     "leap_feed_forward8_backward_fine_work": (_L, [_P, _L, _L, _L, _P, _L, _L, _P, _L, _L]),

@@ -10,12 +10,13 @@ using namespace act;
 
 int64_t up16(int64_t n) { return (n + 15) / 16 * 16; }
 
-// What the backward pass reads: one array's codes and scales after the other's, each from a multiple of 16 bytes on.
+// What the backward pass reads, one array's codes and scales after the other's, each from a multiple of 16 bytes on; or what only the forward
+// pass does, the norm's output and the gated rows.
 struct kept_block {
-    uint8_t *normed, *normed_scales, *sum, *sum_scales, *gated, *gated_scales, *gate, *gate_scales;
-    float *rstd;
+    uint8_t *normed, *normed_scales, *sum = nullptr, *sum_scales = nullptr, *gated, *gated_scales, *gate = nullptr, *gate_scales = nullptr;
+    float *rstd = nullptr;
     int64_t bytes;
-    kept_block(void *base, int64_t rows, int64_t cols, int64_t hidden)
+    kept_block(void *base, int64_t rows, int64_t cols, int64_t hidden, bool backward)
     {
         uint8_t *at = (uint8_t *)base;
         const auto take = [&](int64_t n) {
@@ -24,10 +25,10 @@ struct kept_block {
             return p;
         };
         normed = take(rows * cols), normed_scales = take(rows * groups_of(cols));
-        sum = take(rows * cols), sum_scales = take(rows * groups_of(cols));
+        if (backward) sum = take(rows * cols), sum_scales = take(rows * groups_of(cols));
         gated = take(rows * hidden), gated_scales = take(rows * groups_of(hidden));
-        gate = take(rows * 2 * hidden), gate_scales = take(rows * 2 * groups_of(hidden));
-        rstd = (float *)take(rows * 4);
+        if (backward) gate = take(rows * 2 * hidden), gate_scales = take(rows * 2 * groups_of(hidden));
+        if (backward) rstd = (float *)take(rows * 4);
         bytes = at - (uint8_t *)base;
     }
 };
@@ -49,7 +50,7 @@ struct block_sizes {
     }
     int64_t work(void *kept) const
     {
-        const kept_block K(kept, rows, cols, hidden);
+        const kept_block K(kept, rows, cols, hidden, true);
         const int64_t a = leap_linear8_work(K.normed, rows, cols, up, up_stride, 2 * hidden), b = leap_linear8_work(K.gated, rows, hidden, down, down_stride, out);
         return a > b ? a : b;
     }
@@ -57,7 +58,7 @@ struct block_sizes {
     int64_t dn_bytes() const { return up16(rows * cols * 4); }
     int64_t backward_work(const void *dy, int64_t dy_stride, const du_layout &L) const
     {
-        const kept_block K(nullptr, rows, cols, hidden);
+        const kept_block K(nullptr, rows, cols, hidden, true);
         int64_t most = leap_rms_norm8_work(rows, cols) * 4;
         for (int64_t n : {leap_linear8_backward_work(dy, dy_stride, K.gated, rows, hidden, down, down_stride, out),
                           leap_linear_gate8_work(dy, dy_stride, down, down_stride, out, rows, hidden),
@@ -72,7 +73,7 @@ struct block_sizes {
 extern "C" int64_t leap_feed_forward8_kept(int64_t rows, int64_t cols, int64_t hidden)
 {
     if (bad_sizes(rows, cols) || hidden < 1 || hidden > MOST_COLS / 2 || bad_sizes(rows, 2 * hidden)) return 0;
-    return kept_block(nullptr, rows, cols, hidden).bytes;
+    return kept_block(nullptr, rows, cols, hidden, true).bytes;
 }
 
 extern "C" int64_t leap_feed_forward8_work(int64_t rows, int64_t cols, const void *d_up, int64_t up_stride, int64_t hidden, const void *d_down,
@@ -81,6 +82,24 @@ extern "C" int64_t leap_feed_forward8_work(int64_t rows, int64_t cols, const voi
     const block_sizes S{rows, cols, hidden, out, d_up, d_down, up_stride, down_stride};
     return S.bad() ? 0 : S.work(nullptr);
 }
+
+namespace {
+
+int block_forward(const void *d_x, int64_t x_stride, const void *d_residual, int64_t residual_stride, const void *d_norm_weight, int32_t norm_weight_type,
+                  float eps, const block_sizes &S, void *d_sum, void *d_y, const kept_block &K, void *d_work, void *hip_stream)
+{
+    if (!S.up || !S.down || !d_y) return refuse("null data pointer");
+    if (norm_weight_type != LEAP_F32 && norm_weight_type != LEAP_BF16) return refuse("the norm's weight must be float32 or bfloat16");
+    int rc = leap_rms_norm8(d_x, x_stride, d_residual, residual_stride, LEAP_BF16, d_norm_weight, norm_weight_type, S.rows, S.cols, eps, d_sum, K.normed,
+                            K.normed_scales, K.sum, K.sum_scales, K.rstd, hip_stream);
+    if (rc == LEAP_OK)
+        rc = leap_gated_linear8(K.normed, K.normed_scales, S.rows, S.cols, S.up, S.up_stride, S.hidden, K.gated, K.gated_scales, K.gate, K.gate_scales, d_work,
+                                hip_stream);
+    if (rc == LEAP_OK) rc = leap_linear8(K.gated, K.gated_scales, S.rows, S.hidden, S.down, S.down_stride, S.out, d_y, d_work, hip_stream);
+    return rc;
+}
+
+}  // namespace
 
 extern "C" int leap_feed_forward8(const void *d_x, int64_t x_stride, const void *d_residual, int64_t residual_stride, const void *d_norm_weight,
                                   int32_t norm_weight_type, int64_t rows, int64_t cols, float eps, const void *d_up, int64_t up_stride, int64_t hidden,
@@ -91,16 +110,28 @@ extern "C" int leap_feed_forward8(const void *d_x, int64_t x_stride, const void 
     if (const char *why = S.bad()) return refuse(why);
     if (!rows) return LEAP_OK;
     if (unaligned(d_kept)) return refuse("what is kept needs memory from a multiple of 16 bytes on");
-    if (!d_up || !d_down || !d_y) return refuse("null data pointer");
     if (unaligned(d_work) && S.work(d_kept)) return refuse(NO_WORK);
-    if (norm_weight_type != LEAP_F32 && norm_weight_type != LEAP_BF16) return refuse("the norm's weight must be float32 or bfloat16");
-    const kept_block K(d_kept, rows, cols, hidden);
-    int rc = leap_rms_norm8(d_x, x_stride, d_residual, residual_stride, LEAP_BF16, d_norm_weight, norm_weight_type, rows, cols, eps, d_sum, K.normed,
-                            K.normed_scales, K.sum, K.sum_scales, K.rstd, hip_stream);
-    if (rc == LEAP_OK)
-        rc = leap_gated_linear8(K.normed, K.normed_scales, rows, cols, d_up, up_stride, hidden, K.gated, K.gated_scales, K.gate, K.gate_scales, d_work, hip_stream);
-    if (rc == LEAP_OK) rc = leap_linear8(K.gated, K.gated_scales, rows, hidden, d_down, down_stride, out, d_y, d_work, hip_stream);
-    return rc;
+    return block_forward(d_x, x_stride, d_residual, residual_stride, d_norm_weight, norm_weight_type, eps, S, d_sum, d_y, kept_block(d_kept, rows, cols, hidden, true),
+                         d_work, hip_stream);
+}
+
+extern "C" int64_t leap_feed_forward8_alone_work(int64_t rows, int64_t cols, const void *d_up, int64_t up_stride, int64_t hidden, const void *d_down,
+                                                 int64_t down_stride, int64_t out)
+{
+    const block_sizes S{rows, cols, hidden, out, d_up, d_down, up_stride, down_stride};
+    return S.bad() ? 0 : kept_block(nullptr, rows, cols, hidden, false).bytes + S.work(nullptr);
+}
+
+extern "C" int leap_feed_forward8_alone(const void *d_x, int64_t x_stride, const void *d_residual, int64_t residual_stride, const void *d_norm_weight,
+                                        int32_t norm_weight_type, int64_t rows, int64_t cols, float eps, const void *d_up, int64_t up_stride, int64_t hidden,
+                                        const void *d_down, int64_t down_stride, int64_t out, void *d_sum, void *d_y, void *d_work, void *hip_stream)
+{
+    const block_sizes S{rows, cols, hidden, out, d_up, d_down, up_stride, down_stride};
+    if (const char *why = S.bad()) return refuse(why);
+    if (!rows) return LEAP_OK;
+    if (unaligned(d_work)) return refuse(NO_WORK);
+    const kept_block K(d_work, rows, cols, hidden, false);
+    return block_forward(d_x, x_stride, d_residual, residual_stride, d_norm_weight, norm_weight_type, eps, S, d_sum, d_y, K, (uint8_t *)d_work + K.bytes, hip_stream);
 }
 
 namespace {
@@ -124,7 +155,7 @@ int block_backward(bool fine, const void *d_dy, int64_t dy_stride, const void *d
     if (rows && (d_grad_x || d_grad_norm_weight) && !d_norm_weight) return refuse("null data pointer");
     if (rows && d_grad_norm_weight && !d_grad_x) return refuse("the norm's weight gradient comes with grad_x");
     if (unaligned(d_work)) return refuse(NO_WORK);
-    const kept_block K((void *)d_kept, rows, cols, hidden);
+    const kept_block K((void *)d_kept, rows, cols, hidden, true);
     // du is bfloat16, which the matrix units take: grad_up is 0.0024 of its norm off, grad_norm_weight 0.0024 to 0.0034, where 0.0017 are their own
     // rounding to bfloat16.  A caller who wants that alone asks for a fine du, whose products take twice as long (262144 x 512 through 1024, forward and
     // backward: 4.79 ms, 3.53).  32 bits between the product and the norm: a rounding less in grad_x.

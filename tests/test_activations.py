@@ -346,3 +346,20 @@ def test_parts_refuse_to_cut_a_graph():
     with pytest.raises(ValueError) as refused:
         A.linear8_backward(x, p, wants(big))
     assert "records no gradient" not in str(refused.value)
+
+
+BLOCK_ALONE = BLOCK_FORWARD[:17] + BLOCK_FORWARD[18:]
+
+
+def test_a_block_without_a_backward_pass(lib):
+    """Refusals, and room for the norm's output and the gated rows alone."""
+    for at, value in [(5, 2), (6, -1), (6, 1 << 32), (7, 0), (7, 1 << 21), (1, 63), (3, 63), (8, -1.0), (10, 63), (11, 0), (11, 1 << 20),
+                      (13, 7), (14, 0), (0, 0), (4, 0), (9, 0), (12, 0), (16, 0), (17, 0), (17, P + 8)]:
+        arguments = list(BLOCK_ALONE)
+        arguments[at] = value
+        assert lib.leap_feed_forward8_alone(*arguments) == B.LEAP_INVALID_ARG, (at, value)
+        assert lib.leap_last_error()
+    assert lib.leap_feed_forward8_alone_work(4, 64, P, 64, 16, P, 16, 24) == 256 + 16 + 64 + 16
+    assert lib.leap_feed_forward8_alone_work(4, 64, P, 65, 16, P, 16, 24) == 256 + 16 + 64 + 16 + 32 * 64 * 2
+    assert lib.leap_feed_forward8_alone_work(4, 64, P, 64, 16, P, 16, 0) == 0 and lib.leap_feed_forward8_alone_work(-1, 64, P, 64, 16, P, 16, 8) == 0
+    assert lib.leap_feed_forward8_alone(None, 64, None, 64, None, 1, 0, 64, 1e-6, None, 64, 8, None, 8, 16, *[None] * 4) == B.LEAP_OK

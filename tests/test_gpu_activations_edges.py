@@ -5,7 +5,7 @@ import pytest
 import torch
 
 import activations_reference as R  # noqa: F401
-from test_gpu_activations import A, BF16, F32, weight_of  # noqa: F401
+from test_gpu_activations import A, BF16, F32, _block, weight_of  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -190,3 +190,24 @@ def test_parts_within_a_function_of_ones_own(A):  # noqa: F811
     for call in (lambda: A.pack8(x), lambda: A.linear8(packed, w), lambda: A.gated_linear8(packed, w), lambda: A.rms_norm8(x, torch.ones(64, device="cuda"))):
         with pytest.raises(ValueError, match="records no gradient"):
             call()
+
+
+@pytest.mark.parametrize("rows,cols,hidden,out,added", [(0, 64, 32, 64, True), (1, 32, 32, 32, True), (130, 343, 70, 90, False), (3000, 512, 256, 512, True)])
+def test_a_block_without_a_backward_pass(A, rows, cols, hidden, out, added):  # noqa: F811
+    """The same bits as with one, and none of the memory that only a backward pass reads, whether nothing is recorded or nothing wants a gradient."""
+    x, r, nw, up, _, _, _ = _block(max(rows, 1), cols, hidden, seed=320)
+    x, r, nw, up, down = x[:rows].cuda(), r[:rows].cuda() if added else None, nw.cuda(), up.cuda(), weight_of(out, hidden, 328).cuda()
+    wants = [t.clone().requires_grad_(True) for t in (nw, up, down)]
+    want_y, want_s = A.feed_forward8(x, *wants, residual=r)
+    assert want_y.requires_grad
+    for weights, recording in ((wants, False), ((nw, up, down), True)):
+        gc.collect()
+        torch.cuda.reset_peak_memory_stats()
+        before = torch.cuda.memory_allocated()
+        with torch.set_grad_enabled(recording):
+            y, s = A.feed_forward8(x, *weights, residual=r)
+        most = torch.cuda.max_memory_allocated() - before
+        assert torch.equal(y, want_y) and torch.equal(s, want_s) and not y.requires_grad
+        whole = rows * (2 * out + (2 * cols if added else 0)) + rows * (cols + hidden) * 33 // 32 + 2 * (2 * hidden * (cols + 8) + out * (hidden + 8))
+        assert rows < 1000 or most < whole + 65536                        # the packed sum and both halves, 3 MB, are not there
+        del y, s
