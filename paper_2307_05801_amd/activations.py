@@ -297,8 +297,8 @@ def _norm_weight(weight: torch.Tensor, x, cols: int) -> None:
 
 
 def rms_norm8_backward(grad: torch.Tensor, kept: Packed8, rstd: torch.Tensor, weight: torch.Tensor, grad_sum: torch.Tensor = None,
-                       dtype: torch.dtype = None):
-    """(grad_x, grad_weight) from the gradient of `normed` and, where there is one, of `sum`.  grad_x is the residual's gradient
+                       dtype: torch.dtype = None, need_weight: bool = True):
+    """(grad_x, grad_weight or None if not needed) from the gradient of `normed` and, where there is one, of `sum`.  grad_x is the residual's gradient
     too, of type `dtype` (grad's if not given); grad: that type or float32."""
     _not_recorded(grad, grad_sum)
     dtype = grad.dtype if dtype is None else dtype
@@ -313,12 +313,14 @@ def rms_norm8_backward(grad: torch.Tensor, kept: Packed8, rstd: torch.Tensor, we
     _on_gpu(rstd, "rstd", device)
     if rstd.shape != kept.shape[:-1] or rstd.dtype is not torch.float32 or not rstd.is_contiguous():
         raise ValueError(f"rstd must be contiguous float32 {tuple(kept.shape[:-1])}")
-    grad_weight = _like(weight, weight.dtype)
-    lib = B._activations or B.load_activations()
-    work = torch.empty(lib.leap_rms_norm8_work(rows, cols), dtype=torch.float32, device=device)
+    grad_weight = work = None
+    if need_weight:
+        grad_weight = _like(weight, weight.dtype)
+        lib = B._activations or B.load_activations()
+        work = torch.empty(lib.leap_rms_norm8_work(rows, cols), dtype=torch.float32, device=device)
     _call("leap_rms_norm8_backward", device, grad.data_ptr(), _TYPES[grad.dtype], stride, _address(grad_sum), sum_stride, _TYPES[dtype],
           kept.codes.data_ptr(), kept.scales.data_ptr(), rstd.data_ptr(), weight.data_ptr(), _TYPES[weight.dtype], rows, cols,
-          grad_x.data_ptr(), grad_weight.data_ptr(), work.data_ptr())
+          grad_x.data_ptr(), _address(grad_weight), _address(work))
     return grad_x, grad_weight
 
 

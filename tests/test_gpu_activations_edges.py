@@ -211,3 +211,12 @@ def test_a_block_without_a_backward_pass(A, rows, cols, hidden, out, added):  # 
         whole = rows * (2 * out + (2 * cols if added else 0)) + rows * (cols + hidden) * 33 // 32 + 2 * (2 * hidden * (cols + 8) + out * (hidden + 8))
         assert rows < 1000 or most < whole + 65536                        # the packed sum and both halves, 3 MB, are not there
         del y, s
+
+
+@pytest.mark.parametrize("cols", [40, 512, 2500])
+def test_norm_gradient_without_the_weights(A, cols):  # noqa: F811
+    x, w = _channels(300, cols, 330), torch.ones(cols, device="cuda")
+    _, _, kept, rstd = A.rms_norm8(x, w)
+    want, _ = A.rms_norm8_backward(x, kept, rstd, w)
+    got, none = A.rms_norm8_backward(x, kept, rstd, w, need_weight=False)
+    assert none is None and torch.equal(got, want)
