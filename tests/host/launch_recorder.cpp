@@ -56,6 +56,15 @@ int hipLaunchKernel(const void *host, grid3 grid, grid3 block, void **, size_t, 
 }
 int hipGetLastError() { return 0; }
 
+// The mangled names of all the kernels there are, a line each.
+long registered_kernels(char *to, long room)
+{
+    std::string all;
+    for (const auto &n : names()) all += n.second + "\n";
+    if ((long)all.size() < room) std::memcpy(to, all.c_str(), all.size() + 1);
+    return (long)all.size();
+}
+
 // What was launched since the last call: a kernel's mangled name, its blocks and its threads a line.
 long recorded_launches(char *to, long room)
 {

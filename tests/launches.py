@@ -1,6 +1,7 @@
 """What the operators on activations in 8 bits launch, without a GPU: tests/host/launch_recorder.cpp stands in for the HIP runtime.
 
     record([("leap_pack8", (...)), ...]) -> [(status, [Launch(kernel, parameters, blocks, threads), ...]), ...]
+    kernels() -> {(kernel, parameters), ...}, all that the library has
 
 Arguments are those of include/leap_activations.h; addresses are never touched."""
 import json
@@ -28,20 +29,29 @@ def _build():
         os.replace(tmp, LIB)
 
 
-def record(calls):
+def _run(calls):
     """In a process of its own, which must not have loaded the runtime (nor torch)."""
     _build()
     done = subprocess.run([sys.executable, os.path.abspath(__file__)], input=json.dumps(calls), capture_output=True, text=True, timeout=120)
     assert done.returncode == 0, done.stderr
+    return json.loads(done.stdout)
+
+
+def _name(mangled):
+    found = re.search(r"\d(k_[a-z_]+?)(I(?:L[ib]\d+E)+E)?(?=E|v|P|N|S|$)", mangled)
+    return (found.group(1), tuple(int(v) for v in re.findall(r"L[ib](\d+)E", found.group(2) or ""))) if found else None
+
+
+def record(calls):
     out = []
-    for status, text in json.loads(done.stdout):
-        launches = []
-        for line in text.splitlines():
-            name, *n = line.split()
-            kernel, parameters = re.search(r"\d(k_[a-z_]+?)(I(?:L[ib]\d+E)+E)?(?=E|v|P|N|S|$)", name).groups()
-            launches.append(Launch(kernel, tuple(int(v) for v in re.findall(r"L[ib](\d+)E", parameters or "")), tuple(map(int, n[:3])), int(n[3]) * int(n[4]) * int(n[5])))
-        out.append((status, launches))
+    for status, text in _run(calls)[1:]:
+        lines = [line.split() for line in text.splitlines()]
+        out.append((status, [Launch(*_name(name), tuple(map(int, n[:3])), int(n[3]) * int(n[4]) * int(n[5])) for name, *n in lines]))
     return out
+
+
+def kernels():
+    return set(filter(None, map(_name, _run([])[0].splitlines())))
 
 
 def _main():
@@ -51,7 +61,8 @@ def _main():
     from paper_2307_05801_amd import binding as B
     lib = B.load_activations()
     room = C.create_string_buffer(1 << 20)
-    out = []
+    assert recorder.registered_kernels(room, len(room)) < len(room)
+    out = [room.value.decode()]
     for name, arguments in json.load(sys.stdin):
         status = getattr(lib, name)(*arguments)
         assert recorder.recorded_launches(room, len(room)) < len(room)

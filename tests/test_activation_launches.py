@@ -1,7 +1,8 @@
 """What the operators on activations in 8 bits launch, on the CPU (tests/launches.py): how many blocks, of which kernels."""
 import pytest
 
-from launches import record
+import activation_kernels as K
+from launches import kernels, record
 from paper_2307_05801_amd import binding as B
 
 P = 0x1000
@@ -33,3 +34,27 @@ def test_a_launch_has_fewer_than_2_32_threads():
             assert across * launch.threads < 1 << 32 and along < 1 << 16 and deep == 1, (name, launch)
         mine = sum(launch.blocks[0] for launch in launches if launch.kernel == kernel)
         assert mine == blocks or blocks is None and mine, (name, kernel, mine, blocks)
+
+
+def _call(what, rows, cols, out):
+    if what == K.Y:
+        return "leap_linear8", (P, P, rows, cols, P, cols, out, P, P, 0)
+    if what == K.GATED:
+        return "leap_gated_linear8", (P, P, rows, cols, P, cols, out, P, P, P, P, P, 0)
+    if what in (K.GRAD_X, K.GRAD_X_FULL, K.GRAD_WEIGHT):
+        weight = what == K.GRAD_WEIGHT
+        return "leap_linear8_backward", (P, out, P, P, rows, cols, P, cols, out, None if weight else P, 0 if what == K.GRAD_X_FULL else 1, P if weight else None, P, 0)
+    if what == K.GATE_GRAD:
+        return "leap_linear_gate8_backward", (P, out, P, cols, out, P, P, rows, cols, P, P, 0)
+    return "leap_feed_forward8_backward_fine", (P, out, None, 0, P, 1, rows, 64, P, 64, cols, P, cols, out, P, None, None, P, None, P, 0)
+
+
+def test_sizes_take_the_kernels_they_are_there_for():
+    """And every kernel of the product is there: one that no size takes has no test of its values (test_gpu_activation_kernels.py)."""
+    taken = set()
+    for (what, rows, cols, out, parameters), (status, launches) in zip(K.CASES, record([_call(*c[:4]) for c in K.CASES])):
+        assert status == B.LEAP_OK
+        products = [launch.parameters for launch in launches if launch.kernel == "k_product"]
+        assert parameters in products, (what, rows, cols, out, products)
+        taken.add(("k_product", parameters))
+    assert taken == {k for k in kernels() if k[0] == "k_product"}
