@@ -43,6 +43,10 @@ int leap_pack8(const void *d_x, int32_t type, int64_t stride, int64_t rows, int6
 int leap_unpack8(const uint8_t *d_codes, const uint8_t *d_scales, int64_t rows, int64_t cols, void *d_out, int32_t type,
                  void *hip_stream);
 
+/* The same, but for values beyond the type's largest number (2^128, float16's from 63488 on), which become that number instead of an infinity:
+ * what was finite stays finite. */
+int leap_unpack8_finite(const uint8_t *d_codes, const uint8_t *d_scales, int64_t rows, int64_t cols, void *d_out, int32_t type, void *hip_stream);
+
 /* s = x + residual, rounded to `type` (residual NULL: s = x);  rstd = 1 / sqrt(mean over the row of s^2 + eps);
  * normed = packed s * rstd * weight;  kept = packed s, what the backward pass reads.
  * x, residual: [rows][cols] of `type` with strides; weight: [cols] of weight_type; sum: [rows][cols] of `type` or NULL;

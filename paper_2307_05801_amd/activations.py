@@ -53,8 +53,8 @@ class Packed8:
     def device(self):
         return self.codes.device
 
-    def unpack(self, dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
-        return unpack8(self, dtype)
+    def unpack(self, dtype: torch.dtype = torch.bfloat16, finite: bool = False) -> torch.Tensor:
+        return unpack8(self, dtype, finite)
 
     def __repr__(self):
         return f"Packed8(shape={tuple(self.shape)}, device={self.device})"
@@ -190,9 +190,9 @@ def pack8(x: torch.Tensor) -> Packed8:
     return p
 
 
-def unpack8(packed: Packed8, dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
+def unpack8(packed: Packed8, dtype: torch.dtype = torch.bfloat16, finite: bool = False) -> torch.Tensor:
     """The values held; bfloat16 and float32 hold them exactly (but for 2^128, to which float32's largest numbers round and which is
-    infinity there), float16 those between 2^-14 and 65504."""
+    infinity there), float16 those between 2^-14 and 65504.  finite: what is beyond the type's largest number becomes that instead of an infinity."""
     kind = _TYPES.get(dtype)
     if kind is None:
         raise ValueError(f"dtype must be float32, bfloat16 or float16, not {dtype}")
@@ -200,7 +200,7 @@ def unpack8(packed: Packed8, dtype: torch.dtype = torch.bfloat16) -> torch.Tenso
     _on_gpu(codes, "packed")
     rows, cols, _ = _rows(codes, "packed")
     out = _like(codes, dtype)
-    _call("leap_unpack8", codes.device, codes.data_ptr(), packed.scales.data_ptr(), rows, cols, out.data_ptr(), kind)
+    _call("leap_unpack8_finite" if finite else "leap_unpack8", codes.device, codes.data_ptr(), packed.scales.data_ptr(), rows, cols, out.data_ptr(), kind)
     return out
 
 
@@ -220,7 +220,7 @@ def _unpack_flat(parts, shape, dtype: torch.dtype) -> torch.Tensor:
     to = out.data_ptr()
     for p in parts:
         rows, cols, _ = _rows(p.codes, "packed")
-        _call("leap_unpack8", p.device, p.codes.data_ptr(), p.scales.data_ptr(), rows, cols, to, _TYPES[dtype])
+        _call("leap_unpack8_finite", p.device, p.codes.data_ptr(), p.scales.data_ptr(), rows, cols, to, _TYPES[dtype])
         to += rows * cols * dtype.itemsize
     return out
 
@@ -229,7 +229,8 @@ class keep_in_8_bits(torch.autograd.graph.saved_tensors_hooks):
     """Inside this context what autograd saves for the backward pass is kept packed: plain tensors on a GPU of float32, bfloat16 or
     float16 with at least `min_values` values and evenly spaced rows (no gaps, where they have more than 2^20 columns).  Leaves that want a gradient (weights) and everything
     else are kept as they are; a weight's cast or slice is no leaf: keep its use outside.  The gradients are those of the values held
-    (3 mantissa bits)."""
+    (3 mantissa bits).  What is finite stays so (a mask's lowest number too); infinities come back as NaN: operations that save a tensor masked with
+    them (logsumexp of -inf) belong outside."""
 
     def __init__(self, min_values: int = 1 << 16):
         # What is kept as it is is kept detached: an output that its own operation saves would hold its graph, and that the output.
@@ -252,7 +253,7 @@ class keep_in_8_bits(torch.autograd.graph.saved_tensors_hooks):
         def unpack(kept):
             held, known = kept
             if isinstance(held, Packed8):
-                return held.unpack(known)
+                return held.unpack(known, finite=True)
             if isinstance(held, list):
                 return _unpack_flat(held, *known)
             if held._version != known:

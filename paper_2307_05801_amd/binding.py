@@ -27,6 +27,7 @@ _P, _I, _L = C.c_void_p, C.c_int32, C.c_int64
 ACTIVATION_EXPORTS = {                                       # name: (result, arguments)
     "leap_pack8": (C.c_int, [_P, _I, _L, _L, _L, _P, _P, _P]),
     "leap_unpack8": (C.c_int, [_P, _P, _L, _L, _P, _I, _P]),
+    "leap_unpack8_finite": (C.c_int, [_P, _P, _L, _L, _P, _I, _P]),
     "leap_rms_norm8": (C.c_int, [_P, _L, _P, _L, _I, _P, _I, _L, _L, C.c_float] + [_P] * 7),
     "leap_rms_norm8_work": (_L, [_L, _L]),
     "leap_rms_norm8_backward": (C.c_int, [_P, _I, _L, _P, _L, _I, _P, _P, _P, _P, _I, _L, _L, _P, _P, _P, _P]),

@@ -29,16 +29,19 @@ template <int TYPE> struct element;
 template <> struct element<LEAP_F32> {
     using raw = float;
     static __device__ float to_float(raw v) { return v; }
+    static constexpr float LARGEST = 0x1.fffffep127f;
     static __device__ raw from_float(float v) { return v; }
 };
 template <> struct element<LEAP_BF16> {
     using raw = uint16_t;
     static __device__ float to_float(raw v) { return __uint_as_float((uint32_t)v << 16); }
+    static constexpr float LARGEST = 0x1.fep127f;
     static __device__ raw from_float(float v) { return __builtin_bit_cast(uint16_t, (__bf16)v); }
 };
 template <> struct element<LEAP_F16> {
     using raw = uint16_t;
     static __device__ float to_float(raw v) { return (float)__builtin_bit_cast(_Float16, v); }
+    static constexpr float LARGEST = 65504.0f;
     static __device__ raw from_float(float v) { return __builtin_bit_cast(uint16_t, (_Float16)v); }
 };
 

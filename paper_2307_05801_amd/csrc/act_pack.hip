@@ -39,10 +39,11 @@ __global__ __launch_bounds__(BLOCK) void k_pack(const void *__restrict__ x, int6
     for (int k = 0; k < EACH; ++k) pack_chunk(v[k], n[k], codes, scales, row[k], P.cols, P.groups, col[k], P.past);
 }
 
-// A lane writes 16 bytes, so that neighbouring lanes write whole lines: eight values of 16 bits, four of 32.
+// A lane writes 16 bytes, so that neighbouring lanes write whole lines: eight values of 16 bits, four of 32.  finite: infinities, which nothing but
+// the type's range makes (those packed are NaN), become its largest number.
 template <int TYPE, int EACH>
 __global__ __launch_bounds__(BLOCK) void k_unpack(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scales, rows_part P,
-                                                  void *__restrict__ out)
+                                                  void *__restrict__ out, bool finite)
 {
     constexpr int N = 16 / sizeof(typename element<TYPE>::raw);
     uint32_t c[EACH][2] = {};
@@ -74,6 +75,11 @@ __global__ __launch_bounds__(BLOCK) void k_unpack(const uint8_t *__restrict__ co
     for (int k = 0; k < EACH; ++k) {
         float v[CHUNK];
         decode8(make_uint2(c[k][0], c[k][1]), scale_value(byte[k]), v);
+        if (finite) {
+            constexpr float LARGEST = element<TYPE>::LARGEST;
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] = v[i] > LARGEST ? LARGEST : v[i] < -LARGEST ? -LARGEST : v[i];
+        }
         typename element<TYPE>::raw *to = (typename element<TYPE>::raw *)out + at[k], raw[N];
 #pragma unroll
         for (int i = 0; i < N; ++i) raw[i] = element<TYPE>::from_float(v[i]);
@@ -119,8 +125,9 @@ extern "C" int leap_pack8(const void *d_x, int32_t type, int64_t stride, int64_t
     });
 }
 
-extern "C" int leap_unpack8(const uint8_t *d_codes, const uint8_t *d_scales, int64_t rows, int64_t cols, void *d_out, int32_t type,
-                            void *hip_stream)
+namespace {
+
+int unpack(const uint8_t *d_codes, const uint8_t *d_scales, int64_t rows, int64_t cols, void *d_out, int32_t type, bool finite, void *hip_stream)
 {
     if (!known_type(type)) return refuse("unknown element type");
     if (const char *why = bad_sizes(rows, cols)) return refuse(why);
@@ -129,7 +136,21 @@ extern "C" int leap_unpack8(const uint8_t *d_codes, const uint8_t *d_scales, int
     return by_type(type, [&](auto t) {
         constexpr int EACH = 2, N = 16 / sizeof(typename element<decltype(t)::value>::raw);
         return over_rows<EACH, N>(rows, cols, 16 / N, [&](const rows_part &P, uint32_t blocks) {
-            hipLaunchKernelGGL((k_unpack<decltype(t)::value, EACH>), dim3(blocks), dim3(BLOCK), 0, stream_of(hip_stream), d_codes, d_scales, P, d_out);
+            hipLaunchKernelGGL((k_unpack<decltype(t)::value, EACH>), dim3(blocks), dim3(BLOCK), 0, stream_of(hip_stream), d_codes, d_scales, P, d_out, finite);
         });
     });
+}
+
+}  // namespace
+
+extern "C" int leap_unpack8(const uint8_t *d_codes, const uint8_t *d_scales, int64_t rows, int64_t cols, void *d_out, int32_t type,
+                            void *hip_stream)
+{
+    return unpack(d_codes, d_scales, rows, cols, d_out, type, false, hip_stream);
+}
+
+extern "C" int leap_unpack8_finite(const uint8_t *d_codes, const uint8_t *d_scales, int64_t rows, int64_t cols, void *d_out, int32_t type,
+                                   void *hip_stream)
+{
+    return unpack(d_codes, d_scales, rows, cols, d_out, type, true, hip_stream);
 }

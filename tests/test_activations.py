@@ -363,3 +363,12 @@ def test_a_block_without_a_backward_pass(lib):
     assert lib.leap_feed_forward8_alone_work(4, 64, P, 65, 16, P, 16, 24) == 256 + 16 + 64 + 16 + 32 * 64 * 2
     assert lib.leap_feed_forward8_alone_work(4, 64, P, 64, 16, P, 16, 0) == 0 and lib.leap_feed_forward8_alone_work(-1, 64, P, 64, 16, P, 16, 8) == 0
     assert lib.leap_feed_forward8_alone(None, 64, None, 64, None, 1, 0, 64, 1e-6, None, 64, 8, None, 8, 16, *[None] * 4) == B.LEAP_OK
+
+
+def test_bad_arguments_of_finite_unpacking_are_refused_with_a_message(lib):
+    for at, value in [(5, 9), (2, -1), (3, 0), (3, 1 << 21), (0, 0), (1, 0), (4, 0)]:
+        arguments = [P, P, 4, 64, P, 1, 0]
+        arguments[at] = value
+        assert lib.leap_unpack8_finite(*arguments) == B.LEAP_INVALID_ARG, (at, value)
+        assert lib.leap_last_error()
+    assert lib.leap_unpack8_finite(None, None, 0, 64, None, 0, None) == B.LEAP_OK

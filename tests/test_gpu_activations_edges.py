@@ -220,3 +220,26 @@ def test_norm_gradient_without_the_weights(A, cols):  # noqa: F811
     want, _ = A.rms_norm8_backward(x, kept, rstd, w)
     got, none = A.rms_norm8_backward(x, kept, rstd, w, need_weight=False)
     assert none is None and torch.equal(got, want)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, torch.float16])
+def test_the_types_lowest_number_stays_finite(A, dtype):  # noqa: F811
+    """As a mask has it: its product with a gradient of zero is zero, not NaN.  Infinities and NaN are still held as NaN."""
+    info = torch.finfo(dtype)
+    x = torch.randn(300, 300, device="cuda", generator=torch.Generator(device="cuda").manual_seed(331)).to(dtype)
+    x[::2, 5::7] = info.min
+    x[1::2, 3::5] = info.max
+    x[7, 9], x[8, 290], x[9, 0] = float("inf"), float("-inf"), float("nan")
+    lost = ~torch.isfinite(x)
+    held = R.values(*R.pack(x.cpu())).cuda()
+    want = held.clamp(info.min, info.max).to(dtype)                   # NaN stays NaN
+    for back in (A.pack8(x).unpack(dtype, finite=True), _kept(A, lambda: x)[1]):
+        assert torch.equal(torch.isnan(back), lost) and torch.equal(back[~lost], want[~lost]) and torch.isfinite(back[~lost]).all()
+    assert torch.isinf(A.pack8(x).unpack(dtype)[~lost]).any()
+    x = x.nan_to_num(0.0, 0.0, 0.0)
+    scale = torch.ones(300, 300, dtype=dtype, device="cuda", requires_grad=True)
+    with A.keep_in_8_bits():
+        value = torch.where(x == info.min, 0.0, (x * scale)).float()
+    assert torch.isfinite(torch.autograd.grad(value, scale, torch.zeros_like(value))[0]).all()
+    long = torch.full(((1 << 20) + 5,), info.min, dtype=dtype, device="cuda")
+    assert torch.equal(_kept(A, lambda: long)[1], long)
