@@ -83,6 +83,15 @@ int leap_linear8_backward(const void *d_dy, int64_t dy_stride, const uint8_t *d_
                           const void *d_weight, int64_t w_stride, int64_t out, void *d_grad_x, int32_t grad_x_type,
                           void *d_grad_weight, void *d_work, void *hip_stream);
 
+/* A fine gradient [rows][out] is the sum of two arrays of bfloat16, which holds it to 2^-17 of a value (bfloat16: 2^-9): its values rounded, and
+ * what their rounding leaves.  They lie side by side: with P = out, up to a multiple of 8, a row is 2 * P long and has out values, zeros up to P, what
+ * is left of each, and zeros; rows follow one another without gaps, from a multiple of 16 bytes on.  The same gradients as above from such a dy: products
+ * take twice as long. */
+int64_t leap_linear8_backward_fine_work(const uint8_t *d_codes, int64_t rows, int64_t cols, const void *d_weight, int64_t w_stride, int64_t out);
+int leap_linear8_backward_fine(const void *d_dy, const uint8_t *d_codes, const uint8_t *d_scales, int64_t rows, int64_t cols, const void *d_weight,
+                               int64_t w_stride, int64_t out, void *d_grad_x, int32_t grad_x_type, void *d_grad_weight, void *d_work,
+                               void *hip_stream);
+
 /* The gated product.  u = v W^T in 32 bits with W [2 * out][cols], the gate's rows first: u = (g, p);
  * gated = packed g * sigmoid(g) * p, [rows][out];  kept = packed u as [rows][2][out] (the groups of the two halves apart), or
  * NULL.  d_work: leap_linear8_work() of this weight with its 2 * out rows. */
@@ -99,8 +108,7 @@ int leap_gated_linear8_backward(const void *d_da, int64_t da_stride, const uint8
                                 int64_t w_stride, int64_t out, void *d_grad_x, int32_t grad_x_type, void *d_grad_weight, void *d_work,
                                 void *hip_stream);
 
-/* The same with du held as the sum of two bfloat16, to 2^-17 of a value (2^-9 above), so that grad_x and grad_weight are rounded once, at the end;
- * the products take twice as long, and du twice the room. */
+/* The same with a fine du, so that grad_x and grad_weight are rounded once, at the end; the products take twice as long, and du twice the room. */
 int64_t leap_gated_linear8_backward_fine_work(const uint8_t *d_codes, int64_t rows, int64_t cols, const void *d_weight, int64_t w_stride, int64_t out);
 int leap_gated_linear8_backward_fine(const void *d_da, int64_t da_stride, const uint8_t *d_kept_codes, const uint8_t *d_kept_scales,
                                      const uint8_t *d_codes, const uint8_t *d_scales, int64_t rows, int64_t cols, const void *d_weight,
@@ -118,6 +126,13 @@ int64_t leap_linear_gate8_work(const void *d_dy, int64_t dy_stride, const void *
 int leap_linear_gate8_backward(const void *d_dy, int64_t dy_stride, const void *d_weight, int64_t w_stride, int64_t next,
                                const uint8_t *d_kept_codes, const uint8_t *d_kept_scales, int64_t rows, int64_t out, void *d_du,
                                void *d_work, void *hip_stream);
+
+/* The same to a fine du (of 2 * out values a row, from a multiple of 16 bytes on). */
+int leap_gate8_backward_fine(const void *d_da, int64_t da_stride, const uint8_t *d_kept_codes, const uint8_t *d_kept_scales, int64_t rows,
+                             int64_t out, void *d_du, void *hip_stream);
+int leap_linear_gate8_backward_fine(const void *d_dy, int64_t dy_stride, const void *d_weight, int64_t w_stride, int64_t next,
+                                    const uint8_t *d_kept_codes, const uint8_t *d_kept_scales, int64_t rows, int64_t out, void *d_du,
+                                    void *d_work, void *hip_stream);
 
 /* A feed-forward block of these, as one call:  s = x + residual (NULL: s = x);  y [rows][out] = gated(norm(s) up^T) down^T, with up
  * [2 * hidden][cols] and down [out][hidden], their rows up_stride and down_stride apart, everything plain in bfloat16 (the norm's
@@ -147,8 +162,7 @@ int leap_feed_forward8_backward(const void *d_dy, int64_t dy_stride, const void 
                                 const void *d_down, int64_t down_stride, int64_t out, const void *d_kept, void *d_grad_x,
                                 void *d_grad_norm_weight, void *d_grad_up, void *d_grad_down, void *d_work, void *hip_stream);
 
-/* The same with du, the gradient of the product with `up`, held as the sum of two bfloat16 (leap_gated_linear8_backward_fine says what that
- * takes and gives). */
+/* The same with a fine du, the gradient of the product with `up` (leap_gated_linear8_backward_fine says what that takes and gives). */
 int64_t leap_feed_forward8_backward_fine_work(const void *d_dy, int64_t dy_stride, int64_t rows, int64_t cols, const void *d_up, int64_t up_stride,
                                               int64_t hidden, const void *d_down, int64_t down_stride, int64_t out);
 int leap_feed_forward8_backward_fine(const void *d_dy, int64_t dy_stride, const void *d_grad_sum, int64_t grad_sum_stride, const void *d_norm_weight,

@@ -60,6 +60,45 @@ class Packed8:
         return f"Packed8(shape={tuple(self.shape)}, device={self.device})"
 
 
+class FineGradient:
+    """A gradient as the sum of two tensors of bfloat16, to 2^-17 of a value: `rounded`, and `rest`, what the rounding leaves.  gate8_backward and
+    linear_gate8_backward make it, linear8_backward takes it; float() and its like give a tensor."""
+
+    __slots__ = ("memory", "shape")
+
+    def __init__(self, shape, device):
+        self.shape = torch.Size(shape)
+        # both parts of a row side by side, each up to a multiple of 16 bytes (include/leap_activations.h)
+        self.memory = torch.empty((*shape[:-1], 2, -(-shape[-1] // 8) * 8), dtype=torch.bfloat16, device=device)
+
+    @property
+    def device(self):
+        return self.memory.device
+
+    @property
+    def rounded(self) -> torch.Tensor:
+        return self.memory[..., 0, :self.shape[-1]]
+
+    @property
+    def rest(self) -> torch.Tensor:
+        return self.memory[..., 1, :self.shape[-1]]
+
+    def float(self) -> torch.Tensor:
+        return self.rounded.float() + self.rest.float()
+
+    def double(self) -> torch.Tensor:
+        return self.float().double()
+
+    def cpu(self) -> torch.Tensor:
+        return self.float().cpu()
+
+    def detach(self):
+        return self                                           # it has no graph
+
+    def __repr__(self):
+        return f"FineGradient(shape={tuple(self.shape)}, device={self.device})"
+
+
 def _not_recorded(*tensors) -> None:
     """The results have no graph: silently without one they would train with a part of the gradient."""
     if torch.is_grad_enabled():
@@ -344,19 +383,28 @@ def linear8(x: Packed8, weight: torch.Tensor) -> torch.Tensor:
     return y
 
 
-def linear8_backward(grad: torch.Tensor, x: Packed8, weight: torch.Tensor, need_x: bool = True, need_weight: bool = True,
+def linear8_backward(grad, x: Packed8, weight: torch.Tensor, need_x: bool = True, need_weight: bool = True,
                      dtype: torch.dtype = torch.bfloat16):
-    """(grad_x, grad_weight): dy W (bfloat16, or float32 by `dtype`) and dy^T x (bfloat16); None for one that is not needed."""
-    _not_recorded(grad)
+    """(grad_x, grad_weight): dy W (bfloat16, or float32 by `dtype`) and dy^T x (bfloat16); None for one that is not needed.
+    grad: bfloat16, or a FineGradient, whose products take twice as long."""
+    fine = type(grad) is FineGradient
+    if not fine:
+        _not_recorded(grad)
     rows, cols = _packed_rows(x)
     out, w_stride = _weight(weight, cols, x.device)
-    _, _, stride = _gradient(grad, x.shape[:-1] + (out,), x.device, (torch.bfloat16,), "grad")
+    if fine:
+        if grad.shape != x.shape[:-1] + (out,) or grad.device != x.device:
+            raise ValueError(f"grad {tuple(grad.shape)} is not of this x {tuple(x.shape)} and weight {tuple(weight.shape)}, or on another device")
+    else:
+        _, _, stride = _gradient(grad, x.shape[:-1] + (out,), x.device, (torch.bfloat16,), "grad")
     if dtype not in (torch.bfloat16, torch.float32):
         raise ValueError("grad_x is bfloat16 or float32")
     grad_x = _like(x.codes, dtype) if need_x else None
     grad_weight = _like(weight, torch.bfloat16) if need_weight else None
-    work = _work("leap_linear8_backward_work", x.device, grad.data_ptr(), stride, x.codes.data_ptr(), rows, cols, weight.data_ptr(), w_stride, out)
-    _call("leap_linear8_backward", x.device, grad.data_ptr(), stride, x.codes.data_ptr(), x.scales.data_ptr(), rows, cols, weight.data_ptr(),
+    name, dy = ("leap_linear8_backward_fine", ()) if fine else ("leap_linear8_backward", (stride,))
+    address = grad.memory.data_ptr() if fine else grad.data_ptr()
+    work = _work(name + "_work", x.device, *(() if fine else (address, stride)), x.codes.data_ptr(), rows, cols, weight.data_ptr(), w_stride, out)
+    _call(name, x.device, address, *dy, x.codes.data_ptr(), x.scales.data_ptr(), rows, cols, weight.data_ptr(),
           w_stride, out, _address(grad_x), _TYPES[dtype], _address(grad_weight), _address(work))
     return grad_x, grad_weight
 
@@ -391,34 +439,40 @@ def _kept_halves(kept: Packed8):
     return shape[:-2], shape[-1]
 
 
-def gate8_backward(grad: torch.Tensor, kept: Packed8) -> torch.Tensor:
-    """du [..., 2 * outputs] (bfloat16), the gradient of gated_linear8's u, from that of `gated`."""
+def _empty_du(shape, device, fine: bool):
+    """(du, its address) to be written."""
+    du = FineGradient(shape, device) if fine else torch.empty(shape, dtype=torch.bfloat16, device=device)
+    return du, (du.memory if fine else du).data_ptr()
+
+
+def gate8_backward(grad: torch.Tensor, kept: Packed8, fine: bool = True):
+    """du [..., 2 * outputs], the gradient of gated_linear8's u, from that of `gated`: a FineGradient, or with fine=False rounded to bfloat16."""
     _not_recorded(grad)
     lead, out = _kept_halves(kept)
     rows, _, stride = _gradient(grad, lead + (out,), kept.device, (torch.bfloat16,), "grad")
-    du = torch.empty(lead + (2 * out,), dtype=torch.bfloat16, device=kept.device)
-    _call("leap_gate8_backward", kept.device, grad.data_ptr(), stride, kept.codes.data_ptr(), kept.scales.data_ptr(), rows, out, du.data_ptr())
+    du, address = _empty_du(lead + (2 * out,), kept.device, fine)
+    _call("leap_gate8_backward_fine" if fine else "leap_gate8_backward", kept.device, grad.data_ptr(), stride, kept.codes.data_ptr(), kept.scales.data_ptr(),
+          rows, out, address)
     return du
 
 
-def linear_gate8_backward(grad: torch.Tensor, weight: torch.Tensor, kept: Packed8) -> torch.Tensor:
+def linear_gate8_backward(grad: torch.Tensor, weight: torch.Tensor, kept: Packed8, fine: bool = True):
     """gate8_backward of grad W, which stays in 32 bits: du from the gradient of the product linear8(gated, weight)."""
     _not_recorded(grad)
     lead, out = _kept_halves(kept)
     following, w_stride = _weight(weight, out, kept.device)
     rows, _, stride = _gradient(grad, lead + (following,), kept.device, (torch.bfloat16,), "grad")
-    du = torch.empty(lead + (2 * out,), dtype=torch.bfloat16, device=kept.device)
+    du, address = _empty_du(lead + (2 * out,), kept.device, fine)
     work = _work("leap_linear_gate8_work", kept.device, grad.data_ptr(), stride, weight.data_ptr(), w_stride, following, rows, out)
-    _call("leap_linear_gate8_backward", kept.device, grad.data_ptr(), stride, weight.data_ptr(), w_stride, following, kept.codes.data_ptr(),
-          kept.scales.data_ptr(), rows, out, du.data_ptr(), _address(work))
+    _call("leap_linear_gate8_backward_fine" if fine else "leap_linear_gate8_backward", kept.device, grad.data_ptr(), stride, weight.data_ptr(), w_stride, following, kept.codes.data_ptr(),
+          kept.scales.data_ptr(), rows, out, address, _address(work))
     return du
 
 
 def gated_linear8_backward(grad: torch.Tensor, kept: Packed8, x: Packed8, weight: torch.Tensor, need_x: bool = True, need_weight: bool = True,
-                           fine: bool = False):
-    """(grad_x, grad_weight) of gated_linear8 from the gradient of `gated` (bfloat16).  In between is du, the gradient of u: in bfloat16
-    (the results are 0.0024 of their norm off, 0.0017 of it their own rounding), or, fine, as the sum of two, so that the results' rounding is the only
-    one; the products take twice as long."""
+                           fine: bool = True):
+    """(grad_x, grad_weight) of gated_linear8 from the gradient of `gated` (bfloat16).  In between is du, the gradient of u, a FineGradient, so that
+    the results' rounding is the only one (0.0017 of their norm); with fine=False it is bfloat16 (0.0024), which the products take in half the time."""
     _not_recorded(grad)
     if kept.shape[:-2] != x.shape[:-1]:
         raise ValueError(f"kept {tuple(kept.shape)} is not of this x {tuple(x.shape)}")
@@ -497,11 +551,12 @@ class _FeedForward8(torch.autograd.Function):
 
 
 def feed_forward8(x: torch.Tensor, norm_weight: torch.Tensor, up: torch.Tensor, down: torch.Tensor, residual: torch.Tensor = None,
-                  eps: float = 1e-6, fine: bool = False):
+                  eps: float = 1e-6, fine: bool = True):
     """(y, sum), differentiable: sum = x + residual and y = linear8(gated_linear8(rms_norm8(sum), up), down).  x, residual: bfloat16
     [..., columns]; up: [2 * hidden, columns], the gate's rows first; down: [outputs, hidden].  For a stack of blocks y and sum are the next one's
     x and residual.  Kept for the backward pass, if there is one to come: the norm's output, sum and the hidden rows (three times), all in 8 bits.
-    fine: the gradient of up's product is not rounded to bfloat16 on its way to the gradients of x, norm_weight and up (gated_linear8_backward)."""
+    fine=False: the gradient of up's product is rounded to bfloat16 on its way to the gradients of x, norm_weight and up, whose products then take half
+    the time (gated_linear8_backward says how far off they are)."""
     _on_gpu(x, "x")
     if x.dtype is not torch.bfloat16:
         raise ValueError(f"x must be bfloat16, not {x.dtype}")
@@ -514,7 +569,7 @@ def feed_forward8(x: torch.Tensor, norm_weight: torch.Tensor, up: torch.Tensor, 
 class FeedForward8(torch.nn.Module):
     """feed_forward8 with weights of its own (bfloat16): (x, residual) -> (y, sum)."""
 
-    def __init__(self, columns: int, hidden: int, eps: float = 1e-6, device="cuda:0", fine: bool = False):
+    def __init__(self, columns: int, hidden: int, eps: float = 1e-6, device="cuda:0", fine: bool = True):
         super().__init__()
         self.eps, self.fine = eps, fine
         self.norm_weight = torch.nn.Parameter(torch.ones(columns, dtype=torch.bfloat16, device=device))

@@ -35,6 +35,8 @@ ACTIVATION_EXPORTS = {                                       # name: (result, ar
     "leap_linear8_work": (_L, [_P, _L, _L, _P, _L, _L]),
     "leap_linear8_backward_work": (_L, [_P, _L, _P, _L, _L, _P, _L, _L]),
     "leap_linear8_backward": (C.c_int, [_P, _L, _P, _P, _L, _L, _P, _L, _L, _P, _I, _P, _P, _P]),
+    "leap_linear8_backward_fine_work": (_L, [_P, _L, _L, _P, _L, _L]),
+    "leap_linear8_backward_fine": (C.c_int, [_P, _P, _P, _L, _L, _P, _L, _L, _P, _I, _P, _P, _P]),
     "leap_gated_linear8": (C.c_int, [_P, _P, _L, _L, _P, _L, _L, _P, _P, _P, _P, _P, _P]),
     "leap_gated_linear8_backward_work": (_L, [_P, _L, _L, _P, _L, _L]),
     "leap_gated_linear8_backward": (C.c_int, [_P, _L, _P, _P, _P, _P, _L, _L, _P, _L, _L, _P, _I, _P, _P, _P]),
@@ -43,6 +45,8 @@ ACTIVATION_EXPORTS = {                                       # name: (result, ar
     "leap_gate8_backward": (C.c_int, [_P, _L, _P, _P, _L, _L, _P, _P]),
     "leap_linear_gate8_work": (_L, [_P, _L, _P, _L, _L, _L, _L]),
     "leap_linear_gate8_backward": (C.c_int, [_P, _L, _P, _L, _L, _P, _P, _L, _L, _P, _P, _P]),
+    "leap_gate8_backward_fine": (C.c_int, [_P, _L, _P, _P, _L, _L, _P, _P]),
+    "leap_linear_gate8_backward_fine": (C.c_int, [_P, _L, _P, _L, _L, _P, _P, _L, _L, _P, _P, _P]),
     "leap_feed_forward8_kept": (_L, [_L, _L, _L]),
     "leap_feed_forward8_work": (_L, [_L, _L, _P, _L, _L, _P, _L, _L]),
     "leap_feed_forward8": (C.c_int, [_P, _L, _P, _L, _P, _I, _L, _L, C.c_float, _P, _L, _L, _P, _L, _L] + [_P] * 5),

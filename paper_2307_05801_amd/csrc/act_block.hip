@@ -138,7 +138,7 @@ namespace {
 
 int64_t block_backward_work(bool fine, const void *d_dy, int64_t dy_stride, const block_sizes &S)
 {
-    return S.bad() || bad_stride(dy_stride, S.rows, S.out) ? 0 : S.backward_work(d_dy, dy_stride, du_in_workspace(S.hidden, fine));
+    return S.bad() || bad_stride(dy_stride, S.rows, S.out) ? 0 : S.backward_work(d_dy, dy_stride, padded_layout(S.hidden, fine));
 }
 
 int block_backward(bool fine, const void *d_dy, int64_t dy_stride, const void *d_grad_sum, int64_t grad_sum_stride, const void *d_norm_weight,
@@ -156,10 +156,10 @@ int block_backward(bool fine, const void *d_dy, int64_t dy_stride, const void *d
     if (rows && d_grad_norm_weight && !d_grad_x) return refuse("the norm's weight gradient comes with grad_x");
     if (unaligned(d_work)) return refuse(NO_WORK);
     const kept_block K((void *)d_kept, rows, cols, hidden, true);
-    // du is bfloat16, which the matrix units take: grad_up is 0.0024 of its norm off, grad_norm_weight 0.0024 to 0.0034, where 0.0017 are their own
-    // rounding to bfloat16.  A caller who wants that alone asks for a fine du, whose products take twice as long (262144 x 512 through 1024, forward and
-    // backward: 4.79 ms, 3.53).  32 bits between the product and the norm: a rounding less in grad_x.
-    const du_layout L = du_in_workspace(hidden, fine);
+    // The matrix units take bfloat16.  A fine du is two of those, and its products take twice as long (262144 x 512 through 1024, forward and backward:
+    // 4.79 ms, 3.53); all gradients are 0.0017 of their norm off, their own rounding.  With du rounded, which a caller may ask for, grad_up is 0.0024
+    // off and grad_norm_weight 0.0024 to 0.0034.  32 bits between the product and the norm: a rounding less in grad_x.
+    const du_layout L = padded_layout(hidden, fine);
     uint8_t *const du = (uint8_t *)d_work, *const dn = du + L.bytes(rows), *const work = dn + S.dn_bytes();
     int rc = LEAP_OK;
     if (d_grad_down)

@@ -302,13 +302,12 @@ template <class F> inline int by_type(int32_t type, F &&f)
 // Values from one row to the next where rows of bfloat16 are followed by zeros up to a multiple of 16 bytes: such rows are not laid out anew.
 inline int64_t padded_row(int64_t cols) { return (cols + 7) / 8 * 8; }
 
-// How du [rows][2 * out] lies: in bfloat16, rows `stride` apart with zeros between them; or, fine, as the sum of two such arrays side by side,
-// the rounded values and what their rounding leaves, which is du to 2^-17 of each value.
+// How du [rows][2 * out] lies: in bfloat16, rows `stride` apart with zeros between them; or, fine, as two such arrays side by side.
 struct du_layout {
     int64_t low, stride;               // values from one of du to its rest (0: none); from row to row
     __host__ __device__ int64_t bytes(int64_t rows) const { return rows * stride * 2; }
 };
-inline du_layout du_in_workspace(int64_t out, bool fine) { return {fine ? padded_row(2 * out) : 0, padded_row(2 * out) * (fine ? 2 : 1)}; }
+inline du_layout padded_layout(int64_t out, bool fine) { return {fine ? padded_row(2 * out) : 0, padded_row(2 * out) * (fine ? 2 : 1)}; }
 
 // leap_linear8_backward of a du that lies like that, and leap_linear_gate8_backward to one; `out`: of the weight's rows, twice the gate's.
 int64_t du_backward_work(const du_layout &L, const uint8_t *d_codes, int64_t rows, int64_t cols, const void *d_weight, int64_t w_stride, int64_t out);

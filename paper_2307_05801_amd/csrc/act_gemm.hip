@@ -281,6 +281,7 @@ const char *bad_product(int64_t rows, int64_t cols, int64_t w_stride, int64_t ou
     return bad_stride(w_stride, out, cols);
 }
 
+constexpr const char *NO_FINE = "a fine gradient needs memory from a multiple of 16 bytes on";
 constexpr const char *GATED_LIMIT = "more than 2^19 gated columns";
 
 }  // namespace
@@ -400,6 +401,20 @@ extern "C" int leap_linear8_backward(const void *d_dy, int64_t dy_stride, const 
                     hip_stream);
 }
 
+extern "C" int64_t leap_linear8_backward_fine_work(const uint8_t *d_codes, int64_t rows, int64_t cols, const void *d_weight, int64_t w_stride, int64_t out)
+{
+    return act::du_backward_work({padded_row(out), 2 * padded_row(out)}, d_codes, rows, cols, d_weight, w_stride, out);
+}
+
+extern "C" int leap_linear8_backward_fine(const void *d_dy, const uint8_t *d_codes, const uint8_t *d_scales, int64_t rows, int64_t cols, const void *d_weight,
+                                          int64_t w_stride, int64_t out, void *d_grad_x, int32_t grad_x_type, void *d_grad_weight, void *d_work,
+                                          void *hip_stream)
+{
+    if (rows && unaligned(d_dy)) return refuse(NO_FINE);
+    return act::du_backward(d_dy, {padded_row(out), 2 * padded_row(out)}, d_codes, d_scales, rows, cols, d_weight, w_stride, out, d_grad_x, grad_x_type,
+                            d_grad_weight, d_work, hip_stream);
+}
+
 extern "C" int leap_gated_linear8(const uint8_t *d_codes, const uint8_t *d_scales, int64_t rows, int64_t cols, const void *d_weight, int64_t w_stride,
                                   int64_t out, uint8_t *d_gated_codes, uint8_t *d_gated_scales, uint8_t *d_kept_codes, uint8_t *d_kept_scales,
                                   void *d_work, void *hip_stream)
@@ -443,12 +458,19 @@ extern "C" int leap_gate8_backward(const void *d_da, int64_t da_stride, const ui
     return gate_backward(d_da, da_stride, d_kept_codes, d_kept_scales, rows, out, d_du, du_layout{0, 2 * out}, hip_stream);
 }
 
+extern "C" int leap_gate8_backward_fine(const void *d_da, int64_t da_stride, const uint8_t *d_kept_codes, const uint8_t *d_kept_scales, int64_t rows,
+                                        int64_t out, void *d_du, void *hip_stream)
+{
+    if (rows && unaligned(d_du)) return refuse(NO_FINE);
+    return gate_backward(d_da, da_stride, d_kept_codes, d_kept_scales, rows, out, d_du, padded_layout(out, true), hip_stream);
+}
+
 namespace {
 
 int64_t gated_backward_work(bool fine, const uint8_t *d_codes, int64_t rows, int64_t cols, const void *d_weight, int64_t w_stride, int64_t out)
 {
     if (out > MOST_COLS / 2 || out < 1 || bad_product(rows, cols, w_stride, 2 * out)) return 0;
-    const du_layout L = du_in_workspace(out, fine);
+    const du_layout L = padded_layout(out, fine);
     return L.bytes(rows) + act::du_backward_work(L, d_codes, rows, cols, d_weight, w_stride, 2 * out);
 }
 
@@ -463,9 +485,9 @@ int gated_backward(bool fine, const void *d_da, int64_t da_stride, const uint8_t
     if (rows && (!d_codes || !d_scales || !d_weight)) return refuse("null data pointer");
     if (rows && unaligned(d_work)) return refuse(NO_WORK);
     if (!d_grad_x && !d_grad_weight) return LEAP_OK;
-    // du is bfloat16, which the matrix units take: the results are 0.0024 of their norm off, of which their own rounding to bfloat16 is 0.0017.
-    // A caller who wants that alone asks for a fine du, whose products take twice as long (262144 x 512 -> 2 * 1024 forward and backward: 3.47 ms, 2.25).
-    const du_layout L = du_in_workspace(out, fine);
+    // The matrix units take bfloat16.  A fine du is two of those, and its products take twice as long (262144 x 512 -> 2 * 1024 forward and backward:
+    // 3.47 ms, 2.25); the results are 0.0017 of their norm off, their own rounding to bfloat16.  With du rounded, which a caller may ask for, 0.0024.
+    const du_layout L = padded_layout(out, fine);
     const int rc = gate_backward(d_da, da_stride, d_kept_codes, d_kept_scales, rows, out, d_work, L, hip_stream);
     if (rc != LEAP_OK) return rc;
     return act::du_backward(d_work, L, d_codes, d_scales, rows, cols, d_weight, w_stride, 2 * out, d_grad_x, grad_x_type, d_grad_weight,
@@ -545,4 +567,12 @@ extern "C" int leap_linear_gate8_backward(const void *d_dy, int64_t dy_stride, c
                                           void *d_work, void *hip_stream)
 {
     return act::linear_gate8_backward(d_dy, dy_stride, d_weight, w_stride, next, d_kept_codes, d_kept_scales, rows, out, d_du, du_layout{0, 2 * out}, d_work, hip_stream);
+}
+
+extern "C" int leap_linear_gate8_backward_fine(const void *d_dy, int64_t dy_stride, const void *d_weight, int64_t w_stride, int64_t next,
+                                               const uint8_t *d_kept_codes, const uint8_t *d_kept_scales, int64_t rows, int64_t out, void *d_du,
+                                               void *d_work, void *hip_stream)
+{
+    if (rows && unaligned(d_du)) return refuse(NO_FINE);
+    return act::linear_gate8_backward(d_dy, dy_stride, d_weight, w_stride, next, d_kept_codes, d_kept_scales, rows, out, d_du, padded_layout(out, true), d_work, hip_stream);
 }

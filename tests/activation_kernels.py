@@ -42,7 +42,7 @@ CASES = [
     (GATE_GRAD, 50000, 1024, 1152, (1, 0, 3) + SMALL),         # 205 MB: past the caches
     (GATE_GRAD, 3000, 1100, 1100, (1, 0, 3) + PAIRED),
     (GATE_GRAD, 1000, 1100, 1300, (1, 0, 3) + PAIRED_LOW),
-    (GATE_GRAD_FINE, 25000, 1100, 1029, (1, 0, 4) + SMALL),    # 220 MB: past the caches
+    (GATE_GRAD_FINE, 25000, 1024, 1152, (1, 0, 4) + SMALL),    # 205 MB: past the caches
     (GATE_GRAD_FINE, 9000, 1029, 1100, (1, 0, 4) + SMALL),
     (GATE_GRAD_FINE, 3000, 1100, 1100, (1, 0, 4) + PAIRED),
     (GATE_GRAD_FINE, 1000, 1100, 1300, (1, 0, 4) + PAIRED_LOW),

@@ -25,6 +25,7 @@ def test_a_launch_has_fewer_than_2_32_threads():
         ("leap_gate8_backward", (P, 8, P, P, rows, 8, P, 0), "k_gate_grad", -(-rows * 4 // 256)),
         ("leap_gated_linear8_backward", (P, 3, P, P, P, P, rows, 8, P, 8, 3, P, 1, P, P, 0), "k_gate_grad", -(-rows * 4 // 256)),
         ("leap_linear_gate8_backward", (P, 8, P, 8, 8, P, P, (1 << 32) + 5, 8, P, P, 0), "k_product", (1 << 25) + 1),
+        ("leap_linear_gate8_backward_fine", (P, 8, P, 8, 8, P, P, (1 << 32) + 5, 8, P, P, 0), "k_product", (1 << 25) + 1),
         ("leap_feed_forward8_backward", (P, 8, P, 8, P, 1, rows, 8, P, 8, 3, P, 3, 8, P, P, P, P, P, P, 0), "k_pad_rows", -(-rows // 256)),
     ]
     for (name, arguments, kernel, blocks), (status, launches) in zip(calls, record([c[:2] for c in calls])):
@@ -44,9 +45,7 @@ def _call(what, rows, cols, out):
     if what in (K.GRAD_X, K.GRAD_X_FULL, K.GRAD_WEIGHT):
         weight = what == K.GRAD_WEIGHT
         return "leap_linear8_backward", (P, out, P, P, rows, cols, P, cols, out, None if weight else P, 0 if what == K.GRAD_X_FULL else 1, P if weight else None, P, 0)
-    if what == K.GATE_GRAD:
-        return "leap_linear_gate8_backward", (P, out, P, cols, out, P, P, rows, cols, P, P, 0)
-    return "leap_feed_forward8_backward_fine", (P, out, None, 0, P, 1, rows, 64, P, 64, cols, P, cols, out, P, None, None, P, None, P, 0)
+    return "leap_linear_gate8_backward" + ("_fine" if what == K.GATE_GRAD_FINE else ""), (P, out, P, cols, out, P, P, rows, cols, P, P, 0)
 
 
 def test_sizes_take_the_kernels_they_are_there_for():

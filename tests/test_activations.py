@@ -372,3 +372,18 @@ def test_bad_arguments_of_finite_unpacking_are_refused_with_a_message(lib):
         assert lib.leap_unpack8_finite(*arguments) == B.LEAP_INVALID_ARG, (at, value)
         assert lib.leap_last_error()
     assert lib.leap_unpack8_finite(None, None, 0, 64, None, 0, None) == B.LEAP_OK
+
+
+def test_bad_arguments_around_a_fine_gradient_are_refused_with_a_message(lib):
+    for name, good, bad in (
+            ("leap_linear8_backward_fine", (P, P, P, 4, 64, P, 64, 8, P, 1, P, P, 0), [(3, -1), (4, 0), (6, 63), (7, 0), (9, 2), (0, 0), (0, P + 8), (1, 0), (2, 0), (5, 0), (11, 0), (11, P + 8)]),
+            ("leap_gate8_backward_fine", (P, 8, P, P, 4, 8, P, 0), [(1, 7), (4, -1), (5, 0), (5, 1 << 20), (0, 0), (2, 0), (3, 0), (6, 0), (6, P + 8)]),
+            ("leap_linear_gate8_backward_fine", (P, 8, P, 16, 8, P, P, 4, 16, P, P, 0), [(1, 7), (3, 15), (4, 0), (7, -1), (8, 0), (8, 1 << 20), (0, 0), (2, 0), (5, 0), (6, 0), (9, 0), (9, P + 4)])):
+        for at, value in bad:
+            arguments = list(good)
+            arguments[at] = value
+            assert getattr(lib, name)(*arguments) == B.LEAP_INVALID_ARG, (name, at, value)
+            assert lib.leap_last_error()
+    assert lib.leap_linear8_backward_fine_work(P, 5, 64, P, 64, 9) == (16 + 9) * 64 * 2 + 2 * 16 * 64 * 4
+    assert lib.leap_linear8_backward_fine_work(P, 5, 64, P, 64, 0) == 0 and lib.leap_linear8_backward_fine_work(P, 0, 343, P, 343, 8) == 0
+    assert lib.leap_linear8_backward_fine(None, None, None, 0, 343, None, 343, 8, P, 1, None, None, None) == B.LEAP_OK

@@ -83,36 +83,29 @@ def halves(A, rows, out, seed):  # noqa: F811
     return kept, kept.unpack(F32).double()
 
 
-@cases(K.GATE_GRAD)
+@cases(K.GATE_GRAD, K.GATE_GRAD_FINE)
 def test_gradient_through_the_gate(A, what, rows, cols, out):  # noqa: F811
     (kept, u), (w, wd), (g, gd) = halves(A, rows, cols, 413), weight(out, cols, 414), gradient(rows, out, 415)
     du, size = R.gate_backward(gd @ wd, u)
-    near(A.linear_gate8_backward(g, w, kept), du, du.abs() * R.half_step(BF16) + 2.0 ** -18 * size + torch.finfo(F32).smallest_normal, "du")
+    fine = what == K.GATE_GRAD_FINE
+    got = A.linear_gate8_backward(g, w, kept, fine=fine)
+    near(got, du, du.abs() * (2.0 ** -17 if fine else R.half_step(BF16)) + 2.0 ** -18 * size + torch.finfo(F32).smallest_normal, "du")
+    assert not fine or not got.memory[..., 2 * cols:].any()
 
 
-@cases(K.GATE_GRAD_FINE)
-def test_fine_gradient_through_the_gate(A, what, rows, cols, out):  # noqa: F811
-    """By the block, which alone takes these kernels: 64 columns, `cols` hidden ones."""
-    g = torch.Generator(device="cuda").manual_seed(417)
-    x = torch.randn(rows, 64, device="cuda", generator=g).to(BF16)
-    nw = torch.ones(64, dtype=BF16, device="cuda")
-    up = (torch.randn(2 * cols, 64, device="cuda", generator=g) / 8).to(BF16)
-    (down, dd), (gy, gyd) = weight(out, cols, 418), gradient(rows, out, 419)
-    _, normed, kept_sum, rstd = A.rms_norm8(x, nw)
-    kept = A.gated_linear8(normed, up)[1]
-    leaves = [t.requires_grad_(True) for t in (x, up)]
-    y, _ = A.feed_forward8(x, nw, up, down, fine=True)
-    dx, dup = torch.autograd.grad(y, leaves, gy)
-    du, size = R.gate_backward(gyd @ dd, kept.unpack(F32).double())
-    error = (2.0 ** -17 + 2.0 ** -18) * size
-    v, upd = normed.unpack(F32).double(), up.detach().double()
-    want = du.T @ v
-    near(dup, want, want.abs() * R.half_step(BF16) + error.T @ v.abs() + R.sum_error(2 * rows) * (du.abs().T @ v.abs()), "grad_up")
-    dn, off = du @ upd, error @ upd.abs() + R.sum_error(4 * cols) * (du.abs() @ upd.abs())
-    h = kept_sum.unpack(F32).double()
-    want, size, _, _ = R.rms_norm_backward(dn, h, rstd, nw, None)
-    through = R.rms_norm_backward(off, h, rstd, nw, None)[1]
-    near(dx, want, want.abs() * R.half_step(BF16) + size * R.sum_error(64) + through, "grad_x")
+@pytest.mark.parametrize("rows,cols,out", [(33000, 1030, 1100), (3001, 72, 700), (18414, 343, 1029)])
+def test_gradients_from_a_fine_one(A, rows, cols, out):  # noqa: F811
+    """dy of 11 bits, which takes both of its parts; sums, of values of either sign, are whole numbers of no more than 24."""
+    (x, v), (w, wd) = packed(A, rows, cols, 431), weight(out, cols, 433)
+    dy = whole((rows, out), 2047, 434)
+    grad = A.FineGradient((rows, out), "cuda")
+    grad.memory.zero_()
+    grad.rounded.copy_(dy)
+    grad.rest.copy_(dy - grad.rounded.float())
+    assert torch.equal(grad.float(), dy)
+    dx, dw = A.linear8_backward(grad, x, w, dtype=F32)
+    assert torch.equal(dx, (dy.double() @ wd).float())
+    assert torch.equal(dw, (dy.double().T @ v).to(BF16))
 
 
 def test_norm_past_the_caches(A):  # noqa: F811
@@ -136,7 +129,7 @@ def test_gate_gradient_past_the_caches(A):  # noqa: F811
     rows, out = 50003, 1029
     (kept, u), (g, gd) = halves(A, rows, out, 423), gradient(rows, out, 424)
     du, size = R.gate_backward(gd, u)
-    near(A.gate8_backward(g, kept), du, du.abs() * R.half_step(BF16) + 2.0 ** -18 * size + torch.finfo(F32).smallest_normal, "du")
+    near(A.gate8_backward(g, kept, fine=False), du, du.abs() * R.half_step(BF16) + 2.0 ** -18 * size + torch.finfo(F32).smallest_normal, "du")
     (x, _), (w, wd) = packed(A, rows, 40, 425), weight(2 * out, 40, 427)
     for fine, held in ((False, R.half_step(BF16)), (True, 2.0 ** -17)):
         dx, _ = A.gated_linear8_backward(g, kept, x, w, need_weight=False, fine=fine)

@@ -133,19 +133,22 @@ def test_norm_of_many_long_rows(A):  # noqa: F811
 
 
 def test_gate_gradient_of_many_short_rows(A):  # noqa: F811
-    """du of one gated column; the same through a product of one column."""
+    """du of one gated column; the same through a product of one column; rounded and fine."""
     rows = (1 << 28) + 77
     da = _channels(rows, 1, 309)
     kept = A.Packed8(torch.full((rows, 2, 1), 56, dtype=torch.uint8, device="cuda").view(torch.float8_e4m3fn),        # code 56: 1.0
                      torch.full((rows, 2, 1), 127, dtype=torch.uint8, device="cuda"))
     kept.codes.view(torch.uint8)[1::3, 0] = 64                                                                       # 2.0
     one = torch.ones(1, 1, dtype=BF16, device="cuda")
-    for du in (lambda: A.gate8_backward(da, kept), lambda: A.linear_gate8_backward(da, one, kept)):
+    for du in (lambda: A.gate8_backward(da, kept, fine=False), lambda: A.linear_gate8_backward(da, one, kept, fine=False),
+               lambda: A.gate8_backward(da, kept), lambda: A.linear_gate8_backward(da, one, kept)):
         got = du()
+        fine = isinstance(got, A.FineGradient)
         for begin, end in CHANNELS + [((1 << 28) - 40, (1 << 28) + 40), (rows - 50, rows)]:
             want, size = R.gate_backward(da[begin:end].cpu(), R.values(kept.codes[begin:end].view(torch.uint8).cpu(), kept.scales[begin:end].cpu()))
-            R.assert_close(got[begin:end], want, want.abs() * R.half_step(BF16) + 2.0 ** -18 * size, "du")
-        del got
+            part = got.rounded[begin:end].float() + got.rest[begin:end].float() if fine else got[begin:end]
+            R.assert_close(part, want, want.abs() * (2.0 ** -17 if fine else R.half_step(BF16)) + 2.0 ** -18 * size, "du")
+        del got, part
 
 
 def test_rows_laid_out_by_several_launches(A):  # noqa: F811
