@@ -65,8 +65,8 @@ template <int TYPE> __device__ inline void load8(const void *base, int64_t at, i
 
 // Outputs of more than this go past the caches: little of them is left there when they are read, and they push out what is (2^27
 // bfloat16 values unpacked: 57 us, 68 through the caches; packed 61 and 70).
-// What the next kernel reads pays from further on, the 256 MB cache in mind (du of 18414 x 2058 and of 16384 x 2048 through the caches: a gated
-// step 213 us, 220 past them, a block's 273 and 284).
+// What the next kernel reads pays from further on, the 256 MB cache in mind (du of 18414 x 2058 and of 16384 x 2048, in bfloat16, through the caches: a
+// gated step 213 us, 220 past them, a block's 273 and 284).
 constexpr int64_t PAST_CACHES = (int64_t)64 << 20, READ_NEXT = (int64_t)192 << 20;
 
 typedef uint32_t words4 __attribute__((ext_vector_type(4), aligned(1)));
