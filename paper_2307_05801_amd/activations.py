@@ -266,9 +266,9 @@ def _unpack_flat(parts, shape, dtype: torch.dtype) -> torch.Tensor:
 
 class keep_in_8_bits(torch.autograd.graph.saved_tensors_hooks):
     """Inside this context what autograd saves for the backward pass is kept packed: plain tensors on a GPU of float32, bfloat16 or
-    float16 with at least `min_values` values and evenly spaced rows (no gaps, where they have more than 2^20 columns).  Leaves that want a gradient (weights) and everything
-    else are kept as they are; a weight's cast or slice is no leaf: keep its use outside.  The gradients are those of the values held
-    (3 mantissa bits).  What is finite stays so (a mask's lowest number too); infinities come back as NaN: operations that save a tensor masked with
+    float16 with at least `min_values` values and evenly spaced rows (no gaps, where they have more than 2^20 columns).  Leaves that want
+    a gradient (weights) and everything else are kept as they are; a weight's cast or slice is no leaf: keep its use outside.  The
+    gradients are those of the values held (3 mantissa bits).  What is finite stays so (a mask's lowest number too); infinities come back as NaN: operations that save a tensor masked with
     them (logsumexp of -inf) belong outside."""
 
     def __init__(self, min_values: int = 1 << 16):
@@ -464,8 +464,8 @@ def linear_gate8_backward(grad: torch.Tensor, weight: torch.Tensor, kept: Packed
     rows, _, stride = _gradient(grad, lead + (following,), kept.device, (torch.bfloat16,), "grad")
     du, address = _empty_du(lead + (2 * out,), kept.device, fine)
     work = _work("leap_linear_gate8_work", kept.device, grad.data_ptr(), stride, weight.data_ptr(), w_stride, following, rows, out)
-    _call("leap_linear_gate8_backward_fine" if fine else "leap_linear_gate8_backward", kept.device, grad.data_ptr(), stride, weight.data_ptr(), w_stride, following, kept.codes.data_ptr(),
-          kept.scales.data_ptr(), rows, out, address, _address(work))
+    _call("leap_linear_gate8_backward_fine" if fine else "leap_linear_gate8_backward", kept.device, grad.data_ptr(), stride, weight.data_ptr(), w_stride,
+          following, kept.codes.data_ptr(), kept.scales.data_ptr(), rows, out, address, _address(work))
     return du
 
 
