@@ -23,6 +23,10 @@ class Launch(NamedTuple):
 
 
 def _build():
+    from paper_2307_05801_amd import binding as B
+    if not os.path.exists(B.LIB_PATH):
+        from paper_2307_05801_amd.build import build_library
+        build_library()
     if not os.path.exists(LIB) or os.path.getmtime(LIB) < os.path.getmtime(SRC):
         tmp = f"{LIB}.{os.getpid()}.tmp"
         subprocess.run(["g++", "-O1", "-std=c++17", "-fPIC", "-shared", "-o", tmp, SRC], check=True, capture_output=True)
