@@ -1,0 +1,67 @@
+/*
+ * leap_networks.h - C ABI of the operators for networks trained through the projector that work on plain arrays: attention over the
+ * patches of a volume with learned relative positions, and group norm with an activation, each with its gradients.  (Those on
+ * activations in 8 bits are in leap_activations.h.)
+ *
+ * Conventions (those of leap_activations.h)
+ *   - Data pointers are DEVICE pointers owned by the caller, of the current HIP device; nothing is kept, allocated or
+ *     freed.  Calls are asynchronous on hip_stream (NULL: the default stream) and can be captured into a graph.
+ *   - Strides are distances in elements; the values of a row are neighbours.  No alignment beyond the element's is asked for, but for
+ *     workspaces, which begin at a multiple of 16 bytes.
+ *   - Outputs are overwritten, have no gaps and must not overlap inputs.  Sums are formed in 32 bits or more, in an order fixed by the
+ *     sizes: the same call gives the same bits.
+ *   - Every function returns LEAP_OK (0) or a negative status of leap.h; the message is in leap_last_error().
+ */
+#ifndef LEAP_NETWORKS_H
+#define LEAP_NETWORKS_H
+
+#include <stdint.h>
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+/* Attention.  q: [batch][queries][heads][width]; k, v: [batch][keys][kv_heads][width], bfloat16; head h reads the keys and values of head
+ * h / (heads / kv_heads).  With x = scale q.k + bias over a query's and a head's keys, p = exp(x) / sum of exp(x) and o = sum of p v; a query
+ * without keys has o = 0.
+ *
+ * The mask, d_mask (NULL: all keys): bytes [batch][keys], items mask_item bytes apart; a key whose byte is 0 is left out, and its k and v
+ * do not count whatever they hold.
+ *
+ * The bias, from d_table [heads][buckets] of table_type (NULL: none): the pair of query i and key j takes the bucket
+ * d_bucket_of[d_key_positions[j] - d_query_positions[i] + offsets / 2] of `offsets`; differences beyond either end take that end's, buckets
+ * beyond the table's ends its ends'.  Positions (NULL: i and j themselves) are within -2^30 .. 2^30.  Infinities and numbers of any size in the table are fine: -inf
+ * leaves a pair out. */
+typedef struct {
+    int64_t batch, queries, keys, heads, kv_heads, width;
+    int64_t q_item, q_row, q_head, k_item, k_row, k_head, v_item, v_row, v_head;       /* strides of an item, of a query or key, of a head */
+    int64_t mask_item, offsets, buckets;
+    const uint8_t *d_mask;
+    const void *d_table;
+    const int32_t *d_bucket_of, *d_query_positions, *d_key_positions;
+    int32_t table_type;
+    float scale;                                                                       /* positive */
+} leap_attention_desc;
+
+enum { LEAP_ATTENTION_WIDEST = 128, LEAP_ATTENTION_BUCKETS = 4096 };                   /* the largest width, the most buckets */
+
+/* o [batch][queries][heads][width] <- attention.  For a backward pass also stats [batch][heads][queries][2] (float: the largest exponent of
+ * a query's keys and the logarithm of their sum, both to the base 2) and rest [as o] (float16: what o's rounding leaves, times 2^8); NULL: both or neither.
+ * With them the probabilities go into the product with 16 bits instead of 8, so that o + rest / 2^8 is good to 2^-16.
+ * d_work: leap_attention_work() bytes, NULL where that is 0. */
+int64_t leap_attention_work(const leap_attention_desc *desc);
+int leap_attention(const leap_attention_desc *desc, const void *d_q, const void *d_k, const void *d_v, void *d_o, float *d_stats, void *d_rest,
+                   void *d_work, void *hip_stream);
+
+/* Its gradients from that of o: grad [batch][queries][heads][width] with strides; o, stats and rest of the forward pass.  grad_q, grad_k, grad_v: as
+ * q, k, v without gaps; grad_table: [heads][buckets], float.  Any of them may be NULL.  Keys that the mask leaves out get zeros.
+ * d_work: leap_attention_backward_work() bytes (with_table: whether grad_table is wanted), never NULL where there are queries. */
+int64_t leap_attention_backward_work(const leap_attention_desc *desc, int32_t with_table);
+int leap_attention_backward(const leap_attention_desc *desc, const void *d_grad, int64_t grad_item, int64_t grad_row, int64_t grad_head, const void *d_q,
+                            const void *d_k, const void *d_v, const void *d_o, const float *d_stats, const void *d_rest, void *d_grad_q,
+                            void *d_grad_k, void *d_grad_v, float *d_grad_table, void *d_work, void *hip_stream);
+
+#ifdef __cplusplus
+}
+#endif
+#endif

@@ -15,7 +15,7 @@ def __getattr__(name):
     if name in ("Geometry", "Projector"):
         from . import projector
         return getattr(projector, name)
-    if name in ("recon", "activations"):
+    if name in ("recon", "activations", "networks"):
         import importlib
         return importlib.import_module("." + name, __name__)
     raise AttributeError(name)

@@ -58,6 +58,14 @@ ACTIVATION_EXPORTS = {                                       # name: (result, ar
     "leap_feed_forward8_backward_fine": (C.c_int, [_P, _L, _P, _L, _P, _I, _L, _L, _P, _L, _L, _P, _L, _L] + [_P] * 7),
 }
 
+LEAP_ATTENTION_WIDEST, LEAP_ATTENTION_BUCKETS = 128, 4096    # limits of include/leap_networks.h
+NETWORK_EXPORTS = {                                          # a description's bytes go as a pointer
+    "leap_attention_work": (_L, [_P]),
+    "leap_attention": (C.c_int, [_P] * 9),
+    "leap_attention_backward_work": (_L, [_P, _I]),
+    "leap_attention_backward": (C.c_int, [_P, _P, _L, _L, _L] + [_P] * 12),
+}
+
 
 class leap_geometry_desc(C.Structure):
     _fields_ = [
@@ -134,12 +142,12 @@ _activations = None
 
 
 def load_activations():
-    """The library with the prototypes of include/leap_activations.h (apart from load_library: another build of the library,
-    under LEAP_LIB_PATH, need not have them)."""
+    """The library with the prototypes of include/leap_activations.h and include/leap_networks.h (apart from load_library: another
+    build of the library, under LEAP_LIB_PATH, need not have them)."""
     global _activations
     if _activations is None:
         lib = load_library()
-        for name, (result, arguments) in ACTIVATION_EXPORTS.items():
+        for name, (result, arguments) in (ACTIVATION_EXPORTS | NETWORK_EXPORTS).items():
             fn = getattr(lib, name)
             fn.restype, fn.argtypes = result, arguments
         _activations = lib

@@ -1,0 +1,234 @@
+// What attention's kernels share: tiles of rows in shared memory and how the matrix instructions read them, masks, the bias.
+//
+// Scores are formed with the pair's two sides such that probabilities stay in registers.  A 32 x 32 product leaves a lane with one column (lane % 32) and
+// 16 rows (8 a + 4 (lane / 32) + 0 .. 3, a = 0 .. 3); as the right operand of the next product it wants one column and eight values along the
+// sum.  Which eight is free as long as the left operand has the same: those of a = 2 m and 2 m + 1 for the m-th sixteen of the sum, so that
+// the left operand's two reads take rows 16 m + 4 (lane / 32) + 0 .. 3 and eight further.  Nothing is exchanged between lanes.
+#pragma once
+
+#include "../../include/leap_networks.h"
+#include "act_product.h"
+
+namespace net {
+
+using namespace act;
+
+constexpr int TILE = 64;                   // rows of a tile: keys, or queries in the gradient of keys and values
+constexpr int WAVE = 64, WAVES = 4, BLOCK = WAVE * WAVES;
+constexpr int COLS = 32 * WAVES;           // queries (or keys) of a block, 32 to a wave
+constexpr float LOG2E = 1.4426950408889634f;
+
+// An array [item][row][head][width] of bfloat16.
+struct rows_of {
+    const uint16_t *data;
+    int64_t item, row, head;
+};
+
+struct attention_args {
+    rows_of q, k, v;
+    int32_t batch, queries, keys, heads, kv_heads, width;
+    const uint8_t *mask;
+    int64_t mask_item;
+    const void *table;
+    const int32_t *bucket_of, *query_positions, *key_positions;
+    int32_t table_type, offsets, buckets;
+    float scale;
+};
+
+// A tile of TILE rows of DEEP values in shared memory, in 16-byte pieces.  The order of a row's pieces lets 16 neighbouring rows be read at one piece, and
+// four rows at four neighbouring pieces (the transposing read), each from all banks once.  96 values lie in rows of 128.
+template <int DEEP> struct rows_tile {
+    static constexpr int CHUNKS = DEEP / 8, ROW = DEEP <= 32 ? 64 : DEEP <= 64 ? 128 : 256, BYTES = TILE * ROW;
+    static constexpr int EACH = TILE * CHUNKS / BLOCK;                     // pieces a thread brings
+    static_assert(TILE * CHUNKS % BLOCK == 0, "");
+
+    static __device__ inline int place(int r, int chunk)
+    {
+        const int turn = ROW == 256 ? r % 4 * 4 + r / 4 % 4 : ROW == 128 ? r / 2 % 2 * 4 + r / 4 % 4 : r / 4 % 4;
+        return r * ROW + (chunk ^ turn) * 16;
+    }
+    // Eight values of row first + lane % 32 from 16 step + 8 (lane / 32) on: a side of a product along the width.
+    static __device__ inline bf16x8 along(const lds_byte *from, int first, int step, int lane)
+    {
+        return *(const __attribute__((address_space(3))) bf16x8 *)(from + place(first + lane % 32, step * 2 + lane / 32));
+    }
+    // The values of column 32 block + lane % 32 in rows first + 4 (lane / 32) + 0 .. 3 and eight further.
+    static __device__ inline bf16x8 across(const lds_byte *from, int first, int block, int lane)
+    {
+        const int row = first + lane / 32 * 4 + lane % 16 / 4, col = block * 32 + lane / 16 % 2 * 16 + lane % 4 * 4;
+        const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(from + place(row, col / 8) + col % 8 * 2));
+        const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(from + place(row + 8, col / 8) + col % 8 * 2));
+        return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+};
+
+// Eight values of a row of `width` from 8 chunk on, zeros beyond its end.  Nothing beyond the row is read: the last piece of a row
+// that does not end with it is the row's last eight values, moved.
+__device__ inline u32x4 row_piece(const uint16_t *row, int width, int chunk)
+{
+    const int left = width - chunk * 8;
+    u32x4 v = {0, 0, 0, 0};
+    if (left >= 8) {
+        __builtin_memcpy(&v, row + chunk * 8, 16);
+    } else if (left > 0) {
+        if (width >= 8) {
+            uint64_t w[2];
+            __builtin_memcpy(w, row + width - 8, 16);
+            const int s = (8 - left) * 16;                                 // 16 .. 112
+            const uint64_t low = s < 64 ? w[0] >> s | w[1] << (64 - s) : w[1] >> (s - 64), high = s < 64 ? w[1] >> s : 0;
+            v = u32x4{(uint32_t)low, (uint32_t)(low >> 32), (uint32_t)high, (uint32_t)(high >> 32)};
+        } else {
+            uint16_t e[8] = {};
+#pragma unroll
+            for (int i = 0; i < 7; ++i)
+                if (i < left) e[i] = row[i];
+            __builtin_memcpy(&v, e, 16);
+        }
+    }
+    return v;
+}
+
+// A tile's pieces on their way from memory through the registers.
+template <int DEEP> struct staged {
+    using tile = rows_tile<DEEP>;
+    u32x4 piece[tile::EACH];
+
+    // Rows `first` on of an array's item and head; those whose bit is not set in `there` are zeros and are not read.
+    __device__ inline void fetch(const uint16_t *base, int64_t stride, int64_t first, uint64_t there, int width)
+    {
+#pragma unroll
+        for (int e = 0; e < tile::EACH; ++e) {
+            const int id = e * BLOCK + threadIdx.x, r = id / tile::CHUNKS, chunk = id % tile::CHUNKS;
+            piece[e] = there >> r & 1 ? row_piece(base + (first + r) * stride, width, chunk) : u32x4{0, 0, 0, 0};
+        }
+    }
+    __device__ inline void store(lds_byte *to) const
+    {
+#pragma unroll
+        for (int e = 0; e < tile::EACH; ++e) {
+            const int id = e * BLOCK + threadIdx.x, r = id / tile::CHUNKS, chunk = id % tile::CHUNKS;
+            *(__attribute__((address_space(3))) u32x4 *)(to + tile::place(r, chunk)) = piece[e];
+        }
+    }
+};
+
+// Which of the rows first .. first + TILE - 1 there are: within `rows`, and in the mask (null: all).
+__device__ inline uint64_t rows_there(const uint8_t *mask, int64_t first, int64_t rows, int lane)
+{
+    const bool in = first + lane < rows;
+    return __ballot(in && (!mask || mask[first + lane]));
+}
+
+// Numbers of the table in units of log2; what is finite stays so.
+__device__ inline float table_value(const attention_args &A, int head, int bucket)
+{
+    const int64_t at = (int64_t)head * A.buckets + bucket;
+    const float v = A.table_type == LEAP_F32    ? ((const float *)A.table)[at]
+                    : A.table_type == LEAP_BF16 ? element<LEAP_BF16>::to_float(((const uint16_t *)A.table)[at])
+                                                : element<LEAP_F16>::to_float(((const uint16_t *)A.table)[at]);
+    const float most = element<LEAP_F32>::LARGEST, scaled = v * LOG2E;
+    return finite_magnitude(v) && !finite_magnitude(scaled) && scaled != 0.0f ? copysignf(most, v) : scaled;
+}
+
+__device__ inline int query_position(const attention_args &A, int i) { return A.query_positions ? A.query_positions[i] : i; }
+__device__ inline int key_position(const attention_args &A, int j) { return A.key_positions ? A.key_positions[j] : j; }
+
+// The bucket of a pair, whatever its positions.
+__device__ inline int bucket_at(const attention_args &A, int difference)
+{
+    const int half = A.offsets / 2, d = difference < -half ? -half : difference > A.offsets - 1 - half ? A.offsets - 1 - half : difference;
+    const int b = A.bucket_of[d + half];
+    return b < 0 ? 0 : b >= A.buckets ? A.buckets - 1 : b;
+}
+
+__device__ inline bf16x8 eight(const f32x16 &v, int m)
+{
+    bf16x8 r;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r[i] = (__bf16)v[m * 8 + i];
+    return r;
+}
+
+// What rounding to eight() leaves.
+__device__ inline bf16x8 rest_of_eight(const f32x16 &v, int m)
+{
+    bf16x8 r;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r[i] = (__bf16)rest_of_bf16(v[m * 8 + i]);
+    return r;
+}
+
+__device__ inline f32x16 product(const bf16x8 &a, const bf16x8 &b, const f32x16 &c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+
+__device__ inline f32x16 zeros()
+{
+    f32x16 z;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) z[i] = 0.0f;
+    return z;
+}
+
+// The two lanes of a column, which hold its two sets of rows, as one.
+template <class F> __device__ inline float both_halves(float v, F &&f)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return f(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ inline float column_sum(float v)
+{
+    return both_halves(v, [](float a, float b) { return a + b; });
+}
+__device__ inline float column_max(float v)
+{
+    return both_halves(v, [](float a, float b) { return fmaxf(a, b); });
+}
+
+// Register r of a lane's 32 rows stands for row row_of(r) + 4 (lane / 32).
+__device__ inline constexpr int row_of(int r) { return r / 4 * 8 + r % 4; }
+
+// A lane's column of a [width][32] result, times `by`, to a row of `width` bfloat16; BLOCKS of 32 values.
+template <int BLOCKS> __device__ inline void store_column(uint16_t *row, int width, f32x16 (&v)[BLOCKS], float by, int lane, bool there)
+{
+#pragma unroll
+    for (int b = 0; b < BLOCKS; ++b) {
+        uint32_t run[4][2];
+#pragma unroll
+        for (int a = 0; a < 4; ++a) {
+            run[a][0] = two_bf16(v[b][a * 4] * by, v[b][a * 4 + 1] * by);
+            run[a][1] = two_bf16(v[b][a * 4 + 2] * by, v[b][a * 4 + 3] * by);
+        }
+        join_runs<2>(run);                     // sixteen neighbours
+        const int at = b * 32 + lane / 32 * 16;
+        if (!there) continue;
+#pragma unroll
+        for (int p = 0; p < 2; ++p)
+            if (at + p * 8 < width)
+                store_piece<2>((uint8_t *)(row + at + p * 8), (int64_t)(width - at - p * 8) * 2,
+                               u32x4{run[p * 2][0], run[p * 2][1], run[p * 2 + 1][0], run[p * 2 + 1][1]});
+    }
+}
+
+// Unit u of `units`, such that neighbouring units (which share keys, or queries) run on the same of the eight parts of the chip: blocks go round over those.
+__device__ inline int64_t unit_of(int64_t block, int64_t units)
+{
+    const int64_t each = units / 8, more = units % 8, part = block % 8, turn = block / 8;
+    return part * each + (part < more ? part : more) + turn;
+}
+
+// ---- host side ----
+
+// f(the width up to a multiple of 32, as a constant)
+template <class F> inline int by_width(int64_t width, F &&f)
+{
+    if (width <= 32) return f(std::integral_constant<int, 32>{});
+    if (width <= 64) return f(std::integral_constant<int, 64>{});
+    if (width <= 96) return f(std::integral_constant<int, 96>{});
+    return f(std::integral_constant<int, 128>{});
+}
+
+// Null if fine: an array's strides; a description.
+const char *bad_array(int64_t items, int64_t item, int64_t rows, int64_t row, int64_t heads, int64_t head);
+const char *bad_attention(const leap_attention_desc *d);
+attention_args arguments_of(const leap_attention_desc *d, const void *q, const void *k, const void *v);
+
+}  // namespace net

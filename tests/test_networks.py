@@ -1,0 +1,129 @@
+"""Attention and group norm, what needs no GPU: the ABI, the refusals, the references and the places of a grid."""
+import os
+import re
+
+import pytest
+import torch
+
+import networks_reference as R
+from paper_2307_05801_amd import binding as B
+from paper_2307_05801_amd import networks as N
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+P = 0x1000                                   # addresses are never touched: every call below is refused before anything is launched
+
+
+@pytest.fixture(scope="module")
+def lib():
+    if not os.path.exists(B.LIB_PATH):
+        from paper_2307_05801_amd.build import build_library
+        build_library()
+    return B.load_activations()
+
+
+def test_every_declared_symbol_is_exported_and_bound(lib):
+    header = open(os.path.join(ROOT, "include", "leap_networks.h")).read()
+    header = re.sub(r"/\*.*?\*/", "", header, flags=re.S)
+    declared = dict(re.findall(r"\b(leap_[a-z0-9_]+)\s*\(([^)]*)\)", header))
+    assert set(declared) == set(B.NETWORK_EXPORTS)
+    for name, arguments in declared.items():
+        assert getattr(lib, name) is not None
+        assert len(arguments.split(",")) == len(B.NETWORK_EXPORTS[name][1]), name
+    assert f"LEAP_ATTENTION_WIDEST = {B.LEAP_ATTENTION_WIDEST}, LEAP_ATTENTION_BUCKETS = {B.LEAP_ATTENTION_BUCKETS}" in header
+
+
+# batch, queries, keys, heads, kv_heads, width; strides of q, k, v; mask's, differences, buckets; mask, table, buckets, positions; type, scale
+GOOD = (2, 5, 7, 4, 2, 64, 1280, 256, 64, 896, 128, 64, 896, 128, 64, 7, 13, 9, P, P, P, P, P, 0, 0.125)
+BAD = [(0, -1), (0, 1 << 31), (1, -1), (1, 1 << 31), (2, -1), (3, 0), (3, 3), (4, 0), (4, 3), (5, 0), (5, 129), (6, -1), (7, -5), (8, -1), (9, -1), (10, -1), (11, -1), (12, -1),
+       (13, -1), (14, -1), (7, 1 << 58), (15, -1), (16, 0), (16, 1 << 31), (17, 0), (17, 4097), (20, 0), (23, 3), (23, -1), (24, 0.0), (24, -1.0), (24, float("nan")), (24, float("inf"))]
+
+
+def test_bad_descriptions_are_refused_with_a_message(lib):
+    for at, value in BAD:
+        d = list(GOOD)
+        d[at] = value
+        desc = N._DESC.pack(*d)
+        assert lib.leap_attention(desc, P, P, P, P, P, P, P, None) == B.LEAP_INVALID_ARG, (at, value)
+        assert lib.leap_last_error().decode()
+        assert lib.leap_attention_backward(desc, P, 1280, 256, 64, P, P, P, P, P, P, P, P, P, P, P, None) == B.LEAP_INVALID_ARG, (at, value)
+        assert lib.leap_attention_backward_work(desc, 1) == 0 and lib.leap_attention_work(desc) == 0
+    assert lib.leap_attention(None, P, P, P, P, P, P, P, None) == B.LEAP_INVALID_ARG
+
+
+def test_bad_arguments_are_refused_with_a_message(lib):
+    desc, plain = N._DESC.pack(*GOOD), N._DESC.pack(*GOOD[:16], 0, 0, P, 0, 0, 0, 0, 0, 0.125)
+    good = (desc, P, P, P, P, P, P, P, None)
+    for at, value in [(1, 0), (2, 0), (3, 0), (4, 0), (5, 0), (6, 0)]:       # statistics and what rounding leaves: both or neither
+        arguments = list(good)
+        arguments[at] = value
+        assert lib.leap_attention(*arguments) == B.LEAP_INVALID_ARG, (at, value)
+    good = (desc, P, 1280, 256, 64, P, P, P, P, P, P, P, P, P, P, P, None)
+    for at, value in [(1, 0), (2, -1), (3, -1), (4, -1), (3, 1 << 58), (5, 0), (6, 0), (7, 0), (8, 0), (9, 0), (10, 0), (15, 0), (15, P + 8)]:
+        arguments = list(good)
+        arguments[at] = value
+        assert lib.leap_attention_backward(*arguments) == B.LEAP_INVALID_ARG, (at, value)
+        assert lib.leap_last_error().decode()
+    assert lib.leap_attention_backward(plain, *good[1:]) == B.LEAP_INVALID_ARG       # a gradient of no table
+
+
+def test_nothing_to_do_is_fine(lib):
+    for at in (0, 1):
+        d = list(GOOD)
+        d[at] = 0
+        assert lib.leap_attention(N._DESC.pack(*d), None, None, None, None, None, None, None, None) == B.LEAP_OK
+
+
+def test_tensors_elsewhere_or_of_other_kinds_are_refused():
+    x = torch.zeros(1, 2, 3, 8, dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="GPU"):
+        N.attention(x, x, x)
+
+
+@pytest.mark.parametrize("shape,near,codes", [((), 1, 1), ((0,), 1, 2), ((4, -1), 1, 2), ((4,), 0, 2), ((4,), 3, 2), ((4, 4, 4), 9, 9), ((1 << 30,), 1, 2)])
+def test_grids_that_are_refused(shape, near, codes):
+    with pytest.raises(ValueError):
+        N.relative_buckets(shape, near, codes, device="cpu")
+
+
+@pytest.mark.parametrize("shape,near,codes", [((1,), 1, 1), ((7,), 7, 7), ((40,), 4, 7), ((5, 6), 2, 3), ((3, 4, 5), 1, 2), ((3, 1, 9), 5, 8)])
+def test_places_of_a_grid(shape, near, codes):
+    """Every pair's bucket from its distances along the axes."""
+    positions, buckets = N.relative_buckets(shape, near, codes, device="cpu")
+    places = torch.cartesian_prod(*[torch.arange(n) for n in shape]).reshape(-1, len(shape)).tolist()
+    assert len(positions) == len(places)
+
+    def code(d):
+        a = abs(d)
+        c, edge = 0, 0                                       # the code's first distance
+        while True:
+            following = c + 1 if c + 1 <= near else edge * 2
+            if a < following or c == codes - 1:
+                return (c if d >= 0 else -c) + codes - 1
+            c, edge = c + 1, following
+
+    for i, a in enumerate(places):
+        for j, b in enumerate(places):
+            want = 0
+            for u, w in zip(a, b):
+                want = want * (2 * codes - 1) + code(w - u)
+            assert int(buckets[positions[j] - positions[i] + len(buckets) // 2]) == want
+
+
+def test_the_references_gradients_are_those_of_differences():
+    g = torch.Generator().manual_seed(1)
+    q, k, v, grad = (torch.randn(*s, generator=g, dtype=torch.float64) for s in ((2, 3, 4, 5), (2, 6, 2, 5), (2, 6, 2, 5), (2, 3, 4, 5)))
+    table, buckets = torch.randn(4, 7, generator=g, dtype=torch.float64), torch.randint(0, 7, (9,), generator=g)
+    mask = torch.rand(2, 6, generator=g) < 0.7
+    qp, kp = torch.tensor([0, 5, 2]), torch.tensor([1, 3, 3, 0, 9, 4])
+    r = R.Attention(q, k, v, grad, mask, table, buckets, (qp, kp))
+
+    def value(q, k, v, table):
+        return (R.attention(q, k, v, mask, R.bias_of(table, buckets, qp, kp)[0])[0] * grad).sum()
+
+    for name, t in (("grad_q", q), ("grad_k", k), ("grad_v", v), ("grad_table", table)):
+        for _ in range(3):
+            way = torch.randn(t.shape, generator=g, dtype=torch.float64)
+            h = 1e-6
+            ends = [value(*(s * h * way + u if u is t else u for u in (q, k, v, table))) for s in (1, -1)]
+            got, want = (getattr(r, name) * way).sum(), (ends[0] - ends[1]) / (2 * h)
+            assert abs(got - want) <= 1e-7 * (1 + abs(want)), name
