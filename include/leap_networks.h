@@ -61,6 +61,27 @@ int leap_attention_backward(const leap_attention_desc *desc, const void *d_grad,
                             const void *d_k, const void *d_v, const void *d_o, const float *d_stats, const void *d_rest, void *d_grad_q,
                             void *d_grad_k, void *d_grad_v, float *d_grad_table, void *d_work, void *hip_stream);
 
+/* Group norm with an activation, channels last.  x: [items][voxels][channels] of `type`; a group is channels / groups neighbouring channels of an
+ * item.  With its mean and rstd = 1 / sqrt(variance + eps) over voxels and channels:  u = (x - mean) * rstd * weight + bias,  y = activation(u).
+ * weight, bias: [channels] of weight_type (`type` or float32), or NULL (ones, zeros); y: as x, without gaps.
+ * x_item, x_row: distances of items and of voxels.  stats [items][groups][2] (float: mean, rstd) for the backward pass, or NULL.
+ * d_work: leap_group_norm_work() bytes, NULL where that is 0.  The sums are formed such that a mean far larger than the deviation costs nothing. */
+enum { LEAP_LINEAR = 0, LEAP_RELU = 1, LEAP_SILU = 2 };
+int64_t leap_group_norm_work(int64_t items, int64_t voxels, int64_t channels, int64_t groups);
+int leap_group_norm(const void *d_x, int32_t type, int64_t x_item, int64_t x_row, const void *d_weight, const void *d_bias, int32_t weight_type, int64_t items,
+                    int64_t voxels, int64_t channels, int64_t groups, float eps, int32_t activation, void *d_y, float *d_stats, void *d_work,
+                    void *hip_stream);
+
+/* Its gradients from that of y.  x, weight, bias and stats: of the forward pass (x may be what 8 bits held of it).  With du = grad * activation'(u) and
+ * h = (x - mean) * rstd:  grad_bias = sum over items and voxels of du,  grad_weight = of du * h,  grad_x = rstd * (du * weight - mean over the group
+ * of du * weight - h * mean over the group of du * weight * h).  grad: of `type`, distances grad_item, grad_row.  grad_x: as x, without gaps; grad_weight, grad_bias: [channels]
+ * of weight_type; each may be NULL.  The slope of LEAP_RELU at 0 is 0.  d_work: leap_group_norm_backward_work() bytes, 16-byte aligned. */
+int64_t leap_group_norm_backward_work(int64_t items, int64_t voxels, int64_t channels, int64_t groups);
+int leap_group_norm_backward(const void *d_grad, int64_t grad_item, int64_t grad_row, const void *d_x, int32_t type, int64_t x_item, int64_t x_row,
+                             const void *d_weight, const void *d_bias, int32_t weight_type, const float *d_stats, int64_t items, int64_t voxels,
+                             int64_t channels, int64_t groups, int32_t activation, void *d_grad_x, void *d_grad_weight, void *d_grad_bias, void *d_work,
+                             void *hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

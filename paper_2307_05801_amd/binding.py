@@ -58,12 +58,17 @@ ACTIVATION_EXPORTS = {                                       # name: (result, ar
     "leap_feed_forward8_backward_fine": (C.c_int, [_P, _L, _P, _L, _P, _I, _L, _L, _P, _L, _L, _P, _L, _L] + [_P] * 7),
 }
 
-LEAP_ATTENTION_WIDEST, LEAP_ATTENTION_BUCKETS = 128, 4096    # limits of include/leap_networks.h
+LEAP_ATTENTION_WIDEST, LEAP_ATTENTION_BUCKETS = 128, 4096    # limits of include/leap_networks.h, and its activations
+LEAP_LINEAR, LEAP_RELU, LEAP_SILU = 0, 1, 2
 NETWORK_EXPORTS = {                                          # a description's bytes go as a pointer
     "leap_attention_work": (_L, [_P]),
     "leap_attention": (C.c_int, [_P] * 9),
     "leap_attention_backward_work": (_L, [_P, _I]),
     "leap_attention_backward": (C.c_int, [_P, _P, _L, _L, _L] + [_P] * 12),
+    "leap_group_norm_work": (_L, [_L] * 4),
+    "leap_group_norm": (C.c_int, [_P, _I, _L, _L, _P, _P, _I, _L, _L, _L, _L, C.c_float, _I] + [_P] * 4),
+    "leap_group_norm_backward_work": (_L, [_L] * 4),
+    "leap_group_norm_backward": (C.c_int, [_P, _L, _L, _P, _I, _L, _L, _P, _P, _I, _P, _L, _L, _L, _L, _I] + [_P] * 5),
 }
 
 

@@ -12,7 +12,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libleap_hip.so")
 SOURCES = ["leap_geometry.cpp", "leap_host.cpp", "leap_kernels.hip", "leap_footprint_forward.hip", "leap_footprint_forward_parts.hip", "leap_footprint_back.hip",
-           "leap_footprint_back_pairs.hip", "leap_footprint_back_split.hip", "leap_siddon_back_split.hip", "leap_recon.hip", "act_pack.hip", "act_norm.hip", "act_gemm.hip", "act_block.hip", "net_attention.hip", "net_attention_grad.hip"]
+           "leap_footprint_back_pairs.hip", "leap_footprint_back_split.hip", "leap_siddon_back_split.hip", "leap_recon.hip", "act_pack.hip", "act_norm.hip", "act_gemm.hip", "act_block.hip", "net_attention.hip", "net_attention_grad.hip", "net_group.hip"]
 
 
 def hipcc() -> str:

@@ -1,0 +1,574 @@
+// Group norm with an activation, channels last, and its gradients.
+//
+// A thread has eight neighbouring values of an item at a time and steps from voxel to voxel such that they are always the same channels, whose
+// mean, weight, ... stay in its registers.  Where rows have no gaps and the channels are no multiple of 8, the values are cut in eights regardless of rows: after
+// `period` eights the channels begin anew, so that no length costs more than its values.
+//
+// Sums over a group are formed in three stages that depend on the sizes alone: a thread's values (means and squares about them, a piece of eight voxels exactly in two
+// passes over registers, pieces joined by their means), a block's threads, and in 64 bits the blocks of an item.  Memory bounds it all: x is read
+// twice forward, x and the gradient twice backward.
+#include "../../include/leap_networks.h"
+#include "act_common.h"
+
+namespace {
+
+using namespace act;
+
+constexpr int BLOCK = 256;
+constexpr int PIECE = 8;                    // voxels a thread takes at once
+
+// How an item's values are dealt out to threads.
+struct dealing {
+    int64_t voxels, periods;                // periods of `positions` eights: a voxel, or as many as whole eights need
+    int64_t length;                         // periods of a block
+    int32_t channels, groups, size;         // size: channels of a group
+    int32_t positions, strips, segments;    // eights of a period; blocks along the voxels, across a period
+    int32_t rows;                           // voxels of a period
+};
+
+struct array {
+    const void *data;
+    int64_t item, row;                      // distances in elements
+};
+
+// A thread's part in it.
+struct part {
+    int position, turn, turns, count;       // which eight of a period, which of the block's periods at once; values there
+    int64_t from, to;                       // periods
+    int64_t item, strip;
+
+    __device__ inline part(const dealing &D)
+    {
+        int64_t block = blockIdx.x;
+        const int segment = (int)(block % D.segments);
+        block /= D.segments;
+        strip = block % D.strips, item = block / D.strips;
+        turns = D.positions < BLOCK ? BLOCK / D.positions : 1;
+        position = D.segments > 1 ? segment * BLOCK + (int)threadIdx.x : (int)threadIdx.x % D.positions;
+        turn = D.segments > 1 ? 0 : (int)threadIdx.x / D.positions;
+        const bool there = position < D.positions && turn < turns;
+        count = !there ? 0 : D.rows > 1 || D.channels - position * CHUNK >= CHUNK ? CHUNK : D.channels - position * CHUNK;
+        from = strip * D.length + turn, to = (strip + 1) * D.length < D.periods ? (strip + 1) * D.length : D.periods;
+        if (!there) from = to;
+    }
+    __device__ inline int channel(const dealing &D, int i) const { return D.rows > 1 ? (position * CHUNK + i) % D.channels : position * CHUNK + i; }
+    // Where its eight of a period begin in an item of rows `row` apart, and how many there are.
+    __device__ inline int64_t at(const dealing &D, int64_t period, int64_t row) const { return period * (D.rows > 1 ? (int64_t)D.positions * CHUNK : row) + position * CHUNK; }
+    __device__ inline int there(const dealing &D, int64_t period) const
+    {
+        if (D.rows == 1) return count;
+        const int64_t left = D.voxels * D.channels - at(D, period, 0);
+        return left >= CHUNK ? CHUNK : left > 0 ? (int)left : 0;
+    }
+};
+
+__device__ inline float value_at(const void *p, int type, int64_t i)
+{
+    return type == LEAP_F32 ? ((const float *)p)[i] : type == LEAP_BF16 ? element<LEAP_BF16>::to_float(((const uint16_t *)p)[i]) : element<LEAP_F16>::to_float(((const uint16_t *)p)[i]);
+}
+
+struct group_args {
+    dealing deal;
+    array x, grad;
+    const void *weight, *bias;
+    int32_t weight_type;
+    float eps;
+    int64_t items;
+    float *stats;                           // [items][groups][2]
+    const float *coefficients;              // [items][groups][2]
+    float *parts;
+    void *out;
+    int64_t first;
+};
+
+struct moments {
+    float n, mean, square;                  // square: sum of squares about the mean
+    __device__ inline void join(const moments &o)
+    {
+        const float all = n + o.n;
+        if (o.n == 0.0f) return;
+        const float share = o.n / all, d = o.mean - mean;
+        mean += d * share;
+        square += o.square + d * d * (n * share);
+        n = all;
+    }
+};
+
+// Each slot (eight * 8 + value) of a period: its moments over the block's voxels, to parts [items][strips][slots].
+template <int TYPE> __global__ __launch_bounds__(BLOCK) void k_group_moments(group_args A)
+{
+    const dealing &D = A.deal;
+    const part P(D);
+    const typename element<TYPE>::raw *const x = (const typename element<TYPE>::raw *)A.x.data + P.item * A.x.item;
+    float n = 0.0f, mean[CHUNK] = {}, square[CHUNK] = {};
+    int64_t p = P.from;
+    const int64_t last = D.rows > 1 && P.to == D.periods ? P.to - 1 : P.to;             // a period that may end early comes last, by itself
+    for (; p + (PIECE - 1) * P.turns < last; p += PIECE * P.turns) {
+        float v[PIECE][CHUNK];
+#pragma unroll
+        for (int u = 0; u < PIECE; ++u) load8<TYPE>(x, P.at(D, p + u * P.turns, A.x.row), P.count, v[u]);
+        const float all = n + PIECE, share = PIECE / all, weight = n * share;
+#pragma unroll
+        for (int i = 0; i < CHUNK; ++i) {
+            float m = 0.0f, s = 0.0f;
+#pragma unroll
+            for (int u = 0; u < PIECE; ++u) m += v[u][i];
+            m *= 1.0f / PIECE;
+#pragma unroll
+            for (int u = 0; u < PIECE; ++u) s += (v[u][i] - m) * (v[u][i] - m);
+            const float d = m - mean[i];
+            mean[i] += d * share;
+            square[i] += s + d * d * weight;
+        }
+        n = all;
+    }
+    moments all[CHUNK];
+#pragma unroll
+    for (int i = 0; i < CHUNK; ++i) all[i] = {n, mean[i], square[i]};
+    for (; p < P.to; p += P.turns) {
+        const int there = P.there(D, p);
+        float v[CHUNK];
+        load8<TYPE>(x, P.at(D, p, A.x.row), there, v);
+#pragma unroll
+        for (int i = 0; i < CHUNK; ++i)
+            if (i < there) all[i].join({1.0f, v[i], 0.0f});
+    }
+    // the threads that have the same eight, two by two
+    __shared__ moments room[CHUNK][BLOCK];
+    int half = 1;
+    while (half < P.turns) half *= 2;
+    for (half /= 2; half > 0; half /= 2) {
+        __syncthreads();
+        if (P.turn >= half && P.turn < 2 * half)
+#pragma unroll
+            for (int i = 0; i < CHUNK; ++i) room[i][threadIdx.x] = all[i];
+        __syncthreads();
+        if (P.turn < half && P.turn + half < P.turns)
+#pragma unroll
+            for (int i = 0; i < CHUNK; ++i) all[i].join(room[i][threadIdx.x + half * D.positions]);
+    }
+    if (P.turn == 0 && P.position < D.positions) {
+        moments *const to = (moments *)A.parts + ((P.item * D.strips + P.strip) * D.positions + P.position) * CHUNK;
+#pragma unroll
+        for (int i = 0; i < CHUNK; ++i) to[i] = all[i];
+    }
+}
+
+__device__ inline double block_sum(double v, double *room)
+{
+    room[threadIdx.x] = v;
+    __syncthreads();
+    for (int half = BLOCK / 2; half > 0; half /= 2) {
+        if ((int)threadIdx.x < half) room[threadIdx.x] += room[threadIdx.x + half];
+        __syncthreads();
+    }
+    v = room[0];
+    __syncthreads();
+    return v;
+}
+
+// mean and rstd of a group, a block each.
+__global__ __launch_bounds__(BLOCK) void k_group_stats(group_args A)
+{
+    const dealing &D = A.deal;
+    __shared__ double room[BLOCK];
+    const int64_t unit = A.first + blockIdx.x, item = unit / D.groups, all = (int64_t)D.strips * D.rows * D.size;
+    const int group = (int)(unit % D.groups), each = D.rows * D.size;
+    const moments *const from = (const moments *)A.parts + item * D.strips * D.positions * CHUNK;
+    const auto entry = [&](int64_t e) {
+        const int r = (int)(e % each);
+        return from[e / each * D.positions * CHUNK + r / D.size * D.channels + group * D.size + r % D.size];
+    };
+    double sum = 0.0, square = 0.0;
+    for (int64_t e = threadIdx.x; e < all; e += BLOCK) {
+        const moments m = entry(e);
+        sum += (double)m.n * m.mean;
+    }
+    const double values = (double)D.voxels * D.size, mean = block_sum(sum, room) / values;
+    for (int64_t e = threadIdx.x; e < all; e += BLOCK) {
+        const moments m = entry(e);
+        square += m.square + m.n * (m.mean - mean) * (m.mean - mean);
+    }
+    square = block_sum(square, room) / values;
+    if (threadIdx.x == 0) A.stats[unit * 2] = (float)mean, A.stats[unit * 2 + 1] = (float)(1.0 / sqrt(square + A.eps));
+}
+
+// What a thread knows of its eight channels.
+struct known {
+    float mean[CHUNK], rstd[CHUNK], weight[CHUNK], bias[CHUNK];
+    __device__ inline known(const group_args &A, const part &P)
+    {
+#pragma unroll
+        for (int i = 0; i < CHUNK; ++i) {
+            const bool there = i < P.count;
+            const int c = there ? P.channel(A.deal, i) : 0;
+            const int64_t g = (P.item * A.deal.groups + c / A.deal.size) * 2;
+            mean[i] = there ? A.stats[g] : 0.0f, rstd[i] = there ? A.stats[g + 1] : 0.0f;
+            weight[i] = !there ? 0.0f : A.weight ? value_at(A.weight, A.weight_type, c) : 1.0f;
+            bias[i] = there && A.bias ? value_at(A.bias, A.weight_type, c) : 0.0f;
+        }
+    }
+    // the activation's argument, in both passes from the same steps
+    __device__ inline float argument(float v, int i) const { return __builtin_fmaf(v - mean[i], rstd[i] * weight[i], bias[i]); }
+};
+
+template <int ACTIVATION> __device__ inline float activated(float u) { return ACTIVATION == LEAP_SILU ? u * sigmoid(u) : ACTIVATION == LEAP_RELU ? (u < 0.0f ? 0.0f : u) : u; }
+template <int ACTIVATION> __device__ inline float slope(float u)
+{
+    if (ACTIVATION == LEAP_SILU) {
+        const float s = sigmoid(u);
+        return s * __builtin_fmaf(u, 1.0f - s, 1.0f);
+    }
+    return ACTIVATION == LEAP_RELU && !(u > 0.0f) ? 0.0f : 1.0f;
+}
+
+// f(period, values there) for all of a thread's periods, AT_ONCE of them side by side.
+template <int AT_ONCE, class L, class F> __device__ inline void over_periods(const dealing &D, const part &P, L &&load, F &&use)
+{
+    int64_t p = P.from;
+    for (; p + (AT_ONCE - 1) * P.turns < P.to; p += AT_ONCE * P.turns) {
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u) load(u, p + u * P.turns, P.there(D, p + u * P.turns));
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u) use(u, p + u * P.turns, P.there(D, p + u * P.turns));
+    }
+    for (; p < P.to; p += P.turns) load(0, p, P.there(D, p)), use(0, p, P.there(D, p));
+}
+
+template <int TYPE, int ACTIVATION> __global__ __launch_bounds__(BLOCK) void k_group_apply(group_args A)
+{
+    const dealing &D = A.deal;
+    const part P(D);
+    using raw = typename element<TYPE>::raw;
+    const raw *const x = (const raw *)A.x.data + P.item * A.x.item;
+    raw *const y = (raw *)A.out + P.item * D.voxels * D.channels;
+    const known K(A, P);
+    constexpr int AT_ONCE = 4;
+    float v[AT_ONCE][CHUNK];
+    over_periods<AT_ONCE>(D, P, [&](int u, int64_t p, int n) { load8<TYPE>(x, P.at(D, p, A.x.row), n, v[u]); },
+                          [&](int u, int64_t p, int n) {
+#pragma unroll
+                              for (int i = 0; i < CHUNK; ++i) v[u][i] = activated<ACTIVATION>(K.argument(v[u][i], i));
+                              store8<TYPE>(y, P.at(D, p, D.channels), n, v[u]);
+                          });
+}
+
+// Each slot's sums of du and of du h over the block's voxels, to parts [items][strips][slots][2].
+template <int TYPE, int ACTIVATION> __global__ __launch_bounds__(BLOCK) void k_group_sums(group_args A)
+{
+    const dealing &D = A.deal;
+    const part P(D);
+    using raw = typename element<TYPE>::raw;
+    const raw *const x = (const raw *)A.x.data + P.item * A.x.item, *const grad = (const raw *)A.grad.data + P.item * A.grad.item;
+    const known K(A, P);
+    constexpr int AT_ONCE = 4;
+    float v[AT_ONCE][CHUNK], g[AT_ONCE][CHUNK], one[CHUNK] = {}, two[CHUNK] = {};
+    const auto load = [&](int u, int64_t p, int n) {
+        load8<TYPE>(x, P.at(D, p, A.x.row), n, v[u]);
+        load8<TYPE>(grad, P.at(D, p, A.grad.row), n, g[u]);              // zeros beyond the end
+    };
+    const auto use = [&](int u) {
+#pragma unroll
+        for (int i = 0; i < CHUNK; ++i) {
+            g[u][i] *= slope<ACTIVATION>(K.argument(v[u][i], i));
+            v[u][i] = (v[u][i] - K.mean[i]) * K.rstd[i] * g[u][i];
+        }
+    };
+    int64_t p = P.from;
+    for (; p + (AT_ONCE - 1) * P.turns < P.to; p += AT_ONCE * P.turns) {
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u) load(u, p + u * P.turns, P.there(D, p + u * P.turns));
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u) use(u);
+#pragma unroll
+        for (int i = 0; i < CHUNK; ++i) {
+            one[i] += (g[0][i] + g[1][i]) + (g[2][i] + g[3][i]);
+            two[i] += (v[0][i] + v[1][i]) + (v[2][i] + v[3][i]);
+        }
+    }
+    for (; p < P.to; p += P.turns) {
+        const int n = P.there(D, p);
+        load(0, p, n);
+        use(0);
+#pragma unroll
+        for (int i = 0; i < CHUNK; ++i)
+            if (i < n) one[i] += g[0][i], two[i] += v[0][i];
+    }
+    __shared__ float2 room[CHUNK][BLOCK];
+    int half = 1;
+    while (half < P.turns) half *= 2;
+    for (half /= 2; half > 0; half /= 2) {
+        __syncthreads();
+        if (P.turn >= half && P.turn < 2 * half)
+#pragma unroll
+            for (int i = 0; i < CHUNK; ++i) room[i][threadIdx.x] = make_float2(one[i], two[i]);
+        __syncthreads();
+        if (P.turn < half && P.turn + half < P.turns)
+#pragma unroll
+            for (int i = 0; i < CHUNK; ++i) {
+                const float2 o = room[i][threadIdx.x + half * D.positions];
+                one[i] += o.x, two[i] += o.y;
+            }
+    }
+    if (P.turn == 0 && P.position < D.positions) {
+        float2 *const to = (float2 *)A.parts + ((P.item * D.strips + P.strip) * D.positions + P.position) * CHUNK;
+#pragma unroll
+        for (int i = 0; i < CHUNK; ++i) to[i] = make_float2(one[i], two[i]);
+    }
+}
+
+// A group, a block each: its channels' sums over the item, to channel_sums [items][channels][2], and the means over the group of du weight and du weight h.
+__global__ __launch_bounds__(BLOCK) void k_group_coefficients(group_args A, double *channel_sums, float *coefficients)
+{
+    const dealing &D = A.deal;
+    __shared__ double room[2][BLOCK];
+    const int64_t unit = A.first + blockIdx.x, item = unit / D.groups;
+    const int group = (int)(unit % D.groups);
+    const float2 *const from = (const float2 *)A.parts + item * D.strips * D.positions * CHUNK;
+    const int wide = D.size < BLOCK ? D.size : BLOCK, high = BLOCK / wide, col = threadIdx.x % wide, row = threadIdx.x / wide;
+    const int64_t entries = (int64_t)D.strips * D.rows;
+    double one = 0.0, two = 0.0;
+    for (int c0 = 0; c0 < D.size; c0 += wide) {
+        const int c = c0 + col, channel = group * D.size + c;
+        double a = 0.0, b = 0.0;
+        if (c < D.size && row < high)
+            for (int64_t e = row; e < entries; e += high) {
+                const float2 s = from[e / D.rows * D.positions * CHUNK + e % D.rows * D.channels + channel];
+                a += s.x, b += s.y;
+            }
+        __syncthreads();
+        room[0][threadIdx.x] = a, room[1][threadIdx.x] = b;
+        __syncthreads();
+        if (row == 0 && c < D.size) {
+            for (int r = 1; r < high; ++r) a += room[0][r * wide + col], b += room[1][r * wide + col];
+            double *const to = channel_sums + (item * D.channels + channel) * 2;
+            to[0] = a, to[1] = b;
+            const double w = A.weight ? value_at(A.weight, A.weight_type, channel) : 1.0f;
+            one += w * a, two += w * b;
+        }
+    }
+    __syncthreads();
+    room[0][threadIdx.x] = row == 0 ? one : 0.0, room[1][threadIdx.x] = row == 0 ? two : 0.0;
+    __syncthreads();
+    for (int half = BLOCK / 2; half > 0; half /= 2) {
+        if ((int)threadIdx.x < half) room[0][threadIdx.x] += room[0][threadIdx.x + half], room[1][threadIdx.x] += room[1][threadIdx.x + half];
+        __syncthreads();
+    }
+    if (threadIdx.x < 2) coefficients[unit * 2 + threadIdx.x] = (float)(room[threadIdx.x][0] / ((double)D.voxels * D.size));
+}
+
+// grad_weight, grad_bias: the channels' sums over the items.
+template <int WTYPE> __global__ __launch_bounds__(BLOCK) void k_group_weights(const double *channel_sums, int64_t items, int channels, void *grad_weight, void *grad_bias)
+{
+    using raw = typename element<WTYPE>::raw;
+    const int c = blockIdx.x * BLOCK + threadIdx.x;
+    if (c >= channels) return;
+    double one = 0.0, two = 0.0;
+#pragma unroll 4
+    for (int64_t n = 0; n < items; ++n) one += channel_sums[(n * channels + c) * 2], two += channel_sums[(n * channels + c) * 2 + 1];
+    if (grad_bias) ((raw *)grad_bias)[c] = element<WTYPE>::from_float((float)one);
+    if (grad_weight) ((raw *)grad_weight)[c] = element<WTYPE>::from_float((float)two);
+}
+
+template <int TYPE, int ACTIVATION> __global__ __launch_bounds__(BLOCK) void k_group_grad(group_args A)
+{
+    const dealing &D = A.deal;
+    const part P(D);
+    using raw = typename element<TYPE>::raw;
+    const raw *const x = (const raw *)A.x.data + P.item * A.x.item, *const grad = (const raw *)A.grad.data + P.item * A.grad.item;
+    raw *const out = (raw *)A.out + P.item * D.voxels * D.channels;
+    const known K(A, P);
+    float one[CHUNK], two[CHUNK];
+#pragma unroll
+    for (int i = 0; i < CHUNK; ++i) {
+        const int64_t g = (P.item * D.groups + (i < P.count ? P.channel(D, i) : 0) / D.size) * 2;
+        one[i] = A.coefficients[g], two[i] = A.coefficients[g + 1];
+    }
+    constexpr int AT_ONCE = 4;
+    float v[AT_ONCE][CHUNK], g[AT_ONCE][CHUNK];
+    over_periods<AT_ONCE>(D, P,
+                          [&](int u, int64_t p, int n) {
+                              load8<TYPE>(x, P.at(D, p, A.x.row), n, v[u]);
+                              load8<TYPE>(grad, P.at(D, p, A.grad.row), n, g[u]);
+                          },
+                          [&](int u, int64_t p, int n) {
+#pragma unroll
+                              for (int i = 0; i < CHUNK; ++i) {
+                                  const float du = g[u][i] * slope<ACTIVATION>(K.argument(v[u][i], i)) * K.weight[i];
+                                  v[u][i] = K.rstd[i] * (du - one[i] - (v[u][i] - K.mean[i]) * K.rstd[i] * two[i]);
+                              }
+                              store8<TYPE>(out, P.at(D, p, D.channels), n, v[u]);
+                          });
+}
+
+// ---- host side ----
+
+int64_t divisor(int64_t a, int64_t b) { return b ? divisor(b, a % b) : a; }
+
+// flat: rows of both arrays have no gaps.
+dealing dealing_of(int64_t items, int64_t voxels, int64_t channels, int64_t groups, bool flat)
+{
+    dealing D;
+    const int64_t common = divisor(channels, CHUNK);
+    D.voxels = voxels;
+    D.channels = (int32_t)channels, D.groups = (int32_t)groups, D.size = (int32_t)(channels / groups);
+    D.rows = flat ? (int32_t)(CHUNK / common) : 1;
+    D.positions = (int32_t)(D.rows > 1 ? channels / common : (channels + CHUNK - 1) / CHUNK);
+    D.periods = (voxels + D.rows - 1) / D.rows;
+    D.segments = (D.positions + BLOCK - 1) / BLOCK;
+    const int64_t turns = D.positions < BLOCK ? BLOCK / D.positions : 1;
+    // enough blocks for the chip, and no fewer than a few pieces of each thread
+    int64_t strips = 2048 / (items * D.segments > 0 ? items * D.segments : 1);
+    const int64_t most = D.periods / (turns * 2 * PIECE);
+    strips = strips < most ? strips : most;
+    strips = strips < 1 ? 1 : strips;
+    D.length = (D.periods + strips - 1) / strips;
+    D.length = (D.length + turns - 1) / turns * turns;
+    if (D.length < 1) D.length = 1;
+    D.strips = (int32_t)((D.periods + D.length - 1) / D.length);
+    if (D.strips < 1) D.strips = 1;
+    return D;
+}
+
+const char *bad_group(int64_t items, int64_t voxels, int64_t channels, int64_t groups)
+{
+    if (items < 0 || voxels < 0 || channels < 1) return "sizes must not be negative, and there are channels";
+    if (groups < 1 || channels % groups) return "channels must be a multiple of the groups";
+    if (channels > MOST_COLS || voxels > MOST_VALUES / channels || items > MOST_VALUES / channels / (voxels ? voxels : 1) || items > ((int64_t)1 << 31) / channels)
+        return "more than 2^20 channels, 2^42 values or 2^31 channels of items";
+    return nullptr;
+}
+
+const char *bad_distances(int64_t item, int64_t row, int64_t items, int64_t voxels, int64_t channels)
+{
+    if (item < 0 || item > ((int64_t)1 << 58) / (items + 1)) return "the distance of items is negative or reaches beyond what addresses hold";
+    return bad_stride(row, voxels, channels);
+}
+
+// Bytes of the parts, for the dealing that has more of them.
+int64_t parts_bytes(int64_t items, int64_t voxels, int64_t channels, int64_t groups, int64_t each)
+{
+    int64_t most = 0;
+    for (const bool flat : {false, true}) {
+        const dealing D = dealing_of(items, voxels, channels, groups, flat);
+        const int64_t n = items * D.strips * D.positions * CHUNK * each;
+        most = n > most ? n : most;
+    }
+    return (most + 15) / 16 * 16;
+}
+
+template <class F> int by_activation(int32_t activation, F &&f)
+{
+    if (activation == LEAP_SILU) return f(std::integral_constant<int, LEAP_SILU>{});
+    if (activation == LEAP_RELU) return f(std::integral_constant<int, LEAP_RELU>{});
+    return f(std::integral_constant<int, LEAP_LINEAR>{});
+}
+
+const char *bad_kinds(int32_t type, int32_t weight_type, int32_t activation)
+{
+    if (!known_type(type) || !known_type(weight_type)) return "unknown element type";
+    if (weight_type != type && weight_type != LEAP_F32) return "the weight must be float32 or of x's type";
+    return activation == LEAP_LINEAR || activation == LEAP_RELU || activation == LEAP_SILU ? nullptr : "unknown activation";
+}
+
+}  // namespace
+
+extern "C" int64_t leap_group_norm_work(int64_t items, int64_t voxels, int64_t channels, int64_t groups)
+{
+    if (bad_group(items, voxels, channels, groups) || !items || !voxels) return 0;
+    return parts_bytes(items, voxels, channels, groups, sizeof(moments)) + (items * groups * 8 + 15) / 16 * 16;
+}
+
+extern "C" int leap_group_norm(const void *d_x, int32_t type, int64_t x_item, int64_t x_row, const void *d_weight, const void *d_bias, int32_t weight_type, int64_t items,
+                               int64_t voxels, int64_t channels, int64_t groups, float eps, int32_t activation, void *d_y, float *d_stats, void *d_work,
+                               void *hip_stream)
+{
+    if (const char *why = bad_group(items, voxels, channels, groups)) return refuse(why);
+    if (const char *why = bad_kinds(type, weight_type, activation)) return refuse(why);
+    if (const char *why = bad_distances(x_item, x_row, items, voxels, channels)) return refuse(why);
+    if (!(eps >= 0.0f)) return refuse("eps must not be negative");
+    if (!items || !voxels) return LEAP_OK;
+    if (!d_x || !d_y) return refuse("null data pointer");
+    if (unaligned(d_work)) return refuse(NO_WORK);
+    const hipStream_t st = stream_of(hip_stream);
+    const bool flat = x_row == channels || voxels == 1;
+    group_args A{};
+    A.deal = dealing_of(items, voxels, channels, groups, flat);
+    A.x = {d_x, x_item, x_row};
+    A.weight = d_weight, A.bias = d_bias, A.weight_type = weight_type, A.eps = eps, A.items = items;
+    A.parts = (float *)d_work, A.out = d_y;
+    A.stats = d_stats ? d_stats : (float *)((char *)d_work + parts_bytes(items, voxels, channels, groups, sizeof(moments)));
+    const int64_t blocks = items * A.deal.strips * A.deal.segments;
+    if (blocks >= (int64_t)1 << 24) return refuse("more than 2^24 blocks of items");
+    return by_type(type, [&](auto t) {
+        constexpr int T = decltype(t)::value;
+        hipLaunchKernelGGL((k_group_moments<T>), dim3((unsigned)blocks), dim3(BLOCK), 0, st, A);
+        int rc = launched();
+        if (rc == LEAP_OK)
+            rc = over_blocks(items * groups, [&](int64_t first, unsigned n) {
+                A.first = first;
+                hipLaunchKernelGGL(k_group_stats, dim3(n), dim3(BLOCK), 0, st, A);
+            });
+        if (rc != LEAP_OK) return rc;
+        return by_activation(activation, [&](auto a) {
+            hipLaunchKernelGGL((k_group_apply<T, decltype(a)::value>), dim3((unsigned)blocks), dim3(BLOCK), 0, st, A);
+            return launched();
+        });
+    });
+}
+
+extern "C" int64_t leap_group_norm_backward_work(int64_t items, int64_t voxels, int64_t channels, int64_t groups)
+{
+    if (bad_group(items, voxels, channels, groups)) return 0;
+    if (!items || !voxels) return 16;
+    return parts_bytes(items, voxels, channels, groups, 8) + items * channels * 16 + (items * groups * 8 + 15) / 16 * 16;
+}
+
+extern "C" int leap_group_norm_backward(const void *d_grad, int64_t grad_item, int64_t grad_row, const void *d_x, int32_t type, int64_t x_item, int64_t x_row,
+                                        const void *d_weight, const void *d_bias, int32_t weight_type, const float *d_stats, int64_t items, int64_t voxels,
+                                        int64_t channels, int64_t groups, int32_t activation, void *d_grad_x, void *d_grad_weight, void *d_grad_bias, void *d_work,
+                                        void *hip_stream)
+{
+    if (const char *why = bad_group(items, voxels, channels, groups)) return refuse(why);
+    if (const char *why = bad_kinds(type, weight_type, activation)) return refuse(why);
+    if (const char *why = bad_distances(x_item, x_row, items, voxels, channels)) return refuse(why);
+    if (const char *why = bad_distances(grad_item, grad_row, items, voxels, channels)) return refuse(why);
+    const bool some = items && voxels;
+    if (some && (!d_grad || !d_x || !d_stats)) return refuse("null data pointer");
+    if (unaligned(d_work)) return refuse(NO_WORK);
+    const hipStream_t st = stream_of(hip_stream);
+    group_args A{};
+    A.deal = dealing_of(items, voxels, channels, groups, (x_row == channels && grad_row == channels) || voxels == 1);
+    A.x = {d_x, x_item, x_row}, A.grad = {d_grad, grad_item, grad_row};
+    A.weight = d_weight, A.bias = d_bias, A.weight_type = weight_type, A.items = items;
+    A.stats = (float *)d_stats, A.parts = (float *)d_work, A.out = d_grad_x;
+    double *const channel_sums = (double *)((char *)d_work + parts_bytes(items, voxels, channels, groups, 8));
+    float *const coefficients = (float *)(channel_sums + items * channels * 2);
+    A.coefficients = coefficients;
+    const int64_t blocks = items * A.deal.strips * A.deal.segments;
+    if (blocks >= (int64_t)1 << 24) return refuse("more than 2^24 blocks of items");
+    int rc = LEAP_OK;
+    if (some)
+        rc = by_type(type, [&](auto t) {
+            constexpr int T = decltype(t)::value;
+            return by_activation(activation, [&](auto a) {
+                constexpr int ACT = decltype(a)::value;
+                hipLaunchKernelGGL((k_group_sums<T, ACT>), dim3((unsigned)blocks), dim3(BLOCK), 0, st, A);
+                int status = launched();
+                if (status == LEAP_OK)
+                    status = over_blocks(items * groups, [&](int64_t first, unsigned n) {
+                        A.first = first;
+                        hipLaunchKernelGGL(k_group_coefficients, dim3(n), dim3(BLOCK), 0, st, A, channel_sums, coefficients);
+                    });
+                if (status != LEAP_OK || !d_grad_x) return status;
+                hipLaunchKernelGGL((k_group_grad<T, ACT>), dim3((unsigned)blocks), dim3(BLOCK), 0, st, A);
+                return launched();
+            });
+        });
+    if (rc != LEAP_OK || !(d_grad_weight || d_grad_bias)) return rc;
+    return by_type(weight_type, [&](auto w) {
+        hipLaunchKernelGGL((k_group_weights<decltype(w)::value>), dim3((unsigned)((channels + BLOCK - 1) / BLOCK)), dim3(BLOCK), 0, st, channel_sums,
+                           some ? items : 0, (int)channels, d_grad_weight, d_grad_bias);
+        return launched();
+    });
+}

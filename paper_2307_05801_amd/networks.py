@@ -5,6 +5,8 @@ its blocks, or keeps voxels with their channels last:
 
     positions, buckets = relative_buckets((16, 16, 16), near=4, codes=6)             # places of a volume's patches, once
     o = attention(q, k, v, table=table, positions=positions, buckets=buckets)        # q, k, v: [batch, patches, heads, width]
+    y = group_norm(x, 8, weight, bias, activation="silu")                            # x: [batch, nz, ny, nx, channels]
+    norm = GroupNorm(8, 64, activation="silu"); y = norm(x)                          # the same as a module
 
 Both are differentiable, run in libleap_hip.so on the current HIP stream, and take memory from PyTorch alone.  Tensors are on one GPU; the values of
 a row (the last dimension) are neighbours (else ValueError: `.contiguous()` them).  The same call gives the same bits.
@@ -196,3 +198,124 @@ def relative_buckets(shape, near: int, codes: int, device="cuda:0"):
         positions = (positions[:, None] * (2 * n - 1) + torch.arange(n, dtype=torch.int32)).flatten()
         buckets = (buckets[:, None] * many + axis).flatten()
     return positions.to(device), buckets.to(device)
+
+
+# ---- group norm ---------------------------------------------------------------------------------------------------------
+
+_ACTIVATIONS = {None: B.LEAP_LINEAR, "relu": B.LEAP_RELU, "silu": B.LEAP_SILU}
+
+
+def _voxels(t: torch.Tensor, what: str):
+    """(voxels, distance of items, of voxels) of [batch, ..., channels]; ValueError where an item's voxels are not evenly spaced."""
+    dims, strides, cols = t.shape, t.stride(), t.shape[-1]
+    if t.is_neg():
+        raise ValueError(f"{what} is a negated view, whose memory holds other values; call .resolve_neg()")
+    if t.is_contiguous():
+        voxels = math.prod(dims[1:-1])
+        return voxels, voxels * cols, cols
+    if strides[-1] == 1 or cols == 1:
+        voxels, step = 1, None
+        for n, s in zip(reversed(dims[1:-1]), reversed(strides[1:-1])):
+            if n == 0:
+                return 0, 0, cols
+            if n > 1:
+                if step is None:
+                    step = s
+                elif s != step * voxels:
+                    break
+                voxels *= n
+        else:
+            if step is None or step >= cols:
+                return voxels, strides[0], cols if step is None else step
+    raise ValueError(f"{what}: the channels of a voxel must be neighbours and an item's voxels evenly spaced; call .contiguous()")
+
+
+def _norm_parameter(w, x, what: str):
+    if w is not None:
+        _on_gpu(w, what, x.device)
+        if w.shape != (x.shape[-1],) or not w.is_contiguous() or w.is_neg() or (w.dtype is not torch.float32 and w.dtype is not x.dtype):
+            raise ValueError(f"{what} must be contiguous [{x.shape[-1]}], float32 or {x.dtype}")
+
+
+def _norm_forward(x, groups, weight, bias, activation, eps, keep):
+    """(y, statistics)"""
+    device, batch, channels = x.device, x.shape[0], x.shape[-1]
+    voxels, item, row = _voxels(x, "x")
+    y = torch.empty(x.shape, dtype=x.dtype, device=device)
+    stats = torch.empty((batch, groups, 2), dtype=torch.float32, device=device) if keep else None
+    work = _work(_library().leap_group_norm_work(batch, voxels, channels, groups), device)
+    parameter = weight if weight is not None else bias
+    _call("leap_group_norm", device, x.data_ptr(), _TYPES[x.dtype], item, row, _address(weight), _address(bias),
+          B.LEAP_F32 if parameter is None else _TYPES[parameter.dtype], batch, voxels, channels, groups, eps, activation, y.data_ptr(), _address(stats), _address(work))
+    return y, stats
+
+
+class _GroupNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, bias, groups, activation, eps):
+        y, stats = _norm_forward(x, groups, weight, bias, activation, eps, True)
+        ctx.save_for_backward(x, weight, bias, _bytes(stats))          # hooks may pack x
+        ctx.groups, ctx.activation = groups, activation
+        return y
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, grad):
+        x, weight, bias, stats = ctx.saved_tensors
+        need_x, need_weight, need_bias = ctx.needs_input_grad[:3]
+        device, batch, channels = x.device, x.shape[0], x.shape[-1]
+        try:
+            _, grad_item, grad_row = _voxels(grad, "grad")
+        except ValueError:
+            grad = grad.resolve_neg().contiguous()
+            _, grad_item, grad_row = _voxels(grad, "grad")
+        voxels, item, row = _voxels(x, "x")
+        grad_x = torch.empty(x.shape, dtype=x.dtype, device=device) if need_x else None
+        grad_weight = torch.empty_like(weight) if need_weight else None
+        grad_bias = torch.empty_like(bias) if need_bias else None
+        work = _work(_library().leap_group_norm_backward_work(batch, voxels, channels, ctx.groups), device)
+        parameter = weight if weight is not None else bias
+        _call("leap_group_norm_backward", device, grad.data_ptr(), grad_item, grad_row, x.data_ptr(), _TYPES[x.dtype], item, row, _address(weight), _address(bias),
+              B.LEAP_F32 if parameter is None else _TYPES[parameter.dtype], stats.data_ptr(), batch, voxels, channels, ctx.groups, ctx.activation, _address(grad_x),
+              _address(grad_weight), _address(grad_bias), work.data_ptr())
+        return grad_x, grad_weight, grad_bias, None, None, None
+
+
+def group_norm(x: torch.Tensor, groups: int, weight: torch.Tensor = None, bias: torch.Tensor = None, activation: str = None, eps: float = 1e-5) -> torch.Tensor:
+    """activation((x - mean) * rstd * weight + bias), differentiable in x, weight and bias; mean and rstd = 1 / sqrt(variance + eps) over an item's voxels and a
+    group's channels.
+
+    x: float32, bfloat16 or float16 [batch, ..., channels], channels last (a torch tensor in a channels-last memory format: x.movedim(1, -1)); groups divide the
+    channels, each of neighbouring ones; weight, bias: [channels], x's type or float32, both of one type; activation: None, "relu" or "silu" (u * sigmoid(u)).
+    Kept for the backward pass: x, which may be packed (activations.keep_in_8_bits: the gradients are then those of the values held), and two floats a group."""
+    _on_gpu(x, "x")
+    if x.dtype not in _TYPES or x.dim() < 2 or x.shape[-1] < 1:
+        raise ValueError(f"x must be float32, bfloat16 or float16 [batch, ..., channels], got {x.dtype} {tuple(x.shape)}")
+    if groups < 1 or x.shape[-1] % groups:
+        raise ValueError(f"{groups} groups do not divide {x.shape[-1]} channels")
+    if activation not in _ACTIVATIONS:
+        raise ValueError(f"activation must be None, 'relu' or 'silu', not {activation!r}")
+    if not eps >= 0.0:
+        raise ValueError(f"eps must not be negative, got {eps}")
+    _norm_parameter(weight, x, "weight")
+    _norm_parameter(bias, x, "bias")
+    if weight is not None and bias is not None and weight.dtype is not bias.dtype:
+        raise ValueError(f"weight and bias must be of one type, got {weight.dtype} and {bias.dtype}")
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (x, weight, bias)):
+        return _GroupNorm.apply(x, weight, bias, groups, _ACTIVATIONS[activation], eps)
+    return _norm_forward(x, groups, weight, bias, _ACTIVATIONS[activation], eps, False)[0]
+
+
+class GroupNorm(torch.nn.Module):
+    """group_norm with a weight and a bias of its own (float32)."""
+
+    def __init__(self, groups: int, channels: int, activation: str = None, eps: float = 1e-5, device="cuda:0"):
+        super().__init__()
+        if groups < 1 or channels % groups:
+            raise ValueError(f"{groups} groups do not divide {channels} channels")
+        self.groups, self.activation, self.eps = groups, activation, eps
+        self.weight = torch.nn.Parameter(torch.ones(channels, device=device))
+        self.bias = torch.nn.Parameter(torch.zeros(channels, device=device))
+
+    def forward(self, x: torch.Tensor) -> torch.Tensor:
+        return group_norm(x, self.groups, self.weight, self.bias, self.activation, self.eps)

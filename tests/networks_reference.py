@@ -91,3 +91,62 @@ class Attention:
             self.grad_table = by_bucket(ds)
             # sums of a bucket's pairs: within a block in 32 bits, blocks in 64
             self.grad_table_off = by_bucket(off_ds + sum_error(queries + keys) * ds.abs()) + half_step(table.dtype) * self.grad_table.abs()
+
+
+def _slope(u, activation):
+    s = torch.sigmoid(u)
+    return s * (1 + u * (1 - s)) if activation == "silu" else (u > 0).double() if activation == "relu" else torch.ones_like(u)
+
+
+class GroupNorm:
+    """The values and bounds of one call: y, grad_x, grad_weight, grad_bias and the same names + "_off"; x [batch, ..., channels].
+
+    A value's difference to the mean is off by the roundings of both, half a unit each, of the largest value's size, and the mean by what joining pieces adds: 2^-22 of the
+    largest in all.  The variance's relative error is twice that of the differences, over the deviation, and the roundings of the sums (pieces of eight, a
+    thread's few hundred, a block's).  sigmoid is good to (3 + |u|) 2^-24 or so, and its slope's slope is at most 1/2."""
+
+    def __init__(self, x, groups, weight=None, bias=None, activation=None, eps=1e-5, grad=None):
+        shape, dtype = x.shape, x.dtype
+        batch, channels = shape[0], shape[-1]
+        size, unit = channels // groups, 2.0 ** -24
+        x = x.double().reshape(batch, -1, groups, size)
+        voxels = x.shape[1]
+        w, b = (torch.full((channels,), d, dtype=torch.float64) if t is None else t.double() for t, d in ((weight, 1.0), (bias, 0.0)))
+        w, b = w.view(groups, size), b.view(groups, size)
+        if voxels == 0 or batch == 0:
+            self.y = self.grad_x = self.y_off = self.grad_x_off = torch.zeros(shape, dtype=torch.float64)
+            self.grad_weight = self.grad_bias = self.grad_weight_off = self.grad_bias_off = torch.zeros(channels, dtype=torch.float64)
+            return
+        mean = x.mean((1, 3), keepdim=True)
+        rstd = 1 / torch.sqrt((x - mean).square().mean((1, 3), keepdim=True) + eps)
+        h = (x - mean) * rstd
+        u = h * w + b
+        s = torch.sigmoid(u)
+        y = u * s if activation == "silu" else torch.relu(u) if activation == "relu" else u
+        off_d = 4 * unit * x.abs().amax((1, 3), keepdim=True)
+        off_r = off_d * rstd + sum_error(min(voxels, 512))
+        off_h = off_d * rstd + h.abs() * (off_r + 4 * unit)
+        off_u = w.abs() * off_h + 4 * unit * ((h * w).abs() + b.abs())
+        near = (8 + u.abs()) * unit if activation == "silu" else 0.0
+        self.y, self.y_off = y.reshape(shape), (1.1 * off_u + (near + half_step(dtype)) * y.abs()).reshape(shape)
+        if grad is None:
+            return
+        g = grad.double().reshape(x.shape)
+        du = g * _slope(u, activation)
+        bend = 0.5 * off_u + near if activation == "silu" else (u.abs() <= off_u).double() if activation == "relu" else 0.0     # either side of relu's bend
+        off_du = g.abs() * bend + 2 * unit * du.abs()
+        parameter = dtype if weight is None and bias is None else (weight if weight is not None else bias).dtype
+        many = sum_error(min(batch * voxels, 2048))
+        one, two = du.sum((0, 1)), (du * h).sum((0, 1))
+        off_one = (off_du + many * du.abs()).sum((0, 1))
+        off_two = (off_du * h.abs() + du.abs() * off_h + many * (du * h).abs()).sum((0, 1))
+        self.grad_bias, self.grad_bias_off = one.flatten(), (off_one + half_step(parameter) * one.abs()).flatten()
+        self.grad_weight, self.grad_weight_off = two.flatten(), (off_two + half_step(parameter) * two.abs()).flatten()
+        d = du * w
+        first, second = d.mean((1, 3), keepdim=True), (d * h).mean((1, 3), keepdim=True)
+        off_first = ((off_du + many * du.abs()) * w.abs()).mean((1, 3), keepdim=True)
+        off_second = ((off_du * h.abs() + du.abs() * off_h + many * (du * h).abs()) * w.abs()).mean((1, 3), keepdim=True)
+        grad_x = rstd * (d - first - h * second)
+        size_ = d.abs() + first.abs() + (h * second).abs()
+        off = rstd * (off_du * w.abs() + off_first + h.abs() * off_second + off_h * second.abs() + (8 * unit + off_r) * size_)
+        self.grad_x, self.grad_x_off = grad_x.reshape(shape), (off + half_step(dtype) * grad_x.abs()).reshape(shape)

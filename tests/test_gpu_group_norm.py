@@ -1,0 +1,255 @@
+"""Group norm on the GPU against its definition in 64 bits (tests/networks_reference.py says how far a kernel may be off)."""
+import gc
+
+import pytest
+import torch
+
+import networks_reference as R
+from activations_reference import assert_close
+
+pytestmark = pytest.mark.gpu
+
+BF16, F16, F32 = torch.bfloat16, torch.float16, torch.float32
+
+
+@pytest.fixture(scope="module")
+def N():
+    from paper_2307_05801_amd import networks
+    return networks
+
+
+def rand(shape, seed, dtype=F32):
+    return torch.randn(*shape, generator=torch.Generator().manual_seed(seed)).to(dtype)
+
+
+def inputs(shape, dtype, seed, parameter=None):
+    """x with channels of different size and mean, weight, bias, gradient."""
+    c = shape[-1]
+    x = rand(shape, seed) * torch.exp(0.5 * rand((c,), seed + 1)) + rand((c,), seed + 2)
+    parameter = dtype if parameter is None else parameter
+    return x.to(dtype), (1 + 0.3 * rand((c,), seed + 3)).to(parameter), (0.3 * rand((c,), seed + 4)).to(parameter), rand(shape, seed + 5, dtype)
+
+
+def run(N, x, groups, weight, bias, grad, activation, eps=1e-5):
+    leaves = [t.cuda().detach().requires_grad_(True) for t in (x, weight, bias) if t is not None]
+    rest = iter(leaves[1:])
+    y = N.group_norm(leaves[0], groups, *(None if t is None else next(rest) for t in (weight, bias)), activation=activation, eps=eps)
+    got = iter(torch.autograd.grad(y, leaves, grad.cuda()))
+    return (y.detach(), next(got), *(None if t is None else next(got) for t in (weight, bias)))
+
+
+def check(got, r):
+    for name, t in zip(("y", "grad_x", "grad_weight", "grad_bias"), got):
+        if t is not None:
+            assert_close(t, getattr(r, name), getattr(r, name + "_off"), name)
+
+
+SHAPES = [((1, 1, 8), 1), ((1, 1, 6), 2), ((2, 3, 1), 1), ((2, 50, 3), 3), ((3, 7, 5), 1), ((1, 1000, 5), 5), ((2, 333, 20), 4), ((2, 64, 64), 8), ((1, 4097, 12), 3), ((2, 10, 11, 12, 16), 4),
+          ((1, 77, 343), 7), ((1, 40, 512), 32), ((2, 33, 2100), 7), ((1, 9, 4096), 2), ((2, 5, 2051), 1), ((5, 17000, 8), 2), ((1, 70001, 7), 7), ((40, 300, 24), 3), ((3, 2, 96), 96), ((700, 9), 3)]
+
+
+@pytest.mark.parametrize("shape,groups", SHAPES)
+@pytest.mark.parametrize("dtype,activation", [(F32, "silu"), (BF16, None), (F16, "relu"), (BF16, "silu")])
+def test_shapes(N, shape, groups, dtype, activation):
+    x, w, b, g = inputs(shape, dtype, 1)
+    check(run(N, x, groups, w, b, g, activation), R.GroupNorm(x, groups, w, b, activation, 1e-5, g))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+@pytest.mark.parametrize("activation", [None, "relu", "silu"])
+def test_parameters(N, dtype, activation):
+    """Weights in 32 bits or of x's type, one of them or none."""
+    x, w, b, g = inputs((2, 100, 24), dtype, 11, F32)
+    for weight, bias in ((w, b), (w, None), (None, b), (None, None)):
+        check(run(N, x, 4, weight, bias, g, activation), R.GroupNorm(x, 4, weight, bias, activation, 1e-5, g))
+
+
+@pytest.mark.parametrize("offset", [10.0, 1000.0, 30000.0])
+def test_a_mean_far_larger_than_the_deviation(N, offset):
+    x, w, b, g = inputs((2, 3000, 16), F32, 21)
+    x = x + offset
+    x[:, 0] = -offset                                                # and a first voxel that is far from it
+    check(run(N, x, 2, w, b, g, "silu"), R.GroupNorm(x, 2, w, b, "silu", 1e-5, g))
+
+
+def test_values_all_alike(N):
+    """A variance of zero: the bias comes out."""
+    x, b = torch.full((2, 70, 8), 3.25), rand((8,), 31)
+    y, gx, gw, gb = run(N, x, 2, torch.ones(8), b, torch.ones(2, 70, 8), None)
+    assert torch.equal(y.cpu(), b.expand(2, 70, 8)) and torch.isfinite(gx).all() and not gw.any() and torch.equal(gb.cpu(), torch.full((8,), 140.0))
+
+
+def test_what_is_not_a_number_stays_in_its_group(N):
+    x, w, b, g = inputs((2, 40, 12), F32, 41)
+    for what in (float("nan"), float("inf")):
+        x[1, 7, 5] = what
+        for activation in (None, "relu", "silu"):
+            bad = torch.zeros(x.shape, dtype=torch.bool)
+            bad[1, :, 4:8] = True
+            y, gx, _, _ = run(N, x, 3, w, b, g, activation)
+            assert torch.equal(torch.isnan(y.cpu()), bad) and not torch.isnan(gx.cpu()[~bad]).any()
+
+
+@pytest.mark.parametrize("shape,groups", [((2, 30, 20), 4), ((1, 500, 64), 8), ((3, 10, 7), 1)])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_rows_of_a_wider_array(N, shape, groups, dtype):
+    """x and the gradient as columns of something wider, from any byte on; items in another order; one without gaps and one with."""
+    wide = shape[:-1] + (shape[-1] + 5,)
+    (x, w, b, g), r = inputs(shape, dtype, 51), None
+    r = R.GroupNorm(x, groups, w, b, "silu", 1e-5, g)
+
+    def within(t):
+        to = torch.zeros(wide, dtype=dtype, device="cuda")
+        to[..., 3:3 + shape[-1]] = t.cuda()
+        return to[..., 3:3 + shape[-1]]
+
+    for a, c in ((within(x), within(g)), (within(x), g.cuda()), (x.cuda(), within(g))):
+        check(run(N, a, groups, w, b, c, "silu"), r)
+    across = x.cuda().transpose(0, 1).contiguous().transpose(0, 1)
+    check(run(N, across, groups, w, b, g, "silu"), r)
+
+
+def test_channels_last_memory_of_torch(N):
+    x, w, b, g = inputs((2, 4, 5, 6, 16), BF16, 61)
+    r = R.GroupNorm(x, 4, w, b, "silu", 1e-5, g)
+    t = x.cuda().movedim(-1, 1).contiguous(memory_format=torch.channels_last_3d)
+    check(run(N, t.movedim(1, -1), 4, w, b, g, "silu"), r)
+
+
+def test_a_gradient_of_one_number(N):
+    """The gradient of a sum, which has distance 0, and one that lies across."""
+    x, w, b, g = inputs((2, 30, 16), F32, 71)
+    leaf = x.cuda().requires_grad_(True)
+    got, = torch.autograd.grad(N.group_norm(leaf, 4, w.cuda(), b.cuda(), activation="silu").sum(), leaf)
+    r = R.GroupNorm(x, 4, w, b, "silu", 1e-5, torch.ones(x.shape))
+    assert_close(got, r.grad_x, r.grad_x_off)
+    r = R.GroupNorm(x, 4, w, b, "silu", 1e-5, g)
+    check(run(N, x, 4, w, b, g.transpose(1, 2).contiguous().transpose(1, 2), "silu"), r)
+
+
+@pytest.mark.parametrize("shape", [(0, 5, 8), (2, 0, 8), (0, 0, 8)])
+def test_nothing_to_norm(N, shape):
+    x, w, b, g = inputs(shape, BF16, 81)
+    y, gx, gw, gb = run(N, x, 2, w, b, g, "silu")
+    assert y.shape == shape and gx.shape == shape and not gw.any() and not gb.any()
+
+
+def test_without_a_backward_pass_and_one_by_one(N):
+    x, w, b, g = (t.cuda() for t in inputs((2, 5000, 24), F32, 91))
+    want = run(N, x, 3, w, b, g, "silu")
+    with torch.no_grad():
+        assert torch.equal(N.group_norm(x, 3, w, b, "silu"), want[0])
+    for i in range(3):
+        leaves = [t.detach().requires_grad_(j == i) for j, t in enumerate((x, w, b))]
+        got, = torch.autograd.grad(N.group_norm(leaves[0], 3, *leaves[1:], "silu"), leaves[i], g)
+        assert torch.equal(got, want[1 + i])
+    module = N.GroupNorm(3, 24, "silu")
+    assert torch.equal(module(x), N.group_norm(x, 3, module.weight, module.bias, "silu"))
+
+
+def test_kept_in_8_bits(N):
+    """x packed between the passes: the gradients are those of the values held, with the statistics of the forward pass; a quarter of the memory."""
+    from paper_2307_05801_amd import activations as A
+    x, w, b, g = (t.cuda() for t in inputs((2, 4096, 64), F32, 101))
+    leaf = x.clone().requires_grad_(True)
+
+    def step():
+        moved = leaf * 1.0
+        gc.collect()
+        before = torch.cuda.memory_allocated()
+        y = N.group_norm(moved, 8, w, b, "silu")
+        moved = None
+        return y, torch.cuda.memory_allocated() - before - y.numel() * 4, y
+
+    with A.keep_in_8_bits():
+        y, room, _ = step()
+    assert room < -x.numel() * 4 + 1.1 * x.numel() + 4096               # x itself is gone
+    got, = torch.autograd.grad(y, leaf, g)
+    held = A.pack8(x).unpack(F32).reshape(2, -1, 8, 8).double()
+    whole = x.double().reshape(2, -1, 8, 8)
+    mean = whole.mean((1, 3), keepdim=True)
+    rstd = 1 / torch.sqrt((whole - mean).square().mean((1, 3), keepdim=True) + 1e-5)
+    h, w8, b8 = (held - mean) * rstd, w.double().view(8, 8), b.double().view(8, 8)
+    du = g.double().reshape(h.shape) * R._slope(h * w8 + b8, "silu") * w8
+    want = rstd * (du - du.mean((1, 3), keepdim=True) - h * (du * h).mean((1, 3), keepdim=True))
+    assert (got.double() - want.reshape(x.shape)).norm() <= 2.0 ** -18 * want.norm()
+
+
+def test_what_is_kept_is_freed_and_watched(N):
+    x, w, b, _ = (t.cuda() for t in inputs((2, 500, 64), F32, 111))
+    w.requires_grad_(True)
+    gc.collect()
+    gc.disable()
+    try:
+        before = torch.cuda.memory_allocated()
+        for turn in range(3):
+            y = N.group_norm(x, 8, w, b, "silu")                        # its backward pass never runs
+            del y
+        assert torch.cuda.memory_allocated() == before
+    finally:
+        gc.enable()
+    y = N.group_norm(x, 8, w, b)
+    x.mul_(2.0)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.sum().backward()
+
+
+def test_another_stream_and_graph_replays(N):
+    x, w, b, g = (t.cuda() for t in inputs((3, 5000, 20), BF16, 121))
+
+    def step(x, w, b, g):
+        leaves = [t.detach().requires_grad_(True) for t in (x, w, b)]
+        y = N.group_norm(leaves[0], 4, *leaves[1:], "silu")
+        return [y.detach(), *torch.autograd.grad(y, leaves, g)]
+
+    want = step(x, w, b, g)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = step(x, w, b, g)
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, c) for a, c in zip(got, want))
+    del got
+    places, graphs = [[t.clone() for t in (x, w, b, g)] for _ in range(2)], []
+    for p in places:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            out = step(*p)
+        graphs.append((graph, out))
+    for turn in range(4):
+        graph, out = graphs[turn % 2]
+        new = [(t.float() * (1 + 0.01 * turn)).to(t.dtype) for t in (x, w, b, g)]
+        for at, n in zip(places[turn % 2], new):
+            at.copy_(n)
+        for t in out:
+            t.zero_()
+        graph.replay()
+        want = step(*new)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, c) for a, c in zip(out, want)), turn
+
+
+def test_refusals(N):
+    x, w = torch.zeros(2, 5, 8, device="cuda"), torch.ones(8, device="cuda")
+    good = dict(x=x, groups=2, weight=w, bias=w)
+    N.group_norm(**good)
+    for change in (dict(x=x.double()), dict(x=x.int()), dict(x=x[0, 0]), dict(x=x.transpose(1, 2)), dict(x=torch._neg_view(x)), dict(x=x[..., :0], groups=1), dict(groups=3), dict(groups=0), dict(activation="gelu"),
+                   dict(eps=-1.0), dict(eps=float("nan")), dict(weight=w[:4]), dict(weight=w.half()), dict(weight=w.cpu()), dict(bias=w.double()), dict(weight=w.expand(2, 8)),
+                   dict(x=x.half(), weight=w.half()), dict(weight=torch._neg_view(w)), dict(x=torch.zeros(2, 3, 5, 8, device="cuda").transpose(1, 2))):
+        with pytest.raises(ValueError):
+            N.group_norm(**{**good, **change})
+
+
+def test_many_voxels(N):
+    """More values than 2^31: the ends against the definition (sums of all values in 64 bits)."""
+    voxels, channels = (1 << 26) + 3, 33
+    x = torch.empty(1, voxels, channels, dtype=BF16, device="cuda").normal_(generator=torch.Generator(device="cuda").manual_seed(131))
+    y = N.group_norm(x, 3)
+    for group in range(3):
+        sums = [[f(x[0, at:at + (1 << 22), group * 11:group * 11 + 11].double()) for at in range(0, voxels, 1 << 22)] for f in (torch.sum, lambda t: t.square().sum())]
+        mean, square = (float(torch.stack(s).sum()) / (voxels * 11) for s in sums)
+        rstd = (square - mean * mean + 1e-5) ** -0.5
+        for at in (slice(0, 3), slice(voxels - 3, voxels), slice(1 << 25, (1 << 25) + 3)):
+            want = (x[0, at, group * 11:group * 11 + 11].double() - mean) * rstd
+            assert ((y[0, at, group * 11:group * 11 + 11].double() - want).abs() <= (R.HALF + 1e-5) * want.abs() + 1e-6).all()

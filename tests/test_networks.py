@@ -127,3 +127,42 @@ def test_the_references_gradients_are_those_of_differences():
             ends = [value(*(s * h * way + u if u is t else u for u in (q, k, v, table))) for s in (1, -1)]
             got, want = (getattr(r, name) * way).sum(), (ends[0] - ends[1]) / (2 * h)
             assert abs(got - want) <= 1e-7 * (1 + abs(want)), name
+
+
+# ---- group norm ----
+
+
+def test_bad_arguments_of_group_norm_are_refused_with_a_message(lib):
+    good = (P, 1, 640, 64, P, P, 1, 2, 10, 64, 8, 1e-5, 2, P, P, P, None)
+    for at, value in [(0, 0), (1, 3), (2, -1), (3, 63), (3, -1), (6, 2), (6, 7), (7, -1), (7, 1 << 40), (8, -1), (8, 1 << 40), (9, 0), (9, 1 << 21), (10, 0), (10, 7), (11, -1.0), (11, float("nan")), (12, 3),
+                      (12, -1), (13, 0), (15, 0), (15, P + 8)]:
+        arguments = list(good)
+        arguments[at] = value
+        assert lib.leap_group_norm(*arguments) == B.LEAP_INVALID_ARG, (at, value)
+        assert lib.leap_last_error().decode()
+    good = (P, 640, 64, P, 1, 640, 64, P, P, 1, P, 2, 10, 64, 8, 2, P, P, P, P, None)
+    for at, value in [(0, 0), (1, -1), (2, 63), (3, 0), (4, 3), (5, -1), (6, 63), (9, 2), (10, 0), (11, -1), (12, -1), (13, 0), (14, 7), (15, 3), (19, 0), (19, P + 4)]:
+        arguments = list(good)
+        arguments[at] = value
+        assert lib.leap_group_norm_backward(*arguments) == B.LEAP_INVALID_ARG, (at, value)
+        assert lib.leap_last_error().decode()
+    assert lib.leap_group_norm_work(-1, 10, 64, 8) == 0 and lib.leap_group_norm_work(2, 10, 64, 7) == 0 and lib.leap_group_norm_backward_work(2, 10, 0, 1) == 0
+    assert lib.leap_group_norm(None, 1, 640, 64, None, None, 1, 0, 10, 64, 8, 1e-5, 2, None, None, None, None) == B.LEAP_OK
+    assert lib.leap_group_norm(None, 1, 0, 64, None, None, 1, 2, 0, 64, 8, 1e-5, 2, None, None, None, None) == B.LEAP_OK
+
+
+def test_group_norm_elsewhere_is_refused():
+    with pytest.raises(ValueError, match="GPU"):
+        N.group_norm(torch.zeros(1, 2, 8), 2)
+
+
+def test_the_group_norm_references_gradients_are_those_of_differences():
+    g = torch.Generator().manual_seed(2)
+    x, w, b, grad = (torch.randn(*s, generator=g, dtype=torch.float64) for s in ((2, 5, 6), (6,), (6,), (2, 5, 6)))
+    for activation in (None, "silu", "relu"):
+        r = R.GroupNorm(x, 2, w, b, activation, 1e-3, grad)
+        for name, t in (("grad_x", x), ("grad_weight", w), ("grad_bias", b)):
+            way, h = torch.randn(t.shape, generator=g, dtype=torch.float64), 1e-6
+            ends = [(R.GroupNorm(*(s * h * way + u if u is t else u for u in (x,)), 2, *(s * h * way + u if u is t else u for u in (w, b)), activation, 1e-3).y * grad).sum() for s in (1, -1)]
+            got, want = (getattr(r, name) * way).sum(), (ends[0] - ends[1]) / (2 * h)
+            assert abs(got - want) <= 1e-7 * (1 + abs(want)), (activation, name)
