@@ -24,6 +24,11 @@ struct rows_of {
     int64_t item, row, head;
 };
 
+// Positions of a tile's rows: the least and the largest, and whether every four (from a multiple of four on) are consecutive.
+struct place_range {
+    int32_t low, high, fours, none;
+};
+
 struct attention_args {
     rows_of q, k, v;
     int32_t batch, queries, keys, heads, kv_heads, width;
@@ -33,6 +38,11 @@ struct attention_args {
     const int32_t *bucket_of, *query_positions, *key_positions;
     int32_t table_type, offsets, buckets;
     float scale;
+    // in the workspace, with a table: a number for every difference of positions, in units of log2, heads `line` apart; its bucket; the positions of each TILE rows
+    float *lines;
+    int32_t *line_buckets;
+    place_range *query_places, *key_places;
+    int32_t line;
 };
 
 // A tile of TILE rows of DEEP values in shared memory, in 16-byte pieces.  The order of a row's pieces lets 16 neighbouring rows be read at one piece, and
@@ -64,37 +74,80 @@ template <int DEEP> struct rows_tile {
 
 // Eight values of a row of `width` from 8 chunk on, zeros beyond its end.  Nothing beyond the row is read: the last piece of a row
 // that does not end with it is the row's last eight values, moved.
+__device__ inline u32x4 moved(const u32x4 &v, int values)
+{
+    const uint64_t low = (uint64_t)v[1] << 32 | v[0], high = (uint64_t)v[3] << 32 | v[2];
+    const int s = values * 16;                                             // 16 .. 112
+    const uint64_t a = s < 64 ? low >> s | high << (64 - s) : high >> (s - 64), b = s < 64 ? high >> s : 0;
+    return u32x4{(uint32_t)a, (uint32_t)(a >> 32), (uint32_t)b, (uint32_t)(b >> 32)};
+}
 __device__ inline u32x4 row_piece(const uint16_t *row, int width, int chunk)
 {
     const int left = width - chunk * 8;
     u32x4 v = {0, 0, 0, 0};
-    if (left >= 8) {
-        __builtin_memcpy(&v, row + chunk * 8, 16);
-    } else if (left > 0) {
-        if (width >= 8) {
-            uint64_t w[2];
-            __builtin_memcpy(w, row + width - 8, 16);
-            const int s = (8 - left) * 16;                                 // 16 .. 112
-            const uint64_t low = s < 64 ? w[0] >> s | w[1] << (64 - s) : w[1] >> (s - 64), high = s < 64 ? w[1] >> s : 0;
-            v = u32x4{(uint32_t)low, (uint32_t)(low >> 32), (uint32_t)high, (uint32_t)(high >> 32)};
-        } else {
-            uint16_t e[8] = {};
-#pragma unroll
-            for (int i = 0; i < 7; ++i)
-                if (i < left) e[i] = row[i];
-            __builtin_memcpy(&v, e, 16);
+    if (width >= 8) {
+        if (left > 0) {
+            const int back = left < 8 ? 8 - left : 0;
+            __builtin_memcpy(&v, row + chunk * 8 - back, 16);
+            if (width % 8) v = back ? moved(v, back) : v;
         }
+    } else if (left > 0) {
+        uint16_t e[8] = {};
+#pragma unroll
+        for (int i = 0; i < 7; ++i)
+            if (i < left) e[i] = row[i];
+        __builtin_memcpy(&v, e, 16);
     }
     return v;
 }
 
-// A tile's pieces on their way from memory through the registers.
-template <int DEEP> struct staged {
+// Where a product's side along the width lies in a lane: eight values of its row a step.
+template <int STEPS> __device__ inline void load_side(bf16x8 (&side)[STEPS], const uint16_t *row, int width, bool there, int lane)
+{
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) side[s] = __builtin_bit_cast(bf16x8, there ? row_piece(row, width, s * 2 + lane / 32) : u32x4{0, 0, 0, 0});
+}
+
+// Tiles of one head's rows on their way to shared memory.  DIRECT: past the registers, where rows begin at multiples of 16 bytes, are whole
+// multiples of 8 values, and a tile spans less than 2^31 bytes.  Otherwise through them, so that land() puts down what fetch() has asked for.
+template <int DEEP, bool DIRECT> struct source;
+template <int DEEP> struct source<DEEP, true> {
     using tile = rows_tile<DEEP>;
+    static constexpr int PIECES = tile::BYTES / 1024, EACH = PIECES / WAVES;           // 1 KiB: a wave's fetch
+    static_assert(PIECES % WAVES == 0, "");
+    const uint8_t *base;
+    int64_t stride, end;                   // bytes from row to row; of the array from its first row on
+    uint32_t offset[EACH];                 // of a lane's 16 bytes from its tile's first row on; NOWHERE: not of the row
+
+    __device__ inline source(const uint16_t *rows, int64_t stride_, int64_t count, int width, int wave, int lane) : base((const uint8_t *)rows), stride(stride_ * 2)
+    {
+        end = (count - 1) * stride + width * 2;
+#pragma unroll
+        for (int e = 0; e < EACH; ++e) {
+            const int slot = (e * WAVES + wave) * 64 + lane, r = slot * 16 / tile::ROW, chunk = (tile::place(r, 0) - r * tile::ROW) / 16 ^ slot % (tile::ROW / 16);
+            offset[e] = chunk * 8 < width ? (uint32_t)(r * stride) + chunk * 16 : NOWHERE;
+        }
+    }
+    __device__ inline void fetch(int64_t first, uint64_t there, lds_byte *to, int wave, int lane) const
+    {
+        const u32x4 from = window{base + first * stride, end - first * stride, 0}.buffer();
+#pragma unroll
+        for (int e = 0; e < EACH; ++e) {
+            const int piece = e * WAVES + wave, r = (piece * 64 + lane) * 16 / tile::ROW;
+            fetch16(from, there >> r & 1 ? offset[e] : NOWHERE, to + piece * 1024);
+        }
+    }
+    __device__ inline void land(lds_byte *) const {}
+};
+template <int DEEP> struct source<DEEP, false> {
+    using tile = rows_tile<DEEP>;
+    const uint16_t *base;
+    int64_t stride;
+    int width;
     u32x4 piece[tile::EACH];
 
-    // Rows `first` on of an array's item and head; those whose bit is not set in `there` are zeros and are not read.
-    __device__ inline void fetch(const uint16_t *base, int64_t stride, int64_t first, uint64_t there, int width)
+    __device__ inline source(const uint16_t *rows, int64_t stride_, int64_t, int width_, int, int) : base(rows), stride(stride_), width(width_) {}
+    __device__ inline void fetch(int64_t first, uint64_t there, lds_byte *, int, int)
     {
 #pragma unroll
         for (int e = 0; e < tile::EACH; ++e) {
@@ -102,7 +155,7 @@ template <int DEEP> struct staged {
             piece[e] = there >> r & 1 ? row_piece(base + (first + r) * stride, width, chunk) : u32x4{0, 0, 0, 0};
         }
     }
-    __device__ inline void store(lds_byte *to) const
+    __device__ inline void land(lds_byte *to) const
     {
 #pragma unroll
         for (int e = 0; e < tile::EACH; ++e) {
@@ -112,12 +165,40 @@ template <int DEEP> struct staged {
     }
 };
 
+// All that fetch16 has asked for is in shared memory, of this wave; a barrier makes it so for the block.
+__device__ inline void fetched() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
 // Which of the rows first .. first + TILE - 1 there are: within `rows`, and in the mask (null: all).
 __device__ inline uint64_t rows_there(const uint8_t *mask, int64_t first, int64_t rows, int lane)
 {
     const bool in = first + lane < rows;
     return __ballot(in && (!mask || mask[first + lane]));
 }
+
+// The tiles of an item's keys that have any, one after the other; the mask's bytes are asked for a tile ahead.
+struct key_walk {
+    const uint8_t *mask;
+    int keys;
+    int64_t first;
+    uint64_t bits;
+    uint8_t ahead;
+
+    __device__ inline uint8_t ask(int64_t at, int lane) const { return at + lane < keys ? mask ? mask[at + lane] : 1 : 0; }
+    __device__ inline key_walk(const uint8_t *mask_, int keys_, int lane) : mask(mask_), keys(keys_), first(-TILE)
+    {
+        ahead = ask(0, lane);
+        next(lane);
+    }
+    __device__ inline void next(int lane)
+    {
+        do {
+            first += TILE;
+            bits = __ballot(ahead != 0);
+            ahead = ask(first + TILE, lane);
+        } while (!bits && first < keys);
+    }
+    __device__ inline bool done() const { return first >= keys; }
+};
 
 // Numbers of the table in units of log2; what is finite stays so.
 __device__ inline float table_value(const attention_args &A, int head, int bucket)
@@ -133,13 +214,62 @@ __device__ inline float table_value(const attention_args &A, int head, int bucke
 __device__ inline int query_position(const attention_args &A, int i) { return A.query_positions ? A.query_positions[i] : i; }
 __device__ inline int key_position(const attention_args &A, int j) { return A.key_positions ? A.key_positions[j] : j; }
 
-// The bucket of a pair, whatever its positions.
-__device__ inline int bucket_at(const attention_args &A, int difference)
+// The bucket of a line's number.
+__device__ inline int bucket_at(const attention_args &A, int64_t at)
 {
-    const int half = A.offsets / 2, d = difference < -half ? -half : difference > A.offsets - 1 - half ? A.offsets - 1 - half : difference;
-    const int b = A.bucket_of[d + half];
+    const int b = A.bucket_of[at];
     return b < 0 ? 0 : b >= A.buckets ? A.buckets - 1 : b;
 }
+
+// Register r of a lane's 32 rows stands for row row_of(r) + 4 (lane / 32).
+__device__ inline constexpr int row_of(int r) { return r / 4 * 8 + r % 4; }
+
+// Where in a line the difference of two positions is.
+__device__ inline int line_at(const attention_args &A, int key, int query)
+{
+    const int64_t at = (int64_t)key - query + A.offsets / 2;
+    return at < 0 ? 0 : at >= A.offsets ? A.offsets - 1 : (int)at;
+}
+
+// The part of a line that the pairs of two tiles' rows take: the numbers from `first` (a multiple of four) on, `count` of them.  `inside`: it is within the line and
+// MOST numbers, so that shared memory has it; otherwise pairs look theirs up in memory.
+struct line_window {
+    int first, count;
+    bool inside;
+};
+__device__ inline line_window window_of(const attention_args &A, const place_range &keys, const place_range &queries, int most)
+{
+    const int64_t low = (int64_t)keys.low - queries.high + A.offsets / 2, high = (int64_t)keys.high - queries.low + A.offsets / 2;
+    const int64_t first = low / 4 * 4;
+    return {(int)first, (int)(high - first + 1), low >= 0 && high < A.offsets && high - first < most};
+}
+__device__ inline place_range both(const place_range &a, const place_range &b) { return {a.low < b.low ? a.low : b.low, a.high > b.high ? a.high : b.high, a.fours & b.fours, 0}; }
+
+// Brings a window of 4-byte numbers to shared memory, a KiB a wave.
+__device__ inline void fetch_window(const void *line, int length, const line_window &w, lds_byte *to, int wave, int lane)
+{
+    const u32x4 from = window{(const uint8_t *)line, (int64_t)length * 4, 0}.buffer();
+    for (int piece = wave; piece * 256 < w.count; piece += WAVES) fetch16(from, (uint32_t)(w.first + piece * 256 + lane * 4) * 4, to + piece * 1024);
+}
+
+// f(r, number) for the sixteen pairs of a lane's position with the rows 8 a + 4 (lane / 32) + c of `places`.  The rows are keys (SIGN 1) or queries (-1).  at: the byte
+// in shared memory of a row at position 0.
+template <int SIGN, class F> __device__ inline void over_places(const int *places, bool fours, int at, int lane, F &&f)
+{
+    if (fours) {
+#pragma unroll
+        for (int a = 0; a < 4; ++a) {
+            const int begin = at + SIGN * 4 * places[a * 8 + lane / 32 * 4];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) f(a * 4 + c, begin + SIGN * 4 * c);
+        }
+    } else {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) f(r, at + SIGN * 4 * places[row_of(r) + lane / 32 * 4]);
+    }
+}
+__device__ inline float number_at(int address) { return *(__attribute__((address_space(3))) const float *)(uintptr_t)(uint32_t)address; }
+__device__ inline int address_of(const lds_byte *p) { return (int)(uint32_t)(uintptr_t)p; }
 
 __device__ inline bf16x8 eight(const f32x16 &v, int m)
 {
@@ -183,9 +313,6 @@ __device__ inline float column_max(float v)
     return both_halves(v, [](float a, float b) { return fmaxf(a, b); });
 }
 
-// Register r of a lane's 32 rows stands for row row_of(r) + 4 (lane / 32).
-__device__ inline constexpr int row_of(int r) { return r / 4 * 8 + r % 4; }
-
 // A lane's column of a [width][32] result, times `by`, to a row of `width` bfloat16; BLOCKS of 32 values.
 template <int BLOCKS> __device__ inline void store_column(uint16_t *row, int width, f32x16 (&v)[BLOCKS], float by, int lane, bool there)
 {
@@ -226,9 +353,23 @@ template <class F> inline int by_width(int64_t width, F &&f)
     return f(std::integral_constant<int, 128>{});
 }
 
+// f(flags as constants)
+template <class F> inline int by_flags(F &&f) { return f(); }
+template <class F, class... R> inline int by_flags(F &&f, bool flag, R... rest)
+{
+    if (flag) return by_flags([&](auto... c) { return f(std::true_type{}, c...); }, rest...);
+    return by_flags([&](auto... c) { return f(std::false_type{}, c...); }, rest...);
+}
+
 // Null if fine: an array's strides; a description.
 const char *bad_array(int64_t items, int64_t item, int64_t rows, int64_t row, int64_t heads, int64_t head);
 const char *bad_attention(const leap_attention_desc *d);
 attention_args arguments_of(const leap_attention_desc *d, const void *q, const void *k, const void *v);
+
+// Whether every row of an array is a whole number of aligned 16 bytes and a tile of them within a buffer's reach.
+bool direct_array(const void *p, int64_t item, int64_t row, int64_t head, int64_t width);
+// The lines' workspace, and what writes it; nothing without a table.
+int64_t lines_bytes(const leap_attention_desc *d);
+int write_lines(attention_args &A, void *work, hipStream_t st);
 
 }  // namespace net

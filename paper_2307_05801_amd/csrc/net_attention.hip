@@ -9,6 +9,10 @@ namespace {
 
 using namespace net;
 
+// Numbers of a line in shared memory for a tile's pairs: 191 are enough for rows one after the other, a few hundred on a grid, and 1500 where a tile has the end of one plane
+// of 27 x 22 patches and the next one's beginning.  As many as leave a compute unit room for two blocks.
+constexpr int window_of_tile(int deep) { return deep > 64 ? 1024 : 2048; }
+
 // What becomes of a query beside o.
 struct forward_args {
     attention_args a;
@@ -21,51 +25,63 @@ struct forward_args {
 // would spoil all of the query's alike, and in grad_q that adds up along what the keys have in common (keys and values with a common part as large as what
 // differs, 512 keys: grad_q was 0.020 of its norm off, with four times as large a part 0.34; now 0.003 and 0.007, which is the rounding of ds).  So there the
 // probabilities are the sum of two bfloat16, and what o's rounding leaves is kept.
-template <int DEEP, bool BIAS, bool FINE> __global__ __launch_bounds__(BLOCK) void k_attention(forward_args F)
+template <int DEEP, bool DIRECT, bool BIAS, bool FINE> __global__ __launch_bounds__(BLOCK, 2) void k_attention(forward_args F)
 {
     using tile = rows_tile<DEEP>;
-    constexpr int STEPS = DEEP / 16, BLOCKS = DEEP / 32;
+    constexpr int STEPS = DEEP / 16, BLOCKS = DEEP / 32, WINDOW = window_of_tile(DEEP);
     const attention_args &A = F.a;
-    __shared__ __attribute__((aligned(16))) uint8_t room[4 * tile::BYTES];
+    __shared__ __attribute__((aligned(16))) uint8_t room[4 * tile::BYTES + (BIAS ? 2 * WINDOW * 4 : 0)];
+    __shared__ int places[BIAS ? 2 : 1][TILE];
     lds_byte *const lds = (lds_byte *)room;
-    const int lane = threadIdx.x % WAVE, wave = threadIdx.x / WAVE;
+    const int lane = threadIdx.x % WAVE, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
     const int tiles = (A.queries + COLS - 1) / COLS;
     const int64_t unit = unit_of(blockIdx.x, gridDim.x), item = unit / tiles / A.heads;
     const int head = (int)(unit / tiles % A.heads), kv_head = head / (A.heads / A.kv_heads);
-    const int query = (int)(unit % tiles) * COLS + wave * 32 + lane % 32;
+    const int query0 = (int)(unit % tiles) * COLS, query = query0 + wave * 32 + lane % 32;
     const bool there = query < A.queries;
-    const uint16_t *const k = A.k.data + item * A.k.item + kv_head * A.k.head, *const v = A.v.data + item * A.v.item + kv_head * A.v.head;
-    const uint8_t *const mask = A.mask ? A.mask + item * A.mask_item : nullptr;
+    source<DEEP, DIRECT> k(A.k.data + item * A.k.item + kv_head * A.k.head, A.k.row, A.keys, A.width, wave, lane);
+    source<DEEP, DIRECT> v(A.v.data + item * A.v.item + kv_head * A.v.head, A.v.row, A.keys, A.width, wave, lane);
 
     bf16x8 q[STEPS];
-    {
-        const uint16_t *const row = A.q.data + item * A.q.item + head * A.q.head + query * A.q.row;
-#pragma unroll
-        for (int s = 0; s < STEPS; ++s) q[s] = __builtin_bit_cast(bf16x8, there ? row_piece(row, A.width, s * 2 + lane / 32) : u32x4{0, 0, 0, 0});
-    }
-    const int position = BIAS && there ? query_position(A, query) : 0;
+    load_side<STEPS>(q, A.q.data + item * A.q.item + head * A.q.head + query * A.q.row, A.width, there, lane);
+    const float *const line = BIAS ? A.lines + (int64_t)head * A.line : nullptr;
+    const int position = BIAS ? query_position(A, there ? query : A.queries - 1) : 0;
+    place_range mine;
+    if constexpr (BIAS) mine = both(A.query_places[query0 / TILE], A.query_places[query0 + TILE < A.queries ? query0 / TILE + 1 : query0 / TILE]);
     const float scale = A.scale * LOG2E;
     f32x16 o[BLOCKS];
 #pragma unroll
     for (int b = 0; b < BLOCKS; ++b) o[b] = zeros();
     float m = -INFINITY, sum = 0.0f;
 
-    staged<DEEP> nk, nv;
-    uint64_t bits = rows_there(mask, 0, A.keys, lane);
-    if (bits) nk.fetch(k, A.k.row, 0, bits, A.width), nv.fetch(v, A.v.row, 0, bits, A.width);
-    int turn = 0;
-    for (int64_t first = 0; first < A.keys; first += TILE) {
-        const uint64_t next = rows_there(mask, first + TILE, A.keys, lane);
-        if (!bits) {                                   // of all waves alike
-            bits = next;
-            if (bits) nk.fetch(k, A.k.row, first + TILE, bits, A.width), nv.fetch(v, A.v.row, first + TILE, bits, A.width);
-            continue;
+    key_walk at(A.mask ? A.mask + item * A.mask_item : nullptr, A.keys, lane);
+    line_window window, coming;
+    bool fours = false, coming_fours = false;
+    int place = 0, turn = 0;
+    const auto fetch = [&](int to) {                   // the walk's tile
+        lds_byte *const kt = lds + to * 2 * tile::BYTES;
+        k.fetch(at.first, at.bits, kt, wave, lane);
+        v.fetch(at.first, at.bits, kt + tile::BYTES, wave, lane);
+        if constexpr (BIAS) {
+            const place_range keys = A.key_places[at.first / TILE];
+            coming = window_of(A, keys, mine, WINDOW), coming_fours = keys.fours;
+            if (coming.inside) fetch_window(line, A.offsets, coming, lds + 4 * tile::BYTES + to * WINDOW * 4, wave, lane);
+            if (wave == 0) place = key_position(A, at.first + lane < A.keys ? (int)at.first + lane : A.keys - 1);
         }
+    };
+    if (!at.done()) fetch(0);
+    while (!at.done()) {
         lds_byte *const kt = lds + turn * 2 * tile::BYTES, *const vt = kt + tile::BYTES;
-        nk.store(kt), nv.store(vt);
-        __syncthreads();                               // two pairs of tiles: the one written next was read before the last barrier
-        turn ^= 1;
-        if (next) nk.fetch(k, A.k.row, first + TILE, next, A.width), nv.fetch(v, A.v.row, first + TILE, next, A.width);
+        const uint64_t bits = at.bits;
+        k.land(kt), v.land(vt);
+        if constexpr (BIAS) {
+            if (wave == 0) places[turn][lane] = place;
+            window = coming, fours = coming_fours;
+        }
+        if constexpr (DIRECT || BIAS) fetched();
+        __syncthreads();                               // two pairs of tiles: the one written next was read before this
+        at.next(lane);
+        if (!at.done()) fetch(turn ^ 1);
 
         f32x16 x[2];
 #pragma unroll
@@ -75,20 +91,21 @@ template <int DEEP, bool BIAS, bool FINE> __global__ __launch_bounds__(BLOCK) vo
             for (int s = 0; s < STEPS; ++s) x[h] = product(tile::along(kt, h * 32, s, lane), q[s], x[h]);
         }
         if constexpr (BIAS) {
+            const int from = address_of(lds + 4 * tile::BYTES + turn * WINDOW * 4) + 4 * (A.offsets / 2 - window.first - position);
 #pragma unroll
             for (int h = 0; h < 2; ++h)
+                if (window.inside)
+                    over_places<1>(places[turn] + h * 32, fours, from, lane, [&](int r, int byte) { x[h][r] = __builtin_fmaf(x[h][r], scale, number_at(byte)); });
+                else
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const int64_t key = first + h * 32 + row_of(r) + lane / 32 * 4;
-                    x[h][r] = key < A.keys ? x[h][r] * scale + table_value(A, head, bucket_at(A, key_position(A, (int)key) - position)) : 0.0f;
-                }
+                    for (int r = 0; r < 16; ++r) x[h][r] = __builtin_fmaf(x[h][r], scale, line[line_at(A, places[turn][h * 32 + row_of(r) + lane / 32 * 4], position)]);
         }
         if (~bits) {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const uint32_t mine = (uint32_t)(bits >> (h * 32)) >> (lane / 32 * 4);
+                const uint32_t held = (uint32_t)(bits >> (h * 32)) >> (lane / 32 * 4);
 #pragma unroll
-                for (int r = 0; r < 16; ++r) x[h][r] = mine >> row_of(r) & 1 ? x[h][r] : -INFINITY;
+                for (int r = 0; r < 16; ++r) x[h][r] = held >> row_of(r) & 1 ? x[h][r] : -INFINITY;
             }
         }
         float most = x[0][0];
@@ -124,7 +141,7 @@ template <int DEEP, bool BIAS, bool FINE> __global__ __launch_bounds__(BLOCK) vo
                     if constexpr (FINE) o[b] = product(values, low, o[b]);
                 }
             }
-        bits = next;
+        turn ^= 1;
     }
     sum = column_sum(sum);
     const float by = sum != 0.0f ? 1.0f / sum : 0.0f;                 // (a sum that is not a number: so is o)
@@ -147,9 +164,64 @@ template <int DEEP, bool BIAS, bool FINE> __global__ __launch_bounds__(BLOCK) vo
     }
 }
 
+// A head's number for every difference of positions; and what positions each tile of queries and of keys has.
+__global__ __launch_bounds__(BLOCK) void k_lines(attention_args A)
+{
+    const int64_t id = (int64_t)blockIdx.x * BLOCK + threadIdx.x;
+    if ((int)blockIdx.y < A.heads) {
+        if (id < A.offsets) {
+            const int bucket = bucket_at(A, id);
+            A.lines[(int64_t)blockIdx.y * A.line + id] = table_value(A, blockIdx.y, bucket);
+            if (blockIdx.y == 0) A.line_buckets[id] = bucket;
+        }
+        return;
+    }
+    const int64_t query_tiles = (A.queries + TILE - 1) / TILE, key_tiles = (A.keys + TILE - 1) / TILE, tile = id / WAVE;
+    if (tile >= query_tiles + key_tiles) return;
+    const bool keys = tile >= query_tiles;
+    const int lane = threadIdx.x % WAVE, first = (int)(keys ? tile - query_tiles : tile) * TILE, rows = keys ? A.keys : A.queries, row = first + lane < rows ? first + lane : rows - 1;
+    const int place = keys ? key_position(A, row) : query_position(A, row);
+    int low = place, high = place;
+#pragma unroll
+    for (int d = 1; d < WAVE; d *= 2) {
+        const int a = __shfl_xor(low, d), b = __shfl_xor(high, d);
+        low = a < low ? a : low, high = b > high ? b : high;
+    }
+    const int begin = __shfl(place, lane / 4 * 4);
+    const bool fours = __all(place == begin + lane % 4);               // (not so where the rows end: what there is not has the last one's place)
+    if (lane == 0) (keys ? A.key_places : A.query_places)[keys ? tile - query_tiles : tile] = {low, high, fours, 0};
+}
+
 }  // namespace
 
 namespace net {
+
+bool direct_array(const void *p, int64_t item, int64_t row, int64_t head, int64_t width)
+{
+    return width % 8 == 0 && (uintptr_t)p % 16 == 0 && item % 8 == 0 && row % 8 == 0 && head % 8 == 0 && row < (int64_t)1 << 24;
+}
+
+static int64_t line_length(const leap_attention_desc *d) { return (d->offsets + 3) / 4 * 4; }
+static int64_t tiles_of(int64_t rows) { return (rows + TILE - 1) / TILE; }
+
+int64_t lines_bytes(const leap_attention_desc *d)
+{
+    if (!d->d_table) return 0;
+    return (d->heads + 1) * line_length(d) * 4 + (tiles_of(d->queries) + tiles_of(d->keys)) * (int64_t)sizeof(place_range);
+}
+
+int write_lines(attention_args &A, void *work, hipStream_t st)
+{
+    const int64_t length = (A.offsets + 3) / 4 * 4, tiles = tiles_of(A.queries) + tiles_of(A.keys);
+    A.line = (int32_t)length;
+    A.lines = (float *)work;
+    A.line_buckets = (int32_t *)(A.lines + A.heads * length);
+    A.query_places = (place_range *)(A.line_buckets + length);
+    A.key_places = A.query_places + tiles_of(A.queries);
+    const int64_t threads = A.offsets > tiles * WAVE ? A.offsets : tiles * WAVE;
+    hipLaunchKernelGGL(k_lines, dim3((unsigned)((threads + BLOCK - 1) / BLOCK), (unsigned)(A.heads + 1)), dim3(BLOCK), 0, st, A);
+    return launched();
+}
 
 const char *bad_array(int64_t items, int64_t item, int64_t rows, int64_t row, int64_t heads, int64_t head)
 {
@@ -175,7 +247,8 @@ const char *bad_attention(const leap_attention_desc *d)
     if (d->d_table) {
         if (!known_type(d->table_type)) return "unknown element type";
         if (d->buckets < 1 || d->buckets > LEAP_ATTENTION_BUCKETS) return "1 to 4096 buckets";
-        if (!d->d_bucket_of || d->offsets < 1 || d->offsets > most) return "the table needs the buckets of 1 to 2^30 differences";
+        if (!d->d_bucket_of || d->offsets < 1 || d->offsets > (int64_t)1 << 24 || d->offsets * d->heads > most) return "the table needs the buckets of 1 to 2^24 differences, 2^30 for all heads";
+        if (d->heads >= 65535) return "more than 65534 heads with a table";
     }
     return nullptr;
 }
@@ -192,29 +265,30 @@ attention_args arguments_of(const leap_attention_desc *d, const void *q, const v
 
 extern "C" int64_t leap_attention_work(const leap_attention_desc *desc)
 {
-    (void)desc;
-    return 0;
+    return bad_attention(desc) ? 0 : lines_bytes(desc);
 }
 
 extern "C" int leap_attention(const leap_attention_desc *desc, const void *d_q, const void *d_k, const void *d_v, void *d_o, float *d_stats, void *d_rest,
                               void *d_work, void *hip_stream)
 {
-    (void)d_work;
     if (const char *why = bad_attention(desc)) return refuse(why);
     if (!desc->batch || !desc->queries) return LEAP_OK;
     if (!d_q || !d_o || (desc->keys && (!d_k || !d_v))) return refuse("null data pointer");
     if (!d_rest != !d_stats) return refuse("statistics and what o's rounding leaves: both or neither");
-    const forward_args F{arguments_of(desc, d_q, d_k, d_v), (uint16_t *)d_o, d_stats, (uint16_t *)d_rest};
+    if (leap_attention_work(desc) && unaligned(d_work)) return refuse(NO_WORK);
+    forward_args F{arguments_of(desc, d_q, d_k, d_v), (uint16_t *)d_o, d_stats, (uint16_t *)d_rest};
     const int64_t blocks = desc->batch * desc->heads * ((desc->queries + COLS - 1) / COLS);
     if (blocks >= (int64_t)1 << 24) return refuse("more than 2^31 rows of heads");
+    const hipStream_t st = stream_of(hip_stream);
+    if (desc->d_table) {
+        const int rc = write_lines(F.a, d_work, st);
+        if (rc != LEAP_OK) return rc;
+    }
+    const bool direct = direct_array(d_k, desc->k_item, desc->k_row, desc->k_head, desc->width) && direct_array(d_v, desc->v_item, desc->v_row, desc->v_head, desc->width);
     return by_width(desc->width, [&](auto w) {
-        constexpr int W = decltype(w)::value;
-        const dim3 grid((unsigned)blocks), block(BLOCK);
-        const hipStream_t st = stream_of(hip_stream);
-        if (desc->d_table && d_rest) hipLaunchKernelGGL((k_attention<W, true, true>), grid, block, 0, st, F);
-        else if (desc->d_table) hipLaunchKernelGGL((k_attention<W, true, false>), grid, block, 0, st, F);
-        else if (d_rest) hipLaunchKernelGGL((k_attention<W, false, true>), grid, block, 0, st, F);
-        else hipLaunchKernelGGL((k_attention<W, false, false>), grid, block, 0, st, F);
-        return launched();
+        return by_flags([&](auto straight, auto bias, auto fine) {
+            hipLaunchKernelGGL((k_attention<decltype(w)::value, decltype(straight)::value, decltype(bias)::value, decltype(fine)::value>), dim3((unsigned)blocks), dim3(BLOCK), 0, st, F);
+            return launched();
+        }, direct, desc->d_table != nullptr, d_rest != nullptr);
     });
 }

@@ -54,67 +54,116 @@ __global__ __launch_bounds__(BLOCK) void k_delta(grad_args G)
     if (lane == 0) G.delta[(item * A.heads + head) * (int64_t)A.queries + query] = sum;
 }
 
-// BUCKETS: room for the gradient of a table of up to so many (0: not wanted).
-template <int DEEP, bool BIAS, int BUCKETS> __global__ __launch_bounds__(BLOCK) void k_grad_query(grad_args G)
+// Numbers of a line in shared memory (see net_attention.hip), and how many of them take part in the table's gradient there.
+constexpr int window_of_tile(int deep, int buckets) { return buckets > 512 || deep > 64 ? 1024 : 2048; }
+constexpr int SUMS = 512;
+
+// A table's gradient.  Each wave adds ds to a number for every difference that the tile's pairs have, of its own, so that few of a wave's 64 adds meet in one
+// and no order but the wave's counts.  A tile later, while the others multiply, one wave takes the four waves' sums together and adds them to the buckets', which
+// the block keeps.  Where a tile's differences are too far apart for that, the waves add to the buckets one after the other.
+__device__ inline void add_at(int address, float v)
+{
+    __hip_atomic_fetch_add((__attribute__((address_space(3))) float *)(uintptr_t)(uint32_t)address, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+}
+
+template <int BUCKETS> struct table_sums {
+    float bucket[BUCKETS], difference[2][WAVES][SUMS];
+    int which[2][SUMS];                                    // the buckets of the window
+};
+template <> struct table_sums<0> {};
+
+template <int DEEP, bool DIRECT, bool BIAS, int BUCKETS> __global__ __launch_bounds__(BLOCK, 2) void k_grad_query(grad_args G)
 {
     using tile = rows_tile<DEEP>;
-    constexpr int STEPS = DEEP / 16, BLOCKS = DEEP / 32;
+    constexpr int STEPS = DEEP / 16, BLOCKS = DEEP / 32, WINDOW = window_of_tile(DEEP, BUCKETS);
     const attention_args &A = G.a;
-    __shared__ __attribute__((aligned(16))) uint8_t room[4 * tile::BYTES];
-    __shared__ float table[BUCKETS ? WAVES * BUCKETS : 1];
+    __shared__ __attribute__((aligned(16))) uint8_t room[4 * tile::BYTES + (BIAS ? 2 * WINDOW * 4 : 0)];
+    __shared__ __attribute__((aligned(16))) table_sums<BUCKETS> sums;
+    __shared__ int places[BIAS ? 2 : 1][TILE];
     lds_byte *const lds = (lds_byte *)room;
-    const int lane = threadIdx.x % WAVE, wave = threadIdx.x / WAVE;
+    const int lane = threadIdx.x % WAVE, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
     const int tiles = (A.queries + COLS - 1) / COLS;
     const int64_t units = (int64_t)A.batch * tiles;
-    float *const mine = table + wave * BUCKETS;
-    if constexpr (BUCKETS != 0)
-        for (int b = threadIdx.x; b < WAVES * BUCKETS; b += BLOCK) table[b] = 0.0f;
+    if constexpr (BUCKETS != 0) {
+        for (int b = threadIdx.x; b < BUCKETS; b += BLOCK) sums.bucket[b] = 0.0f;
+        for (int b = threadIdx.x; b < 2 * WAVES * SUMS; b += BLOCK) (&sums.difference[0][0][0])[b] = 0.0f;
+    }
 
     const int64_t block = unit_of(blockIdx.x, gridDim.x);
     // a block a unit, the heads of an item apart; with a table the same head for all units of a block
     const int head = BUCKETS ? (int)(block / G.parts) : (int)(block / tiles % A.heads), kv_head = head / (A.heads / A.kv_heads);
-    const int64_t from = BUCKETS ? block % G.parts : block / tiles / A.heads * tiles + block % tiles, step = BUCKETS ? G.parts : units;
-    for (int64_t unit = from; unit < units; unit += step) {
+    int64_t unit = BUCKETS ? block % G.parts : block / tiles / A.heads * tiles + block % tiles;
+    const float *const line = BIAS ? A.lines + (int64_t)head * A.line : nullptr;
+    const float scale = A.scale * LOG2E;
+    if (unit < units) do {
+        int width = A.width;                               // (what follows from it alone is not to be kept for the next unit: it would fill the registers)
+        asm volatile("" : "+s"(width));
         const int64_t item = unit / tiles;
-        const int query = (int)(unit % tiles) * COLS + wave * 32 + lane % 32;
+        const int query0 = (int)(unit % tiles) * COLS, query = query0 + wave * 32 + lane % 32;
         const bool there = query < A.queries;
-        const uint16_t *const k = A.k.data + item * A.k.item + kv_head * A.k.head, *const v = A.v.data + item * A.v.item + kv_head * A.v.head;
-        const uint8_t *const mask = A.mask ? A.mask + item * A.mask_item : nullptr;
+        source<DEEP, DIRECT> k(A.k.data + item * A.k.item + kv_head * A.k.head, A.k.row, A.keys, width, wave, lane);
+        source<DEEP, DIRECT> v(A.v.data + item * A.v.item + kv_head * A.v.head, A.v.row, A.keys, width, wave, lane);
         bf16x8 q[STEPS], g[STEPS];
-        {
-            const uint16_t *const row = A.q.data + item * A.q.item + head * A.q.head + query * A.q.row;
-            const uint16_t *const grad = G.grad.data + item * G.grad.item + head * G.grad.head + query * G.grad.row;
-#pragma unroll
-            for (int s = 0; s < STEPS; ++s) {
-                q[s] = __builtin_bit_cast(bf16x8, there ? row_piece(row, A.width, s * 2 + lane / 32) : u32x4{0, 0, 0, 0});
-                g[s] = __builtin_bit_cast(bf16x8, there ? row_piece(grad, A.width, s * 2 + lane / 32) : u32x4{0, 0, 0, 0});
-            }
-        }
+        load_side<STEPS>(q, A.q.data + item * A.q.item + head * A.q.head + query * A.q.row, width, there, lane);
+        load_side<STEPS>(g, G.grad.data + item * G.grad.item + head * G.grad.head + query * G.grad.row, width, there, lane);
         const int64_t row = (item * A.heads + head) * (int64_t)A.queries + query;
         const query_stats stats = there ? stats_of(G, row) : query_stats{0.0f, INFINITY};
-        const float delta = there ? G.delta[row] : 0.0f, scale = A.scale * LOG2E, base = stats.most + stats.log;
-        const int position = BIAS && there ? query_position(A, query) : 0;
+        const float delta = there ? G.delta[row] : 0.0f, base = stats.most + stats.log;
+        const int position = BIAS ? query_position(A, there ? query : A.queries - 1) : 0;
+        place_range mine;
+        if constexpr (BIAS) mine = both(A.query_places[query0 / TILE], A.query_places[query0 + TILE < A.queries ? query0 / TILE + 1 : query0 / TILE]);
         f32x16 sum[BLOCKS];
 #pragma unroll
         for (int b = 0; b < BLOCKS; ++b) sum[b] = zeros();
 
-        staged<DEEP> nk, nv;
-        uint64_t bits = rows_there(mask, 0, A.keys, lane);
-        if (bits) nk.fetch(k, A.k.row, 0, bits, A.width), nv.fetch(v, A.v.row, 0, bits, A.width);
-        int turn = 0;
-        __syncthreads();                                   // the unit before has read its tiles
-        for (int64_t first = 0; first < A.keys; first += TILE) {
-            const uint64_t next = rows_there(mask, first + TILE, A.keys, lane);
-            if (!bits) {                                   // of all waves alike
-                bits = next;
-                if (bits) nk.fetch(k, A.k.row, first + TILE, bits, A.width), nv.fetch(v, A.v.row, first + TILE, bits, A.width);
-                continue;
+        key_walk at(A.mask ? A.mask + item * A.mask_item : nullptr, A.keys, lane);
+        line_window window{}, coming{}, before{};
+        bool fours = false, coming_fours = false, pending = false;
+        int place = 0, turn = 0, duty = 0;
+        const auto fetch = [&](int to) {
+            lds_byte *const kt = lds + to * 2 * tile::BYTES;
+            k.fetch(at.first, at.bits, kt, wave, lane);
+            v.fetch(at.first, at.bits, kt + tile::BYTES, wave, lane);
+            if constexpr (BIAS) {
+                const place_range keys = A.key_places[at.first / TILE];
+                coming = window_of(A, keys, mine, WINDOW), coming_fours = keys.fours;
+                if (coming.inside) fetch_window(line, A.offsets, coming, lds + 4 * tile::BYTES + to * WINDOW * 4, wave, lane);
+                if (wave == 0) place = key_position(A, at.first + lane < A.keys ? (int)at.first + lane : A.keys - 1);
             }
+        };
+        // The sums of the tile before, by the wave whose turn it is.
+        const auto settle = [&](int of) {
+            if constexpr (BUCKETS != 0)
+                if (pending && wave == duty)
+                    for (int i = lane; i < before.count; i += WAVE) {
+                        float s = 0.0f;
+#pragma unroll
+                        for (int w = 0; w < WAVES; ++w) s += sums.difference[of][w][i], sums.difference[of][w][i] = 0.0f;
+                        __hip_atomic_fetch_add(&sums.bucket[sums.which[of][i]], s, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+                    }
+            duty = (duty + 1) % WAVES;
+        };
+        __syncthreads();                                   // the unit before has read its tiles
+        if (!at.done()) fetch(0);
+        while (!at.done()) {
             lds_byte *const kt = lds + turn * 2 * tile::BYTES, *const vt = kt + tile::BYTES;
-            nk.store(kt), nv.store(vt);
+            const uint64_t bits = at.bits;
+            k.land(kt), v.land(vt);
+            if constexpr (BIAS) {
+                if (wave == 0) places[turn][lane] = place;
+                window = coming, fours = coming_fours;
+            }
+            if constexpr (DIRECT || BIAS) fetched();
             __syncthreads();
-            turn ^= 1;
-            if (next) nk.fetch(k, A.k.row, first + TILE, next, A.width), nv.fetch(v, A.v.row, first + TILE, next, A.width);
+            const bool near = BUCKETS && window.inside && window.count <= SUMS;
+            if constexpr (BUCKETS != 0)
+                if (near) fetch_window(A.line_buckets, A.offsets, window, (lds_byte *)sums.which[turn], wave, lane);
+            at.next(lane);
+            if (!at.done()) fetch(turn ^ 1);
+            settle(turn ^ 1);
+            const int from_line = address_of(lds + 4 * tile::BYTES + turn * WINDOW * 4) + 4 * (A.offsets / 2 - window.first - position);
+            int to_sums = 0;                               // from a number of the line to the wave's sum of its pairs
+            if constexpr (BUCKETS != 0) to_sums = address_of((lds_byte *)sums.difference[turn][wave]) - address_of(lds + 4 * tile::BYTES + turn * WINDOW * 4);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 f32x16 x = zeros(), dp = zeros();
@@ -123,20 +172,34 @@ template <int DEEP, bool BIAS, int BUCKETS> __global__ __launch_bounds__(BLOCK) 
 #pragma unroll
                 for (int s = 0; s < STEPS; ++s) dp = product(tile::along(vt, h * 32, s, lane), g[s], dp);
                 const uint32_t held = (uint32_t)(bits >> (h * 32)) >> (lane / 32 * 4);
+                const auto ds_of = [&](int r, float exponent) {
+                    x[r] = __builtin_amdgcn_exp2f(exponent) * (dp[r] - delta);
+                    if (~bits) x[r] = held >> row_of(r) & 1 ? x[r] : 0.0f;
+                };
+                if constexpr (BIAS) {
+                    if (window.inside)
+                        over_places<1>(places[turn] + h * 32, fours, from_line, lane, [&](int r, int byte) {
+                            ds_of(r, __builtin_fmaf(x[r], scale, number_at(byte)) - stats.most - stats.log);
+                            if constexpr (BUCKETS != 0)
+                                if (near) add_at(byte + to_sums, x[r]);
+                        });
+                    else
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    float p;
-                    int bucket = 0;
-                    if constexpr (BIAS) {
-                        const int64_t key = first + h * 32 + row_of(r) + lane / 32 * 4;
-                        bucket = key < A.keys ? bucket_at(A, key_position(A, (int)key) - position) : 0;
-                        p = __builtin_amdgcn_exp2f(x[r] * scale + table_value(A, head, bucket) - stats.most - stats.log);
-                    } else {
-                        p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[r], scale, -base));
-                    }
-                    if (~bits) p = held >> row_of(r) & 1 ? p : 0.0f;
-                    x[r] = p * (dp[r] - delta);
-                    if constexpr (BUCKETS != 0) __hip_atomic_fetch_add(&mine[bucket], x[r], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT);
+                        for (int r = 0; r < 16; ++r)
+                            ds_of(r, __builtin_fmaf(x[r], scale, line[line_at(A, places[turn][h * 32 + row_of(r) + lane / 32 * 4], position)]) - stats.most - stats.log);
+                    if constexpr (BUCKETS != 0)
+                        if (!near)
+                            for (int w = 0; w < WAVES; ++w) {
+                                __syncthreads();
+                                if (w == wave)
+#pragma unroll
+                                    for (int r = 0; r < 16; ++r)
+                                        __hip_atomic_fetch_add(&sums.bucket[A.line_buckets[line_at(A, places[turn][h * 32 + row_of(r) + lane / 32 * 4], position)]], x[r], __ATOMIC_RELAXED,
+                                                               __HIP_MEMORY_SCOPE_WORKGROUP);
+                            }
+                } else {
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) ds_of(r, __builtin_fmaf(x[r], scale, -base));
                 }
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
@@ -145,18 +208,20 @@ template <int DEEP, bool BIAS, int BUCKETS> __global__ __launch_bounds__(BLOCK) 
                     for (int b = 0; b < BLOCKS; ++b) sum[b] = product(tile::across(kt, h * 32 + t * 16, b, lane), ds, sum[b]);
                 }
             }
-            bits = next;
+            pending = near, before = window;
+            turn ^= 1;
         }
-        if (G.grad_q) store_column<BLOCKS>(G.grad_q + ((item * A.queries + query) * A.heads + head) * A.width, A.width, sum, A.scale, lane, there);
-    }
+        if constexpr (BUCKETS != 0) {
+            fetched();                                     // the last tile's buckets
+            __syncthreads();
+            settle(turn ^ 1);
+        }
+        if (G.grad_q) store_column<BLOCKS>(G.grad_q + ((item * A.queries + query) * A.heads + head) * width, width, sum, A.scale, lane, there);
+        unit += G.parts;
+    } while (BUCKETS && unit < units);
     if constexpr (BUCKETS != 0) {
         __syncthreads();
-        for (int b = threadIdx.x; b < A.buckets; b += BLOCK) {
-            float sum = 0.0f;
-#pragma unroll
-            for (int w = 0; w < WAVES; ++w) sum += table[w * BUCKETS + b];
-            G.part[block * A.buckets + b] = sum;
-        }
+        for (int b = threadIdx.x; b < A.buckets; b += BLOCK) G.part[block * A.buckets + b] = sums.bucket[b];
     }
 }
 
@@ -172,16 +237,16 @@ __global__ __launch_bounds__(BLOCK) void k_join_table(const float *__restrict__ 
     out[(int64_t)blockIdx.y * buckets + b] = (float)sum;
 }
 
-template <int DEEP, bool BIAS> __global__ __launch_bounds__(BLOCK) void k_grad_key(grad_args G)
+template <int DEEP, bool DIRECT, bool BIAS> __global__ __launch_bounds__(BLOCK, DEEP > 64 ? 1 : 2) void k_grad_key(grad_args G)
 {
     using tile = rows_tile<DEEP>;
-    constexpr int STEPS = DEEP / 16, BLOCKS = DEEP / 32;
+    constexpr int STEPS = DEEP / 16, BLOCKS = DEEP / 32, WINDOW = 2048;
     const attention_args &A = G.a;
-    __shared__ __attribute__((aligned(16))) uint8_t room[4 * tile::BYTES];
+    __shared__ __attribute__((aligned(16))) uint8_t room[4 * tile::BYTES + (BIAS ? 2 * WINDOW * 4 : 0)];
     __shared__ __attribute__((aligned(16))) float most[2][TILE], log[2][TILE], delta[2][TILE];
-    __shared__ __attribute__((aligned(16))) int place[2][TILE];
+    __shared__ int places[BIAS ? 2 : 1][TILE];
     lds_byte *const lds = (lds_byte *)room;
-    const int lane = threadIdx.x % WAVE, wave = threadIdx.x / WAVE;
+    const int lane = threadIdx.x % WAVE, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
     const int blocks = (A.keys + COLS - 1) / COLS, group = A.heads / A.kv_heads, tiles = (A.queries + TILE - 1) / TILE;
     const int64_t unit = unit_of(blockIdx.x, gridDim.x), item = unit / blocks / A.kv_heads;
     const int kv_head = (int)(unit / blocks % A.kv_heads), key0 = (int)(unit % blocks) * COLS, key = key0 + wave * 32 + lane % 32;
@@ -196,71 +261,90 @@ template <int DEEP, bool BIAS> __global__ __launch_bounds__(BLOCK) void k_grad_k
 
     if (any) {
         bf16x8 k[STEPS], v[STEPS];
-        const uint16_t *const krow = A.k.data + item * A.k.item + kv_head * A.k.head + key * A.k.row, *const vrow = A.v.data + item * A.v.item + kv_head * A.v.head + key * A.v.row;
-#pragma unroll
-        for (int s = 0; s < STEPS; ++s) {
-            k[s] = __builtin_bit_cast(bf16x8, held ? row_piece(krow, A.width, s * 2 + lane / 32) : u32x4{0, 0, 0, 0});
-            v[s] = __builtin_bit_cast(bf16x8, held ? row_piece(vrow, A.width, s * 2 + lane / 32) : u32x4{0, 0, 0, 0});
-        }
-        const int position = BIAS && there ? key_position(A, key) : 0;
-        staged<DEEP> nq, ng;
-        query_stats stats;
-        float nd;
-        int np = 0;
-        // Step `at` of group * tiles: tile at % tiles of head at / tiles.
-        const auto fetch = [&](int at) {
-            const int head = kv_head * group + at / tiles;
-            const int64_t first = (int64_t)(at % tiles) * TILE;
-            const uint64_t bits = rows_there(nullptr, first, A.queries, lane);
-            nq.fetch(A.q.data + item * A.q.item + head * A.q.head, A.q.row, first, bits, A.width);
-            ng.fetch(G.grad.data + item * G.grad.item + head * G.grad.head, G.grad.row, first, bits, A.width);
-            if (wave == 0) {
-                const bool in = first + lane < A.queries;
-                const int64_t row = (item * A.heads + head) * (int64_t)A.queries + first + lane;
-                stats = in ? stats_of(G, row) : query_stats{0.0f, INFINITY};
-                nd = in ? G.delta[row] : 0.0f;
-                if (BIAS) np = in ? query_position(A, (int)first + lane) : 0;
-            }
-        };
-        const int steps = group * tiles;
-        if (steps) fetch(0);
-        for (int at = 0; at < steps; ++at) {
-            const int turn = at % 2, head = kv_head * group + at / tiles;
-            lds_byte *const qt = lds + turn * 2 * tile::BYTES, *const gt = qt + tile::BYTES;
-            nq.store(qt), ng.store(gt);
-            if (wave == 0) {
-                most[turn][lane] = BIAS ? stats.most : stats.most + stats.log;
-                log[turn][lane] = stats.log;
-                delta[turn][lane] = nd;
-                place[turn][lane] = np;
-            }
-            __syncthreads();
-            if (at + 1 < steps) fetch(at + 1);
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                f32x16 x = zeros(), dp = zeros();
-#pragma unroll
-                for (int s = 0; s < STEPS; ++s) x = product(tile::along(qt, h * 32, s, lane), k[s], x);
-#pragma unroll
-                for (int s = 0; s < STEPS; ++s) dp = product(tile::along(gt, h * 32, s, lane), v[s], dp);
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const int row = h * 32 + row_of(r) + lane / 32 * 4;
-                    float p;
-                    if constexpr (BIAS)
-                        p = __builtin_amdgcn_exp2f(x[r] * scale + table_value(A, head, bucket_at(A, position - place[turn][row])) - most[turn][row] - log[turn][row]);
-                    else
-                        p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[r], scale, -most[turn][row]));
-                    x[r] = p;
-                    dp[r] = p * (dp[r] - delta[turn][row]);
+        load_side<STEPS>(k, A.k.data + item * A.k.item + kv_head * A.k.head + key * A.k.row, A.width, held, lane);
+        load_side<STEPS>(v, A.v.data + item * A.v.item + kv_head * A.v.head + key * A.v.row, A.width, held, lane);
+        const int position = BIAS ? key_position(A, there ? key : A.keys - 1) : 0;
+        place_range mine;
+        if constexpr (BIAS) mine = both(A.key_places[key0 / TILE], A.key_places[key0 + TILE < A.keys ? key0 / TILE + 1 : key0 / TILE]);
+        // the group's heads one after the other, each head's queries in tiles
+        for (int head = kv_head * group; head < (kv_head + 1) * group; ++head) {
+            source<DEEP, DIRECT> q(A.q.data + item * A.q.item + head * A.q.head, A.q.row, A.queries, A.width, wave, lane);
+            source<DEEP, DIRECT> g(G.grad.data + item * G.grad.item + head * G.grad.head, G.grad.row, A.queries, A.width, wave, lane);
+            const float *const line = BIAS ? A.lines + (int64_t)head * A.line : nullptr;
+            const int64_t row0 = (item * A.heads + head) * (int64_t)A.queries;
+            query_stats stats;
+            float nd;
+            int place = 0;
+            line_window window{}, coming{};
+            bool fours = false, coming_fours = false;
+            const auto fetch = [&](int at, int to) {
+                const int first = at * TILE;
+                const uint64_t bits = A.queries - first >= TILE ? ~(uint64_t)0 : ((uint64_t)1 << (A.queries - first)) - 1;
+                lds_byte *const qt = lds + to * 2 * tile::BYTES;
+                q.fetch(first, bits, qt, wave, lane);
+                g.fetch(first, bits, qt + tile::BYTES, wave, lane);
+                if constexpr (BIAS) {
+                    const place_range queries = A.query_places[at];
+                    coming = window_of(A, mine, queries, WINDOW), coming_fours = queries.fours;
+                    if (coming.inside) fetch_window(line, A.offsets, coming, lds + 4 * tile::BYTES + to * WINDOW * 4, wave, lane);
                 }
+                if (wave == 0) {
+                    const bool in = first + lane < A.queries;
+                    stats = in ? stats_of(G, row0 + first + lane) : query_stats{0.0f, INFINITY};
+                    nd = in ? G.delta[row0 + first + lane] : 0.0f;
+                    if (BIAS) place = query_position(A, in ? first + lane : A.queries - 1);
+                }
+            };
+            __syncthreads();                               // the head before has read its tiles
+            if (tiles) fetch(0, 0);
+            for (int at = 0; at < tiles; ++at) {
+                const int turn = at % 2;
+                lds_byte *const qt = lds + turn * 2 * tile::BYTES, *const gt = qt + tile::BYTES;
+                q.land(qt), g.land(gt);
+                if (wave == 0) {
+                    most[turn][lane] = BIAS ? stats.most : stats.most + stats.log;
+                    log[turn][lane] = stats.log;
+                    delta[turn][lane] = nd;
+                    if (BIAS) places[turn][lane] = place;
+                }
+                if constexpr (BIAS) window = coming, fours = coming_fours;
+                if constexpr (DIRECT || BIAS) fetched();
+                __syncthreads();
+                if (at + 1 < tiles) fetch(at + 1, turn ^ 1);
+                const int from_line = address_of(lds + 4 * tile::BYTES + turn * WINDOW * 4) + 4 * (A.offsets / 2 - window.first + position);
 #pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    const bf16x8 p = eight(x, t), ds = eight(dp, t);
+                for (int h = 0; h < 2; ++h) {
+                    f32x16 x = zeros(), dp = zeros();
 #pragma unroll
-                    for (int b = 0; b < BLOCKS; ++b) {
-                        gv[b] = product(tile::across(gt, h * 32 + t * 16, b, lane), p, gv[b]);
-                        gk[b] = product(tile::across(qt, h * 32 + t * 16, b, lane), ds, gk[b]);
+                    for (int s = 0; s < STEPS; ++s) x = product(tile::along(qt, h * 32, s, lane), k[s], x);
+#pragma unroll
+                    for (int s = 0; s < STEPS; ++s) dp = product(tile::along(gt, h * 32, s, lane), v[s], dp);
+                    const auto p_of = [&](int r, float exponent) {
+                        x[r] = __builtin_amdgcn_exp2f(exponent);
+                        dp[r] = x[r] * (dp[r] - delta[turn][h * 32 + row_of(r) + lane / 32 * 4]);
+                    };
+                    const auto lowered = [&](int r, float score) {
+                        const int row = h * 32 + row_of(r) + lane / 32 * 4;
+                        return score - most[turn][row] - log[turn][row];
+                    };
+                    if constexpr (BIAS) {
+                        if (window.inside)
+                            over_places<-1>(places[turn] + h * 32, fours, from_line, lane, [&](int r, int byte) { p_of(r, lowered(r, __builtin_fmaf(x[r], scale, number_at(byte)))); });
+                        else
+#pragma unroll
+                            for (int r = 0; r < 16; ++r) p_of(r, lowered(r, __builtin_fmaf(x[r], scale, line[line_at(A, position, places[turn][h * 32 + row_of(r) + lane / 32 * 4])])));
+                    } else {
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) p_of(r, __builtin_fmaf(x[r], scale, -most[turn][h * 32 + row_of(r) + lane / 32 * 4]));
+                    }
+#pragma unroll
+                    for (int t = 0; t < 2; ++t) {
+                        const bf16x8 p = eight(x, t), ds = eight(dp, t);
+#pragma unroll
+                        for (int b = 0; b < BLOCKS; ++b) {
+                            gv[b] = product(tile::across(gt, h * 32 + t * 16, b, lane), p, gv[b]);
+                            gk[b] = product(tile::across(qt, h * 32 + t * 16, b, lane), ds, gk[b]);
+                        }
                     }
                 }
             }
@@ -289,7 +373,7 @@ int64_t delta_bytes(const leap_attention_desc *d) { return (d->batch * d->heads 
 extern "C" int64_t leap_attention_backward_work(const leap_attention_desc *desc, int32_t with_table)
 {
     if (bad_attention(desc)) return 0;
-    return delta_bytes(desc) + (with_table && desc->d_table ? desc->heads * table_parts(desc) * desc->buckets * 4 : 0);
+    return delta_bytes(desc) + lines_bytes(desc) + (with_table && desc->d_table ? desc->heads * table_parts(desc) * desc->buckets * 4 : 0);
 }
 
 extern "C" int leap_attention_backward(const leap_attention_desc *desc, const void *d_grad, int64_t grad_item, int64_t grad_row, int64_t grad_head, const void *d_q,
@@ -307,7 +391,7 @@ extern "C" int leap_attention_backward(const leap_attention_desc *desc, const vo
     if ((int64_t)desc->heads / desc->kv_heads * ((desc->queries + TILE - 1) / TILE) >= (int64_t)1 << 31) return refuse("more than 2^37 queries share a key");
     const hipStream_t st = stream_of(hip_stream);
     grad_args G{arguments_of(desc, d_q, d_k, d_v), {(const uint16_t *)d_grad, grad_item, grad_row, grad_head}, (const uint16_t *)d_o, (const uint16_t *)d_rest,
-                d_stats, (float *)d_work, (uint16_t *)d_grad_q, (uint16_t *)d_grad_k, (uint16_t *)d_grad_v, (float *)((char *)d_work + delta_bytes(desc)),
+                d_stats, (float *)d_work, (uint16_t *)d_grad_q, (uint16_t *)d_grad_k, (uint16_t *)d_grad_v, (float *)((char *)d_work + delta_bytes(desc) + lines_bytes(desc)),
                 (int32_t)table_parts(desc), 0};
     int rc = LEAP_OK;
     if (rows && (d_grad_q || d_grad_k || d_grad_v || d_grad_table))
@@ -316,27 +400,35 @@ extern "C" int leap_attention_backward(const leap_attention_desc *desc, const vo
             hipLaunchKernelGGL(k_delta, dim3(blocks), dim3(BLOCK), 0, st, G);
         });
     if (rc != LEAP_OK) return rc;
+    if (desc->d_table && (rows || d_grad_table)) rc = write_lines(G.a, (char *)d_work + delta_bytes(desc), st);
+    if (rc != LEAP_OK) return rc;
+    const bool keys_direct = direct_array(d_k, desc->k_item, desc->k_row, desc->k_head, desc->width) && direct_array(d_v, desc->v_item, desc->v_row, desc->v_head, desc->width);
+    const bool queries_direct = direct_array(d_q, desc->q_item, desc->q_row, desc->q_head, desc->width) && direct_array(d_grad, grad_item, grad_row, grad_head, desc->width);
     return by_width(desc->width, [&](auto w) {
         constexpr int W = decltype(w)::value;
         int status = LEAP_OK;
         if (d_grad_table) {
             const dim3 grid((unsigned)(desc->heads * G.parts));
-            if (desc->buckets <= 512) hipLaunchKernelGGL((k_grad_query<W, true, 512>), grid, dim3(BLOCK), 0, st, G);
-            else hipLaunchKernelGGL((k_grad_query<W, true, LEAP_ATTENTION_BUCKETS>), grid, dim3(BLOCK), 0, st, G);
+            by_flags([&](auto direct, auto few) {
+                hipLaunchKernelGGL((k_grad_query<W, decltype(direct)::value, true, decltype(few)::value ? 512 : LEAP_ATTENTION_BUCKETS>), grid, dim3(BLOCK), 0, st, G);
+                return LEAP_OK;
+            }, keys_direct, desc->buckets <= 512);
             if ((status = launched()) != LEAP_OK) return status;
             const dim3 across((unsigned)((desc->buckets + BLOCK - 1) / BLOCK), (unsigned)desc->heads);
             hipLaunchKernelGGL(k_join_table, across, dim3(BLOCK), 0, st, G.part, G.parts, (int)desc->buckets, d_grad_table);
             status = launched();
         } else if (d_grad_q && rows) {
             const dim3 grid((unsigned)(desc->batch * desc->heads * tiles));
-            if (desc->d_table) hipLaunchKernelGGL((k_grad_query<W, true, 0>), grid, dim3(BLOCK), 0, st, G);
-            else hipLaunchKernelGGL((k_grad_query<W, false, 0>), grid, dim3(BLOCK), 0, st, G);
-            status = launched();
+            status = by_flags([&](auto direct, auto bias) {
+                hipLaunchKernelGGL((k_grad_query<W, decltype(direct)::value, decltype(bias)::value, 0>), grid, dim3(BLOCK), 0, st, G);
+                return launched();
+            }, keys_direct, desc->d_table != nullptr);
         }
         if (status != LEAP_OK || !kept || !(d_grad_k || d_grad_v)) return status;
         const dim3 grid((unsigned)(desc->batch * desc->kv_heads * key_tiles));
-        if (desc->d_table) hipLaunchKernelGGL((k_grad_key<W, true>), grid, dim3(BLOCK), 0, st, G);
-        else hipLaunchKernelGGL((k_grad_key<W, false>), grid, dim3(BLOCK), 0, st, G);
-        return launched();
+        return by_flags([&](auto direct, auto bias) {
+            hipLaunchKernelGGL((k_grad_key<W, decltype(direct)::value, decltype(bias)::value>), grid, dim3(BLOCK), 0, st, G);
+            return launched();
+        }, queries_direct, desc->d_table != nullptr);
     });
 }
