@@ -24,9 +24,9 @@ struct rows_of {
     int64_t item, row, head;
 };
 
-// Positions of a tile's rows: the least and the largest, and whether every four (from a multiple of four on) are consecutive.
+// Positions of a tile's rows: the least and the largest, whether every four (from a multiple of four on) are consecutive, and whether each is larger than the one before.
 struct place_range {
-    int32_t low, high, fours, none;
+    int32_t low, high, fours, rising;
 };
 
 struct attention_args {
@@ -40,7 +40,7 @@ struct attention_args {
     float scale;
     // in the workspace, with a table: a number for every difference of positions, in units of log2, heads `line` apart; its bucket; the positions of each TILE rows
     float *lines;
-    int32_t *line_buckets;
+    uint16_t *line_buckets;
     place_range *query_places, *key_places;
     int32_t line;
 };
@@ -231,7 +231,7 @@ __device__ inline int line_at(const attention_args &A, int key, int query)
     return at < 0 ? 0 : at >= A.offsets ? A.offsets - 1 : (int)at;
 }
 
-// The part of a line that the pairs of two tiles' rows take: the numbers from `first` (a multiple of four) on, `count` of them.  `inside`: it is within the line and
+// The part of a line that the pairs of two tiles' rows take: the numbers from `first` (a multiple of eight) on, `count` of them.  `inside`: it is within the line and
 // MOST numbers, so that shared memory has it; otherwise pairs look theirs up in memory.
 struct line_window {
     int first, count;
@@ -240,16 +240,16 @@ struct line_window {
 __device__ inline line_window window_of(const attention_args &A, const place_range &keys, const place_range &queries, int most)
 {
     const int64_t low = (int64_t)keys.low - queries.high + A.offsets / 2, high = (int64_t)keys.high - queries.low + A.offsets / 2;
-    const int64_t first = low / 4 * 4;
+    const int64_t first = low / 8 * 8;
     return {(int)first, (int)(high - first + 1), low >= 0 && high < A.offsets && high - first < most};
 }
 __device__ inline place_range both(const place_range &a, const place_range &b) { return {a.low < b.low ? a.low : b.low, a.high > b.high ? a.high : b.high, a.fours & b.fours, 0}; }
 
-// Brings a window of 4-byte numbers to shared memory, a KiB a wave.
-__device__ inline void fetch_window(const void *line, int length, const line_window &w, lds_byte *to, int wave, int lane)
+// Brings a window of SIZE-byte numbers to shared memory, a KiB a wave.
+template <int SIZE> __device__ inline void fetch_window(const void *line, int length, const line_window &w, lds_byte *to, int wave, int lane)
 {
-    const u32x4 from = window{(const uint8_t *)line, (int64_t)length * 4, 0}.buffer();
-    for (int piece = wave; piece * 256 < w.count; piece += WAVES) fetch16(from, (uint32_t)(w.first + piece * 256 + lane * 4) * 4, to + piece * 1024);
+    const u32x4 from = window{(const uint8_t *)line, whole((int64_t)length * SIZE, 16), 0}.buffer();
+    for (int piece = wave; piece * (1024 / SIZE) < w.count; piece += WAVES) fetch16(from, (uint32_t)w.first * SIZE + piece * 1024 + lane * 16, to + piece * 1024);
 }
 
 // f(r, number) for the sixteen pairs of a lane's position with the rows 8 a + 4 (lane / 32) + c of `places`.  The rows are keys (SIGN 1) or queries (-1).  at: the byte

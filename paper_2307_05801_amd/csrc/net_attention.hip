@@ -65,7 +65,7 @@ template <int DEEP, bool DIRECT, bool BIAS, bool FINE> __global__ __launch_bound
         if constexpr (BIAS) {
             const place_range keys = A.key_places[at.first / TILE];
             coming = window_of(A, keys, mine, WINDOW), coming_fours = keys.fours;
-            if (coming.inside) fetch_window(line, A.offsets, coming, lds + 4 * tile::BYTES + to * WINDOW * 4, wave, lane);
+            if (coming.inside) fetch_window<4>(line, A.offsets, coming, lds + 4 * tile::BYTES + to * WINDOW * 4, wave, lane);
             if (wave == 0) place = key_position(A, at.first + lane < A.keys ? (int)at.first + lane : A.keys - 1);
         }
     };
@@ -172,7 +172,7 @@ __global__ __launch_bounds__(BLOCK) void k_lines(attention_args A)
         if (id < A.offsets) {
             const int bucket = bucket_at(A, id);
             A.lines[(int64_t)blockIdx.y * A.line + id] = table_value(A, blockIdx.y, bucket);
-            if (blockIdx.y == 0) A.line_buckets[id] = bucket;
+            if (blockIdx.y == 0) A.line_buckets[id] = (uint16_t)bucket;
         }
         return;
     }
@@ -189,7 +189,8 @@ __global__ __launch_bounds__(BLOCK) void k_lines(attention_args A)
     }
     const int begin = __shfl(place, lane / 4 * 4);
     const bool fours = __all(place == begin + lane % 4);               // (not so where the rows end: what there is not has the last one's place)
-    if (lane == 0) (keys ? A.key_places : A.query_places)[keys ? tile - query_tiles : tile] = {low, high, fours, 0};
+    const bool rising = __all(place > __shfl_up(place, 1) || lane == 0 || first + lane >= rows);
+    if (lane == 0) (keys ? A.key_places : A.query_places)[keys ? tile - query_tiles : tile] = {low, high, fours, rising};
 }
 
 }  // namespace
@@ -201,21 +202,21 @@ bool direct_array(const void *p, int64_t item, int64_t row, int64_t head, int64_
     return width % 8 == 0 && (uintptr_t)p % 16 == 0 && item % 8 == 0 && row % 8 == 0 && head % 8 == 0 && row < (int64_t)1 << 24;
 }
 
-static int64_t line_length(const leap_attention_desc *d) { return (d->offsets + 3) / 4 * 4; }
+static int64_t line_length(int64_t offsets) { return (offsets + 7) / 8 * 8; }
 static int64_t tiles_of(int64_t rows) { return (rows + TILE - 1) / TILE; }
 
 int64_t lines_bytes(const leap_attention_desc *d)
 {
     if (!d->d_table) return 0;
-    return (d->heads + 1) * line_length(d) * 4 + (tiles_of(d->queries) + tiles_of(d->keys)) * (int64_t)sizeof(place_range);
+    return d->heads * line_length(d->offsets) * 4 + line_length(d->offsets) * 2 + (tiles_of(d->queries) + tiles_of(d->keys)) * (int64_t)sizeof(place_range);
 }
 
 int write_lines(attention_args &A, void *work, hipStream_t st)
 {
-    const int64_t length = (A.offsets + 3) / 4 * 4, tiles = tiles_of(A.queries) + tiles_of(A.keys);
+    const int64_t length = line_length(A.offsets), tiles = tiles_of(A.queries) + tiles_of(A.keys);
     A.line = (int32_t)length;
     A.lines = (float *)work;
-    A.line_buckets = (int32_t *)(A.lines + A.heads * length);
+    A.line_buckets = (uint16_t *)(A.lines + A.heads * length);
     A.query_places = (place_range *)(A.line_buckets + length);
     A.key_places = A.query_places + tiles_of(A.queries);
     const int64_t threads = A.offsets > tiles * WAVE ? A.offsets : tiles * WAVE;

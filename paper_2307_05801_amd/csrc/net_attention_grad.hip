@@ -54,31 +54,49 @@ __global__ __launch_bounds__(BLOCK) void k_delta(grad_args G)
     if (lane == 0) G.delta[(item * A.heads + head) * (int64_t)A.queries + query] = sum;
 }
 
-// Numbers of a line in shared memory (see net_attention.hip), and how many of them take part in the table's gradient there.
-constexpr int window_of_tile(int deep, int buckets) { return buckets > 512 || deep > 64 ? 1024 : 2048; }
-constexpr int SUMS = 512;
+// Numbers of a line in shared memory (see net_attention.hip).
+constexpr int window_of_tile(int deep) { return deep > 64 ? 1024 : 2048; }
 
-// A table's gradient.  Each wave adds ds to a number for every difference that the tile's pairs have, of its own, so that few of a wave's 64 adds meet in one
-// and no order but the wave's counts.  A tile later, while the others multiply, one wave takes the four waves' sums together and adds them to the buckets', which
-// the block keeps.  Where a tile's differences are too far apart for that, the waves add to the buckets one after the other.
-__device__ inline void add_at(int address, float v)
+// A table's gradient.  Adds of integers to shared memory take a wave 4 cycles, those of floats 192 (3 a lane), and integers' order does not matter.  So a tile's ds, as integers of
+// 2^-24 of the largest of them, are added to a number for every difference that its pairs have: keys rise, so a difference has at most one pair of each of the
+// block's 128 queries, and 128 times 2^24 fits 32 bits.  (The largest is 40 times the root of the mean square or so: the sums are as good as those of 32-bit floats.)
+// In the next tile's time one wave adds the differences' sums, as floats, to their buckets, which the block keeps.
+// Where the differences are too far apart or keys do not rise, ds go to the buckets as two integers, the upper one of 2^-17 of the largest: 8192 of either fit.
+template <int BUCKETS, int WINDOW> struct table_sums {
+    float bucket[BUCKETS];
+    int32_t difference[WINDOW];
+    uint16_t which[WINDOW];                                // the buckets of the window
+    float peak[WAVES];
+};
+template <int WINDOW> struct table_sums<0, WINDOW> {};
+
+// Shared memory's writes of all waves are there for all; what comes from memory is not waited for.
+__device__ inline void shared_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// The largest of a wave.
+__device__ inline float wave_max(float v)
 {
-    __hip_atomic_fetch_add((__attribute__((address_space(3))) float *)(uintptr_t)(uint32_t)address, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+    const auto with = [&](int other) { v = fmaxf(v, __int_as_float(other)); };
+    with(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0xb1, 0xf, 0xf, false));        // the neighbour, the other pair,
+    with(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x4e, 0xf, 0xf, false));
+    with(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x141, 0xf, 0xf, false));       // the other four of eight, the other eight of sixteen
+    with(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x140, 0xf, 0xf, false));
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return column_max(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
 }
 
-template <int BUCKETS> struct table_sums {
-    float bucket[BUCKETS], difference[2][WAVES][SUMS];
-    int which[2][SUMS];                                    // the buckets of the window
-};
-template <> struct table_sums<0> {};
+__device__ inline void add_at(int address, int v)
+{
+    __hip_atomic_fetch_add((__attribute__((address_space(3))) int *)(uintptr_t)(uint32_t)address, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+}
 
 template <int DEEP, bool DIRECT, bool BIAS, int BUCKETS> __global__ __launch_bounds__(BLOCK, 2) void k_grad_query(grad_args G)
 {
     using tile = rows_tile<DEEP>;
-    constexpr int STEPS = DEEP / 16, BLOCKS = DEEP / 32, WINDOW = window_of_tile(DEEP, BUCKETS);
+    constexpr int STEPS = DEEP / 16, BLOCKS = DEEP / 32, WINDOW = window_of_tile(DEEP);
     const attention_args &A = G.a;
     __shared__ __attribute__((aligned(16))) uint8_t room[4 * tile::BYTES + (BIAS ? 2 * WINDOW * 4 : 0)];
-    __shared__ __attribute__((aligned(16))) table_sums<BUCKETS> sums;
+    __shared__ __attribute__((aligned(16))) table_sums<BUCKETS, WINDOW> sums;
     __shared__ int places[BIAS ? 2 : 1][TILE];
     lds_byte *const lds = (lds_byte *)room;
     const int lane = threadIdx.x % WAVE, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
@@ -86,7 +104,7 @@ template <int DEEP, bool DIRECT, bool BIAS, int BUCKETS> __global__ __launch_bou
     const int64_t units = (int64_t)A.batch * tiles;
     if constexpr (BUCKETS != 0) {
         for (int b = threadIdx.x; b < BUCKETS; b += BLOCK) sums.bucket[b] = 0.0f;
-        for (int b = threadIdx.x; b < 2 * WAVES * SUMS; b += BLOCK) (&sums.difference[0][0][0])[b] = 0.0f;
+        for (int b = threadIdx.x; b < WINDOW; b += BLOCK) sums.difference[b] = 0;
     }
 
     const int64_t block = unit_of(blockIdx.x, gridDim.x);
@@ -118,30 +136,32 @@ template <int DEEP, bool DIRECT, bool BIAS, int BUCKETS> __global__ __launch_bou
 
         key_walk at(A.mask ? A.mask + item * A.mask_item : nullptr, A.keys, lane);
         line_window window{}, coming{}, before{};
-        bool fours = false, coming_fours = false, pending = false;
+        bool fours = false, coming_fours = false, rising = false, coming_rising = false, pending = false;
         int place = 0, turn = 0, duty = 0;
+        float unscale = 0.0f;
+        const bool sound = __all(base == base && finite_magnitude(delta) | (delta == 0.0f));       // what is not a number in a query's pairs is in these
         const auto fetch = [&](int to) {
             lds_byte *const kt = lds + to * 2 * tile::BYTES;
             k.fetch(at.first, at.bits, kt, wave, lane);
             v.fetch(at.first, at.bits, kt + tile::BYTES, wave, lane);
             if constexpr (BIAS) {
                 const place_range keys = A.key_places[at.first / TILE];
-                coming = window_of(A, keys, mine, WINDOW), coming_fours = keys.fours;
-                if (coming.inside) fetch_window(line, A.offsets, coming, lds + 4 * tile::BYTES + to * WINDOW * 4, wave, lane);
+                coming = window_of(A, keys, mine, WINDOW), coming_fours = keys.fours, coming_rising = keys.rising;
+                if (coming.inside) fetch_window<4>(line, A.offsets, coming, lds + 4 * tile::BYTES + to * WINDOW * 4, wave, lane);
                 if (wave == 0) place = key_position(A, at.first + lane < A.keys ? (int)at.first + lane : A.keys - 1);
             }
         };
         // The sums of the tile before, by the wave whose turn it is.
-        const auto settle = [&](int of) {
-            if constexpr (BUCKETS != 0)
+        const auto settle = [&] {
+            if constexpr (BUCKETS != 0) {
                 if (pending && wave == duty)
                     for (int i = lane; i < before.count; i += WAVE) {
-                        float s = 0.0f;
-#pragma unroll
-                        for (int w = 0; w < WAVES; ++w) s += sums.difference[of][w][i], sums.difference[of][w][i] = 0.0f;
-                        __hip_atomic_fetch_add(&sums.bucket[sums.which[of][i]], s, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+                        const float s = (float)sums.difference[i] * unscale;
+                        sums.difference[i] = 0;
+                        __hip_atomic_fetch_add(&sums.bucket[sums.which[i]], s, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
                     }
-            duty = (duty + 1) % WAVES;
+                duty = (duty + 1) % WAVES;
+            }
         };
         __syncthreads();                                   // the unit before has read its tiles
         if (!at.done()) fetch(0);
@@ -151,61 +171,93 @@ template <int DEEP, bool DIRECT, bool BIAS, int BUCKETS> __global__ __launch_bou
             k.land(kt), v.land(vt);
             if constexpr (BIAS) {
                 if (wave == 0) places[turn][lane] = place;
-                window = coming, fours = coming_fours;
+                window = coming, fours = coming_fours, rising = coming_rising;
             }
             if constexpr (DIRECT || BIAS) fetched();
             __syncthreads();
-            const bool near = BUCKETS && window.inside && window.count <= SUMS;
-            if constexpr (BUCKETS != 0)
-                if (near) fetch_window(A.line_buckets, A.offsets, window, (lds_byte *)sums.which[turn], wave, lane);
             at.next(lane);
             if (!at.done()) fetch(turn ^ 1);
-            settle(turn ^ 1);
+            settle();
             const int from_line = address_of(lds + 4 * tile::BYTES + turn * WINDOW * 4) + 4 * (A.offsets / 2 - window.first - position);
-            int to_sums = 0;                               // from a number of the line to the wave's sum of its pairs
-            if constexpr (BUCKETS != 0) to_sums = address_of((lds_byte *)sums.difference[turn][wave]) - address_of(lds + 4 * tile::BYTES + turn * WINDOW * 4);
+            f32x16 x[2];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                f32x16 x = zeros(), dp = zeros();
+                x[h] = zeros();
+                f32x16 dp = zeros();
 #pragma unroll
-                for (int s = 0; s < STEPS; ++s) x = product(tile::along(kt, h * 32, s, lane), q[s], x);
+                for (int s = 0; s < STEPS; ++s) x[h] = product(tile::along(kt, h * 32, s, lane), q[s], x[h]);
 #pragma unroll
                 for (int s = 0; s < STEPS; ++s) dp = product(tile::along(vt, h * 32, s, lane), g[s], dp);
                 const uint32_t held = (uint32_t)(bits >> (h * 32)) >> (lane / 32 * 4);
                 const auto ds_of = [&](int r, float exponent) {
-                    x[r] = __builtin_amdgcn_exp2f(exponent) * (dp[r] - delta);
-                    if (~bits) x[r] = held >> row_of(r) & 1 ? x[r] : 0.0f;
+                    x[h][r] = __builtin_amdgcn_exp2f(exponent) * (dp[r] - delta);
+                    if (~bits) x[h][r] = held >> row_of(r) & 1 ? x[h][r] : 0.0f;
                 };
                 if constexpr (BIAS) {
                     if (window.inside)
-                        over_places<1>(places[turn] + h * 32, fours, from_line, lane, [&](int r, int byte) {
-                            ds_of(r, __builtin_fmaf(x[r], scale, number_at(byte)) - stats.most - stats.log);
-                            if constexpr (BUCKETS != 0)
-                                if (near) add_at(byte + to_sums, x[r]);
-                        });
+                        over_places<1>(places[turn] + h * 32, fours, from_line, lane,
+                                       [&](int r, int byte) { ds_of(r, __builtin_fmaf(x[h][r], scale, number_at(byte)) - stats.most - stats.log); });
                     else
 #pragma unroll
                         for (int r = 0; r < 16; ++r)
-                            ds_of(r, __builtin_fmaf(x[r], scale, line[line_at(A, places[turn][h * 32 + row_of(r) + lane / 32 * 4], position)]) - stats.most - stats.log);
-                    if constexpr (BUCKETS != 0)
-                        if (!near)
-                            for (int w = 0; w < WAVES; ++w) {
-                                __syncthreads();
-                                if (w == wave)
-#pragma unroll
-                                    for (int r = 0; r < 16; ++r)
-                                        __hip_atomic_fetch_add(&sums.bucket[A.line_buckets[line_at(A, places[turn][h * 32 + row_of(r) + lane / 32 * 4], position)]], x[r], __ATOMIC_RELAXED,
-                                                               __HIP_MEMORY_SCOPE_WORKGROUP);
-                            }
+                            ds_of(r, __builtin_fmaf(x[h][r], scale, line[line_at(A, places[turn][h * 32 + row_of(r) + lane / 32 * 4], position)]) - stats.most - stats.log);
                 } else {
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) ds_of(r, __builtin_fmaf(x[r], scale, -base));
+                    for (int r = 0; r < 16; ++r) ds_of(r, __builtin_fmaf(x[h][r], scale, -base));
                 }
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
-                    const bf16x8 ds = eight(x, t);
+                    const bf16x8 ds = eight(x[h], t);
 #pragma unroll
                     for (int b = 0; b < BLOCKS; ++b) sum[b] = product(tile::across(kt, h * 32 + t * 16, b, lane), ds, sum[b]);
+                }
+            }
+            const bool near = window.inside && rising;
+            if constexpr (BUCKETS != 0) {
+                float largest = 0.0f;
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) largest = fmaxf(largest, fabsf(x[h][r]));
+                largest = sound ? wave_max(largest) : __builtin_nanf("");
+                if (lane == 0) sums.peak[wave] = largest;
+                shared_barrier();                          // and the sums before are settled
+                largest = 1e-30f;
+                float all = 0.0f;
+#pragma unroll
+                for (int w = 0; w < WAVES; ++w) largest = fmaxf(largest, sums.peak[w]), all += sums.peak[w];
+                all = all == all ? largest : all;          // not a number: nor are the sums
+                if (near) {
+                    fetch_window<2>(A.line_buckets, A.offsets, window, (lds_byte *)sums.which, wave, lane);
+                    const float by = 0x1.fp23f / largest;
+                    unscale = all * (1.0f / 0x1.fp23f);
+                    const int to_sums = address_of((lds_byte *)sums.difference) + 4 * (A.offsets / 2 - window.first - position);
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+                        over_places<1>(places[turn] + h * 32, fours, to_sums, lane, [&](int r, int byte) { add_at(byte, __float2int_rn(x[h][r] * by)); });
+                } else {
+                    constexpr int AT_ONCE = WINDOW / 2;
+                    const float by = 0x1.fp16f / largest;
+                    unscale = all * (1.0f / 0x1.fp16f);
+                    for (int first = 0; first < A.buckets; first += AT_ONCE) {
+#pragma unroll
+                        for (int h = 0; h < 2; ++h)
+#pragma unroll
+                            for (int r = 0; r < 16; ++r) {
+                                const int b = A.line_buckets[line_at(A, places[turn][h * 32 + row_of(r) + lane / 32 * 4], position)] - first;
+                                const float v = x[h][r] * by, upper = rintf(v);
+                                if (b >= 0 && b < AT_ONCE) {
+                                    __hip_atomic_fetch_add(&sums.difference[b * 2], (int)upper, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+                                    __hip_atomic_fetch_add(&sums.difference[b * 2 + 1], __float2int_rn((v - upper) * 0x1p17f), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+                                }
+                            }
+                        shared_barrier();
+                        for (int b = threadIdx.x; b < AT_ONCE && first + b < A.buckets; b += BLOCK) {
+                            sums.bucket[first + b] += ((float)sums.difference[b * 2] + (float)sums.difference[b * 2 + 1] * 0x1p-17f) * unscale;
+                            sums.difference[b * 2] = sums.difference[b * 2 + 1] = 0;
+                        }
+                        shared_barrier();
+                    }
                 }
             }
             pending = near, before = window;
@@ -214,7 +266,7 @@ template <int DEEP, bool DIRECT, bool BIAS, int BUCKETS> __global__ __launch_bou
         if constexpr (BUCKETS != 0) {
             fetched();                                     // the last tile's buckets
             __syncthreads();
-            settle(turn ^ 1);
+            settle();
         }
         if (G.grad_q) store_column<BLOCKS>(G.grad_q + ((item * A.queries + query) * A.heads + head) * width, width, sum, A.scale, lane, there);
         unit += G.parts;
@@ -286,7 +338,7 @@ template <int DEEP, bool DIRECT, bool BIAS> __global__ __launch_bounds__(BLOCK, 
                 if constexpr (BIAS) {
                     const place_range queries = A.query_places[at];
                     coming = window_of(A, mine, queries, WINDOW), coming_fours = queries.fours;
-                    if (coming.inside) fetch_window(line, A.offsets, coming, lds + 4 * tile::BYTES + to * WINDOW * 4, wave, lane);
+                    if (coming.inside) fetch_window<4>(line, A.offsets, coming, lds + 4 * tile::BYTES + to * WINDOW * 4, wave, lane);
                 }
                 if (wave == 0) {
                     const bool in = first + lane < A.queries;
