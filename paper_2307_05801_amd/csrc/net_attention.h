@@ -252,23 +252,23 @@ template <int SIZE> __device__ inline void fetch_window(const void *line, int le
     for (int piece = wave; piece * (1024 / SIZE) < w.count; piece += WAVES) fetch16(from, (uint32_t)w.first * SIZE + piece * 1024 + lane * 16, to + piece * 1024);
 }
 
-// f(r, number) for the sixteen pairs of a lane's position with the rows 8 a + 4 (lane / 32) + c of `places`.  The rows are keys (SIGN 1) or queries (-1).  at: the byte
-// in shared memory of a row at position 0.
-template <int SIGN, class F> __device__ inline void over_places(const int *places, bool fours, int at, int lane, F &&f)
+// f(r, p) for the sixteen pairs of a lane's position with the rows 8 a + 4 (lane / 32) + c of `places`: *p is the pair's number.  The rows are keys (SIGN 1) or queries
+// (-1).  at: the byte in shared memory of the number of a row at position 0.
+template <int SIGN, class T, class F> __device__ inline void over_places(const int *places, bool fours, int at, int lane, F &&f)
 {
+    typedef __attribute__((address_space(3))) T *numbers;
     if (fours) {
 #pragma unroll
         for (int a = 0; a < 4; ++a) {
-            const int begin = at + SIGN * 4 * places[a * 8 + lane / 32 * 4];
+            const numbers begin = (numbers)(uintptr_t)(uint32_t)(at + SIGN * 4 * (places[a * 8 + lane / 32 * 4] + (SIGN < 0 ? 3 : 0)));
 #pragma unroll
-            for (int c = 0; c < 4; ++c) f(a * 4 + c, begin + SIGN * 4 * c);
+            for (int c = 0; c < 4; ++c) f(a * 4 + c, begin + (SIGN < 0 ? 3 - c : c));
         }
     } else {
 #pragma unroll
-        for (int r = 0; r < 16; ++r) f(r, at + SIGN * 4 * places[row_of(r) + lane / 32 * 4]);
+        for (int r = 0; r < 16; ++r) f(r, (numbers)(uintptr_t)(uint32_t)(at + SIGN * 4 * places[row_of(r) + lane / 32 * 4]));
     }
 }
-__device__ inline float number_at(int address) { return *(__attribute__((address_space(3))) const float *)(uintptr_t)(uint32_t)address; }
 __device__ inline int address_of(const lds_byte *p) { return (int)(uint32_t)(uintptr_t)p; }
 
 __device__ inline bf16x8 eight(const f32x16 &v, int m)
@@ -279,14 +279,17 @@ __device__ inline bf16x8 eight(const f32x16 &v, int m)
     return r;
 }
 
-// What rounding to eight() leaves.
-__device__ inline bf16x8 rest_of_eight(const f32x16 &v, int m)
+// What rounding v's m-th eight to `rounded` leaves (nothing here is infinite).
+__device__ inline bf16x8 rest_of_eight(const f32x16 &v, int m, const bf16x8 &rounded)
 {
     bf16x8 r;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) r[i] = (__bf16)rest_of_bf16(v[m * 8 + i]);
+    for (int i = 0; i < 8; ++i) r[i] = (__bf16)(v[m * 8 + i] - (float)rounded[i]);
     return r;
 }
+
+// Inside a branch that is seldom taken: it stays one, instead of selections that are always made.
+__device__ inline void seldom() { asm volatile(""); }
 
 __device__ inline f32x16 product(const bf16x8 &a, const bf16x8 &b, const f32x16 &c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
 

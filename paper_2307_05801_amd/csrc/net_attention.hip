@@ -57,7 +57,7 @@ template <int DEEP, bool DIRECT, bool BIAS, bool FINE> __global__ __launch_bound
     key_walk at(A.mask ? A.mask + item * A.mask_item : nullptr, A.keys, lane);
     line_window window, coming;
     bool fours = false, coming_fours = false;
-    int place = 0, turn = 0;
+    int place = 0;
     const auto fetch = [&](int to) {                   // the walk's tile
         lds_byte *const kt = lds + to * 2 * tile::BYTES;
         k.fetch(at.first, at.bits, kt, wave, lane);
@@ -70,7 +70,9 @@ template <int DEEP, bool DIRECT, bool BIAS, bool FINE> __global__ __launch_bound
         }
     };
     if (!at.done()) fetch(0);
-    while (!at.done()) {
+    // A tile; which of the two pairs it lies in is a constant, so that addresses in shared memory are.
+    const auto one = [&](auto which) {
+        constexpr int turn = decltype(which)::value;
         lds_byte *const kt = lds + turn * 2 * tile::BYTES, *const vt = kt + tile::BYTES;
         const uint64_t bits = at.bits;
         k.land(kt), v.land(vt);
@@ -95,12 +97,13 @@ template <int DEEP, bool DIRECT, bool BIAS, bool FINE> __global__ __launch_bound
 #pragma unroll
             for (int h = 0; h < 2; ++h)
                 if (window.inside)
-                    over_places<1>(places[turn] + h * 32, fours, from, lane, [&](int r, int byte) { x[h][r] = __builtin_fmaf(x[h][r], scale, number_at(byte)); });
+                    over_places<1, const float>(places[turn] + h * 32, fours, from, lane, [&](int r, auto number) { x[h][r] = __builtin_fmaf(x[h][r], scale, *number); });
                 else
 #pragma unroll
                     for (int r = 0; r < 16; ++r) x[h][r] = __builtin_fmaf(x[h][r], scale, line[line_at(A, places[turn][h * 32 + row_of(r) + lane / 32 * 4], position)]);
         }
         if (~bits) {
+            seldom();
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const uint32_t held = (uint32_t)(bits >> (h * 32)) >> (lane / 32 * 4);
@@ -133,7 +136,7 @@ template <int DEEP, bool DIRECT, bool BIAS, bool FINE> __global__ __launch_bound
         for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
-                const bf16x8 p = eight(x[h], t), low = FINE ? rest_of_eight(x[h], t) : p;
+                const bf16x8 p = eight(x[h], t), low = FINE ? rest_of_eight(x[h], t, p) : p;
 #pragma unroll
                 for (int b = 0; b < BLOCKS; ++b) {
                     const bf16x8 values = tile::across(vt, h * 32 + t * 16, b, lane);
@@ -141,7 +144,11 @@ template <int DEEP, bool DIRECT, bool BIAS, bool FINE> __global__ __launch_bound
                     if constexpr (FINE) o[b] = product(values, low, o[b]);
                 }
             }
-        turn ^= 1;
+    };
+    while (!at.done()) {
+        one(std::integral_constant<int, 0>{});
+        if (at.done()) break;
+        one(std::integral_constant<int, 1>{});
     }
     sum = column_sum(sum);
     const float by = sum != 0.0f ? 1.0f / sum : 0.0f;                 // (a sum that is not a number: so is o)

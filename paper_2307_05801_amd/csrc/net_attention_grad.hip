@@ -85,9 +85,12 @@ __device__ inline float wave_max(float v)
     return column_max(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
 }
 
-__device__ inline void add_at(int address, int v)
+// The largest whole number that is not above v: one instruction.
+__device__ inline int floor_of(float v)
 {
-    __hip_atomic_fetch_add((__attribute__((address_space(3))) int *)(uintptr_t)(uint32_t)address, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+    int i;
+    asm("v_cvt_flr_i32_f32 %0, %1" : "=v"(i) : "v"(v));
+    return i;
 }
 
 template <int DEEP, bool DIRECT, bool BIAS, int BUCKETS> __global__ __launch_bounds__(BLOCK, 2) void k_grad_query(grad_args G)
@@ -127,6 +130,8 @@ template <int DEEP, bool DIRECT, bool BIAS, int BUCKETS> __global__ __launch_bou
         const int64_t row = (item * A.heads + head) * (int64_t)A.queries + query;
         const query_stats stats = there ? stats_of(G, row) : query_stats{0.0f, INFINITY};
         const float delta = there ? G.delta[row] : 0.0f, base = stats.most + stats.log;
+        // with a table scores can be so large that the logarithm of their sum is lost in `base`: what is missing is a factor of the query's
+        const float factor = BIAS && stats.log < INFINITY ? __builtin_amdgcn_exp2f(base - stats.most - stats.log) : 0.0f, lowered = factor * delta;
         const int position = BIAS ? query_position(A, there ? query : A.queries - 1) : 0;
         place_range mine;
         if constexpr (BIAS) mine = both(A.query_places[query0 / TILE], A.query_places[query0 + TILE < A.queries ? query0 / TILE + 1 : query0 / TILE]);
@@ -137,7 +142,7 @@ template <int DEEP, bool DIRECT, bool BIAS, int BUCKETS> __global__ __launch_bou
         key_walk at(A.mask ? A.mask + item * A.mask_item : nullptr, A.keys, lane);
         line_window window{}, coming{}, before{};
         bool fours = false, coming_fours = false, rising = false, coming_rising = false, pending = false;
-        int place = 0, turn = 0, duty = 0;
+        int place = 0, duty = 0;
         float unscale = 0.0f;
         const bool sound = __all(base == base && finite_magnitude(delta) | (delta == 0.0f));       // what is not a number in a query's pairs is in these
         const auto fetch = [&](int to) {
@@ -165,7 +170,8 @@ template <int DEEP, bool DIRECT, bool BIAS, int BUCKETS> __global__ __launch_bou
         };
         __syncthreads();                                   // the unit before has read its tiles
         if (!at.done()) fetch(0);
-        while (!at.done()) {
+        const auto one = [&](auto pair) {
+            const int turn = pair;
             lds_byte *const kt = lds + turn * 2 * tile::BYTES, *const vt = kt + tile::BYTES;
             const uint64_t bits = at.bits;
             k.land(kt), v.land(vt);
@@ -190,20 +196,24 @@ template <int DEEP, bool DIRECT, bool BIAS, int BUCKETS> __global__ __launch_bou
                 for (int s = 0; s < STEPS; ++s) dp = product(tile::along(vt, h * 32, s, lane), g[s], dp);
                 const uint32_t held = (uint32_t)(bits >> (h * 32)) >> (lane / 32 * 4);
                 const auto ds_of = [&](int r, float exponent) {
-                    x[h][r] = __builtin_amdgcn_exp2f(exponent) * (dp[r] - delta);
-                    if (~bits) x[h][r] = held >> row_of(r) & 1 ? x[h][r] : 0.0f;
+                    x[h][r] = __builtin_amdgcn_exp2f(exponent) * (BIAS ? __builtin_fmaf(dp[r], factor, -lowered) : dp[r] - delta);
                 };
                 if constexpr (BIAS) {
                     if (window.inside)
-                        over_places<1>(places[turn] + h * 32, fours, from_line, lane,
-                                       [&](int r, int byte) { ds_of(r, __builtin_fmaf(x[h][r], scale, number_at(byte)) - stats.most - stats.log); });
+                        over_places<1, const float>(places[turn] + h * 32, fours, from_line, lane,
+                                                    [&](int r, auto number) { ds_of(r, __builtin_fmaf(x[h][r], scale, *number) - base); });
                     else
 #pragma unroll
                         for (int r = 0; r < 16; ++r)
-                            ds_of(r, __builtin_fmaf(x[h][r], scale, line[line_at(A, places[turn][h * 32 + row_of(r) + lane / 32 * 4], position)]) - stats.most - stats.log);
+                            ds_of(r, __builtin_fmaf(x[h][r], scale, line[line_at(A, places[turn][h * 32 + row_of(r) + lane / 32 * 4], position)]) - base);
                 } else {
 #pragma unroll
                     for (int r = 0; r < 16; ++r) ds_of(r, __builtin_fmaf(x[h][r], scale, -base));
+                }
+                if (~bits) {
+                    seldom();
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) x[h][r] = held >> row_of(r) & 1 ? x[h][r] : 0.0f;
                 }
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
@@ -234,7 +244,9 @@ template <int DEEP, bool DIRECT, bool BIAS, int BUCKETS> __global__ __launch_bou
                     const int to_sums = address_of((lds_byte *)sums.difference) + 4 * (A.offsets / 2 - window.first - position);
 #pragma unroll
                     for (int h = 0; h < 2; ++h)
-                        over_places<1>(places[turn] + h * 32, fours, to_sums, lane, [&](int r, int byte) { add_at(byte, __float2int_rn(x[h][r] * by)); });
+                        over_places<1, int>(places[turn] + h * 32, fours, to_sums, lane, [&](int r, auto sum_of) {
+                            __hip_atomic_fetch_add(sum_of, floor_of(__builtin_fmaf(x[h][r], by, 0.5f)), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+                        });
                 } else {
                     constexpr int AT_ONCE = WINDOW / 2;
                     const float by = 0x1.fp16f / largest;
@@ -261,8 +273,8 @@ template <int DEEP, bool DIRECT, bool BIAS, int BUCKETS> __global__ __launch_bou
                 }
             }
             pending = near, before = window;
-            turn ^= 1;
-        }
+        };
+        for (int turn = 0; !at.done(); turn ^= 1) one(turn);
         if constexpr (BUCKETS != 0) {
             fetched();                                     // the last tile's buckets
             __syncthreads();
@@ -349,15 +361,15 @@ template <int DEEP, bool DIRECT, bool BIAS> __global__ __launch_bounds__(BLOCK, 
             };
             __syncthreads();                               // the head before has read its tiles
             if (tiles) fetch(0, 0);
-            for (int at = 0; at < tiles; ++at) {
-                const int turn = at % 2;
+            const auto one = [&](int at, auto pair) {
+                const int turn = pair;
                 lds_byte *const qt = lds + turn * 2 * tile::BYTES, *const gt = qt + tile::BYTES;
                 q.land(qt), g.land(gt);
                 if (wave == 0) {
                     most[turn][lane] = BIAS ? stats.most : stats.most + stats.log;
                     log[turn][lane] = stats.log;
                     delta[turn][lane] = nd;
-                    if (BIAS) places[turn][lane] = place;
+                    if constexpr (BIAS) places[turn][lane] = place;
                 }
                 if constexpr (BIAS) window = coming, fours = coming_fours;
                 if constexpr (DIRECT || BIAS) fetched();
@@ -381,7 +393,7 @@ template <int DEEP, bool DIRECT, bool BIAS> __global__ __launch_bounds__(BLOCK, 
                     };
                     if constexpr (BIAS) {
                         if (window.inside)
-                            over_places<-1>(places[turn] + h * 32, fours, from_line, lane, [&](int r, int byte) { p_of(r, lowered(r, __builtin_fmaf(x[r], scale, number_at(byte)))); });
+                            over_places<-1, const float>(places[turn] + h * 32, fours, from_line, lane, [&](int r, auto number) { p_of(r, lowered(r, __builtin_fmaf(x[r], scale, *number))); });
                         else
 #pragma unroll
                             for (int r = 0; r < 16; ++r) p_of(r, lowered(r, __builtin_fmaf(x[r], scale, line[line_at(A, position, places[turn][h * 32 + row_of(r) + lane / 32 * 4])])));
@@ -399,7 +411,16 @@ template <int DEEP, bool DIRECT, bool BIAS> __global__ __launch_bounds__(BLOCK, 
                         }
                     }
                 }
-            }
+            };
+            // Two tiles a turn, so that addresses in shared memory are constants: pays (12.3 to 10.4 ms for 32768 patches of 128) where a wave has its SIMD's registers to
+            // itself, not where their number decides (512 windows of 512 patches of 64: 1.42 ms, 1.14 so)
+            if constexpr (DEEP > 64)
+                for (int at = 0; at < tiles; at += 2) {
+                    one(at, std::integral_constant<int, 0>{});
+                    if (at + 1 < tiles) one(at + 1, std::integral_constant<int, 1>{});
+                }
+            else
+                for (int at = 0; at < tiles; ++at) one(at, at % 2);
         }
     }
     // a key that is left out has whatever its zeros gave
