@@ -131,6 +131,11 @@ template <int DEEP> struct source<DEEP, true> {
     __device__ inline void fetch(int64_t first, uint64_t there, lds_byte *to, int wave, int lane) const
     {
         const u32x4 from = window{base + first * stride, end - first * stride, 0}.buffer();
+        if (!~there) {
+#pragma unroll
+            for (int e = 0; e < EACH; ++e) fetch16(from, offset[e], to + (e * WAVES + wave) * 1024);
+            return;
+        }
 #pragma unroll
         for (int e = 0; e < EACH; ++e) {
             const int piece = e * WAVES + wave, r = (piece * 64 + lane) * 16 / tile::ROW;
@@ -178,15 +183,15 @@ __device__ inline uint64_t rows_there(const uint8_t *mask, int64_t first, int64_
 // The tiles of an item's keys that have any, one after the other; the mask's bytes are asked for a tile ahead.
 struct key_walk {
     const uint8_t *mask;
-    int keys;
-    int64_t first;
+    int64_t keys, first;
     uint64_t bits;
     uint8_t ahead;
 
     __device__ inline uint8_t ask(int64_t at, int lane) const { return at + lane < keys ? mask ? mask[at + lane] : 1 : 0; }
-    __device__ inline key_walk(const uint8_t *mask_, int keys_, int lane) : mask(mask_), keys(keys_), first(-TILE)
+    // From `begin`, a multiple of TILE, to `end`.
+    __device__ inline key_walk(const uint8_t *mask_, int64_t begin, int64_t end, int lane) : mask(mask_), keys(end), first(begin - TILE)
     {
-        ahead = ask(0, lane);
+        ahead = ask(begin, lane);
         next(lane);
     }
     __device__ inline void next(int lane)

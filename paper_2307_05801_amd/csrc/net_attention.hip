@@ -2,7 +2,8 @@
 //
 // A block has 128 queries of a head, 32 to a wave, whose values stay in registers; it walks over the keys in tiles of 64, which all four waves
 // read from shared memory.  A wave forms x for 32 keys by 32 queries with a lane a query (net_attention.h says why), keeps the largest so far, m, and
-// the sum of exp2(x - m) of each query in that lane, and multiplies the values summed so far by exp2(m before - m now) where a query's m has grown.
+// the sum of exp2(x - m) of each query in that lane, and multiplies the values summed so far by exp2(m before - m now) where m has grown.  m follows the largest only when a
+// query's has got 2^8 ahead of it: sums of exp2 up to 2^8 are as good, and one of 32 queries has a new largest in nearly every tile.
 #include "net_attention.h"
 
 namespace {
@@ -13,13 +14,20 @@ using namespace net;
 // of 27 x 22 patches and the next one's beginning.  As many as leave a compute unit room for two blocks.
 constexpr int window_of_tile(int deep) { return deep > 64 ? 1024 : 2048; }
 
-// What becomes of a query beside o.
 struct forward_args {
     attention_args a;
     uint16_t *o;
-    float *stats;
-    uint16_t *rest;
+    float *stats;                          // [item][head][query][2], or null
+    uint16_t *rest;                        // what o's rounding leaves
+    // Where queries are few: so many of a block's waves are heads that share keys, not more queries; the keys go to `parts` blocks, `length` of them each (whole
+    // tiles), whose sums (of a query [parts][width], and [parts][2]: m and the sum of exp2) k_join puts together.
+    int32_t abreast, parts, length;
+    float *part_sums, *part_stats;
+    int64_t first;                         // block of this launch of k_join
 };
+
+// What rounding v to bfloat16 leaves, as it is kept.
+__device__ inline uint16_t rest_of(float v) { return element<LEAP_F16>::from_float(rest_of_bf16(v) * 256.0f); }
 
 // BIAS: with a table.  FINE: for a backward pass, which takes delta = grad.o off every product grad.v of a query: an o with its rounding, or with the probabilities',
 // would spoil all of the query's alike, and in grad_q that adds up along what the keys have in common (keys and values with a common part as large as what
@@ -34,10 +42,13 @@ template <int DEEP, bool DIRECT, bool BIAS, bool FINE> __global__ __launch_bound
     __shared__ int places[BIAS ? 2 : 1][TILE];
     lds_byte *const lds = (lds_byte *)room;
     const int lane = threadIdx.x % WAVE, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
-    const int tiles = (A.queries + COLS - 1) / COLS;
-    const int64_t unit = unit_of(blockIdx.x, gridDim.x), item = unit / tiles / A.heads;
-    const int head = (int)(unit / tiles % A.heads), kv_head = head / (A.heads / A.kv_heads);
-    const int query0 = (int)(unit % tiles) * COLS, query = query0 + wave * 32 + lane % 32;
+    const int cols = COLS / F.abreast, tiles = (A.queries + cols - 1) / cols;
+    int64_t unit = unit_of(blockIdx.x, gridDim.x);
+    const int part = (int)(unit % F.parts);
+    unit /= F.parts;
+    const int64_t item = unit / tiles / (A.heads / F.abreast);
+    const int head = (int)(unit / tiles % (A.heads / F.abreast)) * F.abreast + wave % F.abreast, kv_head = head / (A.heads / A.kv_heads);
+    const int query0 = (int)(unit % tiles) * cols, query = query0 + wave / F.abreast * 32 + lane % 32;
     const bool there = query < A.queries;
     source<DEEP, DIRECT> k(A.k.data + item * A.k.item + kv_head * A.k.head, A.k.row, A.keys, A.width, wave, lane);
     source<DEEP, DIRECT> v(A.v.data + item * A.v.item + kv_head * A.v.head, A.v.row, A.keys, A.width, wave, lane);
@@ -54,7 +65,9 @@ template <int DEEP, bool DIRECT, bool BIAS, bool FINE> __global__ __launch_bound
     for (int b = 0; b < BLOCKS; ++b) o[b] = zeros();
     float m = -INFINITY, sum = 0.0f;
 
-    key_walk at(A.mask ? A.mask + item * A.mask_item : nullptr, A.keys, lane);
+    const int64_t end = (int64_t)(part + 1) * F.length;
+    key_walk at(A.mask ? A.mask + item * A.mask_item : nullptr, (int64_t)part * F.length, end < A.keys ? end : A.keys, lane);
+    const bool idle = !__any(there);                   // a wave without queries brings tiles alone
     line_window window, coming;
     bool fours = false, coming_fours = false;
     int place = 0;
@@ -84,6 +97,7 @@ template <int DEEP, bool DIRECT, bool BIAS, bool FINE> __global__ __launch_bound
         __syncthreads();                               // two pairs of tiles: the one written next was read before this
         at.next(lane);
         if (!at.done()) fetch(turn ^ 1);
+        if (idle) return;
 
         f32x16 x[2];
 #pragma unroll
@@ -117,14 +131,15 @@ template <int DEEP, bool DIRECT, bool BIAS, bool FINE> __global__ __launch_bound
 #pragma unroll
             for (int r = 0; r < 16; ++r) most = fmaxf(most, x[h][r]);
         most = column_max(most);
-        const float now = fmaxf(m, BIAS ? most : most * scale), base = now == -INFINITY ? 0.0f : now;
-        if (__any(now > m)) {
-            const float by = __builtin_amdgcn_exp2f(m - base);
+        const float now = fmaxf(m, BIAS ? most : most * scale);
+        if (__any(now > m + 8.0f)) {                   // (the first keys of a query among them: m is -inf before)
+            const float by = now == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - now);
             sum *= by;
 #pragma unroll
             for (int b = 0; b < BLOCKS; ++b) o[b] *= by;
+            m = now;
         }
-        m = now;
+        const float base = m == -INFINITY ? 0.0f : m;
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -151,6 +166,19 @@ template <int DEEP, bool DIRECT, bool BIAS, bool FINE> __global__ __launch_bound
         one(std::integral_constant<int, 1>{});
     }
     sum = column_sum(sum);
+    if (F.parts > 1) {
+        if (!there) return;
+        const int64_t row = ((item * A.heads + head) * (int64_t)A.queries + query) * F.parts + part;
+        if (lane < 32) F.part_stats[row * 2] = m, F.part_stats[row * 2 + 1] = sum;
+#pragma unroll
+        for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const int at = b * 32 + row_of(r) + lane / 32 * 4;
+                if (at < A.width) F.part_sums[row * A.width + at] = o[b][r];
+            }
+        return;
+    }
     const float by = sum != 0.0f ? 1.0f / sum : 0.0f;                 // (a sum that is not a number: so is o)
     const int64_t row = (item * A.queries + query) * A.heads + head;
     store_column<BLOCKS>(F.o + row * A.width, A.width, o, by, lane, there);
@@ -166,9 +194,43 @@ template <int DEEP, bool DIRECT, bool BIAS, bool FINE> __global__ __launch_bound
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
                     const int at = b * 32 + row_of(r) + lane / 32 * 4;
-                    if (at < A.width) F.rest[row * A.width + at] = element<LEAP_F16>::from_float(rest_of_bf16(o[b][r] * by) * 256.0f);
+                    if (at < A.width) F.rest[row * A.width + at] = rest_of(o[b][r] * by);
                 }
     }
+}
+
+// A query of a head from its parts, a wave each.
+__global__ __launch_bounds__(BLOCK) void k_join(forward_args F)
+{
+    const attention_args &A = F.a;
+    const int lane = threadIdx.x % WAVE;
+    const int64_t row = (F.first + blockIdx.x) * WAVES + threadIdx.x / WAVE;               // (item, head, query)
+    if (row >= (int64_t)A.batch * A.heads * A.queries) return;
+    const float *const stats = F.part_stats + row * F.parts * 2;
+    float m = -INFINITY;
+    for (int p = lane; p < F.parts; p += WAVE) m = fmaxf(m, stats[p * 2]);
+#pragma unroll
+    for (int d = 1; d < WAVE; d *= 2) m = fmaxf(m, __shfl_xor(m, d));
+    const float base = m == -INFINITY ? 0.0f : m;
+    const float *const from = F.part_sums + row * F.parts * A.width;
+    float sum = 0.0f, o[2] = {};
+#pragma unroll 4
+    for (int p = 0; p < F.parts; ++p) {
+        const float by = __builtin_amdgcn_exp2f(stats[p * 2] - base);
+        sum += stats[p * 2 + 1] * by;
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            if (lane + i * WAVE < A.width) o[i] += from[(int64_t)p * A.width + lane + i * WAVE] * by;
+    }
+    const float by = sum != 0.0f ? 1.0f / sum : 0.0f;
+    const int64_t query = row % A.queries, head = row / A.queries % A.heads, item = row / A.queries / A.heads, to = (item * A.queries + query) * A.heads + head;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+        if (lane + i * WAVE < A.width) {
+            F.o[to * A.width + lane + i * WAVE] = element<LEAP_BF16>::from_float(o[i] * by);
+            if (F.rest) F.rest[to * A.width + lane + i * WAVE] = rest_of(o[i] * by);
+        }
+    if (F.stats && lane == 0) F.stats[row * 2] = sum != 0.0f ? base : 0.0f, F.stats[row * 2 + 1] = sum != 0.0f ? __builtin_amdgcn_logf(sum) : INFINITY;
 }
 
 // A head's number for every difference of positions; and what positions each tile of queries and of keys has.
@@ -271,9 +333,40 @@ attention_args arguments_of(const leap_attention_desc *d, const void *q, const v
 
 }  // namespace net
 
+namespace {
+
+// How the queries and keys of a call are dealt out to blocks.
+struct shares {
+    int32_t abreast, parts, length;
+    int64_t units;                         // blocks that have all keys
+};
+shares shares_of(const leap_attention_desc *d)
+{
+    shares S;
+    const int64_t group = d->heads / d->kv_heads, tiles = (d->keys + TILE - 1) / TILE;
+    S.abreast = d->d_table ? 1 : d->queries <= 32 && group % 4 == 0 ? 4 : d->queries <= 64 && group % 2 == 0 ? 2 : 1;
+    S.units = d->batch * (d->heads / S.abreast) * ((d->queries + COLS / S.abreast - 1) / (COLS / S.abreast));
+    // Half the chip without work and at least eight tiles to a block: parts of four tiles and more, as many as fill it four times over
+    int64_t parts = 1;
+    if (S.units > 0 && S.units <= 128 && tiles >= 8) {
+        parts = 1024 / S.units;
+        parts = parts < tiles / 4 ? parts : tiles / 4;
+    }
+    const int64_t each = tiles ? (tiles + parts - 1) / parts : 1;
+    S.parts = (int32_t)(tiles ? (tiles + each - 1) / each : 1);
+    S.length = (int32_t)(each * TILE);
+    return S;
+}
+int64_t part_bytes(const leap_attention_desc *d, const shares &S)
+{
+    return S.parts > 1 ? (d->batch * d->heads * d->queries * S.parts * (d->width + 2) * 4 + 15) / 16 * 16 : 0;
+}
+
+}  // namespace
+
 extern "C" int64_t leap_attention_work(const leap_attention_desc *desc)
 {
-    return bad_attention(desc) ? 0 : lines_bytes(desc);
+    return bad_attention(desc) ? 0 : lines_bytes(desc) + part_bytes(desc, shares_of(desc));
 }
 
 extern "C" int leap_attention(const leap_attention_desc *desc, const void *d_q, const void *d_k, const void *d_v, void *d_o, float *d_stats, void *d_rest,
@@ -283,20 +376,28 @@ extern "C" int leap_attention(const leap_attention_desc *desc, const void *d_q, 
     if (!desc->batch || !desc->queries) return LEAP_OK;
     if (!d_q || !d_o || (desc->keys && (!d_k || !d_v))) return refuse("null data pointer");
     if (!d_rest != !d_stats) return refuse("statistics and what o's rounding leaves: both or neither");
-    if (leap_attention_work(desc) && unaligned(d_work)) return refuse(NO_WORK);
-    forward_args F{arguments_of(desc, d_q, d_k, d_v), (uint16_t *)d_o, d_stats, (uint16_t *)d_rest};
-    const int64_t blocks = desc->batch * desc->heads * ((desc->queries + COLS - 1) / COLS);
+    const shares S = shares_of(desc);
+    if (lines_bytes(desc) + part_bytes(desc, S) && unaligned(d_work)) return refuse(NO_WORK);
+    forward_args F{arguments_of(desc, d_q, d_k, d_v), (uint16_t *)d_o, d_stats, (uint16_t *)d_rest, S.abreast, S.parts, S.length, nullptr, nullptr, 0};
+    const int64_t blocks = S.units * S.parts, rows = desc->batch * desc->heads * desc->queries;
     if (blocks >= (int64_t)1 << 24) return refuse("more than 2^31 rows of heads");
+    F.part_sums = (float *)((char *)d_work + lines_bytes(desc));
+    F.part_stats = F.part_sums + rows * S.parts * desc->width;
     const hipStream_t st = stream_of(hip_stream);
     if (desc->d_table) {
         const int rc = write_lines(F.a, d_work, st);
         if (rc != LEAP_OK) return rc;
     }
     const bool direct = direct_array(d_k, desc->k_item, desc->k_row, desc->k_head, desc->width) && direct_array(d_v, desc->v_item, desc->v_row, desc->v_head, desc->width);
-    return by_width(desc->width, [&](auto w) {
+    const int rc = by_width(desc->width, [&](auto w) {
         return by_flags([&](auto straight, auto bias, auto fine) {
             hipLaunchKernelGGL((k_attention<decltype(w)::value, decltype(straight)::value, decltype(bias)::value, decltype(fine)::value>), dim3((unsigned)blocks), dim3(BLOCK), 0, st, F);
             return launched();
         }, direct, desc->d_table != nullptr, d_rest != nullptr);
+    });
+    if (rc != LEAP_OK || S.parts == 1) return rc;
+    return over_blocks((rows + WAVES - 1) / WAVES, [&](int64_t first, unsigned n) {
+        F.first = first;
+        hipLaunchKernelGGL(k_join, dim3(n), dim3(BLOCK), 0, st, F);
     });
 }

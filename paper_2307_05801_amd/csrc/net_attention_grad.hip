@@ -139,7 +139,7 @@ template <int DEEP, bool DIRECT, bool BIAS, int BUCKETS> __global__ __launch_bou
 #pragma unroll
         for (int b = 0; b < BLOCKS; ++b) sum[b] = zeros();
 
-        key_walk at(A.mask ? A.mask + item * A.mask_item : nullptr, A.keys, lane);
+        key_walk at(A.mask ? A.mask + item * A.mask_item : nullptr, 0, A.keys, lane);
         line_window window{}, coming{}, before{};
         bool fours = false, coming_fours = false, rising = false, coming_rising = false, pending = false;
         int place = 0, duty = 0;
@@ -376,16 +376,20 @@ template <int DEEP, bool DIRECT, bool BIAS> __global__ __launch_bounds__(BLOCK, 
                 __syncthreads();
                 if (at + 1 < tiles) fetch(at + 1, turn ^ 1);
                 const int from_line = address_of(lds + 4 * tile::BYTES + turn * WINDOW * 4) + 4 * (A.offsets / 2 - window.first + position);
+                // Half a tile's scores and dp are multiplied while the other half's probabilities are formed: x[h] becomes p, dp[h] ds.
+                f32x16 x[2], dp[2];
+                const auto scores = [&](int h) {
+                    x[h] = zeros(), dp[h] = zeros();
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    f32x16 x = zeros(), dp = zeros();
-#pragma unroll
-                    for (int s = 0; s < STEPS; ++s) x = product(tile::along(qt, h * 32, s, lane), k[s], x);
-#pragma unroll
-                    for (int s = 0; s < STEPS; ++s) dp = product(tile::along(gt, h * 32, s, lane), v[s], dp);
+                    for (int s = 0; s < STEPS; ++s) {
+                        x[h] = product(tile::along(qt, h * 32, s, lane), k[s], x[h]);
+                        dp[h] = product(tile::along(gt, h * 32, s, lane), v[s], dp[h]);
+                    }
+                };
+                const auto probabilities = [&](int h) {
                     const auto p_of = [&](int r, float exponent) {
-                        x[r] = __builtin_amdgcn_exp2f(exponent);
-                        dp[r] = x[r] * (dp[r] - delta[turn][h * 32 + row_of(r) + lane / 32 * 4]);
+                        x[h][r] = __builtin_amdgcn_exp2f(exponent);
+                        dp[h][r] = x[h][r] * (dp[h][r] - delta[turn][h * 32 + row_of(r) + lane / 32 * 4]);
                     };
                     const auto lowered = [&](int r, float score) {
                         const int row = h * 32 + row_of(r) + lane / 32 * 4;
@@ -393,23 +397,54 @@ template <int DEEP, bool DIRECT, bool BIAS> __global__ __launch_bounds__(BLOCK, 
                     };
                     if constexpr (BIAS) {
                         if (window.inside)
-                            over_places<-1, const float>(places[turn] + h * 32, fours, from_line, lane, [&](int r, auto number) { p_of(r, lowered(r, __builtin_fmaf(x[r], scale, *number))); });
+                            over_places<-1, const float>(places[turn] + h * 32, fours, from_line, lane,
+                                                         [&](int r, auto number) { p_of(r, lowered(r, __builtin_fmaf(x[h][r], scale, *number))); });
                         else
 #pragma unroll
-                            for (int r = 0; r < 16; ++r) p_of(r, lowered(r, __builtin_fmaf(x[r], scale, line[line_at(A, position, places[turn][h * 32 + row_of(r) + lane / 32 * 4])])));
+                            for (int r = 0; r < 16; ++r)
+                                p_of(r, lowered(r, __builtin_fmaf(x[h][r], scale, line[line_at(A, position, places[turn][h * 32 + row_of(r) + lane / 32 * 4])])));
                     } else {
 #pragma unroll
-                        for (int r = 0; r < 16; ++r) p_of(r, __builtin_fmaf(x[r], scale, -most[turn][h * 32 + row_of(r) + lane / 32 * 4]));
+                        for (int r = 0; r < 16; ++r) p_of(r, __builtin_fmaf(x[h][r], scale, -most[turn][h * 32 + row_of(r) + lane / 32 * 4]));
                     }
+                };
+                const auto gradients = [&](int h) {
 #pragma unroll
                     for (int t = 0; t < 2; ++t) {
-                        const bf16x8 p = eight(x, t), ds = eight(dp, t);
+                        const bf16x8 p = eight(x[h], t), ds = eight(dp[h], t);
 #pragma unroll
                         for (int b = 0; b < BLOCKS; ++b) {
                             gv[b] = product(tile::across(gt, h * 32 + t * 16, b, lane), p, gv[b]);
                             gk[b] = product(tile::across(qt, h * 32 + t * 16, b, lane), ds, gk[b]);
                         }
                     }
+                };
+                if constexpr (DEEP > 64) {
+                    scores(0);
+                    scores(1);
+                    probabilities(0);
+                    gradients(0);
+                    probabilities(1);
+                    gradients(1);
+                    // A wave has its SIMD to itself: reads of shared memory go ahead of the products that want them, and the probabilities' vector instructions between products.
+                    constexpr int MFMA = 0x8, VECTOR = 0x2, READ = 0x100;
+                    const auto products = [&](auto count, auto reads, auto vectors) {
+#pragma unroll
+                        for (int i = 0; i < decltype(count)::value; ++i) {
+                            __builtin_amdgcn_sched_group_barrier(MFMA, 1, 0);
+                            __builtin_amdgcn_sched_group_barrier(READ, decltype(reads)::value, 0);
+                            if constexpr (decltype(vectors)::value) __builtin_amdgcn_sched_group_barrier(VECTOR, decltype(vectors)::value, 0);
+                        }
+                    };
+                    using std::integral_constant;
+                    __builtin_amdgcn_sched_group_barrier(READ, 6, 0);
+                    products(integral_constant<int, 2 * STEPS + 10>{}, integral_constant<int, 1>{}, integral_constant<int, 0>{});
+                    products(integral_constant<int, 2 * STEPS - 10>{}, integral_constant<int, 2>{}, integral_constant<int, 0>{});
+                    products(integral_constant<int, 4 * BLOCKS>{}, integral_constant<int, 2>{}, integral_constant<int, 6>{});
+                    products(integral_constant<int, 4 * BLOCKS>{}, integral_constant<int, 2>{}, integral_constant<int, 0>{});
+                } else {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) scores(h), probabilities(h), gradients(h);
                 }
             };
             // Two tiles a turn, so that addresses in shared memory are constants: pays (12.3 to 10.4 ms for 32768 patches of 128) where a wave has its SIMD's registers to

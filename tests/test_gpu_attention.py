@@ -63,6 +63,32 @@ def test_widths(N, width):
     check(run(N, *t), R.Attention(*t))
 
 
+# keys in parts, put together by a second kernel; heads that share keys side by side: four, two and one at a time
+FEW = [(1, 1, 5000, 8, 8, 64), (2, 16, 1500, 8, 2, 64), (1, 33, 1100, 4, 1, 64), (1, 64, 700, 6, 1, 32), (1, 65, 600, 4, 1, 40), (3, 5, 513, 4, 1, 49), (1, 3, 2049, 12, 3, 128), (1, 32, 64, 4, 1, 64),
+       (1, 200, 512, 2, 2, 64)]
+
+
+@pytest.mark.parametrize("batch,queries,keys,heads,kv_heads,width", FEW)
+@pytest.mark.parametrize("kind", [None, "late", "scattered", "lengths"])
+def test_few_queries_over_many_keys(N, batch, queries, keys, heads, kv_heads, width, kind):
+    t = inputs(batch, queries, keys, heads, kv_heads, width, 15)
+    mask = masks(batch, keys, kind) if kind else None
+    r = R.Attention(*t, mask=mask)
+    check(run(N, *t, mask=mask), r)
+    with torch.no_grad():
+        o = N.attention(*(x.cuda() for x in t[:3]), mask=None if mask is None else mask.cuda())
+    r = R.Attention(*t, mask=mask, fine=False)
+    assert_close(o, r.o, r.o_off, "o")
+
+
+@pytest.mark.parametrize("batch,queries,keys,heads,kv_heads,width", FEW)
+def test_few_queries_with_a_bias(N, batch, queries, keys, heads, kv_heads, width):
+    t = inputs(batch, queries, keys, heads, kv_heads, width, 16)
+    _, buckets, many = places(queries, keys, "line")
+    table = rand((heads, many), 17, F32)
+    check(run(N, *t, table, None, buckets), R.Attention(*t, None, table, buckets))
+
+
 @pytest.mark.parametrize("scale", [1e-3, 1.0, 3.0])
 def test_scales(N, scale):
     """Probabilities from nearly even to nearly all on one key."""
