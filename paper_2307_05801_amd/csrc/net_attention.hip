@@ -199,38 +199,40 @@ template <int DEEP, bool DIRECT, bool BIAS, bool FINE> __global__ __launch_bound
     }
 }
 
-// A query of a head from its parts, a wave each.
+// A query of a head from its parts, a block each: every wave adds up a fourth of them.
 __global__ __launch_bounds__(BLOCK) void k_join(forward_args F)
 {
     const attention_args &A = F.a;
-    const int lane = threadIdx.x % WAVE;
-    const int64_t row = (F.first + blockIdx.x) * WAVES + threadIdx.x / WAVE;               // (item, head, query)
-    if (row >= (int64_t)A.batch * A.heads * A.queries) return;
-    const float *const stats = F.part_stats + row * F.parts * 2;
+    __shared__ float values[WAVES][LEAP_ATTENTION_WIDEST], sums[WAVES];
+    const int lane = threadIdx.x % WAVE, wave = threadIdx.x / WAVE;
+    const int64_t row = F.first + blockIdx.x;                                              // (item, head, query)
+    const float *const stats = F.part_stats + row * F.parts * 2, *const from = F.part_sums + row * F.parts * A.width;
     float m = -INFINITY;
     for (int p = lane; p < F.parts; p += WAVE) m = fmaxf(m, stats[p * 2]);
 #pragma unroll
     for (int d = 1; d < WAVE; d *= 2) m = fmaxf(m, __shfl_xor(m, d));
     const float base = m == -INFINITY ? 0.0f : m;
-    const float *const from = F.part_sums + row * F.parts * A.width;
     float sum = 0.0f, o[2] = {};
-#pragma unroll 4
-    for (int p = 0; p < F.parts; ++p) {
+#pragma unroll 8
+    for (int p = wave; p < F.parts; p += WAVES) {
         const float by = __builtin_amdgcn_exp2f(stats[p * 2] - base);
         sum += stats[p * 2 + 1] * by;
 #pragma unroll
         for (int i = 0; i < 2; ++i)
             if (lane + i * WAVE < A.width) o[i] += from[(int64_t)p * A.width + lane + i * WAVE] * by;
     }
+    values[wave][lane] = o[0], values[wave][lane + WAVE] = o[1];
+    if (lane == 0) sums[wave] = sum;
+    __syncthreads();
+    sum = sums[0] + sums[1] + sums[2] + sums[3];
     const float by = sum != 0.0f ? 1.0f / sum : 0.0f;
     const int64_t query = row % A.queries, head = row / A.queries % A.heads, item = row / A.queries / A.heads, to = (item * A.queries + query) * A.heads + head;
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-        if (lane + i * WAVE < A.width) {
-            F.o[to * A.width + lane + i * WAVE] = element<LEAP_BF16>::from_float(o[i] * by);
-            if (F.rest) F.rest[to * A.width + lane + i * WAVE] = rest_of(o[i] * by);
-        }
-    if (F.stats && lane == 0) F.stats[row * 2] = sum != 0.0f ? base : 0.0f, F.stats[row * 2 + 1] = sum != 0.0f ? __builtin_amdgcn_logf(sum) : INFINITY;
+    if (const int at = threadIdx.x; at < A.width) {
+        const float v = (values[0][at] + values[1][at] + values[2][at] + values[3][at]) * by;
+        F.o[to * A.width + at] = element<LEAP_BF16>::from_float(v);
+        if (F.rest) F.rest[to * A.width + at] = rest_of(v);
+    }
+    if (F.stats && threadIdx.x == 0) F.stats[row * 2] = sum != 0.0f ? base : 0.0f, F.stats[row * 2 + 1] = sum != 0.0f ? __builtin_amdgcn_logf(sum) : INFINITY;
 }
 
 // A head's number for every difference of positions; and what positions each tile of queries and of keys has.
@@ -346,10 +348,10 @@ shares shares_of(const leap_attention_desc *d)
     const int64_t group = d->heads / d->kv_heads, tiles = (d->keys + TILE - 1) / TILE;
     S.abreast = d->d_table ? 1 : d->queries <= 32 && group % 4 == 0 ? 4 : d->queries <= 64 && group % 2 == 0 ? 2 : 1;
     S.units = d->batch * (d->heads / S.abreast) * ((d->queries + COLS / S.abreast - 1) / (COLS / S.abreast));
-    // Half the chip without work and at least eight tiles to a block: parts of four tiles and more, as many as fill it four times over
+    // Half the chip without work and at least eight tiles to a block: parts of four tiles and more, as many as fill it
     int64_t parts = 1;
     if (S.units > 0 && S.units <= 128 && tiles >= 8) {
-        parts = 1024 / S.units;
+        parts = 512 / S.units;
         parts = parts < tiles / 4 ? parts : tiles / 4;
     }
     const int64_t each = tiles ? (tiles + parts - 1) / parts : 1;
@@ -396,7 +398,7 @@ extern "C" int leap_attention(const leap_attention_desc *desc, const void *d_q, 
         }, direct, desc->d_table != nullptr, d_rest != nullptr);
     });
     if (rc != LEAP_OK || S.parts == 1) return rc;
-    return over_blocks((rows + WAVES - 1) / WAVES, [&](int64_t first, unsigned n) {
+    return over_blocks(rows, [&](int64_t first, unsigned n) {
         F.first = first;
         hipLaunchKernelGGL(k_join, dim3(n), dim3(BLOCK), 0, st, F);
     });
