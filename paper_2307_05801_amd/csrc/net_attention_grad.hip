@@ -54,17 +54,18 @@ __global__ __launch_bounds__(BLOCK) void k_delta(grad_args G)
     if (lane == 0) G.delta[(item * A.heads + head) * (int64_t)A.queries + query] = sum;
 }
 
-// Numbers of a line in shared memory (see net_attention.hip).
-constexpr int window_of_tile(int deep) { return deep > 64 ? 1024 : 2048; }
+// Numbers of a line in shared memory (see net_attention.hip): as many as leave a compute unit room for two blocks.
+constexpr int window_of_tile(int deep, int buckets) { return deep > 64 || buckets > 1024 ? 1024 : 2048; }
 
-// A table's gradient.  Adds of integers to shared memory take a wave 4 cycles, those of floats 192 (3 a lane), and integers' order does not matter.  So a tile's ds, as integers of
-// 2^-24 of the largest of them, are added to a number for every difference that its pairs have: keys rise, so a difference has at most one pair of each of the
-// block's 128 queries, and 128 times 2^24 fits 32 bits.  (The largest is 40 times the root of the mean square or so: the sums are as good as those of 32-bit floats.)
+// A table's gradient.  Adds of integers to shared memory take a wave 4 cycles, those of floats 192 (3 a lane), and integers' order does not matter.  So a tile's ds are added as
+// integers to two numbers for every difference that its pairs have: whole multiples of 2^-24 of the largest of them, and what is left in multiples of 2^-48.  (With the
+// first alone sums were 0.6e-5 to 6e-5 of the table's norm off, since a bucket that nearly all of a query's keys are in has a sum far smaller than its terms.)  Keys rise, so a
+// difference has at most one pair of each of the block's 128 queries, and 128 times 2^24 fits 32 bits.
 // In the next tile's time one wave adds the differences' sums, as floats, to their buckets, which the block keeps.
-// Where the differences are too far apart or keys do not rise, ds go to the buckets as two integers, the upper one of 2^-17 of the largest: 8192 of either fit.
+// Where the differences are too far apart or keys do not rise, ds go to the buckets as two integers, of 2^-17 and 2^-34 of the largest: 8192 of either fit.
 template <int BUCKETS, int WINDOW> struct table_sums {
     float bucket[BUCKETS];
-    int32_t difference[WINDOW];
+    int32_t upper[WINDOW], lower[WINDOW];
     uint16_t which[WINDOW];                                // the buckets of the window
     float peak[WAVES];
 };
@@ -85,18 +86,10 @@ __device__ inline float wave_max(float v)
     return column_max(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
 }
 
-// The largest whole number that is not above v: one instruction.
-__device__ inline int floor_of(float v)
-{
-    int i;
-    asm("v_cvt_flr_i32_f32 %0, %1" : "=v"(i) : "v"(v));
-    return i;
-}
-
 template <int DEEP, bool DIRECT, bool BIAS, int BUCKETS> __global__ __launch_bounds__(BLOCK, 2) void k_grad_query(grad_args G)
 {
     using tile = rows_tile<DEEP>;
-    constexpr int STEPS = DEEP / 16, BLOCKS = DEEP / 32, WINDOW = window_of_tile(DEEP);
+    constexpr int STEPS = DEEP / 16, BLOCKS = DEEP / 32, WINDOW = window_of_tile(DEEP, BUCKETS);
     const attention_args &A = G.a;
     __shared__ __attribute__((aligned(16))) uint8_t room[4 * tile::BYTES + (BIAS ? 2 * WINDOW * 4 : 0)];
     __shared__ __attribute__((aligned(16))) table_sums<BUCKETS, WINDOW> sums;
@@ -107,7 +100,7 @@ template <int DEEP, bool DIRECT, bool BIAS, int BUCKETS> __global__ __launch_bou
     const int64_t units = (int64_t)A.batch * tiles;
     if constexpr (BUCKETS != 0) {
         for (int b = threadIdx.x; b < BUCKETS; b += BLOCK) sums.bucket[b] = 0.0f;
-        for (int b = threadIdx.x; b < WINDOW; b += BLOCK) sums.difference[b] = 0;
+        for (int b = threadIdx.x; b < WINDOW; b += BLOCK) sums.upper[b] = sums.lower[b] = 0;
     }
 
     const int64_t block = unit_of(blockIdx.x, gridDim.x);
@@ -161,8 +154,8 @@ template <int DEEP, bool DIRECT, bool BIAS, int BUCKETS> __global__ __launch_bou
             if constexpr (BUCKETS != 0) {
                 if (pending && wave == duty)
                     for (int i = lane; i < before.count; i += WAVE) {
-                        const float s = (float)sums.difference[i] * unscale;
-                        sums.difference[i] = 0;
+                        const float s = ((float)sums.upper[i] + (float)sums.lower[i] * 0x1p-24f) * unscale;
+                        sums.upper[i] = sums.lower[i] = 0;
                         __hip_atomic_fetch_add(&sums.bucket[sums.which[i]], s, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
                     }
                 duty = (duty + 1) % WAVES;
@@ -241,14 +234,16 @@ template <int DEEP, bool DIRECT, bool BIAS, int BUCKETS> __global__ __launch_bou
                     fetch_window<2>(A.line_buckets, A.offsets, window, (lds_byte *)sums.which, wave, lane);
                     const float by = 0x1.fp23f / largest;
                     unscale = all * (1.0f / 0x1.fp23f);
-                    const int to_sums = address_of((lds_byte *)sums.difference) + 4 * (A.offsets / 2 - window.first - position);
+                    const int to_sums = address_of((lds_byte *)sums.upper) + 4 * (A.offsets / 2 - window.first - position);
 #pragma unroll
                     for (int h = 0; h < 2; ++h)
                         over_places<1, int>(places[turn] + h * 32, fours, to_sums, lane, [&](int r, auto sum_of) {
-                            __hip_atomic_fetch_add(sum_of, floor_of(__builtin_fmaf(x[h][r], by, 0.5f)), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+                            const float v = x[h][r] * by, whole = rintf(v);
+                            __hip_atomic_fetch_add(sum_of, (int)whole, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+                            __hip_atomic_fetch_add(sum_of + WINDOW, (int)((v - whole) * 0x1p24f), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
                         });
                 } else {
-                    constexpr int AT_ONCE = WINDOW / 2;
+                    constexpr int AT_ONCE = WINDOW;
                     const float by = 0x1.fp16f / largest;
                     unscale = all * (1.0f / 0x1.fp16f);
                     for (int first = 0; first < A.buckets; first += AT_ONCE) {
@@ -257,16 +252,16 @@ template <int DEEP, bool DIRECT, bool BIAS, int BUCKETS> __global__ __launch_bou
 #pragma unroll
                             for (int r = 0; r < 16; ++r) {
                                 const int b = A.line_buckets[line_at(A, places[turn][h * 32 + row_of(r) + lane / 32 * 4], position)] - first;
-                                const float v = x[h][r] * by, upper = rintf(v);
+                                const float v = x[h][r] * by, whole = rintf(v);
                                 if (b >= 0 && b < AT_ONCE) {
-                                    __hip_atomic_fetch_add(&sums.difference[b * 2], (int)upper, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
-                                    __hip_atomic_fetch_add(&sums.difference[b * 2 + 1], __float2int_rn((v - upper) * 0x1p17f), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+                                    __hip_atomic_fetch_add(&sums.upper[b], (int)whole, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+                                    __hip_atomic_fetch_add(&sums.lower[b], (int)((v - whole) * 0x1p17f), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
                                 }
                             }
                         shared_barrier();
                         for (int b = threadIdx.x; b < AT_ONCE && first + b < A.buckets; b += BLOCK) {
-                            sums.bucket[first + b] += ((float)sums.difference[b * 2] + (float)sums.difference[b * 2 + 1] * 0x1p-17f) * unscale;
-                            sums.difference[b * 2] = sums.difference[b * 2 + 1] = 0;
+                            sums.bucket[first + b] += ((float)sums.upper[b] + (float)sums.lower[b] * 0x1p-17f) * unscale;
+                            sums.upper[b] = sums.lower[b] = 0;
                         }
                         shared_barrier();
                     }
@@ -518,9 +513,9 @@ extern "C" int leap_attention_backward(const leap_attention_desc *desc, const vo
         if (d_grad_table) {
             const dim3 grid((unsigned)(desc->heads * G.parts));
             by_flags([&](auto direct, auto few) {
-                hipLaunchKernelGGL((k_grad_query<W, decltype(direct)::value, true, decltype(few)::value ? 512 : LEAP_ATTENTION_BUCKETS>), grid, dim3(BLOCK), 0, st, G);
+                hipLaunchKernelGGL((k_grad_query<W, decltype(direct)::value, true, decltype(few)::value ? 1024 : LEAP_ATTENTION_BUCKETS>), grid, dim3(BLOCK), 0, st, G);
                 return LEAP_OK;
-            }, keys_direct, desc->buckets <= 512);
+            }, keys_direct, desc->buckets <= 1024);
             if ((status = launched()) != LEAP_OK) return status;
             const dim3 across((unsigned)((desc->buckets + BLOCK - 1) / BLOCK), (unsigned)desc->heads);
             hipLaunchKernelGGL(k_join_table, across, dim3(BLOCK), 0, st, G.part, G.parts, (int)desc->buckets, d_grad_table);

@@ -2,11 +2,12 @@
 //
 // A thread has eight neighbouring values of an item at a time and steps from voxel to voxel such that they are always the same channels, whose
 // mean, weight, ... stay in its registers.  Where rows have no gaps and the channels are no multiple of 8, the values are cut in eights regardless of rows: after
-// `period` eights the channels begin anew, so that no length costs more than its values.
+// `positions` eights the channels begin anew, so that no length costs more than its values.
 //
 // Sums over a group are formed in three stages that depend on the sizes alone: a thread's values (means and squares about them, a piece of eight voxels exactly in two
 // passes over registers, pieces joined by their means), a block's threads, and in 64 bits the blocks of an item.  Memory bounds it all: x is read
-// twice forward, x and the gradient twice backward.
+// twice forward, x and the gradient twice backward.  So a few items (or one) at a time are read for their sums and, in the opposite order, again, before the next: the second time
+// part of them comes from the cache of 256 MB.
 #include "../../include/leap_networks.h"
 #include "act_common.h"
 
@@ -15,7 +16,8 @@ namespace {
 using namespace act;
 
 constexpr int BLOCK = 256;
-constexpr int PIECE = 8;                    // voxels a thread takes at once
+constexpr int PIECE = 8;                    // voxels a thread takes at once for their moments,
+template <int TYPE> constexpr int AT_ONCE = TYPE == LEAP_F32 ? 2 : 4;      // and x and a gradient (of 32 bytes or 16): as many as leave room for four blocks a compute unit
 
 // How an item's values are dealt out to threads.
 struct dealing {
@@ -34,15 +36,15 @@ struct array {
 // A thread's part in it.
 struct part {
     int position, turn, turns, count;       // which eight of a period, which of the block's periods at once; values there
-    int64_t from, to;                       // periods
+    int64_t from, to, whole;                // periods; up to which they are known to be complete
     int64_t item, strip;
 
-    __device__ inline part(const dealing &D)
+    __device__ inline part(const dealing &D, int64_t item0, bool backwards)
     {
-        int64_t block = blockIdx.x;
+        int64_t block = backwards ? gridDim.x - 1 - blockIdx.x : blockIdx.x;
         const int segment = (int)(block % D.segments);
         block /= D.segments;
-        strip = block % D.strips, item = block / D.strips;
+        strip = block % D.strips, item = item0 + block / D.strips;
         turns = D.positions < BLOCK ? BLOCK / D.positions : 1;
         position = D.segments > 1 ? segment * BLOCK + (int)threadIdx.x : (int)threadIdx.x % D.positions;
         turn = D.segments > 1 ? 0 : (int)threadIdx.x / D.positions;
@@ -50,10 +52,12 @@ struct part {
         count = !there ? 0 : D.rows > 1 || D.channels - position * CHUNK >= CHUNK ? CHUNK : D.channels - position * CHUNK;
         from = strip * D.length + turn, to = (strip + 1) * D.length < D.periods ? (strip + 1) * D.length : D.periods;
         if (!there) from = to;
+        whole = D.rows > 1 && to == D.periods ? to - 1 : to;
     }
     __device__ inline int channel(const dealing &D, int i) const { return D.rows > 1 ? (position * CHUNK + i) % D.channels : position * CHUNK + i; }
-    // Where its eight of a period begin in an item of rows `row` apart, and how many there are.
-    __device__ inline int64_t at(const dealing &D, int64_t period, int64_t row) const { return period * (D.rows > 1 ? (int64_t)D.positions * CHUNK : row) + position * CHUNK; }
+    // Values from one period to the next in an item of rows `row` apart; where its eight of a period begin, and how many there are.
+    __device__ inline int64_t step(const dealing &D, int64_t row) const { return D.rows > 1 ? (int64_t)D.positions * CHUNK : row; }
+    __device__ inline int64_t at(const dealing &D, int64_t period, int64_t row) const { return period * step(D, row) + position * CHUNK; }
     __device__ inline int there(const dealing &D, int64_t period) const
     {
         if (D.rows == 1) return count;
@@ -61,6 +65,31 @@ struct part {
         return left >= CHUNK ? CHUNK : left > 0 ? (int)left : 0;
     }
 };
+
+// Eight values as memory has them.
+template <int TYPE> struct eight_of {
+    using raw = typename element<TYPE>::raw;
+    raw r[CHUNK];
+    // FULL: all of them are there.
+    template <bool FULL> __device__ inline void load(const raw *p, int n)
+    {
+        if (FULL || n >= CHUNK) {
+            __builtin_memcpy(r, p, sizeof r);
+        } else {
+#pragma unroll
+            for (int i = 0; i < CHUNK; ++i) r[i] = i < n ? p[i] : raw(0);
+        }
+    }
+    __device__ inline float operator[](int i) const { return element<TYPE>::to_float(r[i]); }
+};
+
+// step(periods at once, the first of them, values there) for all of a thread's periods: AT_ONCE of them, and one at a time what is left.
+template <int AT_ONCE, class F> __device__ inline void over_periods(const dealing &D, const part &P, F &&f)
+{
+    int64_t p = P.from;
+    for (; p + (AT_ONCE - 1) * P.turns < P.whole; p += AT_ONCE * P.turns) f(std::integral_constant<int, AT_ONCE>{}, p, P.count);
+    for (; p < P.to; p += P.turns) f(std::integral_constant<int, 1>{}, p, P.there(D, p));
+}
 
 __device__ inline float value_at(const void *p, int type, int64_t i)
 {
@@ -73,12 +102,12 @@ struct group_args {
     const void *weight, *bias;
     int32_t weight_type;
     float eps;
-    int64_t items;
     float *stats;                           // [items][groups][2]
     const float *coefficients;              // [items][groups][2]
     float *parts;
     void *out;
-    int64_t first;
+    int64_t first, item0;
+    bool past;                              // outputs past the caches
 };
 
 struct moments {
@@ -95,18 +124,19 @@ struct moments {
 };
 
 // Each slot (eight * 8 + value) of a period: its moments over the block's voxels, to parts [items][strips][slots].
-template <int TYPE> __global__ __launch_bounds__(BLOCK) void k_group_moments(group_args A)
+template <int TYPE, bool FULL> __global__ __launch_bounds__(BLOCK, 4) void k_group_moments(group_args A)
 {
     const dealing &D = A.deal;
-    const part P(D);
-    const typename element<TYPE>::raw *const x = (const typename element<TYPE>::raw *)A.x.data + P.item * A.x.item;
+    const part P(D, A.item0, false);
+    using raw = typename element<TYPE>::raw;
+    const raw *const x = (const raw *)A.x.data + P.item * A.x.item + P.position * CHUNK;
+    const int64_t step = P.step(D, A.x.row);
     float n = 0.0f, mean[CHUNK] = {}, square[CHUNK] = {};
     int64_t p = P.from;
-    const int64_t last = D.rows > 1 && P.to == D.periods ? P.to - 1 : P.to;             // a period that may end early comes last, by itself
-    for (; p + (PIECE - 1) * P.turns < last; p += PIECE * P.turns) {
-        float v[PIECE][CHUNK];
+    for (; p + (PIECE - 1) * P.turns < P.whole; p += PIECE * P.turns) {
+        eight_of<TYPE> v[PIECE];
 #pragma unroll
-        for (int u = 0; u < PIECE; ++u) load8<TYPE>(x, P.at(D, p + u * P.turns, A.x.row), P.count, v[u]);
+        for (int u = 0; u < PIECE; ++u) v[u].template load<FULL>(x + (p + u * P.turns) * step, P.count);
         const float all = n + PIECE, share = PIECE / all, weight = n * share;
 #pragma unroll
         for (int i = 0; i < CHUNK; ++i) {
@@ -127,8 +157,8 @@ template <int TYPE> __global__ __launch_bounds__(BLOCK) void k_group_moments(gro
     for (int i = 0; i < CHUNK; ++i) all[i] = {n, mean[i], square[i]};
     for (; p < P.to; p += P.turns) {
         const int there = P.there(D, p);
-        float v[CHUNK];
-        load8<TYPE>(x, P.at(D, p, A.x.row), there, v);
+        eight_of<TYPE> v;
+        v.template load<false>(x + p * step, there);
 #pragma unroll
         for (int i = 0; i < CHUNK; ++i)
             if (i < there) all[i].join({1.0f, v[i], 0.0f});
@@ -154,11 +184,13 @@ template <int TYPE> __global__ __launch_bounds__(BLOCK) void k_group_moments(gro
     }
 }
 
+constexpr int WIDE = 1024;                 // threads of a block that joins parts
+
 __device__ inline double block_sum(double v, double *room)
 {
     room[threadIdx.x] = v;
     __syncthreads();
-    for (int half = BLOCK / 2; half > 0; half /= 2) {
+    for (int half = WIDE / 2; half > 0; half /= 2) {
         if ((int)threadIdx.x < half) room[threadIdx.x] += room[threadIdx.x + half];
         __syncthreads();
     }
@@ -168,48 +200,48 @@ __device__ inline double block_sum(double v, double *room)
 }
 
 // mean and rstd of a group, a block each.
-__global__ __launch_bounds__(BLOCK) void k_group_stats(group_args A)
+__global__ __launch_bounds__(WIDE) void k_group_stats(group_args A)
 {
     const dealing &D = A.deal;
-    __shared__ double room[BLOCK];
-    const int64_t unit = A.first + blockIdx.x, item = unit / D.groups, all = (int64_t)D.strips * D.rows * D.size;
-    const int group = (int)(unit % D.groups), each = D.rows * D.size;
-    const moments *const from = (const moments *)A.parts + item * D.strips * D.positions * CHUNK;
-    const auto entry = [&](int64_t e) {
-        const int r = (int)(e % each);
-        return from[e / each * D.positions * CHUNK + r / D.size * D.channels + group * D.size + r % D.size];
+    __shared__ double room[WIDE];
+    const int64_t unit = A.first + blockIdx.x, item = unit / D.groups, slots = (int64_t)D.positions * CHUNK;
+    const int group = (int)(unit % D.groups), each = D.rows * D.size;           // slots of a strip
+    const moments *const from = (const moments *)A.parts + item * D.strips * slots + group * D.size;
+    // f(moments) for a thread's share: some of a strip's slots of every few strips
+    const auto over = [&](auto &&f) {
+        const int wide = each < WIDE ? each : WIDE, high = WIDE / wide;
+        if ((int)threadIdx.x >= wide * high) return;
+        for (int e = threadIdx.x % wide; e < each; e += wide) {
+            const moments *const at = from + e / D.size * D.channels + e % D.size;
+#pragma unroll 4
+            for (int s = threadIdx.x / wide; s < D.strips; s += high) f(at[s * slots]);
+        }
     };
     double sum = 0.0, square = 0.0;
-    for (int64_t e = threadIdx.x; e < all; e += BLOCK) {
-        const moments m = entry(e);
-        sum += (double)m.n * m.mean;
-    }
+    over([&](const moments &m) { sum += (double)m.n * m.mean; });
     const double values = (double)D.voxels * D.size, mean = block_sum(sum, room) / values;
-    for (int64_t e = threadIdx.x; e < all; e += BLOCK) {
-        const moments m = entry(e);
-        square += m.square + m.n * (m.mean - mean) * (m.mean - mean);
-    }
+    over([&](const moments &m) { square += m.square + m.n * (m.mean - mean) * (m.mean - mean); });
     square = block_sum(square, room) / values;
     if (threadIdx.x == 0) A.stats[unit * 2] = (float)mean, A.stats[unit * 2 + 1] = (float)(1.0 / sqrt(square + A.eps));
 }
 
-// What a thread knows of its eight channels.
+// What a thread knows of its eight channels: u = (x - mean) by + bias, by = rstd weight.
 struct known {
-    float mean[CHUNK], rstd[CHUNK], weight[CHUNK], bias[CHUNK];
+    float mean[CHUNK], by[CHUNK], bias[CHUNK];
     __device__ inline known(const group_args &A, const part &P)
     {
 #pragma unroll
         for (int i = 0; i < CHUNK; ++i) {
             const bool there = i < P.count;
             const int c = there ? P.channel(A.deal, i) : 0;
-            const int64_t g = (P.item * A.deal.groups + c / A.deal.size) * 2;
-            mean[i] = there ? A.stats[g] : 0.0f, rstd[i] = there ? A.stats[g + 1] : 0.0f;
-            weight[i] = !there ? 0.0f : A.weight ? value_at(A.weight, A.weight_type, c) : 1.0f;
+            mean[i] = there ? A.stats[group_of(A, P, i) * 2] : 0.0f;
+            by[i] = !there ? 0.0f : A.stats[group_of(A, P, i) * 2 + 1] * (A.weight ? value_at(A.weight, A.weight_type, c) : 1.0f);
             bias[i] = there && A.bias ? value_at(A.bias, A.weight_type, c) : 0.0f;
         }
     }
+    static __device__ inline int64_t group_of(const group_args &A, const part &P, int i) { return P.item * A.deal.groups + (i < P.count ? P.channel(A.deal, i) : 0) / A.deal.size; }
     // the activation's argument, in both passes from the same steps
-    __device__ inline float argument(float v, int i) const { return __builtin_fmaf(v - mean[i], rstd[i] * weight[i], bias[i]); }
+    __device__ inline float argument(float v, int i) const { return __builtin_fmaf(v - mean[i], by[i], bias[i]); }
 };
 
 template <int ACTIVATION> __device__ inline float activated(float u) { return ACTIVATION == LEAP_SILU ? u * sigmoid(u) : ACTIVATION == LEAP_RELU ? (u < 0.0f ? 0.0f : u) : u; }
@@ -222,78 +254,60 @@ template <int ACTIVATION> __device__ inline float slope(float u)
     return ACTIVATION == LEAP_RELU && !(u > 0.0f) ? 0.0f : 1.0f;
 }
 
-// f(period, values there) for all of a thread's periods, AT_ONCE of them side by side.
-template <int AT_ONCE, class L, class F> __device__ inline void over_periods(const dealing &D, const part &P, L &&load, F &&use)
-{
-    int64_t p = P.from;
-    for (; p + (AT_ONCE - 1) * P.turns < P.to; p += AT_ONCE * P.turns) {
-#pragma unroll
-        for (int u = 0; u < AT_ONCE; ++u) load(u, p + u * P.turns, P.there(D, p + u * P.turns));
-#pragma unroll
-        for (int u = 0; u < AT_ONCE; ++u) use(u, p + u * P.turns, P.there(D, p + u * P.turns));
-    }
-    for (; p < P.to; p += P.turns) load(0, p, P.there(D, p)), use(0, p, P.there(D, p));
-}
-
-template <int TYPE, int ACTIVATION> __global__ __launch_bounds__(BLOCK) void k_group_apply(group_args A)
+template <int TYPE, bool FULL, int ACTIVATION> __global__ __launch_bounds__(BLOCK, 4) void k_group_apply(group_args A)
 {
     const dealing &D = A.deal;
-    const part P(D);
+    const part P(D, A.item0, true);
     using raw = typename element<TYPE>::raw;
-    const raw *const x = (const raw *)A.x.data + P.item * A.x.item;
-    raw *const y = (raw *)A.out + P.item * D.voxels * D.channels;
+    const raw *const x = (const raw *)A.x.data + P.item * A.x.item + P.position * CHUNK;
+    raw *const y = (raw *)A.out + P.item * D.voxels * D.channels + P.position * CHUNK;
+    const int64_t step = P.step(D, A.x.row), out = P.step(D, D.channels);
     const known K(A, P);
-    constexpr int AT_ONCE = 4;
-    float v[AT_ONCE][CHUNK];
-    over_periods<AT_ONCE>(D, P, [&](int u, int64_t p, int n) { load8<TYPE>(x, P.at(D, p, A.x.row), n, v[u]); },
-                          [&](int u, int64_t p, int n) {
+    over_periods<AT_ONCE<TYPE> * 2>(D, P, [&](auto at_once, int64_t p, int n) {
+        constexpr int N = decltype(at_once)::value;
+        eight_of<TYPE> v[N];
 #pragma unroll
-                              for (int i = 0; i < CHUNK; ++i) v[u][i] = activated<ACTIVATION>(K.argument(v[u][i], i));
-                              store8<TYPE>(y, P.at(D, p, D.channels), n, v[u]);
-                          });
+        for (int u = 0; u < N; ++u) v[u].template load<FULL && N != 1>(x + (p + u * P.turns) * step, n);
+#pragma unroll
+        for (int u = 0; u < N; ++u) {
+            float o[CHUNK];
+#pragma unroll
+            for (int i = 0; i < CHUNK; ++i) o[i] = activated<ACTIVATION>(K.argument(v[u][i], i));
+            store8<TYPE>(y, (p + u * P.turns) * out, FULL && N != 1 ? CHUNK : n, o, A.past);
+        }
+    });
 }
 
 // Each slot's sums of du and of du h over the block's voxels, to parts [items][strips][slots][2].
-template <int TYPE, int ACTIVATION> __global__ __launch_bounds__(BLOCK) void k_group_sums(group_args A)
+template <int TYPE, bool FULL, int ACTIVATION> __global__ __launch_bounds__(BLOCK, 4) void k_group_sums(group_args A)
 {
     const dealing &D = A.deal;
-    const part P(D);
+    const part P(D, A.item0, false);
     using raw = typename element<TYPE>::raw;
-    const raw *const x = (const raw *)A.x.data + P.item * A.x.item, *const grad = (const raw *)A.grad.data + P.item * A.grad.item;
+    const raw *const x = (const raw *)A.x.data + P.item * A.x.item + P.position * CHUNK, *const grad = (const raw *)A.grad.data + P.item * A.grad.item + P.position * CHUNK;
+    const int64_t step = P.step(D, A.x.row), grad_step = P.step(D, A.grad.row);
     const known K(A, P);
-    constexpr int AT_ONCE = 4;
-    float v[AT_ONCE][CHUNK], g[AT_ONCE][CHUNK], one[CHUNK] = {}, two[CHUNK] = {};
-    const auto load = [&](int u, int64_t p, int n) {
-        load8<TYPE>(x, P.at(D, p, A.x.row), n, v[u]);
-        load8<TYPE>(grad, P.at(D, p, A.grad.row), n, g[u]);              // zeros beyond the end
-    };
-    const auto use = [&](int u) {
+    float one[CHUNK] = {}, two[CHUNK] = {};                   // two: of du (x - mean), rstd comes at the end
+    over_periods<TYPE == LEAP_F32 && ACTIVATION == LEAP_SILU ? 2 : 4>(D, P, [&](auto at_once, int64_t p, int n) {
+        constexpr int N = decltype(at_once)::value;
+        eight_of<TYPE> v[N], g[N];
 #pragma unroll
-        for (int i = 0; i < CHUNK; ++i) {
-            g[u][i] *= slope<ACTIVATION>(K.argument(v[u][i], i));
-            v[u][i] = (v[u][i] - K.mean[i]) * K.rstd[i] * g[u][i];
+        for (int u = 0; u < N; ++u) {
+            v[u].template load<FULL && N != 1>(x + (p + u * P.turns) * step, n);
+            g[u].template load<FULL && N != 1>(grad + (p + u * P.turns) * grad_step, n);
         }
-    };
-    int64_t p = P.from;
-    for (; p + (AT_ONCE - 1) * P.turns < P.to; p += AT_ONCE * P.turns) {
 #pragma unroll
-        for (int u = 0; u < AT_ONCE; ++u) load(u, p + u * P.turns, P.there(D, p + u * P.turns));
+        for (int u = 0; u < N; ++u)
 #pragma unroll
-        for (int u = 0; u < AT_ONCE; ++u) use(u);
+            for (int i = 0; i < CHUNK; ++i) {
+                const float du = g[u][i] * slope<ACTIVATION>(K.argument(v[u][i], i));
+                if (N == 1 && i >= n) continue;
+                one[i] += du;                                  // (a thread has a few hundred voxels at most of the largest arrays)
+                two[i] = __builtin_fmaf(du, v[u][i] - K.mean[i], two[i]);
+            }
+    });
 #pragma unroll
-        for (int i = 0; i < CHUNK; ++i) {
-            one[i] += (g[0][i] + g[1][i]) + (g[2][i] + g[3][i]);
-            two[i] += (v[0][i] + v[1][i]) + (v[2][i] + v[3][i]);
-        }
-    }
-    for (; p < P.to; p += P.turns) {
-        const int n = P.there(D, p);
-        load(0, p, n);
-        use(0);
-#pragma unroll
-        for (int i = 0; i < CHUNK; ++i)
-            if (i < n) one[i] += g[0][i], two[i] += v[0][i];
-    }
+    for (int i = 0; i < CHUNK; ++i) two[i] *= P.count ? A.stats[known::group_of(A, P, i) * 2 + 1] : 0.0f;
     __shared__ float2 room[CHUNK][BLOCK];
     int half = 1;
     while (half < P.turns) half *= 2;
@@ -318,43 +332,50 @@ template <int TYPE, int ACTIVATION> __global__ __launch_bounds__(BLOCK) void k_g
 }
 
 // A group, a block each: its channels' sums over the item, to channel_sums [items][channels][2], and the means over the group of du weight and du weight h.
-__global__ __launch_bounds__(BLOCK) void k_group_coefficients(group_args A, double *channel_sums, float *coefficients)
+__global__ __launch_bounds__(WIDE) void k_group_coefficients(group_args A, double *channel_sums, float *coefficients)
 {
     const dealing &D = A.deal;
-    __shared__ double room[2][BLOCK];
-    const int64_t unit = A.first + blockIdx.x, item = unit / D.groups;
+    __shared__ double room[2][WIDE];
+    const int64_t unit = A.first + blockIdx.x, item = unit / D.groups, slots = (int64_t)D.positions * CHUNK;
     const int group = (int)(unit % D.groups);
-    const float2 *const from = (const float2 *)A.parts + item * D.strips * D.positions * CHUNK;
-    const int wide = D.size < BLOCK ? D.size : BLOCK, high = BLOCK / wide, col = threadIdx.x % wide, row = threadIdx.x / wide;
-    const int64_t entries = (int64_t)D.strips * D.rows;
+    const float2 *const from = (const float2 *)A.parts + item * D.strips * slots;
+    const int wide = D.size < WIDE ? D.size : WIDE, high = WIDE / wide, col = threadIdx.x % wide, row = threadIdx.x / wide;
     double one = 0.0, two = 0.0;
     for (int c0 = 0; c0 < D.size; c0 += wide) {
         const int c = c0 + col, channel = group * D.size + c;
         double a = 0.0, b = 0.0;
         if (c < D.size && row < high)
-            for (int64_t e = row; e < entries; e += high) {
-                const float2 s = from[e / D.rows * D.positions * CHUNK + e % D.rows * D.channels + channel];
-                a += s.x, b += s.y;
-            }
+            for (int r = 0; r < D.rows; ++r)
+#pragma unroll 4
+                for (int s = row; s < D.strips; s += high) {
+                    const float2 v = from[s * slots + r * D.channels + channel];
+                    a += v.x, b += v.y;
+                }
         __syncthreads();
         room[0][threadIdx.x] = a, room[1][threadIdx.x] = b;
         __syncthreads();
+        int top = 1;                           // rows of threads, two by two
+        while (top < high) top *= 2;
+        for (int half = top / 2; half > 0; half /= 2) {
+            if (row < half && row + half < high) {
+                room[0][threadIdx.x] += room[0][threadIdx.x + half * wide];
+                room[1][threadIdx.x] += room[1][threadIdx.x + half * wide];
+            }
+            __syncthreads();
+        }
         if (row == 0 && c < D.size) {
-            for (int r = 1; r < high; ++r) a += room[0][r * wide + col], b += room[1][r * wide + col];
+            a = room[0][threadIdx.x], b = room[1][threadIdx.x];
             double *const to = channel_sums + (item * D.channels + channel) * 2;
             to[0] = a, to[1] = b;
             const double w = A.weight ? value_at(A.weight, A.weight_type, channel) : 1.0f;
             one += w * a, two += w * b;
         }
     }
+    const double m = (double)D.voxels * D.size;
     __syncthreads();
-    room[0][threadIdx.x] = row == 0 ? one : 0.0, room[1][threadIdx.x] = row == 0 ? two : 0.0;
-    __syncthreads();
-    for (int half = BLOCK / 2; half > 0; half /= 2) {
-        if ((int)threadIdx.x < half) room[0][threadIdx.x] += room[0][threadIdx.x + half], room[1][threadIdx.x] += room[1][threadIdx.x + half];
-        __syncthreads();
-    }
-    if (threadIdx.x < 2) coefficients[unit * 2 + threadIdx.x] = (float)(room[threadIdx.x][0] / ((double)D.voxels * D.size));
+    one = block_sum(row == 0 ? one : 0.0, room[0]);
+    two = block_sum(row == 0 ? two : 0.0, room[0]);
+    if (threadIdx.x == 0) coefficients[unit * 2] = (float)(one / m), coefficients[unit * 2 + 1] = (float)(two / m);
 }
 
 // grad_weight, grad_bias: the channels' sums over the items.
@@ -370,35 +391,40 @@ template <int WTYPE> __global__ __launch_bounds__(BLOCK) void k_group_weights(co
     if (grad_weight) ((raw *)grad_weight)[c] = element<WTYPE>::from_float((float)two);
 }
 
-template <int TYPE, int ACTIVATION> __global__ __launch_bounds__(BLOCK) void k_group_grad(group_args A)
+template <int TYPE, bool FULL, int ACTIVATION> __global__ __launch_bounds__(BLOCK, 4) void k_group_grad(group_args A)
 {
     const dealing &D = A.deal;
-    const part P(D);
+    const part P(D, A.item0, true);
     using raw = typename element<TYPE>::raw;
-    const raw *const x = (const raw *)A.x.data + P.item * A.x.item, *const grad = (const raw *)A.grad.data + P.item * A.grad.item;
-    raw *const out = (raw *)A.out + P.item * D.voxels * D.channels;
+    const raw *const x = (const raw *)A.x.data + P.item * A.x.item + P.position * CHUNK, *const grad = (const raw *)A.grad.data + P.item * A.grad.item + P.position * CHUNK;
+    raw *const to = (raw *)A.out + P.item * D.voxels * D.channels + P.position * CHUNK;
+    const int64_t step = P.step(D, A.x.row), grad_step = P.step(D, A.grad.row), out = P.step(D, D.channels);
     const known K(A, P);
+    // rstd (du weight - first - h second) = du by - one - (x - mean) two
     float one[CHUNK], two[CHUNK];
 #pragma unroll
     for (int i = 0; i < CHUNK; ++i) {
-        const int64_t g = (P.item * D.groups + (i < P.count ? P.channel(D, i) : 0) / D.size) * 2;
-        one[i] = A.coefficients[g], two[i] = A.coefficients[g + 1];
+        const int64_t g = P.count ? known::group_of(A, P, i) : 0;
+        const float rstd = A.stats[g * 2 + 1];
+        one[i] = A.coefficients[g * 2] * rstd, two[i] = A.coefficients[g * 2 + 1] * rstd * rstd;
     }
-    constexpr int AT_ONCE = 4;
-    float v[AT_ONCE][CHUNK], g[AT_ONCE][CHUNK];
-    over_periods<AT_ONCE>(D, P,
-                          [&](int u, int64_t p, int n) {
-                              load8<TYPE>(x, P.at(D, p, A.x.row), n, v[u]);
-                              load8<TYPE>(grad, P.at(D, p, A.grad.row), n, g[u]);
-                          },
-                          [&](int u, int64_t p, int n) {
+    over_periods<AT_ONCE<TYPE>>(D, P, [&](auto at_once, int64_t p, int n) {
+        constexpr int N = decltype(at_once)::value;
+        eight_of<TYPE> v[N], g[N];
 #pragma unroll
-                              for (int i = 0; i < CHUNK; ++i) {
-                                  const float du = g[u][i] * slope<ACTIVATION>(K.argument(v[u][i], i)) * K.weight[i];
-                                  v[u][i] = K.rstd[i] * (du - one[i] - (v[u][i] - K.mean[i]) * K.rstd[i] * two[i]);
-                              }
-                              store8<TYPE>(out, P.at(D, p, D.channels), n, v[u]);
-                          });
+        for (int u = 0; u < N; ++u) {
+            v[u].template load<FULL && N != 1>(x + (p + u * P.turns) * step, n);
+            g[u].template load<FULL && N != 1>(grad + (p + u * P.turns) * grad_step, n);
+        }
+#pragma unroll
+        for (int u = 0; u < N; ++u) {
+            float o[CHUNK];
+#pragma unroll
+            for (int i = 0; i < CHUNK; ++i)
+                o[i] = g[u][i] * slope<ACTIVATION>(K.argument(v[u][i], i)) * K.by[i] - one[i] - (v[u][i] - K.mean[i]) * two[i];
+            store8<TYPE>(to, (p + u * P.turns) * out, FULL && N != 1 ? CHUNK : n, o, A.past);
+        }
+    });
 }
 
 // ---- host side ----
@@ -418,7 +444,7 @@ dealing dealing_of(int64_t items, int64_t voxels, int64_t channels, int64_t grou
     D.segments = (D.positions + BLOCK - 1) / BLOCK;
     const int64_t turns = D.positions < BLOCK ? BLOCK / D.positions : 1;
     // enough blocks for the chip, and no fewer than a few pieces of each thread
-    int64_t strips = 2048 / (items * D.segments > 0 ? items * D.segments : 1);
+    int64_t strips = 1024 / (items * D.segments > 0 ? items * D.segments : 1);
     const int64_t most = D.periods / (turns * 2 * PIECE);
     strips = strips < most ? strips : most;
     strips = strips < 1 ? 1 : strips;
@@ -445,16 +471,34 @@ const char *bad_distances(int64_t item, int64_t row, int64_t items, int64_t voxe
     return bad_stride(row, voxels, channels);
 }
 
+// Items that are read for their sums and again before the next: `values` of x, or one.
+int64_t items_at_once(int64_t items, int64_t voxels, int64_t channels, int64_t values)
+{
+    int64_t n = values / (voxels * channels > 0 ? voxels * channels : 1);
+    n = n < 1 ? 1 : n < (int64_t)1 << 20 ? n : (int64_t)1 << 20;
+    return n < items ? n : items;
+}
+constexpr int64_t AT_ONCE_FORWARD = (int64_t)1 << 26, AT_ONCE_BACKWARD = (int64_t)1 << 25;
+
 // Bytes of the parts, for the dealing that has more of them.
-int64_t parts_bytes(int64_t items, int64_t voxels, int64_t channels, int64_t groups, int64_t each)
+int64_t parts_bytes(int64_t items, int64_t at_once, int64_t voxels, int64_t channels, int64_t groups, int64_t each)
 {
     int64_t most = 0;
     for (const bool flat : {false, true}) {
-        const dealing D = dealing_of(items, voxels, channels, groups, flat);
+        const dealing D = dealing_of(at_once, voxels, channels, groups, flat);
         const int64_t n = items * D.strips * D.positions * CHUNK * each;
         most = n > most ? n : most;
     }
     return (most + 15) / 16 * 16;
+}
+
+// Outputs of more values than this go past the caches, which x is to stay in.
+constexpr int64_t PAST_VALUES = (int64_t)1 << 25;
+
+// f(whether all threads have eight values but at an item's end)
+template <class F> int by_full(const dealing &D, F &&f)
+{
+    return D.rows > 1 || D.channels % CHUNK == 0 ? f(std::true_type{}) : f(std::false_type{});
 }
 
 template <class F> int by_activation(int32_t activation, F &&f)
@@ -476,7 +520,7 @@ const char *bad_kinds(int32_t type, int32_t weight_type, int32_t activation)
 extern "C" int64_t leap_group_norm_work(int64_t items, int64_t voxels, int64_t channels, int64_t groups)
 {
     if (bad_group(items, voxels, channels, groups) || !items || !voxels) return 0;
-    return parts_bytes(items, voxels, channels, groups, sizeof(moments)) + (items * groups * 8 + 15) / 16 * 16;
+    return parts_bytes(items, items_at_once(items, voxels, channels, AT_ONCE_FORWARD), voxels, channels, groups, sizeof(moments)) + (items * groups * 8 + 15) / 16 * 16;
 }
 
 extern "C" int leap_group_norm(const void *d_x, int32_t type, int64_t x_item, int64_t x_row, const void *d_weight, const void *d_bias, int32_t weight_type, int64_t items,
@@ -491,28 +535,34 @@ extern "C" int leap_group_norm(const void *d_x, int32_t type, int64_t x_item, in
     if (!d_x || !d_y) return refuse("null data pointer");
     if (unaligned(d_work)) return refuse(NO_WORK);
     const hipStream_t st = stream_of(hip_stream);
-    const bool flat = x_row == channels || voxels == 1;
+    const int64_t at_once = items_at_once(items, voxels, channels, AT_ONCE_FORWARD);
     group_args A{};
-    A.deal = dealing_of(items, voxels, channels, groups, flat);
+    A.deal = dealing_of(at_once, voxels, channels, groups, x_row == channels || voxels == 1);
     A.x = {d_x, x_item, x_row};
-    A.weight = d_weight, A.bias = d_bias, A.weight_type = weight_type, A.eps = eps, A.items = items;
-    A.parts = (float *)d_work, A.out = d_y;
-    A.stats = d_stats ? d_stats : (float *)((char *)d_work + parts_bytes(items, voxels, channels, groups, sizeof(moments)));
-    const int64_t blocks = items * A.deal.strips * A.deal.segments;
-    if (blocks >= (int64_t)1 << 24) return refuse("more than 2^24 blocks of items");
+    A.weight = d_weight, A.bias = d_bias, A.weight_type = weight_type, A.eps = eps;
+    A.parts = (float *)d_work, A.out = d_y, A.past = voxels * channels * items > PAST_VALUES;
+    A.stats = d_stats ? d_stats : (float *)((char *)d_work + parts_bytes(items, at_once, voxels, channels, groups, sizeof(moments)));
+    const int64_t each = (int64_t)A.deal.strips * A.deal.segments;
+    if (at_once * each >= (int64_t)1 << 24) return refuse("more than 2^24 blocks of items");
     return by_type(type, [&](auto t) {
-        constexpr int T = decltype(t)::value;
-        hipLaunchKernelGGL((k_group_moments<T>), dim3((unsigned)blocks), dim3(BLOCK), 0, st, A);
-        int rc = launched();
-        if (rc == LEAP_OK)
-            rc = over_blocks(items * groups, [&](int64_t first, unsigned n) {
-                A.first = first;
-                hipLaunchKernelGGL(k_group_stats, dim3(n), dim3(BLOCK), 0, st, A);
-            });
-        if (rc != LEAP_OK) return rc;
         return by_activation(activation, [&](auto a) {
-            hipLaunchKernelGGL((k_group_apply<T, decltype(a)::value>), dim3((unsigned)blocks), dim3(BLOCK), 0, st, A);
-            return launched();
+            return by_full(A.deal, [&](auto full) -> int {
+                constexpr int T = decltype(t)::value;
+                for (A.item0 = 0; A.item0 < items; A.item0 += at_once) {
+                    const int64_t now = items - A.item0 < at_once ? items - A.item0 : at_once;
+                    hipLaunchKernelGGL((k_group_moments<T, decltype(full)::value>), dim3((unsigned)(now * each)), dim3(BLOCK), 0, st, A);
+                    int rc = launched();
+                    if (rc == LEAP_OK)
+                        rc = over_blocks(now * groups, [&](int64_t first, unsigned n) {
+                            A.first = A.item0 * groups + first;
+                            hipLaunchKernelGGL(k_group_stats, dim3(n), dim3(WIDE), 0, st, A);
+                        });
+                    if (rc != LEAP_OK) return rc;
+                    hipLaunchKernelGGL((k_group_apply<T, decltype(full)::value, decltype(a)::value>), dim3((unsigned)(now * each)), dim3(BLOCK), 0, st, A);
+                    if ((rc = launched()) != LEAP_OK) return rc;
+                }
+                return LEAP_OK;
+            });
         });
     });
 }
@@ -521,7 +571,7 @@ extern "C" int64_t leap_group_norm_backward_work(int64_t items, int64_t voxels, 
 {
     if (bad_group(items, voxels, channels, groups)) return 0;
     if (!items || !voxels) return 16;
-    return parts_bytes(items, voxels, channels, groups, 8) + items * channels * 16 + (items * groups * 8 + 15) / 16 * 16;
+    return parts_bytes(items, items_at_once(items, voxels, channels, AT_ONCE_BACKWARD), voxels, channels, groups, 8) + items * channels * 16 + (items * groups * 8 + 15) / 16 * 16;
 }
 
 extern "C" int leap_group_norm_backward(const void *d_grad, int64_t grad_item, int64_t grad_row, const void *d_x, int32_t type, int64_t x_item, int64_t x_row,
@@ -537,32 +587,40 @@ extern "C" int leap_group_norm_backward(const void *d_grad, int64_t grad_item, i
     if (some && (!d_grad || !d_x || !d_stats)) return refuse("null data pointer");
     if (unaligned(d_work)) return refuse(NO_WORK);
     const hipStream_t st = stream_of(hip_stream);
+    const int64_t at_once = items_at_once(items, voxels, channels, AT_ONCE_BACKWARD);
     group_args A{};
-    A.deal = dealing_of(items, voxels, channels, groups, (x_row == channels && grad_row == channels) || voxels == 1);
+    A.deal = dealing_of(at_once, voxels, channels, groups, (x_row == channels && grad_row == channels) || voxels == 1);
     A.x = {d_x, x_item, x_row}, A.grad = {d_grad, grad_item, grad_row};
-    A.weight = d_weight, A.bias = d_bias, A.weight_type = weight_type, A.items = items;
-    A.stats = (float *)d_stats, A.parts = (float *)d_work, A.out = d_grad_x;
-    double *const channel_sums = (double *)((char *)d_work + parts_bytes(items, voxels, channels, groups, 8));
+    A.weight = d_weight, A.bias = d_bias, A.weight_type = weight_type;
+    A.stats = (float *)d_stats, A.parts = (float *)d_work, A.out = d_grad_x, A.past = voxels * channels * items > PAST_VALUES;
+    double *const channel_sums = (double *)((char *)d_work + parts_bytes(items, at_once, voxels, channels, groups, 8));
     float *const coefficients = (float *)(channel_sums + items * channels * 2);
     A.coefficients = coefficients;
-    const int64_t blocks = items * A.deal.strips * A.deal.segments;
-    if (blocks >= (int64_t)1 << 24) return refuse("more than 2^24 blocks of items");
+    const int64_t each = (int64_t)A.deal.strips * A.deal.segments;
+    if (at_once * each >= (int64_t)1 << 24) return refuse("more than 2^24 blocks of items");
     int rc = LEAP_OK;
     if (some)
         rc = by_type(type, [&](auto t) {
-            constexpr int T = decltype(t)::value;
             return by_activation(activation, [&](auto a) {
-                constexpr int ACT = decltype(a)::value;
-                hipLaunchKernelGGL((k_group_sums<T, ACT>), dim3((unsigned)blocks), dim3(BLOCK), 0, st, A);
-                int status = launched();
-                if (status == LEAP_OK)
-                    status = over_blocks(items * groups, [&](int64_t first, unsigned n) {
-                        A.first = first;
-                        hipLaunchKernelGGL(k_group_coefficients, dim3(n), dim3(BLOCK), 0, st, A, channel_sums, coefficients);
-                    });
-                if (status != LEAP_OK || !d_grad_x) return status;
-                hipLaunchKernelGGL((k_group_grad<T, ACT>), dim3((unsigned)blocks), dim3(BLOCK), 0, st, A);
-                return launched();
+                return by_full(A.deal, [&](auto full) -> int {
+                    constexpr int T = decltype(t)::value, ACT = decltype(a)::value;
+                    constexpr bool FULL = decltype(full)::value;
+                    for (A.item0 = 0; A.item0 < items; A.item0 += at_once) {
+                        const int64_t now = items - A.item0 < at_once ? items - A.item0 : at_once;
+                        hipLaunchKernelGGL((k_group_sums<T, FULL, ACT>), dim3((unsigned)(now * each)), dim3(BLOCK), 0, st, A);
+                        int status = launched();
+                        if (status == LEAP_OK)
+                            status = over_blocks(now * groups, [&](int64_t first, unsigned n) {
+                                A.first = A.item0 * groups + first;
+                                hipLaunchKernelGGL(k_group_coefficients, dim3(n), dim3(WIDE), 0, st, A, channel_sums, coefficients);
+                            });
+                        if (status != LEAP_OK) return status;
+                        if (!d_grad_x) continue;
+                        hipLaunchKernelGGL((k_group_grad<T, FULL, ACT>), dim3((unsigned)(now * each)), dim3(BLOCK), 0, st, A);
+                        if ((status = launched()) != LEAP_OK) return status;
+                    }
+                    return LEAP_OK;
+                });
             });
         });
     if (rc != LEAP_OK || !(d_grad_weight || d_grad_bias)) return rc;

@@ -77,35 +77,36 @@ def _description(q, k, v, mask, table, buckets, positions, scale):
 
 
 def _attend(q, k, v, mask, table, buckets, positions, scale, keep):
-    """(o, statistics, rest)"""
+    """(o, the memory of its statistics and of what its rounding leaves)"""
     batch, queries, heads, width = q.shape
     device = q.device
     desc = _description(q, k, v, mask, table, buckets, positions, scale)
     o = torch.empty(q.shape, dtype=BF16, device=device)
-    stats = torch.empty((batch, heads, queries, 2), dtype=torch.float32, device=device) if keep else None
-    rest = torch.empty(q.shape, dtype=torch.float16, device=device) if keep else None
+    kept = stats = rest = None
+    if keep:
+        kept = torch.empty(batch * heads * queries * (8 + 2 * width), dtype=torch.uint8, device=device)
+        stats = kept.data_ptr()
+        rest = stats + batch * heads * queries * 8
     work = _work(_library().leap_attention_work(desc), device)
-    _call("leap_attention", device, desc, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), _address(stats), _address(rest), _address(work))
-    return o, stats, rest
+    _call("leap_attention", device, desc, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), stats, rest, _address(work))
+    return o, kept
 
 
 class _Attention(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, v, table, mask, buckets, places, scale):
-        o, stats, rest = _attend(q, k, v, mask, table, buckets, places, scale, True)
+        o, kept = _attend(q, k, v, mask, table, buckets, places, scale, True)
         # the probabilities are formed again from what made the statistics: nothing of it is packed
-        ctx.save_for_backward(*map(_bytes, (q, k, v, o, stats, rest, table, mask, buckets, *(places or (None, None)))))
+        ctx.save_for_backward(_bytes(q), _bytes(k), _bytes(v), _bytes(o), _bytes(table), kept, mask, buckets, *(places or (None, None)))
         ctx.scale, ctx.table_type = scale, None if table is None else table.dtype
         return o
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, grad):
-        q, k, v, o, stats, rest, table, mask, buckets, *places = ctx.saved_tensors
-        q, k, v, o = (t.view(BF16) for t in (q, k, v, o))
+        q, k, v, o, table, kept, mask, buckets, *places = ctx.saved_tensors
+        q, k, v, o = q.view(BF16), k.view(BF16), v.view(BF16), o.view(BF16)
         table = None if table is None else table.view(ctx.table_type)
-        buckets = None if buckets is None else buckets.view(torch.int32)
-        places = [None if t is None else t.view(torch.int32) for t in places]
         need_q, need_k, need_v, need_table = ctx.needs_input_grad[:4]
         device = q.device
         if grad.stride(3) != 1 or grad.is_neg():
@@ -116,8 +117,9 @@ class _Attention(torch.autograd.Function):
         grad_v = torch.empty(v.shape, dtype=BF16, device=device) if need_v else None
         grad_table = torch.empty(table.shape, dtype=torch.float32, device=device) if need_table else None
         work = _work(_library().leap_attention_backward_work(desc, need_table), device)
+        stats = kept.data_ptr()
         _call("leap_attention_backward", device, desc, grad.data_ptr(), *grad.stride()[:3], q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(),
-              stats.data_ptr(), rest.data_ptr(), _address(grad_q), _address(grad_k), _address(grad_v), _address(grad_table), _address(work))
+              stats, stats + q.shape[0] * q.shape[1] * q.shape[2] * 8, _address(grad_q), _address(grad_k), _address(grad_v), _address(grad_table), _address(work))
         return grad_q, grad_k, grad_v, grad_table.to(ctx.table_type) if need_table else None, None, None, None, None
 
 
