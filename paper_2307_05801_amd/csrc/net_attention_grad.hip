@@ -34,7 +34,17 @@ __device__ inline query_stats stats_of(const grad_args &G, int64_t row)
 
 constexpr int DELTA_LANES = LEAP_ATTENTION_WIDEST / 8, DELTA_ROWS = BLOCK / DELTA_LANES;
 
-// delta: sixteen lanes a row.
+// The sum of grad o over eight values of a row; o is what it was before its rounding.
+__device__ inline float grad_dot_o(const u32x4 &g, const u32x4 &o, const u32x4 &rest)
+{
+    const auto half = [](const u32x4 &v, int i) { return __uint_as_float(i % 2 ? v[i / 2] & 0xffff0000u : v[i / 2] << 16); };
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum += half(g, i) * (half(o, i) + element<LEAP_F16>::to_float((uint16_t)(rest[i / 2] >> (i % 2 * 16))) * 0x1p-8f);
+    return sum;
+}
+
+// delta by itself, where k_grad_query does not run: sixteen lanes a row.
 __global__ __launch_bounds__(BLOCK) void k_delta(grad_args G)
 {
     const attention_args &A = G.a;
@@ -43,12 +53,8 @@ __global__ __launch_bounds__(BLOCK) void k_delta(grad_args G)
     if (row >= (int64_t)A.batch * A.queries * A.heads) return;
     const int head = (int)(row % A.heads);
     const int64_t query = row / A.heads % A.queries, item = row / A.heads / A.queries;
-    const auto halves = [](const u32x4 &v, int i) { return __uint_as_float(i % 2 ? v[i / 2] & 0xffff0000u : v[i / 2] << 16); };
     const u32x4 g = row_piece(G.grad.data + item * G.grad.item + query * G.grad.row + head * G.grad.head, A.width, lane);
-    const u32x4 o = row_piece(G.o + row * A.width, A.width, lane), rest = row_piece(G.rest + row * A.width, A.width, lane);
-    float sum = 0.0f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) sum += halves(g, i) * (halves(o, i) + element<LEAP_F16>::to_float((uint16_t)(rest[i / 2] >> (i % 2 * 16))) * 0x1p-8f);
+    float sum = grad_dot_o(g, row_piece(G.o + row * A.width, A.width, lane), row_piece(G.rest + row * A.width, A.width, lane));
 #pragma unroll
     for (int d = 1; d < DELTA_LANES; d *= 2) sum += __shfl_xor(sum, d);
     if (lane == 0) G.delta[(item * A.heads + head) * (int64_t)A.queries + query] = sum;
@@ -122,7 +128,16 @@ template <int DEEP, bool DIRECT, bool BIAS, int BUCKETS> __global__ __launch_bou
         load_side<STEPS>(g, G.grad.data + item * G.grad.item + head * G.grad.head + query * G.grad.row, width, there, lane);
         const int64_t row = (item * A.heads + head) * (int64_t)A.queries + query;
         const query_stats stats = there ? stats_of(G, row) : query_stats{0.0f, INFINITY};
-        const float delta = there ? G.delta[row] : 0.0f, base = stats.most + stats.log;
+        float delta = 0.0f;
+        {
+            const int64_t at = ((item * A.queries + query) * A.heads + head) * width;
+#pragma unroll
+            for (int s = 0; s < STEPS; ++s)
+                if (there) delta += grad_dot_o(__builtin_bit_cast(u32x4, g[s]), row_piece(G.o + at, width, s * 2 + lane / 32), row_piece(G.rest + at, width, s * 2 + lane / 32));
+            delta = column_sum(delta);
+            if (there && lane < 32) G.delta[row] = delta;          // for k_grad_key
+        }
+        const float base = stats.most + stats.log;
         // with a table scores can be so large that the logarithm of their sum is lost in `base`: what is missing is a factor of the query's
         const float factor = BIAS && stats.log < INFINITY ? __builtin_amdgcn_exp2f(base - stats.most - stats.log) : 0.0f, lowered = factor * delta;
         const int position = BIAS ? query_position(A, there ? query : A.queries - 1) : 0;
@@ -497,7 +512,7 @@ extern "C" int leap_attention_backward(const leap_attention_desc *desc, const vo
                 d_stats, (float *)d_work, (uint16_t *)d_grad_q, (uint16_t *)d_grad_k, (uint16_t *)d_grad_v, (float *)((char *)d_work + delta_bytes(desc) + lines_bytes(desc)),
                 (int32_t)table_parts(desc), 0};
     int rc = LEAP_OK;
-    if (rows && (d_grad_q || d_grad_k || d_grad_v || d_grad_table))
+    if (rows && !d_grad_q && !d_grad_table && (d_grad_k || d_grad_v))
         rc = over_blocks((rows + DELTA_ROWS - 1) / DELTA_ROWS, [&](int64_t first, unsigned blocks) {
             G.first = first;
             hipLaunchKernelGGL(k_delta, dim3(blocks), dim3(BLOCK), 0, st, G);
