@@ -67,7 +67,7 @@ constexpr int window_of_tile(int deep, int buckets) { return deep > 64 || bucket
 // integers to two numbers for every difference that its pairs have: whole multiples of 2^-24 of the largest of them, and what is left in multiples of 2^-48.  (With the
 // first alone sums were 0.6e-5 to 6e-5 of the table's norm off, since a bucket that nearly all of a query's keys are in has a sum far smaller than its terms.)  Keys rise, so a
 // difference has at most one pair of each of the block's 128 queries, and 128 times 2^24 fits 32 bits.
-// In the next tile's time one wave adds the differences' sums, as floats, to their buckets, which the block keeps.
+// In the next tile's time the sums go to their buckets, which the block keeps as floats, a wave to every fourth bucket.
 // Where the differences are too far apart or keys do not rise, ds go to the buckets as two integers, of 2^-17 and 2^-34 of the largest: 8192 of either fit.
 template <int BUCKETS, int WINDOW> struct table_sums {
     float bucket[BUCKETS];
@@ -150,7 +150,7 @@ template <int DEEP, bool DIRECT, bool BIAS, int BUCKETS> __global__ __launch_bou
         key_walk at(A.mask ? A.mask + item * A.mask_item : nullptr, 0, A.keys, lane);
         line_window window{}, coming{}, before{};
         bool fours = false, coming_fours = false, rising = false, coming_rising = false, pending = false;
-        int place = 0, duty = 0;
+        int place = 0;
         float unscale = 0.0f;
         const bool sound = __all(base == base && finite_magnitude(delta) | (delta == 0.0f));       // what is not a number in a query's pairs is in these
         const auto fetch = [&](int to) {
@@ -164,17 +164,18 @@ template <int DEEP, bool DIRECT, bool BIAS, int BUCKETS> __global__ __launch_bou
                 if (wave == 0) place = key_position(A, at.first + lane < A.keys ? (int)at.first + lane : A.keys - 1);
             }
         };
-        // The sums of the tile before, by the wave whose turn it is.
+        // The sums of the tile before: every wave has the buckets of its own, and each of those its order.
         const auto settle = [&] {
-            if constexpr (BUCKETS != 0) {
-                if (pending && wave == duty)
+            if constexpr (BUCKETS != 0)
+                if (pending)
                     for (int i = lane; i < before.count; i += WAVE) {
-                        const float s = ((float)sums.upper[i] + (float)sums.lower[i] * 0x1p-24f) * unscale;
+                        const int bucket = sums.which[i];
+                        if (bucket % WAVES != wave) continue;
+                        const int upper = sums.upper[i], lower = sums.lower[i];
+                        if (!(upper | lower) && unscale == unscale) continue;              // a float's add takes the 3 cycles for every lane that makes one
                         sums.upper[i] = sums.lower[i] = 0;
-                        __hip_atomic_fetch_add(&sums.bucket[sums.which[i]], s, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+                        __hip_atomic_fetch_add(&sums.bucket[bucket], ((float)upper + (float)lower * 0x1p-24f) * unscale, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
                     }
-                duty = (duty + 1) % WAVES;
-            }
         };
         __syncthreads();                                   // the unit before has read its tiles
         if (!at.done()) fetch(0);
