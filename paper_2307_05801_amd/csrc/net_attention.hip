@@ -26,13 +26,18 @@ struct forward_args {
     int64_t first;                         // block of this launch of k_join
 };
 
-// What rounding v to bfloat16 leaves, as it is kept.
-__device__ inline uint16_t rest_of(float v) { return element<LEAP_F16>::from_float(rest_of_bf16(v) * 256.0f); }
+// What rounding v to bfloat16 leaves, as it is kept: the difference of the two numbers' bits, of 16 bits and a sign, whatever v's size.  (2^15 is one where v lies just
+// between two and the lower is taken; one less than that is a unit of 32 bits off.)
+__device__ inline uint16_t rest_of(float v)
+{
+    const int rest = (int)(__float_as_uint(v) - ((uint32_t)element<LEAP_BF16>::from_float(v) << 16));
+    return finite_magnitude(v) ? (uint16_t)(rest < 0x7fff ? rest : 0x7fff) : 0;
+}
 
 // BIAS: with a table.  FINE: for a backward pass, which takes delta = grad.o off every product grad.v of a query: an o with its rounding, or with the probabilities',
 // would spoil all of the query's alike, and in grad_q that adds up along what the keys have in common (keys and values with a common part as large as what
 // differs, 512 keys: grad_q was 0.020 of its norm off, with four times as large a part 0.34; now 0.003 and 0.007, which is the rounding of ds).  So there the
-// probabilities are the sum of two bfloat16, and what o's rounding leaves is kept.
+// probabilities are the sum of two bfloat16, and o's other 16 bits are kept.
 template <int DEEP, bool DIRECT, bool BIAS, bool FINE> __global__ __launch_bounds__(BLOCK, 2) void k_attention(forward_args F)
 {
     using tile = rows_tile<DEEP>;

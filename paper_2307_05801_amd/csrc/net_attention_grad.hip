@@ -34,13 +34,15 @@ __device__ inline query_stats stats_of(const grad_args &G, int64_t row)
 
 constexpr int DELTA_LANES = LEAP_ATTENTION_WIDEST / 8, DELTA_ROWS = BLOCK / DELTA_LANES;
 
-// The sum of grad o over eight values of a row; o is what it was before its rounding.
+// The sum of grad o over eight values of a row; o is what it was before its rounding: its bits and what is to be added to them.
 __device__ inline float grad_dot_o(const u32x4 &g, const u32x4 &o, const u32x4 &rest)
 {
-    const auto half = [](const u32x4 &v, int i) { return __uint_as_float(i % 2 ? v[i / 2] & 0xffff0000u : v[i / 2] << 16); };
     float sum = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) sum += half(g, i) * (half(o, i) + element<LEAP_F16>::to_float((uint16_t)(rest[i / 2] >> (i % 2 * 16))) * 0x1p-8f);
+    for (int i = 0; i < 8; ++i) {
+        const uint32_t gi = i % 2 ? g[i / 2] & 0xffff0000u : g[i / 2] << 16, oi = i % 2 ? o[i / 2] & 0xffff0000u : o[i / 2] << 16;
+        sum += __uint_as_float(gi) * __uint_as_float(oi + (uint32_t)(int32_t)(int16_t)(rest[i / 2] >> (i % 2 * 16)));
+    }
     return sum;
 }
 

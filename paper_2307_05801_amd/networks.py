@@ -132,7 +132,7 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, mask: torch.Ten
     not matter whatever it holds, and a query without keys has zeros.  scale: width ** -0.5 if not given.
 
     table: a learned number [heads, buckets] (float32, bfloat16, float16; at most 4096 buckets) for every head and bucket of relative positions, added to the scaled
-    product.  positions: int32 [rows] of queries and keys alike, or a pair of them (not given: 0, 1, 2, ...), within +-2^30; buckets: int32 [n], the bucket of
+    product.  positions: int32 [rows] of queries and keys alike, or a pair of them (None: 0, 1, 2, ...), within +-2^30; buckets: int32 [n], the bucket of
     key's position - query's position at index n // 2 + that; differences beyond its ends take the ends'.  relative_buckets makes both for a grid of
     patches.  -inf in the table leaves pairs out.
 
@@ -172,8 +172,9 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, mask: torch.Ten
             positions = (positions, positions) if isinstance(positions, torch.Tensor) else tuple(positions)
             if len(positions) != 2:
                 raise ValueError("positions: one tensor, or one of queries and one of keys")
-            _integers(positions[0], queries, device, "positions of queries")
-            _integers(positions[1], keys, device, "positions of keys")
+            for t, n, what in ((positions[0], queries, "queries"), (positions[1], keys, "keys")):
+                if t is not None:
+                    _integers(t, n, device, f"positions of {what}")
     scale = width ** -0.5 if scale is None else float(scale)
     if not 0.0 < scale < 1e30:
         raise ValueError(f"scale must be positive, got {scale}")

@@ -34,7 +34,7 @@ def run(N, q, k, v, grad, table=None, mask=None, buckets=None, positions=None, s
         return t.cuda() if isinstance(t, torch.Tensor) else t
 
     q, k, v, table = (None if t is None else there(t).detach().requires_grad_(True) for t in (q, k, v, table))
-    positions = tuple(map(there, positions)) if isinstance(positions, tuple) else there(positions)
+    positions = tuple(None if t is None else there(t) for t in positions) if isinstance(positions, tuple) else there(positions)
     o = N.attention(q, k, v, table=table, mask=there(mask), buckets=there(buckets), positions=positions, scale=scale)
     wanted = [t for t in (q, k, v, table) if t is not None]
     grads = torch.autograd.grad(o, wanted, there(grad))
@@ -337,6 +337,29 @@ def test_gradients_that_are_wanted(N):
         leaves = [t.cuda().requires_grad_(j == i) for j, t in enumerate((q, k, v, table))]
         got, = torch.autograd.grad(N.attention(*leaves[:3], table=leaves[3], buckets=buckets.cuda()), leaves[i], g.cuda())
         assert torch.equal(got, every[i])
+
+
+@pytest.mark.parametrize("size", [1e-30, 1e-9, 1e6, 1e25])
+def test_values_and_gradients_of_any_size(N, size):
+    """What o's rounding leaves is kept for numbers of every size: the gradients are as good as for ordinary ones."""
+    q, k, v, g = inputs(1, 130, 200, 2, 2, 64, 231)
+    v, g = (v.double() * size).to(BF16), (g.double() / size).to(BF16)
+    table, buckets = rand((2, 9), 232, F32), torch.arange(329, dtype=torch.int32) % 9
+    got, r = run(N, q, k, v, g, table, None, buckets), R.Attention(q, k, v, g, None, table, buckets)
+    check(got, r)
+    assert (got[4].cpu().double() - r.grad_table).norm() <= 1e-5 * r.grad_table.norm()
+
+
+def test_buckets_beyond_the_tables_ends(N):
+    """They take its ends', and positions may be given for queries or keys alone."""
+    t = inputs(1, 70, 90, 2, 2, 64, 241)
+    buckets = torch.arange(159, dtype=torch.int32) - 40
+    buckets[::7] = torch.iinfo(torch.int32).max
+    buckets[1::7] = torch.iinfo(torch.int32).min
+    table = rand((2, 60), 242, F32)
+    places_ = torch.arange(90, dtype=torch.int32).flip(0)
+    for positions in (None, (None, places_), (places_[:70].contiguous(), None)):
+        check(run(N, *t, table, None, buckets, positions), R.Attention(*t, None, table, buckets, positions))
 
 
 def test_keys_and_values_with_a_common_part(N):
