@@ -41,6 +41,7 @@ struct attention_args {
     // in the workspace, with a table: a number for every difference of positions, in units of log2, heads `line` apart; its bucket; the positions of each TILE rows
     float *lines;
     uint16_t *line_buckets;
+    uint8_t *line_rising;                  // of every 64 of them: each is larger than the one before
     place_range *query_places, *key_places;
     int32_t line;
 };
@@ -109,7 +110,7 @@ template <int STEPS> __device__ inline void load_side(bf16x8 (&side)[STEPS], con
 }
 
 // Tiles of one head's rows on their way to shared memory.  DIRECT: past the registers, where rows begin at multiples of 16 bytes, are whole
-// multiples of 8 values, and a tile spans less than 2^31 bytes.  Otherwise through them, so that land() puts down what fetch() has asked for.
+// multiples of 8 values or followed by zeros, and a tile spans less than 2^31 bytes.  Otherwise through them, so that land() puts down what fetch() has asked for.
 template <int DEEP, bool DIRECT> struct source;
 template <int DEEP> struct source<DEEP, true> {
     using tile = rows_tile<DEEP>;
@@ -121,7 +122,7 @@ template <int DEEP> struct source<DEEP, true> {
 
     __device__ inline source(const uint16_t *rows, int64_t stride_, int64_t count, int width, int wave, int lane) : base((const uint8_t *)rows), stride(stride_ * 2)
     {
-        end = (count - 1) * stride + width * 2;
+        end = (count - 1) * stride + whole(width * 2, 16);                  // (rows whose width is no multiple of 8 have zeros up to one, from lay_out)
 #pragma unroll
         for (int e = 0; e < EACH; ++e) {
             const int slot = (e * WAVES + wave) * 64 + lane, r = slot * 16 / tile::ROW, chunk = (tile::place(r, 0) - r * tile::ROW) / 16 ^ slot % (tile::ROW / 16);
@@ -343,6 +344,9 @@ template <int BLOCKS> __device__ inline void store_column(uint16_t *row, int wid
     }
 }
 
+// A number that a wave's lanes have in common, as the compiler is to know.
+__device__ inline int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+
 // Unit u of `units`, such that neighbouring units (which share keys, or queries) run on the same of the eight parts of the chip: blocks go round over those.
 __device__ inline int64_t unit_of(int64_t block, int64_t units)
 {
@@ -376,6 +380,11 @@ attention_args arguments_of(const leap_attention_desc *d, const void *q, const v
 
 // Whether every row of an array is a whole number of aligned 16 bytes and a tile of them within a buffer's reach.
 bool direct_array(const void *p, int64_t item, int64_t row, int64_t head, int64_t width);
+// Rows whose width is no multiple of 8 as rows that are, with zeros behind them: bytes, and what writes them.  Pays (18414 patches of 49: a step of 9.3 ms, 12.4 without)
+// where a row is read again and again: by more than LAID_OUT rows of the other side.
+constexpr int64_t LAID_OUT = 512;
+int64_t laid_out_bytes(int64_t items, int64_t rows, int64_t heads, int64_t width);
+int lay_out(rows_of &array, int64_t items, int64_t rows, int64_t heads, int64_t width, void *to, hipStream_t st);
 // The lines' workspace, and what writes it; nothing without a table.
 int64_t lines_bytes(const leap_attention_desc *d);
 int write_lines(attention_args &A, void *work, hipStream_t st);

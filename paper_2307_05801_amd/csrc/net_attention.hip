@@ -38,7 +38,7 @@ __device__ inline uint16_t rest_of(float v)
 // would spoil all of the query's alike, and in grad_q that adds up along what the keys have in common (keys and values with a common part as large as what
 // differs, 512 keys: grad_q was 0.020 of its norm off, with four times as large a part 0.34; now 0.003 and 0.007, which is the rounding of ds).  So there the
 // probabilities are the sum of two bfloat16, and o's other 16 bits are kept.
-template <int DEEP, bool DIRECT, bool BIAS, bool FINE> __global__ __launch_bounds__(BLOCK, 2) void k_attention(forward_args F)
+template <int DEEP, bool DIRECT, bool BIAS, bool FINE> __global__ __launch_bounds__(BLOCK, DEEP > 64 || !DIRECT ? 2 : 3) void k_attention(forward_args F)
 {
     using tile = rows_tile<DEEP>;
     constexpr int STEPS = DEEP / 16, BLOCKS = DEEP / 32, WINDOW = window_of_tile(DEEP);
@@ -47,13 +47,13 @@ template <int DEEP, bool DIRECT, bool BIAS, bool FINE> __global__ __launch_bound
     __shared__ int places[BIAS ? 2 : 1][TILE];
     lds_byte *const lds = (lds_byte *)room;
     const int lane = threadIdx.x % WAVE, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
-    const int cols = COLS / F.abreast, tiles = (A.queries + cols - 1) / cols;
+    const int cols = COLS / F.abreast, tiles = (A.queries + cols - 1) / cols, across = A.heads / F.abreast;
     int64_t unit = unit_of(blockIdx.x, gridDim.x);
-    const int part = (int)(unit % F.parts);
+    const int part = uniform((int)(unit % F.parts));
     unit /= F.parts;
-    const int64_t item = unit / tiles / (A.heads / F.abreast);
-    const int head = (int)(unit / tiles % (A.heads / F.abreast)) * F.abreast + wave % F.abreast, kv_head = head / (A.heads / A.kv_heads);
-    const int query0 = (int)(unit % tiles) * cols, query = query0 + wave / F.abreast * 32 + lane % 32;
+    const int64_t item = uniform((int)(unit / tiles / across));
+    const int head = uniform((int)(unit / tiles % across) * F.abreast + wave % F.abreast), kv_head = uniform(head / (A.heads / A.kv_heads));
+    const int query0 = uniform((int)(unit % tiles) * cols), query = query0 + uniform(wave / F.abreast) * 32 + lane % 32;
     const bool there = query < A.queries;
     source<DEEP, DIRECT> k(A.k.data + item * A.k.item + kv_head * A.k.head, A.k.row, A.keys, A.width, wave, lane);
     source<DEEP, DIRECT> v(A.v.data + item * A.v.item + kv_head * A.v.head, A.v.row, A.keys, A.width, wave, lane);
@@ -240,6 +240,17 @@ __global__ __launch_bounds__(BLOCK) void k_join(forward_args F)
     if (F.stats && threadIdx.x == 0) F.stats[row * 2] = sum != 0.0f ? base : 0.0f, F.stats[row * 2 + 1] = sum != 0.0f ? __builtin_amdgcn_logf(sum) : INFINITY;
 }
 
+// Rows of `width` to rows of whole 16 bytes, a piece a thread.
+__global__ __launch_bounds__(BLOCK) void k_lay_rows(rows_of from, int rows, int heads, int width, int64_t pieces, int64_t first, uint8_t *to)
+{
+    const int each = (width + 7) / 8;
+    const int64_t id = (first + blockIdx.x) * BLOCK + threadIdx.x;
+    if (id >= pieces) return;
+    const int64_t row = id / each, head = row % heads, at = row / heads % rows, item = row / heads / rows;
+    const u32x4 v = row_piece(from.data + item * from.item + at * from.row + head * from.head, width, (int)(id % each));
+    __builtin_memcpy(to + id * 16, &v, 16);
+}
+
 // A head's number for every difference of positions; and what positions each tile of queries and of keys has.
 __global__ __launch_bounds__(BLOCK) void k_lines(attention_args A)
 {
@@ -248,7 +259,11 @@ __global__ __launch_bounds__(BLOCK) void k_lines(attention_args A)
         if (id < A.offsets) {
             const int bucket = bucket_at(A, id);
             A.lines[(int64_t)blockIdx.y * A.line + id] = table_value(A, blockIdx.y, bucket);
-            if (blockIdx.y == 0) A.line_buckets[id] = (uint16_t)bucket;
+            if (blockIdx.y == 0) {
+                A.line_buckets[id] = (uint16_t)bucket;
+                const bool rising = __all(id + 1 >= A.offsets || bucket_at(A, id + 1) > bucket);
+                if (id % WAVE == 0) A.line_rising[id / WAVE] = rising;
+            }
         }
         return;
     }
@@ -278,13 +293,26 @@ bool direct_array(const void *p, int64_t item, int64_t row, int64_t head, int64_
     return width % 8 == 0 && (uintptr_t)p % 16 == 0 && item % 8 == 0 && row % 8 == 0 && head % 8 == 0 && row < (int64_t)1 << 24;
 }
 
+int64_t laid_out_bytes(int64_t items, int64_t rows, int64_t heads, int64_t width) { return width % 8 ? items * rows * heads * ((width + 7) / 8) * 16 : 0; }
+
+int lay_out(rows_of &array, int64_t items, int64_t rows, int64_t heads, int64_t width, void *to, hipStream_t st)
+{
+    const int64_t pieces = items * rows * heads * ((width + 7) / 8), row = (width + 7) / 8 * 8;
+    const int rc = over_blocks((pieces + BLOCK - 1) / BLOCK, [&](int64_t first, unsigned n) {
+        hipLaunchKernelGGL(k_lay_rows, dim3(n), dim3(BLOCK), 0, st, array, (int)rows, (int)heads, (int)width, pieces, first, (uint8_t *)to);
+    });
+    array = {(const uint16_t *)to, rows * heads * row, heads * row, row};
+    return rc;
+}
+
 static int64_t line_length(int64_t offsets) { return (offsets + 7) / 8 * 8; }
+static int64_t rising_bytes(int64_t offsets) { return (offsets + WAVE * 16 - 1) / (WAVE * 16) * 16; }
 static int64_t tiles_of(int64_t rows) { return (rows + TILE - 1) / TILE; }
 
 int64_t lines_bytes(const leap_attention_desc *d)
 {
     if (!d->d_table) return 0;
-    return d->heads * line_length(d->offsets) * 4 + line_length(d->offsets) * 2 + (tiles_of(d->queries) + tiles_of(d->keys)) * (int64_t)sizeof(place_range);
+    return d->heads * line_length(d->offsets) * 4 + line_length(d->offsets) * 2 + rising_bytes(d->offsets) + (tiles_of(d->queries) + tiles_of(d->keys)) * (int64_t)sizeof(place_range);
 }
 
 int write_lines(attention_args &A, void *work, hipStream_t st)
@@ -293,7 +321,8 @@ int write_lines(attention_args &A, void *work, hipStream_t st)
     A.line = (int32_t)length;
     A.lines = (float *)work;
     A.line_buckets = (uint16_t *)(A.lines + A.heads * length);
-    A.query_places = (place_range *)(A.line_buckets + length);
+    A.line_rising = (uint8_t *)(A.line_buckets + length);
+    A.query_places = (place_range *)(A.line_rising + rising_bytes(A.offsets));
     A.key_places = A.query_places + tiles_of(A.queries);
     const int64_t threads = A.offsets > tiles * WAVE ? A.offsets : tiles * WAVE;
     hipLaunchKernelGGL(k_lines, dim3((unsigned)((threads + BLOCK - 1) / BLOCK), (unsigned)(A.heads + 1)), dim3(BLOCK), 0, st, A);
@@ -369,11 +398,14 @@ int64_t part_bytes(const leap_attention_desc *d, const shares &S)
     return S.parts > 1 ? (d->batch * d->heads * d->queries * S.parts * (d->width + 2) * 4 + 15) / 16 * 16 : 0;
 }
 
+// Of keys, and of values, laid out.
+int64_t laid_out(const leap_attention_desc *d) { return d->queries > LAID_OUT ? laid_out_bytes(d->batch, d->keys, d->kv_heads, d->width) : 0; }
+
 }  // namespace
 
 extern "C" int64_t leap_attention_work(const leap_attention_desc *desc)
 {
-    return bad_attention(desc) ? 0 : lines_bytes(desc) + part_bytes(desc, shares_of(desc));
+    return bad_attention(desc) ? 0 : lines_bytes(desc) + part_bytes(desc, shares_of(desc)) + 2 * laid_out(desc);
 }
 
 extern "C" int leap_attention(const leap_attention_desc *desc, const void *d_q, const void *d_k, const void *d_v, void *d_o, float *d_stats, void *d_rest,
@@ -384,18 +416,25 @@ extern "C" int leap_attention(const leap_attention_desc *desc, const void *d_q, 
     if (!d_q || !d_o || (desc->keys && (!d_k || !d_v))) return refuse("null data pointer");
     if (!d_rest != !d_stats) return refuse("statistics and what o's rounding leaves: both or neither");
     const shares S = shares_of(desc);
-    if (lines_bytes(desc) + part_bytes(desc, S) && unaligned(d_work)) return refuse(NO_WORK);
+    const int64_t lines = lines_bytes(desc), parts = part_bytes(desc, S), laid = laid_out(desc);
+    if (lines + parts + laid && unaligned(d_work)) return refuse(NO_WORK);
     forward_args F{arguments_of(desc, d_q, d_k, d_v), (uint16_t *)d_o, d_stats, (uint16_t *)d_rest, S.abreast, S.parts, S.length, nullptr, nullptr, 0};
     const int64_t blocks = S.units * S.parts, rows = desc->batch * desc->heads * desc->queries;
     if (blocks >= (int64_t)1 << 24) return refuse("more than 2^31 rows of heads");
-    F.part_sums = (float *)((char *)d_work + lines_bytes(desc));
+    F.part_sums = (float *)((char *)d_work + lines);
     F.part_stats = F.part_sums + rows * S.parts * desc->width;
     const hipStream_t st = stream_of(hip_stream);
     if (desc->d_table) {
         const int rc = write_lines(F.a, d_work, st);
         if (rc != LEAP_OK) return rc;
     }
-    const bool direct = direct_array(d_k, desc->k_item, desc->k_row, desc->k_head, desc->width) && direct_array(d_v, desc->v_item, desc->v_row, desc->v_head, desc->width);
+    if (laid) {
+        char *const to = (char *)d_work + lines + parts;
+        int rc = lay_out(F.a.k, desc->batch, desc->keys, desc->kv_heads, desc->width, to, st);
+        if (rc == LEAP_OK) rc = lay_out(F.a.v, desc->batch, desc->keys, desc->kv_heads, desc->width, to + laid, st);
+        if (rc != LEAP_OK) return rc;
+    }
+    const bool direct = laid || (direct_array(d_k, desc->k_item, desc->k_row, desc->k_head, desc->width) && direct_array(d_v, desc->v_item, desc->v_row, desc->v_head, desc->width));
     const int rc = by_width(desc->width, [&](auto w) {
         return by_flags([&](auto straight, auto bias, auto fine) {
             hipLaunchKernelGGL((k_attention<decltype(w)::value, decltype(straight)::value, decltype(bias)::value, decltype(fine)::value>), dim3((unsigned)blocks), dim3(BLOCK), 0, st, F);

@@ -69,7 +69,8 @@ constexpr int window_of_tile(int deep, int buckets) { return deep > 64 || bucket
 // integers to two numbers for every difference that its pairs have: whole multiples of 2^-24 of the largest of them, and what is left in multiples of 2^-48.  (With the
 // first alone sums were 0.6e-5 to 6e-5 of the table's norm off, since a bucket that nearly all of a query's keys are in has a sum far smaller than its terms.)  Keys rise, so a
 // difference has at most one pair of each of the block's 128 queries, and 128 times 2^24 fits 32 bits.
-// In the next tile's time the sums go to their buckets, which the block keeps as floats, a wave to every fourth bucket.
+// In the next tile's time the sums go to their buckets, which the block keeps as floats: without atomic adds where the window's buckets rise (one of its own to
+// every difference: in 512 windows 0.39 ms of 1.97 were such adds), otherwise a wave to every fourth bucket.
 // Where the differences are too far apart or keys do not rise, ds go to the buckets as two integers, of 2^-17 and 2^-34 of the largest: 8192 of either fit.
 template <int BUCKETS, int WINDOW> struct table_sums {
     float bucket[BUCKETS];
@@ -151,7 +152,8 @@ template <int DEEP, bool DIRECT, bool BIAS, int BUCKETS> __global__ __launch_bou
 
         key_walk at(A.mask ? A.mask + item * A.mask_item : nullptr, 0, A.keys, lane);
         line_window window{}, coming{}, before{};
-        bool fours = false, coming_fours = false, rising = false, coming_rising = false, pending = false;
+        bool fours = false, coming_fours = false, rising = false, coming_rising = false, pending = false, apart = false;
+        uint8_t coming_apart = 0;
         int place = 0;
         float unscale = 0.0f;
         const bool sound = __all(base == base && finite_magnitude(delta) | (delta == 0.0f));       // what is not a number in a query's pairs is in these
@@ -164,12 +166,19 @@ template <int DEEP, bool DIRECT, bool BIAS, int BUCKETS> __global__ __launch_bou
                 coming = window_of(A, keys, mine, WINDOW), coming_fours = keys.fours, coming_rising = keys.rising;
                 if (coming.inside) fetch_window<4>(line, A.offsets, coming, lds + 4 * tile::BYTES + to * WINDOW * 4, wave, lane);
                 if (wave == 0) place = key_position(A, at.first + lane < A.keys ? (int)at.first + lane : A.keys - 1);
+                if constexpr (BUCKETS != 0)        // (a window spans less than 64 times 64)
+                    coming_apart = coming.inside && coming.first / WAVE + lane <= (coming.first + coming.count - 1) / WAVE ? A.line_rising[coming.first / WAVE + lane] : 1;
             }
         };
         // The sums of the tile before: every wave has the buckets of its own, and each of those its order.
         const auto settle = [&] {
-            if constexpr (BUCKETS != 0)
-                if (pending)
+            if constexpr (BUCKETS != 0) {
+                if (pending && apart)              // no two of a bucket
+                    for (int i = threadIdx.x; i < before.count; i += BLOCK) {
+                        sums.bucket[sums.which[i]] += ((float)sums.upper[i] + (float)sums.lower[i] * 0x1p-24f) * unscale;
+                        sums.upper[i] = sums.lower[i] = 0;
+                    }
+                else if (pending)
                     for (int i = lane; i < before.count; i += WAVE) {
                         const int bucket = sums.which[i];
                         if (bucket % WAVES != wave) continue;
@@ -178,6 +187,7 @@ template <int DEEP, bool DIRECT, bool BIAS, int BUCKETS> __global__ __launch_bou
                         sums.upper[i] = sums.lower[i] = 0;
                         __hip_atomic_fetch_add(&sums.bucket[bucket], ((float)upper + (float)lower * 0x1p-24f) * unscale, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
                     }
+            }
         };
         __syncthreads();                                   // the unit before has read its tiles
         if (!at.done()) fetch(0);
@@ -190,6 +200,7 @@ template <int DEEP, bool DIRECT, bool BIAS, int BUCKETS> __global__ __launch_bou
                 if (wave == 0) places[turn][lane] = place;
                 window = coming, fours = coming_fours, rising = coming_rising;
             }
+            const bool window_apart = BUCKETS && __all(coming_apart != 0);
             if constexpr (DIRECT || BIAS) fetched();
             __syncthreads();
             at.next(lane);
@@ -285,7 +296,7 @@ template <int DEEP, bool DIRECT, bool BIAS, int BUCKETS> __global__ __launch_bou
                     }
                 }
             }
-            pending = near, before = window;
+            pending = near, before = window, apart = window_apart;
         };
         for (int turn = 0; !at.done(); turn ^= 1) one(turn);
         if constexpr (BUCKETS != 0) {
@@ -487,6 +498,10 @@ int64_t table_parts(const leap_attention_desc *d)
     return units < 1 ? 1 : units < most ? units : most;
 }
 
+// Of keys (and of values), and of queries (and of grad), laid out for the kernel that walks over them.
+int64_t laid_keys(const leap_attention_desc *d) { return d->queries > LAID_OUT ? laid_out_bytes(d->batch, d->keys, d->kv_heads, d->width) : 0; }
+int64_t laid_queries(const leap_attention_desc *d) { return d->keys > LAID_OUT ? laid_out_bytes(d->batch, d->queries, d->heads, d->width) : 0; }
+
 int64_t delta_bytes(const leap_attention_desc *d) { return (d->batch * d->heads * d->queries * 4 + 15) / 16 * 16; }
 
 }  // namespace
@@ -494,7 +509,7 @@ int64_t delta_bytes(const leap_attention_desc *d) { return (d->batch * d->heads 
 extern "C" int64_t leap_attention_backward_work(const leap_attention_desc *desc, int32_t with_table)
 {
     if (bad_attention(desc)) return 0;
-    return delta_bytes(desc) + lines_bytes(desc) + (with_table && desc->d_table ? desc->heads * table_parts(desc) * desc->buckets * 4 : 0);
+    return delta_bytes(desc) + lines_bytes(desc) + 2 * laid_keys(desc) + 2 * laid_queries(desc) + (with_table && desc->d_table ? desc->heads * table_parts(desc) * desc->buckets * 4 : 0);
 }
 
 extern "C" int leap_attention_backward(const leap_attention_desc *desc, const void *d_grad, int64_t grad_item, int64_t grad_row, int64_t grad_head, const void *d_q,
@@ -512,7 +527,7 @@ extern "C" int leap_attention_backward(const leap_attention_desc *desc, const vo
     if ((int64_t)desc->heads / desc->kv_heads * ((desc->queries + TILE - 1) / TILE) >= (int64_t)1 << 31) return refuse("more than 2^37 queries share a key");
     const hipStream_t st = stream_of(hip_stream);
     grad_args G{arguments_of(desc, d_q, d_k, d_v), {(const uint16_t *)d_grad, grad_item, grad_row, grad_head}, (const uint16_t *)d_o, (const uint16_t *)d_rest,
-                d_stats, (float *)d_work, (uint16_t *)d_grad_q, (uint16_t *)d_grad_k, (uint16_t *)d_grad_v, (float *)((char *)d_work + delta_bytes(desc) + lines_bytes(desc)),
+                d_stats, (float *)d_work, (uint16_t *)d_grad_q, (uint16_t *)d_grad_k, (uint16_t *)d_grad_v, (float *)((char *)d_work + delta_bytes(desc) + lines_bytes(desc) + 2 * laid_keys(desc) + 2 * laid_queries(desc)),
                 (int32_t)table_parts(desc), 0};
     int rc = LEAP_OK;
     if (rows && !d_grad_q && !d_grad_table && (d_grad_k || d_grad_v))
@@ -523,8 +538,21 @@ extern "C" int leap_attention_backward(const leap_attention_desc *desc, const vo
     if (rc != LEAP_OK) return rc;
     if (desc->d_table && (rows || d_grad_table)) rc = write_lines(G.a, (char *)d_work + delta_bytes(desc), st);
     if (rc != LEAP_OK) return rc;
-    const bool keys_direct = direct_array(d_k, desc->k_item, desc->k_row, desc->k_head, desc->width) && direct_array(d_v, desc->v_item, desc->v_row, desc->v_head, desc->width);
-    const bool queries_direct = direct_array(d_q, desc->q_item, desc->q_row, desc->q_head, desc->width) && direct_array(d_grad, grad_item, grad_row, grad_head, desc->width);
+    const int64_t laid_k = laid_keys(desc), laid_q = laid_queries(desc);
+    const bool keys_walked = d_grad_table || d_grad_q, queries_walked = d_grad_k || d_grad_v;
+    grad_args of_keys = G;                                 // for k_grad_key, which has its keys as they are
+    char *const to = (char *)d_work + delta_bytes(desc) + lines_bytes(desc);
+    if (laid_k && rows && keys_walked) {
+        rc = lay_out(G.a.k, desc->batch, desc->keys, desc->kv_heads, desc->width, to, st);
+        if (rc == LEAP_OK) rc = lay_out(G.a.v, desc->batch, desc->keys, desc->kv_heads, desc->width, to + laid_k, st);
+    }
+    if (laid_q && rows && queries_walked && rc == LEAP_OK) {
+        rc = lay_out(of_keys.a.q, desc->batch, desc->queries, desc->heads, desc->width, to + 2 * laid_k, st);
+        if (rc == LEAP_OK) rc = lay_out(of_keys.grad, desc->batch, desc->queries, desc->heads, desc->width, to + 2 * laid_k + laid_q, st);
+    }
+    if (rc != LEAP_OK) return rc;
+    const bool keys_direct = laid_k || (direct_array(d_k, desc->k_item, desc->k_row, desc->k_head, desc->width) && direct_array(d_v, desc->v_item, desc->v_row, desc->v_head, desc->width));
+    const bool queries_direct = laid_q || (direct_array(d_q, desc->q_item, desc->q_row, desc->q_head, desc->width) && direct_array(d_grad, grad_item, grad_row, grad_head, desc->width));
     return by_width(desc->width, [&](auto w) {
         constexpr int W = decltype(w)::value;
         int status = LEAP_OK;
@@ -548,7 +576,7 @@ extern "C" int leap_attention_backward(const leap_attention_desc *desc, const vo
         if (status != LEAP_OK || !kept || !(d_grad_k || d_grad_v)) return status;
         const dim3 grid((unsigned)(desc->batch * desc->kv_heads * key_tiles));
         return by_flags([&](auto direct, auto bias) {
-            hipLaunchKernelGGL((k_grad_key<W, decltype(direct)::value, decltype(bias)::value>), grid, dim3(BLOCK), 0, st, G);
+            hipLaunchKernelGGL((k_grad_key<W, decltype(direct)::value, decltype(bias)::value>), grid, dim3(BLOCK), 0, st, of_keys);
             return launched();
         }, queries_direct, desc->d_table != nullptr);
     });

@@ -89,6 +89,22 @@ def test_few_queries_with_a_bias(N, batch, queries, keys, heads, kv_heads, width
     check(run(N, *t, table, None, buckets), R.Attention(*t, None, table, buckets))
 
 
+@pytest.mark.parametrize("batch,queries,keys,heads,kv_heads,width", [(1, 600, 700, 2, 1, 49), (2, 520, 30, 2, 2, 5), (1, 30, 600, 4, 2, 33), (1, 513, 513, 1, 1, 127), (1, 513, 1, 2, 1, 9)])
+@pytest.mark.parametrize("kind", [None, "scattered", "lengths"])
+def test_rows_that_are_laid_out(N, batch, queries, keys, heads, kv_heads, width, kind):
+    """More than 512 of one side, rows that are no multiples of 16 bytes: within a wider array whose other values must not matter."""
+    t = inputs(batch, queries, keys, heads, kv_heads, width, 18)
+    mask = masks(batch, keys, kind) if kind else None
+    r = R.Attention(*t, mask=mask)
+    check(run(N, *t, mask=mask), r)
+    wide = []
+    for x in t:
+        room = torch.full(x.shape[:-1] + (width + 6,), float("nan"), dtype=BF16, device="cuda")
+        room[..., 5:5 + width] = x.cuda()
+        wide.append(room[..., 5:5 + width])
+    check(run(N, *wide, mask=mask), r)
+
+
 @pytest.mark.parametrize("scale", [1e-3, 1.0, 3.0])
 def test_scales(N, scale):
     """Probabilities from nearly even to nearly all on one key."""

@@ -120,6 +120,14 @@ def test_launches_of_attention():
     assert launches[0].blocks[0] == 512                       # four heads abreast, 128 parts of 2048 keys
 
 
+def test_rows_that_are_no_multiples_of_16_bytes_are_laid_out():
+    """Keys and values where more than 512 queries read them; and, backward, queries and gradients where more than 512 keys do."""
+    for queries, keys, forward, backward in ((513, 9, 2, 2), (9, 513, 0, 2), (513, 513, 2, 4), (512, 512, 0, 0)):
+        got = [sum(launch.kernel == "k_lay_rows" for launch in launches) for _, launches in record_attention(attention(1, queries, keys, 2, 1, 49))]
+        assert got == [forward, backward], (queries, keys)
+        assert not any(launch.kernel == "k_lay_rows" for _, launches in record_attention(attention(1, queries, keys, 2, 1, 48)) for launch in launches)
+
+
 def test_every_kernel_of_attention_is_reached():
     calls = []
     for width in (32, 64, 96, 128):
