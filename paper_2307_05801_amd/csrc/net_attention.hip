@@ -4,6 +4,10 @@
 // read from shared memory.  A wave forms x for 32 keys by 32 queries with a lane a query (net_attention.h says why), keeps the largest so far, m, and
 // the sum of exp2(x - m) of each query in that lane, and multiplies the values summed so far by exp2(m before - m now) where m has grown.  m follows the largest only when a
 // query's has got 2^8 ahead of it: sums of exp2 up to 2^8 are as good, and one of 32 queries has a new largest in nearly every tile.
+//
+// What bounds it: at width 64 the vector instructions (six to nine a pair beside an exponential of 16 clocks; 512 windows of 512 patches, 8 heads, a table, kept for a backward pass:
+// 0.95 ms, 290 TFLOP/s), at width 128 those and the matrix instructions about alike (32768 patches, 8 heads: 6.0 ms, 733 TFLOP/s, half as many flops again with the probabilities' second part). Three
+// blocks share a compute unit at width 64 (1155 us with two). Columns of 32, not of 64: with those a wave would need its SIMD's registers for itself.
 #include "net_attention.h"
 
 namespace {
@@ -382,9 +386,9 @@ shares shares_of(const leap_attention_desc *d)
     const int64_t group = d->heads / d->kv_heads, tiles = (d->keys + TILE - 1) / TILE;
     S.abreast = d->d_table ? 1 : d->queries <= 32 && group % 4 == 0 ? 4 : d->queries <= 64 && group % 2 == 0 ? 2 : 1;
     S.units = d->batch * (d->heads / S.abreast) * ((d->queries + COLS / S.abreast - 1) / (COLS / S.abreast));
-    // Half the chip without work and at least eight tiles to a block: parts of four tiles and more, as many as fill it
+    // Half the chip without work and at least sixteen tiles to a block (one query and eight tiles: 11.6 us a call, 16 in two parts): parts of four tiles and more, as many as fill it
     int64_t parts = 1;
-    if (S.units > 0 && S.units <= 128 && tiles >= 8) {
+    if (S.units > 0 && S.units <= 128 && tiles >= 16) {
         parts = 512 / S.units;
         parts = parts < tiles / 4 ? parts : tiles / 4;
     }

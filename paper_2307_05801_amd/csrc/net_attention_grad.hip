@@ -5,6 +5,9 @@
 // Two kernels, each the owner of what it writes, so that no sum depends on an order of arrival: k_grad_query has queries in its lanes and
 // walks over keys as the forward pass does; k_grad_key has keys in its lanes and walks over queries.  Both form the scores and dp: seven products instead
 // of the five of one kernel, which would have to add up grad_q over blocks.
+//
+// 32768 patches, 8 heads of 128: queries 6.3 ms, keys and values 9.7 ms (1050 and 900 TFLOP/s of matrix instructions; the latter's sums leave room for one wave a SIMD). 512
+// windows of 512 patches, 8 heads of 64 with a table: 1.69 and 1.16 ms, bound by vector instructions and, for the table's gradient, adds to shared memory (0.4 ms of the 1.69).
 #include "net_attention.h"
 
 namespace {

@@ -93,6 +93,12 @@ class Attention:
             self.grad_table_off = by_bucket(off_ds + sum_error(queries + keys) * ds.abs()) + half_step(table.dtype) * self.grad_table.abs()
 
 
+def rounding(t, dtype):
+    """How far rounding float64 t to dtype may put it off: half a step, which below float16's least normal number, 2^-14, is 2^-25 whatever the value
+    (steps there are 2^-24; the other types' are below 2^-126)."""
+    return half_step(dtype) * t.abs() + (2.0 ** -25 if dtype is torch.float16 else 0.0)
+
+
 def _slope(u, activation):
     s = torch.sigmoid(u)
     return s * (1 + u * (1 - s)) if activation == "silu" else (u > 0).double() if activation == "relu" else torch.ones_like(u)
@@ -128,7 +134,7 @@ class GroupNorm:
         off_h = off_d * rstd + h.abs() * (off_r + 4 * unit)
         off_u = w.abs() * off_h + 4 * unit * ((h * w).abs() + b.abs())
         near = (8 + u.abs()) * unit if activation == "silu" else 0.0
-        self.y, self.y_off = y.reshape(shape), (1.1 * off_u + (near + half_step(dtype)) * y.abs()).reshape(shape)
+        self.y, self.y_off = y.reshape(shape), (1.1 * off_u + near * y.abs() + rounding(y, dtype)).reshape(shape)
         if grad is None:
             return
         g = grad.double().reshape(x.shape)
@@ -140,8 +146,8 @@ class GroupNorm:
         one, two = du.sum((0, 1)), (du * h).sum((0, 1))
         off_one = (off_du + many * du.abs()).sum((0, 1))
         off_two = (off_du * h.abs() + du.abs() * off_h + many * (du * h).abs()).sum((0, 1))
-        self.grad_bias, self.grad_bias_off = one.flatten(), (off_one + half_step(parameter) * one.abs()).flatten()
-        self.grad_weight, self.grad_weight_off = two.flatten(), (off_two + half_step(parameter) * two.abs()).flatten()
+        self.grad_bias, self.grad_bias_off = one.flatten(), (off_one + rounding(one, parameter)).flatten()
+        self.grad_weight, self.grad_weight_off = two.flatten(), (off_two + rounding(two, parameter)).flatten()
         d = du * w
         first, second = d.mean((1, 3), keepdim=True), (d * h).mean((1, 3), keepdim=True)
         off_first = ((off_du + many * du.abs()) * w.abs()).mean((1, 3), keepdim=True)
@@ -149,4 +155,4 @@ class GroupNorm:
         grad_x = rstd * (d - first - h * second)
         size_ = d.abs() + first.abs() + (h * second).abs()
         off = rstd * (off_du * w.abs() + off_first + h.abs() * off_second + off_h * second.abs() + (8 * unit + off_r) * size_)
-        self.grad_x, self.grad_x_off = grad_x.reshape(shape), (off + half_step(dtype) * grad_x.abs()).reshape(shape)
+        self.grad_x, self.grad_x_off = grad_x.reshape(shape), (off + rounding(grad_x, dtype)).reshape(shape)

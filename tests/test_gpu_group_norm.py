@@ -45,7 +45,7 @@ def check(got, r):
 
 
 SHAPES = [((1, 1, 8), 1), ((1, 1, 6), 2), ((2, 3, 1), 1), ((2, 50, 3), 3), ((3, 7, 5), 1), ((1, 1000, 5), 5), ((2, 333, 20), 4), ((2, 64, 64), 8), ((1, 4097, 12), 3), ((2, 10, 11, 12, 16), 4),
-          ((1, 77, 343), 7), ((1, 40, 512), 32), ((2, 33, 2100), 7), ((1, 9, 4096), 2), ((2, 5, 2051), 1), ((5, 17000, 8), 2), ((1, 70001, 7), 7), ((40, 300, 24), 3), ((3, 2, 96), 96), ((700, 9), 3)]
+          ((1, 77, 343), 7), ((1, 40, 512), 32), ((2, 33, 2100), 7), ((1, 9, 4096), 2), ((2, 5, 2051), 1), ((5, 17000, 8), 2), ((1, 70001, 7), 7), ((40, 300, 24), 3), ((3, 2, 96), 96), ((700, 9), 3), ((2, 2048, 64), 8), ((1, 1, 16384), 1), ((3, 85, 48), 2), ((60, 3, 24), 1), ((1, 2049, 8), 1)]
 
 
 @pytest.mark.parametrize("shape,groups", SHAPES)

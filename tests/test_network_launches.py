@@ -30,7 +30,7 @@ def test_a_launch_of_group_norm_has_fewer_than_2_32_threads():
     calls = [f(*s) for s in SIZES for f in (group, group_backward)] + [group(2, 1000, 20, 4, row=25), group_backward(2, 1000, 20, 4, row=25)]
     for (name, arguments), (status, launches) in zip(calls, record(calls)):
         assert status == B.LEAP_OK, (name, arguments)
-        assert launches[0].kernel == ("k_group_moments" if name == "leap_group_norm" else "k_group_sums")
+        assert launches[0].kernel in (("k_group_moments", "k_group_small") if name == "leap_group_norm" else ("k_group_sums",))
         for launch in launches:
             across, along, deep = launch.blocks
             assert 0 < across * launch.threads < 1 << 32 and along < 1 << 16 and deep == 1, (name, launch)
@@ -43,8 +43,17 @@ def test_items_of_group_norm_are_read_again_before_the_next():
     assert [launch.kernel for launch in many] == ["k_group_moments", "k_group_stats", "k_group_apply"]
 
 
+def test_few_values_take_one_launch():
+    small = [group(1, 256, 64, 8), group(1, 16384 // 8, 64, 8), group(1, 1, 16384, 1), group(64, 256, 64, 8, row=70)]
+    large = [group(1, 16384 // 8 + 1, 64, 8), group(1, 256, 60, 8 - 2), group(65, 256, 64, 8), group(1, 2, 16384, 1)]
+    assert all([launch.kernel for launch in launches] == ["k_group_small"] for _, launches in record(small))
+    assert all(launches[0].kernel == "k_group_moments" for _, launches in record(large))
+    (status, launches), = record([(group(1, 256, 64, 8)[0], group(1, 256, 64, 8)[1][:15] + (None, 0))])
+    assert status == B.LEAP_OK and launches[0].blocks[0] == 8              # needs no workspace
+
+
 def test_every_kernel_of_group_norm_is_reached():
-    calls = [f(2, 1000, channels, 4, type, row) for f in (group, group_backward) for type in (0, 1, 2) for channels, row in ((20, 25), (20, 20))]
+    calls = [f(2, 1000, channels, 4, type, row) for f in (group, group_backward) for type in (0, 1, 2) for channels, row in ((20, 25), (20, 20), (32, 32))]
     calls += [(name, a[:12] + (activation,) + a[13:] if name == "leap_group_norm" else a[:15] + (activation,) + a[16:]) for name, a in calls for activation in (0, 1)]
     calls += [(name, a[:9] + (a[4],) + a[10:]) for name, a in calls if name == "leap_group_norm_backward"]                # weights of x's type
     taken = {(launch.kernel, launch.parameters) for _, launches in record(calls) for launch in launches if launch.kernel.startswith("k_group")}
