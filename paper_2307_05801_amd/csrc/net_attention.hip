@@ -5,9 +5,9 @@
 // the sum of exp2(x - m) of each query in that lane, and multiplies the values summed so far by exp2(m before - m now) where m has grown.  m follows the largest only when a
 // query's has got 2^8 ahead of it: sums of exp2 up to 2^8 are as good, and one of 32 queries has a new largest in nearly every tile.
 //
-// What bounds it: at width 64 the vector instructions (six to nine a pair beside an exponential of 16 clocks; 512 windows of 512 patches, 8 heads, a table, kept for a backward pass:
-// 0.95 ms, 290 TFLOP/s), at width 128 those and the matrix instructions about alike (32768 patches, 8 heads: 6.0 ms, 733 TFLOP/s, half as many flops again with the probabilities' second part). Three
-// blocks share a compute unit at width 64 (1155 us with two). Columns of 32, not of 64: with those a wave would need its SIMD's registers for itself.
+// What bounds it: at width 64 the vector instructions (with a table 13 to 16 a pair, counted; 512 windows of 512 patches, 8 heads, kept for a backward pass: 0.95 ms, 290 TFLOP/s), at
+// width 128 those (10 a pair) and the matrix instructions about alike (32768 patches, 8 heads: 6.0 ms, 730 TFLOP/s, half as many flops again with the probabilities' second part).
+// Three blocks share a compute unit at width 64 (the windows with two: 1.16 ms).
 #include "net_attention.h"
 
 namespace {
@@ -386,7 +386,8 @@ shares shares_of(const leap_attention_desc *d)
     const int64_t group = d->heads / d->kv_heads, tiles = (d->keys + TILE - 1) / TILE;
     S.abreast = d->d_table ? 1 : d->queries <= 32 && group % 4 == 0 ? 4 : d->queries <= 64 && group % 2 == 0 ? 2 : 1;
     S.units = d->batch * (d->heads / S.abreast) * ((d->queries + COLS / S.abreast - 1) / (COLS / S.abreast));
-    // Half the chip without work and at least sixteen tiles to a block (one query and eight tiles: 11.6 us a call, 16 in two parts): parts of four tiles and more, as many as fill it
+    // Half the chip without work and at least sixteen tiles of keys: parts of four tiles and more, as many as fill it. One query, 8 heads of 64, a call: 8 tiles 11 us (16 in two parts),
+    // 15 tiles 17, 16 to 64 tiles in parts 15, which is the host's time for two launches; between 8 and 15 the two sides meet, and what that leaves is 2 us
     int64_t parts = 1;
     if (S.units > 0 && S.units <= 128 && tiles >= 16) {
         parts = 512 / S.units;

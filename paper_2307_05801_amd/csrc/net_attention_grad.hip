@@ -6,8 +6,9 @@
 // walks over keys as the forward pass does; k_grad_key has keys in its lanes and walks over queries.  Both form the scores and dp: seven products instead
 // of the five of one kernel, which would have to add up grad_q over blocks.
 //
-// 32768 patches, 8 heads of 128: queries 6.3 ms, keys and values 9.7 ms (1050 and 900 TFLOP/s of matrix instructions; the latter's sums leave room for one wave a SIMD). 512
-// windows of 512 patches, 8 heads of 64 with a table: 1.69 and 1.16 ms, bound by vector instructions and, for the table's gradient, adds to shared memory (0.4 ms of the 1.69).
+// 32768 patches, 8 heads of 128: queries 6.3 ms, keys and values 9.7 to 10.3 ms (1040, and 860 to 900 TFLOP/s of matrix instructions; the latter's sums leave room for one wave a SIMD).
+// 512 windows of 512 patches, 8 heads of 64 with a table: 1.69 and 1.17 ms, bound by vector instructions (22 and 14 a pair, counted) and, for the table's gradient, adds to shared
+// memory (those to differences took 0.27 ms: without the buckets' 1.58 ms, without either 1.30).
 #include "net_attention.h"
 
 namespace {

@@ -278,7 +278,7 @@ template <int TYPE, bool FULL, int ACTIVATION> __global__ __launch_bounds__(BLOC
     });
 }
 
-// Few values, whole groups of eights: a block has a group of an item in its registers, which takes one launch instead of three (256 voxels of 64 channels: 6 us instead of 22).
+// Few values, whole groups of eights: a block has a group of an item in its registers, which takes one launch instead of three (256 voxels of 64 channels: 6.8 us instead of 22).
 constexpr int SMALL_EIGHTS = 8;            // of a thread
 constexpr int64_t SMALL_GROUP = (int64_t)BLOCK * SMALL_EIGHTS * CHUNK, SMALL = (int64_t)1 << 20;        // values of a group, and of all: neighbouring groups share lines of memory
 
