@@ -27,8 +27,11 @@ BF16 = torch.bfloat16
 
 def _bytes(t):
     """t's memory as autograd is to keep it: as bytes, which hooks that pack what is saved (activations.keep_in_8_bits) leave as they are.  Detached first: a
-    view would hold its base, and an output that its graph."""
-    return None if t is None else t.detach().view(torch.uint8)
+    view would hold its base, and an output that its graph.  Rows of one value may have any last stride (.contiguous() leaves it); as bytes they need one of 1."""
+    if t is None:
+        return None
+    t = t.detach()
+    return (t if t.stride(-1) == 1 else t.as_strided(t.shape, (*t.stride()[:-1], 1))).view(torch.uint8)
 
 
 def _library():
@@ -45,17 +48,14 @@ _DESC = struct.Struct("<18q5Qif")                             # leap_attention_d
 
 
 def _heads(t: torch.Tensor, what: str, device=None):
-    """The tensor [batch, rows, heads, width], checked."""
+    """Checks a tensor [batch, rows, heads, width]."""
     _on_gpu(t, what, device)
     if t.dtype is not BF16 or t.dim() != 4 or not 1 <= t.shape[3] <= B.LEAP_ATTENTION_WIDEST:
         raise ValueError(f"{what} must be bfloat16 [batch, rows, heads, width], width at most {B.LEAP_ATTENTION_WIDEST}, got {t.dtype} {tuple(t.shape)}")
     if t.is_neg():
         raise ValueError(f"{what} is a negated view, whose memory holds other values; call .resolve_neg()")
-    if t.stride(3) != 1:
-        if t.shape[3] > 1:
-            raise ValueError(f"{what}: the values of a row must be neighbours; call .contiguous()")
-        return t.contiguous()
-    return t
+    if t.stride(3) != 1 and t.shape[3] > 1:
+        raise ValueError(f"{what}: the values of a row must be neighbours; call .contiguous()")
 
 
 def _integers(t: torch.Tensor, n: int, device, what: str):
@@ -140,9 +140,10 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, mask: torch.Ten
     the forward pass that a backward pass follows: there probabilities have 16 bits (so o's last bits differ from those without one).  Kept for the
     backward pass: q, k, v and o, as they are also within keep_in_8_bits (the probabilities are formed again from what made them), 2 bytes more a value of
     o, and two floats a query and head."""
-    q = _heads(q, "q")
+    _heads(q, "q")
     device = q.device
-    k, v = _heads(k, "k", device), _heads(v, "v", device)
+    _heads(k, "k", device)
+    _heads(v, "v", device)
     batch, queries, heads, width = q.shape
     keys, kv_heads = k.shape[1], k.shape[2]
     if k.shape[0] != batch or k.shape[3] != width or v.shape != k.shape or kv_heads < 1 or heads < 1 or heads % kv_heads:

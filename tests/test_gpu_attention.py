@@ -308,6 +308,21 @@ def test_rows_from_any_byte_on(N):
     check(run(N, *(w.cuda()[..., 1:50] for w in wide)), R.Attention(*t))
 
 
+def test_rows_of_one_value_and_tables_of_one_bucket_with_any_last_stride(N):
+    q, k, v, g = inputs(2, 5, 37, 3, 3, 1, 313)
+    table, buckets = rand((3, 1), 317, F32), torch.zeros(9, dtype=torch.int32)
+
+    def turned(t):
+        there = torch.empty(*t.shape[:2], 1, t.shape[2], dtype=t.dtype, device="cuda").transpose(2, 3)
+        assert there.stride(3) == 3
+        return there.copy_(t)
+
+    line = torch.empty(3, dtype=F32, device="cuda").as_strided((3, 1), (1, 5)).copy_(table)
+    assert line.stride(1) == 5
+    r = R.Attention(q, k, v, g, table=table, buckets=buckets)
+    check(run(N, turned(q), turned(k), turned(v), turned(g), table=line, buckets=buckets), r)
+
+
 def test_one_item_for_a_batch(N):
     """Keys and values of one item for all (distance 0), heads of one for all: autograd adds the gradients up."""
     q, k, v, g = inputs(1, 50, 90, 2, 2, 32, 121)

@@ -166,3 +166,13 @@ def test_the_group_norm_references_gradients_are_those_of_differences():
             ends = [(R.GroupNorm(*(s * h * way + u if u is t else u for u in (x,)), 2, *(s * h * way + u if u is t else u for u in (w, b)), activation, 1e-3).y * grad).sum() for s in (1, -1)]
             got, want = (getattr(r, name) * way).sum(), (ends[0] - ends[1]) / (2 * h)
             assert abs(got - want) <= 1e-7 * (1 + abs(want)), (activation, name)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16, torch.float32])
+def test_what_is_kept_as_bytes_may_have_any_last_stride_where_rows_have_one_value(dtype):
+    rows = torch.arange(30).to(dtype).reshape(2, 5, 1, 3).transpose(2, 3)                     # [2, 5, 3, 1], last stride 3
+    one = torch.arange(24).to(dtype)[2:].as_strided((5, 1), (2, 9))
+    for t in (rows, one):
+        assert t.stride(-1) != 1
+        assert torch.equal(N._bytes(t).view(dtype), t)
+        assert N._bytes(t).data_ptr() == t.data_ptr()
