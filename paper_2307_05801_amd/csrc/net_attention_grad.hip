@@ -495,6 +495,21 @@ template <int DEEP, bool DIRECT, bool BIAS> __global__ __launch_bounds__(BLOCK, 
     if (G.grad_v) store_column<BLOCKS>(G.grad_v + row, A.width, gv, 1.0f, lane, there);
 }
 
+// Gradients that no query has a part in, eight values of 16 bits a thread.
+__global__ __launch_bounds__(BLOCK) void k_zeros(uint16_t *to, int64_t values, int64_t first)
+{
+    const int64_t at = ((first + blockIdx.x) * BLOCK + threadIdx.x) * CHUNK;
+    if (at < values) store_piece<2>((uint8_t *)(to + at), (values - at) * 2, u32x4{0, 0, 0, 0});
+}
+
+int zeros_to(void *to, int64_t values, hipStream_t st)
+{
+    if (!to) return LEAP_OK;
+    return over_blocks((values + BLOCK * CHUNK - 1) / (BLOCK * CHUNK), [&](int64_t first, unsigned blocks) {
+        hipLaunchKernelGGL(k_zeros, dim3(blocks), dim3(BLOCK), 0, st, (uint16_t *)to, values, first);
+    });
+}
+
 // Blocks that a head's units are dealt out to where the table's gradient is formed: each has room of its own for it.
 int64_t table_parts(const leap_attention_desc *d)
 {
@@ -525,32 +540,37 @@ extern "C" int leap_attention_backward(const leap_attention_desc *desc, const vo
     if (d_grad_table && !desc->d_table) return refuse("the gradient of a table that is not there");
     const int64_t rows = desc->batch * desc->heads * desc->queries, kept = desc->batch * desc->kv_heads * desc->keys;
     if (rows && (!d_grad || !d_q || !d_o || !d_stats || !d_rest || (desc->keys && (!d_k || !d_v)))) return refuse("null data pointer");
-    if ((rows || d_grad_table) && unaligned(d_work)) return refuse(NO_WORK);
+    if (rows && unaligned(d_work)) return refuse(NO_WORK);
     const int64_t tiles = (desc->queries + COLS - 1) / COLS, key_tiles = (desc->keys + COLS - 1) / COLS;
     if (desc->batch * desc->heads * tiles >= (int64_t)1 << 24 || desc->batch * desc->kv_heads * key_tiles >= (int64_t)1 << 24) return refuse("more than 2^31 rows of heads");
     if ((int64_t)desc->heads / desc->kv_heads * ((desc->queries + TILE - 1) / TILE) >= (int64_t)1 << 31) return refuse("more than 2^37 queries share a key");
     const hipStream_t st = stream_of(hip_stream);
+    if (!rows) {                                           // nothing is read, the workspace is not written
+        const int rc = zeros_to(d_grad_k, kept * desc->width, st);
+        const int status = rc == LEAP_OK ? zeros_to(d_grad_v, kept * desc->width, st) : rc;
+        return status == LEAP_OK ? zeros_to(d_grad_table, desc->heads * desc->buckets * 2, st) : status;
+    }
     grad_args G{arguments_of(desc, d_q, d_k, d_v), {(const uint16_t *)d_grad, grad_item, grad_row, grad_head}, (const uint16_t *)d_o, (const uint16_t *)d_rest,
                 d_stats, (float *)d_work, (uint16_t *)d_grad_q, (uint16_t *)d_grad_k, (uint16_t *)d_grad_v, (float *)((char *)d_work + delta_bytes(desc) + lines_bytes(desc) + 2 * laid_keys(desc) + 2 * laid_queries(desc)),
                 (int32_t)table_parts(desc), 0};
     int rc = LEAP_OK;
-    if (rows && !d_grad_q && !d_grad_table && (d_grad_k || d_grad_v))
+    if (!d_grad_q && !d_grad_table && (d_grad_k || d_grad_v))
         rc = over_blocks((rows + DELTA_ROWS - 1) / DELTA_ROWS, [&](int64_t first, unsigned blocks) {
             G.first = first;
             hipLaunchKernelGGL(k_delta, dim3(blocks), dim3(BLOCK), 0, st, G);
         });
     if (rc != LEAP_OK) return rc;
-    if (desc->d_table && (rows || d_grad_table)) rc = write_lines(G.a, (char *)d_work + delta_bytes(desc), st);
+    if (desc->d_table) rc = write_lines(G.a, (char *)d_work + delta_bytes(desc), st);
     if (rc != LEAP_OK) return rc;
     const int64_t laid_k = laid_keys(desc), laid_q = laid_queries(desc);
     const bool keys_walked = d_grad_table || d_grad_q, queries_walked = d_grad_k || d_grad_v;
     grad_args of_keys = G;                                 // for k_grad_key, which has its keys as they are
     char *const to = (char *)d_work + delta_bytes(desc) + lines_bytes(desc);
-    if (laid_k && rows && keys_walked) {
+    if (laid_k && keys_walked) {
         rc = lay_out(G.a.k, desc->batch, desc->keys, desc->kv_heads, desc->width, to, st);
         if (rc == LEAP_OK) rc = lay_out(G.a.v, desc->batch, desc->keys, desc->kv_heads, desc->width, to + laid_k, st);
     }
-    if (laid_q && rows && queries_walked && rc == LEAP_OK) {
+    if (laid_q && queries_walked && rc == LEAP_OK) {
         rc = lay_out(of_keys.a.q, desc->batch, desc->queries, desc->heads, desc->width, to + 2 * laid_k, st);
         if (rc == LEAP_OK) rc = lay_out(of_keys.grad, desc->batch, desc->queries, desc->heads, desc->width, to + 2 * laid_k + laid_q, st);
     }
@@ -570,7 +590,7 @@ extern "C" int leap_attention_backward(const leap_attention_desc *desc, const vo
             const dim3 across((unsigned)((desc->buckets + BLOCK - 1) / BLOCK), (unsigned)desc->heads);
             hipLaunchKernelGGL(k_join_table, across, dim3(BLOCK), 0, st, G.part, G.parts, (int)desc->buckets, d_grad_table);
             status = launched();
-        } else if (d_grad_q && rows) {
+        } else if (d_grad_q) {
             const dim3 grid((unsigned)(desc->batch * desc->heads * tiles));
             status = by_flags([&](auto direct, auto bias) {
                 hipLaunchKernelGGL((k_grad_query<W, decltype(direct)::value, decltype(bias)::value, 0>), grid, dim3(BLOCK), 0, st, G);

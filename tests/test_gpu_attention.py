@@ -538,3 +538,19 @@ def test_one_of_two_devices_is_enough(N):
     t = [x.cuda() for x in inputs(1, 5, 5, 1, 1, 8, 211)]
     with torch.cuda.device(0):
         assert N.attention(*t[:3]).device == t[0].device
+
+
+@pytest.mark.parametrize("batch,queries,keys", [(2, 0, 300), (1, 0, 5), (0, 5, 5), (2, 0, 0)])
+@pytest.mark.parametrize("width", [1, 16, 49])
+def test_no_queries_and_a_table_that_wants_no_gradient(N, batch, queries, keys, width):
+    """Zeros for keys and values, also where the table is frozen or there is none; each by itself too."""
+    q, k, v, _ = (t.cuda() for t in inputs(batch, queries, keys, 2, 1, width, 143))
+    table, buckets = rand((2, 9), 144, F32).cuda(), torch.arange(9, dtype=torch.int32).cuda()
+    for bias in (dict(), dict(table=table, buckets=buckets)):
+        for wanted in ((k, v), (k,), (v,), (q, k)):
+            leaves = [t.detach().requires_grad_(any(t is w for w in wanted)) for t in (q, k, v)]
+            o = N.attention(*leaves, **bias)
+            room = torch.full((1 << 16,), 7.0, device="cuda")       # what memory held before
+            del room
+            got = torch.autograd.grad(o, [t for t in leaves if t.requires_grad], torch.zeros_like(o))
+            assert all(t.shape == w.shape and not t.any() for t, w in zip(got, wanted))

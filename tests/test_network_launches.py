@@ -151,3 +151,32 @@ def test_every_kernel_of_attention_is_reached():
     mine = ("k_attention", "k_grad_query", "k_grad_key", "k_delta", "k_lines", "k_join", "k_join_table")
     names = {k for k in kernels() if k[0] in mine and k != ("k_join", (0,)) and k != ("k_join", (1,)) and k != ("k_join", (2,))}       # (the norm's weights' gradient has a k_join too)
     assert {k for k in taken if k[0] in mine} == names
+
+
+@pytest.mark.parametrize("batch", [0, 2])
+def test_no_kernel_reads_lines_that_are_not_written(batch):
+    """With a table every kernel that takes a number for a pair comes after the one that writes those, whichever gradients are wanted; without queries nothing is read at all."""
+    calls = []
+    for queries in (0, 1, 5, 130):
+        for keys in (0, 300):
+            for wanted in range(1, 16):
+                for buckets in (0, 9):
+                    name, desc, a = attention(batch, queries, keys, 2, 1, 64, buckets, 9)[1]
+                    calls.append((name, desc, a[:10] + [P if wanted >> i & 1 and (buckets or i < 3) else 0 for i in range(4)] + a[14:]))
+                calls.append((name, desc, a))
+            calls.append(attention(batch, queries, keys, 2, 1, 64, 9, 9)[0])
+    for (name, desc, a), (status, launches) in zip(calls, record_attention(calls)):
+        assert status == B.LEAP_OK
+        names = [launch.kernel for launch in launches]
+        for i, launch in enumerate(launches):
+            biased = launch.kernel in ("k_attention", "k_grad_query", "k_grad_key") and launch.parameters[2]
+            assert not biased or "k_lines" in names[:i], (desc, a)
+        if name == "leap_attention_backward" and not (batch and desc[1]):
+            keys = batch and desc[2]
+            assert names == ["k_zeros"] * (bool(a[11] and keys) + bool(a[12] and keys) + bool(a[13])), (desc, a)
+
+
+def test_gradients_without_queries_need_no_memory_but_their_own():
+    name, desc, a = attention(2, 0, 300, 2, 1, 64, 9, 9)[1]
+    (status, launches), = record_attention([(name, desc, [0] + a[1:4] + [0] * 6 + a[10:14] + [0, 0])])
+    assert status == B.LEAP_OK and [launch.kernel for launch in launches] == ["k_zeros"] * 3
