@@ -37,14 +37,14 @@ struct array {
 struct part {
     int position, turn, turns, count;       // which eight of a period, which of the block's periods at once; values there
     int64_t from, to, whole;                // periods; up to which they are known to be complete
-    int64_t item, strip;
+    int64_t item, strip;                    // item: of those at once, which the arrays' addresses begin with
 
-    __device__ inline part(const dealing &D, int64_t item0, bool backwards)
+    __device__ inline part(const dealing &D, bool backwards)
     {
         int64_t block = backwards ? gridDim.x - 1 - blockIdx.x : blockIdx.x;
         const int segment = (int)(block % D.segments);
         block /= D.segments;
-        strip = block % D.strips, item = item0 + block / D.strips;
+        strip = block % D.strips, item = block / D.strips;
         turns = D.positions < BLOCK ? BLOCK / D.positions : 1;
         position = D.segments > 1 ? segment * BLOCK + (int)threadIdx.x : (int)threadIdx.x % D.positions;
         turn = D.segments > 1 ? 0 : (int)threadIdx.x / D.positions;
@@ -106,7 +106,7 @@ struct group_args {
     const float *coefficients;              // [items][groups][2]
     float *parts;
     void *out;
-    int64_t first, item0;
+    int64_t first;
     bool past;                              // outputs past the caches
 };
 
@@ -127,7 +127,7 @@ struct moments {
 template <int TYPE, bool FULL> __global__ __launch_bounds__(BLOCK, 4) void k_group_moments(group_args A)
 {
     const dealing &D = A.deal;
-    const part P(D, A.item0, false);
+    const part P(D, false);
     using raw = typename element<TYPE>::raw;
     const raw *const x = (const raw *)A.x.data + P.item * A.x.item + P.position * CHUNK;
     const int64_t step = P.step(D, A.x.row);
@@ -257,7 +257,7 @@ template <int ACTIVATION> __device__ inline float slope(float u)
 template <int TYPE, bool FULL, int ACTIVATION> __global__ __launch_bounds__(BLOCK, 4) void k_group_apply(group_args A)
 {
     const dealing &D = A.deal;
-    const part P(D, A.item0, true);
+    const part P(D, true);
     using raw = typename element<TYPE>::raw;
     const raw *const x = (const raw *)A.x.data + P.item * A.x.item + P.position * CHUNK;
     raw *const y = (raw *)A.out + P.item * D.voxels * D.channels + P.position * CHUNK;
@@ -340,7 +340,7 @@ template <int TYPE, int ACTIVATION> __global__ __launch_bounds__(BLOCK) void k_g
 template <int TYPE, bool FULL, int ACTIVATION> __global__ __launch_bounds__(BLOCK, 4) void k_group_sums(group_args A)
 {
     const dealing &D = A.deal;
-    const part P(D, A.item0, false);
+    const part P(D, false);
     using raw = typename element<TYPE>::raw;
     const raw *const x = (const raw *)A.x.data + P.item * A.x.item + P.position * CHUNK, *const grad = (const raw *)A.grad.data + P.item * A.grad.item + P.position * CHUNK;
     const int64_t step = P.step(D, A.x.row), grad_step = P.step(D, A.grad.row);
@@ -436,15 +436,20 @@ __global__ __launch_bounds__(WIDE) void k_group_coefficients(group_args A, doubl
     if (threadIdx.x == 0) coefficients[unit * 2] = (float)(one / m), coefficients[unit * 2 + 1] = (float)(two / m);
 }
 
-// grad_weight, grad_bias: the channels' sums over the items.
-template <int WTYPE> __global__ __launch_bounds__(BLOCK) void k_group_weights(const double *channel_sums, int64_t items, int channels, void *grad_weight, void *grad_bias)
+// grad_weight, grad_bias: the channels' sums over the items, after those `before` them (null: none); to `after` as they are where more items follow.
+template <int WTYPE>
+__global__ __launch_bounds__(BLOCK) void k_group_weights(const double *channel_sums, int64_t items, int channels, const double *before, double *after, void *grad_weight, void *grad_bias)
 {
     using raw = typename element<WTYPE>::raw;
     const int c = blockIdx.x * BLOCK + threadIdx.x;
     if (c >= channels) return;
-    double one = 0.0, two = 0.0;
+    double one = before ? before[c * 2] : 0.0, two = before ? before[c * 2 + 1] : 0.0;
 #pragma unroll 4
     for (int64_t n = 0; n < items; ++n) one += channel_sums[(n * channels + c) * 2], two += channel_sums[(n * channels + c) * 2 + 1];
+    if (after) {
+        after[c * 2] = one, after[c * 2 + 1] = two;
+        return;
+    }
     if (grad_bias) ((raw *)grad_bias)[c] = element<WTYPE>::from_float((float)one);
     if (grad_weight) ((raw *)grad_weight)[c] = element<WTYPE>::from_float((float)two);
 }
@@ -452,7 +457,7 @@ template <int WTYPE> __global__ __launch_bounds__(BLOCK) void k_group_weights(co
 template <int TYPE, bool FULL, int ACTIVATION> __global__ __launch_bounds__(BLOCK, 4) void k_group_grad(group_args A)
 {
     const dealing &D = A.deal;
-    const part P(D, A.item0, true);
+    const part P(D, true);
     using raw = typename element<TYPE>::raw;
     const raw *const x = (const raw *)A.x.data + P.item * A.x.item + P.position * CHUNK, *const grad = (const raw *)A.grad.data + P.item * A.grad.item + P.position * CHUNK;
     raw *const to = (raw *)A.out + P.item * D.voxels * D.channels + P.position * CHUNK;
@@ -529,26 +534,51 @@ const char *bad_distances(int64_t item, int64_t row, int64_t items, int64_t voxe
     return bad_stride(row, voxels, channels);
 }
 
-// Items that are read for their sums and again before the next: `values` of x, or one.
-int64_t items_at_once(int64_t items, int64_t voxels, int64_t channels, int64_t values)
-{
-    int64_t n = values / (voxels * channels > 0 ? voxels * channels : 1);
-    n = n < 1 ? 1 : n < (int64_t)1 << 20 ? n : (int64_t)1 << 20;
-    return n < items ? n : items;
-}
 constexpr int64_t AT_ONCE_FORWARD = (int64_t)1 << 26, AT_ONCE_BACKWARD = (int64_t)1 << 25;
 
-// Bytes of the parts, for the dealing that has more of them.
-int64_t parts_bytes(int64_t items, int64_t at_once, int64_t voxels, int64_t channels, int64_t groups, int64_t each)
-{
-    int64_t most = 0;
-    for (const bool flat : {false, true}) {
-        const dealing D = dealing_of(at_once, voxels, channels, groups, flat);
-        const int64_t n = items * D.strips * D.positions * CHUNK * each;
-        most = n > most ? n : most;
+// Items that are read for their sums and again before the next: `values` of x, or one.  The workspace is theirs alone, since the stream orders what works on them before
+// what works on the next.  An item has no fewer slots than channels however few its voxels are, so those at once have no more than an eighth of all values, or 2^20; and values are cut
+// regardless of rows where an item has at least eight periods of them: with a voxel of 63 channels to an item a period would be eight times what there is.
+// Channels' sums are added up after `held` items, a multiple of `at_once`.
+struct plan {
+    dealing deal;
+    int64_t at_once, held;
+
+    // flat: rows of both arrays have no gaps.
+    plan(int64_t items, int64_t voxels, int64_t channels, int64_t groups, bool flat, int64_t values)
+    {
+        const int64_t common = divisor(channels, CHUNK), rows = CHUNK / common, all = items * voxels * channels;
+        flat = flat && voxels >= 8 * rows;
+        const int64_t slots = flat ? channels * rows : (channels + CHUNK - 1) / CHUNK * CHUNK, room = all / 8 > (int64_t)1 << 20 ? all / 8 : (int64_t)1 << 20;
+        const auto at_most = [](int64_t a, int64_t b) { return a < b ? a : b; };
+        at_once = at_most(values / (voxels * channels > 0 ? voxels * channels : 1), room / slots);
+        at_once = at_most(at_most(at_once < 1 ? 1 : at_once, (int64_t)1 << 20), items);
+        const int64_t times = at_once ? room / 2 / (at_once * channels) : 1;
+        held = at_most(at_once * (times < 1 ? 1 : times), items);
+        deal = dealing_of(at_once, voxels, channels, groups, flat);
     }
-    return (most + 15) / 16 * 16;
-}
+    int64_t parts() const { return at_once * deal.strips * deal.positions * CHUNK; }
+};
+
+int64_t sixteens(int64_t bytes) { return (bytes + 15) / 16 * 16; }
+
+// Bytes of the parts, of `each` a slot, and of the channels' sums, for the dealing that has more of them.
+struct room {
+    int64_t parts = 0, coefficients = 0, sums = 0;
+    room(int64_t items, int64_t voxels, int64_t channels, int64_t groups, int64_t values, int64_t each)
+    {
+        for (const bool flat : {false, true}) {
+            const plan L(items, voxels, channels, groups, flat, values);
+            const auto at_least = [](int64_t &a, int64_t b) { a = a > b ? a : b; };
+            at_least(parts, sixteens(L.parts() * each));
+            at_least(coefficients, sixteens(L.at_once * groups * 8));
+            at_least(sums, L.held * channels * 16);
+        }
+    }
+};
+
+// Where item `item` of an array begins.
+const void *item_of(const void *p, int32_t type, int64_t item, int64_t distance) { return (const char *)p + item * distance * (type == LEAP_F32 ? 4 : 2); }
 
 bool is_small(int64_t items, int64_t voxels, int64_t channels, int64_t groups)
 {
@@ -584,7 +614,8 @@ const char *bad_kinds(int32_t type, int32_t weight_type, int32_t activation)
 extern "C" int64_t leap_group_norm_work(int64_t items, int64_t voxels, int64_t channels, int64_t groups)
 {
     if (bad_group(items, voxels, channels, groups) || !items || !voxels || is_small(items, voxels, channels, groups)) return 0;
-    return parts_bytes(items, items_at_once(items, voxels, channels, AT_ONCE_FORWARD), voxels, channels, groups, sizeof(moments)) + (items * groups * 8 + 15) / 16 * 16;
+    const room R(items, voxels, channels, groups, AT_ONCE_FORWARD, sizeof(moments));
+    return R.parts + R.coefficients;
 }
 
 extern "C" int leap_group_norm(const void *d_x, int32_t type, int64_t x_item, int64_t x_row, const void *d_weight, const void *d_bias, int32_t weight_type, int64_t items,
@@ -613,26 +644,28 @@ extern "C" int leap_group_norm(const void *d_x, int32_t type, int64_t x_item, in
         });
     }
     if (unaligned(d_work)) return refuse(NO_WORK);
-    const int64_t at_once = items_at_once(items, voxels, channels, AT_ONCE_FORWARD);
+    const plan L(items, voxels, channels, groups, x_row == channels, AT_ONCE_FORWARD);
+    const room R(items, voxels, channels, groups, AT_ONCE_FORWARD, sizeof(moments));
     group_args A{};
-    A.deal = dealing_of(at_once, voxels, channels, groups, x_row == channels || voxels == 1);
+    A.deal = L.deal;
     A.x = {d_x, x_item, x_row};
     A.weight = d_weight, A.bias = d_bias, A.weight_type = weight_type, A.eps = eps;
-    A.parts = (float *)d_work, A.out = d_y, A.past = voxels * channels * items > PAST_VALUES;
-    A.stats = d_stats ? d_stats : (float *)((char *)d_work + parts_bytes(items, at_once, voxels, channels, groups, sizeof(moments)));
+    A.parts = (float *)d_work, A.past = voxels * channels * items > PAST_VALUES;
     const int64_t each = (int64_t)A.deal.strips * A.deal.segments;
-    if (at_once * each >= (int64_t)1 << 24) return refuse("more than 2^24 blocks of items");
+    if (L.at_once * each >= (int64_t)1 << 24) return refuse("more than 2^24 blocks of items");
     return by_type(type, [&](auto t) {
         return by_activation(activation, [&](auto a) {
             return by_full(A.deal, [&](auto full) -> int {
                 constexpr int T = decltype(t)::value;
-                for (A.item0 = 0; A.item0 < items; A.item0 += at_once) {
-                    const int64_t now = items - A.item0 < at_once ? items - A.item0 : at_once;
+                for (int64_t item = 0; item < items; item += L.at_once) {
+                    const int64_t now = items - item < L.at_once ? items - item : L.at_once;
+                    A.x.data = item_of(d_x, type, item, x_item), A.out = (void *)item_of(d_y, type, item, voxels * channels);
+                    A.stats = d_stats ? d_stats + item * groups * 2 : (float *)((char *)d_work + R.parts);
                     hipLaunchKernelGGL((k_group_moments<T, decltype(full)::value>), dim3((unsigned)(now * each)), dim3(BLOCK), 0, st, A);
                     int rc = launched();
                     if (rc == LEAP_OK)
                         rc = over_blocks(now * groups, [&](int64_t first, unsigned n) {
-                            A.first = A.item0 * groups + first;
+                            A.first = first;
                             hipLaunchKernelGGL(k_group_stats, dim3(n), dim3(WIDE), 0, st, A);
                         });
                     if (rc != LEAP_OK) return rc;
@@ -649,7 +682,8 @@ extern "C" int64_t leap_group_norm_backward_work(int64_t items, int64_t voxels, 
 {
     if (bad_group(items, voxels, channels, groups)) return 0;
     if (!items || !voxels) return 16;
-    return parts_bytes(items, items_at_once(items, voxels, channels, AT_ONCE_BACKWARD), voxels, channels, groups, 8) + items * channels * 16 + (items * groups * 8 + 15) / 16 * 16;
+    const room R(items, voxels, channels, groups, AT_ONCE_BACKWARD, 8);
+    return R.parts + R.sums + channels * 16 + R.coefficients;
 }
 
 extern "C" int leap_group_norm_backward(const void *d_grad, int64_t grad_item, int64_t grad_row, const void *d_x, int32_t type, int64_t x_item, int64_t x_row,
@@ -665,46 +699,57 @@ extern "C" int leap_group_norm_backward(const void *d_grad, int64_t grad_item, i
     if (some && (!d_grad || !d_x || !d_stats)) return refuse("null data pointer");
     if (unaligned(d_work)) return refuse(NO_WORK);
     const hipStream_t st = stream_of(hip_stream);
-    const int64_t at_once = items_at_once(items, voxels, channels, AT_ONCE_BACKWARD);
+    const plan L(items, voxels, channels, groups, x_row == channels && grad_row == channels, AT_ONCE_BACKWARD);
+    const room R(items, voxels, channels, groups, AT_ONCE_BACKWARD, 8);
     group_args A{};
-    A.deal = dealing_of(at_once, voxels, channels, groups, (x_row == channels && grad_row == channels) || voxels == 1);
+    A.deal = L.deal;
     A.x = {d_x, x_item, x_row}, A.grad = {d_grad, grad_item, grad_row};
     A.weight = d_weight, A.bias = d_bias, A.weight_type = weight_type;
-    A.stats = (float *)d_stats, A.parts = (float *)d_work, A.out = d_grad_x, A.past = voxels * channels * items > PAST_VALUES;
-    double *const channel_sums = (double *)((char *)d_work + parts_bytes(items, at_once, voxels, channels, groups, 8));
-    float *const coefficients = (float *)(channel_sums + items * channels * 2);
+    A.parts = (float *)d_work, A.past = voxels * channels * items > PAST_VALUES;
+    double *const channel_sums = (double *)((char *)d_work + R.parts), *const running = channel_sums + R.sums / 8;
+    float *const coefficients = (float *)(running + channels * 2);
     A.coefficients = coefficients;
     const int64_t each = (int64_t)A.deal.strips * A.deal.segments;
-    if (at_once * each >= (int64_t)1 << 24) return refuse("more than 2^24 blocks of items");
-    int rc = LEAP_OK;
-    if (some)
-        rc = by_type(type, [&](auto t) {
-            return by_activation(activation, [&](auto a) {
-                return by_full(A.deal, [&](auto full) -> int {
-                    constexpr int T = decltype(t)::value, ACT = decltype(a)::value;
-                    constexpr bool FULL = decltype(full)::value;
-                    for (A.item0 = 0; A.item0 < items; A.item0 += at_once) {
-                        const int64_t now = items - A.item0 < at_once ? items - A.item0 : at_once;
-                        hipLaunchKernelGGL((k_group_sums<T, FULL, ACT>), dim3((unsigned)(now * each)), dim3(BLOCK), 0, st, A);
-                        int status = launched();
-                        if (status == LEAP_OK)
-                            status = over_blocks(now * groups, [&](int64_t first, unsigned n) {
-                                A.first = A.item0 * groups + first;
-                                hipLaunchKernelGGL(k_group_coefficients, dim3(n), dim3(WIDE), 0, st, A, channel_sums, coefficients);
-                            });
-                        if (status != LEAP_OK) return status;
-                        if (!d_grad_x) continue;
-                        hipLaunchKernelGGL((k_group_grad<T, FULL, ACT>), dim3((unsigned)(now * each)), dim3(BLOCK), 0, st, A);
-                        if ((status = launched()) != LEAP_OK) return status;
+    if (L.at_once * each >= (int64_t)1 << 24) return refuse("more than 2^24 blocks of items");
+    // The sums of the items from `from` to `to`, which channel_sums holds, on the weight's gradient and the bias'.
+    const auto weights = [&](int64_t from, int64_t to) {
+        if (!d_grad_weight && !d_grad_bias) return (int)LEAP_OK;
+        return by_type(weight_type, [&](auto w) {
+            hipLaunchKernelGGL((k_group_weights<decltype(w)::value>), dim3((unsigned)((channels + BLOCK - 1) / BLOCK)), dim3(BLOCK), 0, st, channel_sums, to - from, (int)channels,
+                               from ? running : nullptr, some && to < items ? running : nullptr, d_grad_weight, d_grad_bias);
+            return launched();
+        });
+    };
+    if (!some) return weights(0, 0);
+    return by_type(type, [&](auto t) {
+        return by_activation(activation, [&](auto a) {
+            return by_full(A.deal, [&](auto full) -> int {
+                constexpr int T = decltype(t)::value, ACT = decltype(a)::value;
+                constexpr bool FULL = decltype(full)::value;
+                int64_t held = 0;                          // the first item that channel_sums holds
+                for (int64_t item = 0; item < items; item += L.at_once) {
+                    const int64_t now = items - item < L.at_once ? items - item : L.at_once;
+                    A.x.data = item_of(d_x, type, item, x_item), A.grad.data = item_of(d_grad, type, item, grad_item);
+                    A.stats = (float *)d_stats + item * groups * 2;
+                    hipLaunchKernelGGL((k_group_sums<T, FULL, ACT>), dim3((unsigned)(now * each)), dim3(BLOCK), 0, st, A);
+                    int status = launched();
+                    if (status == LEAP_OK)
+                        status = over_blocks(now * groups, [&](int64_t first, unsigned n) {
+                            A.first = first;
+                            hipLaunchKernelGGL(k_group_coefficients, dim3(n), dim3(WIDE), 0, st, A, channel_sums + (item - held) * channels * 2, coefficients);
+                        });
+                    if (status == LEAP_OK && (item + now - held >= L.held || item + now == items)) {
+                        status = weights(held, item + now);
+                        held = item + now;
                     }
-                    return LEAP_OK;
-                });
+                    if (status != LEAP_OK) return status;
+                    if (!d_grad_x) continue;
+                    A.out = (void *)item_of(d_grad_x, type, item, voxels * channels);
+                    hipLaunchKernelGGL((k_group_grad<T, FULL, ACT>), dim3((unsigned)(now * each)), dim3(BLOCK), 0, st, A);
+                    if ((status = launched()) != LEAP_OK) return status;
+                }
+                return LEAP_OK;
             });
         });
-    if (rc != LEAP_OK || !(d_grad_weight || d_grad_bias)) return rc;
-    return by_type(weight_type, [&](auto w) {
-        hipLaunchKernelGGL((k_group_weights<decltype(w)::value>), dim3((unsigned)((channels + BLOCK - 1) / BLOCK)), dim3(BLOCK), 0, st, channel_sums,
-                           some ? items : 0, (int)channels, d_grad_weight, d_grad_bias);
-        return launched();
     });
 }

@@ -253,3 +253,25 @@ def test_many_voxels(N):
         for at in (slice(0, 3), slice(voxels - 3, voxels), slice(1 << 25, (1 << 25) + 3)):
             want = (x[0, at, group * 11:group * 11 + 11].double() - mean) * rstd
             assert ((y[0, at, group * 11:group * 11 + 11].double() - want).abs() <= (R.HALF + 1e-5) * want.abs() + 1e-6).all()
+
+
+@pytest.mark.parametrize("shape,groups", [((100003, 1, 63), 7), ((70001, 2, 21), 1), ((150001, 3, 16), 2), ((20011, 9, 30), 3), ((33000, 64, 9), 1)])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_many_small_items(N, shape, groups, dtype):
+    """More than are worked on at once: the weight's and the bias' gradients are sums over all of them."""
+    x, w, b, g = inputs(shape, dtype, 141, F32)
+    check(run(N, x, groups, w, b, g, "silu"), R.GroupNorm(x, groups, w, b, "silu", 1e-5, g))
+
+
+def test_memory_of_a_norm_over_rows(N):
+    """2^20 rows of 63 channels, 132 MB: y, the gradient and a workspace of no more than four bytes a value and 48 MiB."""
+    x = torch.empty(1 << 20, 63, dtype=BF16, device="cuda").normal_(generator=torch.Generator(device="cuda").manual_seed(151)).requires_grad_(True)
+    w = torch.ones(63, device="cuda", requires_grad=True)
+    gc.collect()
+    torch.cuda.reset_peak_memory_stats()
+    before = torch.cuda.memory_allocated()
+    y = N.group_norm(x, 7, w)
+    got = torch.autograd.grad(y, (x, w), y.detach())
+    torch.cuda.synchronize()
+    assert torch.cuda.max_memory_allocated() - before <= 2 * x.numel() * 2 + (1 << 20) * 7 * 8 + 4 * x.numel() + (48 << 20) + (1 << 20)
+    assert all(torch.isfinite(t).all() for t in got)

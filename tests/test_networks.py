@@ -176,3 +176,17 @@ def test_what_is_kept_as_bytes_may_have_any_last_stride_where_rows_have_one_valu
         assert t.stride(-1) != 1
         assert torch.equal(N._bytes(t).view(dtype), t)
         assert N._bytes(t).data_ptr() == t.data_ptr()
+
+
+@pytest.mark.parametrize("channels", [1, 3, 7, 8, 20, 63, 64, 343, 2047, 2048])
+@pytest.mark.parametrize("voxels", [1, 2, 3, 8, 63, 64, 65, 4096])
+def test_the_workspace_of_group_norm_is_no_larger_than_its_arrays(lib, channels, voxels):
+    """Of a batch of any number of items: 2.5 bytes a value of x for the forward pass, four for the backward, and 48 MiB that a chip full of blocks takes for small arrays; it was up to
+    a hundred bytes a value."""
+    for items in (1, 5, 1 << 10, 1 << 14, 1 << 20):
+        if items * voxels * channels > 1 << 36 or items * channels > 1 << 31:
+            continue
+        for groups in {1, channels}:
+            values = items * voxels * channels
+            assert lib.leap_group_norm_work(items, voxels, channels, groups) <= (48 << 20) + 5 * values // 2, (items, groups)
+            assert lib.leap_group_norm_backward_work(items, voxels, channels, groups) <= (48 << 20) + 4 * values, (items, groups)
