@@ -50,7 +50,8 @@ __device__ inline float grad_dot_o(const u32x4 &g, const u32x4 &o, const u32x4 &
     return sum;
 }
 
-// delta by itself, where k_grad_query does not run: sixteen lanes a row.
+// delta by itself, where k_grad_query does not run: sixteen lanes a row.  Summed as there, so that the gradient of keys has the same bits whether that of queries is wanted or not: the
+// even pieces one after the other, the odd ones, then both.
 __global__ __launch_bounds__(BLOCK) void k_delta(grad_args G)
 {
     const attention_args &A = G.a;
@@ -60,9 +61,11 @@ __global__ __launch_bounds__(BLOCK) void k_delta(grad_args G)
     const int head = (int)(row % A.heads);
     const int64_t query = row / A.heads % A.queries, item = row / A.heads / A.queries;
     const u32x4 g = row_piece(G.grad.data + item * G.grad.item + query * G.grad.row + head * G.grad.head, A.width, lane);
-    float sum = grad_dot_o(g, row_piece(G.o + row * A.width, A.width, lane), row_piece(G.rest + row * A.width, A.width, lane));
+    const float piece = grad_dot_o(g, row_piece(G.o + row * A.width, A.width, lane), row_piece(G.rest + row * A.width, A.width, lane));
+    float sum = 0.0f;
 #pragma unroll
-    for (int d = 1; d < DELTA_LANES; d *= 2) sum += __shfl_xor(sum, d);
+    for (int s = 0; s < DELTA_LANES; s += 2) sum += __shfl(piece, s + lane % 2, DELTA_LANES);
+    sum += __shfl_xor(sum, 1);
     if (lane == 0) G.delta[(item * A.heads + head) * (int64_t)A.queries + query] = sum;
 }
 

@@ -554,3 +554,14 @@ def test_no_queries_and_a_table_that_wants_no_gradient(N, batch, queries, keys, 
             del room
             got = torch.autograd.grad(o, [t for t in leaves if t.requires_grad], torch.zeros_like(o))
             assert all(t.shape == w.shape and not t.any() for t, w in zip(got, wanted))
+
+
+@pytest.mark.parametrize("width", [8, 32, 49, 64, 96, 128])
+@pytest.mark.parametrize("seed", [151, 251])
+def test_the_gradient_of_keys_does_not_depend_on_what_else_is_wanted(N, width, seed):
+    """Its bits, of 17 million pairs: delta is one sum whichever kernel forms it, and a last bit of it that differs shows in one of 2^16 roundings of ds."""
+    q, k, v, g = (t.cuda() for t in inputs(4, 1024, 1024, 4, 4, width, seed))
+    every = run(N, q, k, v, g)
+    leaves = [t.detach().requires_grad_(i > 0) for i, t in enumerate((q, k, v))]
+    got = torch.autograd.grad(N.attention(*leaves), leaves[1:], g)
+    assert torch.equal(got[0], every[2]) and torch.equal(got[1], every[3])
