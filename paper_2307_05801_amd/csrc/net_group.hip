@@ -5,7 +5,7 @@
 // `positions` eights the channels begin anew, so that no length costs more than its values.
 //
 // Sums over a group are formed in three stages that depend on the sizes alone: a thread's values (means and squares about them, a piece of eight voxels exactly in two
-// passes over registers, pieces joined by their means), a block's threads, and in 64 bits the blocks of an item.  Memory bounds it all: x is read
+// passes over registers, pieces joined by their means; 512 voxels at most), a block's threads, and in 64 bits the blocks of an item.  Memory bounds it all: x is read
 // twice forward, x and the gradient twice backward.  So a few items (or one) at a time are read for their sums and, in the opposite order, again, before the next: the second time
 // part of them comes from the cache of 256 MB. An item of 2^21 voxels of 64 channels in bfloat16: moments 53 us (5.0 TB/s), activation 97 (5.5), sums 118 (4.5), gradient 161 (5.0).
 #include "../../include/leap_networks.h"
@@ -360,7 +360,7 @@ template <int TYPE, bool FULL, int ACTIVATION> __global__ __launch_bounds__(BLOC
             for (int i = 0; i < CHUNK; ++i) {
                 const float du = g[u][i] * slope<ACTIVATION>(K.argument(v[u][i], i));
                 if (N == 1 && i >= n) continue;
-                one[i] += du;                                  // (a thread has a few hundred voxels at most of the largest arrays)
+                one[i] += du;                                  // (MOST_PERIODS of them at most)
                 two[i] = __builtin_fmaf(du, v[u][i] - K.mean[i], two[i]);
             }
     });
@@ -494,6 +494,9 @@ template <int TYPE, bool FULL, int ACTIVATION> __global__ __launch_bounds__(BLOC
 
 int64_t divisor(int64_t a, int64_t b) { return b ? divisor(b, a % b) : a; }
 
+// Periods of a thread at most, since its sums are floats; it has that many of an item of 2^30 values dealt out to 1024 blocks, and larger items have more blocks.
+constexpr int64_t MOST_PERIODS = 512;
+
 // flat: rows of both arrays have no gaps.
 dealing dealing_of(int64_t items, int64_t voxels, int64_t channels, int64_t groups, bool flat)
 {
@@ -510,6 +513,8 @@ dealing dealing_of(int64_t items, int64_t voxels, int64_t channels, int64_t grou
     int64_t strips = 1024 / (items * D.segments > 0 ? items * D.segments : 1);
     const int64_t most = D.periods / (turns * 2 * PIECE);
     strips = strips < most ? strips : most;
+    const int64_t least = (D.periods + turns * MOST_PERIODS - 1) / (turns * MOST_PERIODS);
+    strips = strips < least ? least : strips;
     strips = strips < 1 ? 1 : strips;
     D.length = (D.periods + strips - 1) / strips;
     D.length = (D.length + turns - 1) / turns * turns;

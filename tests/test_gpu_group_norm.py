@@ -275,3 +275,18 @@ def test_memory_of_a_norm_over_rows(N):
     torch.cuda.synchronize()
     assert torch.cuda.max_memory_allocated() - before <= 2 * x.numel() * 2 + (1 << 20) * 7 * 8 + 4 * x.numel() + (48 << 20) + (1 << 20)
     assert all(torch.isfinite(t).all() for t in got)
+
+
+def test_sums_over_many_voxels(N):
+    """2^30 voxels, each with the slope of its channel's bias as du.  512 such numbers one after the other are off by up to half of 512 times 2^-24 of their sum, a block's threads by 8 steps
+    more and the slope itself by some (8 + |u|) units (networks_reference.py)."""
+    voxels, channels = 1 << 30, 8
+    x = torch.zeros(1, voxels, channels, dtype=BF16, device="cuda")
+    b = rand((channels,), 161)
+    w, bias = torch.ones(channels, device="cuda", requires_grad=True), b.cuda().requires_grad_(True)
+    y = N.group_norm(x, 1, w, bias, "silu")
+    assert torch.equal(y[0, 0], y[0, -1]) and torch.equal(y[0, 0], y[0, 1 << 29])
+    gw, gb = torch.autograd.grad(y, (w, bias), torch.ones_like(y))
+    want = voxels * R._slope(b.double(), "silu")
+    assert not gw.any()
+    assert ((gb.cpu().double() - want).abs() <= (256 + 8 + 16) * 2.0 ** -24 * want.abs()).all(), (gb.cpu().double() / want - 1)

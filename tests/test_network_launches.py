@@ -43,6 +43,21 @@ def test_items_of_group_norm_are_read_again_before_the_next():
     assert [launch.kernel for launch in many] == ["k_group_moments", "k_group_stats", "k_group_apply"]
 
 
+@pytest.mark.parametrize("voxels,channels,row", [(1 << 30, 8, None), (1 << 33, 8, None), (1 << 31, 64, None), (1 << 30, 63, None), (1 << 31, 20, 25), (1 << 22, 1 << 13, None), (1 << 20, 1 << 20, None)])
+def test_a_thread_of_group_norm_sums_no_more_than_512_values_of_a_channel(voxels, channels, row):
+    """As floats: however many there are.  A block has 256 threads, and as many of them have one channel as there is room for a period's eights."""
+    for call in (group(1, voxels, channels, 1, row=row), group_backward(1, voxels, channels, 1, row=row)):
+        (status, launches), = record([call])
+        assert status == B.LEAP_OK
+        rows = 1 if row else {0: 1, 1: 8, 2: 4, 3: 8, 4: 2, 5: 8, 6: 4, 7: 8}[channels % 8]
+        eights = -(-channels * rows // 8)
+        segments, turns = -(-eights // 256), max(1, 256 // eights)
+        for launch in launches:
+            if launch.kernel in ("k_group_moments", "k_group_apply", "k_group_sums", "k_group_grad"):
+                strips = launch.blocks[0] // segments
+                assert -(-voxels // rows) <= strips * turns * 512, launch
+
+
 def test_few_values_take_one_launch():
     small = [group(1, 256, 64, 8), group(1, 16384 // 8, 64, 8), group(1, 1, 16384, 1), group(64, 256, 64, 8, row=70)]
     large = [group(1, 16384 // 8 + 1, 64, 8), group(1, 256, 60, 8 - 2), group(65, 256, 64, 8), group(1, 2, 16384, 1)]
