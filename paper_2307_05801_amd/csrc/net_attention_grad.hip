@@ -83,23 +83,26 @@ template <int BUCKETS, int WINDOW> struct table_sums {
     float bucket[BUCKETS];
     int32_t upper[WINDOW], lower[WINDOW];
     uint16_t which[WINDOW];                                // the buckets of the window
-    float peak[WAVES];
+    uint32_t peak[WAVES];                                  // the largest ds of each wave's, its bits
 };
 template <int WINDOW> struct table_sums<0, WINDOW> {};
 
 // Shared memory's writes of all waves are there for all; what comes from memory is not waited for.
 __device__ inline void shared_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
-// The largest of a wave.
-__device__ inline float wave_max(float v)
+// The largest of a wave, of magnitudes as integers: what is not a number is larger than infinity there.
+constexpr uint32_t INFINITE = 0x7f800000u;
+__device__ inline uint32_t wave_max(uint32_t v)
 {
-    const auto with = [&](int other) { v = fmaxf(v, __int_as_float(other)); };
-    with(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0xb1, 0xf, 0xf, false));        // the neighbour, the other pair,
-    with(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x4e, 0xf, 0xf, false));
-    with(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x141, 0xf, 0xf, false));       // the other four of eight, the other eight of sixteen
-    with(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x140, 0xf, 0xf, false));
-    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    return column_max(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
+    const auto with = [&](int other) { v = (uint32_t)other > v ? (uint32_t)other : v; };
+    with(__builtin_amdgcn_update_dpp(0, (int)v, 0xb1, 0xf, 0xf, false));        // the neighbour, the other pair,
+    with(__builtin_amdgcn_update_dpp(0, (int)v, 0x4e, 0xf, 0xf, false));
+    with(__builtin_amdgcn_update_dpp(0, (int)v, 0x141, 0xf, 0xf, false));       // the other four of eight, the other eight of sixteen
+    with(__builtin_amdgcn_update_dpp(0, (int)v, 0x140, 0xf, 0xf, false));
+    const auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    v = a[0] > a[1] ? a[0] : a[1];
+    const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return b[0] > b[1] ? b[0] : b[1];
 }
 
 template <int DEEP, bool DIRECT, bool BIAS, int BUCKETS> __global__ __launch_bounds__(BLOCK, 2) void k_grad_query(grad_args G)
@@ -163,7 +166,6 @@ template <int DEEP, bool DIRECT, bool BIAS, int BUCKETS> __global__ __launch_bou
         uint8_t coming_apart = 0;
         int place = 0;
         float unscale = 0.0f;
-        const bool sound = __all(base == base && finite_magnitude(delta) | (delta == 0.0f));       // what is not a number in a query's pairs is in these
         const auto fetch = [&](int to) {
             lds_byte *const kt = lds + to * 2 * tile::BYTES;
             k.fetch(at.first, at.bits, kt, wave, lane);
@@ -190,7 +192,7 @@ template <int DEEP, bool DIRECT, bool BIAS, int BUCKETS> __global__ __launch_bou
                         const int bucket = sums.which[i];
                         if (bucket % WAVES != wave) continue;
                         const int upper = sums.upper[i], lower = sums.lower[i];
-                        if (!(upper | lower) && unscale == unscale) continue;              // a float's add takes the 3 cycles for every lane that makes one
+                        if (!(upper | lower)) continue;                                    // a float's add takes the 3 cycles for every lane that makes one
                         sums.upper[i] = sums.lower[i] = 0;
                         __hip_atomic_fetch_add(&sums.bucket[bucket], ((float)upper + (float)lower * 0x1p-24f) * unscale, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
                     }
@@ -257,19 +259,39 @@ template <int DEEP, bool DIRECT, bool BIAS, int BUCKETS> __global__ __launch_bou
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) largest = fmaxf(largest, fabsf(x[h][r]));
-                largest = sound ? wave_max(largest) : __builtin_nanf("");
-                if (lane == 0) sums.peak[wave] = largest;
-                shared_barrier();                          // and the sums before are settled
-                largest = 1e-30f;
-                float all = 0.0f;
+                    for (int r = 0; r < 16; ++r) largest = __builtin_elementwise_maximum(largest, fabsf(x[h][r]));
+                const auto of_block = [&] {                // and the sums before are settled
+                    const uint32_t mine = wave_max(__float_as_uint(largest));
+                    if (lane == 0) sums.peak[wave] = mine;
+                    shared_barrier();
+                    uint32_t most = __float_as_uint(1e-30f);
 #pragma unroll
-                for (int w = 0; w < WAVES; ++w) largest = fmaxf(largest, sums.peak[w]), all += sums.peak[w];
-                all = all == all ? largest : all;          // not a number: nor are the sums
+                    for (int w = 0; w < WAVES; ++w) most = sums.peak[w] > most ? sums.peak[w] : most;
+                    return (uint32_t)uniform((int)most);
+                };
+                uint32_t most = of_block();
+                if (most >= INFINITE) {                    // ds that are not finite go to the buckets of their pairs by themselves
+                    seldom();
+                    largest = 0.0f;
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) {
+                            const bool finite = (__float_as_uint(x[h][r]) & 0x7fffffffu) < INFINITE;
+                            if (!finite && there)
+                                __hip_atomic_fetch_add(&sums.bucket[A.line_buckets[line_at(A, places[turn][h * 32 + row_of(r) + lane / 32 * 4], position)]], x[h][r], __ATOMIC_RELAXED,
+                                                       __HIP_MEMORY_SCOPE_WORKGROUP);
+                            x[h][r] = finite ? x[h][r] : 0.0f;
+                            largest = fmaxf(largest, fabsf(x[h][r]));
+                        }
+                    shared_barrier();                      // all have read the peaks
+                    most = of_block();
+                }
+                largest = __uint_as_float(most);
                 if (near) {
                     fetch_window<2>(A.line_buckets, A.offsets, window, (lds_byte *)sums.which, wave, lane);
                     const float by = 0x1.fp23f / largest;
-                    unscale = all * (1.0f / 0x1.fp23f);
+                    unscale = largest * (1.0f / 0x1.fp23f);
                     const int to_sums = address_of((lds_byte *)sums.upper) + 4 * (A.offsets / 2 - window.first - position);
 #pragma unroll
                     for (int h = 0; h < 2; ++h)
@@ -281,7 +303,7 @@ template <int DEEP, bool DIRECT, bool BIAS, int BUCKETS> __global__ __launch_bou
                 } else {
                     constexpr int AT_ONCE = WINDOW;
                     const float by = 0x1.fp16f / largest;
-                    unscale = all * (1.0f / 0x1.fp16f);
+                    unscale = largest * (1.0f / 0x1.fp16f);
                     for (int first = 0; first < A.buckets; first += AT_ONCE) {
 #pragma unroll
                         for (int h = 0; h < 2; ++h)

@@ -565,3 +565,34 @@ def test_the_gradient_of_keys_does_not_depend_on_what_else_is_wanted(N, width, s
     leaves = [t.detach().requires_grad_(i > 0) for i, t in enumerate((q, k, v))]
     got = torch.autograd.grad(N.attention(*leaves), leaves[1:], g)
     assert torch.equal(got[0], every[2]) and torch.equal(got[1], every[3])
+
+
+@pytest.mark.parametrize("what", [float("nan"), float("inf")])
+@pytest.mark.parametrize("kind", ["apart", "alike", "anywhere", "anywhere many", "beyond"])
+@pytest.mark.parametrize("width", [32, 64, 128])
+def test_what_is_not_a_number_reaches_its_own_buckets(N, kind, what, width):
+    """A query or a gradient that is not finite: the table's gradient is not a number in the buckets of the query's pairs, in its head, and what it is without it in all others."""
+    n = 300
+    q, k, v, g = inputs(2, n, n, 2, 2, width, 251)
+    positions = None
+    if kind == "apart":
+        buckets = torch.arange(2 * n - 1, dtype=torch.int32)
+    elif kind == "alike":
+        buckets = torch.arange(2 * n - 1, dtype=torch.int32) // 3
+    elif kind == "beyond":
+        buckets = torch.arange(201, dtype=torch.int32)
+    else:
+        positions = torch.randperm(n, generator=torch.Generator().manual_seed(252)).to(torch.int32)
+        buckets = torch.arange(2 * n - 1, dtype=torch.int32) * (6 if "many" in kind else 1)
+    table = rand((2, int(buckets.max()) + 1), 253, F32)
+    (q if what != what else g)[1, 5 if kind == "beyond" else 130, 1, 3] = what       # (130 has pairs of all differences that are not beyond an end)
+    r = R.Attention(q, k, v, g, None, table, buckets, positions)
+    lost = ~torch.isfinite(r.grad_table)
+    assert lost[1].any() and not lost[1].all() and not lost[0].any()
+    got = run(N, q, k, v, g, table, None, buckets, positions)
+    assert torch.equal(~torch.isfinite(got[4].cpu()), lost)
+    assert_close(got[4].cpu()[~lost], r.grad_table[~lost], r.grad_table_off[~lost], "grad_table")
+    fine = torch.isfinite(r.grad_q).all(3)
+    assert int((~fine).sum()) == 1
+    assert torch.equal(torch.isfinite(got[1].cpu()).all(3), fine)
+    assert_close(got[1].cpu()[fine], r.grad_q[fine], r.grad_q_off[fine], "grad_q")
