@@ -258,24 +258,30 @@ template <int SIZE> __device__ inline void fetch_window(const void *line, int le
     for (int piece = wave; piece * (1024 / SIZE) < w.count; piece += WAVES) fetch16(from, (uint32_t)w.first * SIZE + piece * 1024 + lane * 16, to + piece * 1024);
 }
 
+// Where in shared memory a window's number is for a row at position 0: the window is at `to`, and the lane's position counts with the sign.  Modulo 2^32, as over_places
+// goes on: positions are up to 2^30, so four times one passes 31 bits, and the sum of both is in the window again.
+__device__ inline uint32_t origin_of(const lds_byte *to, const attention_args &A, const line_window &w, int position, bool added)
+{
+    return (uint32_t)(uintptr_t)to + 4u * ((uint32_t)(A.offsets / 2) - (uint32_t)w.first + (added ? (uint32_t)position : 0u - (uint32_t)position));
+}
+
 // f(r, p) for the sixteen pairs of a lane's position with the rows 8 a + 4 (lane / 32) + c of `places`: *p is the pair's number.  The rows are keys (SIGN 1) or queries
-// (-1).  at: the byte in shared memory of the number of a row at position 0.
-template <int SIGN, class T, class F> __device__ inline void over_places(const int *places, bool fours, int at, int lane, F &&f)
+// (-1).  at: origin_of.
+template <int SIGN, class T, class F> __device__ inline void over_places(const int *places, bool fours, uint32_t at, int lane, F &&f)
 {
     typedef __attribute__((address_space(3))) T *numbers;
     if (fours) {
 #pragma unroll
         for (int a = 0; a < 4; ++a) {
-            const numbers begin = (numbers)(uintptr_t)(uint32_t)(at + SIGN * 4 * (places[a * 8 + lane / 32 * 4] + (SIGN < 0 ? 3 : 0)));
+            const numbers begin = (numbers)(uintptr_t)(at + 4u * SIGN * ((uint32_t)places[a * 8 + lane / 32 * 4] + (SIGN < 0 ? 3 : 0)));
 #pragma unroll
             for (int c = 0; c < 4; ++c) f(a * 4 + c, begin + (SIGN < 0 ? 3 - c : c));
         }
     } else {
 #pragma unroll
-        for (int r = 0; r < 16; ++r) f(r, (numbers)(uintptr_t)(uint32_t)(at + SIGN * 4 * places[row_of(r) + lane / 32 * 4]));
+        for (int r = 0; r < 16; ++r) f(r, (numbers)(uintptr_t)(at + 4u * SIGN * (uint32_t)places[row_of(r) + lane / 32 * 4]));
     }
 }
-__device__ inline int address_of(const lds_byte *p) { return (int)(uint32_t)(uintptr_t)p; }
 
 __device__ inline bf16x8 eight(const f32x16 &v, int m)
 {

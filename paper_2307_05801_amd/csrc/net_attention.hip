@@ -116,7 +116,7 @@ template <int DEEP, bool DIRECT, bool BIAS, bool FINE> __global__ __launch_bound
             for (int s = 0; s < STEPS; ++s) x[h] = product(tile::along(kt, h * 32, s, lane), q[s], x[h]);
         }
         if constexpr (BIAS) {
-            const int from = address_of(lds + 4 * tile::BYTES + turn * WINDOW * 4) + 4 * (A.offsets / 2 - window.first - position);
+            const uint32_t from = origin_of(lds + 4 * tile::BYTES + turn * WINDOW * 4, A, window, position, false);
 #pragma unroll
             for (int h = 0; h < 2; ++h)
                 if (window.inside)

@@ -215,7 +215,7 @@ template <int DEEP, bool DIRECT, bool BIAS, int BUCKETS> __global__ __launch_bou
             at.next(lane);
             if (!at.done()) fetch(turn ^ 1);
             settle();
-            const int from_line = address_of(lds + 4 * tile::BYTES + turn * WINDOW * 4) + 4 * (A.offsets / 2 - window.first - position);
+            const uint32_t from_line = origin_of(lds + 4 * tile::BYTES + turn * WINDOW * 4, A, window, position, false);
             f32x16 x[2];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
@@ -292,7 +292,7 @@ template <int DEEP, bool DIRECT, bool BIAS, int BUCKETS> __global__ __launch_bou
                     fetch_window<2>(A.line_buckets, A.offsets, window, (lds_byte *)sums.which, wave, lane);
                     const float by = 0x1.fp23f / largest;
                     unscale = largest * (1.0f / 0x1.fp23f);
-                    const int to_sums = address_of((lds_byte *)sums.upper) + 4 * (A.offsets / 2 - window.first - position);
+                    const uint32_t to_sums = origin_of((lds_byte *)sums.upper, A, window, position, false);
 #pragma unroll
                     for (int h = 0; h < 2; ++h)
                         over_places<1, int>(places[turn] + h * 32, fours, to_sums, lane, [&](int r, auto sum_of) {
@@ -428,7 +428,7 @@ template <int DEEP, bool DIRECT, bool BIAS> __global__ __launch_bounds__(BLOCK, 
                 if constexpr (DIRECT || BIAS) fetched();
                 __syncthreads();
                 if (at + 1 < tiles) fetch(at + 1, turn ^ 1);
-                const int from_line = address_of(lds + 4 * tile::BYTES + turn * WINDOW * 4) + 4 * (A.offsets / 2 - window.first + position);
+                const uint32_t from_line = origin_of(lds + 4 * tile::BYTES + turn * WINDOW * 4, A, window, position, true);
                 // Half a tile's scores and dp are multiplied while the other half's probabilities are formed: x[h] becomes p, dp[h] ds.
                 f32x16 x[2], dp[2];
                 const auto scores = [&](int h) {

@@ -596,3 +596,18 @@ def test_what_is_not_a_number_reaches_its_own_buckets(N, kind, what, width):
     assert int((~fine).sum()) == 1
     assert torch.equal(torch.isfinite(got[1].cpu()).all(3), fine)
     assert_close(got[1].cpu()[fine], r.grad_q[fine], r.grad_q_off[fine], "grad_q")
+
+
+@pytest.mark.parametrize("end", [-(1 << 30), 1 << 30, -(1 << 29) - 150, (1 << 29) - 150])
+@pytest.mark.parametrize("order", ["one after the other", "rising", "any"])
+@pytest.mark.parametrize("width", [32, 128])
+def test_positions_near_their_ends(N, end, order, width):
+    """Up to 2^30 either way, side by side so that a tile's differences are read from shared memory: four times a position passes 31 bits, the address does not."""
+    n = 300
+    t = inputs(2, n, n, 2, 1, width, 261)
+    step = {"one after the other": torch.arange(n), "rising": torch.arange(n) // 3 * 4 + torch.arange(n) % 3, "any": torch.randperm(n, generator=torch.Generator().manual_seed(262))}[order]
+    places_ = (end + step - (int(step.max()) if end == 1 << 30 else 0)).to(torch.int32)
+    assert -(1 << 30) <= int(places_.min()) and int(places_.max()) <= 1 << 30
+    buckets = torch.arange(2 * int(step.max()) + 1, dtype=torch.int32)
+    table = rand((2, len(buckets)), 263, F32)
+    check(run(N, *t, table, None, buckets, places_), R.Attention(*t, None, table, buckets, places_))
