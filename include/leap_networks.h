@@ -44,6 +44,7 @@ typedef struct {
 } leap_attention_desc;
 
 enum { LEAP_ATTENTION_WIDEST = 128, LEAP_ATTENTION_BUCKETS = 4096 };                   /* the largest width, the most buckets */
+enum { LEAP_ATTENTION_OFFSETS = 1 << 24 };                                             /* the most differences; 2^30 for all heads together */
 
 /* o [batch][queries][heads][width] <- attention.  For a backward pass also stats [batch][heads][queries][2] (float: a number m within 8 of the largest exponent of
  * a query's keys, and the logarithm of the sum of what is left of them, x - m, both to the base 2) and rest [as o] (int16: what has to be added to o's bits, followed by 16 zeros, for those of

@@ -58,7 +58,7 @@ ACTIVATION_EXPORTS = {                                       # name: (result, ar
     "leap_feed_forward8_backward_fine": (C.c_int, [_P, _L, _P, _L, _P, _I, _L, _L, _P, _L, _L, _P, _L, _L] + [_P] * 7),
 }
 
-LEAP_ATTENTION_WIDEST, LEAP_ATTENTION_BUCKETS = 128, 4096    # limits of include/leap_networks.h, and its activations
+LEAP_ATTENTION_WIDEST, LEAP_ATTENTION_BUCKETS, LEAP_ATTENTION_OFFSETS = 128, 4096, 1 << 24    # limits of include/leap_networks.h, and its activations
 LEAP_LINEAR, LEAP_RELU, LEAP_SILU = 0, 1, 2
 NETWORK_EXPORTS = {                                          # a description's bytes go as a pointer
     "leap_attention_work": (_L, [_P]),

@@ -357,7 +357,7 @@ const char *bad_attention(const leap_attention_desc *d)
     if (d->d_table) {
         if (!known_type(d->table_type)) return "unknown element type";
         if (d->buckets < 1 || d->buckets > LEAP_ATTENTION_BUCKETS) return "1 to 4096 buckets";
-        if (!d->d_bucket_of || d->offsets < 1 || d->offsets > (int64_t)1 << 24 || d->offsets * d->heads > most) return "the table needs the buckets of 1 to 2^24 differences, 2^30 for all heads";
+        if (!d->d_bucket_of || d->offsets < 1 || d->offsets > LEAP_ATTENTION_OFFSETS || d->offsets * d->heads > most) return "the table needs the buckets of 1 to 2^24 differences, 2^30 for all heads";
         if (d->heads >= 65535) return "more than 65534 heads with a table";
     }
     return nullptr;

@@ -133,7 +133,7 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, mask: torch.Ten
 
     table: a learned number [heads, buckets] (float32, bfloat16, float16; at most 4096 buckets) for every head and bucket of relative positions, added to the scaled
     product.  positions: int32 [rows] of queries and keys alike, or a pair of them (None: 0, 1, 2, ...), within +-2^30; buckets: int32 [n], the bucket of
-    key's position - query's position at index n // 2 + that; differences beyond its ends take the ends'.  relative_buckets makes both for a grid of
+    key's position - query's position at index n // 2 + that, n at most 2^24 and 2^30 / heads; differences beyond its ends take the ends'.  relative_buckets makes both for a grid of
     patches.  -inf in the table leaves pairs out.
 
     Scores, the softmax and sums are 32 bits; probabilities and the gradients of scores are rounded to bfloat16 for the products that sum over them, but for
@@ -188,13 +188,15 @@ def relative_buckets(shape, near: int, codes: int, device="cuda:0"):
     """(positions, buckets), int32, for attention over the patches of a grid, in the order of its memory: shape (n,), (ny, nx), (nz, ny, nx).
 
     On an axis a distance d below `near` has the code d, those from near on one more for each doubling (near .. 2 near - 1: near, then near + 1, ...), and
-    `codes` - 1 is the last; the two directions differ.  A bucket counts the axes' codes through, the last axis fastest: (2 codes - 1) ** axes in all."""
+    `codes` - 1 is the last; the two directions differ.  A bucket counts the axes' codes through, the last axis fastest: (2 codes - 1) ** axes in all.  At most 4096
+    buckets and 2^24 differences ((2 nz - 1) (2 ny - 1) (2 nx - 1)), which is what attention takes."""
     sizes = tuple(int(n) for n in shape)
     if not sizes or any(n < 1 for n in sizes) or not 1 <= near <= codes:
         raise ValueError("a grid has axes of at least one patch, and 1 <= near <= codes")
     many = 2 * codes - 1
-    if many ** len(sizes) > B.LEAP_ATTENTION_BUCKETS or math.prod(2 * n - 1 for n in sizes) > 1 << 30:
-        raise ValueError(f"at most {B.LEAP_ATTENTION_BUCKETS} buckets and 2^30 differences, got {many ** len(sizes)} and {math.prod(2 * n - 1 for n in sizes)}")
+    if many ** len(sizes) > B.LEAP_ATTENTION_BUCKETS or math.prod(2 * n - 1 for n in sizes) > B.LEAP_ATTENTION_OFFSETS:
+        raise ValueError(f"at most {B.LEAP_ATTENTION_BUCKETS} buckets and {B.LEAP_ATTENTION_OFFSETS} differences, got {many ** len(sizes)} and "
+                         f"{math.prod(2 * n - 1 for n in sizes)}")
     positions, buckets = torch.zeros(1, dtype=torch.int32), torch.zeros(1, dtype=torch.int32)
     for n in sizes:
         code = [min(d if d < near else near + (d // near).bit_length() - 1, codes - 1) for d in range(n)]

@@ -190,3 +190,20 @@ def test_the_workspace_of_group_norm_is_no_larger_than_its_arrays(lib, channels,
             values = items * voxels * channels
             assert lib.leap_group_norm_work(items, voxels, channels, groups) <= (48 << 20) + 5 * values // 2, (items, groups)
             assert lib.leap_group_norm_backward_work(items, voxels, channels, groups) <= (48 << 20) + 4 * values, (items, groups)
+
+
+@pytest.mark.parametrize("shape", [((1 << 23) + 1,), (2049, 2049), (129, 129, 129), (1, 4097, 1025)])
+def test_grids_of_more_differences_than_attention_takes_are_refused(lib, shape):
+    with pytest.raises(ValueError, match="differences"):
+        N.relative_buckets(shape, 1, 2, device="cpu")
+    header = open(os.path.join(ROOT, "include", "leap_networks.h")).read()
+    assert B.LEAP_ATTENTION_OFFSETS == 1 << 24 and "LEAP_ATTENTION_OFFSETS = 1 << 24" in header
+    for offsets, status in ((1 << 24, False), ((1 << 24) + 1, True)):
+        d = list(GOOD)
+        d[16] = offsets
+        assert (lib.leap_attention_work(N._DESC.pack(*d)) == 0) is status
+
+
+def test_the_largest_grid_is_taken():
+    positions, buckets = N.relative_buckets((1 << 23,), 1, 2, device="cpu")
+    assert len(positions) == 1 << 23 and len(buckets) == (1 << 24) - 1
