@@ -20,6 +20,7 @@ As with any operator, do not capture a backward pass into a graph while an eager
 from __future__ import annotations
 
 import torch
+from torch.autograd import forward_ad
 
 from . import binding as B
 from .projector import _current_stream
@@ -99,13 +100,21 @@ class FineGradient:
         return f"FineGradient(shape={tuple(self.shape)}, device={self.device})"
 
 
-def _not_recorded(*tensors) -> None:
-    """The results have no graph: silently without one they would train with a part of the gradient."""
+def _records(*tensors) -> bool:
+    """Whether autograd wants something of what is made of the tensors: a graph, or a tangent (forward mode), which an autograd.Function refuses and which would be
+    dropped silently without one."""
     if torch.is_grad_enabled():
         for t in tensors:
             if t is not None and t.requires_grad:
-                raise ValueError("this operator records no gradient, and an argument requires one: use feed_forward8, call it within torch.no_grad() or an "
-                                 "autograd.Function (with the *_backward operators), or hand it .detach()ed tensors")
+                return True
+    return forward_ad._current_level >= 0 and any(t is not None and forward_ad.unpack_dual(t).tangent is not None for t in tensors)
+
+
+def _not_recorded(*tensors) -> None:
+    """The results have no graph: silently without one they would train with a part of the gradient."""
+    if _records(*tensors):
+        raise ValueError("this operator records no gradient, and an argument requires one: use feed_forward8, call it within torch.no_grad() or an "
+                         "autograd.Function (with the *_backward operators), or hand it .detach()ed tensors")
 
 
 def _type_of(t: torch.Tensor, what: str) -> int:
@@ -561,7 +570,7 @@ def feed_forward8(x: torch.Tensor, norm_weight: torch.Tensor, up: torch.Tensor, 
     if x.dtype is not torch.bfloat16:
         raise ValueError(f"x must be bfloat16, not {x.dtype}")
     tensors = (x, residual, norm_weight, up, down)
-    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):
+    if _records(*tensors):
         return _FeedForward8.apply(*tensors, eps, fine)
     return _block_forward(*tensors, eps, False)[:2]
 

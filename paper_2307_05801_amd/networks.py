@@ -8,7 +8,7 @@ its blocks, or keeps voxels with their channels last:
     y = group_norm(x, 8, weight, bias, activation="silu")                            # x: [batch, nz, ny, nx, channels]
     norm = GroupNorm(8, 64, activation="silu"); y = norm(x)                          # the same as a module
 
-Both are differentiable, run in libleap_hip.so on the current HIP stream, and take memory from PyTorch alone.  Tensors are on one GPU; the values of
+Both are differentiable (backward; in forward mode they raise), run in libleap_hip.so on the current HIP stream, and take memory from PyTorch alone.  Tensors are on one GPU; the values of
 a row (the last dimension) are neighbours (else ValueError: `.contiguous()` them).  The same call gives the same bits.
 As with any operator, do not capture a backward pass into a graph while an eager graph of the same leaves is alive.
 """
@@ -20,7 +20,7 @@ import struct
 import torch
 
 from . import binding as B
-from .activations import _TYPES, _address, _call, _on_gpu
+from .activations import _TYPES, _address, _call, _on_gpu, _records
 
 BF16 = torch.bfloat16
 
@@ -179,7 +179,7 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, mask: torch.Ten
     scale = width ** -0.5 if scale is None else float(scale)
     if not 0.0 < scale < 1e30:
         raise ValueError(f"scale must be positive, got {scale}")
-    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (q, k, v, table)):
+    if _records(q, k, v, table):
         return _Attention.apply(q, k, v, table, mask, buckets, positions, scale)
     return _attend(q, k, v, mask, table, buckets, positions, scale, False)[0]
 
@@ -307,7 +307,7 @@ def group_norm(x: torch.Tensor, groups: int, weight: torch.Tensor = None, bias: 
     _norm_parameter(bias, x, "bias")
     if weight is not None and bias is not None and weight.dtype is not bias.dtype:
         raise ValueError(f"weight and bias must be of one type, got {weight.dtype} and {bias.dtype}")
-    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (x, weight, bias)):
+    if _records(x, weight, bias):
         return _GroupNorm.apply(x, weight, bias, groups, _ACTIVATIONS[activation], eps)
     return _norm_forward(x, groups, weight, bias, _ACTIVATIONS[activation], eps, False)[0]
 

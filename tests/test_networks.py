@@ -207,3 +207,21 @@ def test_grids_of_more_differences_than_attention_takes_are_refused(lib, shape):
 def test_the_largest_grid_is_taken():
     positions, buckets = N.relative_buckets((1 << 23,), 1, 2, device="cpu")
     assert len(positions) == 1 << 23 and len(buckets) == (1 << 24) - 1
+
+
+def test_a_tangent_is_not_dropped():
+    """Forward mode: a dual tensor requires no gradient, but an operator that went by that alone would lose its tangent."""
+    from torch.autograd import forward_ad
+    from paper_2307_05801_amd import activations as A
+    x, leaf = torch.ones(3), torch.ones(3, requires_grad=True)
+    assert not A._records(x, None) and A._records(x, leaf, None)
+    with torch.no_grad():
+        assert not A._records(x, leaf)
+    with forward_ad.dual_level():
+        dual = forward_ad.make_dual(x, torch.ones(3))
+        assert not dual.requires_grad and A._records(x, None, dual) and not A._records(x)
+        with torch.no_grad():
+            assert A._records(dual) and not A._records(x, leaf)
+        with pytest.raises(ValueError):
+            A._not_recorded(dual)
+    assert not A._records(x)
