@@ -147,14 +147,15 @@ _activations = None
 
 
 def load_activations():
-    """The library with the prototypes of include/leap_activations.h and include/leap_networks.h (apart from load_library: another
-    build of the library, under LEAP_LIB_PATH, need not have them)."""
+    """The library with the prototypes of include/leap_activations.h, and of include/leap_networks.h if it has those (apart from load_library: another
+    build of the library, under LEAP_LIB_PATH, need not have either; a call of what it lacks raises AttributeError)."""
     global _activations
     if _activations is None:
         lib = load_library()
         for name, (result, arguments) in (ACTIVATION_EXPORTS | NETWORK_EXPORTS).items():
-            fn = getattr(lib, name)
-            fn.restype, fn.argtypes = result, arguments
+            fn = getattr(lib, name) if name in ACTIVATION_EXPORTS else getattr(lib, name, None)
+            if fn is not None:
+                fn.restype, fn.argtypes = result, arguments
         _activations = lib
     return _activations
 

@@ -225,3 +225,24 @@ def test_a_tangent_is_not_dropped():
         with pytest.raises(ValueError):
             A._not_recorded(dual)
     assert not A._records(x)
+
+
+def test_a_library_with_the_operators_in_8_bits_alone_is_taken(monkeypatch):
+    """Another build under LEAP_LIB_PATH; what it lacks raises when it is called, and not before."""
+    class Function:
+        pass
+
+    class Library:
+        def __init__(self, names):
+            self.__dict__.update({name: Function() for name in names})
+
+    monkeypatch.setattr(B, "_activations", None)
+    monkeypatch.setattr(B, "load_library", lambda: Library(B.ACTIVATION_EXPORTS))
+    lib = B.load_activations()
+    assert lib.leap_pack8.argtypes == B.ACTIVATION_EXPORTS["leap_pack8"][1]
+    with pytest.raises(AttributeError):
+        lib.leap_attention
+    monkeypatch.setattr(B, "_activations", None)
+    monkeypatch.setattr(B, "load_library", lambda: Library(()))
+    with pytest.raises(AttributeError):
+        B.load_activations()
