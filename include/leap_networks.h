@@ -67,7 +67,8 @@ int leap_attention_backward(const leap_attention_desc *desc, const void *d_grad,
  * item.  With its mean and rstd = 1 / sqrt(variance + eps) over voxels and channels:  u = (x - mean) * rstd * weight + bias,  y = activation(u).
  * weight, bias: [channels] of weight_type (`type` or float32), or NULL (ones, zeros); y: as x, without gaps.
  * x_item, x_row: distances of items and of voxels.  stats [items][groups][2] (float: mean, rstd) for the backward pass, or NULL.
- * d_work: leap_group_norm_work() bytes, NULL where that is 0.  The sums are formed such that a mean far larger than the deviation costs nothing. */
+ * d_work: leap_group_norm_work() bytes, NULL where that is 0.  The sums are formed such that a mean far larger than the deviation costs nothing;
+ * a voxel's deviation from the mean is at most 2^55, so that 32 bits hold the sums of their squares, and eight of x have a sum that is finite. */
 enum { LEAP_LINEAR = 0, LEAP_RELU = 1, LEAP_SILU = 2 };
 int64_t leap_group_norm_work(int64_t items, int64_t voxels, int64_t channels, int64_t groups);
 int leap_group_norm(const void *d_x, int32_t type, int64_t x_item, int64_t x_row, const void *d_weight, const void *d_bias, int32_t weight_type, int64_t items,

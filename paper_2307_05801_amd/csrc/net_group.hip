@@ -116,9 +116,9 @@ struct moments {
     {
         const float all = n + o.n;
         if (o.n == 0.0f) return;
-        const float share = o.n / all, d = o.mean - mean;
+        const float share = o.n / all, d = o.mean - mean, far = n > 0.0f ? d * d : 0.0f;       // (the first values' square may be beyond what a float holds)
         mean += d * share;
-        square += o.square + d * d * (n * share);
+        square += o.square + far * (n * share);
         n = all;
     }
 };
@@ -146,9 +146,9 @@ template <int TYPE, bool FULL> __global__ __launch_bounds__(BLOCK, 4) void k_gro
             m *= 1.0f / PIECE;
 #pragma unroll
             for (int u = 0; u < PIECE; ++u) s += (v[u][i] - m) * (v[u][i] - m);
-            const float d = m - mean[i];
+            const float d = m - mean[i], far = n > 0.0f ? d * d : 0.0f;
             mean[i] += d * share;
-            square[i] += s + d * d * weight;
+            square[i] += s + far * weight;
         }
         n = all;
     }

@@ -290,3 +290,22 @@ def test_sums_over_many_voxels(N):
     want = voxels * R._slope(b.double(), "silu")
     assert not gw.any()
     assert ((gb.cpu().double() - want).abs() <= (256 + 8 + 16) * 2.0 ** -24 * want.abs()).all(), (gb.cpu().double() / want - 1)
+
+
+@pytest.mark.parametrize("shape,groups", [((2, 3000, 20), 4), ((1, 5, 7), 7), ((2, 2048, 64), 8), ((1, 40000, 24), 3)])
+@pytest.mark.parametrize("size", [1e20, -1e25, 1e37])
+def test_a_mean_whose_square_is_beyond_32_bits(N, shape, groups, size):
+    """All values alike, so the bias comes out; and, to 2^55, values about the mean: those are held exactly, at most two units of 2^-24 of the largest apart."""
+    x, w, b, g = inputs(shape, F32, 171)
+    flat = torch.full(shape, size)
+    y, gx, gw, gb = run(N, flat, groups, w, b, g, "silu")
+    assert_close(y, torch.nn.functional.silu(b.double()).expand(shape), 16 * 2.0 ** -24 * b.abs().double().expand(shape))
+    assert all(torch.isfinite(t).all() for t in (gx, gw, gb))
+    if size == 1e20:
+        near = (flat.view(torch.int32) + torch.randint(-2, 3, shape, generator=torch.Generator().manual_seed(172), dtype=torch.int32)).view(F32)
+        assert (near.double() - size).abs().max() < 2.0 ** 55
+        y = N.group_norm(near.cuda(), groups)
+        assert torch.isfinite(y).all()
+        r = R.GroupNorm(near, groups)
+        # the mean, of 32 bits, is off by half a unit of the largest and by what joining adds: as far as values are apart, so y is off by some times one
+        assert (y.cpu().double() - r.y).abs().max() <= 4.0
