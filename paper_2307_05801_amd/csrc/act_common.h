@@ -210,13 +210,23 @@ __device__ inline float rest_of_bf16(float v)
 
 // 1 / (1 + exp(-g)), off by 2 units of 2^-24 of its value where g >= 0 and by up to 3 + |g| below (6 at -4, 10 at -8, 31 at -30, 66 at -87; exact
 // exponential and reciprocal assumed): the product with the constant rounds, and exp(-g) is the square of exp(-g / 2).  Taking
-// along what the product's rounding leaves would hold it at 5 throughout, in ten instructions instead of six; the results go to codes of 2^-4, to
-// bfloat16, or to two of those, 2^-17.  A square, because an exponent that carries an offset would lose what the offset's size rounds away.  Its 2^-32nd part does not
+// along what the product's rounding leaves holds it at 5 throughout (fine_sigmoid, for results of 32 bits) in eleven instructions instead of six; the results here go to codes of 2^-4, to
+// 16 bits, or to two bfloat16, 2^-17.  A square, because an exponent that carries an offset would lose what the offset's size rounds away.  Its 2^-32nd part does not
 // overflow before the result is zero, and the reciprocal of that, which the hardware forms within a unit but not as a subnormal number, is
 // brought back by a product.
 __device__ inline float sigmoid(float g)
 {
     const float root = __builtin_amdgcn_exp2f(g * -0.72134752f);
+    return __builtin_amdgcn_rcpf(__builtin_fmaf(root * 0x1p-32f, root, 0x1p-32f)) * 0x1p-32f;
+}
+
+// The same with what the exponent's rounding leaves, and what its constant, half of log2(e), has beyond 24 bits.
+__device__ inline float fine_sigmoid(float g)
+{
+    constexpr float HALF_LOG2E = 0x1.715476p-1f, BEYOND = 0x1.4ae0cp-27f, LN2 = 0.69314718f;
+    const float half = g * -HALF_LOG2E, rest = __builtin_fmaf(g, -BEYOND, __builtin_fmaf(g, -HALF_LOG2E, -half));
+    float root = __builtin_amdgcn_exp2f(half);
+    root = fabsf(half) < 128.0f ? __builtin_fmaf(root * LN2, rest, root) : root;       // (beyond, the result is 0 or 1, and what is infinite has no rest)
     return __builtin_amdgcn_rcpf(__builtin_fmaf(root * 0x1p-32f, root, 0x1p-32f)) * 0x1p-32f;
 }
 

@@ -244,11 +244,12 @@ struct known {
     __device__ inline float argument(float v, int i) const { return __builtin_fmaf(v - mean[i], by[i], bias[i]); }
 };
 
-template <int ACTIVATION> __device__ inline float activated(float u) { return ACTIVATION == LEAP_SILU ? u * sigmoid(u) : ACTIVATION == LEAP_RELU ? (u < 0.0f ? 0.0f : u) : u; }
-template <int ACTIVATION> __device__ inline float slope(float u)
+template <int TYPE> __device__ inline float gate(float u) { return TYPE == LEAP_F32 ? fine_sigmoid(u) : sigmoid(u); }
+template <int TYPE, int ACTIVATION> __device__ inline float activated(float u) { return ACTIVATION == LEAP_SILU ? u * gate<TYPE>(u) : ACTIVATION == LEAP_RELU ? (u < 0.0f ? 0.0f : u) : u; }
+template <int TYPE, int ACTIVATION> __device__ inline float slope(float u)
 {
     if (ACTIVATION == LEAP_SILU) {
-        const float s = sigmoid(u);
+        const float s = gate<TYPE>(u);
         return s * __builtin_fmaf(u, 1.0f - s, 1.0f);
     }
     return ACTIVATION == LEAP_RELU && !(u > 0.0f) ? 0.0f : 1.0f;
@@ -272,7 +273,7 @@ template <int TYPE, bool FULL, int ACTIVATION> __global__ __launch_bounds__(BLOC
         for (int u = 0; u < N; ++u) {
             float o[CHUNK];
 #pragma unroll
-            for (int i = 0; i < CHUNK; ++i) o[i] = activated<ACTIVATION>(K.argument(v[u][i], i));
+            for (int i = 0; i < CHUNK; ++i) o[i] = activated<TYPE, ACTIVATION>(K.argument(v[u][i], i));
             store8<TYPE>(y, (p + u * P.turns) * out, FULL && N != 1 ? CHUNK : n, o, A.past);
         }
     });
@@ -330,7 +331,7 @@ template <int TYPE, int ACTIVATION> __global__ __launch_bounds__(BLOCK) void k_g
 #pragma unroll
         for (int i = 0; i < CHUNK; ++i) {
             const float by = rstd * (A.weight ? value_at(A.weight, A.weight_type, c + i) : 1.0f), bias = A.bias ? value_at(A.bias, A.weight_type, c + i) : 0.0f;
-            o[i] = activated<ACTIVATION>(__builtin_fmaf(v[j][i] - mean, by, bias));         // as known::argument has it
+            o[i] = activated<TYPE, ACTIVATION>(__builtin_fmaf(v[j][i] - mean, by, bias));         // as known::argument has it
         }
         store8<TYPE>(y, (int64_t)(id / each) * D.channels + id % each * CHUNK, CHUNK, o);
     }
@@ -358,7 +359,7 @@ template <int TYPE, bool FULL, int ACTIVATION> __global__ __launch_bounds__(BLOC
         for (int u = 0; u < N; ++u)
 #pragma unroll
             for (int i = 0; i < CHUNK; ++i) {
-                const float du = g[u][i] * slope<ACTIVATION>(K.argument(v[u][i], i));
+                const float du = g[u][i] * slope<TYPE, ACTIVATION>(K.argument(v[u][i], i));
                 if (N == 1 && i >= n) continue;
                 one[i] += du;                                  // (MOST_PERIODS of them at most)
                 two[i] = __builtin_fmaf(du, v[u][i] - K.mean[i], two[i]);
@@ -484,7 +485,7 @@ template <int TYPE, bool FULL, int ACTIVATION> __global__ __launch_bounds__(BLOC
             float o[CHUNK];
 #pragma unroll
             for (int i = 0; i < CHUNK; ++i)
-                o[i] = g[u][i] * slope<ACTIVATION>(K.argument(v[u][i], i)) * K.by[i] - one[i] - (v[u][i] - K.mean[i]) * two[i];
+                o[i] = g[u][i] * slope<TYPE, ACTIVATION>(K.argument(v[u][i], i)) * K.by[i] - one[i] - (v[u][i] - K.mean[i]) * two[i];
             store8<TYPE>(to, (p + u * P.turns) * out, FULL && N != 1 ? CHUNK : n, o, A.past);
         }
     });

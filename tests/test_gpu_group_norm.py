@@ -309,3 +309,31 @@ def test_a_mean_whose_square_is_beyond_32_bits(N, shape, groups, size):
         r = R.GroupNorm(near, groups)
         # the mean, of 32 bits, is off by half a unit of the largest and by what joining adds: as far as values are apart, so y is off by some times one
         assert (y.cpu().double() - r.y).abs().max() <= 4.0
+
+
+@pytest.mark.parametrize("voxels,groups", [(8, 1), (8, 2), (5000, 1)])
+def test_silu_to_32_bits(N, voxels, groups):
+    """Values all alike, so u is the bias, from -87 to 30.  Of float32 the sigmoid is off by 5 units of 2^-24 (by half of them where u is positive), two more for each of its exponential's two
+    factors and of its reciprocal, the product by one; with gradients of powers of two the sums of a channel are products and, of eight, three roundings.  slope = s (1 + u (1 - s))."""
+    channels, unit = 2050 if groups == 2 else 2048, 2.0 ** -24
+    b = torch.linspace(-87, 30, channels)
+    x = torch.full((1, voxels, channels), 3.25)
+    leaves = [t.cuda().requires_grad_(True) for t in (x, torch.ones(channels), b)]
+    y = N.group_norm(leaves[0], groups, *leaves[1:], "silu")
+    s = torch.sigmoid(b.double())
+    want = b.double() * s
+    assert ((y[0].detach().cpu().double() - want).abs() <= 12 * unit * want.abs() + 2.0 ** -148).all()
+    grad = torch.zeros(x.shape)
+    grad[:, :8] = 1.0
+    got, = torch.autograd.grad(y, leaves[2], grad.cuda())
+    slope = s * (1 + b.double() * (1 - s))
+    off = 11 * slope.abs() + s * (b.abs().double() * (11 * s + 1) + 1) + 4 * slope.abs()
+    assert ((got.cpu().double() - 8 * slope).abs() <= 8 * (unit * off + 2.0 ** -148)).all()
+
+
+def test_silu_of_what_is_far_off(N):
+    """Beyond what the exponential holds: zeros on one side, the number itself on the other, infinity included."""
+    b = torch.tensor([-1e4, -1e30, -torch.finfo(BF16).max, 1e4, 1e30, torch.finfo(BF16).max, torch.inf, 0.0])       # (float32's largest is infinite in bfloat16)
+    for dtype in (F32, BF16):
+        y = N.group_norm(torch.zeros(1, 4, 8, dtype=dtype, device="cuda"), 1, None, b.to(dtype).cuda(), "silu").cpu()
+        assert torch.equal(y, torch.where(b < 0, 0.0, b).to(dtype).expand(1, 4, 8)), y
