@@ -60,8 +60,8 @@ def _heads(t: torch.Tensor, what: str, device=None):
 
 def _integers(t: torch.Tensor, n: int, device, what: str):
     _on_gpu(t, what, device)
-    if t.dtype is not torch.int32 or t.dim() != 1 or not t.is_contiguous() or (n is not None and t.shape[0] != n):
-        raise ValueError(f"{what} must be contiguous int32 [{'n' if n is None else n}], got {t.dtype} {tuple(t.shape)}")
+    if t.dtype is not torch.int32 or t.dim() != 1 or not t.is_contiguous() or (n is not None and t.shape[0] != n) or t.is_neg():
+        raise ValueError(f"{what} must be contiguous int32 [{'n' if n is None else n}] and no negated view, got {t.dtype} {tuple(t.shape)}")
 
 
 def _description(q, k, v, mask, table, buckets, positions, scale):

@@ -611,3 +611,12 @@ def test_positions_near_their_ends(N, end, order, width):
     buckets = torch.arange(2 * int(step.max()) + 1, dtype=torch.int32)
     table = rand((2, len(buckets)), 263, F32)
     check(run(N, *t, table, None, buckets, places_), R.Attention(*t, None, table, buckets, places_))
+
+
+def test_negated_positions_and_buckets_are_refused(N):
+    x, table = torch.zeros(1, 5, 2, 16, dtype=BF16, device="cuda"), torch.zeros(2, 9, device="cuda")
+    t = torch.arange(9, dtype=torch.int32, device="cuda")
+    N.attention(x, x, x, table=table, buckets=t, positions=t[:5])
+    for bad in (dict(buckets=torch._neg_view(t)), dict(buckets=t, positions=torch._neg_view(t)[:5]), dict(buckets=t, positions=(None, torch._neg_view(t[:5])))):
+        with pytest.raises(ValueError):
+            N.attention(x, x, x, table=table, **bad)

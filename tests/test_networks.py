@@ -246,3 +246,12 @@ def test_a_library_with_the_operators_in_8_bits_alone_is_taken(monkeypatch):
     monkeypatch.setattr(B, "load_library", lambda: Library(()))
     with pytest.raises(AttributeError):
         B.load_activations()
+
+
+def test_positions_and_buckets_that_are_negated_views_are_refused(monkeypatch):
+    """Their memory holds the numbers with the other sign."""
+    monkeypatch.setattr(N, "_on_gpu", lambda *a: None)
+    t = torch.arange(5, dtype=torch.int32)
+    N._integers(t, 5, t.device, "buckets")
+    with pytest.raises(ValueError, match="negated"):
+        N._integers(torch._neg_view(t), 5, t.device, "buckets")
