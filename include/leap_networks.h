@@ -31,7 +31,9 @@ extern "C" {
  * The bias, from d_table [heads][buckets] of table_type (NULL: none): the pair of query i and key j takes the bucket
  * d_bucket_of[d_key_positions[j] - d_query_positions[i] + offsets / 2] of `offsets`; differences beyond either end take that end's, buckets
  * beyond the table's ends its ends'.  Positions (NULL: i and j themselves) are within -2^30 .. 2^30.  Infinities and numbers of any size in the table are fine: -inf
- * leaves a pair out. */
+ * leaves a pair out.
+ *
+ * Sizes: fewer than 2^24 times 128 queries of an item's head, each item's and head's last ones counting as 128; keys alike for the gradients. */
 typedef struct {
     int64_t batch, queries, keys, heads, kv_heads, width;
     int64_t q_item, q_row, q_head, k_item, k_row, k_head, v_item, v_row, v_head;       /* strides of an item, of a query or key, of a head */

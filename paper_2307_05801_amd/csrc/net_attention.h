@@ -379,6 +379,7 @@ template <class F, class... R> inline int by_flags(F &&f, bool flag, R... rest)
     return by_flags([&](auto... c) { return f(std::false_type{}, c...); }, rest...);
 }
 
+constexpr const char *TOO_MANY_BLOCKS = "2^24 or more of an item's 128 queries, or keys, of a head: items times heads times those";
 // Null if fine: an array's strides; a description.
 const char *bad_array(int64_t items, int64_t item, int64_t rows, int64_t row, int64_t heads, int64_t head);
 const char *bad_attention(const leap_attention_desc *d);

@@ -425,7 +425,7 @@ extern "C" int leap_attention(const leap_attention_desc *desc, const void *d_q, 
     if (lines + parts + laid && unaligned(d_work)) return refuse(NO_WORK);
     forward_args F{arguments_of(desc, d_q, d_k, d_v), (uint16_t *)d_o, d_stats, (uint16_t *)d_rest, S.abreast, S.parts, S.length, nullptr, nullptr, 0};
     const int64_t blocks = S.units * S.parts, rows = desc->batch * desc->heads * desc->queries;
-    if (blocks >= (int64_t)1 << 24) return refuse("more than 2^31 rows of heads");
+    if (blocks >= (int64_t)1 << 24) return refuse(TOO_MANY_BLOCKS);
     F.part_sums = (float *)((char *)d_work + lines);
     F.part_stats = F.part_sums + rows * S.parts * desc->width;
     const hipStream_t st = stream_of(hip_stream);

@@ -567,7 +567,7 @@ extern "C" int leap_attention_backward(const leap_attention_desc *desc, const vo
     if (rows && (!d_grad || !d_q || !d_o || !d_stats || !d_rest || (desc->keys && (!d_k || !d_v)))) return refuse("null data pointer");
     if (rows && unaligned(d_work)) return refuse(NO_WORK);
     const int64_t tiles = (desc->queries + COLS - 1) / COLS, key_tiles = (desc->keys + COLS - 1) / COLS;
-    if (desc->batch * desc->heads * tiles >= (int64_t)1 << 24 || desc->batch * desc->kv_heads * key_tiles >= (int64_t)1 << 24) return refuse("more than 2^31 rows of heads");
+    if (desc->batch * desc->heads * tiles >= (int64_t)1 << 24 || desc->batch * desc->kv_heads * key_tiles >= (int64_t)1 << 24) return refuse(TOO_MANY_BLOCKS);
     if ((int64_t)desc->heads / desc->kv_heads * ((desc->queries + TILE - 1) / TILE) >= (int64_t)1 << 31) return refuse("more than 2^37 queries share a key");
     const hipStream_t st = stream_of(hip_stream);
     if (!rows) {                                           // nothing is read, the workspace is not written

@@ -255,3 +255,11 @@ def test_positions_and_buckets_that_are_negated_views_are_refused(monkeypatch):
     N._integers(t, 5, t.device, "buckets")
     with pytest.raises(ValueError, match="negated"):
         N._integers(torch._neg_view(t), 5, t.device, "buckets")
+
+
+def test_more_blocks_than_a_launch_has_are_refused_by_that_name(lib):
+    """2^24 items of one head and query are as many blocks."""
+    plain = [1 << 24, 1, 1, 1, 1, 8] + [8, 8, 8] * 3 + [0, 0, 0, 0, 0, 0, 0, 0, 0, 0.5]
+    desc = N._DESC.pack(*plain)
+    for status in (lib.leap_attention(desc, P, P, P, P, None, None, None, None), lib.leap_attention_backward(desc, P, 8, 8, 8, P, P, P, P, P, P, P, P, P, None, P, None)):
+        assert status == B.LEAP_INVALID_ARG and "2^24" in lib.leap_last_error().decode()
