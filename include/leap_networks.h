@@ -59,6 +59,7 @@ int leap_attention(const leap_attention_desc *desc, const void *d_q, const void 
 /* Its gradients from that of o: grad [batch][queries][heads][width] with strides; o, stats and rest of the forward pass.  grad_q, grad_k, grad_v: as
  * q, k, v without gaps; grad_table: [heads][buckets], float.  Any of them may be NULL.  Keys that the mask leaves out get zeros; without queries all that is wanted is
  * zeros, and nothing is read.  What is not finite in a query, or in its row of grad, reaches in grad_table the buckets of its pairs alone.
+ * A pair's part in grad_table is held to 2^-47 of the largest among those of 128 queries and 64 keys, its sums to 32 bits.
  * d_work: leap_attention_backward_work() bytes (with_table: whether grad_table is wanted), never NULL where there are queries. */
 int64_t leap_attention_backward_work(const leap_attention_desc *desc, int32_t with_table);
 int leap_attention_backward(const leap_attention_desc *desc, const void *d_grad, int64_t grad_item, int64_t grad_row, int64_t grad_head, const void *d_q,

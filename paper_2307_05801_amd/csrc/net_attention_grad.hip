@@ -78,10 +78,15 @@ constexpr int window_of_tile(int deep, int buckets) { return deep > 64 || bucket
 // difference has at most one pair of each of the block's 128 queries, and 128 times 2^24 fits 32 bits.
 // In the next tile's time the sums go to their buckets, which the block keeps as floats: without atomic adds where the window's buckets rise (one of its own to
 // every difference: in 512 windows 0.39 ms of 1.97 were such adds), otherwise a wave to every fourth bucket.
-// Where the differences are too far apart or keys do not rise, ds go to the buckets as two integers, of 2^-17 and 2^-34 of the largest: 8192 of either fit.
+// Where the differences are too far apart or keys do not rise, ds go to the buckets as one integer of 64 bits, of 2^-49 of the largest: 8192 of them fit.
 template <int BUCKETS, int WINDOW> struct table_sums {
     float bucket[BUCKETS];
-    int32_t upper[WINDOW], lower[WINDOW];
+    union {
+        struct {
+            int32_t upper[WINDOW], lower[WINDOW];
+        };
+        uint64_t total[WINDOW];
+    };
     uint16_t which[WINDOW];                                // the buckets of the window
     uint32_t peak[WAVES];                                  // the largest ds of each wave's, its bits
 };
@@ -302,24 +307,23 @@ template <int DEEP, bool DIRECT, bool BIAS, int BUCKETS> __global__ __launch_bou
                         });
                 } else {
                     constexpr int AT_ONCE = WINDOW;
-                    const float by = 0x1.fp16f / largest;
-                    unscale = largest * (1.0f / 0x1.fp16f);
+                    float by = 0x1.fp16f / largest;
+                    unscale = largest * (1.0f / 0x1.fp48f);
                     for (int first = 0; first < A.buckets; first += AT_ONCE) {
+                        asm volatile("" : "+v"(by));       // (the terms are not to be kept from one turn to the next: it would fill the registers)
 #pragma unroll
                         for (int h = 0; h < 2; ++h)
 #pragma unroll
                             for (int r = 0; r < 16; ++r) {
                                 const int b = A.line_buckets[line_at(A, places[turn][h * 32 + row_of(r) + lane / 32 * 4], position)] - first;
                                 const float v = x[h][r] * by, whole = rintf(v);
-                                if (b >= 0 && b < AT_ONCE) {
-                                    __hip_atomic_fetch_add(&sums.upper[b], (int)whole, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
-                                    __hip_atomic_fetch_add(&sums.lower[b], (int)((v - whole) * 0x1p17f), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
-                                }
+                                const int64_t term = ((int64_t)(int)whole << 32) + (int)((v - whole) * 0x1p32f);
+                                if (b >= 0 && b < AT_ONCE) __hip_atomic_fetch_add(&sums.total[b], (uint64_t)term, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
                             }
                         shared_barrier();
                         for (int b = threadIdx.x; b < AT_ONCE && first + b < A.buckets; b += BLOCK) {
-                            sums.bucket[first + b] += ((float)sums.upper[b] + (float)sums.lower[b] * 0x1p-17f) * unscale;
-                            sums.upper[b] = sums.lower[b] = 0;
+                            sums.bucket[first + b] += (float)(int64_t)sums.total[b] * unscale;
+                            sums.total[b] = 0;
                         }
                         shared_barrier();
                     }

@@ -620,3 +620,22 @@ def test_negated_positions_and_buckets_are_refused(N):
     for bad in (dict(buckets=torch._neg_view(t)), dict(buckets=t, positions=torch._neg_view(t)[:5]), dict(buckets=t, positions=(None, torch._neg_view(t[:5])))):
         with pytest.raises(ValueError):
             N.attention(x, x, x, table=table, **bad)
+
+
+@pytest.mark.parametrize("kind", ["line", "few", "even", "anywhere", "anywhere many", "far"])
+@pytest.mark.parametrize("batch,queries,keys,heads,kv_heads,width", [(1, 1, 20, 8, 2, 100), (1, 4, 837, 8, 2, 49), (2, 200, 130, 2, 2, 64)])
+def test_small_sums_of_the_tables_gradient(N, kind, batch, queries, keys, heads, kv_heads, width):
+    """Probabilities nearly all on one key, so that buckets' sums differ by many powers of ten: besides the roundings of the scores each pair's ds is held to 2^-47 of its tile's largest."""
+    t = inputs(batch, queries, keys, heads, kv_heads, width, 271)
+    positions, buckets, many = places(queries, keys, kind)
+    table = rand((heads, many), 273, F32)
+    r = R.Attention(*t, None, table, buckets, positions, 0.5)
+    qp, kp = positions if positions is not None else (torch.arange(queries), torch.arange(keys))
+    bias, index = R.bias_of(table, buckets, qp, kp)
+    _, _, p = R.attention(*t[:3], None, bias, 0.5)
+    group = heads // kv_heads
+    dp = t[3].double().transpose(1, 2) @ t[2].double().transpose(1, 2).repeat_interleave(group, 1).transpose(2, 3)
+    ds = p * (dp - (p * dp).sum(3, keepdim=True))
+    pairs = torch.bincount(index.flatten(), minlength=many) * batch
+    got = run(N, *t, table, None, buckets, positions, 0.5)
+    assert_close(got[4], r.grad_table, r.grad_table_off + pairs * 2.0 ** -47 * ds.abs().max(), "grad_table")
