@@ -6,6 +6,11 @@
 // walks over keys as the forward pass does; k_grad_key has keys in its lanes and walks over queries.  Both form the scores and dp: seven products instead
 // of the five of one kernel, which would have to add up grad_q over blocks.
 //
+// p and ds are 32 bits until they are a side of the products that sum over them, where they are rounded to bfloat16: gradients are 0.0022 to 0.0026 of their norm off, 0.0017 of it by their own
+// rounding.  In two bfloat16 each, as p is in the forward pass, they would take three products more of seven.
+//
+// Neither kernel deals out the side that it walks over: few queries, or few keys, are few blocks (2 x 16 queries over 262144 keys of 8 heads: 16).
+//
 // 32768 patches, 8 heads of 128: queries 6.3 ms, keys and values 9.7 to 10.3 ms (1040, and 860 to 900 TFLOP/s of matrix instructions; the latter's sums leave room for one wave a SIMD).
 // 512 windows of 512 patches, 8 heads of 64 with a table: 1.69 and 1.17 ms, bound by vector instructions (22 and 14 a pair, counted) and, for the table's gradient, adds to shared
 // memory (those to differences took 0.27 ms: without the buckets' 1.58 ms, without either 1.30).
@@ -69,7 +74,8 @@ __global__ __launch_bounds__(BLOCK) void k_delta(grad_args G)
     if (lane == 0) G.delta[(item * A.heads + head) * (int64_t)A.queries + query] = sum;
 }
 
-// Numbers of a line in shared memory (see net_attention.hip): as many as leave a compute unit room for two blocks.
+// Numbers of a line in shared memory (see net_attention.hip): as many as leave a compute unit room for two blocks, up to width 64; above, the tiles and a table's sums leave it one
+// (88 to 101 KB), and without a table's gradient two.
 constexpr int window_of_tile(int deep, int buckets) { return deep > 64 || buckets > 1024 ? 1024 : 2048; }
 
 // A table's gradient.  Adds of integers to shared memory take a wave 4 cycles, those of floats 192 (3 a lane), and integers' order does not matter.  So a tile's ds are added as
@@ -110,7 +116,7 @@ __device__ inline uint32_t wave_max(uint32_t v)
     return b[0] > b[1] ? b[0] : b[1];
 }
 
-template <int DEEP, bool DIRECT, bool BIAS, int BUCKETS> __global__ __launch_bounds__(BLOCK, 2) void k_grad_query(grad_args G)
+template <int DEEP, bool DIRECT, bool BIAS, int BUCKETS> __global__ __launch_bounds__(BLOCK, BUCKETS && DEEP > 64 ? 1 : 2) void k_grad_query(grad_args G)
 {
     using tile = rows_tile<DEEP>;
     constexpr int STEPS = DEEP / 16, BLOCKS = DEEP / 32, WINDOW = window_of_tile(DEEP, BUCKETS);
