@@ -48,9 +48,9 @@ typedef struct {
 enum { LEAP_ATTENTION_WIDEST = 128, LEAP_ATTENTION_BUCKETS = 4096 };                   /* the largest width, the most buckets */
 enum { LEAP_ATTENTION_OFFSETS = 1 << 24 };                                             /* the most differences; 2^30 for all heads together */
 
-/* o [batch][queries][heads][width] <- attention.  For a backward pass also stats [batch][heads][queries][2] (float: a number m within 8 of the largest exponent of
- * a query's keys, and the logarithm of the sum of what is left of them, x - m, both to the base 2) and rest [as o] (int16: what has to be added to o's bits, followed by 16 zeros, for those of
- * the 32-bit number that was rounded); NULL: both or neither.  With them the probabilities go into the product with 16 bits instead of 8.
+/* o [batch][queries][heads][width] <- attention.  For a backward pass also stats [batch][heads][queries][2] (float: two numbers that add up to the
+ * logarithm of a query's sum of exp(x), to the base 2, the second at most half a step of the first and half; 0 and infinity without keys) and rest [as o] (int16: what has to be added to o's bits, followed by 16 zeros, for those of
+ * the 32-bit number that was rounded); NULL: both or neither.  With them the probabilities go into the product with 16 bits instead of 8, with a table with 24.
  * d_work: leap_attention_work() bytes, NULL where that is 0. */
 int64_t leap_attention_work(const leap_attention_desc *desc);
 int leap_attention(const leap_attention_desc *desc, const void *d_q, const void *d_k, const void *d_v, void *d_o, float *d_stats, void *d_rest,

@@ -291,13 +291,24 @@ __device__ inline bf16x8 eight(const f32x16 &v, int m)
     return r;
 }
 
-// What rounding v's m-th eight to `rounded` leaves (nothing here is infinite).
-__device__ inline bf16x8 rest_of_eight(const f32x16 &v, int m, const bf16x8 &rounded)
+// v's m-th eight as the sum of PARTS bfloat16, each of what those before leave (nothing here is infinite).  A difference is one instruction, v - (1, 0).(part, its neighbour) or with (0, 1): exact, as the
+// difference is.  The constants come from registers: of those in an instruction the compiler makes others.
+template <int PARTS> __device__ inline void parts_of_eight(const f32x16 &v, int m, bf16x8 (&part)[PARTS])
 {
-    bf16x8 r;
+    uint32_t low = 0x0000bf80u, high = 0xbf800000u;                        // (-1, 0), (0, -1)
+    if constexpr (PARTS > 1) asm("" : "+s"(low), "+s"(high));
 #pragma unroll
-    for (int i = 0; i < 8; ++i) r[i] = (__bf16)(v[m * 8 + i] - (float)rounded[i]);
-    return r;
+    for (int i = 0; i < 8; i += 2) {
+        float a = v[m * 8 + i], b = v[m * 8 + i + 1];
+#pragma unroll
+        for (int p = 0; p < PARTS; ++p) {
+            const bf16x2 both = {(__bf16)a, (__bf16)b};
+            part[p][i] = both[0], part[p][i + 1] = both[1];
+            if (p + 1 == PARTS) break;
+            a = __builtin_amdgcn_fdot2_f32_bf16(both, __builtin_bit_cast(bf16x2, low), a, false);
+            b = __builtin_amdgcn_fdot2_f32_bf16(both, __builtin_bit_cast(bf16x2, high), b, false);
+        }
+    }
 }
 
 // Inside a branch that is seldom taken: it stays one, instead of selections that are always made.

@@ -82,11 +82,12 @@ constexpr int window_of_tile(int deep, int buckets) { return deep > 64 || bucket
 // integers to two numbers for every difference that its pairs have: whole multiples of 2^-24 of the largest of them, and what is left in multiples of 2^-48.  (With the
 // first alone sums were 0.6e-5 to 6e-5 of the table's norm off, since a bucket that nearly all of a query's keys are in has a sum far smaller than its terms.)  Keys rise, so a
 // difference has at most one pair of each of the block's 128 queries, and 128 times 2^24 fits 32 bits.
-// In the next tile's time the sums go to their buckets, which the block keeps as floats: without atomic adds where the window's buckets rise (one of its own to
+// In the next tile's time the sums go to their buckets, which the block keeps in 64 bits where shared memory has room for them (a bucket of most of a query's keys is a small difference of large tiles'
+// sums: 16 x 211 rows 1.6e-7 of the norm off, 3.0e-7 with floats; no slower), for more than 1024 of width 64 as floats: without atomic adds where the window's buckets rise (one of its own to
 // every difference: in 512 windows 0.39 ms of 1.97 were such adds), otherwise a wave to every fourth bucket.
 // Where the differences are too far apart or keys do not rise, ds go to the buckets as one integer of 64 bits, of 2^-49 of the largest: 8192 of them fit.
-template <int BUCKETS, int WINDOW> struct table_sums {
-    float bucket[BUCKETS];
+template <int BUCKETS, int WINDOW, class SUM> struct table_sums {
+    SUM bucket[BUCKETS];
     union {
         struct {
             int32_t upper[WINDOW], lower[WINDOW];
@@ -96,7 +97,7 @@ template <int BUCKETS, int WINDOW> struct table_sums {
     uint16_t which[WINDOW];                                // the buckets of the window
     uint32_t peak[WAVES];                                  // the largest ds of each wave's, its bits
 };
-template <int WINDOW> struct table_sums<0, WINDOW> {};
+template <int WINDOW, class SUM> struct table_sums<0, WINDOW, SUM> {};
 
 // Shared memory's writes of all waves are there for all; what comes from memory is not waited for.
 __device__ inline void shared_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
@@ -122,14 +123,15 @@ template <int DEEP, bool DIRECT, bool BIAS, int BUCKETS> __global__ __launch_bou
     constexpr int STEPS = DEEP / 16, BLOCKS = DEEP / 32, WINDOW = window_of_tile(DEEP, BUCKETS);
     const attention_args &A = G.a;
     __shared__ __attribute__((aligned(16))) uint8_t room[4 * tile::BYTES + (BIAS ? 2 * WINDOW * 4 : 0)];
-    __shared__ __attribute__((aligned(16))) table_sums<BUCKETS, WINDOW> sums;
+    using sum_of_bucket = std::conditional_t<BUCKETS == LEAP_ATTENTION_BUCKETS && DEEP == 64, float, double>;
+    __shared__ __attribute__((aligned(16))) table_sums<BUCKETS, WINDOW, sum_of_bucket> sums;
     __shared__ int places[BIAS ? 2 : 1][TILE];
     lds_byte *const lds = (lds_byte *)room;
     const int lane = threadIdx.x % WAVE, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
     const int tiles = (A.queries + COLS - 1) / COLS;
     const int64_t units = (int64_t)A.batch * tiles;
     if constexpr (BUCKETS != 0) {
-        for (int b = threadIdx.x; b < BUCKETS; b += BLOCK) sums.bucket[b] = 0.0f;
+        for (int b = threadIdx.x; b < BUCKETS; b += BLOCK) sums.bucket[b] = 0;
         for (int b = threadIdx.x; b < WINDOW; b += BLOCK) sums.upper[b] = sums.lower[b] = 0;
     }
 
@@ -195,7 +197,7 @@ template <int DEEP, bool DIRECT, bool BIAS, int BUCKETS> __global__ __launch_bou
             if constexpr (BUCKETS != 0) {
                 if (pending && apart)              // no two of a bucket
                     for (int i = threadIdx.x; i < before.count; i += BLOCK) {
-                        sums.bucket[sums.which[i]] += ((float)sums.upper[i] + (float)sums.lower[i] * 0x1p-24f) * unscale;
+                        sums.bucket[sums.which[i]] += ((sum_of_bucket)sums.upper[i] + (sum_of_bucket)sums.lower[i] * (sum_of_bucket)0x1p-24) * unscale;
                         sums.upper[i] = sums.lower[i] = 0;
                     }
                 else if (pending)
@@ -205,7 +207,7 @@ template <int DEEP, bool DIRECT, bool BIAS, int BUCKETS> __global__ __launch_bou
                         const int upper = sums.upper[i], lower = sums.lower[i];
                         if (!(upper | lower)) continue;                                    // a float's add takes the 3 cycles for every lane that makes one
                         sums.upper[i] = sums.lower[i] = 0;
-                        __hip_atomic_fetch_add(&sums.bucket[bucket], ((float)upper + (float)lower * 0x1p-24f) * unscale, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+                        __hip_atomic_fetch_add(&sums.bucket[bucket], ((sum_of_bucket)upper + (sum_of_bucket)lower * (sum_of_bucket)0x1p-24) * unscale, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
                     }
             }
         };
@@ -290,7 +292,7 @@ template <int DEEP, bool DIRECT, bool BIAS, int BUCKETS> __global__ __launch_bou
                         for (int r = 0; r < 16; ++r) {
                             const bool finite = (__float_as_uint(x[h][r]) & 0x7fffffffu) < INFINITE;
                             if (!finite && there)
-                                __hip_atomic_fetch_add(&sums.bucket[A.line_buckets[line_at(A, places[turn][h * 32 + row_of(r) + lane / 32 * 4], position)]], x[h][r], __ATOMIC_RELAXED,
+                                __hip_atomic_fetch_add(&sums.bucket[A.line_buckets[line_at(A, places[turn][h * 32 + row_of(r) + lane / 32 * 4], position)]], (sum_of_bucket)x[h][r], __ATOMIC_RELAXED,
                                                        __HIP_MEMORY_SCOPE_WORKGROUP);
                             x[h][r] = finite ? x[h][r] : 0.0f;
                             largest = fmaxf(largest, fabsf(x[h][r]));
@@ -328,7 +330,7 @@ template <int DEEP, bool DIRECT, bool BIAS, int BUCKETS> __global__ __launch_bou
                             }
                         shared_barrier();
                         for (int b = threadIdx.x; b < AT_ONCE && first + b < A.buckets; b += BLOCK) {
-                            sums.bucket[first + b] += (float)(int64_t)sums.total[b] * unscale;
+                            sums.bucket[first + b] += (sum_of_bucket)(int64_t)sums.total[b] * unscale;
                             sums.total[b] = 0;
                         }
                         shared_barrier();
@@ -348,7 +350,7 @@ template <int DEEP, bool DIRECT, bool BIAS, int BUCKETS> __global__ __launch_bou
     } while (BUCKETS && unit < units);
     if constexpr (BUCKETS != 0) {
         __syncthreads();
-        for (int b = threadIdx.x; b < A.buckets; b += BLOCK) G.part[block * A.buckets + b] = sums.bucket[b];
+        for (int b = threadIdx.x; b < A.buckets; b += BLOCK) G.part[block * A.buckets + b] = (float)sums.bucket[b];
     }
 }
 

@@ -137,7 +137,7 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, mask: torch.Ten
     patches.  -inf in the table leaves pairs out.
 
     Scores, the softmax and sums are 32 bits; probabilities and the gradients of scores are rounded to bfloat16 for the products that sum over them, but for
-    the forward pass that a backward pass follows: there probabilities have 16 bits (so o's last bits differ from those without one).  Kept for the
+    the forward pass that a backward pass follows: there probabilities have 16 bits, with a table 24 (so o's last bits differ from those without one).  Kept for the
     backward pass: q, k, v and o, as they are also within keep_in_8_bits (the probabilities are formed again from what made them), 2 bytes more a value of
     o, and two floats a query and head."""
     _heads(q, "q")

@@ -639,3 +639,15 @@ def test_small_sums_of_the_tables_gradient(N, kind, batch, queries, keys, heads,
     pairs = torch.bincount(index.flatten(), minlength=many) * batch
     got = run(N, *t, table, None, buckets, positions, 0.5)
     assert_close(got[4], r.grad_table, r.grad_table_off + pairs * 2.0 ** -47 * ds.abs().max(), "grad_table")
+
+
+@pytest.mark.parametrize("batch,heads,width,shape,near,codes", [(6, 3, 64, (1, 8), 2, 4), (17, 4, 128, (29, 1), 3, 6), (57, 1, 128, (2, 9), 2, 3), (22, 4, 64, (3, 1, 8), 1, 3), (57, 6, 11, (23, 3), 2, 4)])
+def test_the_tables_gradient_is_that_of_32_bits(N, batch, heads, width, shape, near, codes):
+    """Few patches, whose sums hide nothing: of a pair's ds some eight roundings of 2^-24 each (its score's, the exponential's, delta's, dp's), 2^-21 of the norm in all; with probabilities of 16 bits in delta
+    it was 2^-20 and more."""
+    positions, buckets = N.relative_buckets(shape, near, codes, device="cpu")
+    n, many = len(positions), (2 * codes - 1) ** len(shape)
+    t = [rand((batch, n, heads, width), 281 + i) for i in range(4)]
+    table = rand((heads, many), 285, F32, 0.5)
+    got, r = run(N, *t, table, None, buckets, positions), R.Attention(*t, None, table, buckets, positions)
+    assert (got[4].cpu().double() - r.grad_table).norm() <= 2.0 ** -21 * r.grad_table.norm()
