@@ -5,9 +5,9 @@
 // the sum of exp2(x - m) of each query in that lane, and multiplies the values summed so far by exp2(m before - m now) where m has grown.  m follows the largest only when a
 // query's has got 2^8 ahead of it: sums of exp2 up to 2^8 are as good, and one of 32 queries has a new largest in nearly every tile.
 //
-// What bounds it: at width 64 the vector instructions (with a table 13 to 16 a pair, counted; 512 windows of 512 patches, 8 heads, kept for a backward pass: 0.95 ms, 290 TFLOP/s), at
-// width 128 those (10 a pair) and the matrix instructions about alike (32768 patches, 8 heads: 6.0 ms, 730 TFLOP/s, half as many flops again with the probabilities' second part).
-// Three blocks share a compute unit at width 64 (the windows with two: 1.16 ms).
+// What bounds it: at width 64 the vector instructions (with a table 12 to 16 a pair, counted; 512 windows of 512 patches, 8 heads, kept for a backward pass: 1.05 ms, 262 TFLOP/s, twice as many flops with
+// the probabilities' other two parts), at width 128 those (8 a pair) and the matrix instructions about alike (32768 patches, 8 heads: 6.0 ms, 730 TFLOP/s, half as many flops again with the second part).
+// Three blocks share a compute unit at width 64 (the windows, with probabilities in two parts: 0.95 ms, with two blocks 1.16).
 #include "net_attention.h"
 
 namespace {
