@@ -210,7 +210,7 @@ __device__ inline float rest_of_bf16(float v)
 
 // 1 / (1 + exp(-g)), off by 2 units of 2^-24 of its value where g >= 0 and by up to 3 + |g| below (6 at -4, 10 at -8, 31 at -30, 66 at -87; exact
 // exponential and reciprocal assumed): the product with the constant rounds, and exp(-g) is the square of exp(-g / 2).  Taking
-// along what the product's rounding leaves holds it at 5 throughout (fine_sigmoid, for results of 32 bits) in eleven instructions instead of six; the results here go to codes of 2^-4, to
+// along what the product's rounding leaves holds it at 5 throughout (fine_sigmoid, for results of 32 bits) in twelve instructions instead of six; the results here go to codes of 2^-4, to
 // 16 bits, or to two bfloat16, 2^-17.  A square, because an exponent that carries an offset would lose what the offset's size rounds away.  Its 2^-32nd part does not
 // overflow before the result is zero, and the reciprocal of that, which the hardware forms within a unit but not as a subnormal number, is
 // brought back by a product.
