@@ -48,8 +48,8 @@ typedef struct {
 enum { LEAP_ATTENTION_WIDEST = 128, LEAP_ATTENTION_BUCKETS = 4096 };                   /* the largest width, the most buckets */
 enum { LEAP_ATTENTION_OFFSETS = 1 << 24 };                                             /* the most differences; 2^30 for all heads together */
 
-/* o [batch][queries][heads][width] <- attention.  For a backward pass also stats [batch][heads][queries][2] (float: two numbers that add up to the
- * logarithm of a query's sum of exp(x), to the base 2, the second at most half a step of the first and half; 0 and infinity without keys) and rest [as o] (int16: what has to be added to o's bits, followed by 16 zeros, for those of
+/* o [batch][queries][heads][width] <- attention.  For a backward pass also stats [batch][heads][queries][2] (float: a number m within 8 of the largest exponent of
+ * a query's keys, to the base 2, and the sum of 2^(x - m); zeros without keys) and rest [as o] (int16: what has to be added to o's bits, followed by 16 zeros, for those of
  * the 32-bit number that was rounded); NULL: both or neither.  With them the probabilities go into the product with 16 bits instead of 8, with a table with 24.
  * d_work: leap_attention_work() bytes, NULL where that is 0. */
 int64_t leap_attention_work(const leap_attention_desc *desc);
@@ -59,7 +59,7 @@ int leap_attention(const leap_attention_desc *desc, const void *d_q, const void 
 /* Its gradients from that of o: grad [batch][queries][heads][width] with strides; o, stats and rest of the forward pass.  grad_q, grad_k, grad_v: as
  * q, k, v without gaps; grad_table: [heads][buckets], float.  Any of them may be NULL.  Keys that the mask leaves out get zeros; without queries all that is wanted is
  * zeros, and nothing is read.  What is not finite in a query, or in its row of grad, reaches in grad_table the buckets of its pairs alone.
- * A pair's part in grad_table is held to 2^-47 of the largest among those of 128 queries and 64 keys, its sums to 32 bits.
+ * A pair's part in grad_table is held to 2^-46 of the largest among those of 128 queries and 64 keys, its sums to 32 bits.
  * d_work: leap_attention_backward_work() bytes (with_table: whether grad_table is wanted), never NULL where there are queries. */
 int64_t leap_attention_backward_work(const leap_attention_desc *desc, int32_t with_table);
 int leap_attention_backward(const leap_attention_desc *desc, const void *d_grad, int64_t grad_item, int64_t grad_row, int64_t grad_head, const void *d_q,

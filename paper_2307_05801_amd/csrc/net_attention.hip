@@ -38,21 +38,11 @@ __device__ inline uint16_t rest_of(float v)
     return finite_magnitude(v) ? (uint16_t)(rest < 0x7fff ? rest : 0x7fff) : 0;
 }
 
-// The logarithm of a query's sum of exp2(x), from that of exp2(x - m), as a number of its size and what that leaves, of 2^-26: a logarithm of 8 and more would be off by 2^-21, alike for all of a
-// query's probabilities, which a bucket that has nearly all of its pairs does not hide.
-__device__ inline void store_stats(float *to, float m, float sum)
-{
-    const float whole = rintf(__builtin_amdgcn_logf(sum)), first = m + whole, of_m = first - whole;
-    const float left = (m - of_m) + (whole - (first - of_m));                  // of the sum's rounding
-    to[0] = sum != 0.0f ? first : 0.0f;
-    to[1] = sum != 0.0f ? __builtin_amdgcn_logf(sum * __builtin_amdgcn_exp2f(-whole)) + left : INFINITY;
-}
-
 // BIAS: with a table.  FINE: for a backward pass, which takes delta = grad.o off every product grad.v of a query: an o with its rounding, or with the probabilities',
 // would spoil all of the query's alike, and in grad_q that adds up along what the keys have in common (keys and values with a common part as large as what
 // differs, 512 keys: grad_q was 0.020 of its norm off, with four times as large a part 0.34; now 0.003 and 0.007, which is the rounding of ds).  So there the
 // probabilities are the sum of two bfloat16, and o's other 16 bits are kept.  With a table they are the sum of three, their 24 bits: its gradient is 32 bits, and what delta lacks is in every pair of a
-// query, which a bucket that has most of them adds up (of two, from 8 patches to 5397, the gradient is 0.4e-6 to 6e-6 of its norm off, of three 1.6e-7 to 1.5e-6, which is what all in 32 bits has; the forward
+// query, which a bucket that has most of them adds up (of two, from 8 patches to 5397, the gradient is 0.4e-6 to 6e-6 of its norm off, of three 1.4e-7 to 1.3e-6, all in 32 bits 1.4e-7 to 1.2e-6; the forward
 // pass of 512 windows 0.95 ms, with three 1.04).  Otherwise they are rounded to bfloat16 once: o is 0.0022 to 0.0024 of its norm off, 0.0017 of it by its own rounding (of two parts
 // 32768 patches, 8 heads of 128, take 5.5 instead of 4.1 ms, 2 x 16 queries over 262144 keys 89 instead of 74 us).
 template <int DEEP, bool DIRECT, bool BIAS, bool FINE> __global__ __launch_bounds__(BLOCK, DEEP > 64 || !DIRECT ? 2 : 3) void k_attention(forward_args F)
@@ -207,7 +197,7 @@ template <int DEEP, bool DIRECT, bool BIAS, bool FINE> __global__ __launch_bound
     store_column<BLOCKS>(F.o + row * A.width, A.width, o, by, lane, there);
     if (FINE && there && lane < 32) {
         float *const to = F.stats + ((item * A.heads + head) * (int64_t)A.queries + query) * 2;
-        store_stats(to, m, sum);
+        to[0] = sum != 0.0f ? m : 0.0f, to[1] = sum;
     }
     if constexpr (FINE) {
         if (there)
@@ -254,7 +244,7 @@ __global__ __launch_bounds__(BLOCK) void k_join(forward_args F)
         F.o[to * A.width + at] = element<LEAP_BF16>::from_float(v);
         if (F.rest) F.rest[to * A.width + at] = rest_of(v);
     }
-    if (F.stats && threadIdx.x == 0) store_stats(F.stats + row * 2, base, sum);
+    if (F.stats && threadIdx.x == 0) F.stats[row * 2] = base, F.stats[row * 2 + 1] = sum;
 }
 
 // Rows of `width` to rows of whole 16 bytes, a piece a thread.

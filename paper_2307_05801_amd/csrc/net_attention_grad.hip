@@ -33,9 +33,10 @@ struct grad_args {
     int64_t first;                     // block of this launch
 };
 
-// A query's statistics, and what its scores are lowered by: together where scores have no bias, which can be far larger than the logarithm.
+// A query's statistics: probabilities are exp2(x - most) / sum, and zeros where it has no keys.
 struct query_stats {
-    float most, log;
+    float most, sum;
+    __device__ inline float log() const { return sum != 0.0f ? __builtin_amdgcn_logf(sum) : INFINITY; }
 };
 __device__ inline query_stats stats_of(const grad_args &G, int64_t row)
 {
@@ -80,13 +81,13 @@ __global__ __launch_bounds__(BLOCK) void k_delta(grad_args G)
 constexpr int window_of_tile(int deep, int buckets) { return deep > 64 || buckets > 1024 ? 1024 : 2048; }
 
 // A table's gradient.  Adds of integers to shared memory take a wave 4 cycles, those of floats 192 (3 a lane), and integers' order does not matter.  So a tile's ds are added as
-// integers to two numbers for every difference that its pairs have: whole multiples of 2^-24 of the largest of them, and what is left in multiples of 2^-48.  (With the
+// integers to two numbers for every difference that its pairs have: whole multiples of 2^-22 of the largest of them's power of two, which scales without a rounding, and what is left in multiples of 2^-46.  (With the
 // first alone sums were 0.6e-5 to 6e-5 of the table's norm off, since a bucket that nearly all of a query's keys are in has a sum far smaller than its terms.)  Keys rise, so a
-// difference has at most one pair of each of the block's 128 queries, and 128 times 2^24 fits 32 bits.
+// difference has at most one pair of each of the block's 128 queries, and 128 times 2^23 fits 32 bits.
 // In the next tile's time the sums go to their buckets, which the block keeps in 64 bits where shared memory has room for them (a bucket of most of a query's keys is a small difference of large tiles'
-// sums: 16 x 211 rows 1.6e-7 of the norm off, 3.0e-7 with floats; no slower), for more than 1024 of width 64 as floats: without atomic adds where the window's buckets rise (one of its own to
+// sums: 16 x 211 rows 1.4e-7 of the norm off, with floats twice that; no slower), for more than 1024 of width 64 as floats: without atomic adds where the window's buckets rise (one of its own to
 // every difference: in 512 windows 0.39 ms of 1.97 were such adds), otherwise a wave to every fourth bucket.
-// Where the differences are too far apart or keys do not rise, ds go to the buckets as one integer of 64 bits, of 2^-49 of the largest: 8192 of them fit.
+// Where the differences are too far apart or keys do not rise, ds go to the buckets as one integer of 64 bits, of 2^-48 of that power: 8192 of them fit.
 template <int BUCKETS, int WINDOW, class SUM> struct table_sums {
     SUM bucket[BUCKETS];
     union {
@@ -154,7 +155,7 @@ template <int DEEP, bool DIRECT, bool BIAS, int BUCKETS> __global__ __launch_bou
         load_side<STEPS>(q, A.q.data + item * A.q.item + head * A.q.head + query * A.q.row, width, there, lane);
         load_side<STEPS>(g, G.grad.data + item * G.grad.item + head * G.grad.head + query * G.grad.row, width, there, lane);
         const int64_t row = (item * A.heads + head) * (int64_t)A.queries + query;
-        const query_stats stats = there ? stats_of(G, row) : query_stats{0.0f, INFINITY};
+        const query_stats stats = there ? stats_of(G, row) : query_stats{0.0f, 0.0f};
         float delta = 0.0f;
         {
             const int64_t at = ((item * A.queries + query) * A.heads + head) * width;
@@ -164,9 +165,10 @@ template <int DEEP, bool DIRECT, bool BIAS, int BUCKETS> __global__ __launch_bou
             delta = column_sum(delta);
             if (there && lane < 32) G.delta[row] = delta;          // for k_grad_key
         }
-        const float base = stats.most + stats.log;
-        // with a table scores can be so large that the logarithm of their sum is lost in `base`: what is missing is a factor of the query's
-        const float factor = BIAS && stats.log < INFINITY ? __builtin_amdgcn_exp2f(base - stats.most - stats.log) : 0.0f, lowered = factor * delta;
+        // With a table scores can be so large that the logarithm of their sum would be lost in what they are lowered by, and the table's gradient is 32 bits, of which the rounding of exponents
+        // takes the fewer the nearer they are to 0: so there they are lowered by the largest alone, and the sum is a factor of dp's and delta's.
+        const float base = !BIAS ? stats.most + stats.log() : stats.sum != 0.0f ? stats.most : INFINITY;
+        const float factor = BIAS && stats.sum != 0.0f ? 1.0f / stats.sum : 0.0f, lowered = factor * delta;
         const int position = BIAS ? query_position(A, there ? query : A.queries - 1) : 0;
         place_range mine;
         if constexpr (BIAS) mine = both(A.query_places[query0 / TILE], A.query_places[query0 + TILE < A.queries ? query0 / TILE + 1 : query0 / TILE]);
@@ -301,11 +303,11 @@ template <int DEEP, bool DIRECT, bool BIAS, int BUCKETS> __global__ __launch_bou
                     shared_barrier();                      // all have read the peaks
                     most = of_block();
                 }
-                largest = __uint_as_float(most);
+                const uint32_t power = most >> 23;         // of two, of the largest, + 127: 27 to 254
                 if (near) {
                     fetch_window<2>(A.line_buckets, A.offsets, window, (lds_byte *)sums.which, wave, lane);
-                    const float by = 0x1.fp23f / largest;
-                    unscale = largest * (1.0f / 0x1.fp23f);
+                    const float by = __uint_as_float((276 - power) << 23);                     // 2^22 for the power
+                    unscale = __uint_as_float((power - 22) << 23);
                     const uint32_t to_sums = origin_of((lds_byte *)sums.upper, A, window, position, false);
 #pragma unroll
                     for (int h = 0; h < 2; ++h)
@@ -316,8 +318,8 @@ template <int DEEP, bool DIRECT, bool BIAS, int BUCKETS> __global__ __launch_bou
                         });
                 } else {
                     constexpr int AT_ONCE = WINDOW;
-                    float by = 0x1.fp16f / largest;
-                    unscale = largest * (1.0f / 0x1.fp48f);
+                    float by = __uint_as_float((270 - power) << 23);                           // 2^16
+                    const float unit = __uint_as_float(power << 23);
                     for (int first = 0; first < A.buckets; first += AT_ONCE) {
                         asm volatile("" : "+v"(by));       // (the terms are not to be kept from one turn to the next: it would fill the registers)
 #pragma unroll
@@ -331,7 +333,7 @@ template <int DEEP, bool DIRECT, bool BIAS, int BUCKETS> __global__ __launch_bou
                             }
                         shared_barrier();
                         for (int b = threadIdx.x; b < AT_ONCE && first + b < A.buckets; b += BLOCK) {
-                            sums.bucket[first + b] += (sum_of_bucket)(int64_t)sums.total[b] * unscale;
+                            sums.bucket[first + b] += (sum_of_bucket)(int64_t)sums.total[b] * (sum_of_bucket)0x1p-48 * unit;
                             sums.total[b] = 0;
                         }
                         shared_barrier();
@@ -420,7 +422,7 @@ template <int DEEP, bool DIRECT, bool BIAS> __global__ __launch_bounds__(BLOCK, 
                 }
                 if (wave == 0) {
                     const bool in = first + lane < A.queries;
-                    stats = in ? stats_of(G, row0 + first + lane) : query_stats{0.0f, INFINITY};
+                    stats = in ? stats_of(G, row0 + first + lane) : query_stats{0.0f, 0.0f};
                     nd = in ? G.delta[row0 + first + lane] : 0.0f;
                     if (BIAS) place = query_position(A, in ? first + lane : A.queries - 1);
                 }
@@ -432,8 +434,8 @@ template <int DEEP, bool DIRECT, bool BIAS> __global__ __launch_bounds__(BLOCK, 
                 lds_byte *const qt = lds + turn * 2 * tile::BYTES, *const gt = qt + tile::BYTES;
                 q.land(qt), g.land(gt);
                 if (wave == 0) {
-                    most[turn][lane] = BIAS ? stats.most : stats.most + stats.log;
-                    log[turn][lane] = stats.log;
+                    most[turn][lane] = BIAS ? stats.most : stats.most + stats.log();
+                    log[turn][lane] = stats.log();
                     delta[turn][lane] = nd;
                     if constexpr (BIAS) places[turn][lane] = place;
                 }
