@@ -77,7 +77,7 @@ __global__ __launch_bounds__(BLOCK) void k_delta(grad_args G)
 }
 
 // Numbers of a line in shared memory (see net_attention.hip): as many as leave a compute unit room for two blocks, up to width 64; above, the tiles and a table's sums leave it one
-// (88 to 101 KB), and without a table's gradient two.
+// (93 to 117 KB), and without a table's gradient two.
 constexpr int window_of_tile(int deep, int buckets) { return deep > 64 || buckets > 1024 ? 1024 : 2048; }
 
 // A table's gradient.  Adds of integers to shared memory take a wave 4 cycles, those of floats 192 (3 a lane), and integers' order does not matter.  So a tile's ds are added as
