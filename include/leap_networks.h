@@ -49,7 +49,7 @@ enum { LEAP_ATTENTION_WIDEST = 128, LEAP_ATTENTION_BUCKETS = 4096 };            
 enum { LEAP_ATTENTION_OFFSETS = 1 << 24 };                                             /* the most differences; 2^30 for all heads together */
 
 /* o [batch][queries][heads][width] <- attention.  For a backward pass also stats [batch][heads][queries][2] (float: a number m within 8 of the largest exponent of
- * a query's keys, to the base 2, and the sum of 2^(x - m); zeros without keys) and rest [as o] (int16: what has to be added to o's bits, followed by 16 zeros, for those of
+ * a query's keys, to the base 2, and the sum of 2^(x - m), without a table that sum's logarithm; a query without keys has none of it) and rest [as o] (int16: what has to be added to o's bits, followed by 16 zeros, for those of
  * the 32-bit number that was rounded); NULL: both or neither.  With them the probabilities go into the product with 16 bits instead of 8, with a table with 24.
  * d_work: leap_attention_work() bytes, NULL where that is 0. */
 int64_t leap_attention_work(const leap_attention_desc *desc);

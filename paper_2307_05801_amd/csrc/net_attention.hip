@@ -38,6 +38,9 @@ __device__ inline uint16_t rest_of(float v)
     return finite_magnitude(v) ? (uint16_t)(rest < 0x7fff ? rest : 0x7fff) : 0;
 }
 
+// The second of a query's statistics where there is no table: exponents are lowered by it too, in every tile of k_grad_key.
+__device__ inline float log_of(float sum) { return sum != 0.0f ? __builtin_amdgcn_logf(sum) : INFINITY; }
+
 // BIAS: with a table.  FINE: for a backward pass, which takes delta = grad.o off every product grad.v of a query: an o with its rounding, or with the probabilities',
 // would spoil all of the query's alike, and in grad_q that adds up along what the keys have in common (keys and values with a common part as large as what
 // differs, 512 keys: grad_q was 0.020 of its norm off, with four times as large a part 0.34; now 0.003 and 0.007, which is the rounding of ds).  So there the
@@ -197,7 +200,7 @@ template <int DEEP, bool DIRECT, bool BIAS, bool FINE> __global__ __launch_bound
     store_column<BLOCKS>(F.o + row * A.width, A.width, o, by, lane, there);
     if (FINE && there && lane < 32) {
         float *const to = F.stats + ((item * A.heads + head) * (int64_t)A.queries + query) * 2;
-        to[0] = sum != 0.0f ? m : 0.0f, to[1] = sum;
+        to[0] = sum != 0.0f ? m : 0.0f, to[1] = BIAS ? sum : log_of(sum);
     }
     if constexpr (FINE) {
         if (there)
@@ -244,7 +247,7 @@ __global__ __launch_bounds__(BLOCK) void k_join(forward_args F)
         F.o[to * A.width + at] = element<LEAP_BF16>::from_float(v);
         if (F.rest) F.rest[to * A.width + at] = rest_of(v);
     }
-    if (F.stats && threadIdx.x == 0) F.stats[row * 2] = base, F.stats[row * 2 + 1] = sum;
+    if (F.stats && threadIdx.x == 0) F.stats[row * 2] = base, F.stats[row * 2 + 1] = A.table ? sum : log_of(sum);
 }
 
 // Rows of `width` to rows of whole 16 bytes, a piece a thread.

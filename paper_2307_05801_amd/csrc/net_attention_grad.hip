@@ -33,15 +33,16 @@ struct grad_args {
     int64_t first;                     // block of this launch
 };
 
-// A query's statistics: probabilities are exp2(x - most) / sum, and zeros where it has no keys.
+// A query's statistics: probabilities are exp2(x - most) / sum, without a table (BIAS) exp2(x - most - log), and zeros where it has no keys.
 struct query_stats {
-    float most, sum;
-    __device__ inline float log() const { return sum != 0.0f ? __builtin_amdgcn_logf(sum) : INFINITY; }
+    float most, second;
 };
 __device__ inline query_stats stats_of(const grad_args &G, int64_t row)
 {
     return {G.stats[row * 2], G.stats[row * 2 + 1]};
 }
+template <bool BIAS> constexpr query_stats NO_KEYS = {0.0f, BIAS ? 0.0f : INFINITY};
+template <bool BIAS> __device__ inline float log_of(const query_stats &s) { return !BIAS ? s.second : s.second != 0.0f ? __builtin_amdgcn_logf(s.second) : INFINITY; }
 
 constexpr int DELTA_LANES = LEAP_ATTENTION_WIDEST / 8, DELTA_ROWS = BLOCK / DELTA_LANES;
 
@@ -155,7 +156,7 @@ template <int DEEP, bool DIRECT, bool BIAS, int BUCKETS> __global__ __launch_bou
         load_side<STEPS>(q, A.q.data + item * A.q.item + head * A.q.head + query * A.q.row, width, there, lane);
         load_side<STEPS>(g, G.grad.data + item * G.grad.item + head * G.grad.head + query * G.grad.row, width, there, lane);
         const int64_t row = (item * A.heads + head) * (int64_t)A.queries + query;
-        const query_stats stats = there ? stats_of(G, row) : query_stats{0.0f, 0.0f};
+        const query_stats stats = there ? stats_of(G, row) : NO_KEYS<BIAS>;
         float delta = 0.0f;
         {
             const int64_t at = ((item * A.queries + query) * A.heads + head) * width;
@@ -167,8 +168,8 @@ template <int DEEP, bool DIRECT, bool BIAS, int BUCKETS> __global__ __launch_bou
         }
         // With a table scores can be so large that the logarithm of their sum would be lost in what they are lowered by, and the table's gradient is 32 bits, of which the rounding of exponents
         // takes the fewer the nearer they are to 0: so there they are lowered by the largest alone, and the sum is a factor of dp's and delta's.
-        const float base = !BIAS ? stats.most + stats.log() : stats.sum != 0.0f ? stats.most : INFINITY;
-        const float factor = BIAS && stats.sum != 0.0f ? 1.0f / stats.sum : 0.0f, lowered = factor * delta;
+        const float base = !BIAS ? stats.most + stats.second : stats.second != 0.0f ? stats.most : INFINITY;
+        const float factor = BIAS && stats.second != 0.0f ? 1.0f / stats.second : 0.0f, lowered = factor * delta;
         const int position = BIAS ? query_position(A, there ? query : A.queries - 1) : 0;
         place_range mine;
         if constexpr (BIAS) mine = both(A.query_places[query0 / TILE], A.query_places[query0 + TILE < A.queries ? query0 / TILE + 1 : query0 / TILE]);
@@ -422,7 +423,7 @@ template <int DEEP, bool DIRECT, bool BIAS> __global__ __launch_bounds__(BLOCK, 
                 }
                 if (wave == 0) {
                     const bool in = first + lane < A.queries;
-                    stats = in ? stats_of(G, row0 + first + lane) : query_stats{0.0f, 0.0f};
+                    stats = in ? stats_of(G, row0 + first + lane) : NO_KEYS<BIAS>;
                     nd = in ? G.delta[row0 + first + lane] : 0.0f;
                     if (BIAS) place = query_position(A, in ? first + lane : A.queries - 1);
                 }
@@ -434,8 +435,8 @@ template <int DEEP, bool DIRECT, bool BIAS> __global__ __launch_bounds__(BLOCK, 
                 lds_byte *const qt = lds + turn * 2 * tile::BYTES, *const gt = qt + tile::BYTES;
                 q.land(qt), g.land(gt);
                 if (wave == 0) {
-                    most[turn][lane] = BIAS ? stats.most : stats.most + stats.log();
-                    log[turn][lane] = stats.log();
+                    most[turn][lane] = BIAS ? stats.most : stats.most + stats.second;
+                    log[turn][lane] = log_of<BIAS>(stats);
                     delta[turn][lane] = nd;
                     if constexpr (BIAS) places[turn][lane] = place;
                 }
